@@ -56,6 +56,15 @@ extern "C" {
 /* out_dtype of dymoe_moe_ffn_mixed */
 #define DYMOE_OUT_BF16 0
 #define DYMOE_OUT_F32 1
+#define DYMOE_OUT_F16 2        /* the 8-bit integer operators and dymoe_route_scored, as a type of inputs and of outputs */
+#define DYMOE_DTYPE_I8 3       /* x_dtype of dymoe_matmul_int8: codes that dymoe_quantize_rows wrote */
+
+/* score of dymoe_route_scored */
+#define DYMOE_SCORE_SOFTMAX 0
+#define DYMOE_SCORE_SIGMOID 1
+
+/* columns of a row that the 8-bit integer operators take: 127 * 127 * 131072 < 2^31 */
+#define DYMOE_INT8_MAX_K 131072
 
 /* path of dymoe_moe_ffn_mixed */
 #define DYMOE_PATH_AUTO 0
@@ -496,6 +505,80 @@ int dymoe_moe_ffn_mixed_noalloc(dymoe_ctx* ctx, const void* x, const int32_t* id
                                 void* y, void* stream);
 
 /*
+ * Router gating by scores (a router whose experts are balanced by a bias and chosen inside groups), from its logits:
+ *   s[t,e] = 1 / (1 + exp(-logit)) (DYMOE_SCORE_SIGMOID) or the softmax over all E experts (DYMOE_SCORE_SOFTMAX)
+ *   c[t,e] = s[t,e] + bias[e], 64 bits; without a bias experts compare by their logits (the same order)
+ *   groups of E / groups consecutive experts; a group's value is its largest c, or with group_best = 2 the sum of its
+ *     two largest; the top_groups groups of largest value stay (ties to the lower group)
+ *   idx[t,0..k) = the k experts of those groups with the largest c, descending, ties to the lower index
+ *   w[t,j] = s[t, idx[t,j]], divided by their sum when renorm != 0, times factor.
+ * A logit of minus infinity or of its type's lowest finite value is a mask: the expert ranks behind all others, adds nothing to its
+ * group's value beside one that is not masked, and has score and weight 0; it is chosen only where nothing else is left (a token
+ * whose experts are all masked gets the first k of the first groups, with weights 0).  A token with a NaN among its logits, or
+ * with plus infinity under softmax, has NaN weights and scores; its indices are those of k different experts all the same.
+ * logits [T,E] bf16, fp16 or fp32 (dtype: DYMOE_OUT_*), bias [E] fp32 or NULL, idx [T,k] int32, w [T,k] fp32, scores [T,E]
+ * fp32 or NULL (what dymoe_expert_importance takes as probs).  Limits: 1 <= k <= top_groups * (E / groups), groups divides
+ * E, factor > 0; E <= DYMOE_MAX_EXPERTS, k <= 64, groups <= 64 (else DYMOE_ENOTSUP).
+ */
+int dymoe_route_scored(dymoe_ctx* ctx, const void* logits, int dtype, const float* bias, int T, int E, int k, int score,
+                       int groups, int top_groups, int group_best, int renorm, float factor, int32_t* idx, float* w,
+                       float* scores, void* stream);
+
+/*
+ * Dynamic 8-bit quantisation of rows: of tokens, or of a weight matrix's channels.
+ *   a = max_k |x[r,k]|;  scale[r] = a / 127 (fp32);  code = rint(127 x / a), ties to even; a = 0: all codes 0
+ * The codes are those of the real quotient for bf16 and fp16 (for fp32 of one that is right to its last bit).  The value a
+ * code stands for is scale * code.  A row that holds an infinity or a NaN gets scale NaN and codes 0: what is made
+ * from it is NaN, and no other row is touched.
+ * x [rows,K] bf16, fp16 or fp32 (x_dtype: DYMOE_OUT_*), rows ldx values apart (any alignment of the type's own).
+ * scale [rows].  codes, 16-byte aligned:
+ *  DYMOE_LAYOUT_ROWMAJOR  [rows, Kp], Kp = K rounded up to a multiple of 128, zeros behind column K;
+ *  DYMOE_LAYOUT_TILE      the 8-bit tile layout of dymoe_expert_fmt over [rows rounded up to a multiple of 32, Kp], zeros
+ *                         behind both ends: what the weights of the two calls below are held in.
+ * Limits: K <= DYMOE_INT8_MAX_K (else DYMOE_ENOTSUP).
+ */
+int dymoe_quantize_rows(dymoe_ctx* ctx, const void* x, int x_dtype, long rows, long K, long ldx, int layout, int8_t* codes,
+                        float* scale, void* stream);
+
+/*
+ * Matrix product in 8-bit integers with a scale for each token and each channel:
+ *   y[t,n] = x_scale[t] * w_scale[n] * sum_k xq[t,k] wq[n,k]  (+ bias[n])
+ * The sum is exact (int32); the product with the scales and the bias is taken in fp32 and rounded once to the output's type.
+ * x: bf16, fp16 or fp32 [T,K], rows ldx values apart: quantised in the call as by dymoe_quantize_rows (workspace, x_scale
+ * ignored); or DYMOE_DTYPE_I8: codes [T,Kp] and x_scale [T] that dymoe_quantize_rows wrote, ldx = Kp (no workspace).
+ * w, w_scale: wq [N,K] as dymoe_quantize_rows writes it in DYMOE_LAYOUT_TILE, scale [N].  bias [N] fp32 or NULL.
+ * y [T,N] in out_dtype (DYMOE_OUT_*), rows ldy >= N values apart; what lies between them is left as it was.
+ * workspace: dymoe_matmul_int8_workspace_bytes(T, N, K) bytes (0 for invalid sizes), 256-byte aligned, scratch.
+ * Limits: K <= DYMOE_INT8_MAX_K; T, N <= 2^24.  The same inputs give the same bits, whatever rows they stand among.
+ */
+size_t dymoe_matmul_int8_workspace_bytes(int T, int N, int K);
+int dymoe_matmul_int8(dymoe_ctx* ctx, const void* x, int x_dtype, const float* x_scale, long ldx, const int8_t* w,
+                      const float* w_scale, const float* bias, int T, int N, int K, int out_dtype, void* y, long ldy,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* One expert in 8-bit integers: W1, W3 [F,H] and W2 [H,F] as dymoe_quantize_rows writes them in DYMOE_LAYOUT_TILE. */
+typedef struct {
+    const int8_t* q[3];
+    const float* s[3];
+} dymoe_expert_i8;
+
+/*
+ * SwiGLU experts in 8-bit integer arithmetic, activations quantised on the way:
+ *   y[t,:] = sum_{slot<k} w[t,slot] * W2_e q( silu(W1_e q(x_t)) * (W3_e q(x_t)) ),  e = idx[t,slot],
+ * q() the quantiser of dymoe_quantize_rows applied to a whole row, the products those of dymoe_matmul_int8.  Sums of products
+ * are exact; the SwiGLU intermediate is held in fp32 in calls of few pairs and in bf16 in others, the sum over the slots in fp32.
+ * x [T,H] bf16, fp16 or fp32; idx [T,k] int32; w [T,k] fp32; table [E] of dymoe_expert_i8 in device memory; y [T,H] in
+ * out_dtype (every row is written).  A pair whose index lies outside [0,E) contributes nothing, nor does one whose
+ * expert's entry holds a NULL (DYMOE_FLAG_FORMAT_MISSING, dymoe_device_flags).
+ * workspace: dymoe_moe_ffn_int8_workspace_bytes(T,H,F,E,k) bytes (0 for invalid sizes), 256-byte aligned, scratch.
+ * Limits: any H, F up to DYMOE_INT8_MAX_K, E <= DYMOE_MAX_EXPERTS.  No atomics in sums: the same inputs give the same bits.
+ */
+size_t dymoe_moe_ffn_int8_workspace_bytes(int T, int H, int F, int E, int k);
+int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, const int32_t* idx, const float* w,
+                       const dymoe_expert_i8* table, int T, int H, int F, int E, int k, int out_dtype, void* y,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Host-resident experts (Sec. 4.4.1, Phase-Adaptive Prefetcher): the weights a
  * later layer is predicted to need are copied from pinned host memory into
  * device buffers on a side stream while the compute stream works on the current
@@ -633,10 +716,11 @@ size_t dymoe_cache_bytes_resident(const dymoe_cache* cache);
  * Per-kernel timing (diagnostic; the paper reports only end-to-end latency,
  * Sec. 6.1 "Key Metrics", so these serve the roofline accounting).
  * dymoe_timing_enable: launches of the kernels whose bit is set in kernel_mask
- * (bit i = kernel id i, ids 0..21 in the order route, token_norm, importance,
+ * (bit i = kernel id i, ids 0..28 in the order route, token_norm, importance,
  * assign, quantize, gemv_phase1, gemv_phase2, gemv_combine, plan, gemm1, gemm2,
  * gemm_combine, stream_copy, decode_front, attn_stats, attn_colsum, gptq_group,
- * gptq_trail, gptq_hessian, gptq_factor, mfma_peak, route_select; gemv_combine is reserved: the decode path's
+ * gptq_trail, gptq_hessian, gptq_factor, mfma_peak, route_select, route_scored, quantize_rows, matmul_int8, int8_plan, int8_up, int8_down,
+ * int8_combine; gemv_combine is reserved: the decode path's
  * second phase writes y itself and no launch carries that id; route_select is the second of the two launches
  * dymoe_route_topk makes when it cuts the logits by experts as well as by tokens, route then names the first) carry a start and a stop HIP event on the dispatch itself, so
  * the interval is the kernel's execution time on the launch stream; 0 switches

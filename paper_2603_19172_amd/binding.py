@@ -25,7 +25,9 @@ OK, EINVAL, ENOSPC, EHIP, ENOTSUP, ENOCTX = 0, -1, -2, -3, -4, -5
 PHASE_PREFILL, PHASE_DECODE = 0, 1
 FRONT_MAX_TOKENS = 16
 FLAG_FORMAT_MISSING = 1
-OUT_BF16, OUT_F32 = 0, 1
+OUT_BF16, OUT_F32, OUT_F16, DTYPE_I8 = 0, 1, 2, 3
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+INT8_MAX_K = 131072
 PATH_AUTO, PATH_GEMV, PATH_GEMM = 0, 1, 2
 LAYOUT_ROWMAJOR, LAYOUT_TILE = 0, 1
 
@@ -45,11 +47,14 @@ EXPORTS = [
     "dymoe_cache_set_cyclic", "dymoe_cache_lookup",
     "dymoe_cache_block_bytes", "dymoe_cache_bytes_resident",
     "dymoe_timing_enable", "dymoe_timing_read", "dymoe_kernel_name",
+    "dymoe_route_scored", "dymoe_quantize_rows", "dymoe_matmul_int8_workspace_bytes", "dymoe_matmul_int8",
+    "dymoe_moe_ffn_int8_workspace_bytes", "dymoe_moe_ffn_int8",
 ]
 
 KERNELS = ["route", "token_norm", "importance", "assign", "quantize", "gemv_phase1",
            "gemv_phase2", "gemv_combine", "plan", "gemm1", "gemm2", "gemm_combine", "stream_copy", "decode_front",
-           "attn_stats", "attn_colsum", "gptq_group", "gptq_trail", "gptq_hessian", "gptq_factor", "mfma_peak", "route_select"]
+           "attn_stats", "attn_colsum", "gptq_group", "gptq_trail", "gptq_hessian", "gptq_factor", "mfma_peak", "route_select",
+           "route_scored", "quantize_rows", "matmul_int8", "int8_plan", "int8_up", "int8_down", "int8_combine"]
 
 
 class ExpertFmt(C.Structure):
@@ -58,6 +63,11 @@ class ExpertFmt(C.Structure):
                 ("z4", C.c_void_p * 3), ("q2", C.c_void_p * 3), ("s2", C.c_void_p * 3),
                 ("z2", C.c_void_p * 3), ("q8", C.c_void_p * 3), ("s8", C.c_void_p * 3),
                 ("z8", C.c_void_p * 3)]
+
+
+class ExpertI8(C.Structure):
+    """Mirror of dymoe_expert_i8."""
+    _fields_ = [("q", C.c_void_p * 3), ("s", C.c_void_p * 3)]
 
 
 CACHE_MAX_FORMATS, CACHE_MAX_EVICT = 4, 16
@@ -168,6 +178,19 @@ STATIC_SCRATCH_BYTES = 8 << 20
 lib.dymoe_moe_ffn_mixed_noalloc.restype = _i
 lib.dymoe_moe_ffn_mixed_noalloc.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _i, _i, _vp, _vp]
 
+lib.dymoe_route_scored.restype = _i
+lib.dymoe_route_scored.argtypes = [_vp, _vp, _i, _vp] + [_i] * 8 + [C.c_float, _vp, _vp, _vp, _vp]
+lib.dymoe_quantize_rows.restype = _i
+lib.dymoe_quantize_rows.argtypes = [_vp, _vp, _i, _l, _l, _l, _i, _vp, _vp, _vp]
+lib.dymoe_matmul_int8_workspace_bytes.restype = _sz
+lib.dymoe_matmul_int8_workspace_bytes.argtypes = [_i] * 3
+lib.dymoe_matmul_int8.restype = _i
+lib.dymoe_matmul_int8.argtypes = [_vp, _vp, _i, _vp, _l, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _l, _vp, _sz, _vp]
+lib.dymoe_moe_ffn_int8_workspace_bytes.restype = _sz
+lib.dymoe_moe_ffn_int8_workspace_bytes.argtypes = [_i] * 5
+lib.dymoe_moe_ffn_int8.restype = _i
+lib.dymoe_moe_ffn_int8.argtypes = [_vp, _vp, _i, _vp, _vp, _vp] + [_i] * 6 + [_vp, _vp, _sz, _vp]
+
 
 lib.dymoe_timing_enable.restype = _i
 lib.dymoe_timing_enable.argtypes = [_vp, C.c_uint]
@@ -205,6 +228,46 @@ def _ptr(t, dtype=None):
     return t.data_ptr()
 
 
+_OUT_OF = {torch.bfloat16: OUT_BF16, torch.float32: OUT_F32, torch.float16: OUT_F16}
+_TORCH_OUT = {v: t for t, v in _OUT_OF.items()}
+
+
+def _out_dtype(dtype):
+    if dtype not in _OUT_OF:
+        raise TypeError("expected bfloat16, float32 or float16, got %s" % dtype)
+    return _OUT_OF[dtype]
+
+
+def _shape(name, t, shape):
+    if t is not None and t.shape != shape:
+        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
+
+
+def _here(device, *tensors):
+    """The launch goes to the current device with the tensors' addresses: both have to be the context's."""
+    for t in tensors:
+        if t is not None and (t.device.type != "cuda" or t.device.index != device):
+            raise ValueError("tensor on %s, the context is of device %d" % (t.device, device))
+    if torch.cuda.current_device() != device:
+        raise ValueError("the context is of device %d, device %d is current" % (device, torch.cuda.current_device()))
+
+
+def _up(n, m):
+    return (n + m - 1) // m * m
+
+
+def _pitch(t):
+    """Values from one row of a matrix to the next."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _rows_ptr(t):
+    """Device pointer of a matrix whose rows may lie apart."""
+    if t.dim() != 2 or t.shape[1] > 1 and t.stride(1) != 1 or _pitch(t) < t.shape[1]:
+        raise ValueError("expected a matrix with contiguous columns and rows that do not overlap")
+    return t.data_ptr()
+
+
 def _stream(stream):
     if stream is None:
         stream = torch.cuda.current_stream()
@@ -213,6 +276,14 @@ def _stream(stream):
 
 def workspace_bytes(T, H, F, E, k) -> int:
     return int(lib.dymoe_workspace_bytes(T, H, F, E, k))
+
+
+def matmul_int8_workspace_bytes(T, N, K) -> int:
+    return int(lib.dymoe_matmul_int8_workspace_bytes(T, N, K))
+
+
+def moe_ffn_int8_workspace_bytes(T, H, F, E, k) -> int:
+    return int(lib.dymoe_moe_ffn_int8_workspace_bytes(T, H, F, E, k))
 
 
 def format_present(entry, bits) -> bool:
@@ -485,6 +556,80 @@ class Context:
                                    C.byref(fl), _stream(stream)), "dymoe_mfma_peak")
         return fl.value
 
+    # -- routing by scores and the products in 8-bit integers
+    def route_scored(self, logits, k, bias=None, score=SCORE_SIGMOID, groups=1, top_groups=1, group_best=1, renorm=True,
+                     factor=1.0, idx=None, w=None, scores=None, stream=None):
+        """logits [T, E] bf16 / fp16 / fp32 -> idx [T, k] int32, w [T, k] fp32; scores: a [T, E] fp32 tensor to fill."""
+        (T, E), dtype = logits.shape, _out_dtype(logits.dtype)
+        if idx is None:
+            idx = torch.empty((T, k), dtype=torch.int32, device=logits.device)
+        if w is None:
+            w = torch.empty((T, k), dtype=torch.float32, device=logits.device)
+        _shape("bias", bias, (E,))
+        _shape("idx", idx, (T, k))
+        _shape("w", w, (T, k))
+        _shape("scores", scores, (T, E))
+        _here(self.device, logits, bias, idx, w, scores)
+        _check(lib.dymoe_route_scored(self._h, _ptr(logits), dtype, _ptr(bias, torch.float32), T, E, k, score,
+                                      groups, top_groups, group_best, 1 if renorm else 0, float(factor), _ptr(idx, torch.int32),
+                                      _ptr(w, torch.float32), _ptr(scores, torch.float32), _stream(stream)), "dymoe_route_scored")
+        return idx, w
+
+    def quantize_rows(self, x, layout=LAYOUT_ROWMAJOR, out=None, stream=None):
+        """x [rows, K] bf16 / fp16 / fp32, columns contiguous -> (int8 codes, fp32 scale [rows])."""
+        rows, K = x.shape
+        shape = (_up(rows, 32) if layout == LAYOUT_TILE else rows, _up(K, 128))
+        if out is None:
+            out = (torch.empty(shape, dtype=torch.int8, device=x.device), torch.empty((rows,), dtype=torch.float32, device=x.device))
+        codes, scale = out
+        _shape("codes", codes, shape)
+        _shape("scale", scale, (rows,))
+        _here(self.device, x, codes, scale)
+        _check(lib.dymoe_quantize_rows(self._h, _rows_ptr(x), _out_dtype(x.dtype), rows, K, _pitch(x), layout,
+                                       _ptr(codes, torch.int8), _ptr(scale, torch.float32), _stream(stream)), "dymoe_quantize_rows")
+        return out
+
+    def matmul_int8(self, x, w, x_scale=None, bias=None, out_dtype=OUT_BF16, y=None, workspace=None, stream=None):
+        """x [T, K] bf16 / fp16 / fp32, or int8 codes [T, Kp] with x_scale [T]; w: (codes, scale [N]) in the tile layout.
+        Returns y [T, N], of the type of `y` where that is given."""
+        codes, scale = w
+        (T, K), N = x.shape, scale.shape[0]
+        coded = x.dtype == torch.int8
+        _shape("w", codes, (_up(N, 32), _up(K, 128)))
+        _shape("bias", bias, (N,))
+        if coded:
+            _shape("x", x, (T, _up(K, 128)))
+            _shape("x_scale", x_scale, (T,))
+        if y is None:
+            y = torch.empty((T, N), dtype=_TORCH_OUT[out_dtype], device=x.device)
+        _shape("y", y, (T, N))
+        if workspace is None and not coded:
+            workspace = torch.empty((matmul_int8_workspace_bytes(T, N, K),), dtype=torch.uint8, device=x.device)
+        _here(self.device, x, codes, scale, x_scale, bias, y, workspace)
+        _check(lib.dymoe_matmul_int8(self._h, _rows_ptr(x), DTYPE_I8 if coded else _out_dtype(x.dtype), _ptr(x_scale, torch.float32),
+                                     _pitch(x), _ptr(codes, torch.int8), _ptr(scale, torch.float32), _ptr(bias, torch.float32), T, N, K,
+                                     _out_dtype(y.dtype), _rows_ptr(y), _pitch(y), _ptr(workspace, torch.uint8),
+                                     0 if workspace is None else workspace.numel(), _stream(stream)), "dymoe_matmul_int8")
+        return y
+
+    def moe_ffn_int8(self, x, idx, w, table, F, out_dtype=OUT_BF16, y=None, workspace=None, stream=None):
+        """x [T, H] bf16 / fp16 / fp32; idx, w [T, k]; table: make_int8_table's.  Returns y [T, H]."""
+        T, H = x.shape
+        k = idx.shape[1]
+        E = table.numel() * table.element_size() // C.sizeof(ExpertI8)
+        _shape("idx", idx, (T, k))
+        _shape("w", w, (T, k))
+        if y is None:
+            y = torch.empty((T, H), dtype=_TORCH_OUT[out_dtype], device=x.device)
+        _shape("y", y, (T, H))
+        if workspace is None:
+            workspace = torch.empty((moe_ffn_int8_workspace_bytes(T, H, F, E, k),), dtype=torch.uint8, device=x.device)
+        _here(self.device, x, idx, w, table, y, workspace)
+        _check(lib.dymoe_moe_ffn_int8(self._h, _ptr(x), _out_dtype(x.dtype), _ptr(idx, torch.int32), _ptr(w, torch.float32),
+                                      _ptr(table), T, H, F, E, k, _out_dtype(y.dtype), _ptr(y), _ptr(workspace, torch.uint8),
+                                      workspace.numel(), _stream(stream)), "dymoe_moe_ffn_int8")
+        return y
+
     # -- S5
     def moe_ffn_mixed(self, x, idx, w, bits, table, F, out_dtype=OUT_BF16, path=PATH_AUTO,
                       group=64, y=None, workspace=None, stream=None):
@@ -503,6 +648,17 @@ class Context:
                                        _ptr(workspace, torch.uint8), workspace.numel(),
                                        _stream(stream)), "dymoe_moe_ffn_mixed")
         return y
+
+
+def make_int8_table(experts, device):
+    """The device-resident dymoe_expert_i8[E] of experts that are three (codes, scale) pairs each, in the tile layout
+    (Context.quantize_rows); an expert given as None has an empty entry.  The caller keeps the pairs alive."""
+    arr = (ExpertI8 * len(experts))()
+    for e, pairs in enumerate(experts):
+        for i, (codes, scale) in enumerate(pairs or ()):
+            arr[e].q[i] = _ptr(codes, torch.int8)
+            arr[e].s[i] = _ptr(scale, torch.float32)
+    return torch.frombuffer(bytearray(bytes(arr)), dtype=torch.uint8).to(device)
 
 
 def make_expert_table(experts, device):

@@ -220,6 +220,13 @@ const char* dymoe_kernel_name(int kernel)
     case DYMOE_K_GPTQ_FACTOR: return "gptq_step_kernel";
     case DYMOE_K_MFMA_PEAK: return "mfma_peak_kernel";
     case DYMOE_K_ROUTE_SELECT: return "route_select_kernel";
+    case DYMOE_K_ROUTE_SCORED: return "route_scored_kernel";
+    case DYMOE_K_QUANTIZE_ROWS: return "quantize_rows_kernel";
+    case DYMOE_K_MATMUL_INT8: return "i8_small_kernel<0>";
+    case DYMOE_K_INT8_PLAN: return "i8_plan_kernel";
+    case DYMOE_K_INT8_UP: return "i8_small_kernel<1>";
+    case DYMOE_K_INT8_DOWN: return "i8_small_kernel<2>";
+    case DYMOE_K_INT8_COMBINE: return "i8_combine_kernel";
     default: return nullptr;
     }
 }

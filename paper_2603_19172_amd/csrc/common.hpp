@@ -33,6 +33,13 @@ enum {
     DYMOE_K_GPTQ_FACTOR,
     DYMOE_K_MFMA_PEAK,
     DYMOE_K_ROUTE_SELECT,
+    DYMOE_K_ROUTE_SCORED,
+    DYMOE_K_QUANTIZE_ROWS,
+    DYMOE_K_MATMUL_INT8,
+    DYMOE_K_INT8_PLAN,
+    DYMOE_K_INT8_UP,
+    DYMOE_K_INT8_DOWN,
+    DYMOE_K_INT8_COMBINE,
     DYMOE_K_COUNT
 };
 

@@ -1,0 +1,249 @@
+// Routing by scores: sigmoid or softmax of the router's logits, a bias that decides who is chosen but not with which weight, a
+// selection among the best groups of experts, top-k, weights divided by their sum and scaled.
+//
+// One wavefront per token, lane l holding experts l, l + 64, ...; nothing is shared between tokens.  Scores are numbers of 64 bits: with
+// a bias the order of two experts depends on how s + b is rounded, and of 8192 tokens with 256 experts a few have neighbours nearer
+// than 32 bits tell apart.  A round of the top-k looks for the largest key, the compared value rounded to 32 bits in an order-preserving
+// pattern (six instructions through the vector unit); only where two experts share that pattern are the 64 bits looked at.
+#include <float.h>
+
+#include "int8_device.hpp"
+
+namespace dymoe {
+
+// 1 / d, d in [1, inf): the instruction's estimate and two Newton steps (infinity's inverse would make NaN in them)
+__device__ __forceinline__ double inverse(double d)
+{
+    d = fmin(d, 1e300);
+    double r = __builtin_amdgcn_rcp(d);
+    r = fma(fma(-d, r, 1.0), r, r);
+    return fma(fma(-d, r, 1.0), r, r);
+}
+
+__device__ __forceinline__ double lane_double(double v, int lane)       // lane the same for the whole wavefront
+{
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, lane);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), lane);
+    return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+}
+
+__device__ __forceinline__ double wave_sum_f64(double v)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+    return v;
+}
+
+__device__ __forceinline__ uint32_t order_key(float f)
+{
+    const uint32_t u = __float_as_uint(f);
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+
+// NPL: experts a lane holds.  DT: type of the logits.
+template <int NPL, int DT>
+__global__ __launch_bounds__(256) void route_scored_kernel(const char* __restrict__ logits, const float* __restrict__ bias, int T, int E,
+                                                           int k, int sigmoid, int groups, int top_groups, int best, int renorm,
+                                                           float factor, int32_t* __restrict__ idx, float* __restrict__ w,
+                                                           float* __restrict__ scores)
+{
+    extern __shared__ double s_value[];                       // a wavefront's compared values, where there are groups
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const long t = (long)blockIdx.x * 4 + wave;
+    if (t >= T) return;                                       // (no barriers below)
+    const double kLow = -__builtin_inf();
+    const float lowest = DT == DYMOE_OUT_F32 ? -FLT_MAX : DT == DYMOE_OUT_F16 ? -65504.0f : -0x1.fep127f;
+
+    float l[NPL];
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < NPL; i++) {
+        const int e = lane + 64 * i;
+        l[i] = -__builtin_inff();
+        if (e < E) {
+            const long at = t * E + e;
+            if constexpr (DT == DYMOE_OUT_F32) l[i] = ((const DYMOE_GLOBAL float*)logits)[at];
+            else if constexpr (DT == DYMOE_OUT_F16) l[i] = (float)((const DYMOE_GLOBAL _Float16*)logits)[at];
+            else l[i] = bf16_bits_to_f32(((const DYMOE_GLOBAL uint16_t*)logits)[at]);
+            l[i] += 0.0f;                                     // (-0 is 0: the two are one number and tie)
+            bad |= l[i] != l[i];
+            if (!(l[i] > lowest)) l[i] = -__builtin_inff();   // masked; NaN ranks with the masked ones
+        }
+    }
+    // scores
+    double s[NPL], c[NPL];
+    if (sigmoid) {
+#pragma unroll
+        for (int i = 0; i < NPL; i++) s[i] = l[i] == -__builtin_inff() ? 0.0 : inverse(1.0 + exp(-(double)l[i]));
+    } else {
+        uint32_t mk = 0;
+#pragma unroll
+        for (int i = 0; i < NPL; i++) mk = max(mk, order_key(l[i]));
+        mk = wave_max_u32(mk);
+        const float m = __uint_as_float(mk & 0x80000000u ? mk ^ 0x80000000u : ~mk);
+        bad |= m == __builtin_inff();
+        double sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < NPL; i++) {
+            s[i] = l[i] == -__builtin_inff() ? 0.0 : exp((double)l[i] - (double)m);
+            sum += s[i];
+        }
+        sum = wave_sum_f64(sum);
+        const double inv = sum > 0.0 ? inverse(sum) : 0.0;
+#pragma unroll
+        for (int i = 0; i < NPL; i++) s[i] *= inv;
+    }
+    bad = __ballot(bad) != 0;
+    // what is compared: the score with its bias, or, in the same order, the logit
+#pragma unroll
+    for (int i = 0; i < NPL; i++) {
+        const int e = lane + 64 * i;
+        c[i] = l[i] == -__builtin_inff() ? kLow : bias ? s[i] + (double)bias[min(e, E - 1)] : groups > 1 && best == 2 ? s[i] : (double)l[i];
+        if (c[i] != c[i]) c[i] = kLow;
+    }
+    uint32_t key[NPL];
+    uint64_t kept = ~0ull;
+    const int per = E / groups;
+    if (groups > 1) {
+        double* const v = s_value + wave * (NPL * 64);
+#pragma unroll
+        for (int i = 0; i < NPL; i++) v[lane + 64 * i] = c[i];
+        __builtin_amdgcn_wave_barrier();
+        // lanes to a group: a power of two, so that a group's lanes meet in a butterfly
+        int lg = 1;
+        while (2 * lg * groups <= 64) lg *= 2;
+        const int g = lane / lg, part = lane & (lg - 1);
+        double v1 = kLow, v2 = kLow;
+        if (g < groups)
+            for (int j = part; j < per; j += lg) {
+                const double d = v[g * per + j];
+                v2 = fmax(v2, fmin(v1, d));
+                v1 = fmax(v1, d);
+            }
+        for (int o = 1; o < lg; o *= 2) {
+            const double a = __shfl_xor(v1, o, kWave), b = __shfl_xor(v2, o, kWave);
+            v2 = fmax(fmax(v2, b), fmin(v1, a));
+            v1 = fmax(v1, a);
+        }
+        const double value = best == 2 && v2 > kLow ? v1 + v2 : v1;
+        int rank = 0;
+        for (int h = 0; h < groups; h++) {
+            const double o = lane_double(value, h * lg);
+            rank += (o > value) || (o == value && h < g);
+        }
+        const uint64_t in = __ballot(g < groups && part == 0 && rank < top_groups);
+        kept = 0;
+        for (int h = 0; h < groups; h++) kept |= ((in >> (h * lg)) & 1ull) << h;
+        // (the order inside the groups is the logits' where no bias moves it)
+        if (!bias && best == 2) {
+#pragma unroll
+            for (int i = 0; i < NPL; i++) c[i] = (double)l[i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < NPL; i++) {
+        const int e = lane + 64 * i;
+        const bool in = e < E && (groups == 1 || ((kept >> (e / per)) & 1ull));
+        key[i] = in ? order_key((float)c[i]) : 0u;            // 0: cannot be chosen
+    }
+    if (scores) {
+#pragma unroll
+        for (int i = 0; i < NPL; i++) {
+            const int e = lane + 64 * i;
+            if (e < E) scores[t * E + e] = bad ? __builtin_nanf("") : (float)s[i];
+        }
+    }
+    int mine = 0;
+    double weight = 0.0;
+    for (int j = 0; j < k; j++) {
+        uint32_t best_key = key[0];
+#pragma unroll
+        for (int i = 1; i < NPL; i++) best_key = max(best_key, key[i]);
+        best_key = wave_max_u32(best_key);
+        int n = 0;
+        uint32_t first = 0xffffffffu;
+#pragma unroll
+        for (int i = NPL - 1; i >= 0; i--) {
+            const uint64_t at = __ballot(key[i] == best_key);
+            n += __popcll(at);
+            if (at) first = 64 * i + (uint32_t)__builtin_ctzll(at);
+        }
+        if (n > 1 && bias) {                                  // (without a bias the keys are the logits themselves)
+            double top = kLow;
+#pragma unroll
+            for (int i = 0; i < NPL; i++) top = fmax(top, key[i] == best_key ? c[i] : kLow);
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) top = fmax(top, __shfl_xor(top, o, kWave));
+#pragma unroll
+            for (int i = NPL - 1; i >= 0; i--) {
+                const uint64_t at = __ballot(key[i] == best_key && c[i] == top);
+                if (at) first = 64 * i + (uint32_t)__builtin_ctzll(at);
+            }
+        }
+        const int owner = __builtin_amdgcn_readfirstlane((int)(first & 63u)), which = __builtin_amdgcn_readfirstlane((int)(first >> 6));
+        double sw = 0.0;
+#pragma unroll
+        for (int i = 0; i < NPL; i++)
+            if (which == i) {
+                sw = lane_double(s[i], owner);
+                if (lane == owner) key[i] = 0u;
+            }
+        if (lane == j) {
+            mine = (int)first;
+            weight = sw;
+        }
+    }
+    if (renorm) {
+        const double sum = wave_sum_f64(weight);
+        weight = sum > 0.0 ? weight / sum : 0.0;
+    }
+    if (lane < k) {
+        idx[t * k + lane] = mine;
+        w[t * k + lane] = bad ? __builtin_nanf("") : (float)(weight * (double)factor);
+    }
+}
+
+template <int DT>
+static void route_scored_launch(dymoe_ctx* ctx, const void* logits, const float* bias, int T, int E, int k, int sigmoid, int groups,
+                                int top_groups, int best, int renorm, float factor, int32_t* idx, float* w, float* scores, hipStream_t st)
+{
+    const dim3 grid((unsigned)((T + 3L) / 4));
+#define DYMOE_RSCORED(NPL)                                                                                                        \
+    dymoe_launch(ctx, DYMOE_K_ROUTE_SCORED, route_scored_kernel<NPL, DT>, grid, dim3(256), groups > 1 ? 4 * NPL * 64 * 8 : 0, st, \
+                 (const char*)logits, bias, T, E, k, sigmoid, groups, top_groups, best, renorm, factor, idx, w, scores)
+    if (E <= 64) DYMOE_RSCORED(1);
+    else if (E <= 128) DYMOE_RSCORED(2);
+    else if (E <= 256) DYMOE_RSCORED(4);
+    else if (E <= 512) DYMOE_RSCORED(8);
+    else DYMOE_RSCORED(16);
+#undef DYMOE_RSCORED
+}
+
+}  // namespace dymoe
+
+extern "C" int dymoe_route_scored(dymoe_ctx* ctx, const void* logits, int dtype, const float* bias, int T, int E, int k, int score,
+                                  int groups, int top_groups, int group_best, int renorm, float factor, int32_t* idx, float* w,
+                                  float* scores, void* stream)
+{
+    DYMOE_REQUIRE(T >= 0 && E > 0 && k > 0 && k <= E);
+    DYMOE_REQUIRE(dtype == DYMOE_OUT_BF16 || dtype == DYMOE_OUT_F32 || dtype == DYMOE_OUT_F16);
+    DYMOE_REQUIRE(score == DYMOE_SCORE_SIGMOID || score == DYMOE_SCORE_SOFTMAX);
+    DYMOE_REQUIRE(groups >= 1 && E % groups == 0 && top_groups >= 1 && top_groups <= groups);
+    DYMOE_REQUIRE(group_best == 1 || group_best == 2);
+    DYMOE_REQUIRE((long)top_groups * (E / groups) >= k);
+    DYMOE_REQUIRE(factor > 0.0f && factor <= FLT_MAX);
+    if (T > 0) DYMOE_REQUIRE(logits && idx && w);
+    DYMOE_REQUIRE(dymoe_aligned(logits, dymoe::dtype_bytes(dtype)) && dymoe_aligned(idx, 4) && dymoe_aligned(w, 4));
+    DYMOE_REQUIRE(dymoe_aligned(bias, 4) && dymoe_aligned(scores, 4));
+    if (E > DYMOE_MAX_EXPERTS || k > 64 || groups > 64) return DYMOE_ENOTSUP;
+    if (!ctx) return DYMOE_ENOCTX;
+    if (T == 0) return DYMOE_OK;
+    auto launch = dymoe::route_scored_launch<DYMOE_OUT_BF16>;
+    if (dtype == DYMOE_OUT_F32) launch = dymoe::route_scored_launch<DYMOE_OUT_F32>;
+    else if (dtype == DYMOE_OUT_F16) launch = dymoe::route_scored_launch<DYMOE_OUT_F16>;
+    launch(ctx, logits, bias, T, E, k, score == DYMOE_SCORE_SIGMOID, groups, top_groups, group_best, renorm, factor, idx, w, scores,
+           (hipStream_t)stream);
+    DYMOE_HIP_LAUNCH_CHECK();
+    return DYMOE_OK;
+}
