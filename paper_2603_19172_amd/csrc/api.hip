@@ -51,6 +51,7 @@ int ffn_static_scratch_address(void** out);
 int ffn_device_flags_address(unsigned** out);
 int ffn_gemm_init();
 int route_init();
+int i8_init();
 
 }  // namespace dymoe
 
@@ -110,6 +111,7 @@ int dymoe_create(dymoe_ctx** out, int device)
         if (rc == DYMOE_OK) rc = dymoe::ffn_device_flags_address(&c->device_flags);
         if (rc == DYMOE_OK) rc = dymoe::ffn_gemm_init();
         if (rc == DYMOE_OK) rc = dymoe::route_init();
+        if (rc == DYMOE_OK) rc = dymoe::i8_init();
         if (hipSetDevice(prev) != hipSuccess) rc = DYMOE_EHIP;
     }
     if (rc != DYMOE_OK) {

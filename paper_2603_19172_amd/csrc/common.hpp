@@ -322,6 +322,33 @@ __device__ __forceinline__ float token_norm(const uint16_t* __restrict__ row, in
     return sqrtf(wave_sum(acc));
 }
 
+// 16 bytes of LDS at a byte address
+__device__ __forceinline__ uint4 lds_read16(uint32_t addr)
+{
+    const u32x4_t v = *(const __attribute__((address_space(3))) u32x4_t*)(uintptr_t)addr;
+    return __builtin_bit_cast(uint4, v);
+}
+
+__device__ __forceinline__ void lds_write16(uint32_t addr, const uint4 v)
+{
+    *(__attribute__((address_space(3))) u32x4_t*)(uintptr_t)addr = __builtin_bit_cast(u32x4_t, v);
+}
+
+__device__ __forceinline__ void lds_write8(uint32_t addr, const uint2 v)
+{
+    *(__attribute__((address_space(3))) u32x2_t*)(uintptr_t)addr = __builtin_bit_cast(u32x2_t, v);
+}
+
+__device__ __forceinline__ uint32_t lds_read4(uint32_t addr)
+{
+    return *(const __attribute__((address_space(3))) uint32_t*)(uintptr_t)addr;
+}
+
+__device__ __forceinline__ void lds_write4(uint32_t addr, uint32_t v)
+{
+    *(__attribute__((address_space(3))) uint32_t*)(uintptr_t)addr = v;
+}
+
 // 16 bytes a lane, global memory -> LDS[lds_addr_lane0 + 16 * lane] without passing through registers.
 // The instruction is issued from inline assembly so that the compiler does not
 // make every later LDS read wait for it; completion is awaited explicitly

@@ -214,35 +214,6 @@ __device__ __forceinline__ void load_strip(const StripSrc& src, int kt, StripRaw
     load_scale_zero<BITS>(src, kt, raw);
 }
 
-// 16 bytes of LDS at a byte address
-__device__ __forceinline__ uint4 lds_read16(uint32_t addr)
-{
-    const u32x4_t v = *(const __attribute__((address_space(3))) u32x4_t*)(uintptr_t)addr;
-    return __builtin_bit_cast(uint4, v);
-}
-
-__device__ __forceinline__ void lds_write16(uint32_t addr, const uint4 v)
-{
-    *(__attribute__((address_space(3))) u32x4_t*)(uintptr_t)addr = __builtin_bit_cast(u32x4_t, v);
-}
-
-typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ void lds_write8(uint32_t addr, const uint2 v)
-{
-    *(__attribute__((address_space(3))) u32x2_t*)(uintptr_t)addr = __builtin_bit_cast(u32x2_t, v);
-}
-
-__device__ __forceinline__ uint32_t lds_read4(uint32_t addr)
-{
-    return *(const __attribute__((address_space(3))) uint32_t*)(uintptr_t)addr;
-}
-
-__device__ __forceinline__ void lds_write4(uint32_t addr, uint32_t v)
-{
-    *(__attribute__((address_space(3))) uint32_t*)(uintptr_t)addr = v;
-}
-
 // second GEMM's epilogue: a wavefront's own LDS area, 32 rows of 256 bytes + 16 of padding
 constexpr uint32_t kEpiRowBytes = 272;
 constexpr uint32_t kEpiWaveBytes = 32 * kEpiRowBytes;

@@ -114,7 +114,7 @@ struct I8Args {
     const float* bias;
     void* out;
     long ldo, P;
-    int rows, Kp, N, E, k, out_dtype;
+    int rows, Kp, N, E, k, out_dtype, aligned;     // aligned: the plain product's rows start where four outputs may be stored at once
 };
 
 enum { kI8Plain = 0, kI8Up = 1, kI8Down = 2 };
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(256) void i8_small_kernel(const I8Args A)
 #pragma unroll
         for (int i = 0; i < 4; i++) {
             const int n = n0 + i;
-            if (n < A.N) store_out(A.out, (row0 + ln) * A.ldo + n, DYMOE_OUT_BF16, silu_times(v[0][i] * xs * sa[n], v[1][i] * xs * sb[n]));
+            if (n < A.N) store_out(A.out, (row0 + ln) * A.ldo + n, DYMOE_OUT_F32, silu_times(v[0][i] * xs * sa[n], v[1][i] * xs * sb[n]));
         }
         return;
     }
@@ -220,6 +220,315 @@ __global__ __launch_bounds__(256) void i8_small_kernel(const I8Args A)
             if (MODE == kI8Plain && A.bias) o += A.bias[n];
             store_out(A.out, (long)(row0 + ln) * A.ldo + n, MODE == kI8Plain ? A.out_dtype : DYMOE_OUT_F32, o);
         }
+}
+
+// ----------------------------------------------------------------------------
+// Tiles of up to 128 or 256 rows.  A workgroup of four wavefronts owns eight strips of 32 weight rows (two a wavefront) and walks K in steps
+// of 256 columns.
+//  * Weights come straight into registers: a tile's bytes lie in the order of the matrix instruction's operand, so a wavefront's load is 1 KiB
+//    of contiguous memory.  A register is requested anew, for the next step, as soon as the last instruction that reads it has been issued.
+//  * The rows' codes are shared by the wavefronts through two LDS buffers that global memory fills directly; 16-byte chunk c of row r lies at
+//    position c ^ (r & 15), which spreads the operand reads (one chunk of 32 rows) over all banks.
+//  * Up to 128 rows: 128 accumulator registers a lane, two workgroups on a compute unit, one's waits covered by the other's products.
+//    Up to 256 rows: 256 accumulator registers, one workgroup; for experts that meet so few tokens that the weights' bytes, not the
+//    products, bound the call: they are then read once.
+constexpr int kI8Step = 256;                    // columns of a step
+constexpr uint32_t kI8EpiRow = 272;             // epilogue: bytes of a row of 64 fp32 in LDS, 16 of them padding
+constexpr uint32_t kI8EpiWave = 32 * kI8EpiRow;
+
+struct I8Strip {
+    uint4 r[8];       // chunk j = 4 * (128-column tile of the step) + 16-byte chunk of the lane's half of that tile
+};
+
+// chunk j of step ks of the strip at p (this lane's first 16 bytes); tiles behind the last re-read it
+__device__ __forceinline__ uint4 i8_chunk(const char* p, uint32_t lane16, int tile, int c)
+{
+    return load_global<uint4>(p + (long)tile * 4096 + c * 1024 + lane16);
+}
+
+template <int NTF>
+struct I8Stage {
+    static constexpr int kCopies = 2 * NTF;     // 32 NTF rows of 256 bytes, 16 rows an instruction of the workgroup
+    const char* base;
+    uint32_t off[kCopies];
+    uint32_t lds;
+};
+
+struct I8Ops {
+    uint4 t0, t1;
+};
+
+// Chunks [J0, J1) of a step.  The operands of the next pair of chunks are read while the products of this one are issued.
+template <int NTF, int J1>
+__device__ __forceinline__ void i8_step(I8Strip& ra, I8Strip& rb, const char* sa, const char* sb, uint32_t lane16, int tile_next, int nkt,
+                                        uint32_t xa, i32x16_t (&acc)[2][NTF])
+{
+    constexpr int kStepMask = 0x2 | 0x4;        // vector and scalar arithmetic may cross; products, LDS and memory accesses may not
+    I8Ops ops;
+    ops.t0 = lds_read16(xa);
+    ops.t1 = lds_read16(xa ^ 16u);
+#pragma unroll
+    for (int jj = 0; jj < J1 / 2; jj++) {
+#pragma unroll
+        for (int tf = 0; tf < NTF; tf++) {
+            const bool wrap = tf == NTF - 1;
+            const bool last = wrap && jj == J1 / 2 - 1;
+            const int nj = wrap ? jj + 1 : jj, nf = wrap ? 0 : tf + 1;
+            I8Ops nxt = ops;
+            if (!last) {
+                // chunks 2 nj, 2 nj + 1 of the lane's columns: position 8 * tile + 4 * half + chunk, the half already in xa
+                const uint32_t at = (xa ^ (uint32_t)(((nj >> 1) << 7) | ((nj & 1) << 5))) + (uint32_t)nf * (32 * kI8Step);
+                nxt.t0 = lds_read16(at);
+                nxt.t1 = lds_read16(at ^ 16u);
+            }
+            __builtin_amdgcn_sched_barrier(kStepMask);
+            acc[0][tf] = mfma_i8(ra.r[2 * jj], ops.t0, acc[0][tf]);
+            acc[1][tf] = mfma_i8(rb.r[2 * jj], ops.t0, acc[1][tf]);
+            acc[0][tf] = mfma_i8(ra.r[2 * jj + 1], ops.t1, acc[0][tf]);
+            acc[1][tf] = mfma_i8(rb.r[2 * jj + 1], ops.t1, acc[1][tf]);
+            ops = nxt;
+            __builtin_amdgcn_sched_barrier(kStepMask);
+        }
+        const int tile = min(tile_next + (jj >> 1), nkt - 1), c = 2 * (jj & 1);
+        ra.r[2 * jj] = i8_chunk(sa, lane16, tile, c);
+        ra.r[2 * jj + 1] = i8_chunk(sa, lane16, tile, c + 1);
+        rb.r[2 * jj] = i8_chunk(sb, lane16, tile, c);
+        rb.r[2 * jj + 1] = i8_chunk(sb, lane16, tile, c + 1);
+        __builtin_amdgcn_sched_barrier(kStepMask);
+    }
+}
+
+// four neighbouring outputs of a row
+__device__ __forceinline__ void i8_store4(void* out, long at, int dt, bool whole, int left, const float (&v)[4])
+{
+    if (whole) {
+        if (dt == DYMOE_OUT_F32) {
+            store_global((float*)out + at, make_float4(v[0], v[1], v[2], v[3]));
+        } else if (dt == DYMOE_OUT_F16) {
+            store_global((uint16_t*)out + at, make_uint2(pack_half2(v[0], v[1]), pack_half2(v[2], v[3])));
+        } else {
+            typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+            const bf16x4_t b = {(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+            store_global((uint16_t*)out + at, __builtin_bit_cast(uint2, b));
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+        if (i < left) store_out(out, at + i, dt, v[i]);
+}
+
+template <int MODE, int NTF>
+__device__ __forceinline__ void i8_tile(const I8Args& A, const int32_t* perm, const char* qa, const char* qb, const float* sa, const float* sb,
+                                        int row0, int rows, int bx, uint32_t xs_base, uint32_t buf_bytes)
+{
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int ln = lane & 31, kb = lane >> 5;
+    const uint32_t lane16 = (uint32_t)lane * 16u;
+    i32x16_t acc[2][NTF] = {};
+    I8Stage<NTF> stage;
+    {
+        // wavefront w fills rows 16 i + 4 w .. + 3: lane l row l / 16 of them, the chunk that belongs at position l % 16
+        const int rb = 4 * wave + (lane >> 4);
+        const int chunk = (lane & 15) ^ (rb & 15);
+#pragma unroll
+        for (int i = 0; i < I8Stage<NTF>::kCopies; i++) {
+            const int r = min(16 * i + rb, rows - 1);         // rows behind the last: computed and dropped
+            const uint32_t src = MODE == kI8Up ? (uint32_t)(perm[row0 + r] / A.k) : (uint32_t)r;
+            stage.off[i] = src * (uint32_t)A.Kp + 16u * (uint32_t)chunk;      // below 4 GiB: checked by the launcher
+        }
+        stage.base = A.x + (MODE == kI8Up ? 0 : (long)row0 * A.Kp);
+        stage.lds = __builtin_amdgcn_readfirstlane(xs_base + (uint32_t)wave * 1024u);
+    }
+    const int nkt = A.Kp >> 7, steps = (nkt + 1) >> 1;
+    // (the last step's second half may lie behind the rows' end: its chunks are then those of the first half, and go unused)
+    const uint32_t back = (nkt & 1) && (((lane & 15) ^ ((4 * wave + (lane >> 4)) & 15)) & 8) ? 128u : 0u;
+    auto copy = [&](int ks, uint32_t at) {
+        const char* const base = stage.base + (long)ks * kI8Step;
+        const uint32_t less = ks == steps - 1 ? back : 0u;
+#pragma unroll
+        for (int i = 0; i < I8Stage<NTF>::kCopies; i++) lds_copy16(base, stage.off[i] - less, stage.lds + at + (uint32_t)i * 4096u);
+    };
+    const uint32_t xa0 = xs_base + (uint32_t)ln * kI8Step + (((uint32_t)kb << 6) ^ ((uint32_t)(ln & 15) << 4));
+    I8Strip ra, rb;
+    copy(0, 0);
+#pragma unroll
+    for (int j = 0; j < 8; j++) {
+        ra.r[j] = i8_chunk(qa, lane16, min(j >> 2, nkt - 1), j & 3);
+        rb.r[j] = i8_chunk(qb, lane16, min(j >> 2, nkt - 1), j & 3);
+    }
+    wait_lds_copies<0>();
+    __syncthreads();
+    uint32_t at = 0;
+    for (int ks = 0; ks < nkt >> 1; ks++) {
+        copy(min(ks + 1, steps - 1), at ^ buf_bytes);
+        i8_step<NTF, 8>(ra, rb, qa, qb, lane16, 2 * (ks + 1), nkt, xa0 + at, acc);
+        wait_lds_copies<16>();          // the copies are older than the sixteen loads of weights
+        __syncthreads();
+        at ^= buf_bytes;
+    }
+    if (nkt & 1) {
+        i8_step<NTF, 4>(ra, rb, qa, qb, lane16, nkt - 1, nkt, xa0 + at, acc);
+        __syncthreads();
+    }
+
+    // Epilogue.  A lane holds, of its token's row, four neighbouring outputs in each group of four registers; the wavefront turns a fragment
+    // round in an area of its own, so that a row leaves in whole lines.
+    const uint32_t area = xs_base + (uint32_t)wave * kI8EpiWave;
+    const uint32_t wr = area + (uint32_t)ln * kI8EpiRow + (uint32_t)kb * 16u;
+    const int chunk = MODE == kI8Up ? lane & 7 : lane & 15;
+    const int n = MODE == kI8Up ? (4 * bx + wave) * 32 + 4 * chunk : (4 * bx + wave) * 64 + 4 * chunk;
+    float sc[4], add[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        sc[i] = MODE != kI8Up ? sa[min(n + i, A.N - 1)] : 0.f;
+        if (MODE == kI8Plain && A.bias) add[i] = A.bias[min(n + i, A.N - 1)];
+    }
+    const int left = A.N - n;
+    const int dt = MODE == kI8Plain ? A.out_dtype : DYMOE_OUT_F32;
+    const bool whole = left >= 4 && (MODE != kI8Plain || A.aligned);
+#pragma unroll
+    for (int tf = 0; tf < NTF; tf++) {
+        if (MODE == kI8Up) {
+            const int r = min(32 * tf + ln, rows - 1);
+            const float xs = A.xs[perm[row0 + r] / A.k];
+#pragma unroll
+            for (int g = 0; g < 4; g++) {
+                float h[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const int f = min((4 * bx + wave) * 32 + 8 * g + 4 * kb + i, A.N - 1);
+                    h[i] = silu_times((float)acc[0][tf][4 * g + i] * xs * sa[f], (float)acc[1][tf][4 * g + i] * xs * sb[f]);
+                }
+                lds_write16(wr + 32u * g, make_uint4(__float_as_uint(h[0]), __float_as_uint(h[1]), __float_as_uint(h[2]), __float_as_uint(h[3])));
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < 2; s++)
+#pragma unroll
+                for (int g = 0; g < 4; g++)
+                    lds_write16(wr + (uint32_t)(s * 128 + g * 32), make_uint4((uint32_t)acc[s][tf][4 * g], (uint32_t)acc[s][tf][4 * g + 1],
+                                                                              (uint32_t)acc[s][tf][4 * g + 2], (uint32_t)acc[s][tf][4 * g + 3]));
+        }
+        // (a wavefront's LDS accesses execute in order and the area is its own: no barrier)
+        constexpr int kSub = MODE == kI8Up ? 8 : 4;       // rows an instruction reads
+        const int rsub = MODE == kI8Up ? lane >> 3 : lane >> 4;
+#pragma unroll
+        for (int j = 0; j < 32 / kSub; j++) {
+            const int rr = rsub + kSub * j, row = 32 * tf + rr;
+            const uint4 u = lds_read16(area + (uint32_t)rr * kI8EpiRow + (uint32_t)chunk * 16u);
+            if (row >= rows || left <= 0) continue;
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+            float v[4];
+            if (MODE == kI8Up) {
+#pragma unroll
+                for (int i = 0; i < 4; i++) v[i] = __uint_as_float(w[i]);
+            } else {
+                const float xs = A.xs[row0 + row];
+#pragma unroll
+                for (int i = 0; i < 4; i++) v[i] = (float)(int)w[i] * xs * sc[i] + add[i];
+            }
+            i8_store4(A.out, (long)(row0 + row) * A.ldo + n, dt, whole, left, v);
+        }
+    }
+}
+
+// MAXF: fragments of 32 rows a tile may have
+template <int MODE, int MAXF>
+__global__ __launch_bounds__(256, MAXF == 4 ? 2 : 1) void i8_gemm_kernel(const I8Args A)
+{
+    extern __shared__ __attribute__((aligned(1024))) char xs_raw[];
+    const uint32_t xs = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)xs_raw;
+    constexpr uint32_t kBuf = 32u * MAXF * kI8Step;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const I8Plan pp = i8_plan(const_cast<int32_t*>(A.plan), A.E, A.P);
+    const int cols = MODE == kI8Up ? 128 : 256;
+    const int nblk = (A.N + cols - 1) / cols;
+    const int tiles = MODE == kI8Plain ? (A.rows + 32 * MAXF - 1) / (32 * MAXF) : pp.meta[0];
+    // Workgroups go to the 8 XCDs, each with an L2 of its own, in turn: XCD c takes the c-th of eight runs of neighbouring units, a column
+    // block's (plain product) or an expert's (grouped) tiles next to each other.
+    const long total = (long)tiles * nblk;
+    const long per = (total + 7) / 8;
+    const long unit = (long)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if ((long)(blockIdx.x >> 3) >= per || unit >= total) return;
+    int tile, bx;
+    if (MODE == kI8Plain) {
+        bx = (int)(unit / tiles);
+        tile = (int)(unit - (long)bx * tiles);
+    } else {
+        tile = (int)(unit / nblk);
+        bx = (int)(unit - (long)tile * nblk);
+    }
+    int row0, rows;
+    const char *qa, *qb;
+    const float *sa, *sb;
+    const long strip = 32L * A.Kp, last = (A.N + 31) / 32 - 1;
+    const long na = MODE == kI8Up ? 4L * bx + wave : 8L * bx + 2 * wave;
+    const long oa = min(na, last) * strip, ob = min(MODE == kI8Up ? na : na + 1, last) * strip;      // strips behind the last re-read it
+    if (MODE == kI8Plain) {
+        row0 = tile * 32 * MAXF;
+        rows = min(32 * MAXF, A.rows - row0);
+        qa = A.w.q + oa;
+        qb = A.w.q + ob;
+        sa = sb = A.w.s;
+    } else {
+        const int e = pp.tiles[4 * tile];
+        row0 = pp.tiles[4 * tile + 1];
+        rows = pp.tiles[4 * tile + 2];
+        const dymoe_expert_i8 ex = A.table[e];
+        qa = (const char*)ex.q[MODE == kI8Up ? 0 : 2] + oa;
+        qb = (const char*)ex.q[MODE == kI8Up ? 1 : 2] + ob;
+        sa = ex.s[MODE == kI8Up ? 0 : 2];
+        sb = ex.s[MODE == kI8Up ? 1 : 2];
+    }
+#define DYMOE_I8_TILE(NTF) i8_tile<MODE, NTF>(A, pp.perm, qa, qb, sa, sb, row0, rows, bx, xs, kBuf)
+    const int ntf = (rows + 31) >> 5;
+    if constexpr (MAXF == 4) {
+        switch (ntf) {
+        case 1: DYMOE_I8_TILE(1); break;
+        case 2: DYMOE_I8_TILE(2); break;
+        case 3: DYMOE_I8_TILE(3); break;
+        default: DYMOE_I8_TILE(4); break;
+        }
+    } else {
+        switch (ntf) {
+        case 1: DYMOE_I8_TILE(1); break;
+        case 2: DYMOE_I8_TILE(2); break;
+        case 3: DYMOE_I8_TILE(3); break;
+        case 4: DYMOE_I8_TILE(4); break;
+        case 5: DYMOE_I8_TILE(5); break;
+        case 6: DYMOE_I8_TILE(6); break;
+        case 7: DYMOE_I8_TILE(7); break;
+        default: DYMOE_I8_TILE(8); break;
+        }
+    }
+#undef DYMOE_I8_TILE
+}
+
+template <int MODE, int MAXF>
+static int i8_allow_lds()
+{
+    return hipFuncSetAttribute((const void*)i8_gemm_kernel<MODE, MAXF>, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * 32 * MAXF * kI8Step) == hipSuccess
+               ? DYMOE_OK : DYMOE_EHIP;
+}
+
+// per-device set-up, with the device current
+int i8_init()
+{
+    const int rc[6] = {i8_allow_lds<kI8Plain, 4>(), i8_allow_lds<kI8Up, 4>(), i8_allow_lds<kI8Down, 4>(),
+                       i8_allow_lds<kI8Plain, 8>(), i8_allow_lds<kI8Up, 8>(), i8_allow_lds<kI8Down, 8>()};
+    for (int r : rc)
+        if (r != DYMOE_OK) return r;
+    return DYMOE_OK;
+}
+
+// units: (tiles, column blocks) pairs at most
+template <int MODE>
+static void i8_gemm_launch(dymoe_ctx* ctx, int id, int maxf, long units, hipStream_t st, const I8Args& A)
+{
+    const dim3 grid((unsigned)(8 * ((units + 7) / 8)));
+    if (maxf == 4) dymoe_launch(ctx, id, i8_gemm_kernel<MODE, 4>, grid, dim3(256), 2 * 32 * 4 * kI8Step, st, A);
+    else dymoe_launch(ctx, id, i8_gemm_kernel<MODE, 8>, grid, dim3(256), 2 * 32 * 8 * kI8Step, st, A);
 }
 
 // y[t] = sum over the slots, in their order, of gate times the pair's output
@@ -300,7 +609,13 @@ extern "C" int dymoe_matmul_int8(dymoe_ctx* ctx, const void* x, int x_dtype, con
     A.Kp = (int)L.Kp;
     A.N = N;
     A.out_dtype = out_dtype;
-    dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_small_kernel<kI8Plain>, dim3((unsigned)blocks), dim3(256), 0, st, A);
+    A.aligned = dymoe_aligned(y, 4 * dtype_bytes(out_dtype)) && ldy % 4 == 0;
+    if (T > 32) {
+        const int maxf = 4;
+        i8_gemm_launch<kI8Plain>(ctx, DYMOE_K_MATMUL_INT8, maxf, ((T + 32L * maxf - 1) / (32 * maxf)) * ((N + 255L) / 256), st, A);
+    } else {
+        dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_small_kernel<kI8Plain>, dim3((unsigned)blocks), dim3(256), 0, st, A);
+    }
     DYMOE_HIP_LAUNCH_CHECK();
     return DYMOE_OK;
 }
@@ -323,7 +638,7 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     DYMOE_REQUIRE(dymoe_aligned(x, dtype_bytes(x_dtype)) && dymoe_aligned(y, dtype_bytes(out_dtype)) && dymoe_aligned(workspace, 256));
     DYMOE_REQUIRE(dymoe_aligned(idx, 4) && dymoe_aligned(w, 4) && dymoe_aligned(table, 8));
     if (E > DYMOE_MAX_EXPERTS || H > DYMOE_INT8_MAX_K || F > DYMOE_INT8_MAX_K) return DYMOE_ENOTSUP;
-    if ((long)T * k > 0x7fffffffL / 4) return DYMOE_ENOTSUP;
+    if ((long)T * k > 0x7fffffffL / 4 || (long)T * up_to(H, 128) > 0xffffffffL) return DYMOE_ENOTSUP;      // (32-bit offsets into the codes)
     const I8FfnLayout L = i8_ffn_layout(T, H, F, E, k);
     if (workspace_bytes < L.total) return DYMOE_ENOSPC;
     const long up = (long)L.max_tiles * ((F + 31L) / 32), down = (long)L.max_tiles * ((H + 63L) / 64);
@@ -336,7 +651,9 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     int rc = quantize_rows(ctx, x, x_dtype, T, H, H, 0, ws + L.xq, (float*)(ws + L.xs), st);
     if (rc != DYMOE_OK) return rc;
     int32_t* const plan = (int32_t*)(ws + L.plan);
-    dymoe_launch(ctx, DYMOE_K_INT8_PLAN, i8_plan_kernel, dim3(1), dim3(kI8PlanThreads), 0, st, idx, table, P, E, kI8TileSmall, plan,
+    const int maxf = T <= 32 || P <= 8L * E ? 1 : P <= 200L * E ? 8 : 4;
+    const long tiles = P / (32 * maxf) + (E < P ? E : P);
+    dymoe_launch(ctx, DYMOE_K_INT8_PLAN, i8_plan_kernel, dim3(1), dim3(kI8PlanThreads), 0, st, idx, table, P, E, 32 * maxf, plan,
                  ctx->device_flags);
     I8Args A = {};
     A.x = ws + L.xq;
@@ -350,8 +667,9 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     A.N = F;
     A.E = E;
     A.k = k;
-    dymoe_launch(ctx, DYMOE_K_INT8_UP, i8_small_kernel<kI8Up>, dim3((unsigned)up), dim3(256), 0, st, A);
-    rc = quantize_rows(ctx, ws + L.h, DYMOE_OUT_BF16, P, F, (long)L.Fp, 0, ws + L.hq, (float*)(ws + L.hs), st);
+    if (maxf == 1) dymoe_launch(ctx, DYMOE_K_INT8_UP, i8_small_kernel<kI8Up>, dim3((unsigned)up), dim3(256), 0, st, A);
+    else i8_gemm_launch<kI8Up>(ctx, DYMOE_K_INT8_UP, maxf, tiles * ((F + 127L) / 128), st, A);
+    rc = quantize_rows(ctx, ws + L.h, DYMOE_OUT_F32, P, F, (long)L.Fp, 0, ws + L.hq, (float*)(ws + L.hs), st);
     if (rc != DYMOE_OK) return rc;
     A.x = ws + L.hq;
     A.xs = (const float*)(ws + L.hs);
@@ -359,7 +677,8 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     A.ldo = (long)L.Hp;
     A.Kp = (int)L.Fp;
     A.N = H;
-    dymoe_launch(ctx, DYMOE_K_INT8_DOWN, i8_small_kernel<kI8Down>, dim3((unsigned)down), dim3(256), 0, st, A);
+    if (maxf == 1) dymoe_launch(ctx, DYMOE_K_INT8_DOWN, i8_small_kernel<kI8Down>, dim3((unsigned)down), dim3(256), 0, st, A);
+    else i8_gemm_launch<kI8Down>(ctx, DYMOE_K_INT8_DOWN, maxf, tiles * ((H + 255L) / 256), st, A);
     const long items = (long)T * ((H + 3) / 4);
     dymoe_launch(ctx, DYMOE_K_INT8_COMBINE, i8_combine_kernel, dim3((unsigned)((items + 255) / 256)), dim3(256), 0, st,
                  (const float*)(ws + L.part), (long)L.Hp, i8_plan(plan, E, P).where, w, T, H, k, out_dtype, y);

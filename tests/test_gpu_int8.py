@@ -5,7 +5,7 @@ Tolerances, from the formulas:
   64-bit arithmetic (a few operations of 2^-53, a sum of at most 1024 of them).
 * matmul: the sum is exact; its conversion, two products and the bias's addition are four roundings of 2^-24 each of what they round, and
   the output's type adds half a step: 2^-8 (bf16), 2^-11 (fp16), 2^-24 (fp32) of the result, below 2^-14 half of 2^-24 for fp16.
-* moe_ffn: beside those, the intermediate h reaches the quantiser with a relative error eps: 2^-8 for its bf16 form plus 2^-16 for
+* moe_ffn: beside those, the intermediate h reaches the quantiser with a relative error eps of 2^-16:
   fp32 sums, scales and the sigmoid (an exponential of arguments up to 64: 2^-18, the rest an order less).  Its scale moves by as
   much, so h / scale moves by up to 2 eps |h| / scale of a step: a code flips with that probability, by one step, and
   what it stands for drifts by eps of itself.  Codes flip independently of each other: an output's deviation is
@@ -26,7 +26,7 @@ pytestmark = pytest.mark.gpu
 HALF = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11, torch.float32: 2.0 ** -24}
 LOWEST = {t: torch.finfo(t).min for t in HALF}
 OUT = {torch.bfloat16: B.OUT_BF16, torch.float16: B.OUT_F16, torch.float32: B.OUT_F32}
-EPS_H = 2.0 ** -8 + 2.0 ** -16
+EPS_H = 2.0 ** -16
 
 
 @pytest.fixture(scope="module")
