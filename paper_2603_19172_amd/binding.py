@@ -246,9 +246,9 @@ def _shape(name, t, shape):
 def _here(device, *tensors):
     """The launch goes to the current device with the tensors' addresses: both have to be the context's."""
     for t in tensors:
-        if t is not None and (t.device.type != "cuda" or t.device.index != device):
+        if t is not None and t.get_device() != device:
             raise ValueError("tensor on %s, the context is of device %d" % (t.device, device))
-    if torch.cuda.current_device() != device:
+    if torch._C._cuda_getDevice() != device:
         raise ValueError("the context is of device %d, device %d is current" % (device, torch.cuda.current_device()))
 
 
@@ -269,8 +269,8 @@ def _rows_ptr(t):
 
 
 def _stream(stream):
-    if stream is None:
-        stream = torch.cuda.current_stream()
+    if stream is None:      # (torch.cuda.current_stream() makes an object first: 2.9 us of a call's 10.7)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 

@@ -223,6 +223,257 @@ __global__ __launch_bounds__(256) void i8_small_kernel(const I8Args A)
 }
 
 // ----------------------------------------------------------------------------
+// A few rows (decode): a stream of weights.  A workgroup owns 16 weight rows (of W1 and of W3 in the up projection), its wavefronts take the
+// 128-column tiles of K in turn and meet in LDS; every wavefront requests its first kI8Ahead tiles before anything else, so that the
+// rows' quantisation, which every workgroup then does for itself where the rows are few, costs no launch and hides behind them.
+// v_mfma_i32_16x16x64_i8: lane l holds weight row l % 16 and row l % 16 of the codes, columns 64 (l / 32) + 32 j + 16 (l / 16 % 2) of a
+// tile in its j-th product (any order of columns will do that is the same on both sides).
+constexpr int kI8Ahead = 4;
+constexpr int kI8ThinRows = 16;
+constexpr int kI8ThinWaves = 8;
+constexpr int kI8FuseRows = 4;                  // rows up to which a workgroup quantises them itself
+constexpr long kI8FuseBytes = 64 * 1024;        // and the codes' bytes in LDS
+
+typedef int i32x4acc_t __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ i32x4acc_t mfma16_i8(const uint4 a, const uint4 b, const i32x4acc_t c)
+{
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4_t, a), __builtin_bit_cast(i32x4_t, b), c, 0, 0, 0);
+}
+
+template <int S>
+struct I8Thin {
+    uint4 w[kI8Ahead][S][2];
+    const char* q[S];          // the strips' tiles, at the sixteen rows' half
+    uint32_t off;              // this lane's 16 bytes of the first product
+    int kt, nkt, by;           // next tile to multiply, tiles, distance of this wavefront's tiles
+
+    __device__ __forceinline__ void load(int d, int tile)
+    {
+#pragma unroll
+        for (int s = 0; s < S; s++)
+#pragma unroll
+            for (int j = 0; j < 2; j++) w[d][s][j] = load_global<uint4>(q[s] + (long)tile * 4096 + j * 2048 + off);
+    }
+    __device__ __forceinline__ void start(int first, int tiles, int stride, int lane)
+    {
+        kt = first;
+        nkt = tiles;
+        by = stride;
+        off = (uint32_t)((lane >> 4 & 1) * 1024 + (lane >> 5) * 512 + (lane & 15) * 16);
+#pragma unroll
+        for (int d = 0; d < kI8Ahead; d++)
+            if (kt + d * by < nkt) load(d, kt + d * by);
+    }
+    // row(col): 16 codes of this lane's row from column col on
+    template <class Row>
+    __device__ __forceinline__ void run(i32x4acc_t (&acc)[S], int lane, Row row)
+    {
+        const int col = 64 * (lane >> 5) + 16 * (lane >> 4 & 1);
+        while (kt < nkt) {
+#pragma unroll
+            for (int d = 0; d < kI8Ahead; d++) {
+                if (kt < nkt) {
+                    const uint4 b0 = row(kt * 128 + col), b1 = row(kt * 128 + col + 32);
+#pragma unroll
+                    for (int s = 0; s < S; s++) {
+                        acc[s] = mfma16_i8(w[d][s][0], b0, acc[s]);
+                        acc[s] = mfma16_i8(w[d][s][1], b1, acc[s]);
+                    }
+                    if (kt + kI8Ahead * by < nkt) load(d, kt + kI8Ahead * by);
+                }
+                kt += by;
+            }
+        }
+    }
+};
+
+// The codes of `rows` rows into LDS (Kp + 16 bytes apart) and their scales, by a whole workgroup.
+template <int DT>
+__device__ __forceinline__ void i8_rows_to_lds(const char* x, long pitch, int rows, int K, int Kp, char* s_codes, float* s_scale, uint32_t* s_max)
+{
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, n = blockDim.x, waves = n / kWave;
+    for (int r = 0; r < rows; r++) {
+        uint32_t m = 0;
+        for (int col = tid * 8; col < K; col += n * 8) m = peak8<DT>(load8<DT>(x + r * pitch, col, K), m);
+        m = wave_max_u32(peak_bits<DT>(m));
+        if (lane == 0) s_max[r * waves + wave] = m;
+    }
+    __syncthreads();
+    for (int r = 0; r < rows; r++) {
+        uint32_t m = 0;
+        for (int w = 0; w < waves; w++) m = max(m, s_max[r * waves + w]);
+        float sc;
+        const RowQ q = row_q(peak_value<DT>(m), sc);
+        if (tid == 0) s_scale[r] = sc;
+        for (int col = tid * 8; col < Kp; col += n * 8)
+            *(uint2*)(s_codes + (long)r * (Kp + 16) + col) = codes8<DT>(load8<DT>(x + r * pitch, col, K), q);
+    }
+    __syncthreads();
+}
+
+__device__ __forceinline__ void i8_rows_to_lds(int dt, const char* x, long pitch, int rows, int K, int Kp, char* s_codes, float* s_scale, uint32_t* s_max)
+{
+    if (dt == DYMOE_OUT_F32) i8_rows_to_lds<DYMOE_OUT_F32>(x, pitch, rows, K, Kp, s_codes, s_scale, s_max);
+    else if (dt == DYMOE_OUT_F16) i8_rows_to_lds<DYMOE_OUT_F16>(x, pitch, rows, K, Kp, s_codes, s_scale, s_max);
+    else i8_rows_to_lds<DYMOE_OUT_BF16>(x, pitch, rows, K, Kp, s_codes, s_scale, s_max);
+}
+
+struct I8ThinArgs {
+    const char* x;            // FUSE: the rows themselves, else their codes
+    const float* xs;
+    const int32_t* idx;       // experts: [P]
+    const float* gate;
+    const dymoe_expert_i8* table;
+    unsigned* flags;
+    I8Mat w;
+    const float* bias;
+    void* out;
+    long ldx, ldo;            // ldx: bytes from row to row
+    int x_dtype, rows, K, Kp, N, E, k, P, out_dtype;
+};
+
+// The plain product of up to 16 rows, and the up projection of up to 64 pairs: the workgroup of a pair that comes first among those of its
+// expert (or 16, 32, ... behind the first) takes the next sixteen of them.
+template <int MODE, bool FUSE>
+__global__ __launch_bounds__(64 * kI8ThinWaves) void i8_thin_kernel(const I8ThinArgs A)
+{
+    constexpr int S = MODE == kI8Up ? 2 : 1;
+    extern __shared__ __attribute__((aligned(16))) char s_codes[];
+    __shared__ int s_sum[kI8ThinWaves][S][4][kWave];
+    __shared__ float s_scale[kI8ThinRows];
+    __shared__ uint32_t s_max[kI8FuseRows * kI8ThinWaves];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int ln = lane & 15;
+    const int nblk = (A.N + 15) / 16;
+    const int pair = blockIdx.x / nblk, bx = blockIdx.x - pair * nblk;
+    int rows = A.rows, mine = min(ln, A.rows - 1);          // this lane's row: a token of the plain product, a pair of the experts
+    const float *sa, *sb;
+    I8Thin<S> thin;
+    const long strip = (long)(bx >> 1) * 32 * A.Kp + (bx & 1) * 256;
+    if (MODE == kI8Plain) {
+        thin.q[0] = A.w.q + strip;
+        sa = sb = A.w.s;
+    } else {
+        const int my_e = lane < A.P ? A.idx[lane] : -1;
+        const int e = __builtin_amdgcn_readlane(my_e, pair);
+        if ((unsigned)e >= (unsigned)A.E) return;
+        const uint64_t all = __ballot(my_e == e);
+        const int rank = __popcll(all & ((1ull << pair) - 1));
+        if (rank & (kI8ThinRows - 1)) return;
+        const dymoe_expert_i8 ex = A.table[e];
+        if (!i8_present(ex)) {
+            if (tid == 0) atomicOr(A.flags, DYMOE_FLAG_FORMAT_MISSING);
+            return;
+        }
+        rows = min(kI8ThinRows, __popcll(all) - rank);
+        uint64_t left = all >> pair << pair;                 // this tile's pairs and those behind it
+        const int want = min(ln, rows - 1);
+        for (int i = 0; i < want; i++) left &= left - 1;
+        mine = __builtin_ctzll(left);
+        thin.q[0] = (const char*)ex.q[0] + strip;
+        thin.q[S - 1] = (const char*)ex.q[S - 1] + strip;
+        sa = ex.s[0];
+        sb = ex.s[1];
+    }
+    const int nkt = A.Kp >> 7;
+    thin.start(wave, nkt, kI8ThinWaves, lane);
+    const int token = MODE == kI8Up ? mine / A.k : mine;
+    i32x4acc_t acc[S] = {};
+    if constexpr (FUSE) {
+        i8_rows_to_lds(A.x_dtype, A.x, A.ldx, MODE == kI8Up ? A.P / A.k : A.rows, A.K, A.Kp, s_codes, s_scale, s_max);
+        const char* const row = s_codes + token * (A.Kp + 16);
+        thin.run(acc, lane, [&](int col) { return *(const uint4*)(row + col); });
+    } else {
+        const char* const row = A.x + (long)token * A.ldx;
+        thin.run(acc, lane, [&](int col) { return load_global<uint4>(row + col); });
+    }
+#pragma unroll
+    for (int s = 0; s < S; s++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) s_sum[wave][s][i][lane] = acc[s][i];
+    __syncthreads();
+    // wavefronts 0 .. 3 finish weight rows 4 (l / 16) + wave of row l % 16
+    if (wave >= 4 || ln >= rows) return;
+    int sum[S];
+#pragma unroll
+    for (int s = 0; s < S; s++) {
+        sum[s] = 0;
+#pragma unroll
+        for (int w = 0; w < kI8ThinWaves; w++) sum[s] += s_sum[w][s][wave][lane];
+    }
+    const int n = 16 * bx + 4 * (lane >> 4) + wave;
+    if (n >= A.N) return;
+    const float xs = FUSE ? s_scale[token] : A.xs[token];
+    if (MODE == kI8Up) {
+        ((DYMOE_GLOBAL float*)A.out)[mine * A.ldo + n] = silu_times((float)sum[0] * xs * sa[n], (float)sum[S - 1] * xs * sb[n]);
+    } else {
+        float o = (float)sum[0] * xs * sa[n];
+        if (A.bias) o += A.bias[n];
+        store_out(A.out, mine * A.ldo + n, A.out_dtype, o);
+    }
+}
+
+// The down projection of up to kI8FuseRows tokens with the sum over their slots: a workgroup owns 16 outputs of one token; its wavefronts
+// share out the token's pairs, or a pair's tiles where there are fewer pairs than wavefronts.  Every workgroup quantises the
+// intermediate's rows itself.
+constexpr int kI8LastWaves = 16;
+
+__global__ __launch_bounds__(64 * kI8LastWaves) void i8_thin_down_kernel(const I8ThinArgs A)
+{
+    extern __shared__ __attribute__((aligned(16))) char s_codes[];
+    __shared__ int s_sum[64][16];
+    __shared__ float s_scale[64];
+    __shared__ uint32_t s_max[64 * kI8LastWaves];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    // the workgroups of one strip go to one XCD, whose L2 then has the weights that several tokens need
+    const int nblk = (A.N + 15) / 16, j = blockIdx.x >> 3;
+    const int t = j % A.rows, bx = j / A.rows * 8 + (blockIdx.x & 7);
+    if (bx >= nblk) return;
+    const int k = A.k, seg = max(1, kI8LastWaves / k), units = k * seg;
+    const long strip = (long)(bx >> 1) * 32 * A.Kp + (bx & 1) * 256;
+    const int nkt = A.Kp >> 7;
+    I8Thin<1> thin;
+    bool ok = false;
+    auto begin = [&](int u) {
+        const int e = __builtin_amdgcn_readfirstlane(A.idx[t * k + u / seg]);
+        ok = (unsigned)e < (unsigned)A.E;
+        if (ok) {
+            const dymoe_expert_i8 ex = A.table[e];
+            ok = i8_present(ex);
+            thin.q[0] = (const char*)ex.q[2] + strip;
+        }
+        if (ok) thin.start(u % seg, nkt, seg, lane);
+    };
+    if (wave < units) begin(wave);
+    i8_rows_to_lds<DYMOE_OUT_F32>(A.x + (long)t * k * A.ldx, A.ldx, k, A.K, A.Kp, s_codes, s_scale, s_max);
+    for (int u = wave; u < units; u += kI8LastWaves) {
+        if (u != wave) begin(u);
+        i32x4acc_t acc[1] = {};
+        if (ok) {
+            const char* const row = s_codes + (long)(u / seg) * (A.Kp + 16);
+            thin.run(acc, lane, [&](int col) { return *(const uint4*)(row + col); });
+        }
+        if ((lane & 15) == 0) {
+#pragma unroll
+            for (int i = 0; i < 4; i++) s_sum[u][4 * (lane >> 4) + i] = acc[0][i];
+        }
+    }
+    __syncthreads();
+    const int n = 16 * bx + tid;
+    if (tid >= 16 || n >= A.N) return;
+    float y = 0.0f;
+    for (int i = 0; i < k; i++) {
+        const int e = A.idx[t * k + i];
+        if ((unsigned)e >= (unsigned)A.E || !i8_present(A.table[e])) continue;
+        int sum = 0;
+        for (int s = 0; s < seg; s++) sum += s_sum[i * seg + s][tid];
+        y = fmaf(A.gate[t * k + i], (float)sum * s_scale[i] * A.table[e].s[2][n], y);
+    }
+    store_out(A.out, t * A.ldo + n, A.out_dtype, y);
+}
+
+// ----------------------------------------------------------------------------
 // Tiles of up to 128 or 256 rows.  A workgroup of four wavefronts owns eight strips of 32 weight rows (two a wavefront) and walks K in steps
 // of 256 columns.
 //  * Weights come straight into registers: a tile's bytes lie in the order of the matrix instruction's operand, so a wavefront's load is 1 KiB
@@ -519,6 +770,9 @@ int i8_init()
                        i8_allow_lds<kI8Plain, 8>(), i8_allow_lds<kI8Up, 8>(), i8_allow_lds<kI8Down, 8>()};
     for (int r : rc)
         if (r != DYMOE_OK) return r;
+    const void* const thin[3] = {(const void*)i8_thin_kernel<kI8Plain, true>, (const void*)i8_thin_kernel<kI8Up, true>, (const void*)i8_thin_down_kernel};
+    for (const void* f : thin)
+        if (hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kI8FuseBytes) != hipSuccess) return DYMOE_EHIP;
     return DYMOE_OK;
 }
 
@@ -591,10 +845,11 @@ extern "C" int dymoe_matmul_int8(dymoe_ctx* ctx, const void* x, int x_dtype, con
     if (T == 0) return DYMOE_OK;
     hipStream_t st = (hipStream_t)stream;
     char* const ws = (char*)workspace;
+    const bool thin = T <= kI8ThinRows, fuse = thin && !coded && T <= kI8FuseRows && T * (long)(L.Kp + 16) <= kI8FuseBytes;
     I8Args A = {};
     A.x = (const char*)x;
     A.xs = x_scale;
-    if (!coded) {
+    if (!coded && !fuse) {
         const int rc = quantize_rows(ctx, x, x_dtype, T, K, ldx, 0, ws + L.xq, (float*)(ws + L.xs), st);
         if (rc != DYMOE_OK) return rc;
         A.x = ws + L.xq;
@@ -609,6 +864,27 @@ extern "C" int dymoe_matmul_int8(dymoe_ctx* ctx, const void* x, int x_dtype, con
     A.Kp = (int)L.Kp;
     A.N = N;
     A.out_dtype = out_dtype;
+    if (thin) {
+        I8ThinArgs B = {};
+        B.x = A.x;
+        B.xs = A.xs;
+        B.w = A.w;
+        B.bias = bias;
+        B.out = y;
+        B.ldx = fuse ? ldx * dtype_bytes(x_dtype) : (long)L.Kp;
+        B.ldo = ldy;
+        B.x_dtype = x_dtype;
+        B.rows = T;
+        B.K = K;
+        B.Kp = (int)L.Kp;
+        B.N = N;
+        B.out_dtype = out_dtype;
+        const dim3 grid((unsigned)((N + 15) / 16)), block(64 * kI8ThinWaves);
+        if (fuse) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_thin_kernel<kI8Plain, true>, grid, block, T * (L.Kp + 16), st, B);
+        else dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_thin_kernel<kI8Plain, false>, grid, block, 0, st, B);
+        DYMOE_HIP_LAUNCH_CHECK();
+        return DYMOE_OK;
+    }
     A.aligned = dymoe_aligned(y, 4 * dtype_bytes(out_dtype)) && ldy % 4 == 0;
     if (T > 32) {
         const int maxf = 4;
@@ -648,6 +924,39 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     hipStream_t st = (hipStream_t)stream;
     char* const ws = (char*)workspace;
     const long P = (long)T * k;
+    if (T <= kI8FuseRows && k <= 64 && P <= 64 && T * (long)(L.Hp + 16) <= kI8FuseBytes && k * (long)(L.Fp + 16) <= kI8FuseBytes) {
+        I8ThinArgs B = {};
+        B.x = (const char*)x;
+        B.idx = idx;
+        B.table = table;
+        B.flags = ctx->device_flags;
+        B.out = ws + L.h;
+        B.ldx = (long)H * dtype_bytes(x_dtype);
+        B.ldo = (long)L.Fp;
+        B.x_dtype = x_dtype;
+        B.rows = T;
+        B.K = H;
+        B.Kp = (int)L.Hp;
+        B.N = F;
+        B.E = E;
+        B.k = k;
+        B.P = (int)P;
+        dymoe_launch(ctx, DYMOE_K_INT8_UP, i8_thin_kernel<kI8Up, true>, dim3((unsigned)(P * ((F + 15) / 16))), dim3(64 * kI8ThinWaves),
+                     T * (L.Hp + 16), st, B);
+        B.x = ws + L.h;
+        B.gate = w;
+        B.out = y;
+        B.ldx = (long)L.Fp * 4;
+        B.ldo = H;
+        B.K = F;
+        B.Kp = (int)L.Fp;
+        B.N = H;
+        B.out_dtype = out_dtype;
+        dymoe_launch(ctx, DYMOE_K_INT8_DOWN, i8_thin_down_kernel, dim3((unsigned)(8 * T * (((H + 15) / 16 + 7) / 8))), dim3(64 * kI8LastWaves),
+                     k * (L.Fp + 16), st, B);
+        DYMOE_HIP_LAUNCH_CHECK();
+        return DYMOE_OK;
+    }
     int rc = quantize_rows(ctx, x, x_dtype, T, H, H, 0, ws + L.xq, (float*)(ws + L.xs), st);
     if (rc != DYMOE_OK) return rc;
     int32_t* const plan = (int32_t*)(ws + L.plan);
