@@ -13,18 +13,17 @@ namespace dymoe {
 int quantize_rows(dymoe_ctx* ctx, const void* x, int dtype, long rows, long K, long ldx, int tiles, void* codes, float* scale, hipStream_t st);
 
 struct I8Plan {
-    int32_t* offsets;     // [E + 1] first position of each expert
     int32_t* meta;        // [8]: tiles
     int32_t* perm;        // [P] position -> pair
     int32_t* where;       // [P] pair -> position, -1: left out
-    int32_t* tiles;       // [4 max_tiles]: expert, first position, rows, unused
+    int32_t* tiles;       // [8 max_tiles]: the tile's expert, its first position, its pairs, its first tile, its tiles (3 unused)
 };
 
 __host__ __device__ inline I8Plan i8_plan(int32_t* p, int E, long P)
 {
     I8Plan r;
-    r.offsets = p;
-    r.meta = r.offsets + E + 1;
+    (void)E;
+    r.meta = p;
     r.perm = r.meta + 8;
     r.where = r.perm + P;
     r.tiles = r.where + P;
@@ -36,67 +35,94 @@ __device__ __forceinline__ bool i8_present(const dymoe_expert_i8& x)
     return (x.q[0] != nullptr) & (x.q[1] != nullptr) & (x.q[2] != nullptr) & (x.s[0] != nullptr) & (x.s[1] != nullptr) & (x.s[2] != nullptr);
 }
 
-// Counting sort of the pairs by expert and the list of tiles, by one workgroup.
+// Counting sort of the pairs by expert and the list of tiles, by one workgroup.  Experts come by falling number of pairs, so that the largest
+// tiles start first.  A pair's turn in its expert is what the counter held before it: kept in registers (in `where` beyond the first
+// kI8PlanKeep pairs of a thread) until the experts' first positions are known, so that there is one pass of atomics.  The turns
+// come in any order, and nothing that is computed depends on it.
 constexpr int kI8PlanThreads = 1024;
+constexpr int kI8PlanKeep = 16;
 
 __global__ __launch_bounds__(kI8PlanThreads) void i8_plan_kernel(const int32_t* __restrict__ idx, const dymoe_expert_i8* __restrict__ table,
                                                                  long P, int E, int tile_rows, int32_t* __restrict__ plan,
                                                                  unsigned* __restrict__ flags)
 {
-    __shared__ int s_count[DYMOE_MAX_EXPERTS], s_at[DYMOE_MAX_EXPERTS], s_wave[2][kI8PlanThreads / kWave];
-    __shared__ int s_held[DYMOE_MAX_EXPERTS];
+    __shared__ int s_count[DYMOE_MAX_EXPERTS], s_sorted[DYMOE_MAX_EXPERTS], s_at[DYMOE_MAX_EXPERTS], s_wave[2][kI8PlanThreads / kWave];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const I8Plan pp = i8_plan(plan, E, P);
-    if (tid < E) {
-        s_count[tid] = 0;
-        s_held[tid] = i8_present(table[tid]);
+    int e_of[kI8PlanKeep], turn[kI8PlanKeep];
+#pragma unroll
+    for (int i = 0; i < kI8PlanKeep; i++) {
+        const long p = tid + (long)i * kI8PlanThreads;
+        e_of[i] = p < P ? idx[p] : -1;
     }
+    const bool held = tid < E && i8_present(table[tid]);
+    if (tid < E) s_count[tid] = 0;
     __syncthreads();
-    for (long p = tid; p < P; p += kI8PlanThreads) {
+#pragma unroll
+    for (int i = 0; i < kI8PlanKeep; i++)
+        if ((unsigned)e_of[i] < (unsigned)E) turn[i] = atomicAdd(&s_count[e_of[i]], 1);
+    for (long p = tid + (long)kI8PlanKeep * kI8PlanThreads; p < P; p += kI8PlanThreads) {
         const int e = idx[p];
-        if ((unsigned)e < (unsigned)E) atomicAdd(&s_count[e], 1);
+        if ((unsigned)e < (unsigned)E) pp.where[p] = atomicAdd(&s_count[e], 1);
     }
     __syncthreads();
     int n = tid < E ? s_count[tid] : 0;
-    if (n > 0 && !s_held[tid]) {
+    if (n > 0 && !held) {
         atomicOr(flags, DYMOE_FLAG_FORMAT_MISSING);
         n = 0;
     }
-    const int tiles = (n + tile_rows - 1) / tile_rows;
-    const int n_in = wave_scan_dpp_i32(n), t_in = wave_scan_dpp_i32(tiles);
+    if (tid < E) s_at[tid] = n;
+    __syncthreads();
+    if (tid < E) {
+        int rank = 0;
+        for (int e = 0; e < E; e++) {
+            const int o = s_at[e];
+            rank += (o > n) || (o == n && e < tid);
+        }
+        s_sorted[rank] = tid;
+    }
+    __syncthreads();
+    const int e = tid < E ? s_sorted[tid] : 0;
+    n = tid < E ? s_at[e] : 0;
+    const int m = (n + tile_rows - 1) / tile_rows;
+    const int n_in = wave_scan_dpp_i32(n), t_in = wave_scan_dpp_i32(m);
     if (lane == kWave - 1) {
         s_wave[0][wave] = n_in;
         s_wave[1][wave] = t_in;
     }
     __syncthreads();
-    int n0 = n_in - n, t0 = t_in - tiles;
+    int n0 = n_in - n, t0 = t_in - m;
     for (int w = 0; w < wave; w++) {
         n0 += s_wave[0][w];
         t0 += s_wave[1][w];
     }
     if (tid < E) {
-        s_at[tid] = n0;
-        pp.offsets[tid] = n0;
-        if (tid == E - 1) pp.offsets[E] = n0 + n;
-        for (int i = 0; i < tiles; i++) {
-            int32_t* const t = pp.tiles + 4L * (t0 + i);
-            t[0] = tid;
-            t[1] = n0 + i * tile_rows;
-            t[2] = min(tile_rows, n - i * tile_rows);
+        s_at[e] = n > 0 ? n0 : -1;               // (every thread has read its count)
+        for (int i = 0; i < m; i++) {
+            int32_t* const t = pp.tiles + 8L * (t0 + i);
+            t[0] = e;
+            t[1] = n0;
+            t[2] = n;
+            t[3] = t0;
+            t[4] = m;
         }
     }
-    if (tid == kI8PlanThreads - 1) pp.meta[0] = t0 + tiles;
+    if (tid == kI8PlanThreads - 1) pp.meta[0] = t0 + m;
     __syncthreads();
-    // (an expert's pairs come in any order: nothing that is computed depends on it)
-    for (long p = tid; p < P; p += kI8PlanThreads) {
-        const int e = idx[p];
+    auto place = [&](long p, int x, int rank) {
         int at = -1;
-        if ((unsigned)e < (unsigned)E && s_held[e]) {
-            at = atomicAdd(&s_at[e], 1);
+        if ((unsigned)x < (unsigned)E && s_at[x] >= 0) {
+            at = s_at[x] + rank;
             pp.perm[at] = (int32_t)p;
         }
         pp.where[p] = at;
+    };
+#pragma unroll
+    for (int i = 0; i < kI8PlanKeep; i++) {
+        const long p = tid + (long)i * kI8PlanThreads;
+        if (p < P) place(p, e_of[i], turn[i]);
     }
+    for (long p = tid + (long)kI8PlanKeep * kI8PlanThreads; p < P; p += kI8PlanThreads) place(p, idx[p], pp.where[p]);
 }
 
 // One weight matrix as a launch reads it: codes in tiles, scales.
@@ -151,9 +177,10 @@ __global__ __launch_bounds__(256) void i8_small_kernel(const I8Args A)
         sa = sb = A.w.s;
     } else {
         if (tile >= pp.meta[0]) return;
-        const int e = pp.tiles[4 * tile];
-        row0 = pp.tiles[4 * tile + 1];
-        rows = pp.tiles[4 * tile + 2];
+        const int32_t* const t = pp.tiles + 8L * tile;
+        const int e = t[0], i = (tile - t[3]) * kI8TileSmall;
+        row0 = t[1] + i;
+        rows = min(kI8TileSmall, t[2] - i);
         const dymoe_expert_i8 ex = A.table[e];
         if (MODE == kI8Up) {
             qa = (const char*)ex.q[0] + bx * strip;
@@ -474,32 +501,34 @@ __global__ __launch_bounds__(64 * kI8LastWaves) void i8_thin_down_kernel(const I
 }
 
 // ----------------------------------------------------------------------------
-// Tiles of up to 128 or 256 rows.  A workgroup of four wavefronts owns eight strips of 32 weight rows (two a wavefront) and walks K in steps
-// of 256 columns.
+// Tiles of up to 128 rows.  A workgroup of four wavefronts owns S strips of 32 weight rows a wavefront and walks K in steps of KT tiles of 128
+// columns.
 //  * Weights come straight into registers: a tile's bytes lie in the order of the matrix instruction's operand, so a wavefront's load is 1 KiB
 //    of contiguous memory.  A register is requested anew, for the next step, as soon as the last instruction that reads it has been issued.
 //  * The rows' codes are shared by the wavefronts through two LDS buffers that global memory fills directly; 16-byte chunk c of row r lies at
-//    position c ^ (r & 15), which spreads the operand reads (one chunk of 32 rows) over all banks.
-//  * Up to 128 rows: 128 accumulator registers a lane, two workgroups on a compute unit, one's waits covered by the other's products.
-//    Up to 256 rows: 256 accumulator registers, one workgroup; for experts that meet so few tokens that the weights' bytes, not the
-//    products, bound the call: they are then read once.
-constexpr int kI8Step = 256;                    // columns of a step
-constexpr uint32_t kI8EpiRow = 272;             // epilogue: bytes of a row of 64 fp32 in LDS, 16 of them padding
-constexpr uint32_t kI8EpiWave = 32 * kI8EpiRow;
+//    position c ^ (r & mask), which spreads the operand reads (one chunk of 32 rows) over all banks.
+//  * Several workgroups on a compute unit, one's waits, prologue and epilogue covered by the others' products.
+// Two shapes: S = 2, KT = 2 (128 accumulator registers a lane, two workgroups a compute unit) reads half as much LDS for a product; S = 1,
+// KT = 1 (64, four workgroups) has more loads on their way and twice as many workgroups, for calls that the weights' bytes bound.
+template <int S>
+constexpr uint32_t kI8EpiRow = S == 2 ? 272 : 144;     // epilogue: bytes of a row of 32 S sums in LDS, 16 of them padding
+template <int S>
+constexpr uint32_t kI8EpiWave = 32 * kI8EpiRow<S>;
 
-struct I8Strip {
-    uint4 r[8];       // chunk j = 4 * (128-column tile of the step) + 16-byte chunk of the lane's half of that tile
+template <int S, int KT>
+struct I8Strips {
+    uint4 r[S][4 * KT];       // chunk j = 4 * (tile of the step) + 16-byte chunk of the lane's half of that tile
 };
 
-// chunk j of step ks of the strip at p (this lane's first 16 bytes); tiles behind the last re-read it
+// chunk c of a tile of the strip at p
 __device__ __forceinline__ uint4 i8_chunk(const char* p, uint32_t lane16, int tile, int c)
 {
     return load_global<uint4>(p + (long)tile * 4096 + c * 1024 + lane16);
 }
 
-template <int NTF>
+template <int NTF, int KT>
 struct I8Stage {
-    static constexpr int kCopies = 2 * NTF;     // 32 NTF rows of 256 bytes, 16 rows an instruction of the workgroup
+    static constexpr int kCopies = NTF * KT;    // an instruction of the workgroup fills 4 KiB
     const char* base;
     uint32_t off[kCopies];
     uint32_t lds;
@@ -509,42 +538,44 @@ struct I8Ops {
     uint4 t0, t1;
 };
 
-// Chunks [J0, J1) of a step.  The operands of the next pair of chunks are read while the products of this one are issued.
-template <int NTF, int J1>
-__device__ __forceinline__ void i8_step(I8Strip& ra, I8Strip& rb, const char* sa, const char* sb, uint32_t lane16, int tile_next, int nkt,
-                                        uint32_t xa, i32x16_t (&acc)[2][NTF])
+// The first TILES tiles of a step.  The operands of the next pair of chunks are read while the products of this one are issued.
+template <int NTF, int S, int KT, int TILES>
+__device__ __forceinline__ void i8_step(I8Strips<S, KT>& w, const char* const (&q)[S], uint32_t lane16, int tile_next, int nkt, uint32_t xa,
+                                        i32x16_t (&acc)[S][NTF])
 {
     constexpr int kStepMask = 0x2 | 0x4;        // vector and scalar arithmetic may cross; products, LDS and memory accesses may not
+    constexpr int kPairs = 2 * TILES;
     I8Ops ops;
     ops.t0 = lds_read16(xa);
     ops.t1 = lds_read16(xa ^ 16u);
 #pragma unroll
-    for (int jj = 0; jj < J1 / 2; jj++) {
+    for (int jj = 0; jj < kPairs; jj++) {
 #pragma unroll
         for (int tf = 0; tf < NTF; tf++) {
             const bool wrap = tf == NTF - 1;
-            const bool last = wrap && jj == J1 / 2 - 1;
+            const bool last = wrap && jj == kPairs - 1;
             const int nj = wrap ? jj + 1 : jj, nf = wrap ? 0 : tf + 1;
             I8Ops nxt = ops;
             if (!last) {
                 // chunks 2 nj, 2 nj + 1 of the lane's columns: position 8 * tile + 4 * half + chunk, the half already in xa
-                const uint32_t at = (xa ^ (uint32_t)(((nj >> 1) << 7) | ((nj & 1) << 5))) + (uint32_t)nf * (32 * kI8Step);
+                const uint32_t at = (xa ^ (uint32_t)(((nj >> 1) << 7) | ((nj & 1) << 5))) + (uint32_t)nf * (32 * 128 * KT);
                 nxt.t0 = lds_read16(at);
                 nxt.t1 = lds_read16(at ^ 16u);
             }
             __builtin_amdgcn_sched_barrier(kStepMask);
-            acc[0][tf] = mfma_i8(ra.r[2 * jj], ops.t0, acc[0][tf]);
-            acc[1][tf] = mfma_i8(rb.r[2 * jj], ops.t0, acc[1][tf]);
-            acc[0][tf] = mfma_i8(ra.r[2 * jj + 1], ops.t1, acc[0][tf]);
-            acc[1][tf] = mfma_i8(rb.r[2 * jj + 1], ops.t1, acc[1][tf]);
+#pragma unroll
+            for (int s = 0; s < S; s++) acc[s][tf] = mfma_i8(w.r[s][2 * jj], ops.t0, acc[s][tf]);
+#pragma unroll
+            for (int s = 0; s < S; s++) acc[s][tf] = mfma_i8(w.r[s][2 * jj + 1], ops.t1, acc[s][tf]);
             ops = nxt;
             __builtin_amdgcn_sched_barrier(kStepMask);
         }
         const int tile = min(tile_next + (jj >> 1), nkt - 1), c = 2 * (jj & 1);
-        ra.r[2 * jj] = i8_chunk(sa, lane16, tile, c);
-        ra.r[2 * jj + 1] = i8_chunk(sa, lane16, tile, c + 1);
-        rb.r[2 * jj] = i8_chunk(sb, lane16, tile, c);
-        rb.r[2 * jj + 1] = i8_chunk(sb, lane16, tile, c + 1);
+#pragma unroll
+        for (int s = 0; s < S; s++) {
+            w.r[s][2 * jj] = i8_chunk(q[s], lane16, tile, c);
+            w.r[s][2 * jj + 1] = i8_chunk(q[s], lane16, tile, c + 1);
+        }
         __builtin_amdgcn_sched_barrier(kStepMask);
     }
 }
@@ -569,78 +600,72 @@ __device__ __forceinline__ void i8_store4(void* out, long at, int dt, bool whole
         if (i < left) store_out(out, at + i, dt, v[i]);
 }
 
-template <int MODE, int NTF>
-__device__ __forceinline__ void i8_tile(const I8Args& A, const int32_t* perm, const char* qa, const char* qb, const float* sa, const float* sb,
+// qw: this wavefront's strips; sa, sb: the scales of the matrices
+template <int MODE, int NTF, int S, int KT>
+__device__ __forceinline__ void i8_tile(const I8Args& A, const int32_t* perm, const char* const (&qw)[S], const float* sa, const float* sb,
                                         int row0, int rows, int bx, uint32_t xs_base, uint32_t buf_bytes)
 {
+    constexpr int kLanes = 8 * KT;              // lanes (16-byte chunks) to a row of a step
+    constexpr int kRowsWave = 64 / kLanes;      // rows that a wavefront's copy fills
+    constexpr uint32_t kRow = 128 * KT;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int ln = lane & 31, kb = lane >> 5;
     const uint32_t lane16 = (uint32_t)lane * 16u;
-    i32x16_t acc[2][NTF] = {};
-    I8Stage<NTF> stage;
-    {
-        // wavefront w fills rows 16 i + 4 w .. + 3: lane l row l / 16 of them, the chunk that belongs at position l % 16
-        const int rb = 4 * wave + (lane >> 4);
-        const int chunk = (lane & 15) ^ (rb & 15);
+    i32x16_t acc[S][NTF] = {};
+    I8Stage<NTF, KT> stage;
+    const int rb = kRowsWave * wave + lane / kLanes;                         // (rows of a thread agree in r & mask)
+    const int chunk = (lane & (kLanes - 1)) ^ (rb & (kLanes - 1));
 #pragma unroll
-        for (int i = 0; i < I8Stage<NTF>::kCopies; i++) {
-            const int r = min(16 * i + rb, rows - 1);         // rows behind the last: computed and dropped
-            const uint32_t src = MODE == kI8Up ? (uint32_t)(perm[row0 + r] / A.k) : (uint32_t)r;
-            stage.off[i] = src * (uint32_t)A.Kp + 16u * (uint32_t)chunk;      // below 4 GiB: checked by the launcher
-        }
-        stage.base = A.x + (MODE == kI8Up ? 0 : (long)row0 * A.Kp);
-        stage.lds = __builtin_amdgcn_readfirstlane(xs_base + (uint32_t)wave * 1024u);
+    for (int i = 0; i < I8Stage<NTF, KT>::kCopies; i++) {
+        const int r = min(4 * kRowsWave * i + rb, rows - 1);                 // rows behind the last: computed and dropped
+        const uint32_t src = MODE == kI8Up ? (uint32_t)(perm[row0 + r] / A.k) : (uint32_t)r;
+        stage.off[i] = src * (uint32_t)A.Kp + 16u * (uint32_t)chunk;          // below 4 GiB: checked by the launcher
     }
-    const int nkt = A.Kp >> 7, steps = (nkt + 1) >> 1;
-    // (the last step's second half may lie behind the rows' end: its chunks are then those of the first half, and go unused)
-    const uint32_t back = (nkt & 1) && (((lane & 15) ^ ((4 * wave + (lane >> 4)) & 15)) & 8) ? 128u : 0u;
+    stage.base = A.x + (MODE == kI8Up ? 0 : (long)row0 * A.Kp);
+    stage.lds = __builtin_amdgcn_readfirstlane(xs_base + (uint32_t)wave * 1024u);
+    const int nkt = A.Kp >> 7, steps = (nkt + KT - 1) / KT;
+    // (two tiles a step: the last step's second may lie behind the rows' end: its chunks are then those of the first, and go unused)
+    const uint32_t back = KT == 2 && (nkt & 1) && (chunk & 8) ? 128u : 0u;
     auto copy = [&](int ks, uint32_t at) {
-        const char* const base = stage.base + (long)ks * kI8Step;
+        const char* const base = stage.base + (long)ks * kRow;
         const uint32_t less = ks == steps - 1 ? back : 0u;
 #pragma unroll
-        for (int i = 0; i < I8Stage<NTF>::kCopies; i++) lds_copy16(base, stage.off[i] - less, stage.lds + at + (uint32_t)i * 4096u);
+        for (int i = 0; i < I8Stage<NTF, KT>::kCopies; i++) lds_copy16(base, stage.off[i] - less, stage.lds + at + (uint32_t)i * 4096u);
     };
-    const uint32_t xa0 = xs_base + (uint32_t)ln * kI8Step + (((uint32_t)kb << 6) ^ ((uint32_t)(ln & 15) << 4));
-    I8Strip ra, rb;
+    const uint32_t xa0 = xs_base + (uint32_t)ln * kRow + (((uint32_t)kb << 6) ^ ((uint32_t)(ln & (kLanes - 1)) << 4));
+    I8Strips<S, KT> w;
     copy(0, 0);
 #pragma unroll
-    for (int j = 0; j < 8; j++) {
-        ra.r[j] = i8_chunk(qa, lane16, min(j >> 2, nkt - 1), j & 3);
-        rb.r[j] = i8_chunk(qb, lane16, min(j >> 2, nkt - 1), j & 3);
-    }
+    for (int j = 0; j < 4 * KT; j++)
+#pragma unroll
+        for (int s = 0; s < S; s++) w.r[s][j] = i8_chunk(qw[s], lane16, min(j >> 2, nkt - 1), j & 3);
     wait_lds_copies<0>();
     __syncthreads();
     uint32_t at = 0;
-    for (int ks = 0; ks < nkt >> 1; ks++) {
+    for (int ks = 0; ks < nkt / KT; ks++) {
         copy(min(ks + 1, steps - 1), at ^ buf_bytes);
-        i8_step<NTF, 8>(ra, rb, qa, qb, lane16, 2 * (ks + 1), nkt, xa0 + at, acc);
-        wait_lds_copies<16>();          // the copies are older than the sixteen loads of weights
+        i8_step<NTF, S, KT, KT>(w, qw, lane16, KT * (ks + 1), nkt, xa0 + at, acc);
+        wait_lds_copies<4 * S * KT>();          // the copies are older than the loads of weights
         __syncthreads();
         at ^= buf_bytes;
     }
-    if (nkt & 1) {
-        i8_step<NTF, 4>(ra, rb, qa, qb, lane16, nkt - 1, nkt, xa0 + at, acc);
-        __syncthreads();
+    if constexpr (KT == 2) {
+        if (nkt & 1) {
+            i8_step<NTF, S, KT, 1>(w, qw, lane16, nkt - 1, nkt, xa0 + at, acc);
+            __syncthreads();
+        }
     }
 
     // Epilogue.  A lane holds, of its token's row, four neighbouring outputs in each group of four registers; the wavefront turns a fragment
     // round in an area of its own, so that a row leaves in whole lines.
-    const uint32_t area = xs_base + (uint32_t)wave * kI8EpiWave;
-    const uint32_t wr = area + (uint32_t)ln * kI8EpiRow + (uint32_t)kb * 16u;
-    const int chunk = MODE == kI8Up ? lane & 7 : lane & 15;
-    const int n = MODE == kI8Up ? (4 * bx + wave) * 32 + 4 * chunk : (4 * bx + wave) * 64 + 4 * chunk;
-    float sc[4], add[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-        sc[i] = MODE != kI8Up ? sa[min(n + i, A.N - 1)] : 0.f;
-        if (MODE == kI8Plain && A.bias) add[i] = A.bias[min(n + i, A.N - 1)];
-    }
-    const int left = A.N - n;
+    const uint32_t area = xs_base + (uint32_t)wave * kI8EpiWave<S>;
+    const uint32_t wr = area + (uint32_t)ln * kI8EpiRow<S> + (uint32_t)kb * 16u;
+    const bool vec = MODE != kI8Plain || A.aligned;
     const int dt = MODE == kI8Plain ? A.out_dtype : DYMOE_OUT_F32;
-    const bool whole = left >= 4 && (MODE != kI8Plain || A.aligned);
+    if constexpr (MODE == kI8Up && S == 2) {
+        const int n = (4 * bx + wave) * 32 + 4 * (lane & 7), left = A.N - n;
 #pragma unroll
-    for (int tf = 0; tf < NTF; tf++) {
-        if (MODE == kI8Up) {
+        for (int tf = 0; tf < NTF; tf++) {
             const int r = min(32 * tf + ln, rows - 1);
             const float xs = A.xs[perm[row0 + r] / A.k];
 #pragma unroll
@@ -649,140 +674,180 @@ __device__ __forceinline__ void i8_tile(const I8Args& A, const int32_t* perm, co
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
                     const int f = min((4 * bx + wave) * 32 + 8 * g + 4 * kb + i, A.N - 1);
-                    h[i] = silu_times((float)acc[0][tf][4 * g + i] * xs * sa[f], (float)acc[1][tf][4 * g + i] * xs * sb[f]);
+                    h[i] = silu_times((float)acc[0][tf][4 * g + i] * xs * sa[f], (float)acc[S - 1][tf][4 * g + i] * xs * sb[f]);
                 }
                 lds_write16(wr + 32u * g, make_uint4(__float_as_uint(h[0]), __float_as_uint(h[1]), __float_as_uint(h[2]), __float_as_uint(h[3])));
             }
-        } else {
+            // (a wavefront's LDS accesses execute in order and the area is its own: no barrier)
 #pragma unroll
-            for (int s = 0; s < 2; s++)
-#pragma unroll
-                for (int g = 0; g < 4; g++)
-                    lds_write16(wr + (uint32_t)(s * 128 + g * 32), make_uint4((uint32_t)acc[s][tf][4 * g], (uint32_t)acc[s][tf][4 * g + 1],
-                                                                              (uint32_t)acc[s][tf][4 * g + 2], (uint32_t)acc[s][tf][4 * g + 3]));
-        }
-        // (a wavefront's LDS accesses execute in order and the area is its own: no barrier)
-        constexpr int kSub = MODE == kI8Up ? 8 : 4;       // rows an instruction reads
-        const int rsub = MODE == kI8Up ? lane >> 3 : lane >> 4;
-#pragma unroll
-        for (int j = 0; j < 32 / kSub; j++) {
-            const int rr = rsub + kSub * j, row = 32 * tf + rr;
-            const uint4 u = lds_read16(area + (uint32_t)rr * kI8EpiRow + (uint32_t)chunk * 16u);
-            if (row >= rows || left <= 0) continue;
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-            float v[4];
-            if (MODE == kI8Up) {
-#pragma unroll
-                for (int i = 0; i < 4; i++) v[i] = __uint_as_float(w[i]);
-            } else {
-                const float xs = A.xs[row0 + row];
-#pragma unroll
-                for (int i = 0; i < 4; i++) v[i] = (float)(int)w[i] * xs * sc[i] + add[i];
+            for (int j = 0; j < 4; j++) {
+                const int rr = (lane >> 3) + 8 * j, row = 32 * tf + rr;
+                const uint4 u = lds_read16(area + (uint32_t)rr * kI8EpiRow<S> + (uint32_t)(lane & 7) * 16u);
+                if (row >= rows || left <= 0) continue;
+                const float v[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
+                i8_store4(A.out, (long)(row0 + row) * A.ldo + n, dt, left >= 4, left, v);
             }
-            i8_store4(A.out, (long)(row0 + row) * A.ldo + n, dt, whole, left, v);
+        }
+        return;
+    }
+    constexpr int kOut = 8 * S;                 // lanes to a row of the wavefront's 32 S sums
+    auto put = [&](int tf) {
+#pragma unroll
+        for (int s = 0; s < S; s++)
+#pragma unroll
+            for (int g = 0; g < 4; g++)
+                lds_write16(wr + (uint32_t)(s * 128 + g * 32), make_uint4((uint32_t)acc[s][tf][4 * g], (uint32_t)acc[s][tf][4 * g + 1],
+                                                                          (uint32_t)acc[s][tf][4 * g + 2], (uint32_t)acc[s][tf][4 * g + 3]));
+    };
+    if constexpr (MODE == kI8Up) {
+        // one strip a wavefront: wavefronts 0, 1 have W1's sums of 64 features, 2, 3 have W3's of the same
+        const int f = 4 * (lane & 15), n = 64 * bx + f, left = A.N - n;
+        float c1[4], c3[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            c1[i] = sa[min(n + i, A.N - 1)];
+            c3[i] = sb[min(n + i, A.N - 1)];
+        }
+#pragma unroll
+        for (int tf = 0; tf < NTF; tf++) {
+            put(tf);
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 2; j++) {
+                const int rr = 8 * wave + 4 * j + (lane >> 4), row = 32 * tf + rr;
+                const uint32_t from = xs_base + (uint32_t)(f >> 5) * kI8EpiWave<S> + (uint32_t)rr * kI8EpiRow<S> + (uint32_t)(f & 31) * 4u;
+                const uint4 a = lds_read16(from), u = lds_read16(from + 2 * kI8EpiWave<S>);
+                if (row >= rows || left <= 0) continue;
+                const float xs = A.xs[perm[row0 + row] / A.k];
+                const uint32_t av[4] = {a.x, a.y, a.z, a.w}, uv[4] = {u.x, u.y, u.z, u.w};
+                float v[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++) v[i] = silu_times((float)(int)av[i] * xs * c1[i], (float)(int)uv[i] * xs * c3[i]);
+                i8_store4(A.out, (long)(row0 + row) * A.ldo + n, dt, left >= 4, left, v);
+            }
+            __syncthreads();
+        }
+    } else {
+        const int n = (4 * bx + wave) * 32 * S + 4 * (lane & (kOut - 1)), left = A.N - n;
+        float sc[4], add[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            sc[i] = sa[min(n + i, A.N - 1)];
+            if (MODE == kI8Plain && A.bias) add[i] = A.bias[min(n + i, A.N - 1)];
+        }
+#pragma unroll
+        for (int tf = 0; tf < NTF; tf++) {
+            put(tf);
+            // (a wavefront's LDS accesses execute in order and the area is its own: no barrier)
+#pragma unroll
+            for (int j = 0; j < 32 * kOut / 64; j++) {
+                const int rr = lane / kOut + 64 / kOut * j, row = 32 * tf + rr;
+                const uint4 u = lds_read16(area + (uint32_t)rr * kI8EpiRow<S> + (uint32_t)(lane & (kOut - 1)) * 16u);
+                if (row >= rows || left <= 0) continue;
+                const float xs = A.xs[row0 + row];
+                const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
+                float v[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++) v[i] = (float)(int)w4[i] * xs * sc[i] + add[i];
+                i8_store4(A.out, (long)(row0 + row) * A.ldo + n, dt, left >= 4 && vec, left, v);
+            }
         }
     }
 }
 
-// MAXF: fragments of 32 rows a tile may have
-template <int MODE, int MAXF>
-__global__ __launch_bounds__(256, MAXF == 4 ? 2 : 1) void i8_gemm_kernel(const I8Args A)
+constexpr int kI8Run = 16;      // neighbouring units that an XCD takes at a time
+
+// columns of a workgroup's block
+template <int MODE, int S>
+constexpr int kI8Cols = (MODE == kI8Up ? 64 : 128) * S;
+
+template <int MODE, int S, int KT>
+__global__ __launch_bounds__(256, S == 2 ? 2 : 4) void i8_gemm_kernel(const I8Args A)
 {
     extern __shared__ __attribute__((aligned(1024))) char xs_raw[];
     const uint32_t xs = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)xs_raw;
-    constexpr uint32_t kBuf = 32u * MAXF * kI8Step;
+    constexpr uint32_t kBuf = (uint32_t)kI8TileRows * 128 * KT;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const I8Plan pp = i8_plan(const_cast<int32_t*>(A.plan), A.E, A.P);
-    const int cols = MODE == kI8Up ? 128 : 256;
+    constexpr int cols = kI8Cols<MODE, S>;
     const int nblk = (A.N + cols - 1) / cols;
-    const int tiles = MODE == kI8Plain ? (A.rows + 32 * MAXF - 1) / (32 * MAXF) : pp.meta[0];
-    // Workgroups go to the 8 XCDs, each with an L2 of its own, in turn: XCD c takes the c-th of eight runs of neighbouring units, a column
-    // block's (plain product) or an expert's (grouped) tiles next to each other.
+    const int tiles = MODE == kI8Plain ? (A.rows + kI8TileRows - 1) / kI8TileRows : pp.meta[0];
+    // Workgroups go to the 8 XCDs, each with an L2 of its own, in turn.  A unit is a tile and a column block; units that read the same weights
+    // (the tiles of a matrix or expert, for one column block) are neighbours, and an XCD takes runs of neighbours.
     const long total = (long)tiles * nblk;
-    const long per = (total + 7) / 8;
-    const long unit = (long)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if ((long)(blockIdx.x >> 3) >= per || unit >= total) return;
-    int tile, bx;
-    if (MODE == kI8Plain) {
-        bx = (int)(unit / tiles);
-        tile = (int)(unit - (long)bx * tiles);
-    } else {
-        tile = (int)(unit / nblk);
-        bx = (int)(unit - (long)tile * nblk);
-    }
-    int row0, rows;
-    const char *qa, *qb;
+    const int c = blockIdx.x & 7, j = blockIdx.x >> 3;
+    const long unit = ((long)(j / kI8Run) * 8 + c) * kI8Run + j % kI8Run;
+    if (unit >= total) return;
+    int row0, rows, bx;
+    const char* qw[S];
     const float *sa, *sb;
     const long strip = 32L * A.Kp, last = (A.N + 31) / 32 - 1;
-    const long na = MODE == kI8Up ? 4L * bx + wave : 8L * bx + 2 * wave;
-    const long oa = min(na, last) * strip, ob = min(MODE == kI8Up ? na : na + 1, last) * strip;      // strips behind the last re-read it
+    auto strip_at = [&](const void* q, long nt) { return (const char*)q + min(nt, last) * strip; };    // strips behind the last re-read it
     if (MODE == kI8Plain) {
-        row0 = tile * 32 * MAXF;
-        rows = min(32 * MAXF, A.rows - row0);
-        qa = A.w.q + oa;
-        qb = A.w.q + ob;
+        bx = (int)(unit / tiles);
+        row0 = (int)(unit - (long)bx * tiles) * kI8TileRows;
+        rows = min(kI8TileRows, A.rows - row0);
+#pragma unroll
+        for (int s = 0; s < S; s++) qw[s] = strip_at(A.w.q, (4L * bx + wave) * S + s);
         sa = sb = A.w.s;
     } else {
-        const int e = pp.tiles[4 * tile];
-        row0 = pp.tiles[4 * tile + 1];
-        rows = pp.tiles[4 * tile + 2];
+        const int32_t* const t = pp.tiles + 8 * (unit / nblk);
+        const int e = t[0], n = t[2], m = t[4];
+        const long local = unit - (long)t[3] * nblk;
+        bx = (int)(local / m);
+        const int i = (int)(local - (long)bx * m) * kI8TileRows;
+        row0 = t[1] + i;
+        rows = min(kI8TileRows, n - i);
         const dymoe_expert_i8 ex = A.table[e];
-        qa = (const char*)ex.q[MODE == kI8Up ? 0 : 2] + oa;
-        qb = (const char*)ex.q[MODE == kI8Up ? 1 : 2] + ob;
-        sa = ex.s[MODE == kI8Up ? 0 : 2];
-        sb = ex.s[MODE == kI8Up ? 1 : 2];
+        if (MODE == kI8Up) {
+            sa = ex.s[0];
+            sb = ex.s[1];
+            if constexpr (S == 2) {
+                qw[0] = strip_at(ex.q[0], 4L * bx + wave);
+                qw[S - 1] = strip_at(ex.q[1], 4L * bx + wave);
+            } else {
+                qw[0] = strip_at(wave < 2 ? ex.q[0] : ex.q[1], 2L * bx + (wave & 1));
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < S; s++) qw[s] = strip_at(ex.q[2], (4L * bx + wave) * S + s);
+            sa = sb = ex.s[2];
+        }
     }
-#define DYMOE_I8_TILE(NTF) i8_tile<MODE, NTF>(A, pp.perm, qa, qb, sa, sb, row0, rows, bx, xs, kBuf)
-    const int ntf = (rows + 31) >> 5;
-    if constexpr (MAXF == 4) {
-        switch (ntf) {
-        case 1: DYMOE_I8_TILE(1); break;
-        case 2: DYMOE_I8_TILE(2); break;
-        case 3: DYMOE_I8_TILE(3); break;
-        default: DYMOE_I8_TILE(4); break;
-        }
-    } else {
-        switch (ntf) {
-        case 1: DYMOE_I8_TILE(1); break;
-        case 2: DYMOE_I8_TILE(2); break;
-        case 3: DYMOE_I8_TILE(3); break;
-        case 4: DYMOE_I8_TILE(4); break;
-        case 5: DYMOE_I8_TILE(5); break;
-        case 6: DYMOE_I8_TILE(6); break;
-        case 7: DYMOE_I8_TILE(7); break;
-        default: DYMOE_I8_TILE(8); break;
-        }
+#define DYMOE_I8_TILE(NTF) i8_tile<MODE, NTF, S, KT>(A, pp.perm, qw, sa, sb, row0, rows, bx, xs, kBuf)
+    // one instantiation per number of fragments of 32 rows: the accumulators then sit in fixed registers for the whole loop
+    switch ((rows + 31) >> 5) {
+    case 1: DYMOE_I8_TILE(1); break;
+    case 2: DYMOE_I8_TILE(2); break;
+    case 3: DYMOE_I8_TILE(3); break;
+    default: DYMOE_I8_TILE(4); break;
     }
 #undef DYMOE_I8_TILE
 }
 
-template <int MODE, int MAXF>
-static int i8_allow_lds()
-{
-    return hipFuncSetAttribute((const void*)i8_gemm_kernel<MODE, MAXF>, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * 32 * MAXF * kI8Step) == hipSuccess
-               ? DYMOE_OK : DYMOE_EHIP;
-}
+template <int S, int KT>
+constexpr int kI8Lds = 2 * kI8TileRows * 128 * KT;
 
 // per-device set-up, with the device current
 int i8_init()
 {
-    const int rc[6] = {i8_allow_lds<kI8Plain, 4>(), i8_allow_lds<kI8Up, 4>(), i8_allow_lds<kI8Down, 4>(),
-                       i8_allow_lds<kI8Plain, 8>(), i8_allow_lds<kI8Up, 8>(), i8_allow_lds<kI8Down, 8>()};
-    for (int r : rc)
-        if (r != DYMOE_OK) return r;
-    const void* const thin[3] = {(const void*)i8_thin_kernel<kI8Plain, true>, (const void*)i8_thin_kernel<kI8Up, true>, (const void*)i8_thin_down_kernel};
-    for (const void* f : thin)
-        if (hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kI8FuseBytes) != hipSuccess) return DYMOE_EHIP;
-    return DYMOE_OK;
+    auto allow = [](const void* f, int bytes) { return hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess; };
+    bool ok = allow((const void*)i8_gemm_kernel<kI8Plain, 2, 2>, kI8Lds<2, 2>) && allow((const void*)i8_gemm_kernel<kI8Up, 2, 2>, kI8Lds<2, 2>) &&
+              allow((const void*)i8_gemm_kernel<kI8Down, 2, 2>, kI8Lds<2, 2>);
+    ok = ok && allow((const void*)i8_thin_kernel<kI8Plain, true>, (int)kI8FuseBytes) && allow((const void*)i8_thin_kernel<kI8Up, true>, (int)kI8FuseBytes) &&
+         allow((const void*)i8_thin_down_kernel, (int)kI8FuseBytes);
+    return ok ? DYMOE_OK : DYMOE_EHIP;
 }
 
-// units: (tiles, column blocks) pairs at most
+// tiles: their number, or the most there can be
 template <int MODE>
-static void i8_gemm_launch(dymoe_ctx* ctx, int id, int maxf, long units, hipStream_t st, const I8Args& A)
+static void i8_gemm_launch(dymoe_ctx* ctx, int id, int strips, long tiles, hipStream_t st, const I8Args& A)
 {
-    const dim3 grid((unsigned)(8 * ((units + 7) / 8)));
-    if (maxf == 4) dymoe_launch(ctx, id, i8_gemm_kernel<MODE, 4>, grid, dim3(256), 2 * 32 * 4 * kI8Step, st, A);
-    else dymoe_launch(ctx, id, i8_gemm_kernel<MODE, 8>, grid, dim3(256), 2 * 32 * 8 * kI8Step, st, A);
+    const int cols = strips == 2 ? kI8Cols<MODE, 2> : kI8Cols<MODE, 1>;
+    const long units = tiles * ((A.N + cols - 1) / cols), run = 8 * kI8Run;
+    const dim3 grid((unsigned)((units + run - 1) / run * run));
+    if (strips == 2) dymoe_launch(ctx, id, i8_gemm_kernel<MODE, 2, 2>, grid, dim3(256), kI8Lds<2, 2>, st, A);
+    else dymoe_launch(ctx, id, i8_gemm_kernel<MODE, 1, 1>, grid, dim3(256), kI8Lds<1, 1>, st, A);
 }
 
 // y[t] = sum over the slots, in their order, of gate times the pair's output
@@ -887,8 +952,8 @@ extern "C" int dymoe_matmul_int8(dymoe_ctx* ctx, const void* x, int x_dtype, con
     }
     A.aligned = dymoe_aligned(y, 4 * dtype_bytes(out_dtype)) && ldy % 4 == 0;
     if (T > 32) {
-        const int maxf = 4;
-        i8_gemm_launch<kI8Plain>(ctx, DYMOE_K_MATMUL_INT8, maxf, ((T + 32L * maxf - 1) / (32 * maxf)) * ((N + 255L) / 256), st, A);
+        const long tiles = (T + kI8TileRows - 1L) / kI8TileRows;
+        i8_gemm_launch<kI8Plain>(ctx, DYMOE_K_MATMUL_INT8, tiles * ((N + 255L) / 256) >= 2L * ctx->num_cu ? 2 : 1, tiles, st, A);
     } else {
         dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_small_kernel<kI8Plain>, dim3((unsigned)blocks), dim3(256), 0, st, A);
     }
@@ -917,8 +982,8 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     if ((long)T * k > 0x7fffffffL / 4 || (long)T * up_to(H, 128) > 0xffffffffL) return DYMOE_ENOTSUP;      // (32-bit offsets into the codes)
     const I8FfnLayout L = i8_ffn_layout(T, H, F, E, k);
     if (workspace_bytes < L.total) return DYMOE_ENOSPC;
-    const long up = (long)L.max_tiles * ((F + 31L) / 32), down = (long)L.max_tiles * ((H + 63L) / 64);
-    if (up > 0x7fffffffL || down > 0x7fffffffL || (long)T * ((H + 3) / 4) > 0x7fffffffL * 256L) return DYMOE_ENOTSUP;
+    const long up = (long)L.max_tiles * ((F + 31L) / 32), down = (long)L.max_tiles * ((H + 63L) / 64);      // workgroups at most
+    if (up > 0x7fff0000L || down > 0x7fff0000L || (long)T * ((H + 3) / 4) > 0x7fffffffL * 256L) return DYMOE_ENOTSUP;
     if (!ctx) return DYMOE_ENOCTX;
     if (T == 0) return DYMOE_OK;
     hipStream_t st = (hipStream_t)stream;
@@ -960,9 +1025,10 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     int rc = quantize_rows(ctx, x, x_dtype, T, H, H, 0, ws + L.xq, (float*)(ws + L.xs), st);
     if (rc != DYMOE_OK) return rc;
     int32_t* const plan = (int32_t*)(ws + L.plan);
-    const int maxf = T <= 32 || P <= 8L * E ? 1 : P <= 200L * E ? 8 : 4;
-    const long tiles = P / (32 * maxf) + (E < P ? E : P);
-    dymoe_launch(ctx, DYMOE_K_INT8_PLAN, i8_plan_kernel, dim3(1), dim3(kI8PlanThreads), 0, st, idx, table, P, E, 32 * maxf, plan,
+    const bool small = T <= 32 || P <= 8L * E;
+    const int tile_rows = small ? kI8TileSmall : kI8TileRows, strips = P <= 200L * E ? 1 : 2;
+    const long tiles = P / tile_rows + (E < P ? E : P);
+    dymoe_launch(ctx, DYMOE_K_INT8_PLAN, i8_plan_kernel, dim3(1), dim3(kI8PlanThreads), 0, st, idx, table, P, E, tile_rows, plan,
                  ctx->device_flags);
     I8Args A = {};
     A.x = ws + L.xq;
@@ -976,8 +1042,8 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     A.N = F;
     A.E = E;
     A.k = k;
-    if (maxf == 1) dymoe_launch(ctx, DYMOE_K_INT8_UP, i8_small_kernel<kI8Up>, dim3((unsigned)up), dim3(256), 0, st, A);
-    else i8_gemm_launch<kI8Up>(ctx, DYMOE_K_INT8_UP, maxf, tiles * ((F + 127L) / 128), st, A);
+    if (small) dymoe_launch(ctx, DYMOE_K_INT8_UP, i8_small_kernel<kI8Up>, dim3((unsigned)up), dim3(256), 0, st, A);
+    else i8_gemm_launch<kI8Up>(ctx, DYMOE_K_INT8_UP, strips, tiles, st, A);
     rc = quantize_rows(ctx, ws + L.h, DYMOE_OUT_F32, P, F, (long)L.Fp, 0, ws + L.hq, (float*)(ws + L.hs), st);
     if (rc != DYMOE_OK) return rc;
     A.x = ws + L.hq;
@@ -986,8 +1052,8 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     A.ldo = (long)L.Hp;
     A.Kp = (int)L.Fp;
     A.N = H;
-    if (maxf == 1) dymoe_launch(ctx, DYMOE_K_INT8_DOWN, i8_small_kernel<kI8Down>, dim3((unsigned)down), dim3(256), 0, st, A);
-    else i8_gemm_launch<kI8Down>(ctx, DYMOE_K_INT8_DOWN, maxf, tiles * ((H + 255L) / 256), st, A);
+    if (small) dymoe_launch(ctx, DYMOE_K_INT8_DOWN, i8_small_kernel<kI8Down>, dim3((unsigned)down), dim3(256), 0, st, A);
+    else i8_gemm_launch<kI8Down>(ctx, DYMOE_K_INT8_DOWN, strips, tiles, st, A);
     const long items = (long)T * ((H + 3) / 4);
     dymoe_launch(ctx, DYMOE_K_INT8_COMBINE, i8_combine_kernel, dim3((unsigned)((items + 255) / 256)), dim3(256), 0, st,
                  (const float*)(ws + L.part), (long)L.Hp, i8_plan(plan, E, P).where, w, T, H, k, out_dtype, y);

@@ -36,7 +36,7 @@ static inline I8FfnLayout i8_ffn_layout(long T, long H, long F, long E, long k)
     L.hq = take(P * L.Fp);
     L.hs = take(P * 4);
     L.part = take(P * L.Hp * 4);
-    L.plan = take(((size_t)E + 1 + 8 + 2 * P + 4 * (size_t)L.max_tiles) * 4);
+    L.plan = take((8 + 2 * P + 8 * (size_t)L.max_tiles) * 4);
     L.total = at;
     return L;
 }
