@@ -5,6 +5,8 @@
 // the same bits.
 #include <float.h>
 
+#include <type_traits>
+
 #include "int8_device.hpp"
 #include "int8_layout.hpp"
 
@@ -143,6 +145,22 @@ struct I8Args {
     int rows, Kp, N, E, k, out_dtype, aligned;     // aligned: the plain product's rows start where four outputs may be stored at once
 };
 
+// Memory that a wavefront's loads share a base in: the base in scalar registers, a lane's offset and the load's own in 32 bits each.
+struct I8Src {
+    __amdgpu_buffer_rsrc_t r;
+
+    __device__ __forceinline__ void set(const void* p, uint32_t bytes)
+    {
+        const uint64_t u = (uint64_t)p;
+        const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)u), hi = __builtin_amdgcn_readfirstlane((int)(uint32_t)(u >> 32));
+        r = __builtin_amdgcn_make_buffer_rsrc((void*)(((uint64_t)hi << 32) | lo), 0, (int)bytes, 0x00020000);
+    }
+    __device__ __forceinline__ uint4 load(uint32_t lane, uint32_t all) const
+    {
+        return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)lane, (int)all, 0));
+    }
+};
+
 enum { kI8Plain = 0, kI8Up = 1, kI8Down = 2 };
 
 __device__ __forceinline__ i32x16_t mfma_i8(const uint4 a, const uint4 b, const i32x16_t c)
@@ -271,8 +289,8 @@ __device__ __forceinline__ i32x4acc_t mfma16_i8(const uint4 a, const uint4 b, co
 template <int S>
 struct I8Thin {
     uint4 w[kI8Ahead][S][2];
-    const char* q[S];          // the strips' tiles, at the sixteen rows' half
-    uint32_t off;              // this lane's 16 bytes of the first product
+    I8Src q[S];                // the strips
+    uint32_t off;              // this lane's 16 bytes of the first product, in the sixteen rows' half of the strip
     int kt, nkt, by;           // next tile to multiply, tiles, distance of this wavefront's tiles
 
     __device__ __forceinline__ void load(int d, int tile)
@@ -280,14 +298,14 @@ struct I8Thin {
 #pragma unroll
         for (int s = 0; s < S; s++)
 #pragma unroll
-            for (int j = 0; j < 2; j++) w[d][s][j] = load_global<uint4>(q[s] + (long)tile * 4096 + j * 2048 + off);
+            for (int j = 0; j < 2; j++) w[d][s][j] = q[s].load(off + (uint32_t)(j * 2048), (uint32_t)tile * 4096u);
     }
-    __device__ __forceinline__ void start(int first, int tiles, int stride, int lane)
+    __device__ __forceinline__ void start(int first, int tiles, int stride, int half, int lane)
     {
         kt = first;
         nkt = tiles;
         by = stride;
-        off = (uint32_t)((lane >> 4 & 1) * 1024 + (lane >> 5) * 512 + (lane & 15) * 16);
+        off = (uint32_t)((lane >> 4 & 1) * 1024 + (lane >> 5) * 512 + half * 256 + (lane & 15) * 16);
 #pragma unroll
         for (int d = 0; d < kI8Ahead; d++)
             if (kt + d * by < nkt) load(d, kt + d * by);
@@ -377,9 +395,10 @@ __global__ __launch_bounds__(64 * kI8ThinWaves) void i8_thin_kernel(const I8Thin
     int rows = A.rows, mine = min(ln, A.rows - 1);          // this lane's row: a token of the plain product, a pair of the experts
     const float *sa, *sb;
     I8Thin<S> thin;
-    const long strip = (long)(bx >> 1) * 32 * A.Kp + (bx & 1) * 256;
+    const long strip = (long)(bx >> 1) * 32 * A.Kp;
+    const uint32_t bytes = 32u * (uint32_t)A.Kp;
     if (MODE == kI8Plain) {
-        thin.q[0] = A.w.q + strip;
+        thin.q[0].set(A.w.q + strip, bytes);
         sa = sb = A.w.s;
     } else {
         const int my_e = lane < A.P ? A.idx[lane] : -1;
@@ -398,13 +417,13 @@ __global__ __launch_bounds__(64 * kI8ThinWaves) void i8_thin_kernel(const I8Thin
         const int want = min(ln, rows - 1);
         for (int i = 0; i < want; i++) left &= left - 1;
         mine = __builtin_ctzll(left);
-        thin.q[0] = (const char*)ex.q[0] + strip;
-        thin.q[S - 1] = (const char*)ex.q[S - 1] + strip;
+        thin.q[0].set((const char*)ex.q[0] + strip, bytes);
+        thin.q[S - 1].set((const char*)ex.q[S - 1] + strip, bytes);
         sa = ex.s[0];
         sb = ex.s[1];
     }
     const int nkt = A.Kp >> 7;
-    thin.start(wave, nkt, kI8ThinWaves, lane);
+    thin.start(wave, nkt, kI8ThinWaves, bx & 1, lane);
     const int token = MODE == kI8Up ? mine / A.k : mine;
     i32x4acc_t acc[S] = {};
     if constexpr (FUSE) {
@@ -458,7 +477,8 @@ __global__ __launch_bounds__(64 * kI8LastWaves) void i8_thin_down_kernel(const I
     const int t = j % A.rows, bx = j / A.rows * 8 + (blockIdx.x & 7);
     if (bx >= nblk) return;
     const int k = A.k, seg = max(1, kI8LastWaves / k), units = k * seg;
-    const long strip = (long)(bx >> 1) * 32 * A.Kp + (bx & 1) * 256;
+    const long strip = (long)(bx >> 1) * 32 * A.Kp;
+    const uint32_t bytes = 32u * (uint32_t)A.Kp;
     const int nkt = A.Kp >> 7;
     I8Thin<1> thin;
     bool ok = false;
@@ -468,9 +488,9 @@ __global__ __launch_bounds__(64 * kI8LastWaves) void i8_thin_down_kernel(const I
         if (ok) {
             const dymoe_expert_i8 ex = A.table[e];
             ok = i8_present(ex);
-            thin.q[0] = (const char*)ex.q[2] + strip;
+            thin.q[0].set((const char*)ex.q[2] + strip, bytes);
         }
-        if (ok) thin.start(u % seg, nkt, seg, lane);
+        if (ok) thin.start(u % seg, nkt, seg, bx & 1, lane);
     };
     if (wave < units) begin(wave);
     i8_rows_to_lds<DYMOE_OUT_F32>(A.x + (long)t * k * A.ldx, A.ldx, k, A.K, A.Kp, s_codes, s_scale, s_max);
@@ -520,10 +540,10 @@ struct I8Strips {
     uint4 r[S][4 * KT];       // chunk j = 4 * (tile of the step) + 16-byte chunk of the lane's half of that tile
 };
 
-// chunk c of a tile of the strip at p
-__device__ __forceinline__ uint4 i8_chunk(const char* p, uint32_t lane16, int tile, int c)
+// chunk c of a tile of a strip
+__device__ __forceinline__ uint4 i8_chunk(const I8Src& q, uint32_t lane16, int tile, int c)
 {
-    return load_global<uint4>(p + (long)tile * 4096 + c * 1024 + lane16);
+    return q.load(lane16 + (uint32_t)(c * 1024), (uint32_t)tile * 4096u);
 }
 
 template <int NTF, int KT>
@@ -540,7 +560,7 @@ struct I8Ops {
 
 // The first TILES tiles of a step.  The operands of the next pair of chunks are read while the products of this one are issued.
 template <int NTF, int S, int KT, int TILES>
-__device__ __forceinline__ void i8_step(I8Strips<S, KT>& w, const char* const (&q)[S], uint32_t lane16, int tile_next, int nkt, uint32_t xa,
+__device__ __forceinline__ void i8_step(I8Strips<S, KT>& w, const I8Src (&q)[S], uint32_t lane16, int tile_next, int nkt, uint32_t xa,
                                         i32x16_t (&acc)[S][NTF])
 {
     constexpr int kStepMask = 0x2 | 0x4;        // vector and scalar arithmetic may cross; products, LDS and memory accesses may not
@@ -600,64 +620,14 @@ __device__ __forceinline__ void i8_store4(void* out, long at, int dt, bool whole
         if (i < left) store_out(out, at + i, dt, v[i]);
 }
 
-// qw: this wavefront's strips; sa, sb: the scales of the matrices
-template <int MODE, int NTF, int S, int KT>
-__device__ __forceinline__ void i8_tile(const I8Args& A, const int32_t* perm, const char* const (&qw)[S], const float* sa, const float* sb,
-                                        int row0, int rows, int bx, uint32_t xs_base, uint32_t buf_bytes)
+// Epilogue.  A lane holds, of its token's row, four neighbouring outputs in each group of four registers; the wavefront turns a fragment
+// round in an LDS area of its own, so that a row leaves in whole lines.
+template <int MODE, int NTF, int S>
+__device__ __forceinline__ void i8_finish(const I8Args& A, const int32_t* perm, const i32x16_t (&acc)[S][NTF], const float* sa, const float* sb,
+                                          int row0, int rows, int bx, uint32_t xs_base)
 {
-    constexpr int kLanes = 8 * KT;              // lanes (16-byte chunks) to a row of a step
-    constexpr int kRowsWave = 64 / kLanes;      // rows that a wavefront's copy fills
-    constexpr uint32_t kRow = 128 * KT;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int ln = lane & 31, kb = lane >> 5;
-    const uint32_t lane16 = (uint32_t)lane * 16u;
-    i32x16_t acc[S][NTF] = {};
-    I8Stage<NTF, KT> stage;
-    const int rb = kRowsWave * wave + lane / kLanes;                         // (rows of a thread agree in r & mask)
-    const int chunk = (lane & (kLanes - 1)) ^ (rb & (kLanes - 1));
-#pragma unroll
-    for (int i = 0; i < I8Stage<NTF, KT>::kCopies; i++) {
-        const int r = min(4 * kRowsWave * i + rb, rows - 1);                 // rows behind the last: computed and dropped
-        const uint32_t src = MODE == kI8Up ? (uint32_t)(perm[row0 + r] / A.k) : (uint32_t)r;
-        stage.off[i] = src * (uint32_t)A.Kp + 16u * (uint32_t)chunk;          // below 4 GiB: checked by the launcher
-    }
-    stage.base = A.x + (MODE == kI8Up ? 0 : (long)row0 * A.Kp);
-    stage.lds = __builtin_amdgcn_readfirstlane(xs_base + (uint32_t)wave * 1024u);
-    const int nkt = A.Kp >> 7, steps = (nkt + KT - 1) / KT;
-    // (two tiles a step: the last step's second may lie behind the rows' end: its chunks are then those of the first, and go unused)
-    const uint32_t back = KT == 2 && (nkt & 1) && (chunk & 8) ? 128u : 0u;
-    auto copy = [&](int ks, uint32_t at) {
-        const char* const base = stage.base + (long)ks * kRow;
-        const uint32_t less = ks == steps - 1 ? back : 0u;
-#pragma unroll
-        for (int i = 0; i < I8Stage<NTF, KT>::kCopies; i++) lds_copy16(base, stage.off[i] - less, stage.lds + at + (uint32_t)i * 4096u);
-    };
-    const uint32_t xa0 = xs_base + (uint32_t)ln * kRow + (((uint32_t)kb << 6) ^ ((uint32_t)(ln & (kLanes - 1)) << 4));
-    I8Strips<S, KT> w;
-    copy(0, 0);
-#pragma unroll
-    for (int j = 0; j < 4 * KT; j++)
-#pragma unroll
-        for (int s = 0; s < S; s++) w.r[s][j] = i8_chunk(qw[s], lane16, min(j >> 2, nkt - 1), j & 3);
-    wait_lds_copies<0>();
-    __syncthreads();
-    uint32_t at = 0;
-    for (int ks = 0; ks < nkt / KT; ks++) {
-        copy(min(ks + 1, steps - 1), at ^ buf_bytes);
-        i8_step<NTF, S, KT, KT>(w, qw, lane16, KT * (ks + 1), nkt, xa0 + at, acc);
-        wait_lds_copies<4 * S * KT>();          // the copies are older than the loads of weights
-        __syncthreads();
-        at ^= buf_bytes;
-    }
-    if constexpr (KT == 2) {
-        if (nkt & 1) {
-            i8_step<NTF, S, KT, 1>(w, qw, lane16, nkt - 1, nkt, xa0 + at, acc);
-            __syncthreads();
-        }
-    }
-
-    // Epilogue.  A lane holds, of its token's row, four neighbouring outputs in each group of four registers; the wavefront turns a fragment
-    // round in an area of its own, so that a row leaves in whole lines.
     const uint32_t area = xs_base + (uint32_t)wave * kI8EpiWave<S>;
     const uint32_t wr = area + (uint32_t)ln * kI8EpiRow<S> + (uint32_t)kb * 16u;
     const bool vec = MODE != kI8Plain || A.aligned;
@@ -755,68 +725,234 @@ __device__ __forceinline__ void i8_tile(const I8Args& A, const int32_t* perm, co
     }
 }
 
+// qw: this wavefront's strips; sa, sb: the scales of the matrices
+template <int MODE, int NTF, int S, int KT>
+__device__ __forceinline__ void i8_tile(const I8Args& A, const int32_t* perm, const I8Src (&qw)[S], const float* sa, const float* sb,
+                                        int row0, int rows, int bx, uint32_t xs_base, uint32_t buf_bytes)
+{
+    constexpr int kLanes = 8 * KT;              // lanes (16-byte chunks) to a row of a step
+    constexpr int kRowsWave = 64 / kLanes;      // rows that a wavefront's copy fills
+    constexpr uint32_t kRow = 128 * KT;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int ln = lane & 31, kb = lane >> 5;
+    const uint32_t lane16 = (uint32_t)lane * 16u;
+    i32x16_t acc[S][NTF] = {};
+    I8Stage<NTF, KT> stage;
+    const int rb = kRowsWave * wave + lane / kLanes;                         // (rows of a thread agree in r & mask)
+    const int chunk = (lane & (kLanes - 1)) ^ (rb & (kLanes - 1));
+#pragma unroll
+    for (int i = 0; i < I8Stage<NTF, KT>::kCopies; i++) {
+        const int r = min(4 * kRowsWave * i + rb, rows - 1);                 // rows behind the last: computed and dropped
+        const uint32_t src = MODE == kI8Up ? (uint32_t)(perm[row0 + r] / A.k) : (uint32_t)r;
+        stage.off[i] = src * (uint32_t)A.Kp + 16u * (uint32_t)chunk;          // below 4 GiB: checked by the launcher
+    }
+    stage.base = A.x + (MODE == kI8Up ? 0 : (long)row0 * A.Kp);
+    stage.lds = __builtin_amdgcn_readfirstlane(xs_base + (uint32_t)wave * 1024u);
+    const int nkt = A.Kp >> 7, steps = (nkt + KT - 1) / KT;
+    // (two tiles a step: the last step's second may lie behind the rows' end: its chunks are then those of the first, and go unused)
+    const uint32_t back = KT == 2 && (nkt & 1) && (chunk & 8) ? 128u : 0u;
+    auto copy = [&](int ks, uint32_t at) {
+        const char* const base = stage.base + (long)ks * kRow;
+        const uint32_t less = ks == steps - 1 ? back : 0u;
+#pragma unroll
+        for (int i = 0; i < I8Stage<NTF, KT>::kCopies; i++) lds_copy16(base, stage.off[i] - less, stage.lds + at + (uint32_t)i * 4096u);
+    };
+    const uint32_t xa0 = xs_base + (uint32_t)ln * kRow + (((uint32_t)kb << 6) ^ ((uint32_t)(ln & (kLanes - 1)) << 4));
+    I8Strips<S, KT> w;
+    copy(0, 0);
+#pragma unroll
+    for (int j = 0; j < 4 * KT; j++)
+#pragma unroll
+        for (int s = 0; s < S; s++) w.r[s][j] = i8_chunk(qw[s], lane16, min(j >> 2, nkt - 1), j & 3);
+    wait_lds_copies<0>();
+    __syncthreads();
+    uint32_t at = 0;
+    for (int ks = 0; ks < nkt / KT; ks++) {
+        copy(min(ks + 1, steps - 1), at ^ buf_bytes);
+        i8_step<NTF, S, KT, KT>(w, qw, lane16, KT * (ks + 1), nkt, xa0 + at, acc);
+        wait_lds_copies<4 * S * KT>();          // the copies are older than the loads of weights
+        __syncthreads();
+        at ^= buf_bytes;
+    }
+    if constexpr (KT == 2) {
+        if (nkt & 1) {
+            i8_step<NTF, S, KT, 1>(w, qw, lane16, nkt - 1, nkt, xa0 + at, acc);
+            __syncthreads();
+        }
+    }
+
+    i8_finish<MODE, NTF, S>(A, perm, acc, sa, sb, row0, rows, bx, xs_base);
+}
+
+// Tiles of up to 160 rows for calls that the weights' bytes bound (experts that meet a few dozen tokens to some hundred): one strip a
+// wavefront, four tiles of weights on their way in registers, the rows' codes through registers into two LDS buffers.  Bytes on
+// their way are what sets the rate of such a stream; with the rows copied to LDS directly, as above, the loads of weights could run
+// ahead by one step only, because a count of outstanding loads that lets the copies through has to wait for all loads before them.
+constexpr int kI8Deep = 4;
+
+template <int MODE, int NTF>
+__device__ __forceinline__ void i8_wide_tile(const I8Args& A, const int32_t* perm, const I8Src& qw, const float* sa, const float* sb, int row0,
+                                             int rows, int bx, uint32_t xs_base)
+{
+    constexpr uint32_t kBuf = 32u * NTF * 128u;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int ln = lane & 31, kb = lane >> 5;
+    const uint32_t lane16 = (uint32_t)lane * 16u;
+    i32x16_t acc[1][NTF] = {};
+    const int rb = 8 * wave + (lane >> 3);
+    const uint32_t chunk = (uint32_t)((lane & 7) ^ (rb & 7)) * 16u;
+    uint32_t off[NTF];
+#pragma unroll
+    for (int i = 0; i < NTF; i++) {
+        const int r = min(32 * i + rb, rows - 1);                            // rows behind the last: computed and dropped
+        off[i] = (MODE == kI8Up ? (uint32_t)(perm[row0 + r] / A.k) : (uint32_t)r) * (uint32_t)A.Kp + chunk;
+    }
+    I8Src base;
+    base.set(A.x + (MODE == kI8Up ? 0 : (long)row0 * A.Kp), MODE == kI8Up ? (uint32_t)A.rows * (uint32_t)A.Kp : (uint32_t)rows * (uint32_t)A.Kp);
+    const int nkt = A.Kp >> 7;
+    uint4 w[kI8Deep][4], xr[2][NTF];
+    auto load_w = [&](uint4 (&to)[4], int tile, int c) { to[c] = i8_chunk(qw, lane16, min(tile, nkt - 1), c); };
+    auto load_x = [&](uint4 (&to)[NTF], int tile) {
+#pragma unroll
+        for (int i = 0; i < NTF; i++) to[i] = base.load(off[i], (uint32_t)min(tile, nkt - 1) * 128u);
+    };
+    auto put_x = [&](const uint4 (&from)[NTF], uint32_t buf) {
+#pragma unroll
+        for (int i = 0; i < NTF; i++) lds_write16(xs_base + buf + (uint32_t)(i * 4096 + wave * 1024) + lane16, from[i]);
+    };
+    load_x(xr[0], 0);
+#pragma unroll
+    for (int d = 0; d < kI8Deep; d++) {
+#pragma unroll
+        for (int c = 0; c < 4; c++) load_w(w[d], d, c);
+    }
+    load_x(xr[1], 1);
+    put_x(xr[0], 0);
+    load_x(xr[0], 2);
+    __syncthreads();
+    const uint32_t xa0 = xs_base + (uint32_t)ln * 128u + (((uint32_t)kb << 6) ^ ((uint32_t)(ln & 7) << 4));
+    constexpr int kMask = 0x2 | 0x4;             // vector and scalar arithmetic may cross; products, LDS and memory accesses may not
+    auto step = [&](int k, auto slot) __attribute__((always_inline)) {
+        constexpr int d = slot(), odd = d & 1;   // k % 4, k % 2
+        put_x(xr[odd ^ 1], odd ? 0u : kBuf);
+        load_x(xr[odd ^ 1], k + 3);
+        __builtin_amdgcn_sched_barrier(kMask);
+        const uint32_t xa = xa0 + (odd ? kBuf : 0u);
+        I8Ops ops;
+        ops.t0 = lds_read16(xa);
+        ops.t1 = lds_read16(xa ^ 16u);
+#pragma unroll
+        for (int jj = 0; jj < 2; jj++) {
+#pragma unroll
+            for (int tf = 0; tf < NTF; tf++) {
+                const bool wrap = tf == NTF - 1, last = wrap && jj == 1;
+                I8Ops nxt = ops;
+                if (!last) {
+                    const uint32_t at = (xa ^ (uint32_t)((wrap ? jj + 1 : jj) << 5)) + (uint32_t)(wrap ? 0 : tf + 1) * 4096u;
+                    nxt.t0 = lds_read16(at);
+                    nxt.t1 = lds_read16(at ^ 16u);
+                }
+                __builtin_amdgcn_sched_barrier(kMask);
+                acc[0][tf] = mfma_i8(w[d][2 * jj], ops.t0, acc[0][tf]);
+                acc[0][tf] = mfma_i8(w[d][2 * jj + 1], ops.t1, acc[0][tf]);
+                ops = nxt;
+                __builtin_amdgcn_sched_barrier(kMask);
+            }
+            load_w(w[d], k + kI8Deep, 2 * jj);
+            load_w(w[d], k + kI8Deep, 2 * jj + 1);
+            __builtin_amdgcn_sched_barrier(kMask);
+        }
+        __syncthreads();
+    };
+    int k = 0;
+    for (; k + 4 <= nkt; k += 4) {
+        step(k, std::integral_constant<int, 0>());
+        step(k + 1, std::integral_constant<int, 1>());
+        step(k + 2, std::integral_constant<int, 2>());
+        step(k + 3, std::integral_constant<int, 3>());
+    }
+    if (k < nkt) step(k, std::integral_constant<int, 0>());
+    if (k + 1 < nkt) step(k + 1, std::integral_constant<int, 1>());
+    if (k + 2 < nkt) step(k + 2, std::integral_constant<int, 2>());
+    i8_finish<MODE, NTF, 1>(A, perm, acc, sa, sb, row0, rows, bx, xs_base);
+}
+
 constexpr int kI8Run = 16;      // neighbouring units that an XCD takes at a time
 
 // columns of a workgroup's block
 template <int MODE, int S>
 constexpr int kI8Cols = (MODE == kI8Up ? 64 : 128) * S;
 
+template <int S>
+struct I8Unit {
+    I8Src qw[S];              // this wavefront's strips
+    const float *sa, *sb;     // the matrices' scales
+    int row0, rows, bx;
+};
+
+// The unit of a workgroup; false: none.  Workgroups go to the 8 XCDs, each with an L2 of its own, in turn.  A unit is a tile and a column
+// block; units that read the same weights (the tiles of a matrix or expert, for one column block) are neighbours, and an XCD takes runs
+// of neighbours.
+template <int MODE, int S, int ROWS>
+__device__ __forceinline__ bool i8_unit(const I8Args& A, const I8Plan& pp, I8Unit<S>& u)
+{
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    constexpr int cols = kI8Cols<MODE, S>;
+    const int nblk = (A.N + cols - 1) / cols;
+    const int tiles = MODE == kI8Plain ? (A.rows + ROWS - 1) / ROWS : pp.meta[0];
+    const long total = (long)tiles * nblk;
+    const int c = blockIdx.x & 7, j = blockIdx.x >> 3;
+    const long unit = ((long)(j / kI8Run) * 8 + c) * kI8Run + j % kI8Run;
+    if (unit >= total) return false;
+    const long strip = 32L * A.Kp, last = (A.N + 31) / 32 - 1;
+    auto strip_at = [&](I8Src& to, const void* q, long nt) { to.set((const char*)q + min(nt, last) * strip, (uint32_t)strip); };    // strips behind the last re-read it
+    if (MODE == kI8Plain) {
+        u.bx = (int)(unit / tiles);
+        u.row0 = (int)(unit - (long)u.bx * tiles) * ROWS;
+        u.rows = min(ROWS, A.rows - u.row0);
+#pragma unroll
+        for (int s = 0; s < S; s++) strip_at(u.qw[s], A.w.q, (4L * u.bx + wave) * S + s);
+        u.sa = u.sb = A.w.s;
+        return true;
+    }
+    const int32_t* const t = pp.tiles + 8 * (unit / nblk);
+    const int e = t[0], n = t[2], m = t[4];
+    const long local = unit - (long)t[3] * nblk;
+    u.bx = (int)(local / m);
+    const int i = (int)(local - (long)u.bx * m) * ROWS;
+    u.row0 = t[1] + i;
+    u.rows = min(ROWS, n - i);
+    const dymoe_expert_i8 ex = A.table[e];
+    if (MODE == kI8Up) {
+        u.sa = ex.s[0];
+        u.sb = ex.s[1];
+        if constexpr (S == 2) {
+            strip_at(u.qw[0], ex.q[0], 4L * u.bx + wave);
+            strip_at(u.qw[S - 1], ex.q[1], 4L * u.bx + wave);
+        } else {
+            strip_at(u.qw[0], wave < 2 ? ex.q[0] : ex.q[1], 2L * u.bx + (wave & 1));
+        }
+    } else {
+#pragma unroll
+        for (int s = 0; s < S; s++) strip_at(u.qw[s], ex.q[2], (4L * u.bx + wave) * S + s);
+        u.sa = u.sb = ex.s[2];
+    }
+    return true;
+}
+
+__device__ __forceinline__ uint32_t lds_base(char* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)p; }
+
 template <int MODE, int S, int KT>
 __global__ __launch_bounds__(256, S == 2 ? 2 : 4) void i8_gemm_kernel(const I8Args A)
 {
     extern __shared__ __attribute__((aligned(1024))) char xs_raw[];
-    const uint32_t xs = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)xs_raw;
     constexpr uint32_t kBuf = (uint32_t)kI8TileRows * 128 * KT;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const I8Plan pp = i8_plan(const_cast<int32_t*>(A.plan), A.E, A.P);
-    constexpr int cols = kI8Cols<MODE, S>;
-    const int nblk = (A.N + cols - 1) / cols;
-    const int tiles = MODE == kI8Plain ? (A.rows + kI8TileRows - 1) / kI8TileRows : pp.meta[0];
-    // Workgroups go to the 8 XCDs, each with an L2 of its own, in turn.  A unit is a tile and a column block; units that read the same weights
-    // (the tiles of a matrix or expert, for one column block) are neighbours, and an XCD takes runs of neighbours.
-    const long total = (long)tiles * nblk;
-    const int c = blockIdx.x & 7, j = blockIdx.x >> 3;
-    const long unit = ((long)(j / kI8Run) * 8 + c) * kI8Run + j % kI8Run;
-    if (unit >= total) return;
-    int row0, rows, bx;
-    const char* qw[S];
-    const float *sa, *sb;
-    const long strip = 32L * A.Kp, last = (A.N + 31) / 32 - 1;
-    auto strip_at = [&](const void* q, long nt) { return (const char*)q + min(nt, last) * strip; };    // strips behind the last re-read it
-    if (MODE == kI8Plain) {
-        bx = (int)(unit / tiles);
-        row0 = (int)(unit - (long)bx * tiles) * kI8TileRows;
-        rows = min(kI8TileRows, A.rows - row0);
-#pragma unroll
-        for (int s = 0; s < S; s++) qw[s] = strip_at(A.w.q, (4L * bx + wave) * S + s);
-        sa = sb = A.w.s;
-    } else {
-        const int32_t* const t = pp.tiles + 8 * (unit / nblk);
-        const int e = t[0], n = t[2], m = t[4];
-        const long local = unit - (long)t[3] * nblk;
-        bx = (int)(local / m);
-        const int i = (int)(local - (long)bx * m) * kI8TileRows;
-        row0 = t[1] + i;
-        rows = min(kI8TileRows, n - i);
-        const dymoe_expert_i8 ex = A.table[e];
-        if (MODE == kI8Up) {
-            sa = ex.s[0];
-            sb = ex.s[1];
-            if constexpr (S == 2) {
-                qw[0] = strip_at(ex.q[0], 4L * bx + wave);
-                qw[S - 1] = strip_at(ex.q[1], 4L * bx + wave);
-            } else {
-                qw[0] = strip_at(wave < 2 ? ex.q[0] : ex.q[1], 2L * bx + (wave & 1));
-            }
-        } else {
-#pragma unroll
-            for (int s = 0; s < S; s++) qw[s] = strip_at(ex.q[2], (4L * bx + wave) * S + s);
-            sa = sb = ex.s[2];
-        }
-    }
-#define DYMOE_I8_TILE(NTF) i8_tile<MODE, NTF, S, KT>(A, pp.perm, qw, sa, sb, row0, rows, bx, xs, kBuf)
+    I8Unit<S> u;
+    if (!i8_unit<MODE, S, kI8TileRows>(A, pp, u)) return;
+#define DYMOE_I8_TILE(NTF) i8_tile<MODE, NTF, S, KT>(A, pp.perm, u.qw, u.sa, u.sb, u.row0, u.rows, u.bx, lds_base(xs_raw), kBuf)
     // one instantiation per number of fragments of 32 rows: the accumulators then sit in fixed registers for the whole loop
-    switch ((rows + 31) >> 5) {
+    switch ((u.rows + 31) >> 5) {
     case 1: DYMOE_I8_TILE(1); break;
     case 2: DYMOE_I8_TILE(2); break;
     case 3: DYMOE_I8_TILE(3); break;
@@ -824,6 +960,26 @@ __global__ __launch_bounds__(256, S == 2 ? 2 : 4) void i8_gemm_kernel(const I8Ar
     }
 #undef DYMOE_I8_TILE
 }
+
+template <int MODE>
+__global__ __launch_bounds__(256, 2) void i8_wide_kernel(const I8Args A)
+{
+    extern __shared__ __attribute__((aligned(1024))) char xs_raw[];
+    const I8Plan pp = i8_plan(const_cast<int32_t*>(A.plan), A.E, A.P);
+    I8Unit<1> u;
+    if (!i8_unit<MODE, 1, kI8TileWide>(A, pp, u)) return;
+#define DYMOE_I8_TILE(NTF) i8_wide_tile<MODE, NTF>(A, pp.perm, u.qw[0], u.sa, u.sb, u.row0, u.rows, u.bx, lds_base(xs_raw))
+    switch ((u.rows + 31) >> 5) {
+    case 1: DYMOE_I8_TILE(1); break;
+    case 2: DYMOE_I8_TILE(2); break;
+    case 3: DYMOE_I8_TILE(3); break;
+    case 4: DYMOE_I8_TILE(4); break;
+    default: DYMOE_I8_TILE(5); break;
+    }
+#undef DYMOE_I8_TILE
+}
+
+constexpr int kI8WideLds = 2 * kI8TileWide * 128;
 
 template <int S, int KT>
 constexpr int kI8Lds = 2 * kI8TileRows * 128 * KT;
@@ -839,7 +995,7 @@ int i8_init()
     return ok ? DYMOE_OK : DYMOE_EHIP;
 }
 
-// tiles: their number, or the most there can be
+// tiles: their number, or the most there can be; strips a wavefront: 2, 1, or 0 for the wide tiles
 template <int MODE>
 static void i8_gemm_launch(dymoe_ctx* ctx, int id, int strips, long tiles, hipStream_t st, const I8Args& A)
 {
@@ -847,7 +1003,8 @@ static void i8_gemm_launch(dymoe_ctx* ctx, int id, int strips, long tiles, hipSt
     const long units = tiles * ((A.N + cols - 1) / cols), run = 8 * kI8Run;
     const dim3 grid((unsigned)((units + run - 1) / run * run));
     if (strips == 2) dymoe_launch(ctx, id, i8_gemm_kernel<MODE, 2, 2>, grid, dim3(256), kI8Lds<2, 2>, st, A);
-    else dymoe_launch(ctx, id, i8_gemm_kernel<MODE, 1, 1>, grid, dim3(256), kI8Lds<1, 1>, st, A);
+    else if (strips == 1) dymoe_launch(ctx, id, i8_gemm_kernel<MODE, 1, 1>, grid, dim3(256), kI8Lds<1, 1>, st, A);
+    else dymoe_launch(ctx, id, i8_wide_kernel<MODE>, grid, dim3(256), kI8WideLds, st, A);
 }
 
 // y[t] = sum over the slots, in their order, of gate times the pair's output
@@ -1026,7 +1183,8 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     if (rc != DYMOE_OK) return rc;
     int32_t* const plan = (int32_t*)(ws + L.plan);
     const bool small = T <= 32 || P <= 8L * E;
-    const int tile_rows = small ? kI8TileSmall : kI8TileRows, strips = P <= 200L * E ? 1 : 2;
+    const int strips = P <= 200L * E ? 0 : 2;
+    const int tile_rows = small ? kI8TileSmall : strips == 0 ? kI8TileWide : kI8TileRows;
     const long tiles = P / tile_rows + (E < P ? E : P);
     dymoe_launch(ctx, DYMOE_K_INT8_PLAN, i8_plan_kernel, dim3(1), dim3(kI8PlanThreads), 0, st, idx, table, P, E, tile_rows, plan,
                  ctx->device_flags);
@@ -1042,6 +1200,7 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     A.N = F;
     A.E = E;
     A.k = k;
+    A.rows = T;
     if (small) dymoe_launch(ctx, DYMOE_K_INT8_UP, i8_small_kernel<kI8Up>, dim3((unsigned)up), dim3(256), 0, st, A);
     else i8_gemm_launch<kI8Up>(ctx, DYMOE_K_INT8_UP, strips, tiles, st, A);
     rc = quantize_rows(ctx, ws + L.h, DYMOE_OUT_F32, P, F, (long)L.Fp, 0, ws + L.hq, (float*)(ws + L.hs), st);

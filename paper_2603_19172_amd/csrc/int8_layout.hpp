@@ -6,6 +6,7 @@
 namespace dymoe {
 
 constexpr int kI8TileRows = 128;      // token rows of a tile of the grouped products
+constexpr int kI8TileWide = 160;      // of a tile where the weights' bytes bound the call
 constexpr int kI8TileSmall = 32;      // of a tile where experts meet few tokens: one fragment
 
 static inline size_t i8_round(size_t v, size_t m) { return (v + m - 1) / m * m; }
