@@ -15,7 +15,7 @@ namespace dymoe {
 int quantize_rows(dymoe_ctx* ctx, const void* x, int dtype, long rows, long K, long ldx, int tiles, void* codes, float* scale, hipStream_t st);
 
 struct I8Plan {
-    int32_t* meta;        // [8]: tiles
+    int32_t* meta;        // [8]: tiles, wide tiles behind them
     int32_t* perm;        // [P] position -> pair
     int32_t* where;       // [P] pair -> position, -1: left out
     int32_t* tiles;       // [8 max_tiles]: the tile's expert, its first position, its pairs, its first tile, its tiles (3 unused)
@@ -45,7 +45,7 @@ constexpr int kI8PlanThreads = 1024;
 constexpr int kI8PlanKeep = 16;
 
 __global__ __launch_bounds__(kI8PlanThreads) void i8_plan_kernel(const int32_t* __restrict__ idx, const dymoe_expert_i8* __restrict__ table,
-                                                                 long P, int E, int tile_rows, int32_t* __restrict__ plan,
+                                                                 long P, int E, int small, int32_t* __restrict__ plan,
                                                                  unsigned* __restrict__ flags)
 {
     __shared__ int s_count[DYMOE_MAX_EXPERTS], s_sorted[DYMOE_MAX_EXPERTS], s_at[DYMOE_MAX_EXPERTS], s_wave[2][kI8PlanThreads / kWave];
@@ -86,7 +86,8 @@ __global__ __launch_bounds__(kI8PlanThreads) void i8_plan_kernel(const int32_t* 
     __syncthreads();
     const int e = tid < E ? s_sorted[tid] : 0;
     n = tid < E ? s_at[e] : 0;
-    const int m = (n + tile_rows - 1) / tile_rows;
+    const bool one = !small && n <= kI8TileWide;             // a wide tile
+    const int rows = small ? kI8TileSmall : one ? kI8TileWide : kI8TileRows, m = (n + rows - 1) / rows;
     const int n_in = wave_scan_dpp_i32(n), t_in = wave_scan_dpp_i32(m);
     if (lane == kWave - 1) {
         s_wave[0][wave] = n_in;
@@ -109,7 +110,12 @@ __global__ __launch_bounds__(kI8PlanThreads) void i8_plan_kernel(const int32_t* 
             t[4] = m;
         }
     }
-    if (tid == kI8PlanThreads - 1) pp.meta[0] = t0 + m;
+    // (experts come by falling load: those of one wide tile are the last)
+    const int wide = __syncthreads_count(one && n > 0);
+    if (tid == kI8PlanThreads - 1) {
+        pp.meta[0] = t0 + m - wide;
+        pp.meta[1] = wide;
+    }
     __syncthreads();
     auto place = [&](long p, int x, int rank) {
         int at = -1;
@@ -141,6 +147,8 @@ struct I8Args {
     I8Mat w;                          // the plain product
     const float* bias;
     void* out;
+    float* strip_scale;               // down projection with 16-bit outputs: [E][strips of 32 outputs]; null: 32-bit ones
+    float sum_scale;                  // largest sum there can be -> 2^15
     long ldo, P;
     int rows, Kp, N, E, k, out_dtype, aligned;     // aligned: the plain product's rows start where four outputs may be stored at once
 };
@@ -155,9 +163,11 @@ struct I8Src {
         const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)u), hi = __builtin_amdgcn_readfirstlane((int)(uint32_t)(u >> 32));
         r = __builtin_amdgcn_make_buffer_rsrc((void*)(((uint64_t)hi << 32) | lo), 0, (int)bytes, 0x00020000);
     }
+    // NT: streamed through once
+    template <bool NT = false>
     __device__ __forceinline__ uint4 load(uint32_t lane, uint32_t all) const
     {
-        return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)lane, (int)all, 0));
+        return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)lane, (int)all, NT ? 2 : 0));
     }
 };
 
@@ -298,7 +308,7 @@ struct I8Thin {
 #pragma unroll
         for (int s = 0; s < S; s++)
 #pragma unroll
-            for (int j = 0; j < 2; j++) w[d][s][j] = q[s].load(off + (uint32_t)(j * 2048), (uint32_t)tile * 4096u);
+            for (int j = 0; j < 2; j++) w[d][s][j] = q[s].template load<true>(off + (uint32_t)(j * 2048), (uint32_t)tile * 4096u);
     }
     __device__ __forceinline__ void start(int first, int tiles, int stride, int half, int lane)
     {
@@ -525,8 +535,8 @@ __global__ __launch_bounds__(64 * kI8LastWaves) void i8_thin_down_kernel(const I
 // columns.
 //  * Weights come straight into registers: a tile's bytes lie in the order of the matrix instruction's operand, so a wavefront's load is 1 KiB
 //    of contiguous memory.  A register is requested anew, for the next step, as soon as the last instruction that reads it has been issued.
-//  * The rows' codes are shared by the wavefronts through two LDS buffers that global memory fills directly; 16-byte chunk c of row r lies at
-//    position c ^ (r & mask), which spreads the operand reads (one chunk of 32 rows) over all banks.
+//  * The rows' codes are shared by the wavefronts through two LDS buffers that global memory fills directly; the 16-byte chunks
+//    of a row are turned by its number, which spreads the operand reads (one chunk of 32 rows) over all banks.
 //  * Several workgroups on a compute unit, one's waits, prologue and epilogue covered by the others' products.
 // Two shapes: S = 2, KT = 2 (128 accumulator registers a lane, two workgroups a compute unit) reads half as much LDS for a product; S = 1,
 // KT = 1 (64, four workgroups) has more loads on their way and twice as many workgroups, for calls that the weights' bytes bound.
@@ -557,6 +567,13 @@ struct I8Stage {
 struct I8Ops {
     uint4 t0, t1;
 };
+
+// What a row's chunks are turned by in LDS: sixteen rows' chunks of one number then lie on 64 different banks.
+template <int KT>
+__device__ __forceinline__ int i8_turn(int row)
+{
+    return KT == 2 ? row & 15 : (row >> 1) & 7;      // (rows of 128 bytes: the row's parity is half of the banks already)
+}
 
 // The first TILES tiles of a step.  The operands of the next pair of chunks are read while the products of this one are issued.
 template <int NTF, int S, int KT, int TILES>
@@ -624,7 +641,7 @@ __device__ __forceinline__ void i8_store4(void* out, long at, int dt, bool whole
 // round in an LDS area of its own, so that a row leaves in whole lines.
 template <int MODE, int NTF, int S>
 __device__ __forceinline__ void i8_finish(const I8Args& A, const int32_t* perm, const i32x16_t (&acc)[S][NTF], const float* sa, const float* sb,
-                                          int row0, int rows, int bx, uint32_t xs_base)
+                                          int row0, int rows, int bx, int expert, uint32_t xs_base)
 {
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int ln = lane & 31, kb = lane >> 5;
@@ -705,6 +722,20 @@ __device__ __forceinline__ void i8_finish(const I8Args& A, const int32_t* perm, 
             sc[i] = sa[min(n + i, A.N - 1)];
             if (MODE == kI8Plain && A.bias) add[i] = A.bias[min(n + i, A.N - 1)];
         }
+        const bool half = MODE == kI8Down && A.strip_scale;
+        if (half) {
+            // A pair's outputs in 16 bits: fp16 of sum * sum_scale * (channel's scale / the strip's largest), at most 2^15 and 2^-12 of itself
+            // off, a sixteenth of what the bf16 output of the call rounds; the rest of the factors goes to the sum over the slots.
+            float m = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3]));
+            m = fmaxf(m, __shfl_xor(m, 1, kWave));
+            m = fmaxf(m, __shfl_xor(m, 2, kWave));
+            m = fmaxf(m, __shfl_xor(m, 4, kWave));
+            const float c = m > 0.0f ? A.sum_scale / m : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; i++) sc[i] *= c;
+            if (left > 0 && (lane & 7) == 0 && lane < kOut)      // (every tile of an expert writes the same)
+                A.strip_scale[(long)expert * ((A.N + 31) / 32) + n / 32] = m / A.sum_scale;
+        }
 #pragma unroll
         for (int tf = 0; tf < NTF; tf++) {
             put(tf);
@@ -714,9 +745,15 @@ __device__ __forceinline__ void i8_finish(const I8Args& A, const int32_t* perm, 
                 const int rr = lane / kOut + 64 / kOut * j, row = 32 * tf + rr;
                 const uint4 u = lds_read16(area + (uint32_t)rr * kI8EpiRow<S> + (uint32_t)(lane & (kOut - 1)) * 16u);
                 if (row >= rows || left <= 0) continue;
-                const float xs = A.xs[row0 + row];
                 const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
                 float v[4];
+                if (half) {
+#pragma unroll
+                    for (int i = 0; i < 4; i++) v[i] = (float)(int)w4[i] * sc[i];
+                    store_global((uint16_t*)A.out + (long)(row0 + row) * A.ldo + n, make_uint2(pack_half2(v[0], v[1]), pack_half2(v[2], v[3])));
+                    continue;
+                }
+                const float xs = A.xs[row0 + row];
 #pragma unroll
                 for (int i = 0; i < 4; i++) v[i] = (float)(int)w4[i] * xs * sc[i] + add[i];
                 i8_store4(A.out, (long)(row0 + row) * A.ldo + n, dt, left >= 4 && vec, left, v);
@@ -728,7 +765,7 @@ __device__ __forceinline__ void i8_finish(const I8Args& A, const int32_t* perm, 
 // qw: this wavefront's strips; sa, sb: the scales of the matrices
 template <int MODE, int NTF, int S, int KT>
 __device__ __forceinline__ void i8_tile(const I8Args& A, const int32_t* perm, const I8Src (&qw)[S], const float* sa, const float* sb,
-                                        int row0, int rows, int bx, uint32_t xs_base, uint32_t buf_bytes)
+                                        int row0, int rows, int bx, int expert, uint32_t xs_base, uint32_t buf_bytes)
 {
     constexpr int kLanes = 8 * KT;              // lanes (16-byte chunks) to a row of a step
     constexpr int kRowsWave = 64 / kLanes;      // rows that a wavefront's copy fills
@@ -738,8 +775,8 @@ __device__ __forceinline__ void i8_tile(const I8Args& A, const int32_t* perm, co
     const uint32_t lane16 = (uint32_t)lane * 16u;
     i32x16_t acc[S][NTF] = {};
     I8Stage<NTF, KT> stage;
-    const int rb = kRowsWave * wave + lane / kLanes;                         // (rows of a thread agree in r & mask)
-    const int chunk = (lane & (kLanes - 1)) ^ (rb & (kLanes - 1));
+    const int rb = kRowsWave * wave + lane / kLanes;                         // (a thread's rows are turned alike)
+    const int chunk = (lane & (kLanes - 1)) ^ i8_turn<KT>(rb);
 #pragma unroll
     for (int i = 0; i < I8Stage<NTF, KT>::kCopies; i++) {
         const int r = min(4 * kRowsWave * i + rb, rows - 1);                 // rows behind the last: computed and dropped
@@ -757,7 +794,7 @@ __device__ __forceinline__ void i8_tile(const I8Args& A, const int32_t* perm, co
 #pragma unroll
         for (int i = 0; i < I8Stage<NTF, KT>::kCopies; i++) lds_copy16(base, stage.off[i] - less, stage.lds + at + (uint32_t)i * 4096u);
     };
-    const uint32_t xa0 = xs_base + (uint32_t)ln * kRow + (((uint32_t)kb << 6) ^ ((uint32_t)(ln & (kLanes - 1)) << 4));
+    const uint32_t xa0 = xs_base + (uint32_t)ln * kRow + (((uint32_t)kb << 6) ^ ((uint32_t)i8_turn<KT>(ln) << 4));
     I8Strips<S, KT> w;
     copy(0, 0);
 #pragma unroll
@@ -781,7 +818,7 @@ __device__ __forceinline__ void i8_tile(const I8Args& A, const int32_t* perm, co
         }
     }
 
-    i8_finish<MODE, NTF, S>(A, perm, acc, sa, sb, row0, rows, bx, xs_base);
+    i8_finish<MODE, NTF, S>(A, perm, acc, sa, sb, row0, rows, bx, expert, xs_base);
 }
 
 // Tiles of up to 160 rows for calls that the weights' bytes bound (experts that meet a few dozen tokens to some hundred): one strip a
@@ -792,7 +829,7 @@ constexpr int kI8Deep = 4;
 
 template <int MODE, int NTF>
 __device__ __forceinline__ void i8_wide_tile(const I8Args& A, const int32_t* perm, const I8Src& qw, const float* sa, const float* sb, int row0,
-                                             int rows, int bx, uint32_t xs_base)
+                                             int rows, int bx, int expert, uint32_t xs_base)
 {
     constexpr uint32_t kBuf = 32u * NTF * 128u;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -800,7 +837,7 @@ __device__ __forceinline__ void i8_wide_tile(const I8Args& A, const int32_t* per
     const uint32_t lane16 = (uint32_t)lane * 16u;
     i32x16_t acc[1][NTF] = {};
     const int rb = 8 * wave + (lane >> 3);
-    const uint32_t chunk = (uint32_t)((lane & 7) ^ (rb & 7)) * 16u;
+    const uint32_t chunk = (uint32_t)((lane & 7) ^ i8_turn<1>(rb)) * 16u;
     uint32_t off[NTF];
 #pragma unroll
     for (int i = 0; i < NTF; i++) {
@@ -830,7 +867,7 @@ __device__ __forceinline__ void i8_wide_tile(const I8Args& A, const int32_t* per
     put_x(xr[0], 0);
     load_x(xr[0], 2);
     __syncthreads();
-    const uint32_t xa0 = xs_base + (uint32_t)ln * 128u + (((uint32_t)kb << 6) ^ ((uint32_t)(ln & 7) << 4));
+    const uint32_t xa0 = xs_base + (uint32_t)ln * 128u + (((uint32_t)kb << 6) ^ ((uint32_t)i8_turn<1>(ln) << 4));
     constexpr int kMask = 0x2 | 0x4;             // vector and scalar arithmetic may cross; products, LDS and memory accesses may not
     auto step = [&](int k, auto slot) __attribute__((always_inline)) {
         constexpr int d = slot(), odd = d & 1;   // k % 4, k % 2
@@ -874,7 +911,7 @@ __device__ __forceinline__ void i8_wide_tile(const I8Args& A, const int32_t* per
     if (k < nkt) step(k, std::integral_constant<int, 0>());
     if (k + 1 < nkt) step(k + 1, std::integral_constant<int, 1>());
     if (k + 2 < nkt) step(k + 2, std::integral_constant<int, 2>());
-    i8_finish<MODE, NTF, 1>(A, perm, acc, sa, sb, row0, rows, bx, xs_base);
+    i8_finish<MODE, NTF, 1>(A, perm, acc, sa, sb, row0, rows, bx, expert, xs_base);
 }
 
 constexpr int kI8Run = 16;      // neighbouring units that an XCD takes at a time
@@ -887,37 +924,47 @@ template <int S>
 struct I8Unit {
     I8Src qw[S];              // this wavefront's strips
     const float *sa, *sb;     // the matrices' scales
-    int row0, rows, bx;
+    int row0, rows, bx, expert;
 };
 
-// The unit of a workgroup; false: none.  Workgroups go to the 8 XCDs, each with an L2 of its own, in turn.  A unit is a tile and a column
-// block; units that read the same weights (the tiles of a matrix or expert, for one column block) are neighbours, and an XCD takes runs
-// of neighbours.
-template <int MODE, int S, int ROWS>
-__device__ __forceinline__ bool i8_unit(const I8Args& A, const I8Plan& pp, I8Unit<S>& u)
+// Workgroups go to the 8 XCDs, each with an L2 of its own, in turn.  A unit is a tile and a column block; units that read the same weights
+// (the tiles of a matrix or expert, for one column block) are neighbours, and an XCD takes runs of neighbours.
+__device__ __forceinline__ long i8_run() { return (long)((blockIdx.x >> 3) / kI8Run) * 8 + (blockIdx.x & 7); }
+__device__ __forceinline__ int i8_turn_in_run() { return (blockIdx.x >> 3) % kI8Run; }
+
+// strip nt of a matrix; strips behind the last re-read it
+__device__ __forceinline__ void i8_strip(I8Src& to, const I8Args& A, const void* q, long nt)
+{
+    const long strip = 32L * A.Kp;
+    to.set((const char*)q + min(nt, (A.N + 31) / 32 - 1L) * strip, (uint32_t)strip);
+}
+
+template <int S>
+__device__ __forceinline__ bool i8_plain_unit(const I8Args& A, I8Unit<S>& u)
 {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    constexpr int cols = kI8Cols<MODE, S>;
-    const int nblk = (A.N + cols - 1) / cols;
-    const int tiles = MODE == kI8Plain ? (A.rows + ROWS - 1) / ROWS : pp.meta[0];
-    const long total = (long)tiles * nblk;
-    const int c = blockIdx.x & 7, j = blockIdx.x >> 3;
-    const long unit = ((long)(j / kI8Run) * 8 + c) * kI8Run + j % kI8Run;
-    if (unit >= total) return false;
-    const long strip = 32L * A.Kp, last = (A.N + 31) / 32 - 1;
-    auto strip_at = [&](I8Src& to, const void* q, long nt) { to.set((const char*)q + min(nt, last) * strip, (uint32_t)strip); };    // strips behind the last re-read it
-    if (MODE == kI8Plain) {
-        u.bx = (int)(unit / tiles);
-        u.row0 = (int)(unit - (long)u.bx * tiles) * ROWS;
-        u.rows = min(ROWS, A.rows - u.row0);
+    const int cols = kI8Cols<kI8Plain, S>, nblk = (A.N + cols - 1) / cols, tiles = (A.rows + kI8TileRows - 1) / kI8TileRows;
+    const long unit = i8_run() * kI8Run + i8_turn_in_run();
+    if (unit >= (long)tiles * nblk) return false;
+    u.bx = (int)(unit / tiles);
+    u.row0 = (int)(unit - (long)u.bx * tiles) * kI8TileRows;
+    u.rows = min(kI8TileRows, A.rows - u.row0);
 #pragma unroll
-        for (int s = 0; s < S; s++) strip_at(u.qw[s], A.w.q, (4L * u.bx + wave) * S + s);
-        u.sa = u.sb = A.w.s;
-        return true;
-    }
-    const int32_t* const t = pp.tiles + 8 * (unit / nblk);
+    for (int s = 0; s < S; s++) i8_strip(u.qw[s], A, A.w.q, (4L * u.bx + wave) * S + s);
+    u.sa = u.sb = A.w.s;
+    return true;
+}
+
+// unit `unit` of the tiles from `first` on, tiles of ROWS rows
+template <int MODE, int S, int ROWS>
+__device__ __forceinline__ void i8_expert_unit(const I8Args& A, const I8Plan& pp, int first, long unit, I8Unit<S>& u)
+{
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int cols = kI8Cols<MODE, S>, nblk = (A.N + cols - 1) / cols;
+    const int32_t* const t = pp.tiles + 8 * (first + unit / nblk);
     const int e = t[0], n = t[2], m = t[4];
-    const long local = unit - (long)t[3] * nblk;
+    const long local = unit - (long)(t[3] - first) * nblk;
+    u.expert = e;
     u.bx = (int)(local / m);
     const int i = (int)(local - (long)u.bx * m) * ROWS;
     u.row0 = t[1] + i;
@@ -927,30 +974,28 @@ __device__ __forceinline__ bool i8_unit(const I8Args& A, const I8Plan& pp, I8Uni
         u.sa = ex.s[0];
         u.sb = ex.s[1];
         if constexpr (S == 2) {
-            strip_at(u.qw[0], ex.q[0], 4L * u.bx + wave);
-            strip_at(u.qw[S - 1], ex.q[1], 4L * u.bx + wave);
+            i8_strip(u.qw[0], A, ex.q[0], 4L * u.bx + wave);
+            i8_strip(u.qw[S - 1], A, ex.q[1], 4L * u.bx + wave);
         } else {
-            strip_at(u.qw[0], wave < 2 ? ex.q[0] : ex.q[1], 2L * u.bx + (wave & 1));
+            i8_strip(u.qw[0], A, wave < 2 ? ex.q[0] : ex.q[1], 2L * u.bx + (wave & 1));
         }
     } else {
 #pragma unroll
-        for (int s = 0; s < S; s++) strip_at(u.qw[s], ex.q[2], (4L * u.bx + wave) * S + s);
+        for (int s = 0; s < S; s++) i8_strip(u.qw[s], A, ex.q[2], (4L * u.bx + wave) * S + s);
         u.sa = u.sb = ex.s[2];
     }
-    return true;
 }
 
 __device__ __forceinline__ uint32_t lds_base(char* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)p; }
 
-template <int MODE, int S, int KT>
-__global__ __launch_bounds__(256, S == 2 ? 2 : 4) void i8_gemm_kernel(const I8Args A)
+template <int S, int KT>
+__global__ __launch_bounds__(256, S == 2 ? 2 : 4) void i8_matmul_kernel(const I8Args A)
 {
     extern __shared__ __attribute__((aligned(1024))) char xs_raw[];
     constexpr uint32_t kBuf = (uint32_t)kI8TileRows * 128 * KT;
-    const I8Plan pp = i8_plan(const_cast<int32_t*>(A.plan), A.E, A.P);
     I8Unit<S> u;
-    if (!i8_unit<MODE, S, kI8TileRows>(A, pp, u)) return;
-#define DYMOE_I8_TILE(NTF) i8_tile<MODE, NTF, S, KT>(A, pp.perm, u.qw, u.sa, u.sb, u.row0, u.rows, u.bx, lds_base(xs_raw), kBuf)
+    if (!i8_plain_unit<S>(A, u)) return;
+#define DYMOE_I8_TILE(NTF) i8_tile<kI8Plain, NTF, S, KT>(A, nullptr, u.qw, u.sa, u.sb, u.row0, u.rows, u.bx, 0, lds_base(xs_raw), kBuf)
     // one instantiation per number of fragments of 32 rows: the accumulators then sit in fixed registers for the whole loop
     switch ((u.rows + 31) >> 5) {
     case 1: DYMOE_I8_TILE(1); break;
@@ -961,77 +1006,106 @@ __global__ __launch_bounds__(256, S == 2 ? 2 : 4) void i8_gemm_kernel(const I8Ar
 #undef DYMOE_I8_TILE
 }
 
+// Experts.  One that more than kI8TileWide pairs go to takes tiles of 128 rows and two strips a wavefront; the others, whose weights' bytes
+// bound them, one wide tile.  Runs of the two kinds alternate in proportion, so that the chip multiplies while it reads.
 template <int MODE>
-__global__ __launch_bounds__(256, 2) void i8_wide_kernel(const I8Args A)
+__global__ __launch_bounds__(256, 2) void i8_experts_kernel(const I8Args A)
 {
     extern __shared__ __attribute__((aligned(1024))) char xs_raw[];
+    const uint32_t xs = lds_base(xs_raw);
     const I8Plan pp = i8_plan(const_cast<int32_t*>(A.plan), A.E, A.P);
-    I8Unit<1> u;
-    if (!i8_unit<MODE, 1, kI8TileWide>(A, pp, u)) return;
-#define DYMOE_I8_TILE(NTF) i8_wide_tile<MODE, NTF>(A, pp.perm, u.qw[0], u.sa, u.sb, u.row0, u.rows, u.bx, lds_base(xs_raw))
-    switch ((u.rows + 31) >> 5) {
-    case 1: DYMOE_I8_TILE(1); break;
-    case 2: DYMOE_I8_TILE(2); break;
-    case 3: DYMOE_I8_TILE(3); break;
-    case 4: DYMOE_I8_TILE(4); break;
-    default: DYMOE_I8_TILE(5); break;
-    }
+    const int tall = pp.meta[0], wide = pp.meta[1];
+    const int c2 = kI8Cols<MODE, 2>, c1 = kI8Cols<MODE, 1>;
+    const long units2 = (long)tall * ((A.N + c2 - 1) / c2), units1 = (long)wide * ((A.N + c1 - 1) / c1);
+    const long runs2 = (units2 + kI8Run - 1) / kI8Run, runs1 = (units1 + kI8Run - 1) / kI8Run, runs = runs1 + runs2;
+    const long run = i8_run();
+    if (run >= runs) return;
+    const long before = run * runs2 / runs, upto = (run + 1) * runs2 / runs;      // runs of tall tiles before this one, and with it
+    if (upto > before) {
+        const long unit = before * kI8Run + i8_turn_in_run();
+        if (unit >= units2) return;
+        I8Unit<2> u;
+        i8_expert_unit<MODE, 2, kI8TileRows>(A, pp, 0, unit, u);
+#define DYMOE_I8_TILE(NTF) i8_tile<MODE, NTF, 2, 2>(A, pp.perm, u.qw, u.sa, u.sb, u.row0, u.rows, u.bx, u.expert, xs, (uint32_t)kI8TileRows * 256u)
+        switch ((u.rows + 31) >> 5) {
+        case 1: DYMOE_I8_TILE(1); break;
+        case 2: DYMOE_I8_TILE(2); break;
+        case 3: DYMOE_I8_TILE(3); break;
+        default: DYMOE_I8_TILE(4); break;
+        }
 #undef DYMOE_I8_TILE
+    } else {
+        const long unit = (run - before) * kI8Run + i8_turn_in_run();
+        if (unit >= units1) return;
+        I8Unit<1> u;
+        i8_expert_unit<MODE, 1, kI8TileWide>(A, pp, tall, unit, u);
+#define DYMOE_I8_TILE(NTF) i8_wide_tile<MODE, NTF>(A, pp.perm, u.qw[0], u.sa, u.sb, u.row0, u.rows, u.bx, u.expert, xs)
+        switch ((u.rows + 31) >> 5) {
+        case 1: DYMOE_I8_TILE(1); break;
+        case 2: DYMOE_I8_TILE(2); break;
+        case 3: DYMOE_I8_TILE(3); break;
+        case 4: DYMOE_I8_TILE(4); break;
+        default: DYMOE_I8_TILE(5); break;
+        }
+#undef DYMOE_I8_TILE
+    }
 }
 
-constexpr int kI8WideLds = 2 * kI8TileWide * 128;
-
-template <int S, int KT>
+template <int KT>
 constexpr int kI8Lds = 2 * kI8TileRows * 128 * KT;
+static_assert(2 * kI8TileWide * 128 <= kI8Lds<2>, "the wide tiles' buffers fit in the tall ones'");
+static_assert(4 * kI8EpiWave<2> <= kI8Lds<2> && 4 * kI8EpiWave<1> <= kI8Lds<1>, "the epilogue areas fit in the buffers");
+static_assert(4 * kI8EpiWave<1> <= 2 * 32 * 128 * 4, "also in those of a wide tile");
 
 // per-device set-up, with the device current
 int i8_init()
 {
     auto allow = [](const void* f, int bytes) { return hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess; };
-    bool ok = allow((const void*)i8_gemm_kernel<kI8Plain, 2, 2>, kI8Lds<2, 2>) && allow((const void*)i8_gemm_kernel<kI8Up, 2, 2>, kI8Lds<2, 2>) &&
-              allow((const void*)i8_gemm_kernel<kI8Down, 2, 2>, kI8Lds<2, 2>);
+    bool ok = allow((const void*)i8_matmul_kernel<2, 2>, kI8Lds<2>) && allow((const void*)i8_experts_kernel<kI8Up>, kI8Lds<2>) &&
+              allow((const void*)i8_experts_kernel<kI8Down>, kI8Lds<2>);
     ok = ok && allow((const void*)i8_thin_kernel<kI8Plain, true>, (int)kI8FuseBytes) && allow((const void*)i8_thin_kernel<kI8Up, true>, (int)kI8FuseBytes) &&
          allow((const void*)i8_thin_down_kernel, (int)kI8FuseBytes);
     return ok ? DYMOE_OK : DYMOE_EHIP;
 }
 
-// tiles: their number, or the most there can be; strips a wavefront: 2, 1, or 0 for the wide tiles
-template <int MODE>
-static void i8_gemm_launch(dymoe_ctx* ctx, int id, int strips, long tiles, hipStream_t st, const I8Args& A)
+// workgroups for `units` units and `kinds` kinds of them, whose last runs need not be whole
+static dim3 i8_grid(long units, int kinds)
 {
-    const int cols = strips == 2 ? kI8Cols<MODE, 2> : kI8Cols<MODE, 1>;
-    const long units = tiles * ((A.N + cols - 1) / cols), run = 8 * kI8Run;
-    const dim3 grid((unsigned)((units + run - 1) / run * run));
-    if (strips == 2) dymoe_launch(ctx, id, i8_gemm_kernel<MODE, 2, 2>, grid, dim3(256), kI8Lds<2, 2>, st, A);
-    else if (strips == 1) dymoe_launch(ctx, id, i8_gemm_kernel<MODE, 1, 1>, grid, dim3(256), kI8Lds<1, 1>, st, A);
-    else dymoe_launch(ctx, id, i8_wide_kernel<MODE>, grid, dim3(256), kI8WideLds, st, A);
+    return dim3((unsigned)(((units + kI8Run - 1) / kI8Run + kinds - 1 + 7) / 8 * 8 * kI8Run));
 }
 
-// y[t] = sum over the slots, in their order, of gate times the pair's output
-__global__ __launch_bounds__(256) void i8_combine_kernel(const float* __restrict__ part, long ldp, const int32_t* __restrict__ where,
-                                                         const float* __restrict__ gate, int T, int H, int k, int out_dtype,
-                                                         void* __restrict__ y)
+// y[t] = sum over the slots, in their order, of gate times the pair's output.  A workgroup takes 2048 outputs of a token.
+template <bool HALF>
+__global__ __launch_bounds__(256) void i8_combine_kernel(const char* __restrict__ part, long ldp, const float* __restrict__ hs,
+                                                         const float* __restrict__ strip_scale, const int32_t* __restrict__ idx,
+                                                         const int32_t* __restrict__ where, const float* __restrict__ gate, int H, int k,
+                                                         int out_dtype, int aligned, void* __restrict__ y)
 {
-    const int per = (H + 3) / 4;
-    const long i = (long)blockIdx.x * 256 + threadIdx.x;
-    const long t = i / per;
-    const int h = (int)(i - t * per) * 4;
-    if (t >= T) return;
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int blocks = (H + 2047) / 2048;
+    const long t = blockIdx.x / blocks;
+    const int h = (int)(blockIdx.x - t * blocks) * 2048 + threadIdx.x * 8;
+    if (h >= H) return;
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
     for (int j = 0; j < k; j++) {
         const int at = where[t * k + j];
         if (at < 0) continue;
-        const float g = gate[t * k + j];
-        const float4 v = load_global<float4>(part + at * ldp + h);
-        sum.x = fmaf(g, v.x, sum.x);
-        sum.y = fmaf(g, v.y, sum.y);
-        sum.z = fmaf(g, v.z, sum.z);
-        sum.w = fmaf(g, v.w, sum.w);
-    }
-    const float o[4] = {sum.x, sum.y, sum.z, sum.w};
+        float g = gate[t * k + j];
+        if constexpr (HALF) {
+            g *= hs[at] * strip_scale[(long)idx[t * k + j] * ((H + 31) / 32) + h / 32];
+            const half8_t v = __builtin_bit_cast(half8_t, load_global<uint4>(part + (at * ldp + h) * 2));
 #pragma unroll
-    for (int u = 0; u < 4; u++)
-        if (h + u < H) store_out(y, t * H + h + u, out_dtype, o[u]);
+            for (int i = 0; i < 8; i++) sum[i] = fmaf(g, (float)v[i], sum[i]);
+        } else {
+            const float4 a = load_global<float4>(part + (at * ldp + h) * 4), b = load_global<float4>(part + (at * ldp + h + 4) * 4);
+            const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int i = 0; i < 8; i++) sum[i] = fmaf(g, v[i], sum[i]);
+        }
+    }
+    const float lo[4] = {sum[0], sum[1], sum[2], sum[3]}, hi[4] = {sum[4], sum[5], sum[6], sum[7]};
+    i8_store4(y, t * H + h, out_dtype, aligned && h + 4 <= H, H - h, lo);
+    i8_store4(y, t * H + h + 4, out_dtype, aligned && h + 8 <= H, H - h - 4, hi);
 }
 
 }  // namespace dymoe
@@ -1110,7 +1184,9 @@ extern "C" int dymoe_matmul_int8(dymoe_ctx* ctx, const void* x, int x_dtype, con
     A.aligned = dymoe_aligned(y, 4 * dtype_bytes(out_dtype)) && ldy % 4 == 0;
     if (T > 32) {
         const long tiles = (T + kI8TileRows - 1L) / kI8TileRows;
-        i8_gemm_launch<kI8Plain>(ctx, DYMOE_K_MATMUL_INT8, tiles * ((N + 255L) / 256) >= 2L * ctx->num_cu ? 2 : 1, tiles, st, A);
+        const long units2 = tiles * ((N + 255L) / 256), units1 = tiles * ((N + 127L) / 128);
+        if (units2 >= 2L * ctx->num_cu) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_matmul_kernel<2, 2>, i8_grid(units2, 1), dim3(256), kI8Lds<2>, st, A);
+        else dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_matmul_kernel<1, 1>, i8_grid(units1, 1), dim3(256), kI8Lds<1>, st, A);
     } else {
         dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_small_kernel<kI8Plain>, dim3((unsigned)blocks), dim3(256), 0, st, A);
     }
@@ -1140,7 +1216,7 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     const I8FfnLayout L = i8_ffn_layout(T, H, F, E, k);
     if (workspace_bytes < L.total) return DYMOE_ENOSPC;
     const long up = (long)L.max_tiles * ((F + 31L) / 32), down = (long)L.max_tiles * ((H + 63L) / 64);      // workgroups at most
-    if (up > 0x7fff0000L || down > 0x7fff0000L || (long)T * ((H + 3) / 4) > 0x7fffffffL * 256L) return DYMOE_ENOTSUP;
+    if (up > 0x7fff0000L || down > 0x7fff0000L || T * ((H + 2047L) / 2048) > 0x7fffffffL) return DYMOE_ENOTSUP;
     if (!ctx) return DYMOE_ENOCTX;
     if (T == 0) return DYMOE_OK;
     hipStream_t st = (hipStream_t)stream;
@@ -1183,10 +1259,9 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     if (rc != DYMOE_OK) return rc;
     int32_t* const plan = (int32_t*)(ws + L.plan);
     const bool small = T <= 32 || P <= 8L * E;
-    const int strips = P <= 200L * E ? 0 : 2;
-    const int tile_rows = small ? kI8TileSmall : strips == 0 ? kI8TileWide : kI8TileRows;
-    const long tiles = P / tile_rows + (E < P ? E : P);
-    dymoe_launch(ctx, DYMOE_K_INT8_PLAN, i8_plan_kernel, dim3(1), dim3(kI8PlanThreads), 0, st, idx, table, P, E, tile_rows, plan,
+    // Workgroups at most: an expert of n pairs has n / 128 + 1 tall tiles at half as many column blocks, or one wide tile.
+    const long tall = P / kI8TileRows + P / (kI8TileWide + 1), wide = E < P ? E : P;
+    dymoe_launch(ctx, DYMOE_K_INT8_PLAN, i8_plan_kernel, dim3(1), dim3(kI8PlanThreads), 0, st, idx, table, P, E, small ? 1 : 0, plan,
                  ctx->device_flags);
     I8Args A = {};
     A.x = ws + L.xq;
@@ -1202,7 +1277,7 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     A.k = k;
     A.rows = T;
     if (small) dymoe_launch(ctx, DYMOE_K_INT8_UP, i8_small_kernel<kI8Up>, dim3((unsigned)up), dim3(256), 0, st, A);
-    else i8_gemm_launch<kI8Up>(ctx, DYMOE_K_INT8_UP, strips, tiles, st, A);
+    else dymoe_launch(ctx, DYMOE_K_INT8_UP, i8_experts_kernel<kI8Up>, i8_grid(tall * ((F + 127L) / 128) + wide * ((F + 63L) / 64), 2), dim3(256), kI8Lds<2>, st, A);
     rc = quantize_rows(ctx, ws + L.h, DYMOE_OUT_F32, P, F, (long)L.Fp, 0, ws + L.hq, (float*)(ws + L.hs), st);
     if (rc != DYMOE_OK) return rc;
     A.x = ws + L.hq;
@@ -1211,11 +1286,16 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     A.ldo = (long)L.Hp;
     A.Kp = (int)L.Fp;
     A.N = H;
+    const bool half = !small && out_dtype == DYMOE_OUT_BF16;
+    A.strip_scale = half ? (float*)(ws + L.strips) : nullptr;
+    A.sum_scale = 32768.0f / (16129.0f * (float)F);
     if (small) dymoe_launch(ctx, DYMOE_K_INT8_DOWN, i8_small_kernel<kI8Down>, dim3((unsigned)down), dim3(256), 0, st, A);
-    else i8_gemm_launch<kI8Down>(ctx, DYMOE_K_INT8_DOWN, strips, tiles, st, A);
-    const long items = (long)T * ((H + 3) / 4);
-    dymoe_launch(ctx, DYMOE_K_INT8_COMBINE, i8_combine_kernel, dim3((unsigned)((items + 255) / 256)), dim3(256), 0, st,
-                 (const float*)(ws + L.part), (long)L.Hp, i8_plan(plan, E, P).where, w, T, H, k, out_dtype, y);
+    else dymoe_launch(ctx, DYMOE_K_INT8_DOWN, i8_experts_kernel<kI8Down>, i8_grid(tall * ((H + 255L) / 256) + wide * ((H + 127L) / 128), 2), dim3(256), kI8Lds<2>, st, A);
+    const dim3 grid((unsigned)(T * ((H + 2047L) / 2048)));
+    auto combine = half ? i8_combine_kernel<true> : i8_combine_kernel<false>;
+    dymoe_launch(ctx, DYMOE_K_INT8_COMBINE, combine, grid, dim3(256), 0, st, ws + L.part, (long)L.Hp, (const float*)(ws + L.hs),
+                 (const float*)(ws + L.strips), idx, i8_plan(plan, E, P).where, w, H, k, out_dtype,
+                 H % 4 == 0 && dymoe_aligned(y, 4 * dtype_bytes(out_dtype)), y);
     DYMOE_HIP_LAUNCH_CHECK();
     return DYMOE_OK;
 }

@@ -16,7 +16,8 @@ struct I8FfnLayout {
     size_t xq, xs;     // [T, Hp] codes and [T] scales of the activations
     size_t h;          // [P, Fp] SwiGLU intermediate, by position (pairs sorted by expert)
     size_t hq, hs;     // [P, Fp] its codes, [P] their scales
-    size_t part;       // [P, Hp] fp32 outputs of the pairs, by position
+    size_t part;       // [P, Hp] outputs of the pairs, by position: fp32, or fp16 with
+    size_t strips;     // [E, strips of 32 outputs] their scales
     size_t plan;       // int32, see I8Plan
     size_t total;
     int max_tiles;
@@ -37,6 +38,7 @@ static inline I8FfnLayout i8_ffn_layout(long T, long H, long F, long E, long k)
     L.hq = take(P * L.Fp);
     L.hs = take(P * 4);
     L.part = take(P * L.Hp * 4);
+    L.strips = take((size_t)E * ((size_t)H + 31) / 32 * 4 + (size_t)E * 4);
     L.plan = take((8 + 2 * P + 8 * (size_t)L.max_tiles) * 4);
     L.total = at;
     return L;
