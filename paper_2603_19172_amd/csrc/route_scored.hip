@@ -11,13 +11,35 @@
 
 namespace dymoe {
 
-// 1 / d, d in [1, inf): the instruction's estimate and two Newton steps (infinity's inverse would make NaN in them)
+// 1 / d, d in [1, 1e308]: the instruction's estimate and two Newton steps
 __device__ __forceinline__ double inverse(double d)
 {
-    d = fmin(d, 1e300);
     double r = __builtin_amdgcn_rcp(d);
     r = fma(fma(-d, r, 1.0), r, r);
     return fma(fma(-d, r, 1.0), r, r);
+}
+
+// e^x for |x| <= 709: x = n ln 2 + r, |r| <= 0.3466, and the Taylor polynomial of degree 13, whose next term is below 2^-57 of the sum.
+// (Half the instructions of the library's, which four experts a lane spend a third of the kernel on.)
+__device__ __forceinline__ double exp_of(double x)
+{
+    const double n = __builtin_rint(x * 1.4426950408889634);
+    const double r = fma(n, -2.3190468138462996e-17, fma(n, -0.6931471805599453, x));
+    double p = 1.0 / 6227020800.0;
+    p = fma(p, r, 1.0 / 479001600.0);
+    p = fma(p, r, 1.0 / 39916800.0);
+    p = fma(p, r, 1.0 / 3628800.0);
+    p = fma(p, r, 1.0 / 362880.0);
+    p = fma(p, r, 1.0 / 40320.0);
+    p = fma(p, r, 1.0 / 5040.0);
+    p = fma(p, r, 1.0 / 720.0);
+    p = fma(p, r, 1.0 / 120.0);
+    p = fma(p, r, 1.0 / 24.0);
+    p = fma(p, r, 1.0 / 6.0);
+    p = fma(p, r, 0.5);
+    p = fma(p, r, 1.0);
+    p = fma(p, r, 1.0);
+    return __builtin_amdgcn_ldexp(p, (int)n);
 }
 
 __device__ __forceinline__ double lane_double(double v, int lane)       // lane the same for the whole wavefront
@@ -44,7 +66,7 @@ __device__ __forceinline__ uint32_t order_key(float f)
 // NPL: experts a lane holds.  DT: type of the logits.
 template <int NPL, int DT>
 __global__ __launch_bounds__(256) void route_scored_kernel(const char* __restrict__ logits, const float* __restrict__ bias, int T, int E,
-                                                           int k, int sigmoid, int groups, int top_groups, int best, int renorm,
+                                                           int k, int sigmoid, int groups, int top_groups, int best, uint32_t per_group, int renorm,
                                                            float factor, int32_t* __restrict__ idx, float* __restrict__ w,
                                                            float* __restrict__ scores)
 {
@@ -75,7 +97,7 @@ __global__ __launch_bounds__(256) void route_scored_kernel(const char* __restric
     double s[NPL], c[NPL];
     if (sigmoid) {
 #pragma unroll
-        for (int i = 0; i < NPL; i++) s[i] = l[i] == -__builtin_inff() ? 0.0 : inverse(1.0 + exp(-(double)l[i]));
+        for (int i = 0; i < NPL; i++) s[i] = l[i] == -__builtin_inff() ? 0.0 : inverse(1.0 + exp_of(-(double)fminf(fmaxf(l[i], -700.0f), 700.0f)));
     } else {
         uint32_t mk = 0;
 #pragma unroll
@@ -86,7 +108,8 @@ __global__ __launch_bounds__(256) void route_scored_kernel(const char* __restric
         double sum = 0.0;
 #pragma unroll
         for (int i = 0; i < NPL; i++) {
-            s[i] = l[i] == -__builtin_inff() ? 0.0 : exp((double)l[i] - (double)m);
+            // (a difference beyond 700 is a score below 2^-1000: 0 in the call's types)
+            s[i] = l[i] == -__builtin_inff() ? 0.0 : exp_of(fmax((double)l[i] - (double)m, -700.0));
             sum += s[i];
         }
         sum = wave_sum_f64(sum);
@@ -144,7 +167,7 @@ __global__ __launch_bounds__(256) void route_scored_kernel(const char* __restric
 #pragma unroll
     for (int i = 0; i < NPL; i++) {
         const int e = lane + 64 * i;
-        const bool in = e < E && (groups == 1 || ((kept >> (e / per)) & 1ull));
+        const bool in = e < E && (groups == 1 || ((kept >> ((uint32_t)e * per_group >> 21)) & 1ull));      // its group, e / per
         key[i] = in ? order_key((float)c[i]) : 0u;            // 0: cannot be chosen
     }
     if (scores) {
@@ -154,45 +177,84 @@ __global__ __launch_bounds__(256) void route_scored_kernel(const char* __restric
             if (e < E) scores[t * E + e] = bad ? __builtin_nanf("") : (float)s[i];
         }
     }
+    // A lane keeps its keys in falling order, so that a round compares one key a lane: the lane that has the round's
+    // largest gives it up and shows its next.
+    int which[NPL];
+#pragma unroll
+    for (int i = 0; i < NPL; i++) which[i] = i;
+    // (Batcher's merging network: 1, 5, 19 or 63 comparisons)
+#pragma unroll
+    for (int p = 1; p < NPL; p *= 2)
+#pragma unroll
+        for (int d = p; d >= 1; d /= 2)
+#pragma unroll
+            for (int j = d % p; j + d < NPL; j += 2 * d)
+#pragma unroll
+                for (int i = 0; i < d; i++)
+                    if (i + j + d < NPL && (i + j) / (2 * p) == (i + j + d) / (2 * p)) {
+                        const bool swap = key[i + j + d] > key[i + j];
+                        const uint32_t ka = key[i + j], kb = key[i + j + d];
+                        const int wa = which[i + j], wb = which[i + j + d];
+                        key[i + j] = swap ? kb : ka;
+                        key[i + j + d] = swap ? ka : kb;
+                        which[i + j] = swap ? wb : wa;
+                        which[i + j + d] = swap ? wa : wb;
+                    }
     int mine = 0;
-    double weight = 0.0;
     for (int j = 0; j < k; j++) {
-        uint32_t best_key = key[0];
+        const uint32_t top = wave_max_u32(key[0]);
+        uint64_t at = __ballot(key[0] == top);
+        int owner = __builtin_ctzll(at), first;
+        // more than one expert with that key, in several lanes or in one lane's next place
+        const uint64_t again = NPL > 1 ? __ballot(key[0] == top && key[NPL > 1 ? 1 : 0] == top) : 0;
+        if (((at & (at - 1)) | again) == 0) {
+            first = 64 * __builtin_amdgcn_readlane(which[0], owner) + owner;
+        } else {
+            // the largest of the 64-bit values (without a bias the keys are the logits themselves), then the lowest index
+            double best = kLow, of[NPL];
+            if (bias) {
 #pragma unroll
-        for (int i = 1; i < NPL; i++) best_key = max(best_key, key[i]);
-        best_key = wave_max_u32(best_key);
-        int n = 0;
-        uint32_t first = 0xffffffffu;
+                for (int i = 0; i < NPL; i++) {
+                    of[i] = kLow;
 #pragma unroll
-        for (int i = NPL - 1; i >= 0; i--) {
-            const uint64_t at = __ballot(key[i] == best_key);
-            n += __popcll(at);
-            if (at) first = 64 * i + (uint32_t)__builtin_ctzll(at);
-        }
-        if (n > 1 && bias) {                                  // (without a bias the keys are the logits themselves)
-            double top = kLow;
+                    for (int u = 0; u < NPL; u++) of[i] = which[i] == u ? c[u] : of[i];
+                    best = fmax(best, key[i] == top ? of[i] : kLow);
+                }
 #pragma unroll
-            for (int i = 0; i < NPL; i++) top = fmax(top, key[i] == best_key ? c[i] : kLow);
+                for (int o = 32; o > 0; o >>= 1) best = fmax(best, __shfl_xor(best, o, kWave));
+            }
+            uint32_t low = 0xffffffffu;
 #pragma unroll
-            for (int o = 32; o > 0; o >>= 1) top = fmax(top, __shfl_xor(top, o, kWave));
+            for (int i = 0; i < NPL; i++)
+                if (key[i] == top && (!bias || of[i] == best)) low = min(low, (uint32_t)(64 * which[i] + lane));
+            first = (int)~wave_max_u32(~low);
+            owner = first & 63;
+            // to the front of its lane
+            const int slot = first >> 6;
+            if (lane == owner) {
 #pragma unroll
-            for (int i = NPL - 1; i >= 0; i--) {
-                const uint64_t at = __ballot(key[i] == best_key && c[i] == top);
-                if (at) first = 64 * i + (uint32_t)__builtin_ctzll(at);
+                for (int i = NPL - 1; i > 0; i--)
+                    if (key[i] == top && which[i] == slot) {
+                        which[i] = which[0];
+                        which[0] = slot;
+                    }
             }
         }
-        const int owner = __builtin_amdgcn_readfirstlane((int)(first & 63u)), which = __builtin_amdgcn_readfirstlane((int)(first >> 6));
-        double sw = 0.0;
+        if (lane == owner) {
 #pragma unroll
-        for (int i = 0; i < NPL; i++)
-            if (which == i) {
-                sw = lane_double(s[i], owner);
-                if (lane == owner) key[i] = 0u;
+            for (int i = 0; i + 1 < NPL; i++) {
+                key[i] = key[i + 1];
+                which[i] = which[i + 1];
             }
-        if (lane == j) {
-            mine = (int)first;
-            weight = sw;
+            key[NPL - 1] = 0u;
         }
+        if (lane == j) mine = first;
+    }
+    double weight = 0.0;
+#pragma unroll
+    for (int i = 0; i < NPL; i++) {
+        const double v = __shfl(s[i], mine & 63, kWave);
+        if (lane < k && (mine >> 6) == i) weight = v;
     }
     if (renorm) {
         const double sum = wave_sum_f64(weight);
@@ -211,7 +273,8 @@ static void route_scored_launch(dymoe_ctx* ctx, const void* logits, const float*
     const dim3 grid((unsigned)((T + 3L) / 4));
 #define DYMOE_RSCORED(NPL)                                                                                                        \
     dymoe_launch(ctx, DYMOE_K_ROUTE_SCORED, route_scored_kernel<NPL, DT>, grid, dim3(256), groups > 1 ? 4 * NPL * 64 * 8 : 0, st, \
-                 (const char*)logits, bias, T, E, k, sigmoid, groups, top_groups, best, renorm, factor, idx, w, scores)
+                 (const char*)logits, bias, T, E, k, sigmoid, groups, top_groups, best,                   \
+                 (uint32_t)((1 << 21) / (E / groups) + 1), renorm, factor, idx, w, scores)
     if (E <= 64) DYMOE_RSCORED(1);
     else if (E <= 128) DYMOE_RSCORED(2);
     else if (E <= 256) DYMOE_RSCORED(4);
