@@ -14,21 +14,28 @@ namespace dymoe {
 
 int quantize_rows(dymoe_ctx* ctx, const void* x, int dtype, long rows, long K, long ldx, int tiles, void* codes, float* scale, hipStream_t st);
 
+// A tile of an expert: all that a workgroup has to know before its first load of weights.
+struct __attribute__((aligned(16))) I8TileRec {
+    int32_t expert, first, pairs;     // the expert, its first position, its pairs
+    int32_t tile0, tiles;             // its first tile, its tiles
+    int32_t unused[3];
+    dymoe_expert_i8 mat;
+};
+
 struct I8Plan {
     int32_t* meta;        // [8]: tiles, wide tiles behind them
     int32_t* perm;        // [P] position -> pair
     int32_t* where;       // [P] pair -> position, -1: left out
-    int32_t* tiles;       // [8 max_tiles]: the tile's expert, its first position, its pairs, its first tile, its tiles (3 unused)
+    I8TileRec* tiles;
 };
 
-__host__ __device__ inline I8Plan i8_plan(int32_t* p, int E, long P)
+__host__ __device__ inline I8Plan i8_plan(int32_t* p, long P)
 {
     I8Plan r;
-    (void)E;
     r.meta = p;
     r.perm = r.meta + 8;
     r.where = r.perm + P;
-    r.tiles = r.where + P;
+    r.tiles = (I8TileRec*)(p + 8 + (2 * P + 3) / 4 * 4);
     return r;
 }
 
@@ -44,13 +51,17 @@ __device__ __forceinline__ bool i8_present(const dymoe_expert_i8& x)
 constexpr int kI8PlanThreads = 1024;
 constexpr int kI8PlanKeep = 16;
 
-__global__ __launch_bounds__(kI8PlanThreads) void i8_plan_kernel(const int32_t* __restrict__ idx, const dymoe_expert_i8* __restrict__ table,
-                                                                 long P, int E, int small, int32_t* __restrict__ plan,
-                                                                 unsigned* __restrict__ flags)
+struct I8PlanLds {
+    int count[DYMOE_MAX_EXPERTS], sorted[DYMOE_MAX_EXPERTS], at[DYMOE_MAX_EXPERTS], wave[2][kI8PlanThreads / kWave];
+};
+
+__device__ __forceinline__ void i8_make_plan(I8PlanLds& lds, const int32_t* __restrict__ idx, const dymoe_expert_i8* __restrict__ table, long P, int E,
+                                             int small, int32_t* __restrict__ plan, unsigned* __restrict__ flags)
 {
-    __shared__ int s_count[DYMOE_MAX_EXPERTS], s_sorted[DYMOE_MAX_EXPERTS], s_at[DYMOE_MAX_EXPERTS], s_wave[2][kI8PlanThreads / kWave];
+    int *const s_count = lds.count, *const s_sorted = lds.sorted, *const s_at = lds.at;
+    int (*const s_wave)[kI8PlanThreads / kWave] = lds.wave;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
-    const I8Plan pp = i8_plan(plan, E, P);
+    const I8Plan pp = i8_plan(plan, P);
     int e_of[kI8PlanKeep], turn[kI8PlanKeep];
 #pragma unroll
     for (int i = 0; i < kI8PlanKeep; i++) {
@@ -102,12 +113,14 @@ __global__ __launch_bounds__(kI8PlanThreads) void i8_plan_kernel(const int32_t* 
     if (tid < E) {
         s_at[e] = n > 0 ? n0 : -1;               // (every thread has read its count)
         for (int i = 0; i < m; i++) {
-            int32_t* const t = pp.tiles + 8L * (t0 + i);
-            t[0] = e;
-            t[1] = n0;
-            t[2] = n;
-            t[3] = t0;
-            t[4] = m;
+            I8TileRec t = {};
+            t.expert = e;
+            t.first = n0;
+            t.pairs = n;
+            t.tile0 = t0;
+            t.tiles = m;
+            t.mat = table[e];
+            pp.tiles[t0 + i] = t;
         }
     }
     // (experts come by falling load: those of one wide tile are the last)
@@ -131,6 +144,64 @@ __global__ __launch_bounds__(kI8PlanThreads) void i8_plan_kernel(const int32_t* 
         if (p < P) place(p, e_of[i], turn[i]);
     }
     for (long p = tid + (long)kI8PlanKeep * kI8PlanThreads; p < P; p += kI8PlanThreads) place(p, idx[p], pp.where[p]);
+}
+
+// The plan by the first workgroup, the codes of the activations by the others, four rows each: neither needs the other, and a launch of its
+// own would cost either as much as its work.  CH: 16 bytes a thread times CH hold a row.
+template <int DT, int CH>
+__global__ __launch_bounds__(kI8PlanThreads) void i8_prep_kernel(const int32_t* __restrict__ idx, const dymoe_expert_i8* __restrict__ table, long P,
+                                                                 int E, int small, int32_t* __restrict__ plan, unsigned* __restrict__ flags,
+                                                                 const char* __restrict__ x, int T, int K, char* __restrict__ codes,
+                                                                 float* __restrict__ scale)
+{
+    __shared__ I8PlanLds lds;
+    if (blockIdx.x == 0) {
+        i8_make_plan(lds, idx, table, P, E, small, plan, flags);
+        return;
+    }
+    constexpr int kThreads = kI8PlanThreads / 4;                 // to a row
+    const int t = threadIdx.x % kThreads, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const long row = (long)(blockIdx.x - 1) * 4 + threadIdx.x / kThreads;
+    const int Kp = (int)up_to(K, 128);
+    const char* const src = x + row * K * dtype_bytes(DT);
+    Raw8<DT> v[CH];
+    uint32_t m = 0;
+#pragma unroll
+    for (int c = 0; c < CH; c++) v[c] = load8<DT>(src, (c * kThreads + t) * 8, row < T ? K : 0);
+#pragma unroll
+    for (int c = 0; c < CH; c++) m = peak8<DT>(v[c], m);
+    m = wave_max_u32(peak_bits<DT>(m));
+    if (lane == 0) lds.count[wave] = (int)m;
+    __syncthreads();
+    if (row >= T) return;
+    const int w0 = wave & ~3;
+    m = max(max((uint32_t)lds.count[w0], (uint32_t)lds.count[w0 + 1]), max((uint32_t)lds.count[w0 + 2], (uint32_t)lds.count[w0 + 3]));
+    float sc;
+    const RowQ q = row_q(peak_value<DT>(m), sc);
+    if (t == 0) scale[row] = sc;
+#pragma unroll
+    for (int c = 0; c < CH; c++) {
+        const int col = (c * kThreads + t) * 8;
+        if (col < Kp) store_global(codes + row * Kp + col, codes8<DT>(v[c], q));
+    }
+}
+
+template <int DT>
+static void i8_prep_launch(dymoe_ctx* ctx, const int32_t* idx, const dymoe_expert_i8* table, long P, int E, int small, int32_t* plan, const void* x,
+                           int T, int K, void* codes, float* scale, hipStream_t st)
+{
+    const dim3 grid((unsigned)(1 + (T + 3L) / 4)), block(kI8PlanThreads);
+    auto kernel = K <= 4096 ? i8_prep_kernel<DT, 2> : i8_prep_kernel<DT, 8>;
+    dymoe_launch(ctx, DYMOE_K_INT8_PLAN, kernel, grid, block, 0, st, idx, table, P, E, small, plan, ctx->device_flags, (const char*)x, T, K,
+                 (char*)codes, scale);
+}
+
+// (a row of more than 16384 values: its codes by a launch of their own, this one for the plan)
+__global__ __launch_bounds__(kI8PlanThreads) void i8_plan_kernel(const int32_t* __restrict__ idx, const dymoe_expert_i8* __restrict__ table, long P,
+                                                                 int E, int small, int32_t* __restrict__ plan, unsigned* __restrict__ flags)
+{
+    __shared__ I8PlanLds lds;
+    i8_make_plan(lds, idx, table, P, E, small, plan, flags);
 }
 
 // One weight matrix as a launch reads it: codes in tiles, scales.
@@ -179,103 +250,6 @@ __device__ __forceinline__ i32x16_t mfma_i8(const uint4 a, const uint4 b, const 
 }
 
 __device__ __forceinline__ float silu_times(float a, float u) { return a * __builtin_amdgcn_rcpf(1.0f + __expf(-a)) * u; }
-
-// Tiles of one fragment (up to 32 rows): the four wavefronts of a workgroup share two strips of 32 weight rows and split K.  Nothing is
-// shared before the end: weights and rows come straight into registers.
-template <int MODE>
-__global__ __launch_bounds__(256) void i8_small_kernel(const I8Args A)
-{
-    __shared__ __attribute__((aligned(16))) int s_red[4 * 2 * 16 * kWave];
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-    const int ln = lane & 31, kb = lane >> 5;
-    const int cols = MODE == kI8Up ? 32 : 64;
-    const int nblk = (A.N + cols - 1) / cols;
-    const int tile = blockIdx.x / nblk, bx = blockIdx.x - tile * nblk;
-    int row0, rows;
-    const char *qa, *qb;
-    const float *sa, *sb;
-    const I8Plan pp = i8_plan(const_cast<int32_t*>(A.plan), A.E, A.P);
-    const long strip = 32L * A.Kp;
-    const long last = (A.N + 31) / 32 - 1;
-    if (MODE == kI8Plain) {
-        row0 = tile * kI8TileSmall;
-        rows = min(kI8TileSmall, A.rows - row0);
-        qa = A.w.q + 2L * bx * strip;
-        qb = A.w.q + min(2L * bx + 1, last) * strip;
-        sa = sb = A.w.s;
-    } else {
-        if (tile >= pp.meta[0]) return;
-        const int32_t* const t = pp.tiles + 8L * tile;
-        const int e = t[0], i = (tile - t[3]) * kI8TileSmall;
-        row0 = t[1] + i;
-        rows = min(kI8TileSmall, t[2] - i);
-        const dymoe_expert_i8 ex = A.table[e];
-        if (MODE == kI8Up) {
-            qa = (const char*)ex.q[0] + bx * strip;
-            qb = (const char*)ex.q[1] + bx * strip;
-            sa = ex.s[0];
-            sb = ex.s[1];
-        } else {
-            qa = (const char*)ex.q[2] + 2L * bx * strip;
-            qb = (const char*)ex.q[2] + min(2L * bx + 1, last) * strip;
-            sa = sb = ex.s[2];
-        }
-    }
-    const int r = min(ln, rows - 1);                  // rows behind the last: computed and dropped
-    const long src = MODE == kI8Up ? pp.perm[row0 + r] / A.k : row0 + r;
-    const char* const xp = A.x + src * A.Kp + 64 * kb;
-    i32x16_t acc[2] = {};
-    const int nkt = A.Kp >> 7;
-    for (int kt = wave; kt < nkt; kt += 4) {
-        uint4 a[4], b[4], t[4];
-#pragma unroll
-        for (int c = 0; c < 4; c++) {
-            a[c] = load_global<uint4>(qa + (long)kt * 4096 + c * 1024 + lane * 16);
-            b[c] = load_global<uint4>(qb + (long)kt * 4096 + c * 1024 + lane * 16);
-            t[c] = load_global<uint4>(xp + (long)kt * 128 + c * 16);
-        }
-#pragma unroll
-        for (int c = 0; c < 4; c++) {
-            acc[0] = mfma_i8(a[c], t[c], acc[0]);
-            acc[1] = mfma_i8(b[c], t[c], acc[1]);
-        }
-    }
-#pragma unroll
-    for (int s = 0; s < 2; s++)
-#pragma unroll
-        for (int i = 0; i < 16; i++) s_red[((wave * 2 + s) * 16 + i) * kWave + lane] = acc[s][i];
-    __syncthreads();
-    // wavefront w finishes registers 4 w .. 4 w + 3 of both strips: weight rows 8 w + 4 kb + 0 .. 3, token ln
-    float v[2][4];
-#pragma unroll
-    for (int s = 0; s < 2; s++)
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int* const at = s_red + (s * 16 + 4 * wave + i) * kWave + lane;
-            v[s][i] = (float)(at[0] + at[2048] + at[4096] + at[6144]);
-        }
-    if (ln >= rows) return;
-    const float xs = A.xs[src];
-    const int n0 = cols * bx + 8 * wave + 4 * kb;
-    if (MODE == kI8Up) {
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int n = n0 + i;
-            if (n < A.N) store_out(A.out, (row0 + ln) * A.ldo + n, DYMOE_OUT_F32, silu_times(v[0][i] * xs * sa[n], v[1][i] * xs * sb[n]));
-        }
-        return;
-    }
-#pragma unroll
-    for (int s = 0; s < 2; s++)
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int n = n0 + 32 * s + i;
-            if (n >= A.N) continue;
-            float o = v[s][i] * xs * sa[n];
-            if (MODE == kI8Plain && A.bias) o += A.bias[n];
-            store_out(A.out, (long)(row0 + ln) * A.ldo + n, MODE == kI8Plain ? A.out_dtype : DYMOE_OUT_F32, o);
-        }
-}
 
 // ----------------------------------------------------------------------------
 // A few rows (decode): a stream of weights.  A workgroup owns 16 weight rows (of W1 and of W3 in the up projection), its wavefronts take the
@@ -961,15 +935,14 @@ __device__ __forceinline__ void i8_expert_unit(const I8Args& A, const I8Plan& pp
 {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int cols = kI8Cols<MODE, S>, nblk = (A.N + cols - 1) / cols;
-    const int32_t* const t = pp.tiles + 8 * (first + unit / nblk);
-    const int e = t[0], n = t[2], m = t[4];
-    const long local = unit - (long)(t[3] - first) * nblk;
-    u.expert = e;
-    u.bx = (int)(local / m);
-    const int i = (int)(local - (long)u.bx * m) * ROWS;
-    u.row0 = t[1] + i;
-    u.rows = min(ROWS, n - i);
-    const dymoe_expert_i8 ex = A.table[e];
+    const I8TileRec t = pp.tiles[first + unit / nblk];
+    const long local = unit - (long)(t.tile0 - first) * nblk;
+    u.expert = t.expert;
+    u.bx = (int)(local / t.tiles);
+    const int i = (int)(local - (long)u.bx * t.tiles) * ROWS;
+    u.row0 = t.first + i;
+    u.rows = min(ROWS, t.pairs - i);
+    const dymoe_expert_i8& ex = t.mat;
     if (MODE == kI8Up) {
         u.sa = ex.s[0];
         u.sb = ex.s[1];
@@ -1013,7 +986,7 @@ __global__ __launch_bounds__(256, 2) void i8_experts_kernel(const I8Args A)
 {
     extern __shared__ __attribute__((aligned(1024))) char xs_raw[];
     const uint32_t xs = lds_base(xs_raw);
-    const I8Plan pp = i8_plan(const_cast<int32_t*>(A.plan), A.E, A.P);
+    const I8Plan pp = i8_plan(const_cast<int32_t*>(A.plan), A.P);
     const int tall = pp.meta[0], wide = pp.meta[1];
     const int c2 = kI8Cols<MODE, 2>, c1 = kI8Cols<MODE, 1>;
     const long units2 = (long)tall * ((A.N + c2 - 1) / c2), units1 = (long)wide * ((A.N + c1 - 1) / c1);
@@ -1055,6 +1028,7 @@ template <int KT>
 constexpr int kI8Lds = 2 * kI8TileRows * 128 * KT;
 static_assert(2 * kI8TileWide * 128 <= kI8Lds<2>, "the wide tiles' buffers fit in the tall ones'");
 static_assert(4 * kI8EpiWave<2> <= kI8Lds<2> && 4 * kI8EpiWave<1> <= kI8Lds<1>, "the epilogue areas fit in the buffers");
+static_assert(sizeof(I8TileRec) == 80, "as the workspace has it");
 static_assert(4 * kI8EpiWave<1> <= 2 * 32 * 128 * 4, "also in those of a wide tile");
 
 // per-device set-up, with the device current
@@ -1072,6 +1046,141 @@ int i8_init()
 static dim3 i8_grid(long units, int kinds)
 {
     return dim3((unsigned)(((units + kI8Run - 1) / kI8Run + kinds - 1 + 7) / 8 * 8 * kI8Run));
+}
+
+// ----------------------------------------------------------------------------
+// Tiles of up to 32 NTF rows where rows or columns are too few for the shapes above (decode batches on experts, narrow matrices): a workgroup
+// owns 32 weight rows (of W1 and of W3 in the up projection) and its NW wavefronts take the 128-column tiles of K in turn.  Nothing is
+// shared before the end: weights and codes come straight into registers, a tile ahead, and the sums meet in LDS.
+template <int MODE, int NTF, int NW>
+__global__ __launch_bounds__(64 * NW) void i8_small_kernel(const I8Args A)
+{
+    constexpr int S = MODE == kI8Up ? 2 : 1, kSums = S * NTF, kRows = 32 * NTF;
+    __shared__ int s_red[4][kSums][16][kWave];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int ln = lane & 31, kb = lane >> 5;
+    const int nblk = (A.N + 31) / 32;
+    const I8Plan pp = i8_plan(const_cast<int32_t*>(A.plan), A.P);
+    const long strip = 32L * A.Kp;
+    int row0, rows, bx;
+    I8Src q[S], x;
+    const float *sa, *sb;
+    if (MODE == kI8Plain) {
+        const int tiles = (A.rows + kRows - 1) / kRows;
+        bx = blockIdx.x / tiles;
+        row0 = (blockIdx.x - bx * tiles) * kRows;
+        rows = min(kRows, A.rows - row0);
+        q[0].set(A.w.q + bx * strip, (uint32_t)strip);
+        sa = sb = A.w.s;
+    } else {
+        const int tile = blockIdx.x / nblk;
+        bx = blockIdx.x - tile * nblk;
+        if (tile >= pp.meta[0]) return;
+        const I8TileRec t = pp.tiles[tile];
+        const int i = (tile - t.tile0) * kRows;
+        row0 = t.first + i;
+        rows = min(kRows, t.pairs - i);
+        q[0].set((const char*)t.mat.q[MODE == kI8Up ? 0 : 2] + bx * strip, (uint32_t)strip);
+        q[S - 1].set((const char*)t.mat.q[MODE == kI8Up ? 1 : 2] + bx * strip, (uint32_t)strip);
+        sa = t.mat.s[MODE == kI8Up ? 0 : 2];
+        sb = t.mat.s[MODE == kI8Up ? 1 : 2];
+    }
+    struct Tile {
+        uint4 w[S][4], x[NTF][4];
+    };
+    const uint32_t lane16 = (uint32_t)lane * 16u;
+    uint32_t off[NTF];
+    const int nkt = A.Kp >> 7;
+    auto load_w = [&](Tile& t, int kt) {
+#pragma unroll
+        for (int s = 0; s < S; s++)
+#pragma unroll
+            for (int c = 0; c < 4; c++) t.w[s][c] = q[s].template load<true>(lane16 + (uint32_t)(c * 1024), (uint32_t)kt * 4096u);
+    };
+    auto load_x = [&](Tile& t, int kt) {
+#pragma unroll
+        for (int f = 0; f < NTF; f++)
+#pragma unroll
+            for (int c = 0; c < 4; c++) t.x[f][c] = x.load(off[f] + (uint32_t)(c * 16), (uint32_t)kt * 128u);
+    };
+    Tile a, b;
+    int kt = wave;
+    if (kt < nkt) load_w(a, kt);               // (the weights need nothing of the rows)
+#pragma unroll
+    for (int f = 0; f < NTF; f++) {
+        const int r = min(32 * f + ln, rows - 1);                            // rows behind the last: computed and dropped
+        off[f] = (MODE == kI8Up ? (uint32_t)(pp.perm[row0 + r] / A.k) : (uint32_t)r) * (uint32_t)A.Kp + 64u * (uint32_t)kb;
+    }
+    x.set(A.x + (MODE == kI8Up ? 0 : (long)row0 * A.Kp), (uint32_t)(MODE == kI8Up ? A.rows : rows) * (uint32_t)A.Kp);
+    if (kt < nkt) load_x(a, kt);
+    i32x16_t acc[S][NTF] = {};
+    auto multiply = [&](const Tile& t) {
+#pragma unroll
+        for (int c = 0; c < 4; c++)
+#pragma unroll
+            for (int s = 0; s < S; s++)
+#pragma unroll
+                for (int f = 0; f < NTF; f++) acc[s][f] = mfma_i8(t.w[s][c], t.x[f][c], acc[s][f]);
+    };
+    while (kt < nkt) {
+        if (kt + NW < nkt) {
+            load_w(b, kt + NW);
+            load_x(b, kt + NW);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(a);
+        kt += NW;
+        if (kt >= nkt) break;
+        if (kt + NW < nkt) {
+            load_w(a, kt + NW);
+            load_x(a, kt + NW);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(b);
+        kt += NW;
+    }
+    auto put = [&](int at) {
+#pragma unroll
+        for (int s = 0; s < S; s++)
+#pragma unroll
+            for (int f = 0; f < NTF; f++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) s_red[at][s * NTF + f][i][lane] = acc[s][f][i];
+    };
+    if constexpr (NW == 8) {
+        if (wave >= 4) put(wave - 4);
+        __syncthreads();
+        if (wave < 4) {
+#pragma unroll
+            for (int s = 0; s < S; s++)
+#pragma unroll
+                for (int f = 0; f < NTF; f++)
+#pragma unroll
+                    for (int i = 0; i < 16; i++) acc[s][f][i] += s_red[wave][s * NTF + f][i][lane];
+            put(wave);                          // (its own place, read by none but it)
+        }
+    } else {
+        put(wave);
+    }
+    __syncthreads();
+    // a wavefront finishes four registers of a fragment: weight rows 8 g + 4 kb + 0 .. 3, token ln
+    for (int item = wave; item < 4 * NTF; item += NW) {
+        const int f = item >> 2, g = item & 3, row = 32 * f + ln;
+        if (row >= rows) continue;
+        const int n = 32 * bx + 8 * g + 4 * kb, left = A.N - n;
+        if (left <= 0) continue;
+        const float xs = A.xs[MODE == kI8Up ? pp.perm[row0 + row] / A.k : row0 + row];
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int m = min(n + i, A.N - 1);
+            auto sum = [&](int at) { return (float)(s_red[0][at][4 * g + i][lane] + s_red[1][at][4 * g + i][lane] + s_red[2][at][4 * g + i][lane] + s_red[3][at][4 * g + i][lane]); };
+            v[i] = sum(f) * xs * sa[m];
+            if (MODE == kI8Up) v[i] = silu_times(v[i], sum(NTF + f) * xs * sb[m]);
+            if (MODE == kI8Plain && A.bias) v[i] += A.bias[m];
+        }
+        i8_store4(A.out, (long)(row0 + row) * A.ldo + n, MODE == kI8Plain ? A.out_dtype : DYMOE_OUT_F32, left >= 4 && (MODE != kI8Plain || A.aligned), left, v);
+    }
 }
 
 // y[t] = sum over the slots, in their order, of gate times the pair's output.  A workgroup takes 2048 outputs of a token.
@@ -1135,8 +1244,7 @@ extern "C" int dymoe_matmul_int8(dymoe_ctx* ctx, const void* x, int x_dtype, con
     if (T > (1 << 24) || N > (1 << 24)) return DYMOE_ENOTSUP;
     const I8MatLayout L = i8_mat_layout(T, N, K);
     if (!coded && T > 0 && workspace_bytes < L.total) return DYMOE_ENOSPC;
-    const long blocks = ((T + kI8TileSmall - 1L) / kI8TileSmall) * ((N + 63L) / 64);
-    if (blocks > 0x7fffffffL) return DYMOE_ENOTSUP;
+    if (((T + 63L) / 64) * ((N + 31L) / 32) > 0x7fff0000L) return DYMOE_ENOTSUP;
     if (!ctx) return DYMOE_ENOCTX;
     if (T == 0) return DYMOE_OK;
     hipStream_t st = (hipStream_t)stream;
@@ -1182,13 +1290,15 @@ extern "C" int dymoe_matmul_int8(dymoe_ctx* ctx, const void* x, int x_dtype, con
         return DYMOE_OK;
     }
     A.aligned = dymoe_aligned(y, 4 * dtype_bytes(out_dtype)) && ldy % 4 == 0;
-    if (T > 32) {
+    if (T > 64) {
         const long tiles = (T + kI8TileRows - 1L) / kI8TileRows;
         const long units2 = tiles * ((N + 255L) / 256), units1 = tiles * ((N + 127L) / 128);
         if (units2 >= 2L * ctx->num_cu) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_matmul_kernel<2, 2>, i8_grid(units2, 1), dim3(256), kI8Lds<2>, st, A);
         else dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_matmul_kernel<1, 1>, i8_grid(units1, 1), dim3(256), kI8Lds<1>, st, A);
     } else {
-        dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_small_kernel<kI8Plain>, dim3((unsigned)blocks), dim3(256), 0, st, A);
+        const long strips = (N + 31L) / 32;
+        if (T <= 32) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_small_kernel<kI8Plain, 1, 8>, dim3((unsigned)strips), dim3(512), 0, st, A);
+        else dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_small_kernel<kI8Plain, 2, 8>, dim3((unsigned)((T + 63L) / 64 * strips)), dim3(512), 0, st, A);
     }
     DYMOE_HIP_LAUNCH_CHECK();
     return DYMOE_OK;
@@ -1215,7 +1325,7 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     if ((long)T * k > 0x7fffffffL / 4 || (long)T * up_to(H, 128) > 0xffffffffL) return DYMOE_ENOTSUP;      // (32-bit offsets into the codes)
     const I8FfnLayout L = i8_ffn_layout(T, H, F, E, k);
     if (workspace_bytes < L.total) return DYMOE_ENOSPC;
-    const long up = (long)L.max_tiles * ((F + 31L) / 32), down = (long)L.max_tiles * ((H + 63L) / 64);      // workgroups at most
+    const long up = (long)L.max_tiles * ((F + 31L) / 32), down = (long)L.max_tiles * ((H + 31L) / 32);      // workgroups at most
     if (up > 0x7fff0000L || down > 0x7fff0000L || T * ((H + 2047L) / 2048) > 0x7fffffffL) return DYMOE_ENOTSUP;
     if (!ctx) return DYMOE_ENOCTX;
     if (T == 0) return DYMOE_OK;
@@ -1255,14 +1365,21 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
         DYMOE_HIP_LAUNCH_CHECK();
         return DYMOE_OK;
     }
-    int rc = quantize_rows(ctx, x, x_dtype, T, H, H, 0, ws + L.xq, (float*)(ws + L.xs), st);
-    if (rc != DYMOE_OK) return rc;
-    int32_t* const plan = (int32_t*)(ws + L.plan);
     const bool small = T <= 32 || P <= 8L * E;
     // Workgroups at most: an expert of n pairs has n / 128 + 1 tall tiles at half as many column blocks, or one wide tile.
     const long tall = P / kI8TileRows + P / (kI8TileWide + 1), wide = E < P ? E : P;
-    dymoe_launch(ctx, DYMOE_K_INT8_PLAN, i8_plan_kernel, dim3(1), dim3(kI8PlanThreads), 0, st, idx, table, P, E, small ? 1 : 0, plan,
-                 ctx->device_flags);
+    int32_t* const plan = (int32_t*)(ws + L.plan);
+    int rc = DYMOE_OK;
+    if (H <= 16384) {
+        auto prep = i8_prep_launch<DYMOE_OUT_BF16>;
+        if (x_dtype == DYMOE_OUT_F32) prep = i8_prep_launch<DYMOE_OUT_F32>;
+        else if (x_dtype == DYMOE_OUT_F16) prep = i8_prep_launch<DYMOE_OUT_F16>;
+        prep(ctx, idx, table, P, E, small, plan, x, T, H, ws + L.xq, (float*)(ws + L.xs), st);
+    } else {
+        rc = quantize_rows(ctx, x, x_dtype, T, H, H, 0, ws + L.xq, (float*)(ws + L.xs), st);
+        if (rc != DYMOE_OK) return rc;
+        dymoe_launch(ctx, DYMOE_K_INT8_PLAN, i8_plan_kernel, dim3(1), dim3(kI8PlanThreads), 0, st, idx, table, P, E, (int)small, plan, ctx->device_flags);
+    }
     I8Args A = {};
     A.x = ws + L.xq;
     A.xs = (const float*)(ws + L.xs);
@@ -1276,7 +1393,7 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     A.E = E;
     A.k = k;
     A.rows = T;
-    if (small) dymoe_launch(ctx, DYMOE_K_INT8_UP, i8_small_kernel<kI8Up>, dim3((unsigned)up), dim3(256), 0, st, A);
+    if (small) dymoe_launch(ctx, DYMOE_K_INT8_UP, i8_small_kernel<kI8Up, 1, 4>, dim3((unsigned)up), dim3(256), 0, st, A);
     else dymoe_launch(ctx, DYMOE_K_INT8_UP, i8_experts_kernel<kI8Up>, i8_grid(tall * ((F + 127L) / 128) + wide * ((F + 63L) / 64), 2), dim3(256), kI8Lds<2>, st, A);
     rc = quantize_rows(ctx, ws + L.h, DYMOE_OUT_F32, P, F, (long)L.Fp, 0, ws + L.hq, (float*)(ws + L.hs), st);
     if (rc != DYMOE_OK) return rc;
@@ -1289,12 +1406,12 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     const bool half = !small && out_dtype == DYMOE_OUT_BF16;
     A.strip_scale = half ? (float*)(ws + L.strips) : nullptr;
     A.sum_scale = 32768.0f / (16129.0f * (float)F);
-    if (small) dymoe_launch(ctx, DYMOE_K_INT8_DOWN, i8_small_kernel<kI8Down>, dim3((unsigned)down), dim3(256), 0, st, A);
+    if (small) dymoe_launch(ctx, DYMOE_K_INT8_DOWN, i8_small_kernel<kI8Down, 1, 4>, dim3((unsigned)down), dim3(256), 0, st, A);
     else dymoe_launch(ctx, DYMOE_K_INT8_DOWN, i8_experts_kernel<kI8Down>, i8_grid(tall * ((H + 255L) / 256) + wide * ((H + 127L) / 128), 2), dim3(256), kI8Lds<2>, st, A);
     const dim3 grid((unsigned)(T * ((H + 2047L) / 2048)));
     auto combine = half ? i8_combine_kernel<true> : i8_combine_kernel<false>;
     dymoe_launch(ctx, DYMOE_K_INT8_COMBINE, combine, grid, dim3(256), 0, st, ws + L.part, (long)L.Hp, (const float*)(ws + L.hs),
-                 (const float*)(ws + L.strips), idx, i8_plan(plan, E, P).where, w, H, k, out_dtype,
+                 (const float*)(ws + L.strips), idx, i8_plan(plan, P).where, w, H, k, out_dtype,
                  H % 4 == 0 && dymoe_aligned(y, 4 * dtype_bytes(out_dtype)), y);
     DYMOE_HIP_LAUNCH_CHECK();
     return DYMOE_OK;

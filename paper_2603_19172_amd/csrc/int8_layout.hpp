@@ -39,7 +39,7 @@ static inline I8FfnLayout i8_ffn_layout(long T, long H, long F, long E, long k)
     L.hs = take(P * 4);
     L.part = take(P * L.Hp * 4);
     L.strips = take((size_t)E * ((size_t)H + 31) / 32 * 4 + (size_t)E * 4);
-    L.plan = take((8 + 2 * P + 8 * (size_t)L.max_tiles) * 4);
+    L.plan = take((8 + i8_round(2 * P, 4) + 20 * (size_t)L.max_tiles) * 4);        // (a tile's record: 80 bytes)
     L.total = at;
     return L;
 }
