@@ -44,22 +44,26 @@ __device__ __forceinline__ bool i8_present(const dymoe_expert_i8& x)
     return (x.q[0] != nullptr) & (x.q[1] != nullptr) & (x.q[2] != nullptr) & (x.s[0] != nullptr) & (x.s[1] != nullptr) & (x.s[2] != nullptr);
 }
 
-// Counting sort of the pairs by expert and the list of tiles, by one workgroup.  Experts come by falling number of pairs, so that the largest
-// tiles start first.  A pair's turn in its expert is what the counter held before it: kept in registers (in `where` beyond the first
-// kI8PlanKeep pairs of a thread) until the experts' first positions are known, so that there is one pass of atomics.  The turns
-// come in any order, and nothing that is computed depends on it.
+// Counting sort of the pairs by expert and the list of tiles, by one workgroup: tall tiles first, then wide ones, by expert.  A pair's turn
+// in its expert is what the counter held before it: kept in registers (in `where` beyond the first kI8PlanKeep pairs of a thread)
+// until the experts' first positions are known, so that there is one pass of atomics.  The turns come in any order, and nothing that is
+// computed depends on it.  The sorted pairs and the tiles' experts pass through LDS where they fit: written from the threads that
+// know them, 16384 pairs cost 7 us in stores of four bytes each, and an expert's sixteen records 3 us in one thread.
 constexpr int kI8PlanThreads = 1024;
 constexpr int kI8PlanKeep = 16;
+constexpr int kI8PlanPairs = kI8PlanKeep * kI8PlanThreads;
+constexpr int kI8PlanTiles = 4096;
+
+static_assert(kI8PlanThreads == DYMOE_MAX_EXPERTS, "a thread for every expert");
 
 struct I8PlanLds {
-    int count[DYMOE_MAX_EXPERTS], sorted[DYMOE_MAX_EXPERTS], at[DYMOE_MAX_EXPERTS], wave[2][kI8PlanThreads / kWave];
+    int count[DYMOE_MAX_EXPERTS], at[DYMOE_MAX_EXPERTS], tile0[DYMOE_MAX_EXPERTS], wave[3][kI8PlanThreads / kWave];
+    uint16_t owner[kI8PlanTiles], perm[kI8PlanPairs];
 };
 
 __device__ __forceinline__ void i8_make_plan(I8PlanLds& lds, const int32_t* __restrict__ idx, const dymoe_expert_i8* __restrict__ table, long P, int E,
                                              int small, int32_t* __restrict__ plan, unsigned* __restrict__ flags)
 {
-    int *const s_count = lds.count, *const s_sorted = lds.sorted, *const s_at = lds.at;
-    int (*const s_wave)[kI8PlanThreads / kWave] = lds.wave;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const I8Plan pp = i8_plan(plan, P);
     int e_of[kI8PlanKeep], turn[kI8PlanKeep];
@@ -69,72 +73,76 @@ __device__ __forceinline__ void i8_make_plan(I8PlanLds& lds, const int32_t* __re
         e_of[i] = p < P ? idx[p] : -1;
     }
     const bool held = tid < E && i8_present(table[tid]);
-    if (tid < E) s_count[tid] = 0;
+    lds.count[tid] = 0;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kI8PlanKeep; i++)
-        if ((unsigned)e_of[i] < (unsigned)E) turn[i] = atomicAdd(&s_count[e_of[i]], 1);
-    for (long p = tid + (long)kI8PlanKeep * kI8PlanThreads; p < P; p += kI8PlanThreads) {
+        if ((unsigned)e_of[i] < (unsigned)E) turn[i] = atomicAdd(&lds.count[e_of[i]], 1);
+    for (long p = tid + (long)kI8PlanPairs; p < P; p += kI8PlanThreads) {
         const int e = idx[p];
-        if ((unsigned)e < (unsigned)E) pp.where[p] = atomicAdd(&s_count[e], 1);
+        if ((unsigned)e < (unsigned)E) pp.where[p] = atomicAdd(&lds.count[e], 1);
     }
     __syncthreads();
-    int n = tid < E ? s_count[tid] : 0;
+    int n = lds.count[tid];
     if (n > 0 && !held) {
         atomicOr(flags, DYMOE_FLAG_FORMAT_MISSING);
         n = 0;
     }
-    if (tid < E) s_at[tid] = n;
-    __syncthreads();
-    if (tid < E) {
-        int rank = 0;
-        for (int e = 0; e < E; e++) {
-            const int o = s_at[e];
-            rank += (o > n) || (o == n && e < tid);
-        }
-        s_sorted[rank] = tid;
-    }
-    __syncthreads();
-    const int e = tid < E ? s_sorted[tid] : 0;
-    n = tid < E ? s_at[e] : 0;
     const bool one = !small && n <= kI8TileWide;             // a wide tile
     const int rows = small ? kI8TileSmall : one ? kI8TileWide : kI8TileRows, m = (n + rows - 1) / rows;
-    const int n_in = wave_scan_dpp_i32(n), t_in = wave_scan_dpp_i32(m);
+    const int n_in = wave_scan_dpp_i32(n), m2_in = wave_scan_dpp_i32(one ? 0 : m), m1_in = wave_scan_dpp_i32(one ? m : 0);
     if (lane == kWave - 1) {
-        s_wave[0][wave] = n_in;
-        s_wave[1][wave] = t_in;
+        lds.wave[0][wave] = n_in;
+        lds.wave[1][wave] = m2_in;
+        lds.wave[2][wave] = m1_in;
     }
     __syncthreads();
-    int n0 = n_in - n, t0 = t_in - m;
-    for (int w = 0; w < wave; w++) {
-        n0 += s_wave[0][w];
-        t0 += s_wave[1][w];
-    }
-    if (tid < E) {
-        s_at[e] = n > 0 ? n0 : -1;               // (every thread has read its count)
-        for (int i = 0; i < m; i++) {
-            I8TileRec t = {};
-            t.expert = e;
-            t.first = n0;
-            t.pairs = n;
-            t.tile0 = t0;
-            t.tiles = m;
-            t.mat = table[e];
-            pp.tiles[t0 + i] = t;
+    int n0 = n_in - n, t2 = m2_in, t1 = m1_in, all2 = 0, all1 = 0;
+    for (int w = 0; w < kI8PlanThreads / kWave; w++) {
+        const int a2 = lds.wave[1][w], a1 = lds.wave[2][w];
+        if (w < wave) {
+            n0 += lds.wave[0][w];
+            t2 += a2;
+            t1 += a1;
         }
+        all2 += a2;
+        all1 += a1;
     }
-    // (experts come by falling load: those of one wide tile are the last)
-    const int wide = __syncthreads_count(one && n > 0);
-    if (tid == kI8PlanThreads - 1) {
-        pp.meta[0] = t0 + m - wide;
-        pp.meta[1] = wide;
+    const int t0 = one ? all2 + t1 - m : t2 - m;
+    auto record = [&](int e, int first, int pairs, int tile0, int tiles) {
+        I8TileRec t = {};
+        t.expert = e;
+        t.first = first;
+        t.pairs = pairs;
+        t.tile0 = tile0;
+        t.tiles = tiles;
+        t.mat = table[e];
+        return t;
+    };
+    lds.at[tid] = n > 0 ? n0 : -1;
+    lds.count[tid] = n;
+    lds.tile0[tid] = t0;
+    for (int i = 0; i < m; i++) {
+        if (t0 + i < kI8PlanTiles) lds.owner[t0 + i] = (uint16_t)tid;
+        else pp.tiles[t0 + i] = record(tid, n0, n, t0, m);
+    }
+    if (tid == 0) {
+        pp.meta[0] = all2;
+        pp.meta[1] = all1;
     }
     __syncthreads();
+    for (int i = tid; i < min(all1 + all2, kI8PlanTiles); i += kI8PlanThreads) {
+        const int e = lds.owner[i], c = lds.count[e];
+        const int per = small ? kI8TileSmall : c <= kI8TileWide ? kI8TileWide : kI8TileRows;
+        pp.tiles[i] = record(e, lds.at[e], c, lds.tile0[e], (c + per - 1) / per);
+    }
+    const bool fits = P <= kI8PlanPairs;
     auto place = [&](long p, int x, int rank) {
         int at = -1;
-        if ((unsigned)x < (unsigned)E && s_at[x] >= 0) {
-            at = s_at[x] + rank;
-            pp.perm[at] = (int32_t)p;
+        if ((unsigned)x < (unsigned)E && lds.at[x] >= 0) {
+            at = lds.at[x] + rank;
+            if (fits) lds.perm[at] = (uint16_t)p;
+            else pp.perm[at] = (int32_t)p;
         }
         pp.where[p] = at;
     };
@@ -143,7 +151,12 @@ __device__ __forceinline__ void i8_make_plan(I8PlanLds& lds, const int32_t* __re
         const long p = tid + (long)i * kI8PlanThreads;
         if (p < P) place(p, e_of[i], turn[i]);
     }
-    for (long p = tid + (long)kI8PlanKeep * kI8PlanThreads; p < P; p += kI8PlanThreads) place(p, idx[p], pp.where[p]);
+    for (long p = tid + (long)kI8PlanPairs; p < P; p += kI8PlanThreads) place(p, idx[p], pp.where[p]);
+    if (!fits) return;
+    __syncthreads();
+    int sorted = 0;
+    for (int w = 0; w < kI8PlanThreads / kWave; w++) sorted += lds.wave[0][w];
+    for (int i = tid; i < sorted; i += kI8PlanThreads) pp.perm[i] = lds.perm[i];
 }
 
 // The plan by the first workgroup, the codes of the activations by the others, four rows each: neither needs the other, and a launch of its
