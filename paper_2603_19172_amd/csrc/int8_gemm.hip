@@ -234,7 +234,7 @@ struct I8Args {
     float* strip_scale;               // down projection with 16-bit outputs: [E][strips of 32 outputs]; null: 32-bit ones
     float sum_scale;                  // largest sum there can be -> 2^15
     long ldo, P;
-    int rows, Kp, N, E, k, out_dtype, aligned;     // aligned: the plain product's rows start where four outputs may be stored at once
+    int rows, Kp, N, E, k, out_dtype, aligned, tiled;     // aligned: the plain product's rows start where four outputs may be stored at once
 };
 
 // Memory that a wavefront's loads share a base in: the base in scalar registers, a lane's offset and the load's own in 32 bits each.
@@ -927,9 +927,8 @@ __device__ __forceinline__ void i8_strip(I8Src& to, const I8Args& A, const void*
 }
 
 template <int S>
-__device__ __forceinline__ bool i8_plain_unit(const I8Args& A, I8Unit<S>& u)
+__device__ __forceinline__ bool i8_plain_unit(const I8Args& A, I8Unit<S>& u, int wave)
 {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int cols = kI8Cols<kI8Plain, S>, nblk = (A.N + cols - 1) / cols, tiles = (A.rows + kI8TileRows - 1) / kI8TileRows;
     const long unit = i8_run() * kI8Run + i8_turn_in_run();
     if (unit >= (long)tiles * nblk) return false;
@@ -980,7 +979,7 @@ __global__ __launch_bounds__(256, S == 2 ? 2 : 4) void i8_matmul_kernel(const I8
     extern __shared__ __attribute__((aligned(1024))) char xs_raw[];
     constexpr uint32_t kBuf = (uint32_t)kI8TileRows * 128 * KT;
     I8Unit<S> u;
-    if (!i8_plain_unit<S>(A, u)) return;
+    if (!i8_plain_unit<S>(A, u, __builtin_amdgcn_readfirstlane(threadIdx.x / kWave))) return;
 #define DYMOE_I8_TILE(NTF) i8_tile<kI8Plain, NTF, S, KT>(A, nullptr, u.qw, u.sa, u.sb, u.row0, u.rows, u.bx, 0, lds_base(xs_raw), kBuf)
     // one instantiation per number of fragments of 32 rows: the accumulators then sit in fixed registers for the whole loop
     switch ((u.rows + 31) >> 5) {
@@ -990,6 +989,106 @@ __global__ __launch_bounds__(256, S == 2 ? 2 : 4) void i8_matmul_kernel(const I8
     default: DYMOE_I8_TILE(4); break;
     }
 #undef DYMOE_I8_TILE
+}
+
+// The plain product where its tiles are fewer than the chip takes: G groups of four wavefronts share a tile of 128 x 128 outputs and split K,
+// each with LDS buffers of its own; at the end a fragment after the other meets in LDS and the groups finish eight of its rows each.  (Alone on
+// a compute unit a step costs 0.8 us, the latency of its copies; 256 x 4096 outputs over 4096 columns took 32 of them.)
+template <int NTF, int G>
+__device__ __forceinline__ void i8_split_tile(const I8Args& A, const I8Unit<1>& u, int wave, int group, uint32_t xs_base)
+{
+    constexpr uint32_t kBuf = (uint32_t)kI8TileRows * 128;
+    const int lane = threadIdx.x & (kWave - 1), ln = lane & 31, kb = lane >> 5;
+    const uint32_t lane16 = (uint32_t)lane * 16u, own = xs_base + (uint32_t)group * 2u * kBuf;
+    const int nkt = A.Kp >> 7, per = (nkt + G - 1) / G, first = group * per;
+    const int tiles = max(0, min(per, nkt - first));
+    i32x16_t acc[1][NTF] = {};
+    I8Stage<NTF, 1> stage;
+    const int rb = 8 * wave + (lane >> 3);
+    const uint32_t chunk = (uint32_t)((lane & 7) ^ i8_turn<1>(rb)) * 16u;
+#pragma unroll
+    for (int i = 0; i < NTF; i++) stage.off[i] = (uint32_t)min(32 * i + rb, u.rows - 1) * (uint32_t)A.Kp + chunk;
+    stage.base = A.x + (long)u.row0 * A.Kp;
+    stage.lds = __builtin_amdgcn_readfirstlane(own + (uint32_t)wave * 1024u);
+    auto copy = [&](int k, uint32_t at) {
+        const char* const base = stage.base + (long)min(first + k, nkt - 1) * 128;       // (past a group's last: its bytes go unused)
+#pragma unroll
+        for (int i = 0; i < NTF; i++) lds_copy16(base, stage.off[i], stage.lds + at + (uint32_t)i * 4096u);
+    };
+    const uint32_t xa0 = own + (uint32_t)ln * 128u + (((uint32_t)kb << 6) ^ ((uint32_t)i8_turn<1>(ln) << 4));
+    I8Strips<1, 1> w;
+    copy(0, 0);
+#pragma unroll
+    for (int j = 0; j < 4; j++) w.r[0][j] = i8_chunk(u.qw[0], lane16, min(first, nkt - 1), j);
+    wait_lds_copies<0>();
+    __syncthreads();
+    uint32_t at = 0;
+    for (int k = 0; k < per; k++) {
+        if (k < tiles) {
+            copy(k + 1, at ^ kBuf);
+            i8_step<NTF, 1, 1, 1>(w, u.qw, lane16, first + k + 1, nkt, xa0 + at, acc);
+            wait_lds_copies<4>();               // the copies are older than the loads of weights
+        }
+        __syncthreads();
+        at ^= kBuf;
+    }
+    // fragments in turn: [group][wavefront][row of 32 sums]
+    const uint32_t area = xs_base + (uint32_t)(group * 4 + wave) * kI8EpiWave<1>;
+    const int n = (4 * u.bx + wave) * 32 + 4 * (lane & 7), left = A.N - n;
+    float sc[4], add[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        sc[i] = u.sa[min(n + i, A.N - 1)];
+        if (A.bias) add[i] = A.bias[min(n + i, A.N - 1)];
+    }
+#pragma unroll
+    for (int tf = 0; tf < NTF; tf++) {
+#pragma unroll
+        for (int g = 0; g < 4; g++)
+            lds_write16(area + (uint32_t)ln * kI8EpiRow<1> + (uint32_t)(kb * 16 + g * 32),
+                        make_uint4((uint32_t)acc[0][tf][4 * g], (uint32_t)acc[0][tf][4 * g + 1], (uint32_t)acc[0][tf][4 * g + 2], (uint32_t)acc[0][tf][4 * g + 3]));
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 4 / G; j++) {
+            const int rr = 8 * (group + G * j) + (lane >> 3), row = 32 * tf + rr;
+            uint32_t sum[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int g = 0; g < G; g++) {
+                const uint4 p = lds_read16(xs_base + (uint32_t)(g * 4 + wave) * kI8EpiWave<1> + (uint32_t)rr * kI8EpiRow<1> + (uint32_t)(lane & 7) * 16u);
+                sum[0] += p.x;
+                sum[1] += p.y;
+                sum[2] += p.z;
+                sum[3] += p.w;
+            }
+            if (row >= u.rows || left <= 0) continue;
+            const float xs = A.xs[u.row0 + row];
+            float v[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) v[i] = (float)(int)sum[i] * xs * sc[i] + add[i];
+            i8_store4(A.out, (long)(u.row0 + row) * A.ldo + n, A.out_dtype, left >= 4 && A.aligned, left, v);
+        }
+        __syncthreads();
+    }
+}
+
+template <int G>
+constexpr int kI8SplitLds = G * 2 * kI8TileRows * 128;
+
+template <int G>
+__global__ __launch_bounds__(256 * G, 4) void i8_split_kernel(const I8Args A)
+{
+    extern __shared__ __attribute__((aligned(1024))) char xs_raw[];
+    static_assert(4 * G * kI8EpiWave<1> <= kI8SplitLds<G>, "the epilogue areas fit in the buffers");
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    I8Unit<1> u;
+    if (!i8_plain_unit<1>(A, u, wave & 3)) return;
+    const uint32_t xs = lds_base(xs_raw);
+    switch ((u.rows + 31) >> 5) {
+    case 1: i8_split_tile<1, G>(A, u, wave & 3, wave >> 2, xs); break;
+    case 2: i8_split_tile<2, G>(A, u, wave & 3, wave >> 2, xs); break;
+    case 3: i8_split_tile<3, G>(A, u, wave & 3, wave >> 2, xs); break;
+    default: i8_split_tile<4, G>(A, u, wave & 3, wave >> 2, xs); break;
+    }
 }
 
 // Experts.  One that more than kI8TileWide pairs go to takes tiles of 128 rows and two strips a wavefront; the others, whose weights' bytes
@@ -1050,6 +1149,7 @@ int i8_init()
     auto allow = [](const void* f, int bytes) { return hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess; };
     bool ok = allow((const void*)i8_matmul_kernel<2, 2>, kI8Lds<2>) && allow((const void*)i8_experts_kernel<kI8Up>, kI8Lds<2>) &&
               allow((const void*)i8_experts_kernel<kI8Down>, kI8Lds<2>);
+    ok = ok && allow((const void*)i8_split_kernel<2>, kI8SplitLds<2>) && allow((const void*)i8_split_kernel<4>, kI8SplitLds<4>);
     ok = ok && allow((const void*)i8_thin_kernel<kI8Plain, true>, (int)kI8FuseBytes) && allow((const void*)i8_thin_kernel<kI8Up, true>, (int)kI8FuseBytes) &&
          allow((const void*)i8_thin_down_kernel, (int)kI8FuseBytes);
     return ok ? DYMOE_OK : DYMOE_EHIP;
@@ -1064,9 +1164,11 @@ static dim3 i8_grid(long units, int kinds)
 // ----------------------------------------------------------------------------
 // Tiles of up to 32 NTF rows where rows or columns are too few for the shapes above (decode batches on experts, narrow matrices): a workgroup
 // owns 32 weight rows (of W1 and of W3 in the up projection) and its NW wavefronts take the 128-column tiles of K in turn.  Nothing is
-// shared before the end: weights and codes come straight into registers, a tile ahead, and the sums meet in LDS.
-template <int MODE, int NTF, int NW>
-__global__ __launch_bounds__(64 * NW) void i8_small_kernel(const I8Args A)
+// shared before the end: weights and codes come straight into registers, D tiles of a wavefront on their way, and the sums meet in LDS.
+// A load of codes that lie row by row touches a line for each of its 64 lanes; the plain product therefore has its rows quantised into
+// the weights' tile layout (A.tiled), where it is 1 KiB of contiguous memory.
+template <int MODE, int NTF, int NW, int D>
+__global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void i8_small_kernel(const I8Args A)
 {
     constexpr int S = MODE == kI8Up ? 2 : 1, kSums = S * NTF, kRows = 32 * NTF;
     __shared__ int s_red[4][kSums][16][kWave];
@@ -1104,6 +1206,8 @@ __global__ __launch_bounds__(64 * NW) void i8_small_kernel(const I8Args A)
     const uint32_t lane16 = (uint32_t)lane * 16u;
     uint32_t off[NTF];
     const int nkt = A.Kp >> 7;
+    // bytes from one 16-byte chunk of a lane's columns to the next, and from one tile to the next
+    const uint32_t chunk = MODE == kI8Plain && A.tiled ? 1024u : 16u, step = MODE == kI8Plain && A.tiled ? 4096u : 128u;
     auto load_w = [&](Tile& t, int kt) {
 #pragma unroll
         for (int s = 0; s < S; s++)
@@ -1114,18 +1218,23 @@ __global__ __launch_bounds__(64 * NW) void i8_small_kernel(const I8Args A)
 #pragma unroll
         for (int f = 0; f < NTF; f++)
 #pragma unroll
-            for (int c = 0; c < 4; c++) t.x[f][c] = x.load(off[f] + (uint32_t)(c * 16), (uint32_t)kt * 128u);
+            for (int c = 0; c < 4; c++) t.x[f][c] = x.load(off[f], (uint32_t)kt * step + (uint32_t)c * chunk);
     };
-    Tile a, b;
+    Tile ring[D];
     int kt = wave;
-    if (kt < nkt) load_w(a, kt);               // (the weights need nothing of the rows)
+#pragma unroll
+    for (int d = 0; d < D; d++)
+        if (kt + d * NW < nkt) load_w(ring[d], kt + d * NW);               // (the weights need nothing of the rows)
 #pragma unroll
     for (int f = 0; f < NTF; f++) {
         const int r = min(32 * f + ln, rows - 1);                            // rows behind the last: computed and dropped
         off[f] = (MODE == kI8Up ? (uint32_t)(pp.perm[row0 + r] / A.k) : (uint32_t)r) * (uint32_t)A.Kp + 64u * (uint32_t)kb;
+        if (MODE == kI8Plain && A.tiled) off[f] = (uint32_t)min(f, (rows - 1) >> 5) * (uint32_t)strip + lane16;
     }
-    x.set(A.x + (MODE == kI8Up ? 0 : (long)row0 * A.Kp), (uint32_t)(MODE == kI8Up ? A.rows : rows) * (uint32_t)A.Kp);
-    if (kt < nkt) load_x(a, kt);
+    x.set(A.x + (MODE == kI8Up ? 0 : (long)row0 * A.Kp), (uint32_t)(MODE == kI8Up ? A.rows : MODE == kI8Plain && A.tiled ? (rows + 31) & ~31 : rows) * (uint32_t)A.Kp);
+#pragma unroll
+    for (int d = 0; d < D; d++)
+        if (kt + d * NW < nkt) load_x(ring[d], kt + d * NW);
     i32x16_t acc[S][NTF] = {};
     auto multiply = [&](const Tile& t) {
 #pragma unroll
@@ -1136,21 +1245,19 @@ __global__ __launch_bounds__(64 * NW) void i8_small_kernel(const I8Args A)
                 for (int f = 0; f < NTF; f++) acc[s][f] = mfma_i8(t.w[s][c], t.x[f][c], acc[s][f]);
     };
     while (kt < nkt) {
-        if (kt + NW < nkt) {
-            load_w(b, kt + NW);
-            load_x(b, kt + NW);
+#pragma unroll
+        for (int d = 0; d < D; d++) {
+            if (kt < nkt) {
+                multiply(ring[d]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (kt + D * NW < nkt) {
+                    load_w(ring[d], kt + D * NW);
+                    load_x(ring[d], kt + D * NW);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            kt += NW;
         }
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(a);
-        kt += NW;
-        if (kt >= nkt) break;
-        if (kt + NW < nkt) {
-            load_w(a, kt + NW);
-            load_x(a, kt + NW);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(b);
-        kt += NW;
     }
     auto put = [&](int at) {
 #pragma unroll
@@ -1262,12 +1369,13 @@ extern "C" int dymoe_matmul_int8(dymoe_ctx* ctx, const void* x, int x_dtype, con
     if (T == 0) return DYMOE_OK;
     hipStream_t st = (hipStream_t)stream;
     char* const ws = (char*)workspace;
-    const bool thin = T <= kI8ThinRows, fuse = thin && !coded && T <= kI8FuseRows && T * (long)(L.Kp + 16) <= kI8FuseBytes;
+    const bool thin = T <= kI8ThinRows, small = !thin && ((T + 63L) / 64) * ((N + 31L) / 32) <= ctx->num_cu * 5L / 4, fuse = thin && !coded && T <= kI8FuseRows && T * (long)(L.Kp + 16) <= kI8FuseBytes;
     I8Args A = {};
     A.x = (const char*)x;
     A.xs = x_scale;
     if (!coded && !fuse) {
-        const int rc = quantize_rows(ctx, x, x_dtype, T, K, ldx, 0, ws + L.xq, (float*)(ws + L.xs), st);
+        A.tiled = small;
+        const int rc = quantize_rows(ctx, x, x_dtype, T, K, ldx, small, ws + L.xq, (float*)(ws + L.xs), st);
         if (rc != DYMOE_OK) return rc;
         A.x = ws + L.xq;
         A.xs = (const float*)(ws + L.xs);
@@ -1303,15 +1411,18 @@ extern "C" int dymoe_matmul_int8(dymoe_ctx* ctx, const void* x, int x_dtype, con
         return DYMOE_OK;
     }
     A.aligned = dymoe_aligned(y, 4 * dtype_bytes(out_dtype)) && ldy % 4 == 0;
-    if (T > 64) {
+    if (!small) {
         const long tiles = (T + kI8TileRows - 1L) / kI8TileRows;
         const long units2 = tiles * ((N + 255L) / 256), units1 = tiles * ((N + 127L) / 128);
-        if (units2 >= 2L * ctx->num_cu) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_matmul_kernel<2, 2>, i8_grid(units2, 1), dim3(256), kI8Lds<2>, st, A);
-        else dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_matmul_kernel<1, 1>, i8_grid(units1, 1), dim3(256), kI8Lds<1>, st, A);
+        const long cu = ctx->num_cu;
+        if (units1 <= cu && L.Kp >= 1024) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_split_kernel<4>, i8_grid(units1, 1), dim3(1024), kI8SplitLds<4>, st, A);
+        else if (units1 <= cu * 5 / 4) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_split_kernel<2>, i8_grid(units1, 1), dim3(512), kI8SplitLds<2>, st, A);
+        else if (units2 < 2 * cu || L.Kp < 2048) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_matmul_kernel<1, 1>, i8_grid(units1, 1), dim3(256), kI8Lds<1>, st, A);
+        else dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_matmul_kernel<2, 2>, i8_grid(units2, 1), dim3(256), kI8Lds<2>, st, A);
     } else {
         const long strips = (N + 31L) / 32;
-        if (T <= 32) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_small_kernel<kI8Plain, 1, 8>, dim3((unsigned)strips), dim3(512), 0, st, A);
-        else dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_small_kernel<kI8Plain, 2, 8>, dim3((unsigned)((T + 63L) / 64 * strips)), dim3(512), 0, st, A);
+        if (T <= 32) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_small_kernel<kI8Plain, 1, 8, 4>, dim3((unsigned)strips), dim3(512), 0, st, A);
+        else dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_small_kernel<kI8Plain, 2, 8, 3>, dim3((unsigned)((T + 63L) / 64 * strips)), dim3(512), 0, st, A);
     }
     DYMOE_HIP_LAUNCH_CHECK();
     return DYMOE_OK;
@@ -1406,7 +1517,7 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     A.E = E;
     A.k = k;
     A.rows = T;
-    if (small) dymoe_launch(ctx, DYMOE_K_INT8_UP, i8_small_kernel<kI8Up, 1, 4>, dim3((unsigned)up), dim3(256), 0, st, A);
+    if (small) dymoe_launch(ctx, DYMOE_K_INT8_UP, i8_small_kernel<kI8Up, 1, 4, 1>, dim3((unsigned)up), dim3(256), 0, st, A);
     else dymoe_launch(ctx, DYMOE_K_INT8_UP, i8_experts_kernel<kI8Up>, i8_grid(tall * ((F + 127L) / 128) + wide * ((F + 63L) / 64), 2), dim3(256), kI8Lds<2>, st, A);
     rc = quantize_rows(ctx, ws + L.h, DYMOE_OUT_F32, P, F, (long)L.Fp, 0, ws + L.hq, (float*)(ws + L.hs), st);
     if (rc != DYMOE_OK) return rc;
@@ -1419,7 +1530,7 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     const bool half = !small && out_dtype == DYMOE_OUT_BF16;
     A.strip_scale = half ? (float*)(ws + L.strips) : nullptr;
     A.sum_scale = 32768.0f / (16129.0f * (float)F);
-    if (small) dymoe_launch(ctx, DYMOE_K_INT8_DOWN, i8_small_kernel<kI8Down, 1, 4>, dim3((unsigned)down), dim3(256), 0, st, A);
+    if (small) dymoe_launch(ctx, DYMOE_K_INT8_DOWN, i8_small_kernel<kI8Down, 1, 4, 1>, dim3((unsigned)down), dim3(256), 0, st, A);
     else dymoe_launch(ctx, DYMOE_K_INT8_DOWN, i8_experts_kernel<kI8Down>, i8_grid(tall * ((H + 255L) / 256) + wide * ((H + 127L) / 128), 2), dim3(256), kI8Lds<2>, st, A);
     const dim3 grid((unsigned)(T * ((H + 2047L) / 2048)));
     auto combine = half ? i8_combine_kernel<true> : i8_combine_kernel<false>;

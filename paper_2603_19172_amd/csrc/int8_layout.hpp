@@ -46,7 +46,7 @@ static inline I8FfnLayout i8_ffn_layout(long T, long H, long F, long E, long k)
 
 struct I8MatLayout {
     size_t Kp;
-    size_t xq, xs;     // [T, Kp] codes and [T] scales of the activations
+    size_t xq, xs;     // [T up to a multiple of 32, Kp] codes and [T] scales of the activations
     size_t total;
 };
 
@@ -56,7 +56,7 @@ static inline I8MatLayout i8_mat_layout(long T, long N, long K)
     I8MatLayout L;
     L.Kp = i8_round((size_t)K, 128);
     L.xq = 0;
-    L.xs = i8_round((size_t)T * L.Kp, 256);
+    L.xs = i8_round(i8_round((size_t)T, 32) * L.Kp, 256);
     L.total = L.xs + i8_round((size_t)T * 4, 256);
     return L;
 }
