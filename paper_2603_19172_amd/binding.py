@@ -229,48 +229,56 @@ def _ptr(t, dtype=None):
 
 
 _OUT_OF = {torch.bfloat16: OUT_BF16, torch.float32: OUT_F32, torch.float16: OUT_F16}
+_IN_OF = {**_OUT_OF, torch.int8: DTYPE_I8}
 _TORCH_OUT = {v: t for t, v in _OUT_OF.items()}
+_current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
-def _out_dtype(dtype):
-    if dtype not in _OUT_OF:
-        raise TypeError("expected bfloat16, float32 or float16, got %s" % dtype)
-    return _OUT_OF[dtype]
-
-
-def _shape(name, t, shape):
-    if t is not None and t.shape != shape:
-        raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
-
-
-def _here(device, *tensors):
-    """The launch goes to the current device with the tensors' addresses: both have to be the context's."""
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise ValueError("tensor on %s, the context is of device %d" % (t.device, device))
-    if torch._C._cuda_getDevice() != device:
-        raise ValueError("the context is of device %d, device %d is current" % (device, torch.cuda.current_device()))
+def _dtype_code(t, codes=_OUT_OF):
+    code = codes.get(t.dtype)
+    if code is None:
+        raise TypeError("expected bfloat16, float32 or float16, got %s" % t.dtype)
+    return code
 
 
 def _up(n, m):
     return (n + m - 1) // m * m
 
 
-def _pitch(t):
-    """Values from one row of a matrix to the next."""
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
-
-
-def _rows_ptr(t):
-    """Device pointer of a matrix whose rows may lie apart."""
-    if t.dim() != 2 or t.shape[1] > 1 and t.stride(1) != 1 or _pitch(t) < t.shape[1]:
+def _matrix(t):
+    """(rows, columns, values from row to row) of a matrix whose rows may lie apart."""
+    rows, cols = t.shape
+    pitch, step = t.stride()
+    if rows <= 1:
+        pitch = cols or 1
+    if step != 1 and cols > 1 or pitch < cols:
         raise ValueError("expected a matrix with contiguous columns and rows that do not overlap")
+    return rows, cols, pitch
+
+
+def _at(t, device, dtype=None, shape=None):
+    """Device pointer of a tensor on the context's device (None -> NULL); with a shape, of a contiguous one of that shape."""
+    if t is None:
+        return None
+    if dtype is not None and t.dtype is not dtype:
+        raise TypeError("expected %s, got %s" % (dtype, t.dtype))
+    if shape is not None and (t.shape != shape or not t.is_contiguous()):
+        raise ValueError("expected a contiguous tensor of shape %s, got %s" % (tuple(shape), tuple(t.shape)))
+    if t.get_device() != device:
+        raise ValueError("tensor on %s, the context is of device %d" % (t.device, device))
     return t.data_ptr()
+
+
+def _stream_of(device, stream):
+    """The stream's handle.  A launch goes to the current device: it has to be the context's."""
+    if _current_device() != device:
+        raise ValueError("the context is of device %d, device %d is current" % (device, _current_device()))
+    return _raw_stream(device) if stream is None else _stream(stream)
 
 
 def _stream(stream):
     if stream is None:      # (torch.cuda.current_stream() makes an object first: 2.9 us of a call's 10.7)
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        return _raw_stream(_current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -560,74 +568,63 @@ class Context:
     def route_scored(self, logits, k, bias=None, score=SCORE_SIGMOID, groups=1, top_groups=1, group_best=1, renorm=True,
                      factor=1.0, idx=None, w=None, scores=None, stream=None):
         """logits [T, E] bf16 / fp16 / fp32 -> idx [T, k] int32, w [T, k] fp32; scores: a [T, E] fp32 tensor to fill."""
-        (T, E), dtype = logits.shape, _out_dtype(logits.dtype)
+        (T, E), dev, dtype = logits.shape, self.device, _dtype_code(logits)
         if idx is None:
             idx = torch.empty((T, k), dtype=torch.int32, device=logits.device)
         if w is None:
             w = torch.empty((T, k), dtype=torch.float32, device=logits.device)
-        _shape("bias", bias, (E,))
-        _shape("idx", idx, (T, k))
-        _shape("w", w, (T, k))
-        _shape("scores", scores, (T, E))
-        _here(self.device, logits, bias, idx, w, scores)
-        _check(lib.dymoe_route_scored(self._h, _ptr(logits), dtype, _ptr(bias, torch.float32), T, E, k, score,
-                                      groups, top_groups, group_best, 1 if renorm else 0, float(factor), _ptr(idx, torch.int32),
-                                      _ptr(w, torch.float32), _ptr(scores, torch.float32), _stream(stream)), "dymoe_route_scored")
+        _check(lib.dymoe_route_scored(self._h, _at(logits, dev, None, (T, E)), dtype, _at(bias, dev, torch.float32, (E,)), T, E, k, score,
+                                      groups, top_groups, group_best, 1 if renorm else 0, factor, _at(idx, dev, torch.int32, (T, k)),
+                                      _at(w, dev, torch.float32, (T, k)), _at(scores, dev, torch.float32, (T, E)),
+                                      _stream_of(dev, stream)), "dymoe_route_scored")
         return idx, w
 
     def quantize_rows(self, x, layout=LAYOUT_ROWMAJOR, out=None, stream=None):
         """x [rows, K] bf16 / fp16 / fp32, columns contiguous -> (int8 codes, fp32 scale [rows])."""
-        rows, K = x.shape
+        (rows, K, pitch), dev = _matrix(x), self.device
         shape = (_up(rows, 32) if layout == LAYOUT_TILE else rows, _up(K, 128))
         if out is None:
             out = (torch.empty(shape, dtype=torch.int8, device=x.device), torch.empty((rows,), dtype=torch.float32, device=x.device))
-        codes, scale = out
-        _shape("codes", codes, shape)
-        _shape("scale", scale, (rows,))
-        _here(self.device, x, codes, scale)
-        _check(lib.dymoe_quantize_rows(self._h, _rows_ptr(x), _out_dtype(x.dtype), rows, K, _pitch(x), layout,
-                                       _ptr(codes, torch.int8), _ptr(scale, torch.float32), _stream(stream)), "dymoe_quantize_rows")
+        _check(lib.dymoe_quantize_rows(self._h, _at(x, dev), _dtype_code(x), rows, K, pitch, layout, _at(out[0], dev, torch.int8, shape),
+                                       _at(out[1], dev, torch.float32, (rows,)), _stream_of(dev, stream)), "dymoe_quantize_rows")
         return out
 
     def matmul_int8(self, x, w, x_scale=None, bias=None, out_dtype=OUT_BF16, y=None, workspace=None, stream=None):
         """x [T, K] bf16 / fp16 / fp32, or int8 codes [T, Kp] with x_scale [T]; w: (codes, scale [N]) in the tile layout.
         Returns y [T, N], of the type of `y` where that is given."""
         codes, scale = w
-        (T, K), N = x.shape, scale.shape[0]
-        coded = x.dtype == torch.int8
-        _shape("w", codes, (_up(N, 32), _up(K, 128)))
-        _shape("bias", bias, (N,))
-        if coded:
-            _shape("x", x, (T, _up(K, 128)))
-            _shape("x_scale", x_scale, (T,))
+        (T, K, pitch), N, dev, dtype = _matrix(x), scale.shape[0], self.device, _dtype_code(x, _IN_OF)
+        if dtype == DTYPE_I8:
+            if K % 128 or x_scale is None:
+                raise ValueError("int8 codes come as quantize_rows wrote them, with their scales")
+        elif workspace is None:
+            workspace = torch.empty((matmul_int8_workspace_bytes(T, N, K),), dtype=torch.uint8, device=x.device)
         if y is None:
             y = torch.empty((T, N), dtype=_TORCH_OUT[out_dtype], device=x.device)
-        _shape("y", y, (T, N))
-        if workspace is None and not coded:
-            workspace = torch.empty((matmul_int8_workspace_bytes(T, N, K),), dtype=torch.uint8, device=x.device)
-        _here(self.device, x, codes, scale, x_scale, bias, y, workspace)
-        _check(lib.dymoe_matmul_int8(self._h, _rows_ptr(x), DTYPE_I8 if coded else _out_dtype(x.dtype), _ptr(x_scale, torch.float32),
-                                     _pitch(x), _ptr(codes, torch.int8), _ptr(scale, torch.float32), _ptr(bias, torch.float32), T, N, K,
-                                     _out_dtype(y.dtype), _rows_ptr(y), _pitch(y), _ptr(workspace, torch.uint8),
-                                     0 if workspace is None else workspace.numel(), _stream(stream)), "dymoe_matmul_int8")
+        rows, cols, ldy = _matrix(y)
+        if rows != T or cols != N:
+            raise ValueError("y has shape %s, expected %s" % (tuple(y.shape), (T, N)))
+        _check(lib.dymoe_matmul_int8(self._h, _at(x, dev), dtype, _at(x_scale, dev, torch.float32, (T,)), pitch,
+                                     _at(codes, dev, torch.int8, (_up(N, 32), _up(K, 128))), _at(scale, dev, torch.float32, (N,)),
+                                     _at(bias, dev, torch.float32, (N,)), T, N, K, _dtype_code(y), _at(y, dev), ldy,
+                                     _at(workspace, dev, torch.uint8), 0 if workspace is None else workspace.numel(),
+                                     _stream_of(dev, stream)), "dymoe_matmul_int8")
         return y
 
     def moe_ffn_int8(self, x, idx, w, table, F, out_dtype=OUT_BF16, y=None, workspace=None, stream=None):
         """x [T, H] bf16 / fp16 / fp32; idx, w [T, k]; table: make_int8_table's.  Returns y [T, H]."""
-        T, H = x.shape
-        k = idx.shape[1]
+        (T, H), k, dev = x.shape, idx.shape[1], self.device
         E = table.numel() * table.element_size() // C.sizeof(ExpertI8)
-        _shape("idx", idx, (T, k))
-        _shape("w", w, (T, k))
+        if not table.is_contiguous():
+            raise ValueError("the table has to be contiguous")
         if y is None:
             y = torch.empty((T, H), dtype=_TORCH_OUT[out_dtype], device=x.device)
-        _shape("y", y, (T, H))
         if workspace is None:
             workspace = torch.empty((moe_ffn_int8_workspace_bytes(T, H, F, E, k),), dtype=torch.uint8, device=x.device)
-        _here(self.device, x, idx, w, table, y, workspace)
-        _check(lib.dymoe_moe_ffn_int8(self._h, _ptr(x), _out_dtype(x.dtype), _ptr(idx, torch.int32), _ptr(w, torch.float32),
-                                      _ptr(table), T, H, F, E, k, _out_dtype(y.dtype), _ptr(y), _ptr(workspace, torch.uint8),
-                                      workspace.numel(), _stream(stream)), "dymoe_moe_ffn_int8")
+        _check(lib.dymoe_moe_ffn_int8(self._h, _at(x, dev, None, (T, H)), _dtype_code(x), _at(idx, dev, torch.int32, (T, k)),
+                                      _at(w, dev, torch.float32, (T, k)), _at(table, dev), T, H, F, E, k, _dtype_code(y),
+                                      _at(y, dev, None, (T, H)), _at(workspace, dev, torch.uint8), workspace.numel(),
+                                      _stream_of(dev, stream)), "dymoe_moe_ffn_int8")
         return y
 
     # -- S5

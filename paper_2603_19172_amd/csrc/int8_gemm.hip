@@ -273,8 +273,9 @@ __device__ __forceinline__ float silu_times(float a, float u) { return a * __bui
 constexpr int kI8Ahead = 4;
 constexpr int kI8ThinRows = 16;
 constexpr int kI8ThinWaves = 8;
-constexpr int kI8FuseRows = 4;                  // rows up to which a workgroup quantises them itself
-constexpr long kI8FuseBytes = 64 * 1024;        // and the codes' bytes in LDS
+constexpr int kI8FuseRows = 4;                  // tokens up to which the experts' workgroups quantise rows themselves
+constexpr long kI8FuseBytes = 64 * 1024;        // the codes' bytes in LDS at most
+constexpr long kI8FuseReads = 16 << 20;         // values that the workgroups of a plain product read to quantise them, together, at most
 
 typedef int i32x4acc_t __attribute__((ext_vector_type(4)));
 
@@ -335,6 +336,21 @@ template <int DT>
 __device__ __forceinline__ void i8_rows_to_lds(const char* x, long pitch, int rows, int K, int Kp, char* s_codes, float* s_scale, uint32_t* s_max)
 {
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, n = blockDim.x, waves = n / kWave;
+    if (2 * rows >= waves || K <= 1024) {           // a wavefront a row: nothing to hand over
+        for (int r = wave; r < rows; r += waves) {
+            uint32_t m = 0;
+#pragma unroll 2
+            for (int col = lane * 8; col < K; col += kWave * 8) m = peak8<DT>(load8<DT>(x + r * pitch, col, K), m);
+            float sc;
+            const RowQ q = row_q(peak_value<DT>(wave_max_u32(peak_bits<DT>(m))), sc);
+            if (lane == 0) s_scale[r] = sc;
+#pragma unroll 2
+            for (int col = lane * 8; col < Kp; col += kWave * 8)
+                *(uint2*)(s_codes + (long)r * (Kp + 16) + col) = codes8<DT>(load8<DT>(x + r * pitch, col, K), q);
+        }
+        __syncthreads();
+        return;
+    }
     for (int r = 0; r < rows; r++) {
         uint32_t m = 0;
         for (int col = tid * 8; col < K; col += n * 8) m = peak8<DT>(load8<DT>(x + r * pitch, col, K), m);
@@ -378,13 +394,13 @@ struct I8ThinArgs {
 // The plain product of up to 16 rows, and the up projection of up to 64 pairs: the workgroup of a pair that comes first among those of its
 // expert (or 16, 32, ... behind the first) takes the next sixteen of them.
 template <int MODE, bool FUSE>
-__global__ __launch_bounds__(64 * kI8ThinWaves) void i8_thin_kernel(const I8ThinArgs A)
+__global__ __launch_bounds__(64 * kI8ThinWaves, 4) void i8_thin_kernel(const I8ThinArgs A)
 {
     constexpr int S = MODE == kI8Up ? 2 : 1;
     extern __shared__ __attribute__((aligned(16))) char s_codes[];
     __shared__ int s_sum[kI8ThinWaves][S][4][kWave];
     __shared__ float s_scale[kI8ThinRows];
-    __shared__ uint32_t s_max[kI8FuseRows * kI8ThinWaves];
+    __shared__ uint32_t s_max[kI8ThinRows * kI8ThinWaves];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int ln = lane & 15;
     const int nblk = (A.N + 15) / 16;
@@ -1369,7 +1385,7 @@ extern "C" int dymoe_matmul_int8(dymoe_ctx* ctx, const void* x, int x_dtype, con
     if (T == 0) return DYMOE_OK;
     hipStream_t st = (hipStream_t)stream;
     char* const ws = (char*)workspace;
-    const bool thin = T <= kI8ThinRows, small = !thin && ((T + 63L) / 64) * ((N + 31L) / 32) <= ctx->num_cu * 5L / 4, fuse = thin && !coded && T <= kI8FuseRows && T * (long)(L.Kp + 16) <= kI8FuseBytes;
+    const bool thin = T <= kI8ThinRows, small = !thin && ((T + 63L) / 64) * ((N + 31L) / 32) <= ctx->num_cu * 5L / 4, fuse = thin && !coded && T * (long)(L.Kp + 16) <= kI8FuseBytes && (N + 15L) / 16 * T * K <= kI8FuseReads;
     I8Args A = {};
     A.x = (const char*)x;
     A.xs = x_scale;
