@@ -73,11 +73,12 @@ def matmul(xq, xs, wq, ws):
 
 
 def moe_ffn(x, idx, gate, experts, eps_h):
-    """experts: per expert None or three (codes, scale) pairs, row-major.  Returns y [T, H] and, beside it, a bound on what a
-    kernel may be off where the intermediate carries a relative error of eps_h: see tests/test_gpu_int8.py."""
+    """experts: per expert None or three (codes, scale) pairs, row-major.  Returns y [T, H]; a bound on what a kernel may be off
+    where the intermediate carries a relative error of eps_h, that a chance of 2e-9 an output exceeds; its mean square; and what it
+    may be off beside that where the pairs' outputs are rounded to fp16.  tests/test_gpu_int8.py derives them."""
     T, H = x.shape
     xq, xs = quantize_rows(x)
-    y, var, drift = np.zeros((T, H)), np.zeros((T, H)), np.zeros((T, H))
+    y, var, drift, half, most = (np.zeros((T, H)) for _ in range(5))
     for t in range(T):
         for j, e in enumerate(idx[t]):
             if not 0 <= e < len(experts) or experts[e] is None:
@@ -93,5 +94,9 @@ def moe_ffn(x, idx, gate, experts, eps_h):
             o = w2 @ hv
             y[t] += g * o
             drift[t] += abs(g) * np.abs(o) * eps_h
-            var[t] += g * g * (w2 ** 2 @ np.minimum(2.0 * eps_h * np.abs(h) * step + (eps_h * hv) ** 2, (2 * step) ** 2))
-    return y, 6.0 * np.sqrt(var) + drift
+            half[t] += abs(g) * (np.abs(o) * 2.0 ** -11 + 2.0 ** -40 * 127 * 127 * h.size * step * float(s2.max()))
+            var[t] += g * g * (w2 ** 2 @ (2.0 * eps_h * np.abs(h) * step))
+            most[t] = np.maximum(most[t], abs(g) * step * np.abs(w2).max(axis=1))
+    rare = math.log(2.0 / 2e-9)
+    bound = most * rare / 3.0 + np.sqrt((most * rare / 3.0) ** 2 + 2.0 * var * rare)
+    return y, bound * (eps_h > 0) + drift, var + drift ** 2, half

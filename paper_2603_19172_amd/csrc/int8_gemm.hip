@@ -733,9 +733,8 @@ __device__ __forceinline__ void i8_finish(const I8Args& A, const int32_t* perm, 
             m = fmaxf(m, __shfl_xor(m, 1, kWave));
             m = fmaxf(m, __shfl_xor(m, 2, kWave));
             m = fmaxf(m, __shfl_xor(m, 4, kWave));
-            const float c = m > 0.0f ? A.sum_scale / m : 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; i++) sc[i] *= c;
+            for (int i = 0; i < 4; i++) sc[i] = m > 0.0f ? A.sum_scale * (sc[i] / m) : 0.0f * sc[i];      // (a scale that is NaN stays)
             if (left > 0 && (lane & 7) == 0 && lane < kOut)      // (every tile of an expert writes the same)
                 A.strip_scale[(long)expert * ((A.N + 31) / 32) + n / 32] = m / A.sum_scale;
         }

@@ -199,3 +199,38 @@ class MoELayer:
             self.quantize(store, st)
         self.ffn(x, store, st)
         return self.y
+
+
+class Int8Experts:
+    """A layer's experts in 8-bit integers, a scale a channel: quantised and laid out once from bf16 (or fp16, fp32) matrices, with
+    the dymoe_expert_i8 table that points at them.  An expert given as None has no entry: its tokens' pairs are left out."""
+
+    def __init__(self, ctx, w, device):
+        # w: list over experts of [W1 [F,H], W3 [F,H], W2 [H,F]] tensors on `device`
+        self.E = len(w)
+        self.pairs = [None if ex is None else [ctx.quantize_rows(m, layout=B.LAYOUT_TILE) for m in ex] for ex in w]
+        self.table = B.make_int8_table(self.pairs, device)
+
+
+class Int8MoELayer:
+    """A layer whose router scores (dymoe_route_scored) and whose experts are 8-bit integers (dymoe_moe_ffn_int8), every buffer
+    pre-allocated: a step is three library calls on one stream, or two where the caller has the logits."""
+
+    def __init__(self, ctx, T, H, F, E, k, score=B.SCORE_SIGMOID, groups=1, top_groups=1, group_best=1, renorm=True, factor=1.0,
+                 out_dtype=B.OUT_BF16, device="cuda:0"):
+        self.ctx, self.T, self.H, self.F, self.E, self.k = ctx, T, H, F, E, k
+        self.routing = dict(score=score, groups=groups, top_groups=top_groups, group_best=group_best, renorm=renorm, factor=factor)
+        self.logits = torch.empty((T, E), dtype=torch.float32, device=device)
+        self.scores = torch.empty((T, E), dtype=torch.float32, device=device)
+        self.idx = torch.empty((T, k), dtype=torch.int32, device=device)
+        self.gate = torch.empty((T, k), dtype=torch.float32, device=device)
+        self.y = torch.empty((T, H), dtype=B._TORCH_OUT[out_dtype], device=device)
+        self.ws_router = torch.empty((B.matmul_int8_workspace_bytes(T, E, H),), dtype=torch.uint8, device=device)
+        self.ws = torch.empty((B.moe_ffn_int8_workspace_bytes(T, H, F, E, k),), dtype=torch.uint8, device=device)
+
+    def step(self, x, experts, router=None, logits=None, bias=None, stream=None):
+        """router: (codes, scale) of the [E, H] router in the tile layout; or logits [T, E] that the caller has."""
+        if logits is None:
+            logits = self.ctx.matmul_int8(x, router, y=self.logits, workspace=self.ws_router, stream=stream)
+        self.ctx.route_scored(logits, self.k, bias=bias, idx=self.idx, w=self.gate, scores=self.scores, stream=stream, **self.routing)
+        return self.ctx.moe_ffn_int8(x, self.idx, self.gate, experts.table, self.F, y=self.y, workspace=self.ws, stream=stream)

@@ -8,8 +8,15 @@ Tolerances, from the formulas:
 * moe_ffn: beside those, the intermediate h reaches the quantiser with a relative error eps of 2^-16:
   fp32 sums, scales and the sigmoid (an exponential of arguments up to 64: 2^-18, the rest an order less).  Its scale moves by as
   much, so h / scale moves by up to 2 eps |h| / scale of a step: a code flips with that probability, by one step, and
-  what it stands for drifts by eps of itself.  Codes flip independently of each other: an output's deviation is
-  a sum over the F codes, within six standard deviations of that sum plus eps of each pair's output (a chance of 2e-9 an output).
+  what it stands for drifts by eps of itself.  Codes flip independently of each other: an output's deviation is the drift, eps of
+  each pair's output, and a sum over the F codes of independent terms, each 0 or one step times a weight.  Often there are
+  none or a few flips in a row, so the sum is no Gaussian one; Bernstein's inequality holds for any number of them: beyond
+  M L / 3 + sqrt((M L / 3)^2 + 2 L V) with a chance of 2 exp(-L) at most, V the sum of the variances, M the largest term.
+  L = ln(1e9), a chance of 2e-9 an output.  And over the outputs of a hundred tokens or more, hundreds of flips, the mean square of
+  the deviations is what the variances say: at most four times it.
+  With bf16 outputs a call of many pairs rounds each pair's output to fp16 before the sum over the slots, scaled so that the
+  largest sum there can be, 127 * 127 * F steps of the intermediate times the largest channel scale, is 2^15: half a step is 2^-11
+  of the pair's output, or, below 2^-14, 2^-25 on that scale, 2^-40 of the largest sum (int8_oracle.moe_ffn's last result).
 """
 import math
 
@@ -19,6 +26,7 @@ import torch
 
 from oracle import int8_oracle as Q
 from paper_2603_19172_amd import binding as B
+from paper_2603_19172_amd.layer import Int8Experts, Int8MoELayer
 from gpu_helpers import DEV
 
 pytestmark = pytest.mark.gpu
@@ -319,7 +327,9 @@ def check_ffn(ctx, x, idx, gate, dev, host, F, out=torch.bfloat16, table=None):
     y = torch.full((T + 2, H), 77.0, dtype=out, device=DEV)
     ctx.moe_ffn_int8(x, idx, gate, table, F, y=y[:T], workspace=ws)
     torch.cuda.synchronize()
-    ref, dev_tol = Q.moe_ffn(f64(x), idx.cpu().numpy(), f64(gate), host, EPS_H)
+    ref, dev_tol, square, half = Q.moe_ffn(f64(x), idx.cpu().numpy(), f64(gate), host, EPS_H)
+    if out == torch.bfloat16:
+        dev_tol, square = dev_tol + half, square + half ** 2
     got = f64(y[:T])
     # sums over k slots of fp32 products, and the output's type
     k = idx.shape[1]
@@ -328,6 +338,9 @@ def check_ffn(ctx, x, idx, gate, dev, host, F, out=torch.bfloat16, table=None):
     worst = (np.abs(got - ref) / np.maximum(tol, 1e-300)).max() if got.size else 0.0
     print("T=%d H=%d F=%d: worst %.2f of the bound" % (T, H, F, worst), flush=True)
     assert worst <= 1.0
+    if T >= 100:
+        rounding = HALF[out] * np.abs(ref) + (k + 6) * 2.0 ** -24 * np.abs(ref) + 2.0 ** -24 * np.abs(ref).max()
+        assert ((got - ref) ** 2).sum() <= 4.0 * (square + rounding ** 2).sum()
     assert (y[T:] == 77).all()
     return y[:T]
 
@@ -400,6 +413,64 @@ def test_ffn_skewed_load(ctx):
     check_ffn(ctx, randn(1, 400, 128), idx, gate, dev, host, 96)
 
 
+def test_ffn_rows_longer_than_the_first_launch_takes(ctx):
+    """Activations whose codes are a launch of their own."""
+    dev, host = make_experts(ctx, 21, 2, 16500, 40)
+    for T in (1, 20, 40):
+        idx, gate = routing(T, T, 2, 1)
+        check_ffn(ctx, randn(T, T, 16500), idx, gate, dev, host, 40)
+
+
+@pytest.mark.parametrize("T,E,k,popular", [(2100, 8, 8, 0.0), (5000, 40, 4, 1.0)])
+def test_ffn_more_pairs_than_a_plan_holds_in_lds(ctx, T, E, k, popular):
+    dev, host = make_experts(ctx, 22, E, 64, 32)
+    idx, gate = routing(3, T, E, k, popular)
+    check_ffn(ctx, randn(4, T, 64), idx, gate, dev, host, 32)
+
+
+def test_ffn_more_tiles_than_a_plan_holds_in_lds(ctx):
+    """Rows are the same bits as in a call of their own size's kernels, whatever rows they stand among."""
+    T, H, F, E, k, part = 66000, 40, 24, 8, 8, 8000
+    dev, _ = make_experts(ctx, 23, E, H, F)
+    table = B.make_int8_table(dev, DEV)
+    idx, gate = routing(5, T, E, k)
+    x = randn(6, T, H)
+    whole = ctx.moe_ffn_int8(x, idx, gate, table, F)
+    for lo in range(0, T, part):
+        hi = min(T, lo + part)
+        assert torch.equal(ctx.moe_ffn_int8(x[lo:hi], idx[lo:hi], gate[lo:hi], table, F), whole[lo:hi])
+
+
+@pytest.mark.parametrize("T", [3, 40, 300])
+def test_ffn_weights_at_the_ends_of_the_range(ctx, T):
+    """Scales that are tiny, zero, and NaN: a channel of W2 that is no number is that output, and no other."""
+    E, H, F = 2, 96, 64
+    mats = [[randn(50 + 3 * e + i, *s, std=0.05) for i, s in enumerate(((F, H), (F, H), (H, F)))] for e in range(E)]
+    mats[0][2][5] = 0
+    mats[0][2][40:] *= 2.0 ** -126
+    mats[1][2][64:] = 0
+    dev = [[ctx.quantize_rows(m, layout=B.LAYOUT_TILE) for m in ex] for ex in mats]
+    host = [[Q.quantize_rows(f64(m)) for m in ex] for ex in mats]
+    idx, gate = routing(T, T, E, 2)
+    x = randn(T, T, H)
+    clean = check_ffn(ctx, x, idx, gate, dev, host, F).clone()
+    mats[1][2][7, 3] = math.inf
+    dev[1][2] = ctx.quantize_rows(mats[1][2], layout=B.LAYOUT_TILE)
+    y = ctx.moe_ffn_int8(x, idx, gate, B.make_int8_table(dev, DEV), F)
+    rest = torch.arange(H, device=DEV) != 7
+    assert torch.isnan(y[:, 7]).all() and torch.equal(y[:, rest], clean[:, rest])
+
+
+@pytest.mark.parametrize("T", [200, 400])
+def test_ffn_tall_and_wide_tiles_side_by_side(ctx, T):
+    """One expert with several tiles of 128 rows, others with a few pairs each; loads on both sides of where the kinds change."""
+    E, H, F = 12, 200, 264
+    dev, host = make_experts(ctx, 24, E, H, F)
+    for n in (160, 161, 128, 129, 33, T):
+        idx = torch.stack([torch.arange(T) % (E - 1) + 1, torch.where(torch.arange(T) < n, 0, -1)], 1).to(torch.int32).to(DEV)
+        check_ffn(ctx, randn(T + n, T, H), idx, torch.full((T, 2), 0.5, device=DEV), dev, host, F)
+
+
 # ------------------------------------------------------------------------------------------------------------------ as they are used
 
 @pytest.mark.parametrize("T", [1, 9, 50, 300])
@@ -442,6 +513,48 @@ def test_router_and_experts_together_on_another_stream_and_in_a_graph(ctx, T):
         got = bufs["y"].clone()
         assert torch.equal(got, step(x, eager))
         assert r > 0 or not torch.equal(got, first)
+
+
+@pytest.mark.parametrize("T", [1, 33, 260])
+def test_layer_class_is_its_calls(ctx, T):
+    H, F, E, k = 192, 256, 16, 4
+    mats = [[randn(700 + 3 * e + i, *s, std=0.05) for i, s in enumerate(((F, H), (F, H), (H, F)))] for e in range(E)]
+    mats[3] = None
+    experts = Int8Experts(ctx, mats, DEV)
+    router = ctx.quantize_rows(randn(69, E, H, std=0.1), layout=B.LAYOUT_TILE)
+    bias = randn(68, E, dtype=torch.float32, std=0.05)
+    x = randn(T, T, H)
+    layer = Int8MoELayer(ctx, T, H, F, E, k, groups=4, top_groups=2, group_best=2, factor=2.5)
+    y = layer.step(x, experts, router=router, bias=bias)
+    logits = ctx.matmul_int8(x, router, out_dtype=B.OUT_F32)
+    idx, w = ctx.route_scored(logits, k, bias=bias, groups=4, top_groups=2, group_best=2, factor=2.5)
+    assert torch.equal(layer.idx, idx) and torch.equal(layer.gate, w)
+    assert torch.equal(y, ctx.moe_ffn_int8(x, idx, w, experts.table, F))
+    assert torch.equal(layer.step(x, experts, logits=logits, bias=bias), y)
+    assert ctx.device_flags() in (0, B.FLAG_FORMAT_MISSING)
+
+
+def test_two_calls_at_once_on_two_streams(ctx):
+    """Workspaces of their own: nothing else is shared."""
+    H, F, E, k, T = 256, 512, 8, 2, 300
+    dev, _ = make_experts(ctx, 25, E, H, F)
+    table = B.make_int8_table(dev, DEV)
+    wt, _ = weight(ctx, 26, 400, H)
+    x = randn(27, T, H)
+    idx, gate = routing(28, T, E, k)
+    ref = ctx.moe_ffn_int8(x, idx, gate, table, F), ctx.matmul_int8(x, wt)
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    got = []
+    for _ in range(5):
+        with torch.cuda.stream(a):
+            y = ctx.moe_ffn_int8(x, idx, gate, table, F)
+        with torch.cuda.stream(b):
+            z = ctx.matmul_int8(x, wt)
+        got.append((y, z))
+    torch.cuda.synchronize()
+    for y, z in got:
+        assert torch.equal(y, ref[0]) and torch.equal(z, ref[1])
 
 
 def test_scores_feed_the_importance_and_the_mixed_layer(ctx):

@@ -78,7 +78,7 @@ def test_ffn_oracle_against_a_dense_swiglu():
         experts.append([Q.quantize_rows(rng.standard_normal(s) * 0.1) for s in ((F, H), (F, H), (H, F))])
     idx = np.array([[0, 1], [1, 0], [1, -1]])
     gate = rng.random((T, 2))
-    y, tol = Q.moe_ffn(x, idx, gate, experts, 0.0)
+    y, tol, _, _ = Q.moe_ffn(x, idx, gate, experts, 0.0)
     ref = np.zeros((T, H))
     for t in range(T):
         for j in range(2):
