@@ -727,16 +727,28 @@ __device__ __forceinline__ void i8_finish(const I8Args& A, const int32_t* perm, 
         }
         const bool half = MODE == kI8Down && A.strip_scale;
         if (half) {
-            // A pair's outputs in 16 bits: fp16 of sum * sum_scale * (channel's scale / the strip's largest), at most 2^15 and 2^-12 of itself
-            // off, a sixteenth of what the bf16 output of the call rounds; the rest of the factors goes to the sum over the slots.
-            float m = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3]));
-            m = fmaxf(m, __shfl_xor(m, 1, kWave));
-            m = fmaxf(m, __shfl_xor(m, 2, kWave));
-            m = fmaxf(m, __shfl_xor(m, 4, kWave));
+            // A pair's outputs in 16 bits: fp16 of sum * sum_scale * (channel's scale / the strip's largest), at most 2^15 and 2^-11 of itself
+            // off, an eighth of what the bf16 output of the call rounds; the rest of the factors goes to the sum over the slots.  fp16's
+            // least step, 2^-25 to either side, is F * 2^-26 / (channel's scale / the strip's largest) units of the whole-number
+            // sum: less than half a unit at F = 131072 while a strip's scales lie within 2^8 of each other.  Where they do not (or one is
+            // infinite) the ratio stays out of the 16 bits and the sum over the slots takes each channel's own scale; a negative
+            // scale of the strip says so.
+            float m = 0.0f, lo = __builtin_inff();
 #pragma unroll
-            for (int i = 0; i < 4; i++) sc[i] = m > 0.0f ? A.sum_scale * (sc[i] / m) : 0.0f * sc[i];      // (a scale that is NaN stays)
+            for (int i = 0; i < 4; i++) {
+                m = fmaxf(m, fabsf(sc[i]));
+                if (sc[i] != 0.0f) lo = fminf(lo, fabsf(sc[i]));          // (a channel of zeros has sums of zero; NaN is passed over)
+            }
+#pragma unroll
+            for (int o = 1; o < 8; o *= 2) {
+                m = fmaxf(m, __shfl_xor(m, o, kWave));
+                lo = fminf(lo, __shfl_xor(lo, o, kWave));
+            }
+            const bool apart = lo < m * 0x1p-8f || m == __builtin_inff();
+#pragma unroll
+            for (int i = 0; i < 4; i++) sc[i] = apart ? A.sum_scale : m > 0.0f ? A.sum_scale * (sc[i] / m) : 0.0f * sc[i];      // (a scale that is NaN stays)
             if (left > 0 && (lane & 7) == 0 && lane < kOut)      // (every tile of an expert writes the same)
-                A.strip_scale[(long)expert * ((A.N + 31) / 32) + n / 32] = m / A.sum_scale;
+                A.strip_scale[(long)expert * ((A.N + 31) / 32) + n / 32] = (apart ? -1.0f : m) / A.sum_scale;
         }
 #pragma unroll
         for (int tf = 0; tf < NTF; tf++) {
@@ -1321,22 +1333,26 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void i8_small_kernel(cons
 // y[t] = sum over the slots, in their order, of gate times the pair's output.  A workgroup takes 2048 outputs of a token.
 template <bool HALF>
 __global__ __launch_bounds__(256) void i8_combine_kernel(const char* __restrict__ part, long ldp, const float* __restrict__ hs,
-                                                         const float* __restrict__ strip_scale, const int32_t* __restrict__ idx,
-                                                         const int32_t* __restrict__ where, const float* __restrict__ gate, int H, int k,
-                                                         int out_dtype, int aligned, void* __restrict__ y)
+                                                         const float* __restrict__ strip_scale, const dymoe_expert_i8* __restrict__ table,
+                                                         const int32_t* __restrict__ idx, const int32_t* __restrict__ where,
+                                                         const float* __restrict__ gate, int H, int k, int out_dtype, int aligned,
+                                                         void* __restrict__ y)
 {
     const int blocks = (H + 2047) / 2048;
     const long t = blockIdx.x / blocks;
     const int h = (int)(blockIdx.x - t * blocks) * 2048 + threadIdx.x * 8;
     if (h >= H) return;
     float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    bool apart = false;             // a strip whose scales lie apart: the slots again, each channel with its own
 #pragma unroll 4
     for (int j = 0; j < k; j++) {
         const int at = where[t * k + j];
         if (at < 0) continue;
         float g = gate[t * k + j];
         if constexpr (HALF) {
-            g *= hs[at] * strip_scale[(long)idx[t * k + j] * ((H + 31) / 32) + h / 32];
+            const float ss = strip_scale[(long)idx[t * k + j] * ((H + 31) / 32) + h / 32];
+            apart |= ss < 0.0f;
+            g *= hs[at] * ss;
             const half8_t v = __builtin_bit_cast(half8_t, load_global<uint4>(part + (at * ldp + h) * 2));
 #pragma unroll
             for (int i = 0; i < 8; i++) sum[i] = fmaf(g, (float)v[i], sum[i]);
@@ -1345,6 +1361,19 @@ __global__ __launch_bounds__(256) void i8_combine_kernel(const char* __restrict_
             const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
             for (int i = 0; i < 8; i++) sum[i] = fmaf(g, v[i], sum[i]);
+        }
+    }
+    if (HALF && apart) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) sum[i] = 0.0f;
+        for (int j = 0; j < k; j++) {
+            const int at = where[t * k + j];
+            if (at < 0) continue;
+            const int e = idx[t * k + j];
+            const float ss = strip_scale[(long)e * ((H + 31) / 32) + h / 32], g = gate[t * k + j] * (hs[at] * fabsf(ss));
+            const half8_t v = __builtin_bit_cast(half8_t, load_global<uint4>(part + (at * ldp + h) * 2));
+#pragma unroll
+            for (int i = 0; i < 8; i++) sum[i] = fmaf(g * (ss < 0.0f ? table[e].s[2][min(h + i, H - 1)] : 1.0f), (float)v[i], sum[i]);
         }
     }
     const float lo[4] = {sum[0], sum[1], sum[2], sum[3]}, hi[4] = {sum[4], sum[5], sum[6], sum[7]};
@@ -1550,7 +1579,7 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     const dim3 grid((unsigned)(T * ((H + 2047L) / 2048)));
     auto combine = half ? i8_combine_kernel<true> : i8_combine_kernel<false>;
     dymoe_launch(ctx, DYMOE_K_INT8_COMBINE, combine, grid, dim3(256), 0, st, ws + L.part, (long)L.Hp, (const float*)(ws + L.hs),
-                 (const float*)(ws + L.strips), idx, i8_plan(plan, P).where, w, H, k, out_dtype,
+                 (const float*)(ws + L.strips), table, idx, i8_plan(plan, P).where, w, H, k, out_dtype,
                  H % 4 == 0 && dymoe_aligned(y, 4 * dtype_bytes(out_dtype)), y);
     DYMOE_HIP_LAUNCH_CHECK();
     return DYMOE_OK;

@@ -461,6 +461,43 @@ def test_ffn_weights_at_the_ends_of_the_range(ctx, T):
     assert torch.isnan(y[:, 7]).all() and torch.equal(y[:, rest], clean[:, rest])
 
 
+@pytest.mark.parametrize("T,spread", [(40, 40), (300, 9), (300, 40), (700, 100)])
+def test_ffn_channels_far_apart(ctx, T, spread):
+    """Neighbouring channels of W2 whose scales lie up to 2^spread apart: each is as exact as it would be alone.  The rounding of a pair's output to
+    fp16 is half a step of 2^-11 of it, or half of the least step: of sums scaled so that 127 * 127 * F steps of the intermediate are 2^15,
+    times a channel's share of its strip's largest scale where that is 2^-8 or more and one where it is less, 2^-25; so
+    2^-25 * 127 * 127 * F * 2^-15 * 2^8 steps of the intermediate times the channel's own scale at most."""
+    E, H, F, k = 2, 168, 264, 2
+    g = torch.Generator().manual_seed(T + spread)
+    mats = [[randn(90 + 3 * e + i, *s, std=0.05) for i, s in enumerate(((F, H), (F, H), (H, F)))] for e in range(E)]
+    for e in range(E):
+        down = torch.randint(0, spread + 1, (H, 1), generator=g)
+        down[64:96] = 3                              # (a strip of equal channels beside the others)
+        mats[e][2] = (mats[e][2].float() * (0.5 ** down.double()).float().to(DEV)).to(torch.bfloat16)
+    mats[0][2][33] = 0
+    dev = [[ctx.quantize_rows(m, layout=B.LAYOUT_TILE) for m in ex] for ex in mats]
+    host = [[Q.quantize_rows(f64(m)) for m in ex] for ex in mats]
+    idx, gate = routing(T, T, E, k)
+    idx[: T // 8, 1] = -1
+    x = randn(T, T, H)
+    y = f64(ctx.moe_ffn_int8(x, idx, gate, B.make_int8_table(dev, DEV), F))
+    ix = idx.cpu().numpy()
+    ref, bound, _, _ = Q.moe_ffn(f64(x), ix, f64(gate), host, EPS_H)
+    size = sum(np.abs(Q.moe_ffn(f64(x), ix[:, j:j + 1], f64(gate)[:, j:j + 1], host, 0.0)[0]) for j in range(k))
+    least = np.zeros_like(ref)
+    for t in range(T):
+        for j in range(k):
+            if ix[t, j] >= 0:
+                (q1, s1), (q3, s3), (q2, s2) = host[ix[t, j]]
+                xq, xs = Q.quantize_rows(f64(x[t:t + 1]))
+                a, u = (Q.matmul(xq, xs, q, s)[0] for q, s in ((q1, s1), (q3, s3)))
+                step = np.abs(a / (1.0 + np.exp(-a)) * u).max() / 127.0
+                least[t] += abs(float(gate[t, j])) * 2.0 ** -32 * 127 * 127 * F * step * s2
+    tol = bound + 2.0 ** -11 * size + least + HALF[torch.bfloat16] * (np.abs(ref) + bound) + (k + 6) * 2.0 ** -24 * (size + bound)
+    assert (np.abs(y - ref) <= tol).all()
+    assert (y[:, 64:96] != 0).all()
+
+
 @pytest.mark.parametrize("T", [200, 400])
 def test_ffn_tall_and_wide_tiles_side_by_side(ctx, T):
     """One expert with several tiles of 128 rows, others with a few pairs each; loads on both sides of where the kinds change."""
