@@ -262,6 +262,9 @@ __device__ __forceinline__ i32x16_t mfma_i8(const uint4 a, const uint4 b, const 
     return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4_t, a), __builtin_bit_cast(i32x4_t, b), c, 0, 0, 0);
 }
 
+// An output of a product: two roundings and the addition's, in every shape alike, whatever the compiler would contract.
+__device__ __forceinline__ float i8_value(int sum, float xs, float sc, float add) { return fmaf((float)sum * xs, sc, add); }
+
 __device__ __forceinline__ float silu_times(float a, float u) { return a * __builtin_amdgcn_rcpf(1.0f + __expf(-a)) * u; }
 
 // ----------------------------------------------------------------------------
@@ -465,11 +468,9 @@ __global__ __launch_bounds__(64 * kI8ThinWaves, 4) void i8_thin_kernel(const I8T
     if (n >= A.N) return;
     const float xs = FUSE ? s_scale[token] : A.xs[token];
     if (MODE == kI8Up) {
-        ((DYMOE_GLOBAL float*)A.out)[mine * A.ldo + n] = silu_times((float)sum[0] * xs * sa[n], (float)sum[S - 1] * xs * sb[n]);
+        ((DYMOE_GLOBAL float*)A.out)[mine * A.ldo + n] = silu_times(i8_value(sum[0], xs, sa[n], 0.0f), i8_value(sum[S - 1], xs, sb[n], 0.0f));
     } else {
-        float o = (float)sum[0] * xs * sa[n];
-        if (A.bias) o += A.bias[n];
-        store_out(A.out, mine * A.ldo + n, A.out_dtype, o);
+        store_out(A.out, mine * A.ldo + n, A.out_dtype, i8_value(sum[0], xs, sa[n], A.bias ? A.bias[n] : 0.0f));
     }
 }
 
@@ -664,7 +665,7 @@ __device__ __forceinline__ void i8_finish(const I8Args& A, const int32_t* perm, 
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
                     const int f = min((4 * bx + wave) * 32 + 8 * g + 4 * kb + i, A.N - 1);
-                    h[i] = silu_times((float)acc[0][tf][4 * g + i] * xs * sa[f], (float)acc[S - 1][tf][4 * g + i] * xs * sb[f]);
+                    h[i] = silu_times(i8_value(acc[0][tf][4 * g + i], xs, sa[f], 0.0f), i8_value(acc[S - 1][tf][4 * g + i], xs, sb[f], 0.0f));
                 }
                 lds_write16(wr + 32u * g, make_uint4(__float_as_uint(h[0]), __float_as_uint(h[1]), __float_as_uint(h[2]), __float_as_uint(h[3])));
             }
@@ -712,7 +713,7 @@ __device__ __forceinline__ void i8_finish(const I8Args& A, const int32_t* perm, 
                 const uint32_t av[4] = {a.x, a.y, a.z, a.w}, uv[4] = {u.x, u.y, u.z, u.w};
                 float v[4];
 #pragma unroll
-                for (int i = 0; i < 4; i++) v[i] = silu_times((float)(int)av[i] * xs * c1[i], (float)(int)uv[i] * xs * c3[i]);
+                for (int i = 0; i < 4; i++) v[i] = silu_times(i8_value((int)av[i], xs, c1[i], 0.0f), i8_value((int)uv[i], xs, c3[i], 0.0f));
                 i8_store4(A.out, (long)(row0 + row) * A.ldo + n, dt, left >= 4, left, v);
             }
             __syncthreads();
@@ -769,7 +770,7 @@ __device__ __forceinline__ void i8_finish(const I8Args& A, const int32_t* perm, 
                 }
                 const float xs = A.xs[row0 + row];
 #pragma unroll
-                for (int i = 0; i < 4; i++) v[i] = (float)(int)w4[i] * xs * sc[i] + add[i];
+                for (int i = 0; i < 4; i++) v[i] = i8_value((int)w4[i], xs, sc[i], add[i]);
                 i8_store4(A.out, (long)(row0 + row) * A.ldo + n, dt, left >= 4 && vec, left, v);
             }
         }
@@ -1091,7 +1092,7 @@ __device__ __forceinline__ void i8_split_tile(const I8Args& A, const I8Unit<1>& 
             const float xs = A.xs[u.row0 + row];
             float v[4];
 #pragma unroll
-            for (int i = 0; i < 4; i++) v[i] = (float)(int)sum[i] * xs * sc[i] + add[i];
+            for (int i = 0; i < 4; i++) v[i] = i8_value((int)sum[i], xs, sc[i], add[i]);
             i8_store4(A.out, (long)(u.row0 + row) * A.ldo + n, A.out_dtype, left >= 4 && A.aligned, left, v);
         }
         __syncthreads();
@@ -1321,10 +1322,9 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void i8_small_kernel(cons
 #pragma unroll
         for (int i = 0; i < 4; i++) {
             const int m = min(n + i, A.N - 1);
-            auto sum = [&](int at) { return (float)(s_red[0][at][4 * g + i][lane] + s_red[1][at][4 * g + i][lane] + s_red[2][at][4 * g + i][lane] + s_red[3][at][4 * g + i][lane]); };
-            v[i] = sum(f) * xs * sa[m];
-            if (MODE == kI8Up) v[i] = silu_times(v[i], sum(NTF + f) * xs * sb[m]);
-            if (MODE == kI8Plain && A.bias) v[i] += A.bias[m];
+            auto sum = [&](int at) { return s_red[0][at][4 * g + i][lane] + s_red[1][at][4 * g + i][lane] + s_red[2][at][4 * g + i][lane] + s_red[3][at][4 * g + i][lane]; };
+            v[i] = i8_value(sum(f), xs, sa[m], MODE == kI8Plain && A.bias ? A.bias[m] : 0.0f);
+            if (MODE == kI8Up) v[i] = silu_times(v[i], i8_value(sum(NTF + f), xs, sb[m], 0.0f));
         }
         i8_store4(A.out, (long)(row0 + row) * A.ldo + n, MODE == kI8Plain ? A.out_dtype : DYMOE_OUT_F32, left >= 4 && (MODE != kI8Plain || A.aligned), left, v);
     }

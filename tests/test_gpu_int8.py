@@ -298,6 +298,17 @@ def test_matmul_rows_do_not_depend_on_their_company(ctx):
         assert torch.equal(ctx.matmul_int8(x[lo:hi], wt), y[lo:hi])
 
 
+@pytest.mark.parametrize("N,K", [(520, 1200), (4100, 2100)])
+def test_matmul_rows_with_a_bias_do_not_depend_on_their_company(ctx, N, K):
+    """The bias's addition is rounded alike in every shape the product is computed in."""
+    T = 2500
+    wt, _ = weight(ctx, 6, N, K)
+    x, bias = randn(6, T, K), randn(7, N, dtype=torch.float32)
+    y = ctx.matmul_int8(x, wt, bias=bias, out_dtype=B.OUT_F32)
+    for lo, hi in ((0, 1), (3, 8), (100, 117), (200, 260), (0, 130), (1, 400), (300, 1700)):
+        assert torch.equal(ctx.matmul_int8(x[lo:hi], wt, bias=bias, out_dtype=B.OUT_F32), y[lo:hi])
+
+
 # ------------------------------------------------------------------------------------------------------------------ experts
 
 def make_experts(ctx, seed, E, H, F, absent=()):
