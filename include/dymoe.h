@@ -518,7 +518,8 @@ int dymoe_moe_ffn_mixed_noalloc(dymoe_ctx* ctx, const void* x, const int32_t* id
  * with plus infinity under softmax, has NaN weights and scores; its indices are those of k different experts all the same.
  * logits [T,E] bf16, fp16 or fp32 (dtype: DYMOE_OUT_*), bias [E] fp32 or NULL, idx [T,k] int32, w [T,k] fp32, scores [T,E]
  * fp32 or NULL (what dymoe_expert_importance takes as probs).  Limits: 1 <= k <= top_groups * (E / groups), groups divides
- * E, factor > 0; E <= DYMOE_MAX_EXPERTS, k <= 64, groups <= 64 (else DYMOE_ENOTSUP).
+ * E, factor > 0; E <= DYMOE_MAX_EXPERTS, k <= 64, groups <= 64, T < 2^26 (else DYMOE_ENOTSUP).  Scores below e^-700 (of the
+ * largest, under softmax) count as e^-700.
  */
 int dymoe_route_scored(dymoe_ctx* ctx, const void* logits, int dtype, const float* bias, int T, int E, int k, int score,
                        int groups, int top_groups, int group_best, int renorm, float factor, int32_t* idx, float* w,
@@ -566,12 +567,14 @@ typedef struct {
  * SwiGLU experts in 8-bit integer arithmetic, activations quantised on the way:
  *   y[t,:] = sum_{slot<k} w[t,slot] * W2_e q( silu(W1_e q(x_t)) * (W3_e q(x_t)) ),  e = idx[t,slot],
  * q() the quantiser of dymoe_quantize_rows applied to a whole row, the products those of dymoe_matmul_int8.  Sums of products
- * are exact; the SwiGLU intermediate is held in fp32 in calls of few pairs and in bf16 in others, the sum over the slots in fp32.
+ * are exact; the SwiGLU intermediate is held in fp32, and so is the sum over the slots.  With bf16 outputs a call of more than 32
+ * tokens and 8 E pairs rounds each pair's output to fp16 before that sum (2^-11 of itself, beside the 2^-8 of y's own rounding).
  * x [T,H] bf16, fp16 or fp32; idx [T,k] int32; w [T,k] fp32; table [E] of dymoe_expert_i8 in device memory; y [T,H] in
  * out_dtype (every row is written).  A pair whose index lies outside [0,E) contributes nothing, nor does one whose
  * expert's entry holds a NULL (DYMOE_FLAG_FORMAT_MISSING, dymoe_device_flags).
  * workspace: dymoe_moe_ffn_int8_workspace_bytes(T,H,F,E,k) bytes (0 for invalid sizes), 256-byte aligned, scratch.
- * Limits: any H, F up to DYMOE_INT8_MAX_K, E <= DYMOE_MAX_EXPERTS.  No atomics in sums: the same inputs give the same bits.
+ * Limits: any H, F up to DYMOE_INT8_MAX_K, E <= DYMOE_MAX_EXPERTS; T k < 2^29, T times H rounded up to 128 < 2^32 and T times
+ * H / 2048 rounded up < 2^23 (else DYMOE_ENOTSUP).  No atomics in sums: the same inputs give the same bits.
  */
 size_t dymoe_moe_ffn_int8_workspace_bytes(int T, int H, int F, int E, int k);
 int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, const int32_t* idx, const float* w,

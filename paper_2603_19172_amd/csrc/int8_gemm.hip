@@ -109,22 +109,24 @@ __device__ __forceinline__ void i8_make_plan(I8PlanLds& lds, const int32_t* __re
         all1 += a1;
     }
     const int t0 = one ? all2 + t1 - m : t2 - m;
-    auto record = [&](int e, int first, int pairs, int tile0, int tiles) {
-        I8TileRec t = {};
-        t.expert = e;
-        t.first = first;
-        t.pairs = pairs;
-        t.tile0 = tile0;
-        t.tiles = tiles;
-        t.mat = table[e];
-        return t;
+    // (in 16-byte pieces: a record put together first would pass through scratch memory)
+    auto record = [&](I8TileRec* to, int e, int first, int pairs, int tile0, int tiles) {
+        uint4* const at = (uint4*)to;
+        const uint2* const mat = (const uint2*)(table + e);
+        store_global(at, make_uint4((uint32_t)e, (uint32_t)first, (uint32_t)pairs, (uint32_t)tile0));
+        store_global(at + 1, make_uint4((uint32_t)tiles, 0u, 0u, 0u));
+#pragma unroll
+        for (int i = 0; i < 3; i++) {
+            const uint2 lo = load_global<uint2>(mat + 2 * i), hi = load_global<uint2>(mat + 2 * i + 1);
+            store_global(at + 2 + i, make_uint4(lo.x, lo.y, hi.x, hi.y));
+        }
     };
     lds.at[tid] = n > 0 ? n0 : -1;
     lds.count[tid] = n;
     lds.tile0[tid] = t0;
     for (int i = 0; i < m; i++) {
         if (t0 + i < kI8PlanTiles) lds.owner[t0 + i] = (uint16_t)tid;
-        else pp.tiles[t0 + i] = record(tid, n0, n, t0, m);
+        else record(&pp.tiles[t0 + i], tid, n0, n, t0, m);
     }
     if (tid == 0) {
         pp.meta[0] = all2;
@@ -134,7 +136,7 @@ __device__ __forceinline__ void i8_make_plan(I8PlanLds& lds, const int32_t* __re
     for (int i = tid; i < min(all1 + all2, kI8PlanTiles); i += kI8PlanThreads) {
         const int e = lds.owner[i], c = lds.count[e];
         const int per = small ? kI8TileSmall : c <= kI8TileWide ? kI8TileWide : kI8TileRows;
-        pp.tiles[i] = record(e, lds.at[e], c, lds.tile0[e], (c + per - 1) / per);
+        record(&pp.tiles[i], e, lds.at[e], c, lds.tile0[e], (c + per - 1) / per);
     }
     const bool fits = P <= kI8PlanPairs;
     auto place = [&](long p, int x, int rank) {
@@ -227,14 +229,13 @@ struct I8Args {
     const char* x;                    // codes of the rows, Kp columns each
     const float* xs;
     const int32_t* plan;              // grouped products
-    const dymoe_expert_i8* table;
     I8Mat w;                          // the plain product
     const float* bias;
     void* out;
     float* strip_scale;               // down projection with 16-bit outputs: [E][strips of 32 outputs]; null: 32-bit ones
     float sum_scale;                  // largest sum there can be -> 2^15
     long ldo, P;
-    int rows, Kp, N, E, k, out_dtype, aligned, tiled;     // aligned: the plain product's rows start where four outputs may be stored at once
+    int rows, Kp, N, k, out_dtype, aligned, tiled;     // aligned: the plain product's rows start where four outputs may be stored at once
 };
 
 // Memory that a wavefront's loads share a base in: the base in scalar registers, a lane's offset and the load's own in 32 bits each.
@@ -280,9 +281,7 @@ constexpr int kI8FuseRows = 4;                  // tokens up to which the expert
 constexpr long kI8FuseBytes = 64 * 1024;        // the codes' bytes in LDS at most
 constexpr long kI8FuseReads = 16 << 20;         // values that the workgroups of a plain product read to quantise them, together, at most
 
-typedef int i32x4acc_t __attribute__((ext_vector_type(4)));
-
-__device__ __forceinline__ i32x4acc_t mfma16_i8(const uint4 a, const uint4 b, const i32x4acc_t c)
+__device__ __forceinline__ i32x4_t mfma16_i8(const uint4 a, const uint4 b, const i32x4_t c)
 {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4_t, a), __builtin_bit_cast(i32x4_t, b), c, 0, 0, 0);
 }
@@ -313,7 +312,7 @@ struct I8Thin {
     }
     // row(col): 16 codes of this lane's row from column col on
     template <class Row>
-    __device__ __forceinline__ void run(i32x4acc_t (&acc)[S], int lane, Row row)
+    __device__ __forceinline__ void run(i32x4_t (&acc)[S], int lane, Row row)
     {
         const int col = 64 * (lane >> 5) + 16 * (lane >> 4 & 1);
         while (kt < nkt) {
@@ -441,7 +440,7 @@ __global__ __launch_bounds__(64 * kI8ThinWaves, 4) void i8_thin_kernel(const I8T
     const int nkt = A.Kp >> 7;
     thin.start(wave, nkt, kI8ThinWaves, bx & 1, lane);
     const int token = MODE == kI8Up ? mine / A.k : mine;
-    i32x4acc_t acc[S] = {};
+    i32x4_t acc[S] = {};
     if constexpr (FUSE) {
         i8_rows_to_lds(A.x_dtype, A.x, A.ldx, MODE == kI8Up ? A.P / A.k : A.rows, A.K, A.Kp, s_codes, s_scale, s_max);
         const char* const row = s_codes + token * (A.Kp + 16);
@@ -510,7 +509,7 @@ __global__ __launch_bounds__(64 * kI8LastWaves) void i8_thin_down_kernel(const I
     i8_rows_to_lds<DYMOE_OUT_F32>(A.x + (long)t * k * A.ldx, A.ldx, k, A.K, A.Kp, s_codes, s_scale, s_max);
     for (int u = wave; u < units; u += kI8LastWaves) {
         if (u != wave) begin(u);
-        i32x4acc_t acc[1] = {};
+        i32x4_t acc[1] = {};
         if (ok) {
             const char* const row = s_codes + (long)(u / seg) * (A.Kp + 16);
             thin.run(acc, lane, [&](int col) { return *(const uint4*)(row + col); });
@@ -1168,7 +1167,7 @@ template <int KT>
 constexpr int kI8Lds = 2 * kI8TileRows * 128 * KT;
 static_assert(2 * kI8TileWide * 128 <= kI8Lds<2>, "the wide tiles' buffers fit in the tall ones'");
 static_assert(4 * kI8EpiWave<2> <= kI8Lds<2> && 4 * kI8EpiWave<1> <= kI8Lds<1>, "the epilogue areas fit in the buffers");
-static_assert(sizeof(I8TileRec) == 80, "as the workspace has it");
+static_assert(sizeof(I8TileRec) == 80 && offsetof(I8TileRec, mat) == 32, "as the plan writes it");
 static_assert(4 * kI8EpiWave<1> <= 2 * 32 * 128 * 4, "also in those of a wide tile");
 
 // per-device set-up, with the device current
@@ -1388,7 +1387,7 @@ using namespace dymoe;
 extern "C" size_t dymoe_matmul_int8_workspace_bytes(int T, int N, int K)
 {
     if (T < 0 || N <= 0 || K <= 0 || K > DYMOE_INT8_MAX_K) return 0;
-    return i8_mat_layout(T, N, K).total;
+    return i8_mat_layout(T, K).total;
 }
 
 extern "C" int dymoe_matmul_int8(dymoe_ctx* ctx, const void* x, int x_dtype, const float* x_scale, long ldx, const int8_t* w,
@@ -1406,7 +1405,7 @@ extern "C" int dymoe_matmul_int8(dymoe_ctx* ctx, const void* x, int x_dtype, con
     DYMOE_REQUIRE(dymoe_aligned(x_scale, 4) && dymoe_aligned(w_scale, 4) && dymoe_aligned(bias, 4) && dymoe_aligned(workspace, 256));
     if (K > DYMOE_INT8_MAX_K) return DYMOE_ENOTSUP;
     if (T > (1 << 24) || N > (1 << 24)) return DYMOE_ENOTSUP;
-    const I8MatLayout L = i8_mat_layout(T, N, K);
+    const I8MatLayout L = i8_mat_layout(T, K);
     if (!coded && T > 0 && workspace_bytes < L.total) return DYMOE_ENOSPC;
     if (((T + 63L) / 64) * ((N + 31L) / 32) > 0x7fff0000L) return DYMOE_ENOTSUP;
     if (!ctx) return DYMOE_ENOCTX;
@@ -1490,11 +1489,11 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     DYMOE_REQUIRE(dymoe_aligned(x, dtype_bytes(x_dtype)) && dymoe_aligned(y, dtype_bytes(out_dtype)) && dymoe_aligned(workspace, 256));
     DYMOE_REQUIRE(dymoe_aligned(idx, 4) && dymoe_aligned(w, 4) && dymoe_aligned(table, 8));
     if (E > DYMOE_MAX_EXPERTS || H > DYMOE_INT8_MAX_K || F > DYMOE_INT8_MAX_K) return DYMOE_ENOTSUP;
-    if ((long)T * k > 0x7fffffffL / 4 || (long)T * up_to(H, 128) > 0xffffffffL) return DYMOE_ENOTSUP;      // (32-bit offsets into the codes)
+    if ((long)T * k >= 1L << 29 || (long)T * up_to(H, 128) >= 1L << 32) return DYMOE_ENOTSUP;      // (32-bit offsets into the codes)
     const I8FfnLayout L = i8_ffn_layout(T, H, F, E, k);
     if (workspace_bytes < L.total) return DYMOE_ENOSPC;
     const long up = (long)L.max_tiles * ((F + 31L) / 32), down = (long)L.max_tiles * ((H + 31L) / 32);      // workgroups at most
-    if (up > 0x7fff0000L || down > 0x7fff0000L || T * ((H + 2047L) / 2048) > 0x7fffffffL) return DYMOE_ENOTSUP;
+    if (up > 0x7fff0000L || down > 0x7fff0000L || T * ((H + 2047L) / 2048) >= 1L << 23) return DYMOE_ENOTSUP;      // (256 threads a row, 2^32 a grid)
     if (!ctx) return DYMOE_ENOCTX;
     if (T == 0) return DYMOE_OK;
     hipStream_t st = (hipStream_t)stream;
@@ -1552,13 +1551,11 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     A.x = ws + L.xq;
     A.xs = (const float*)(ws + L.xs);
     A.plan = plan;
-    A.table = table;
     A.out = ws + L.h;
     A.ldo = (long)L.Fp;
     A.P = P;
     A.Kp = (int)L.Hp;
     A.N = F;
-    A.E = E;
     A.k = k;
     A.rows = T;
     if (small) dymoe_launch(ctx, DYMOE_K_INT8_UP, i8_small_kernel<kI8Up, 1, 4, 1>, dim3((unsigned)up), dim3(256), 0, st, A);

@@ -50,9 +50,8 @@ struct I8MatLayout {
     size_t total;
 };
 
-static inline I8MatLayout i8_mat_layout(long T, long N, long K)
+static inline I8MatLayout i8_mat_layout(long T, long K)
 {
-    (void)N;
     I8MatLayout L;
     L.Kp = i8_round((size_t)K, 128);
     L.xq = 0;

@@ -86,11 +86,20 @@ static int quantize_rows_launch(dymoe_ctx* ctx, const void* x, long rows, long K
     return DYMOE_OK;
 }
 
+// rows of a launch at most: 1024 threads a row stay below the 2^32 of a grid
+constexpr long kRowsLaunch = 1L << 21;
+
 int quantize_rows(dymoe_ctx* ctx, const void* x, int dtype, long rows, long K, long ldx, int tiles, void* codes, float* scale, hipStream_t st)
 {
-    if (dtype == DYMOE_OUT_F32) return quantize_rows_launch<DYMOE_OUT_F32>(ctx, x, rows, K, ldx, tiles, codes, scale, st);
-    if (dtype == DYMOE_OUT_F16) return quantize_rows_launch<DYMOE_OUT_F16>(ctx, x, rows, K, ldx, tiles, codes, scale, st);
-    return quantize_rows_launch<DYMOE_OUT_BF16>(ctx, x, rows, K, ldx, tiles, codes, scale, st);
+    auto launch = quantize_rows_launch<DYMOE_OUT_BF16>;
+    if (dtype == DYMOE_OUT_F32) launch = quantize_rows_launch<DYMOE_OUT_F32>;
+    else if (dtype == DYMOE_OUT_F16) launch = quantize_rows_launch<DYMOE_OUT_F16>;
+    for (long r = 0; r < rows; r += kRowsLaunch) {
+        const long n = rows - r < kRowsLaunch ? rows - r : kRowsLaunch;
+        const int rc = launch(ctx, (const char*)x + r * ldx * dtype_bytes(dtype), n, K, ldx, tiles, (char*)codes + r * up_to(K, 128), scale + r, st);
+        if (rc != DYMOE_OK) return rc;
+    }
+    return DYMOE_OK;
 }
 
 }  // namespace dymoe

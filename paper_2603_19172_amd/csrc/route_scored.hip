@@ -299,7 +299,7 @@ extern "C" int dymoe_route_scored(dymoe_ctx* ctx, const void* logits, int dtype,
     if (T > 0) DYMOE_REQUIRE(logits && idx && w);
     DYMOE_REQUIRE(dymoe_aligned(logits, dymoe::dtype_bytes(dtype)) && dymoe_aligned(idx, 4) && dymoe_aligned(w, 4));
     DYMOE_REQUIRE(dymoe_aligned(bias, 4) && dymoe_aligned(scores, 4));
-    if (E > DYMOE_MAX_EXPERTS || k > 64 || groups > 64) return DYMOE_ENOTSUP;
+    if (E > DYMOE_MAX_EXPERTS || k > 64 || groups > 64 || T >= 1 << 26) return DYMOE_ENOTSUP;      // (64 threads a token, 2^32 a grid)
     if (!ctx) return DYMOE_ENOCTX;
     if (T == 0) return DYMOE_OK;
     auto launch = dymoe::route_scored_launch<DYMOE_OUT_BF16>;

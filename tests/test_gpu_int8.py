@@ -215,6 +215,23 @@ def test_rows_apart_and_unaligned(ctx, K, pitch, off):
 
 # ------------------------------------------------------------------------------------------------------------------ product
 
+@pytest.mark.parametrize("layout", [B.LAYOUT_ROWMAJOR, B.LAYOUT_TILE])
+def test_rows_of_more_than_one_launch(ctx, layout):
+    rows, K = (1 << 21) + 37, 5
+    x = randn(8, rows, K)
+    codes, scale = ctx.quantize_rows(x, layout=layout)
+    cut = (1 << 21) - 64                             # both sides of the launches' border
+    want, ws = Q.quantize_rows(f64(x[cut:]))
+    if layout == B.LAYOUT_TILE:
+        want = Q.tiles(want)
+    else:
+        want = np.pad(want, ((0, 0), (0, 128 - K)))
+    assert np.array_equal(codes[cut:].cpu().numpy().reshape(want.shape), want)
+    assert np.array_equal(scale[cut:].cpu().numpy(), ws.astype(np.float32))
+    peak = x.double().abs().amax(1) / 127.0          # (scale: that, rounded once)
+    assert ((scale.double() - peak).abs() <= 2.0 ** -24 * peak).all() and torch.equal(codes[:64], ctx.quantize_rows(x[:64], layout=layout)[0])
+
+
 def matmul_bound(prod, y, dtype):
     return 4 * 2.0 ** -24 * np.abs(prod) + (HALF[dtype] + 2 * 2.0 ** -24) * np.abs(y) + (2.0 ** -25 if dtype == torch.float16 else 0.0)
 

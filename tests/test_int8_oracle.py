@@ -130,6 +130,16 @@ def test_argument_checks_come_before_device_work():
     assert ff(T=1 << 29, n=1 << 62) == B.ENOTSUP
 
 
+def test_calls_beyond_a_grid_are_refused():
+    lib = B.lib
+    rs = lambda T: lib.dymoe_route_scored(None, P, 0, None, T, 8, 2, 1, 1, 1, 1, 1, 1.0, P, P, None, None)
+    assert rs((1 << 26) - 1) == B.ENOCTX and rs(1 << 26) == B.ENOTSUP
+    ff = lambda T, H, k: lib.dymoe_moe_ffn_int8(None, P, 0, P, P, P, T, H, 8, 8, k, 0, P, P, 1 << 62, None)
+    assert ff((1 << 23) - 1, 128, 1) == B.ENOCTX and ff(1 << 23, 128, 1) == B.ENOTSUP
+    assert ff((1 << 22) - 1, 1024, 8) == B.ENOCTX and ff(1 << 22, 1024, 8) == B.ENOTSUP
+    assert ff((1 << 22) - 1, 2050, 1) == B.ENOTSUP and ff((1 << 20) - 1, 4096, 1) == B.ENOCTX
+
+
 def test_binding_checks_shapes_and_types():
     class Fake:
         _h, device = None, 0
