@@ -722,17 +722,19 @@ size_t dymoe_cache_bytes_resident(const dymoe_cache* cache);
  * (bit i = kernel id i, ids 0..28 in the order route, token_norm, importance,
  * assign, quantize, gemv_phase1, gemv_phase2, gemv_combine, plan, gemm1, gemm2,
  * gemm_combine, stream_copy, decode_front, attn_stats, attn_colsum, gptq_group,
- * gptq_trail, gptq_hessian, gptq_factor, mfma_peak, route_select, route_scored, quantize_rows, matmul_int8, int8_plan, int8_up, int8_down,
- * int8_combine; gemv_combine is reserved: the decode path's
+ * gptq_trail, gptq_hessian, gptq_factor, mfma_peak, route_select, route_scored, quantize_rows, matmul_int8,
+ * int8_plan, int8_up, int8_down, int8_combine; gemv_combine is reserved: the decode path's
  * second phase writes y itself and no launch carries that id; route_select is the second of the two launches
- * dymoe_route_topk makes when it cuts the logits by experts as well as by tokens, route then names the first) carry a start and a stop HIP event on the dispatch itself, so
+ * dymoe_route_topk makes when it cuts the logits by experts as well as by tokens, route then names the first;
+ * int8_down of a few tokens includes the sum over the slots) carry a start and a stop HIP event on the dispatch itself, so
  * the interval is the kernel's execution time on the launch stream; 0 switches
  * timing off.  Either way, records not yet read are dropped.
  * dymoe_timing_read: waits for the recorded launches of `kernel`, drops their records and returns
  * their summed duration in milliseconds and their count (host pointers).
  * Do not enable timing while the stream is being captured into a graph.
  * dymoe_kernel_name: the kernel's name as a profiler shows it, NULL if unknown.  Where sizes choose between kernels
- * for a step it is one of theirs (attn_rowstats_kernel, for attn_rowstats_wide_kernel as well); gptq_group and
+ * for a step it is one of theirs (attn_rowstats_kernel, for attn_rowstats_wide_kernel as well; i8_matmul_kernel and
+ * i8_experts_kernel, for the shapes of few rows as well); gptq_group and
  * gptq_trail are launches of one kernel, a panel alone and a panel with the columns behind it.
  */
 int dymoe_timing_enable(dymoe_ctx* ctx, unsigned kernel_mask);

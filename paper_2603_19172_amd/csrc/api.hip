@@ -224,10 +224,10 @@ const char* dymoe_kernel_name(int kernel)
     case DYMOE_K_ROUTE_SELECT: return "route_select_kernel";
     case DYMOE_K_ROUTE_SCORED: return "route_scored_kernel";
     case DYMOE_K_QUANTIZE_ROWS: return "quantize_rows_kernel";
-    case DYMOE_K_MATMUL_INT8: return "i8_small_kernel<0>";
-    case DYMOE_K_INT8_PLAN: return "i8_plan_kernel";
-    case DYMOE_K_INT8_UP: return "i8_small_kernel<1>";
-    case DYMOE_K_INT8_DOWN: return "i8_small_kernel<2>";
+    case DYMOE_K_MATMUL_INT8: return "i8_matmul_kernel";
+    case DYMOE_K_INT8_PLAN: return "i8_prep_kernel";
+    case DYMOE_K_INT8_UP: return "i8_experts_kernel<1>";
+    case DYMOE_K_INT8_DOWN: return "i8_experts_kernel<2>";
     case DYMOE_K_INT8_COMBINE: return "i8_combine_kernel";
     default: return nullptr;
     }

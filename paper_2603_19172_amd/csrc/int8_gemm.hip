@@ -48,7 +48,8 @@ __device__ __forceinline__ bool i8_present(const dymoe_expert_i8& x)
 // in its expert is what the counter held before it: kept in registers (in `where` beyond the first kI8PlanKeep pairs of a thread)
 // until the experts' first positions are known, so that there is one pass of atomics.  The turns come in any order, and nothing that is
 // computed depends on it.  The sorted pairs and the tiles' experts pass through LDS where they fit: written from the threads that
-// know them, 16384 pairs cost 7 us in stores of four bytes each, and an expert's sixteen records 3 us in one thread.
+// know them, 16384 pairs cost 7 us in stores of four bytes each, and an expert's sixteen records 3 us in one thread.  16384 pairs of 128
+// experts 13.6 us with 2048 rows' codes beside it, 488 pairs 4.9: latencies of one workgroup's passes, not bytes.
 constexpr int kI8PlanThreads = 1024;
 constexpr int kI8PlanKeep = 16;
 constexpr int kI8PlanPairs = kI8PlanKeep * kI8PlanThreads;
@@ -274,12 +275,25 @@ __device__ __forceinline__ float silu_times(float a, float u) { return a * __bui
 // rows' quantisation, which every workgroup then does for itself where the rows are few, costs no launch and hides behind them.
 // v_mfma_i32_16x16x64_i8: lane l holds weight row l % 16 and row l % 16 of the codes, columns 64 (l / 32) + 32 j + 16 (l / 16 % 2) of a
 // tile in its j-th product (any order of columns will do that is the same on both sides).
+// Bound by the weights' bytes: one token on two experts of 14336 x 4096, up 38.7 us (6.0 TB/s) and down 24.1 us (4.9 TB/s); a matrix of
+// 128256 x 4096 and one token 83 us (6.3 TB/s).
 constexpr int kI8Ahead = 4;
 constexpr int kI8ThinRows = 16;
 constexpr int kI8ThinWaves = 8;
-constexpr int kI8FuseRows = 4;                  // tokens up to which the experts' workgroups quantise rows themselves
+// Up to 8 rows any matrix, up to 16 while the outputs are few (a workgroup reads its rows' codes for 16 weight rows only): 16 rows of 4096
+// values, N = 4096 8.8 us here and 10.0 in the shapes below, N = 14336 18.6 / 20.3, N = 32000 31 / 31.5, N = 64000 58.6 / 52.6.
+constexpr long kI8ThinOut = 3 << 18;
+// Tokens up to which the experts' workgroups quantise rows themselves: two launches instead of five, but every workgroup of the down
+// projection reads its token's intermediate, and an expert that two tokens share is read for each.  One token on 8 of 128 experts of 768 x 2048
+// 18.1 us and 25.1 in five launches, two 26.3 / 30.3, three 38.9 / 36.7, four 42.4 / 39.8; 2 of 8 experts of 14336 x 4096: 66 / 75,
+// 113 / 114, 163 / 140, 188 / 155.
+constexpr int kI8FuseRows = 2;
 constexpr long kI8FuseBytes = 64 * 1024;        // the codes' bytes in LDS at most
-constexpr long kI8FuseReads = 16 << 20;         // values that the workgroups of a plain product read to quantise them, together, at most
+// The plain product's workgroups quantise where that is less than a launch of its own: T * K values for a workgroup, and all
+// workgroups' together.  With T = 8, N = 1536, K = 2048 5.1 us and 5.9 with the launch, T = 16 6.9 / 6.3; T = 1 on 4096 x 14336 13.5 / 16.7, T = 4
+// 21.8 / 17.1; T = 2 on 4096 x 4096 6.8 / 7.8, T = 4 8.2 / 7.9; T = 2 on 14336 x 4096 14.8 / 14.2.
+constexpr long kI8FuseRow = 16 << 10;
+constexpr long kI8FuseReads = 4 << 20;
 
 __device__ __forceinline__ i32x4_t mfma16_i8(const uint4 a, const uint4 b, const i32x4_t c)
 {
@@ -338,7 +352,7 @@ template <int DT>
 __device__ __forceinline__ void i8_rows_to_lds(const char* x, long pitch, int rows, int K, int Kp, char* s_codes, float* s_scale, uint32_t* s_max)
 {
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, n = blockDim.x, waves = n / kWave;
-    if (2 * rows >= waves || K <= 1024) {           // a wavefront a row: nothing to hand over
+    if (3 * rows >= waves || K <= 1024) {           // a wavefront a row: nothing to hand over
         for (int r = wave; r < rows; r += waves) {
             uint32_t m = 0;
 #pragma unroll 2
@@ -543,6 +557,9 @@ __global__ __launch_bounds__(64 * kI8LastWaves) void i8_thin_down_kernel(const I
 //  * Several workgroups on a compute unit, one's waits, prologue and epilogue covered by the others' products.
 // Two shapes: S = 2, KT = 2 (128 accumulator registers a lane, two workgroups a compute unit) reads half as much LDS for a product; S = 1,
 // KT = 1 (64, four workgroups) has more loads on their way and twice as many workgroups, for calls that the weights' bytes bound.
+// 2048 x 14336 x 4096: 131 us, 1.84 POP/s (with random codes; the same kernel takes 102 us on zeros, since the clock follows the power: products from
+// registers alone reach 4.4 POP/s on quiet data and 3.4 on random).  Without its copies of rows it takes 129 us, without its loads
+// of weights 113, with neither 104 to 108: the products and their LDS reads are what is left.
 template <int S>
 constexpr uint32_t kI8EpiRow = S == 2 ? 272 : 144;     // epilogue: bytes of a row of 32 S sums in LDS, 16 of them padding
 template <int S>
@@ -839,6 +856,8 @@ __device__ __forceinline__ void i8_tile(const I8Args& A, const int32_t* perm, co
 // wavefront, four tiles of weights on their way in registers, the rows' codes through registers into two LDS buffers.  Bytes on
 // their way are what sets the rate of such a stream; with the rows copied to LDS directly, as above, the loads of weights could run
 // ahead by one step only, because a count of outstanding loads that lets the copies through has to wait for all loads before them.
+// Eight experts of 14336 x 4096, 64 to 160 pairs each: up 230 us (4.1 TB/s of weights), without its products 217, without its rows 208; with
+// non-temporal loads of the weights 238.
 constexpr int kI8Deep = 4;
 
 template <int MODE, int NTF>
@@ -928,7 +947,7 @@ __device__ __forceinline__ void i8_wide_tile(const I8Args& A, const int32_t* per
     i8_finish<MODE, NTF, 1>(A, perm, acc, sa, sb, row0, rows, bx, expert, xs_base);
 }
 
-constexpr int kI8Run = 16;      // neighbouring units that an XCD takes at a time
+constexpr int kI8Run = 16;      // neighbouring units that an XCD takes at a time: the weights of a tile row stay in its L2
 
 // columns of a workgroup's block
 template <int MODE, int S>
@@ -1020,7 +1039,8 @@ __global__ __launch_bounds__(256, S == 2 ? 2 : 4) void i8_matmul_kernel(const I8
 
 // The plain product where its tiles are fewer than the chip takes: G groups of four wavefronts share a tile of 128 x 128 outputs and split K,
 // each with LDS buffers of its own; at the end a fragment after the other meets in LDS and the groups finish eight of its rows each.  (Alone on
-// a compute unit a step costs 0.8 us, the latency of its copies; 256 x 4096 outputs over 4096 columns took 32 of them.)
+// a compute unit a step costs 0.8 us, the latency of its copies; 256 x 4096 outputs over 4096 columns took 32 of them, 26.8 us, and in four
+// groups 22.)
 template <int NTF, int G>
 __device__ __forceinline__ void i8_split_tile(const I8Args& A, const I8Unit<1>& u, int wave, int group, uint32_t xs_base)
 {
@@ -1120,6 +1140,9 @@ __global__ __launch_bounds__(256 * G, 4) void i8_split_kernel(const I8Args A)
 
 // Experts.  One that more than kI8TileWide pairs go to takes tiles of 128 rows and two strips a wavefront; the others, whose weights' bytes
 // bound them, one wide tile.  Runs of the two kinds alternate in proportion, so that the chip multiplies while it reads.
+// The whole call with 160, 128 and 96 as the wide tiles' limit, and with tall tiles alone: 512 tokens, 2 of 8 experts of 14336 x 4096 353, 368, 388
+// and 387 us, 2048 tokens 851, 874, 855 and 886; 2048 tokens, 8 of 128 experts of 768 x 2048 228, 235, 234 and 248, 512 tokens 157, 159, 158 and 158.
+// Up and down: 228 and 120 us (512 tokens, large experts; 4.1 TB/s of weights), 127 and 85 (2048, small ones, loads skewed).
 template <int MODE>
 __global__ __launch_bounds__(256, 2) void i8_experts_kernel(const I8Args A)
 {
@@ -1194,6 +1217,7 @@ static dim3 i8_grid(long units, int kinds)
 // shared before the end: weights and codes come straight into registers, D tiles of a wavefront on their way, and the sums meet in LDS.
 // A load of codes that lie row by row touches a line for each of its 64 lanes; the plain product therefore has its rows quantised into
 // the weights' tile layout (A.tiled), where it is 1 KiB of contiguous memory.
+// 61 x 1536 x 2048: 5.8 us (10.8 in tiles of 128 x 128); 61 tokens, 8 of 128 experts of 768 x 2048: up 61 us (6.5 TB/s), down 31.8 (6.3 TB/s).
 template <int MODE, int NTF, int NW, int D>
 __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void i8_small_kernel(const I8Args A)
 {
@@ -1329,7 +1353,8 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void i8_small_kernel(cons
     }
 }
 
-// y[t] = sum over the slots, in their order, of gate times the pair's output.  A workgroup takes 2048 outputs of a token.
+// y[t] = sum over the slots, in their order, of gate times the pair's output.  A workgroup takes 2048 outputs of a token.  Bound by the pairs'
+// bytes: 16384 pairs of 2048 outputs in 16 bits 14.1 us (4.8 TB/s).
 template <bool HALF>
 __global__ __launch_bounds__(256) void i8_combine_kernel(const char* __restrict__ part, long ldp, const float* __restrict__ hs,
                                                          const float* __restrict__ strip_scale, const dymoe_expert_i8* __restrict__ table,
@@ -1412,7 +1437,11 @@ extern "C" int dymoe_matmul_int8(dymoe_ctx* ctx, const void* x, int x_dtype, con
     if (T == 0) return DYMOE_OK;
     hipStream_t st = (hipStream_t)stream;
     char* const ws = (char*)workspace;
-    const bool thin = T <= kI8ThinRows, small = !thin && ((T + 63L) / 64) * ((N + 31L) / 32) <= ctx->num_cu * 5L / 4, fuse = thin && !coded && T * (long)(L.Kp + 16) <= kI8FuseBytes && (N + 15L) / 16 * T * K <= kI8FuseReads;
+    const bool thin = T <= kI8ThinRows && (T <= 8 || (long)T * N <= kI8ThinOut);
+    // (strips of 32 columns: up to 1.25 of them a compute unit, beyond which they come in two rounds; T = 128, N = K = 4096: 13.9 us and 21.8 in
+    // tiles of 128 x 128 with K split; T = 100, N = 14336, K = 4096: 39 and 22)
+    const bool small = !thin && ((T + 63L) / 64) * ((N + 31L) / 32) <= ctx->num_cu * 5L / 4;
+    const bool fuse = thin && !coded && (long)T * K <= kI8FuseRow && (N + 15L) / 16 * T * K < kI8FuseReads;
     I8Args A = {};
     A.x = (const char*)x;
     A.xs = x_scale;
@@ -1455,12 +1484,16 @@ extern "C" int dymoe_matmul_int8(dymoe_ctx* ctx, const void* x, int x_dtype, con
     }
     A.aligned = dymoe_aligned(y, 4 * dtype_bytes(out_dtype)) && ldy % 4 == 0;
     if (!small) {
+        // (K split in four up to a tile a compute unit: 256 x 4096 x 4096 22 us, unsplit 26.8, as 32-column strips 24.7.  In two a little beyond.
+        // Two strips a wavefront from two workgroups a compute unit on, where K is long enough for their longer start: 8192 x 8192 x 8192
+        // 492 us, one strip 551; 4096 x 9000 x 700 67 and 57.)
         const long tiles = (T + kI8TileRows - 1L) / kI8TileRows;
         const long units2 = tiles * ((N + 255L) / 256), units1 = tiles * ((N + 127L) / 128);
         const long cu = ctx->num_cu;
-        if (units1 <= cu && L.Kp >= 1024) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_split_kernel<4>, i8_grid(units1, 1), dim3(1024), kI8SplitLds<4>, st, A);
-        else if (units1 <= cu * 5 / 4) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_split_kernel<2>, i8_grid(units1, 1), dim3(512), kI8SplitLds<2>, st, A);
-        else if (units2 < 2 * cu || L.Kp < 2048) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_matmul_kernel<1, 1>, i8_grid(units1, 1), dim3(256), kI8Lds<1>, st, A);
+        const dim3 grid1 = i8_grid(units1, 1);
+        if (units1 <= cu && L.Kp >= 1024) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_split_kernel<4>, grid1, dim3(1024), kI8SplitLds<4>, st, A);
+        else if (units1 <= cu * 5 / 4) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_split_kernel<2>, grid1, dim3(512), kI8SplitLds<2>, st, A);
+        else if (units2 < 2 * cu || L.Kp < 2048) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_matmul_kernel<1, 1>, grid1, dim3(256), kI8Lds<1>, st, A);
         else dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_matmul_kernel<2, 2>, i8_grid(units2, 1), dim3(256), kI8Lds<2>, st, A);
     } else {
         const long strips = (N + 31L) / 32;
@@ -1532,7 +1565,11 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
         DYMOE_HIP_LAUNCH_CHECK();
         return DYMOE_OK;
     }
-    const bool small = T <= 32 || P <= 8L * E;
+    // Tiles of 32 rows and a sum in LDS while an expert meets 20 pairs or fewer on average (or never more than 32): 64 tokens, 2 of 8 experts of
+    // 14336 x 4096 (16 pairs an expert) 239 us and 267 in wide tiles, 80 tokens (20) 255 / 269, 96 (24) 274 / 273, 128 (32) 386 / 281; 8 of 128 experts
+    // of 768 x 2048, 256 tokens (16) 128 / 143, 320 (20) 135.5 / 146.4, 384 (24) 146.2 / 149.4, 512 (32) 192 / 157; 32 tokens on all of 8 such experts
+    // 25.8 / 34.3.
+    const bool small = T <= 32 || P <= 20L * E;
     // Workgroups at most: an expert of n pairs has n / 128 + 1 tall tiles at half as many column blocks, or one wide tile.
     const long tall = P / kI8TileRows + P / (kI8TileWide + 1), wide = E < P ? E : P;
     int32_t* const plan = (int32_t*)(ws + L.plan);
@@ -1558,8 +1595,10 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     A.N = F;
     A.k = k;
     A.rows = T;
+    const dim3 up_grid = i8_grid(tall * ((F + 127L) / 128) + wide * ((F + 63L) / 64), 2);
+    const dim3 down_grid = i8_grid(tall * ((H + 255L) / 256) + wide * ((H + 127L) / 128), 2);
     if (small) dymoe_launch(ctx, DYMOE_K_INT8_UP, i8_small_kernel<kI8Up, 1, 4, 1>, dim3((unsigned)up), dim3(256), 0, st, A);
-    else dymoe_launch(ctx, DYMOE_K_INT8_UP, i8_experts_kernel<kI8Up>, i8_grid(tall * ((F + 127L) / 128) + wide * ((F + 63L) / 64), 2), dim3(256), kI8Lds<2>, st, A);
+    else dymoe_launch(ctx, DYMOE_K_INT8_UP, i8_experts_kernel<kI8Up>, up_grid, dim3(256), kI8Lds<2>, st, A);
     rc = quantize_rows(ctx, ws + L.h, DYMOE_OUT_F32, P, F, (long)L.Fp, 0, ws + L.hq, (float*)(ws + L.hs), st);
     if (rc != DYMOE_OK) return rc;
     A.x = ws + L.hq;
@@ -1572,7 +1611,7 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     A.strip_scale = half ? (float*)(ws + L.strips) : nullptr;
     A.sum_scale = 32768.0f / (16129.0f * (float)F);
     if (small) dymoe_launch(ctx, DYMOE_K_INT8_DOWN, i8_small_kernel<kI8Down, 1, 4, 1>, dim3((unsigned)down), dim3(256), 0, st, A);
-    else dymoe_launch(ctx, DYMOE_K_INT8_DOWN, i8_experts_kernel<kI8Down>, i8_grid(tall * ((H + 255L) / 256) + wide * ((H + 127L) / 128), 2), dim3(256), kI8Lds<2>, st, A);
+    else dymoe_launch(ctx, DYMOE_K_INT8_DOWN, i8_experts_kernel<kI8Down>, down_grid, dim3(256), kI8Lds<2>, st, A);
     const dim3 grid((unsigned)(T * ((H + 2047L) / 2048)));
     auto combine = half ? i8_combine_kernel<true> : i8_combine_kernel<false>;
     dymoe_launch(ctx, DYMOE_K_INT8_COMBINE, combine, grid, dim3(256), 0, st, ws + L.part, (long)L.Hp, (const float*)(ws + L.hs),

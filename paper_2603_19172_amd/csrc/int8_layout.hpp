@@ -16,8 +16,8 @@ struct I8FfnLayout {
     size_t xq, xs;     // [T, Hp] codes and [T] scales of the activations
     size_t h;          // [P, Fp] SwiGLU intermediate, by position (pairs sorted by expert)
     size_t hq, hs;     // [P, Fp] its codes, [P] their scales
-    size_t part;       // [P, Hp] outputs of the pairs, by position: fp32, or fp16 with
-    size_t strips;     // [E, strips of 32 outputs] their scales
+    size_t part;       // [P, Hp] outputs of the pairs, by position: fp32, or fp16 and
+    size_t strips;     // [E, strips of 32 outputs] their scales (negative: each channel has its own)
     size_t plan;       // int32, see I8Plan
     size_t total;
     int max_tiles;

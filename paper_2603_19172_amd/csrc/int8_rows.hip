@@ -2,8 +2,9 @@
 //
 // a = max |x|, scale = a / 127, code = rint(127 x / a).  A stream of bytes: 2 read and 1 written a value (bf16 or fp16).  A row stays in
 // the registers of the threads that share it between the search for its largest value and its codes, so it is read once.  A wavefront
-// takes a row of up to 4096 values where the rows are many; with few rows, or longer ones, the four wavefronts of a workgroup share
-// one, and beyond 16384 values sixteen.
+// takes a row of up to 2048 values where the rows are many; with few rows, or longer ones, the four wavefronts of a workgroup share
+// one, and beyond 16384 values sixteen.  8191 rows of 14336 in bf16 65 us, 5.4 TB/s, what a copy of a GiB reaches on this card (5.2 to
+// 5.5); 24 rows of 4096 2.6 us, a launch's latencies.
 #include "int8_device.hpp"
 
 namespace dymoe {
@@ -68,12 +69,13 @@ static int quantize_rows_launch(dymoe_ctx* ctx, const void* x, long rows, long K
     dymoe_launch(ctx, DYMOE_K_QUANTIZE_ROWS, quantize_rows_kernel<DT, WAVES, CH>,                                               \
                  dim3((unsigned)(WAVES == 1 ? (out_rows + 3) / 4 : out_rows)), dim3(WAVES == 1 ? 256 : 64 * WAVES), 0, st,      \
                  (const char*)x, rows, K, ldx, tiles, out_rows, (char*)codes, scale)
-    // a wavefront a row once that fills the chip's wavefront slots about twice
-    const bool many = out_rows >= 16L * ctx->num_cu;
+    // A wavefront a row of up to 2048 values once there are eight for a compute unit, else a workgroup a row: 2048 rows of 768 3.4 us and 4.1, of
+    // 2048 4.0 / 4.5, 16384 rows 8.4 / 14.1 and 16.9 / 18.0; 512 rows 4.5 / 4.1 and 3.4 / 3.0.  Rows of 4096 are a workgroup's at any number: 65536
+    // of them 137 us, by a wavefront each 147.
+    const bool many = out_rows >= 8L * ctx->num_cu;
     if (Kp <= 512) DYMOE_QROWS(1, 1);
     else if (Kp <= 1024 && many) DYMOE_QROWS(1, 2);
     else if (Kp <= 2048 && many) DYMOE_QROWS(1, 4);
-    else if (Kp <= 4096 && many) DYMOE_QROWS(1, 8);
     else if (Kp <= 2048) DYMOE_QROWS(4, 1);
     else if (Kp <= 4096) DYMOE_QROWS(4, 2);
     else if (Kp <= 8192) DYMOE_QROWS(4, 4);

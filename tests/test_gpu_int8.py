@@ -326,6 +326,19 @@ def test_matmul_rows_with_a_bias_do_not_depend_on_their_company(ctx, N, K):
         assert torch.equal(ctx.matmul_int8(x[lo:hi], wt, bias=bias, out_dtype=B.OUT_F32), y[lo:hi])
 
 
+@pytest.mark.parametrize("T", [1, 8, 12, 16, 40])
+def test_matmul_many_outputs(ctx, T):
+    """Wider matrices than the shapes of a few rows are for from nine rows on."""
+    N, K = 90001, 130
+    wt, (wq, ws) = weight(ctx, T, N, K)
+    x, bias = randn(T, T, K), randn(T + 1, N, dtype=torch.float32)
+    y = f64(ctx.matmul_int8(x, wt, bias=bias, out_dtype=B.OUT_F32))
+    xq, xs = Q.quantize_rows(f64(x))
+    prod = Q.matmul(xq, xs, wq, ws)
+    want = prod + f64(bias)
+    assert (np.abs(y - want) <= matmul_bound(prod, want, torch.float32)).all()
+
+
 # ------------------------------------------------------------------------------------------------------------------ experts
 
 def make_experts(ctx, seed, E, H, F, absent=()):
