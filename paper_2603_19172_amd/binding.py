@@ -282,6 +282,17 @@ def _stream(stream):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _empty(shape, dtype, device, stream):
+    """Memory that a call on `stream` allocates: of that stream, so that no other work gets it back before the call has run."""
+    if stream is None or _stream(stream) == _raw_stream(_current_device()):
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = _stream(stream)
+        stream = torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def workspace_bytes(T, H, F, E, k) -> int:
     return int(lib.dymoe_workspace_bytes(T, H, F, E, k))
 
@@ -570,9 +581,9 @@ class Context:
         """logits [T, E] bf16 / fp16 / fp32 -> idx [T, k] int32, w [T, k] fp32; scores: a [T, E] fp32 tensor to fill."""
         (T, E), dev, dtype = logits.shape, self.device, _dtype_code(logits)
         if idx is None:
-            idx = torch.empty((T, k), dtype=torch.int32, device=logits.device)
+            idx = _empty((T, k), torch.int32, logits.device, stream)
         if w is None:
-            w = torch.empty((T, k), dtype=torch.float32, device=logits.device)
+            w = _empty((T, k), torch.float32, logits.device, stream)
         _check(lib.dymoe_route_scored(self._h, _at(logits, dev, None, (T, E)), dtype, _at(bias, dev, torch.float32, (E,)), T, E, k, score,
                                       groups, top_groups, group_best, 1 if renorm else 0, factor, _at(idx, dev, torch.int32, (T, k)),
                                       _at(w, dev, torch.float32, (T, k)), _at(scores, dev, torch.float32, (T, E)),
@@ -584,7 +595,7 @@ class Context:
         (rows, K, pitch), dev = _matrix(x), self.device
         shape = (_up(rows, 32) if layout == LAYOUT_TILE else rows, _up(K, 128))
         if out is None:
-            out = (torch.empty(shape, dtype=torch.int8, device=x.device), torch.empty((rows,), dtype=torch.float32, device=x.device))
+            out = (_empty(shape, torch.int8, x.device, stream), _empty((rows,), torch.float32, x.device, stream))
         _check(lib.dymoe_quantize_rows(self._h, _at(x, dev), _dtype_code(x), rows, K, pitch, layout, _at(out[0], dev, torch.int8, shape),
                                        _at(out[1], dev, torch.float32, (rows,)), _stream_of(dev, stream)), "dymoe_quantize_rows")
         return out
@@ -598,9 +609,9 @@ class Context:
             if K % 128 or x_scale is None:
                 raise ValueError("int8 codes come as quantize_rows wrote them, with their scales")
         elif workspace is None:
-            workspace = torch.empty((matmul_int8_workspace_bytes(T, N, K),), dtype=torch.uint8, device=x.device)
+            workspace = _empty((matmul_int8_workspace_bytes(T, N, K),), torch.uint8, x.device, stream)
         if y is None:
-            y = torch.empty((T, N), dtype=_TORCH_OUT[out_dtype], device=x.device)
+            y = _empty((T, N), _TORCH_OUT[out_dtype], x.device, stream)
         rows, cols, ldy = _matrix(y)
         if rows != T or cols != N:
             raise ValueError("y has shape %s, expected %s" % (tuple(y.shape), (T, N)))
@@ -618,9 +629,9 @@ class Context:
         if not table.is_contiguous():
             raise ValueError("the table has to be contiguous")
         if y is None:
-            y = torch.empty((T, H), dtype=_TORCH_OUT[out_dtype], device=x.device)
+            y = _empty((T, H), _TORCH_OUT[out_dtype], x.device, stream)
         if workspace is None:
-            workspace = torch.empty((moe_ffn_int8_workspace_bytes(T, H, F, E, k),), dtype=torch.uint8, device=x.device)
+            workspace = _empty((moe_ffn_int8_workspace_bytes(T, H, F, E, k),), torch.uint8, x.device, stream)
         _check(lib.dymoe_moe_ffn_int8(self._h, _at(x, dev, None, (T, H)), _dtype_code(x), _at(idx, dev, torch.int32, (T, k)),
                                       _at(w, dev, torch.float32, (T, k)), _at(table, dev), T, H, F, E, k, _dtype_code(y),
                                       _at(y, dev, None, (T, H)), _at(workspace, dev, torch.uint8), workspace.numel(),

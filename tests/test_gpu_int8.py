@@ -635,6 +635,29 @@ def test_two_calls_at_once_on_two_streams(ctx):
         assert torch.equal(y, ref[0]) and torch.equal(z, ref[1])
 
 
+@pytest.mark.parametrize("handle", [False, True])
+def test_memory_of_a_call_belongs_to_its_stream(ctx, monkeypatch, handle):
+    """What a call on another stream allocates is not given to the current stream's work before the call has run."""
+    x = randn(3, 200, 512)
+    wt, _ = weight(ctx, 9, 300, 512)
+    dev, _ = make_experts(ctx, 9, 4, 512, 256)
+    table = B.make_int8_table(dev, DEV)
+    idx, gate = routing(9, 200, 4, 2)
+    want = ctx.matmul_int8(x, wt), ctx.moe_ffn_int8(x, idx, gate, table, 256)
+    taken, at = [], B._at
+    monkeypatch.setattr(B, "_at", lambda t, *a: (taken.append((t.data_ptr(), t.numel())) if t is not None and t.dtype is torch.uint8 and t is not table else None) or at(t, *a))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    stream = s.cuda_stream if handle else s
+    got = ctx.matmul_int8(x, wt, stream=stream), ctx.moe_ffn_int8(x, idx, gate, table, 256, stream=stream)
+    assert len(taken) == 2
+    for ptr, n in taken:
+        mine = [torch.empty(n, dtype=torch.uint8, device=DEV) for _ in range(4)]
+        assert all(t.data_ptr() != ptr for t in mine)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_scores_feed_the_importance_and_the_mixed_layer(ctx):
     """The router's outputs are what the precision steps take."""
     T, E, k = 3, 16, 4
