@@ -284,7 +284,7 @@ def _stream(stream):
 
 def _empty(shape, dtype, device, stream):
     """Memory that a call on `stream` allocates: of that stream, so that no other work gets it back before the call has run."""
-    if stream is None or _stream(stream) == _raw_stream(_current_device()):
+    if stream is None or device.type != "cuda" or _stream(stream) == _raw_stream(_current_device()):
         return torch.empty(shape, dtype=dtype, device=device)
     if not isinstance(stream, torch.cuda.Stream):
         handle = _stream(stream)
@@ -662,7 +662,15 @@ def make_int8_table(experts, device):
     """The device-resident dymoe_expert_i8[E] of experts that are three (codes, scale) pairs each, in the tile layout
     (Context.quantize_rows); an expert given as None has an empty entry.  The caller keeps the pairs alive."""
     arr = (ExpertI8 * len(experts))()
+    size = None
     for e, pairs in enumerate(experts):
+        if pairs is not None:
+            (c1, s1), (c3, s3), (c2, s2) = pairs
+            F, H = s1.numel(), s2.numel()
+            up, down = (_up(F, 32), _up(H, 128)), (_up(H, 32), _up(F, 128))
+            if s3.numel() != F or (size or (F, H)) != (F, H) or tuple(c1.shape) != up or tuple(c3.shape) != up or tuple(c2.shape) != down:
+                raise ValueError("expert %d: codes and scales of W1, W3 [F, H] and W2 [H, F] in the tile layout, of one size in a table" % e)
+            size = (F, H)
         for i, (codes, scale) in enumerate(pairs or ()):
             arr[e].q[i] = _ptr(codes, torch.int8)
             arr[e].s[i] = _ptr(scale, torch.float32)

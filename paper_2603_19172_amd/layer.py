@@ -207,7 +207,12 @@ class Int8Experts:
 
     def __init__(self, ctx, w, device):
         # w: list over experts of [W1 [F,H], W3 [F,H], W2 [H,F]] tensors on `device`
-        self.E = len(w)
+        sizes = {tuple(ex[0].shape) for ex in w if ex is not None}
+        if len(sizes) != 1:
+            raise ValueError("the experts of a layer have one size")
+        (self.F, self.H), self.E = sizes.pop(), len(w)
+        if any([tuple(m.shape) for m in ex] != [(self.F, self.H), (self.F, self.H), (self.H, self.F)] for ex in w if ex is not None):
+            raise ValueError("an expert is W1 [F, H], W3 [F, H], W2 [H, F]")
         self.pairs = [None if ex is None else [ctx.quantize_rows(m, layout=B.LAYOUT_TILE) for m in ex] for ex in w]
         self.table = B.make_int8_table(self.pairs, device)
 
@@ -230,6 +235,8 @@ class Int8MoELayer:
 
     def step(self, x, experts, router=None, logits=None, bias=None, stream=None):
         """router: (codes, scale) of the [E, H] router in the tile layout; or logits [T, E] that the caller has."""
+        if (experts.E, experts.H, experts.F) != (self.E, self.H, self.F):
+            raise ValueError("the layer is made for other experts")
         if logits is None:
             logits = self.ctx.matmul_int8(x, router, y=self.logits, workspace=self.ws_router, stream=stream)
         self.ctx.route_scored(logits, self.k, bias=bias, idx=self.idx, w=self.gate, scores=self.scores, stream=stream, **self.routing)

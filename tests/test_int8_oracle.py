@@ -8,6 +8,7 @@ import torch
 
 from oracle import int8_oracle as Q
 from paper_2603_19172_amd import binding as B
+from paper_2603_19172_amd.layer import Int8Experts, Int8MoELayer
 
 P = 0x10000  # a non-null, aligned dummy "pointer"; never dereferenced by validation
 
@@ -168,3 +169,33 @@ def test_binding_checks_shapes_and_types():
         call("moe_ffn_int8", f(4, 16), f(3, 2, dtype=torch.int32), f(4, 2), f(96, dtype=torch.uint8), 16)
     with pytest.raises(ValueError):                                             # everything in order, but not on the context's device
         call("matmul_int8", f(4, 100), w)
+
+
+def test_layer_class_refuses_experts_of_other_sizes():
+    class Ctx:
+        def quantize_rows(self, m, layout):
+            n, k = -(-m.shape[0] // 32) * 32, -(-m.shape[1] // 128) * 128
+            return torch.zeros((n, k), dtype=torch.int8), torch.zeros(m.shape[0])
+    ex = lambda H, F: [torch.zeros(F, H), torch.zeros(F, H), torch.zeros(H, F)]
+    good = Int8Experts(Ctx(), [ex(40, 24), None, ex(40, 24)], "cpu")
+    assert (good.E, good.H, good.F) == (3, 40, 24) and good.table.numel() == 3 * 48
+    for bad in ([ex(40, 24), ex(40, 25)], [None], [ex(40, 24)[:2] + [torch.zeros(24, 40)]], [ex(40, 24)[:2]]):
+        with pytest.raises(ValueError):
+            Int8Experts(Ctx(), bad, "cpu")
+    for sizes in ((3, 40, 32), (3, 41, 24), (4, 40, 24)):
+        E, H, F = sizes
+        layer = Int8MoELayer(Ctx(), 4, H, F, E, 2, device="cpu")
+        with pytest.raises(ValueError):
+            layer.step(torch.zeros(4, H), good, logits=torch.zeros(4, E))
+
+
+def test_table_refuses_matrices_that_do_not_fit_together():
+    pair = lambda n, k: (torch.zeros((-(-n // 32) * 32, -(-k // 128) * 128), dtype=torch.int8), torch.zeros(n))
+    ex = lambda H, F: [pair(F, H), pair(F, H), pair(H, F)]
+    assert B.make_int8_table([ex(200, 40), None, ex(200, 40)], "cpu").numel() == 3 * 48
+    for bad in ([ex(200, 40), ex(200, 41)], [[pair(40, 200), pair(41, 200), pair(200, 40)]], [[pair(40, 200), pair(40, 300), pair(200, 40)]],
+                [[pair(40, 200), pair(40, 200), pair(200, 140)]], [ex(200, 40)[:2]]):
+        with pytest.raises(ValueError):
+            B.make_int8_table(bad, "cpu")
+    with pytest.raises(TypeError):
+        B.make_int8_table([[(c.float(), s) for c, s in ex(200, 40)]], "cpu")
