@@ -448,6 +448,17 @@ def test_ffn_token_that_is_no_number_stays_alone(ctx, T):
     assert torch.isnan(y[T // 2]).all() and torch.equal(y[rest], clean[rest])
 
 
+@pytest.mark.parametrize("T,k", [(1, 64), (2, 32), (1, 65), (2, 33), (3, 20), (40, 16)])
+@pytest.mark.parametrize("same", [False, True])
+def test_ffn_many_slots_and_the_same_expert_in_several(ctx, T, k, same):
+    E, H, F = 70, 136, 72
+    dev, host = make_experts(ctx, 31, E, H, F)
+    g = torch.Generator().manual_seed(T + k)
+    idx = torch.randint(0, 3, (T, k), generator=g) if same else torch.rand((T, E), generator=g).argsort(1)[:, :k]
+    gate = torch.rand((T, k), generator=g).float().to(DEV) / k
+    check_ffn(ctx, randn(T * k, T, H), idx.to(torch.int32).to(DEV), gate, dev, host, F)
+
+
 def test_ffn_skewed_load(ctx):
     dev, host = make_experts(ctx, 15, 32, 128, 96)
     idx, gate = routing(1, 400, 32, 4, popular=1.5)
