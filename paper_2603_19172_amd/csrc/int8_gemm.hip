@@ -763,7 +763,8 @@ __device__ __forceinline__ void i8_finish(const I8Args& A, const int32_t* perm, 
             }
             const bool apart = lo < m * 0x1p-8f || m == __builtin_inff();
 #pragma unroll
-            for (int i = 0; i < 4; i++) sc[i] = apart ? A.sum_scale : m > 0.0f ? A.sum_scale * (sc[i] / m) : 0.0f * sc[i];      // (a scale that is NaN stays)
+            for (int i = 0; i < 4; i++)                                   // (a scale that is NaN stays)
+                sc[i] = apart ? A.sum_scale : m > 0.0f ? A.sum_scale * (sc[i] / m) : 0.0f * sc[i];
             if (left > 0 && (lane & 7) == 0 && lane < kOut)      // (every tile of an expert writes the same)
                 A.strip_scale[(long)expert * ((A.N + 31) / 32) + n / 32] = (apart ? -1.0f : m) / A.sum_scale;
         }
@@ -947,7 +948,10 @@ __device__ __forceinline__ void i8_wide_tile(const I8Args& A, const int32_t* per
     i8_finish<MODE, NTF, 1>(A, perm, acc, sa, sb, row0, rows, bx, expert, xs_base);
 }
 
-constexpr int kI8Run = 16;      // neighbouring units that an XCD takes at a time: the weights of a tile row stay in its L2
+// Neighbouring units that an XCD takes at a time.  Plain products with 4, 8, 16, 32 and 64: 2048 x 14336 x 4096 140, 140, 142, 146 and 146 us,
+// 2048 x 4096 x 14336 149, 145.5, 148, 147 and 150, 2048 x 1536 x 2048 21, 22, 23, 23 and 36; the experts (2 of 8 of 14336 x 4096, 2048 tokens)
+// 915, 897, 878, 894 and 955.
+constexpr int kI8Run = 16, kI8RunPlain = 8;
 
 // columns of a workgroup's block
 template <int MODE, int S>
@@ -962,8 +966,10 @@ struct I8Unit {
 
 // Workgroups go to the 8 XCDs, each with an L2 of its own, in turn.  A unit is a tile and a column block; units that read the same weights
 // (the tiles of a matrix or expert, for one column block) are neighbours, and an XCD takes runs of neighbours.
-__device__ __forceinline__ long i8_run() { return (long)((blockIdx.x >> 3) / kI8Run) * 8 + (blockIdx.x & 7); }
-__device__ __forceinline__ int i8_turn_in_run() { return (blockIdx.x >> 3) % kI8Run; }
+template <int RUN>
+__device__ __forceinline__ long i8_run() { return (long)((blockIdx.x >> 3) / RUN) * 8 + (blockIdx.x & 7); }
+template <int RUN>
+__device__ __forceinline__ int i8_turn_in_run() { return (blockIdx.x >> 3) % RUN; }
 
 // strip nt of a matrix; strips behind the last re-read it
 __device__ __forceinline__ void i8_strip(I8Src& to, const I8Args& A, const void* q, long nt)
@@ -976,7 +982,7 @@ template <int S>
 __device__ __forceinline__ bool i8_plain_unit(const I8Args& A, I8Unit<S>& u, int wave)
 {
     const int cols = kI8Cols<kI8Plain, S>, nblk = (A.N + cols - 1) / cols, tiles = (A.rows + kI8TileRows - 1) / kI8TileRows;
-    const long unit = i8_run() * kI8Run + i8_turn_in_run();
+    const long unit = i8_run<kI8RunPlain>() * kI8RunPlain + i8_turn_in_run<kI8RunPlain>();
     if (unit >= (long)tiles * nblk) return false;
     u.bx = (int)(unit / tiles);
     u.row0 = (int)(unit - (long)u.bx * tiles) * kI8TileRows;
@@ -1093,7 +1099,8 @@ __device__ __forceinline__ void i8_split_tile(const I8Args& A, const I8Unit<1>& 
 #pragma unroll
         for (int g = 0; g < 4; g++)
             lds_write16(area + (uint32_t)ln * kI8EpiRow<1> + (uint32_t)(kb * 16 + g * 32),
-                        make_uint4((uint32_t)acc[0][tf][4 * g], (uint32_t)acc[0][tf][4 * g + 1], (uint32_t)acc[0][tf][4 * g + 2], (uint32_t)acc[0][tf][4 * g + 3]));
+                        make_uint4((uint32_t)acc[0][tf][4 * g], (uint32_t)acc[0][tf][4 * g + 1], (uint32_t)acc[0][tf][4 * g + 2],
+                                   (uint32_t)acc[0][tf][4 * g + 3]));
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < 4 / G; j++) {
@@ -1101,7 +1108,8 @@ __device__ __forceinline__ void i8_split_tile(const I8Args& A, const I8Unit<1>& 
             uint32_t sum[4] = {0, 0, 0, 0};
 #pragma unroll
             for (int g = 0; g < G; g++) {
-                const uint4 p = lds_read16(xs_base + (uint32_t)(g * 4 + wave) * kI8EpiWave<1> + (uint32_t)rr * kI8EpiRow<1> + (uint32_t)(lane & 7) * 16u);
+                const uint32_t from = xs_base + (uint32_t)(g * 4 + wave) * kI8EpiWave<1> + (uint32_t)rr * kI8EpiRow<1>;
+                const uint4 p = lds_read16(from + (uint32_t)(lane & 7) * 16u);
                 sum[0] += p.x;
                 sum[1] += p.y;
                 sum[2] += p.z;
@@ -1153,11 +1161,11 @@ __global__ __launch_bounds__(256, 2) void i8_experts_kernel(const I8Args A)
     const int c2 = kI8Cols<MODE, 2>, c1 = kI8Cols<MODE, 1>;
     const long units2 = (long)tall * ((A.N + c2 - 1) / c2), units1 = (long)wide * ((A.N + c1 - 1) / c1);
     const long runs2 = (units2 + kI8Run - 1) / kI8Run, runs1 = (units1 + kI8Run - 1) / kI8Run, runs = runs1 + runs2;
-    const long run = i8_run();
+    const long run = i8_run<kI8Run>();
     if (run >= runs) return;
     const long before = run * runs2 / runs, upto = (run + 1) * runs2 / runs;      // runs of tall tiles before this one, and with it
     if (upto > before) {
-        const long unit = before * kI8Run + i8_turn_in_run();
+        const long unit = before * kI8Run + i8_turn_in_run<kI8Run>();
         if (unit >= units2) return;
         I8Unit<2> u;
         i8_expert_unit<MODE, 2, kI8TileRows>(A, pp, 0, unit, u);
@@ -1170,7 +1178,7 @@ __global__ __launch_bounds__(256, 2) void i8_experts_kernel(const I8Args A)
         }
 #undef DYMOE_I8_TILE
     } else {
-        const long unit = (run - before) * kI8Run + i8_turn_in_run();
+        const long unit = (run - before) * kI8Run + i8_turn_in_run<kI8Run>();
         if (unit >= units1) return;
         I8Unit<1> u;
         i8_expert_unit<MODE, 1, kI8TileWide>(A, pp, tall, unit, u);
@@ -1200,15 +1208,15 @@ int i8_init()
     bool ok = allow((const void*)i8_matmul_kernel<2, 2>, kI8Lds<2>) && allow((const void*)i8_experts_kernel<kI8Up>, kI8Lds<2>) &&
               allow((const void*)i8_experts_kernel<kI8Down>, kI8Lds<2>);
     ok = ok && allow((const void*)i8_split_kernel<2>, kI8SplitLds<2>) && allow((const void*)i8_split_kernel<4>, kI8SplitLds<4>);
-    ok = ok && allow((const void*)i8_thin_kernel<kI8Plain, true>, (int)kI8FuseBytes) && allow((const void*)i8_thin_kernel<kI8Up, true>, (int)kI8FuseBytes) &&
+    ok = ok && allow((const void*)i8_thin_kernel<kI8Up, true>, (int)kI8FuseBytes) &&
          allow((const void*)i8_thin_down_kernel, (int)kI8FuseBytes);
     return ok ? DYMOE_OK : DYMOE_EHIP;
 }
 
 // workgroups for `units` units and `kinds` kinds of them, whose last runs need not be whole
-static dim3 i8_grid(long units, int kinds)
+static dim3 i8_grid(long units, int kinds, int run)
 {
-    return dim3((unsigned)(((units + kI8Run - 1) / kI8Run + kinds - 1 + 7) / 8 * 8 * kI8Run));
+    return dim3((unsigned)(((units + run - 1) / run + kinds - 1 + 7) / 8 * 8 * run));
 }
 
 // ----------------------------------------------------------------------------
@@ -1282,7 +1290,8 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void i8_small_kernel(cons
         off[f] = (MODE == kI8Up ? (uint32_t)(pp.perm[row0 + r] / A.k) : (uint32_t)r) * (uint32_t)A.Kp + 64u * (uint32_t)kb;
         if (MODE == kI8Plain && A.tiled) off[f] = (uint32_t)min(f, (rows - 1) >> 5) * (uint32_t)strip + lane16;
     }
-    x.set(A.x + (MODE == kI8Up ? 0 : (long)row0 * A.Kp), (uint32_t)(MODE == kI8Up ? A.rows : MODE == kI8Plain && A.tiled ? (rows + 31) & ~31 : rows) * (uint32_t)A.Kp);
+    const int held = MODE == kI8Up ? A.rows : MODE == kI8Plain && A.tiled ? (rows + 31) & ~31 : rows;
+    x.set(A.x + (MODE == kI8Up ? 0 : (long)row0 * A.Kp), (uint32_t)held * (uint32_t)A.Kp);
 #pragma unroll
     for (int d = 0; d < D; d++)
         if (kt + d * NW < nkt) load_x(ring[d], kt + d * NW);
@@ -1345,11 +1354,17 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void i8_small_kernel(cons
 #pragma unroll
         for (int i = 0; i < 4; i++) {
             const int m = min(n + i, A.N - 1);
-            auto sum = [&](int at) { return s_red[0][at][4 * g + i][lane] + s_red[1][at][4 * g + i][lane] + s_red[2][at][4 * g + i][lane] + s_red[3][at][4 * g + i][lane]; };
+            auto sum = [&](int at) {
+                int all = 0;
+#pragma unroll
+                for (int w = 0; w < 4; w++) all += s_red[w][at][4 * g + i][lane];
+                return all;
+            };
             v[i] = i8_value(sum(f), xs, sa[m], MODE == kI8Plain && A.bias ? A.bias[m] : 0.0f);
             if (MODE == kI8Up) v[i] = silu_times(v[i], i8_value(sum(NTF + f), xs, sb[m], 0.0f));
         }
-        i8_store4(A.out, (long)(row0 + row) * A.ldo + n, MODE == kI8Plain ? A.out_dtype : DYMOE_OUT_F32, left >= 4 && (MODE != kI8Plain || A.aligned), left, v);
+        const bool whole = left >= 4 && (MODE != kI8Plain || A.aligned);
+        i8_store4(A.out, (long)(row0 + row) * A.ldo + n, MODE == kI8Plain ? A.out_dtype : DYMOE_OUT_F32, whole, left, v);
     }
 }
 
@@ -1490,11 +1505,11 @@ extern "C" int dymoe_matmul_int8(dymoe_ctx* ctx, const void* x, int x_dtype, con
         const long tiles = (T + kI8TileRows - 1L) / kI8TileRows;
         const long units2 = tiles * ((N + 255L) / 256), units1 = tiles * ((N + 127L) / 128);
         const long cu = ctx->num_cu;
-        const dim3 grid1 = i8_grid(units1, 1);
+        const dim3 grid1 = i8_grid(units1, 1, kI8RunPlain);
         if (units1 <= cu && L.Kp >= 1024) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_split_kernel<4>, grid1, dim3(1024), kI8SplitLds<4>, st, A);
         else if (units1 <= cu * 5 / 4) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_split_kernel<2>, grid1, dim3(512), kI8SplitLds<2>, st, A);
         else if (units2 < 2 * cu || L.Kp < 2048) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_matmul_kernel<1, 1>, grid1, dim3(256), kI8Lds<1>, st, A);
-        else dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_matmul_kernel<2, 2>, i8_grid(units2, 1), dim3(256), kI8Lds<2>, st, A);
+        else dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_matmul_kernel<2, 2>, i8_grid(units2, 1, kI8RunPlain), dim3(256), kI8Lds<2>, st, A);
     } else {
         const long strips = (N + 31L) / 32;
         if (T <= 32) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_small_kernel<kI8Plain, 1, 8, 4>, dim3((unsigned)strips), dim3(512), 0, st, A);
@@ -1595,8 +1610,8 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     A.N = F;
     A.k = k;
     A.rows = T;
-    const dim3 up_grid = i8_grid(tall * ((F + 127L) / 128) + wide * ((F + 63L) / 64), 2);
-    const dim3 down_grid = i8_grid(tall * ((H + 255L) / 256) + wide * ((H + 127L) / 128), 2);
+    const dim3 up_grid = i8_grid(tall * ((F + 127L) / 128) + wide * ((F + 63L) / 64), 2, kI8Run);
+    const dim3 down_grid = i8_grid(tall * ((H + 255L) / 256) + wide * ((H + 127L) / 128), 2, kI8Run);
     if (small) dymoe_launch(ctx, DYMOE_K_INT8_UP, i8_small_kernel<kI8Up, 1, 4, 1>, dim3((unsigned)up), dim3(256), 0, st, A);
     else dymoe_launch(ctx, DYMOE_K_INT8_UP, i8_experts_kernel<kI8Up>, up_grid, dim3(256), kI8Lds<2>, st, A);
     rc = quantize_rows(ctx, ws + L.h, DYMOE_OUT_F32, P, F, (long)L.Fp, 0, ws + L.hq, (float*)(ws + L.hs), st);

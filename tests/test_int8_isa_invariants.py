@@ -50,5 +50,11 @@ def test_no_kernel_spills():
         assert [k for k, n in kernels if int(n)] in ([], [k for k, _ in kernels if "quantize_rows_kernelILi1ELi16ELi16E" in k])
 
 
+def test_products_and_plan_use_no_scratch_memory():
+    text = "\n".join(_assembly("int8_gemm.hip"))
+    kernels = re.findall(r"\.name:\s+(_Z\S+)\s+\.private_segment_fixed_size:\s+(\d+)", text)
+    assert len(kernels) >= 20 and all(n == "0" for _, n in kernels)
+
+
 def test_a_wait_state_between_m0_and_the_load():
     m0_rule("int8_gemm.hip")
