@@ -567,14 +567,13 @@ typedef struct {
  * SwiGLU experts in 8-bit integer arithmetic, activations quantised on the way:
  *   y[t,:] = sum_{slot<k} w[t,slot] * W2_e q( silu(W1_e q(x_t)) * (W3_e q(x_t)) ),  e = idx[t,slot],
  * q() the quantiser of dymoe_quantize_rows applied to a whole row, the products those of dymoe_matmul_int8.  Sums of products
- * are exact; the SwiGLU intermediate is held in fp32, and so is the sum over the slots.  With bf16 outputs a call of more than 32
- * tokens and 8 E pairs rounds each pair's output to fp16 before that sum (2^-11 of itself, beside the 2^-8 of y's own rounding).
+ * are exact; the SwiGLU intermediate, each pair's output and the sum over the slots are held in fp32, rounded once to y's type.
  * x [T,H] bf16, fp16 or fp32; idx [T,k] int32; w [T,k] fp32; table [E] of dymoe_expert_i8 in device memory; y [T,H] in
  * out_dtype (every row is written).  A pair whose index lies outside [0,E) contributes nothing, nor does one whose
  * expert's entry holds a NULL (DYMOE_FLAG_FORMAT_MISSING, dymoe_device_flags).
  * workspace: dymoe_moe_ffn_int8_workspace_bytes(T,H,F,E,k) bytes (0 for invalid sizes), 256-byte aligned, scratch.
  * Limits: any H, F up to DYMOE_INT8_MAX_K, E <= DYMOE_MAX_EXPERTS; T k < 2^29, T times H rounded up to 128 < 2^32 and T times
- * H / 2048 rounded up < 2^23 (else DYMOE_ENOTSUP).  No atomics in sums: the same inputs give the same bits.
+ * H / 2048 rounded up < 2^23 (else DYMOE_ENOTSUP).  The same inputs give the same bits, whatever tokens they stand among.
  */
 size_t dymoe_moe_ffn_int8_workspace_bytes(int T, int H, int F, int E, int k);
 int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, const int32_t* idx, const float* w,

@@ -3,8 +3,6 @@
 //   y[t, n] = xs[t] ws[n] sum_k xq[t, k] wq[n, k]
 // The sums are whole numbers of 32 bits (127 * 127 * K < 2^31 up to K = 131072), so their order does not matter and every split of K gives
 // the same bits.
-#include <float.h>
-
 #include <type_traits>
 
 #include "int8_device.hpp"
@@ -16,9 +14,8 @@ int quantize_rows(dymoe_ctx* ctx, const void* x, int dtype, long rows, long K, l
 
 // A tile of an expert: all that a workgroup has to know before its first load of weights.
 struct __attribute__((aligned(16))) I8TileRec {
-    int32_t expert, first, pairs;     // the expert, its first position, its pairs
+    int32_t first, pairs;             // the expert's first position, its pairs
     int32_t tile0, tiles;             // its first tile, its tiles
-    int32_t unused[3];
     dymoe_expert_i8 mat;
 };
 
@@ -114,12 +111,11 @@ __device__ __forceinline__ void i8_make_plan(I8PlanLds& lds, const int32_t* __re
     auto record = [&](I8TileRec* to, int e, int first, int pairs, int tile0, int tiles) {
         uint4* const at = (uint4*)to;
         const uint2* const mat = (const uint2*)(table + e);
-        store_global(at, make_uint4((uint32_t)e, (uint32_t)first, (uint32_t)pairs, (uint32_t)tile0));
-        store_global(at + 1, make_uint4((uint32_t)tiles, 0u, 0u, 0u));
+        store_global(at, make_uint4((uint32_t)first, (uint32_t)pairs, (uint32_t)tile0, (uint32_t)tiles));
 #pragma unroll
         for (int i = 0; i < 3; i++) {
             const uint2 lo = load_global<uint2>(mat + 2 * i), hi = load_global<uint2>(mat + 2 * i + 1);
-            store_global(at + 2 + i, make_uint4(lo.x, lo.y, hi.x, hi.y));
+            store_global(at + 1 + i, make_uint4(lo.x, lo.y, hi.x, hi.y));
         }
     };
     lds.at[tid] = n > 0 ? n0 : -1;
@@ -233,8 +229,6 @@ struct I8Args {
     I8Mat w;                          // the plain product
     const float* bias;
     void* out;
-    float* strip_scale;               // down projection with 16-bit outputs: [E][strips of 32 outputs]; null: 32-bit ones
-    float sum_scale;                  // largest sum there can be -> 2^15
     long ldo, P;
     int rows, Kp, N, k, out_dtype, aligned, tiled;     // aligned: the plain product's rows start where four outputs may be stored at once
 };
@@ -661,7 +655,7 @@ __device__ __forceinline__ void i8_store4(void* out, long at, int dt, bool whole
 // round in an LDS area of its own, so that a row leaves in whole lines.
 template <int MODE, int NTF, int S>
 __device__ __forceinline__ void i8_finish(const I8Args& A, const int32_t* perm, const i32x16_t (&acc)[S][NTF], const float* sa, const float* sb,
-                                          int row0, int rows, int bx, int expert, uint32_t xs_base)
+                                          int row0, int rows, int bx, uint32_t xs_base)
 {
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int ln = lane & 31, kb = lane >> 5;
@@ -742,32 +736,6 @@ __device__ __forceinline__ void i8_finish(const I8Args& A, const int32_t* perm, 
             sc[i] = sa[min(n + i, A.N - 1)];
             if (MODE == kI8Plain && A.bias) add[i] = A.bias[min(n + i, A.N - 1)];
         }
-        const bool half = MODE == kI8Down && A.strip_scale;
-        if (half) {
-            // A pair's outputs in 16 bits: fp16 of sum * sum_scale * (channel's scale / the strip's largest), at most 2^15 and 2^-11 of itself
-            // off, an eighth of what the bf16 output of the call rounds; the rest of the factors goes to the sum over the slots.  fp16's
-            // least step, 2^-25 to either side, is F * 2^-26 / (channel's scale / the strip's largest) units of the whole-number
-            // sum: less than half a unit at F = 131072 while a strip's scales lie within 2^8 of each other.  Where they do not (or one is
-            // infinite) the ratio stays out of the 16 bits and the sum over the slots takes each channel's own scale; a negative
-            // scale of the strip says so.
-            float m = 0.0f, lo = __builtin_inff();
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                m = fmaxf(m, fabsf(sc[i]));
-                if (sc[i] != 0.0f) lo = fminf(lo, fabsf(sc[i]));          // (a channel of zeros has sums of zero; NaN is passed over)
-            }
-#pragma unroll
-            for (int o = 1; o < 8; o *= 2) {
-                m = fmaxf(m, __shfl_xor(m, o, kWave));
-                lo = fminf(lo, __shfl_xor(lo, o, kWave));
-            }
-            const bool apart = lo < m * 0x1p-8f || m == __builtin_inff();
-#pragma unroll
-            for (int i = 0; i < 4; i++)                                   // (a scale that is NaN stays)
-                sc[i] = apart ? A.sum_scale : m > 0.0f ? A.sum_scale * (sc[i] / m) : 0.0f * sc[i];
-            if (left > 0 && (lane & 7) == 0 && lane < kOut)      // (every tile of an expert writes the same)
-                A.strip_scale[(long)expert * ((A.N + 31) / 32) + n / 32] = (apart ? -1.0f : m) / A.sum_scale;
-        }
 #pragma unroll
         for (int tf = 0; tf < NTF; tf++) {
             put(tf);
@@ -779,12 +747,6 @@ __device__ __forceinline__ void i8_finish(const I8Args& A, const int32_t* perm, 
                 if (row >= rows || left <= 0) continue;
                 const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
                 float v[4];
-                if (half) {
-#pragma unroll
-                    for (int i = 0; i < 4; i++) v[i] = (float)(int)w4[i] * sc[i];
-                    store_global((uint16_t*)A.out + (long)(row0 + row) * A.ldo + n, make_uint2(pack_half2(v[0], v[1]), pack_half2(v[2], v[3])));
-                    continue;
-                }
                 const float xs = A.xs[row0 + row];
 #pragma unroll
                 for (int i = 0; i < 4; i++) v[i] = i8_value((int)w4[i], xs, sc[i], add[i]);
@@ -797,7 +759,7 @@ __device__ __forceinline__ void i8_finish(const I8Args& A, const int32_t* perm, 
 // qw: this wavefront's strips; sa, sb: the scales of the matrices
 template <int MODE, int NTF, int S, int KT>
 __device__ __forceinline__ void i8_tile(const I8Args& A, const int32_t* perm, const I8Src (&qw)[S], const float* sa, const float* sb,
-                                        int row0, int rows, int bx, int expert, uint32_t xs_base, uint32_t buf_bytes)
+                                        int row0, int rows, int bx, uint32_t xs_base, uint32_t buf_bytes)
 {
     constexpr int kLanes = 8 * KT;              // lanes (16-byte chunks) to a row of a step
     constexpr int kRowsWave = 64 / kLanes;      // rows that a wavefront's copy fills
@@ -850,7 +812,7 @@ __device__ __forceinline__ void i8_tile(const I8Args& A, const int32_t* perm, co
         }
     }
 
-    i8_finish<MODE, NTF, S>(A, perm, acc, sa, sb, row0, rows, bx, expert, xs_base);
+    i8_finish<MODE, NTF, S>(A, perm, acc, sa, sb, row0, rows, bx, xs_base);
 }
 
 // Tiles of up to 160 rows for calls that the weights' bytes bound (experts that meet a few dozen tokens to some hundred): one strip a
@@ -863,7 +825,7 @@ constexpr int kI8Deep = 4;
 
 template <int MODE, int NTF>
 __device__ __forceinline__ void i8_wide_tile(const I8Args& A, const int32_t* perm, const I8Src& qw, const float* sa, const float* sb, int row0,
-                                             int rows, int bx, int expert, uint32_t xs_base)
+                                             int rows, int bx, uint32_t xs_base)
 {
     constexpr uint32_t kBuf = 32u * NTF * 128u;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -945,7 +907,7 @@ __device__ __forceinline__ void i8_wide_tile(const I8Args& A, const int32_t* per
     if (k < nkt) step(k, std::integral_constant<int, 0>());
     if (k + 1 < nkt) step(k + 1, std::integral_constant<int, 1>());
     if (k + 2 < nkt) step(k + 2, std::integral_constant<int, 2>());
-    i8_finish<MODE, NTF, 1>(A, perm, acc, sa, sb, row0, rows, bx, expert, xs_base);
+    i8_finish<MODE, NTF, 1>(A, perm, acc, sa, sb, row0, rows, bx, xs_base);
 }
 
 // Neighbouring units that an XCD takes at a time.  Plain products with 4, 8, 16, 32 and 64: 2048 x 14336 x 4096 140, 140, 142, 146 and 146 us,
@@ -961,7 +923,7 @@ template <int S>
 struct I8Unit {
     I8Src qw[S];              // this wavefront's strips
     const float *sa, *sb;     // the matrices' scales
-    int row0, rows, bx, expert;
+    int row0, rows, bx;
 };
 
 // Workgroups go to the 8 XCDs, each with an L2 of its own, in turn.  A unit is a tile and a column block; units that read the same weights
@@ -1001,7 +963,6 @@ __device__ __forceinline__ void i8_expert_unit(const I8Args& A, const I8Plan& pp
     const int cols = kI8Cols<MODE, S>, nblk = (A.N + cols - 1) / cols;
     const I8TileRec t = pp.tiles[first + unit / nblk];
     const long local = unit - (long)(t.tile0 - first) * nblk;
-    u.expert = t.expert;
     u.bx = (int)(local / t.tiles);
     const int i = (int)(local - (long)u.bx * t.tiles) * ROWS;
     u.row0 = t.first + i;
@@ -1032,7 +993,7 @@ __global__ __launch_bounds__(256, S == 2 ? 2 : 4) void i8_matmul_kernel(const I8
     constexpr uint32_t kBuf = (uint32_t)kI8TileRows * 128 * KT;
     I8Unit<S> u;
     if (!i8_plain_unit<S>(A, u, __builtin_amdgcn_readfirstlane(threadIdx.x / kWave))) return;
-#define DYMOE_I8_TILE(NTF) i8_tile<kI8Plain, NTF, S, KT>(A, nullptr, u.qw, u.sa, u.sb, u.row0, u.rows, u.bx, 0, lds_base(xs_raw), kBuf)
+#define DYMOE_I8_TILE(NTF) i8_tile<kI8Plain, NTF, S, KT>(A, nullptr, u.qw, u.sa, u.sb, u.row0, u.rows, u.bx, lds_base(xs_raw), kBuf)
     // one instantiation per number of fragments of 32 rows: the accumulators then sit in fixed registers for the whole loop
     switch ((u.rows + 31) >> 5) {
     case 1: DYMOE_I8_TILE(1); break;
@@ -1169,7 +1130,7 @@ __global__ __launch_bounds__(256, 2) void i8_experts_kernel(const I8Args A)
         if (unit >= units2) return;
         I8Unit<2> u;
         i8_expert_unit<MODE, 2, kI8TileRows>(A, pp, 0, unit, u);
-#define DYMOE_I8_TILE(NTF) i8_tile<MODE, NTF, 2, 2>(A, pp.perm, u.qw, u.sa, u.sb, u.row0, u.rows, u.bx, u.expert, xs, (uint32_t)kI8TileRows * 256u)
+#define DYMOE_I8_TILE(NTF) i8_tile<MODE, NTF, 2, 2>(A, pp.perm, u.qw, u.sa, u.sb, u.row0, u.rows, u.bx, xs, (uint32_t)kI8TileRows * 256u)
         switch ((u.rows + 31) >> 5) {
         case 1: DYMOE_I8_TILE(1); break;
         case 2: DYMOE_I8_TILE(2); break;
@@ -1182,7 +1143,7 @@ __global__ __launch_bounds__(256, 2) void i8_experts_kernel(const I8Args A)
         if (unit >= units1) return;
         I8Unit<1> u;
         i8_expert_unit<MODE, 1, kI8TileWide>(A, pp, tall, unit, u);
-#define DYMOE_I8_TILE(NTF) i8_wide_tile<MODE, NTF>(A, pp.perm, u.qw[0], u.sa, u.sb, u.row0, u.rows, u.bx, u.expert, xs)
+#define DYMOE_I8_TILE(NTF) i8_wide_tile<MODE, NTF>(A, pp.perm, u.qw[0], u.sa, u.sb, u.row0, u.rows, u.bx, xs)
         switch ((u.rows + 31) >> 5) {
         case 1: DYMOE_I8_TILE(1); break;
         case 2: DYMOE_I8_TILE(2); break;
@@ -1198,7 +1159,7 @@ template <int KT>
 constexpr int kI8Lds = 2 * kI8TileRows * 128 * KT;
 static_assert(2 * kI8TileWide * 128 <= kI8Lds<2>, "the wide tiles' buffers fit in the tall ones'");
 static_assert(4 * kI8EpiWave<2> <= kI8Lds<2> && 4 * kI8EpiWave<1> <= kI8Lds<1>, "the epilogue areas fit in the buffers");
-static_assert(sizeof(I8TileRec) == 80 && offsetof(I8TileRec, mat) == 32, "as the plan writes it");
+static_assert(sizeof(I8TileRec) == 64 && offsetof(I8TileRec, mat) == 16, "as the plan writes it");
 static_assert(4 * kI8EpiWave<1> <= 2 * 32 * 128 * 4, "also in those of a wide tile");
 
 // per-device set-up, with the device current
@@ -1369,11 +1330,8 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void i8_small_kernel(cons
 }
 
 // y[t] = sum over the slots, in their order, of gate times the pair's output.  A workgroup takes 2048 outputs of a token.  Bound by the pairs'
-// bytes: 16384 pairs of 2048 outputs in 16 bits 14.1 us (4.8 TB/s).
-template <bool HALF>
-__global__ __launch_bounds__(256) void i8_combine_kernel(const char* __restrict__ part, long ldp, const float* __restrict__ hs,
-                                                         const float* __restrict__ strip_scale, const dymoe_expert_i8* __restrict__ table,
-                                                         const int32_t* __restrict__ idx, const int32_t* __restrict__ where,
+// bytes.
+__global__ __launch_bounds__(256) void i8_combine_kernel(const float* __restrict__ part, long ldp, const int32_t* __restrict__ where,
                                                          const float* __restrict__ gate, int H, int k, int out_dtype, int aligned,
                                                          void* __restrict__ y)
 {
@@ -1382,38 +1340,15 @@ __global__ __launch_bounds__(256) void i8_combine_kernel(const char* __restrict_
     const int h = (int)(blockIdx.x - t * blocks) * 2048 + threadIdx.x * 8;
     if (h >= H) return;
     float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    bool apart = false;             // a strip whose scales lie apart: the slots again, each channel with its own
 #pragma unroll 4
     for (int j = 0; j < k; j++) {
         const int at = where[t * k + j];
         if (at < 0) continue;
-        float g = gate[t * k + j];
-        if constexpr (HALF) {
-            const float ss = strip_scale[(long)idx[t * k + j] * ((H + 31) / 32) + h / 32];
-            apart |= ss < 0.0f;
-            g *= hs[at] * ss;
-            const half8_t v = __builtin_bit_cast(half8_t, load_global<uint4>(part + (at * ldp + h) * 2));
+        const float g = gate[t * k + j];
+        const float4 a = load_global<float4>(part + at * ldp + h), b = load_global<float4>(part + at * ldp + h + 4);
+        const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-            for (int i = 0; i < 8; i++) sum[i] = fmaf(g, (float)v[i], sum[i]);
-        } else {
-            const float4 a = load_global<float4>(part + (at * ldp + h) * 4), b = load_global<float4>(part + (at * ldp + h + 4) * 4);
-            const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-            for (int i = 0; i < 8; i++) sum[i] = fmaf(g, v[i], sum[i]);
-        }
-    }
-    if (HALF && apart) {
-#pragma unroll
-        for (int i = 0; i < 8; i++) sum[i] = 0.0f;
-        for (int j = 0; j < k; j++) {
-            const int at = where[t * k + j];
-            if (at < 0) continue;
-            const int e = idx[t * k + j];
-            const float ss = strip_scale[(long)e * ((H + 31) / 32) + h / 32], g = gate[t * k + j] * (hs[at] * fabsf(ss));
-            const half8_t v = __builtin_bit_cast(half8_t, load_global<uint4>(part + (at * ldp + h) * 2));
-#pragma unroll
-            for (int i = 0; i < 8; i++) sum[i] = fmaf(g * (ss < 0.0f ? table[e].s[2][min(h + i, H - 1)] : 1.0f), (float)v[i], sum[i]);
-        }
+        for (int i = 0; i < 8; i++) sum[i] = fmaf(g, v[i], sum[i]);
     }
     const float lo[4] = {sum[0], sum[1], sum[2], sum[3]}, hi[4] = {sum[4], sum[5], sum[6], sum[7]};
     i8_store4(y, t * H + h, out_dtype, aligned && h + 4 <= H, H - h, lo);
@@ -1622,16 +1557,11 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     A.ldo = (long)L.Hp;
     A.Kp = (int)L.Fp;
     A.N = H;
-    const bool half = !small && out_dtype == DYMOE_OUT_BF16;
-    A.strip_scale = half ? (float*)(ws + L.strips) : nullptr;
-    A.sum_scale = 32768.0f / (16129.0f * (float)F);
     if (small) dymoe_launch(ctx, DYMOE_K_INT8_DOWN, i8_small_kernel<kI8Down, 1, 4, 1>, dim3((unsigned)down), dim3(256), 0, st, A);
     else dymoe_launch(ctx, DYMOE_K_INT8_DOWN, i8_experts_kernel<kI8Down>, down_grid, dim3(256), kI8Lds<2>, st, A);
     const dim3 grid((unsigned)(T * ((H + 2047L) / 2048)));
-    auto combine = half ? i8_combine_kernel<true> : i8_combine_kernel<false>;
-    dymoe_launch(ctx, DYMOE_K_INT8_COMBINE, combine, grid, dim3(256), 0, st, ws + L.part, (long)L.Hp, (const float*)(ws + L.hs),
-                 (const float*)(ws + L.strips), table, idx, i8_plan(plan, P).where, w, H, k, out_dtype,
-                 H % 4 == 0 && dymoe_aligned(y, 4 * dtype_bytes(out_dtype)), y);
+    dymoe_launch(ctx, DYMOE_K_INT8_COMBINE, i8_combine_kernel, grid, dim3(256), 0, st, (const float*)(ws + L.part), (long)L.Hp,
+                 i8_plan(plan, P).where, w, H, k, out_dtype, H % 4 == 0 && dymoe_aligned(y, 4 * dtype_bytes(out_dtype)), y);
     DYMOE_HIP_LAUNCH_CHECK();
     return DYMOE_OK;
 }

@@ -16,8 +16,7 @@ struct I8FfnLayout {
     size_t xq, xs;     // [T, Hp] codes and [T] scales of the activations
     size_t h;          // [P, Fp] SwiGLU intermediate, by position (pairs sorted by expert)
     size_t hq, hs;     // [P, Fp] its codes, [P] their scales
-    size_t part;       // [P, Hp] outputs of the pairs, by position: fp32, or fp16 and
-    size_t strips;     // [E, strips of 32 outputs] their scales (negative: each channel has its own)
+    size_t part;       // [P, Hp] outputs of the pairs, by position
     size_t plan;       // int32, see I8Plan
     size_t total;
     int max_tiles;
@@ -38,8 +37,7 @@ static inline I8FfnLayout i8_ffn_layout(long T, long H, long F, long E, long k)
     L.hq = take(P * L.Fp);
     L.hs = take(P * 4);
     L.part = take(P * L.Hp * 4);
-    L.strips = take((size_t)E * ((size_t)H + 31) / 32 * 4 + (size_t)E * 4);
-    L.plan = take((8 + i8_round(2 * P, 4) + 20 * (size_t)L.max_tiles) * 4);        // (a tile's record: 80 bytes)
+    L.plan = take((8 + i8_round(2 * P, 4) + 16 * (size_t)L.max_tiles) * 4);        // (a tile's record: 64 bytes)
     L.total = at;
     return L;
 }
