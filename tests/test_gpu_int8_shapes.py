@@ -52,3 +52,59 @@ def test_ffn_channel_scales_at_the_large_end(ctx, T):  # noqa: F811
     host = [[Q.quantize_rows(G.f64(m)) for m in ex] for ex in mats]
     idx, gate = G.routing(T, T, E, k)
     G.check_ffn(ctx, G.randn(T, T, H, std=2.0 ** -40), idx, gate, dev, host, F)
+
+
+SILU_T = [(1, 1), (2, 1), (2, 2), (20, 1), (64, 2), (200, 1), (300, 2), (700, 2)]
+
+
+@pytest.mark.parametrize("T,E", SILU_T)
+def test_ffn_swiglu_is_of_32_bits(ctx, T, E):  # noqa: F811
+    """An expert of one feature shows its intermediate: its code is 127 or -127, its scale |h| / 127, and an output 127 |h| times powers
+    of two.  Here scales are powers of two too, so a = W1 x and u = W3 x are exact.  In steps of 2^-24 of what they round: exp 2 (1 ulp) and
+    its argument's correction 1, 1 + exp 1, the reciprocal 2, exp times it 1, the products with a and u 1 each, h / 127 and its product with
+    the sum 1 each: 11 at most, and products of those; 12 allowed."""
+    H, F = 128, 1
+    for trial in range(1 if T > 8 else 24):
+        c = (torch.arange(T) * 37 + 23 * trial) % 161 - 80
+        x = torch.zeros((T, H))
+        x[:, 0], x[:, 1] = 127, c.float()
+        dev = []
+        shift = [2.0 ** -(3 * e) for e in range(E)]                # expert e: a = c / 8^e
+        for e in range(E):
+            w1, w3, w2 = torch.zeros((F, H)), torch.zeros((F, H)), torch.full((H, F), 127 * 2.0 ** -3)
+            w1[0, 1], w1[0, 2] = shift[e], 127 * shift[e]           # (x's column 2 is zero: there for the scale)
+            w3[0, 0] = 127 * 2.0 ** -14                             # u = 127 * 127 * 2^-14
+            w2[1::2] *= -1
+            dev.append([ctx.quantize_rows(m.to(DEV), layout=B.LAYOUT_TILE) for m in (w1, w3, w2)])
+        idx = (torch.arange(T) % E).to(torch.int32)[:, None]
+        y = G.f64(ctx.moe_ffn_int8(x.to(torch.bfloat16).to(DEV), idx.to(DEV), torch.ones((T, 1), device=DEV), B.make_int8_table(dev, DEV), F,
+                                   out_dtype=B.OUT_F32))
+        a = c.double().numpy() * np.array(shift)[idx[:, 0].numpy()]
+        want = 127 * 2.0 ** -3 * (a / (1.0 + np.exp(-a)) * (127 * 127 * 2.0 ** -14))
+        want = want[:, None] * np.where(np.arange(H) % 2, -1.0, 1.0)
+        off = np.abs(y - want) / np.maximum(np.abs(want), 1e-300)
+        assert (np.abs(y - want) <= 12 * 2.0 ** -24 * np.abs(want)).all(), "%.1f steps" % (off.max() * 2 ** 24)
+
+
+@pytest.mark.parametrize("T", [1, 2, 20, 200, 400])
+def test_ffn_swiglu_beyond_the_exponentials_range(ctx, T):  # noqa: F811
+    """a from 128 up to 2.5e38, where a log2 e is no number of 32 bits, is a itself times u, and up to -128 it is 0."""
+    H, F = 128, 1
+    for up in (2.0, 2.0 ** 121):
+        c = ((torch.arange(T) * 7) % 31 + 64) * (1 - torch.arange(T) % 3 // 2 * 2)        # 64 .. 94, every third negative
+        x = torch.zeros((T, H))
+        x[:, 0], x[:, 1] = 127, c.float()
+        w1, w3 = torch.zeros((F, H)), torch.zeros((F, H))
+        w1[0, 1], w3[0, 0] = up, 127 * 2.0 ** -74
+        if up < 4:
+            w1[0, 2] = 127 * up                     # (x's column 2 is zero; where 127 up is no number, up itself has code 127)
+        w2 = torch.full((H, F), 127 * 2.0 ** -3)
+        dev = [[ctx.quantize_rows(m.to(DEV), layout=B.LAYOUT_TILE) for m in (w1, w3, w2)]]
+        scale = float(dev[0][0][1][0])
+        a = c.double().numpy() * (127.0 if up > 4 else 1.0) * scale
+        assert np.abs(a).max() >= (2.36e38 if up > 4 and T > 2 else 128)
+        y = G.f64(ctx.moe_ffn_int8(x.to(torch.bfloat16).to(DEV), torch.zeros((T, 1), dtype=torch.int32, device=DEV),
+                                   torch.ones((T, 1), device=DEV), B.make_int8_table(dev, DEV), F, out_dtype=B.OUT_F32))
+        want = np.where(a > 0, a, 0.0) * (127 * 127 * 2.0 ** -74) * 127 * 2.0 ** -3
+        # roundings: a (its sum and scale) 2, the two products of the SwiGLU 2, the reciprocal of 1 is 1, h / 127 and its product 2
+        assert (np.abs(y - want[:, None]) <= 8 * 2.0 ** -24 * np.abs(want)[:, None]).all()
