@@ -623,11 +623,14 @@ class Context:
         return y
 
     def moe_ffn_int8(self, x, idx, w, table, F, out_dtype=OUT_BF16, y=None, workspace=None, stream=None):
-        """x [T, H] bf16 / fp16 / fp32; idx, w [T, k]; table: make_int8_table's.  Returns y [T, H]."""
+        """x [T, H] bf16 / fp16 / fp32; idx, w [T, k]; table: make_int8_table's, or dymoe_expert_i8 entries of the caller's own, whose
+        matrices then have to be of sizes H and F.  Returns y [T, H]."""
         (T, H), k, dev = x.shape, idx.shape[1], self.device
-        E = table.numel() * table.element_size() // C.sizeof(ExpertI8)
-        if not table.is_contiguous():
-            raise ValueError("the table has to be contiguous")
+        E, rest = divmod(table.numel() * table.element_size(), C.sizeof(ExpertI8))
+        if rest or not E or not table.is_contiguous():
+            raise ValueError("the table has to be contiguous and of whole entries")
+        if getattr(table, "sizes", (H, F)) != (H, F):
+            raise ValueError("x and F say H = %d, F = %d; the table's experts are of H = %d, F = %d" % (H, F, *table.sizes))
         if y is None:
             y = _empty((T, H), _TORCH_OUT[out_dtype], x.device, stream)
         if workspace is None:
@@ -674,7 +677,10 @@ def make_int8_table(experts, device):
         for i, (codes, scale) in enumerate(pairs or ()):
             arr[e].q[i] = _ptr(codes, torch.int8)
             arr[e].s[i] = _ptr(scale, torch.float32)
-    return torch.frombuffer(bytearray(bytes(arr)), dtype=torch.uint8).to(device)
+    table = torch.frombuffer(bytearray(bytes(arr)), dtype=torch.uint8).to(device)
+    if size is not None:
+        table.sizes = (size[1], size[0])        # H, F: what the calls check theirs against
+    return table
 
 
 def make_expert_table(experts, device):
