@@ -663,9 +663,9 @@ class Context:
 
 def make_int8_table(experts, device):
     """The device-resident dymoe_expert_i8[E] of experts that are three (codes, scale) pairs each, in the tile layout
-    (Context.quantize_rows); an expert given as None has an empty entry.  The caller keeps the pairs alive."""
+    (Context.quantize_rows), on that device; an expert given as None has an empty entry.  The caller keeps the pairs alive."""
     arr = (ExpertI8 * len(experts))()
-    size = None
+    size, device = None, torch.empty(0, device=device).device           # ("cuda" has an index then)
     for e, pairs in enumerate(experts):
         if pairs is not None:
             (c1, s1), (c3, s3), (c2, s2) = pairs
@@ -675,6 +675,10 @@ def make_int8_table(experts, device):
                 raise ValueError("expert %d: codes and scales of W1, W3 [F, H] and W2 [H, F] in the tile layout, of one size in a table" % e)
             size = (F, H)
         for i, (codes, scale) in enumerate(pairs or ()):
+            if codes.device != device or scale.device != device:
+                raise ValueError("expert %d: codes on %s and scales on %s, the table's device is %s" % (e, codes.device, scale.device, device))
+            if codes.data_ptr() % 16:
+                raise ValueError("expert %d: codes have to be 16-byte aligned" % e)
             arr[e].q[i] = _ptr(codes, torch.int8)
             arr[e].s[i] = _ptr(scale, torch.float32)
     table = torch.frombuffer(bytearray(bytes(arr)), dtype=torch.uint8).to(device)

@@ -33,3 +33,20 @@ def test_experts_of_other_sizes_than_the_tables_are_refused():
     for bad in (torch.zeros(100, dtype=torch.uint8), torch.zeros(0, dtype=torch.uint8)):
         with pytest.raises(ValueError, match="whole entries"):
             ffn(200, 40, bad)
+
+
+def test_tables_refuse_pointers_that_a_kernel_could_not_follow():
+    other = expert(200, 40, "meta")
+    for bad in ([other], [expert(200, 40), other], [expert(200, 40)[:2] + other[2:]], [[(c, s.to("meta")) for c, s in expert(200, 40)]]):
+        with pytest.raises(ValueError, match="device"):
+            B.make_int8_table(bad, "cpu")
+    for i in range(3):
+        ex = expert(200, 40)
+        codes, scale = ex[i]
+        flat = torch.zeros(codes.numel() + 16, dtype=torch.int8)
+        for off in (1, 8):
+            ex[i] = (flat[off:off + codes.numel()].view(codes.shape), scale)
+            with pytest.raises(ValueError, match="16-byte"):
+                B.make_int8_table([ex], "cpu")
+        ex[i] = (flat[16:].view(codes.shape), scale)
+        assert B.make_int8_table([ex], "cpu").numel() == 48
