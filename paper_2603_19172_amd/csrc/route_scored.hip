@@ -301,14 +301,19 @@ extern "C" int dymoe_route_scored(dymoe_ctx* ctx, const void* logits, int dtype,
     if (T > 0) DYMOE_REQUIRE(logits && idx && w);
     DYMOE_REQUIRE(dymoe_aligned(logits, dymoe::dtype_bytes(dtype)) && dymoe_aligned(idx, 4) && dymoe_aligned(w, 4));
     DYMOE_REQUIRE(dymoe_aligned(bias, 4) && dymoe_aligned(scores, 4));
-    if (E > DYMOE_MAX_EXPERTS || k > 64 || groups > 64 || T >= 1 << 26) return DYMOE_ENOTSUP;      // (64 threads a token, 2^32 a grid)
+    if (E > DYMOE_MAX_EXPERTS || k > 64 || groups > 64 || T >= 1 << 26) return DYMOE_ENOTSUP;
     if (!ctx) return DYMOE_ENOCTX;
     if (T == 0) return DYMOE_OK;
     auto launch = dymoe::route_scored_launch<DYMOE_OUT_BF16>;
     if (dtype == DYMOE_OUT_F32) launch = dymoe::route_scored_launch<DYMOE_OUT_F32>;
     else if (dtype == DYMOE_OUT_F16) launch = dymoe::route_scored_launch<DYMOE_OUT_F16>;
-    launch(ctx, logits, bias, T, E, k, score == DYMOE_SCORE_SIGMOID, groups, top_groups, group_best, renorm, factor, idx, w, scores,
-           (hipStream_t)stream);
+    // tokens of a launch at most: 64 threads a token, and a grid has to stay below 2^32 of them
+    constexpr int kTokens = 1 << 25;
+    for (int t = 0; t < T; t += kTokens) {
+        const int n = T - t < kTokens ? T - t : kTokens;
+        launch(ctx, (const char*)logits + (size_t)t * E * dymoe::dtype_bytes(dtype), bias, n, E, k, score == DYMOE_SCORE_SIGMOID, groups, top_groups,
+               group_best, renorm, factor, idx + (size_t)t * k, w + (size_t)t * k, scores ? scores + (size_t)t * E : nullptr, (hipStream_t)stream);
+    }
     DYMOE_HIP_LAUNCH_CHECK();
     return DYMOE_OK;
 }

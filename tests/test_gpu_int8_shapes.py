@@ -108,3 +108,19 @@ def test_ffn_swiglu_beyond_the_exponentials_range(ctx, T):  # noqa: F811
         want = np.where(a > 0, a, 0.0) * (127 * 127 * 2.0 ** -74) * 127 * 2.0 ** -3
         # roundings: a (its sum and scale) 2, the two products of the SwiGLU 2, the reciprocal of 1 is 1, h / 127 and its product 2
         assert (np.abs(y - want[:, None]) <= 8 * 2.0 ** -24 * np.abs(want)[:, None]).all()
+
+
+@pytest.mark.parametrize("T", [(1 << 25) - 1, (1 << 25) + 5, (1 << 26) - 1])
+def test_route_tokens_up_to_the_limit(ctx, T):  # noqa: F811
+    """As many tokens as the call takes, a launch's and more than one's: each is written, and as it is among few."""
+    E = 2
+    logits = torch.empty((T, E), dtype=torch.bfloat16, device=DEV)
+    logits[:, 0], logits[:, 1] = 0.0, 1.0
+    logits[::3, 0] = 2.0
+    scores = torch.full((T, E), 7.0, device=DEV)
+    idx, w = ctx.route_scored(logits, 1, renorm=False, scores=scores)
+    few = torch.zeros((6, E), device=DEV)
+    fi, fw = ctx.route_scored(logits[:6], 1, renorm=False, scores=few)
+    assert fi[:, 0].tolist() == [0, 1, 1, 0, 1, 1]
+    for r in range(6):
+        assert (idx[r::6] == fi[r]).all() and (w[r::6] == fw[r]).all() and (scores[r::6] == few[r]).all()
