@@ -6,7 +6,7 @@
 #include <type_traits>
 
 #include "int8_device.hpp"
-#include "int8_layout.hpp"
+#include "int8_rule.hpp"
 
 namespace dymoe {
 
@@ -282,23 +282,7 @@ __device__ __forceinline__ float silu_times(float a, float u)
 // Bound by the weights' bytes: one token on two experts of 14336 x 4096, up 38.7 us (6.0 TB/s) and down 24.1 us (4.9 TB/s); a matrix of
 // 128256 x 4096 and one token 83 us (6.3 TB/s).
 constexpr int kI8Ahead = 4;
-constexpr int kI8ThinRows = 16;
 constexpr int kI8ThinWaves = 8;
-// Up to 8 rows any matrix, up to 16 while the outputs are few (a workgroup reads its rows' codes for 16 weight rows only): 16 rows of 4096
-// values, N = 4096 8.8 us here and 10.0 in the shapes below, N = 14336 18.6 / 20.3, N = 32000 31 / 31.5, N = 64000 58.6 / 52.6.
-constexpr long kI8ThinOut = 3 << 18;
-// Tokens up to which the experts' workgroups quantise rows themselves: two launches instead of five, but every workgroup of the down
-// projection reads its token's intermediate, and an expert that two tokens share is read for each.  One token on 8 of 128 experts of 768 x 2048
-// 18.1 us and 25.1 in five launches, two 26.3 / 30.3, three 38.9 / 36.7, four 42.4 / 39.8; 2 of 8 experts of 14336 x 4096: 66 / 75,
-// 113 / 114, 163 / 140, 188 / 155.
-constexpr int kI8FuseRows = 2;
-constexpr long kI8FuseBytes = 64 * 1024;        // the codes' bytes in LDS at most
-// The plain product's workgroups quantise where that is less than a launch of its own: T * K values for a workgroup, and all
-// workgroups' together.  With T = 8, N = 1536, K = 2048 5.1 us and 5.9 with the launch, T = 16 6.9 / 6.3; T = 1 on 4096 x 14336 13.5 / 16.7, T = 4
-// 21.8 / 17.1; T = 2 on 4096 x 4096 6.8 / 7.8, T = 4 8.2 / 7.9; T = 2 on 14336 x 4096 14.8 / 14.2.
-constexpr long kI8FuseRow = 16 << 10;
-constexpr long kI8FuseReads = 4 << 20;
-
 __device__ __forceinline__ i32x4_t mfma16_i8(const uint4 a, const uint4 b, const i32x4_t c)
 {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4_t, a), __builtin_bit_cast(i32x4_t, b), c, 0, 0, 0);
@@ -1392,16 +1376,13 @@ extern "C" int dymoe_matmul_int8(dymoe_ctx* ctx, const void* x, int x_dtype, con
     if (T > (1 << 24) || N > (1 << 24)) return DYMOE_ENOTSUP;
     const I8MatLayout L = i8_mat_layout(T, K);
     if (!coded && T > 0 && workspace_bytes < L.total) return DYMOE_ENOSPC;
-    if (((T + 63L) / 64) * ((N + 31L) / 32) > 0x7fff0000L) return DYMOE_ENOTSUP;
+    if (i8_strip_units(T, N) > 0x7fff0000L) return DYMOE_ENOTSUP;
     if (!ctx) return DYMOE_ENOCTX;
     if (T == 0) return DYMOE_OK;
     hipStream_t st = (hipStream_t)stream;
     char* const ws = (char*)workspace;
-    const bool thin = T <= kI8ThinRows && (T <= 8 || (long)T * N <= kI8ThinOut);
-    // (strips of 32 columns: up to 1.25 of them a compute unit, beyond which they come in two rounds; T = 128, N = K = 4096: 13.9 us and 21.8 in
-    // tiles of 128 x 128 with K split; T = 100, N = 14336, K = 4096: 39 and 22)
-    const bool small = !thin && ((T + 63L) / 64) * ((N + 31L) / 32) <= ctx->num_cu * 5L / 4;
-    const bool fuse = thin && !coded && (long)T * K <= kI8FuseRow && (N + 15L) / 16 * T * K < kI8FuseReads;
+    const I8MatChoice c = i8_mat_choice(T, N, K, coded, ctx->num_cu);
+    const bool small = c.shape == I8MatShape::kSmall32 || c.shape == I8MatShape::kSmall64, fuse = c.fuse;
     I8Args A = {};
     A.x = (const char*)x;
     A.xs = x_scale;
@@ -1421,7 +1402,7 @@ extern "C" int dymoe_matmul_int8(dymoe_ctx* ctx, const void* x, int x_dtype, con
     A.Kp = (int)L.Kp;
     A.N = N;
     A.out_dtype = out_dtype;
-    if (thin) {
+    if (c.shape == I8MatShape::kThin) {
         I8ThinArgs B = {};
         B.x = A.x;
         B.xs = A.xs;
@@ -1443,22 +1424,26 @@ extern "C" int dymoe_matmul_int8(dymoe_ctx* ctx, const void* x, int x_dtype, con
         return DYMOE_OK;
     }
     A.aligned = dymoe_aligned(y, 4 * dtype_bytes(out_dtype)) && ldy % 4 == 0;
-    if (!small) {
-        // (K split in four up to a tile a compute unit: 256 x 4096 x 4096 22 us, unsplit 26.8, as 32-column strips 24.7.  In two a little beyond.
-        // Two strips a wavefront from two workgroups a compute unit on, where K is long enough for their longer start: 8192 x 8192 x 8192
-        // 492 us, one strip 551; 4096 x 9000 x 700 67 and 57.)
-        const long tiles = (T + kI8TileRows - 1L) / kI8TileRows;
-        const long units2 = tiles * ((N + 255L) / 256), units1 = tiles * ((N + 127L) / 128);
-        const long cu = ctx->num_cu;
-        const dim3 grid1 = i8_grid(units1, 1, kI8RunPlain);
-        if (units1 <= cu && L.Kp >= 1024) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_split_kernel<4>, grid1, dim3(1024), kI8SplitLds<4>, st, A);
-        else if (units1 <= cu * 5 / 4) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_split_kernel<2>, grid1, dim3(512), kI8SplitLds<2>, st, A);
-        else if (units2 < 2 * cu || L.Kp < 2048) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_matmul_kernel<1, 1>, grid1, dim3(256), kI8Lds<1>, st, A);
-        else dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_matmul_kernel<2, 2>, i8_grid(units2, 1, kI8RunPlain), dim3(256), kI8Lds<2>, st, A);
-    } else {
-        const long strips = (N + 31L) / 32;
-        if (T <= 32) dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_small_kernel<kI8Plain, 1, 8, 4>, dim3((unsigned)strips), dim3(512), 0, st, A);
-        else dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_small_kernel<kI8Plain, 2, 8, 3>, dim3((unsigned)((T + 63L) / 64 * strips)), dim3(512), 0, st, A);
+    const long tiles = (T + kI8TileRows - 1L) / kI8TileRows, strips = (N + 31L) / 32;
+    const dim3 grid1 = i8_grid(tiles * ((N + 127L) / 128), 1, kI8RunPlain);
+    switch (c.shape) {
+    case I8MatShape::kSmall32:
+        dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_small_kernel<kI8Plain, 1, 8, 4>, dim3((unsigned)strips), dim3(512), 0, st, A);
+        break;
+    case I8MatShape::kSmall64:
+        dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_small_kernel<kI8Plain, 2, 8, 3>, dim3((unsigned)i8_strip_units(T, N)), dim3(512), 0, st, A);
+        break;
+    case I8MatShape::kSplit4:
+        dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_split_kernel<4>, grid1, dim3(1024), kI8SplitLds<4>, st, A);
+        break;
+    case I8MatShape::kSplit2:
+        dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_split_kernel<2>, grid1, dim3(512), kI8SplitLds<2>, st, A);
+        break;
+    case I8MatShape::kOne:
+        dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_matmul_kernel<1, 1>, grid1, dim3(256), kI8Lds<1>, st, A);
+        break;
+    default:
+        dymoe_launch(ctx, DYMOE_K_MATMUL_INT8, i8_matmul_kernel<2, 2>, i8_grid(tiles * ((N + 255L) / 256), 1, kI8RunPlain), dim3(256), kI8Lds<2>, st, A);
     }
     DYMOE_HIP_LAUNCH_CHECK();
     return DYMOE_OK;
@@ -1492,7 +1477,8 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     hipStream_t st = (hipStream_t)stream;
     char* const ws = (char*)workspace;
     const long P = (long)T * k;
-    if (T <= kI8FuseRows && k <= 64 && P <= 64 && T * (long)(L.Hp + 16) <= kI8FuseBytes && k * (long)(L.Fp + 16) <= kI8FuseBytes) {
+    const I8FfnShape shape = i8_ffn_choice(T, H, F, E, k);
+    if (shape == I8FfnShape::kThin) {
         I8ThinArgs B = {};
         B.x = (const char*)x;
         B.idx = idx;
@@ -1525,11 +1511,7 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
         DYMOE_HIP_LAUNCH_CHECK();
         return DYMOE_OK;
     }
-    // Tiles of 32 rows and a sum in LDS while an expert meets 20 pairs or fewer on average (or never more than 32): 64 tokens, 2 of 8 experts of
-    // 14336 x 4096 (16 pairs an expert) 239 us and 267 in wide tiles, 80 tokens (20) 255 / 269, 96 (24) 274 / 273, 128 (32) 386 / 281; 8 of 128 experts
-    // of 768 x 2048, 256 tokens (16) 128 / 143, 320 (20) 135.5 / 146.4, 384 (24) 146.2 / 149.4, 512 (32) 192 / 157; 32 tokens on all of 8 such experts
-    // 25.8 / 34.3.
-    const bool small = T <= 32 || P <= 20L * E;
+    const bool small = shape == I8FfnShape::kSmall;
     // Workgroups at most: an expert of n pairs has n / 128 + 1 tall tiles at half as many column blocks, or one wide tile.
     const long tall = P / kI8TileRows + P / (kI8TileWide + 1), wide = E < P ? E : P;
     int32_t* const plan = (int32_t*)(ws + L.plan);

@@ -124,3 +124,43 @@ def test_route_tokens_up_to_the_limit(ctx, T):  # noqa: F811
     assert fi[:, 0].tolist() == [0, 1, 1, 0, 1, 1]
     for r in range(6):
         assert (idx[r::6] == fi[r]).all() and (w[r::6] == fw[r]).all() and (scores[r::6] == few[r]).all()
+
+
+# (shape of csrc/int8_rule.hpp, tokens, outputs, columns): tiles of 128 columns odd and even in number, one more than a multiple of four for K split in
+# four, fewer than its groups need; last tiles of rows of one, two and three fragments; the steady state of every loop
+PRODUCTS = [("two", 2081, 8003, 2100), ("two", 2068, 8003, 2300), ("two", 2118, 8192, 2048), ("one", 1500, 4100, 2100), ("one", 2433, 9001, 700),
+            ("split2", 1100, 3000, 700), ("split2", 1064, 4200, 2100), ("split4", 130, 4100, 2100), ("split4", 600, 3000, 1030),
+            ("small64", 127, 4099, 2100), ("small32", 29, 8003, 2300), ("thin", 16, 4099, 2100), ("thin", 5, 8003, 14336)]
+
+
+def big(seed, *shape, std=1.0, dtype=torch.bfloat16):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    return (torch.randn(shape, generator=g, device=DEV) * std).to(dtype)
+
+
+def codes64(x):
+    """The oracle's codes and scales of the rows of x, as tensors of 64 bits on the GPU."""
+    c, s = Q.quantize_rows(G.f64(x))
+    return torch.from_numpy(c.astype(np.float64)).to(DEV), torch.from_numpy(s.astype(np.float64)).to(DEV)
+
+
+@pytest.mark.parametrize("shape,T,N,K", PRODUCTS)
+def test_matmul_shapes_match_the_oracle(ctx, shape, T, N, K):  # noqa: F811
+    """Every output of every shape, in each type, with a bias and without, rows of the output aligned for wide stores and not."""
+    w, x = big(T, N, K, std=0.05), big(N, T, K)
+    wt = ctx.quantize_rows(w, layout=B.LAYOUT_TILE)
+    (wq, ws), (xq, xs) = codes64(w), codes64(x)
+    prod = (xq @ wq.T) * xs[:, None] * ws[None, :]
+    bias = big(3, N, dtype=torch.float32)
+    xc, xsc = ctx.quantize_rows(x)
+    for out in (torch.bfloat16, torch.float32, torch.float16):
+        for b, gap in ((None, -N % 4), (bias, -N % 4 + 2)):
+            y = torch.full((T + 1, N + gap), 77.0, dtype=out, device=DEV)
+            ctx.matmul_int8(x, wt, bias=b, y=y[:T, :N])
+            ref = prod if b is None else prod + b.double()
+            tol = 4 * 2.0 ** -24 * prod.abs() + (G.HALF[out] + 2 * 2.0 ** -24) * ref.abs() + (2.0 ** -25 if out == torch.float16 else 0.0)
+            assert ((y[:T, :N].double() - ref).abs() <= tol).all()
+            assert (y[T] == 77).all() and (y[:, N:] == 77).all()
+            z = torch.full((T + 1, N + gap), 77.0, dtype=out, device=DEV)
+            ctx.matmul_int8(xc, wt, x_scale=xsc, bias=b, y=z[:T, :N])
+            assert torch.equal(y, z)
