@@ -164,3 +164,63 @@ def test_matmul_shapes_match_the_oracle(ctx, shape, T, N, K):  # noqa: F811
             z = torch.full((T + 1, N + gap), 77.0, dtype=out, device=DEV)
             ctx.matmul_int8(xc, wt, x_scale=xsc, bias=b, y=z[:T, :N])
             assert torch.equal(y, z)
+
+
+# pairs of each expert: tall tiles from 161 on, wide ones up to 160, their last tiles of every number of fragments
+LOADS = [276, 336, 161, 160, 129, 100, 70, 40, 20]
+EXPERTS = [(700, 1100, 2200), (700, 2048, 1000), (700, 2100, 1920), (700, 1664, 2432)]          # tokens, H, F
+LONG_ROWS = [(100, 16500, 40), (100, 40, 16500), (700, 16500, 264)]
+
+
+def ffn_reference(x, idx, gate, host, eps):
+    """int8_oracle.moe_ffn's y and bound for every expert's pairs at once, in 64 bits on the GPU; and the sum over the slots of what
+    their outputs are in size.  host: an expert's three (codes, scales) of 64 bits."""
+    T, H = x.shape
+    xq, xs = codes64(x)
+    y, var, drift, most, size = (torch.zeros((T, H), dtype=torch.float64, device=DEV) for _ in range(5))
+    widest = 0.0
+    for e, ((q1, s1), (q3, s3), (q2, s2)) in enumerate(host):
+        t, j = (idx == e).nonzero(as_tuple=True)
+        a, u = ((xq[t] @ q.T) * xs[t][:, None] * s for q, s in ((q1, s1), (q3, s3)))
+        widest = max(widest, float(a.abs().max()))
+        h = a / (1.0 + torch.exp(-a)) * u
+        step = h.abs().amax(1, keepdim=True) / 127.0
+        g, w2 = gate[t, j].double()[:, None], q2 * s2[:, None]
+        o = (torch.round(h / step) * step) @ w2.T
+        for i in range(idx.shape[1]):                            # (a token at most once for each slot: no two writers of a row)
+            m = j == i
+            r = t[m]
+            y[r] += (g * o)[m]
+            size[r] += (g.abs() * o.abs())[m]
+            drift[r] += (g.abs() * o.abs() * eps)[m]
+            var[r] += (g * g * ((2.0 * eps * h.abs() * step) @ (w2 ** 2).T))[m]
+            most[r] = torch.maximum(most[r], (g.abs() * step * w2.abs().amax(1))[m])
+    assert widest <= 16.0
+    rare = float(np.log(2.0 / 2e-9))
+    return y, most * rare / 3.0 + torch.sqrt((most * rare / 3.0) ** 2 + 2.0 * var * rare) + drift, size
+
+
+@pytest.mark.parametrize("T,H,F", EXPERTS + LONG_ROWS)
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32, torch.float16])
+def test_ffn_tiles_of_long_rows_match_the_oracle(ctx, T, H, F, out):  # noqa: F811
+    """Experts' tiles in their loops' steady state.  The intermediate's relative error with |a| <= 16, in steps of 2^-24: a's own three roundings
+    times 1 + |a|, 51; the sigmoid and its products 8.5; u's three: 63, so eps = 2^-18 in what test_gpu_int8 derives.  Beside it, of each
+    pair's output: the scale of its codes, the sum's conversion and its two products 4, a slot's multiply-add one for each slot, the
+    output's type."""
+    k = 2
+    loads = LOADS if T == 700 else [T, T // 2]
+    E = len(loads)
+    slots = torch.cat([torch.full((n,), e) for e, n in enumerate(loads)] + [torch.full((T * k - sum(loads),), -1)])
+    idx = slots[torch.randperm(T * k, generator=torch.Generator().manual_seed(H))].view(T, k).to(torch.int32).to(DEV)
+    gate = big(F, T, k, dtype=torch.float32).abs() + 0.1
+    mats = [[big(700 + 3 * e + i, *s, std=0.5 * s[1] ** -0.5) for i, s in enumerate(((F, H), (F, H), (H, F)))] for e in range(E)]
+    table = [[ctx.quantize_rows(m, layout=B.LAYOUT_TILE) for m in ex] for ex in mats]
+    x = big(H + F, T, H)
+    ref, bound, size = ffn_reference(x, idx, gate, [[codes64(m) for m in ex] for ex in mats], 2.0 ** -18)
+    y = torch.full((T + 1, H), 77.0, dtype=out, device=DEV)
+    ws = torch.full((B.moe_ffn_int8_workspace_bytes(T, H, F, E, k),), 0xFF, dtype=torch.uint8, device=DEV)
+    ctx.moe_ffn_int8(x, idx, gate, B.make_int8_table(table, DEV), F, y=y[:T], workspace=ws)
+    tol = bound + (k + 4) * 2.0 ** -24 * (size + bound) + G.HALF[out] * (ref.abs() + bound) + (2.0 ** -25 if out == torch.float16 else 0.0)
+    off = (y[:T].double() - ref).abs()
+    print("T=%d H=%d F=%d: worst %.2f of the bound" % (T, H, F, float((off / tol.clamp_min(1e-300)).max())), flush=True)
+    assert (off <= tol).all() and (y[T] == 77).all()

@@ -49,6 +49,12 @@ def test_the_gpu_tests_take_the_shapes_they_name(product, experts):
     for shape, T, N, K in G.PRODUCTS:
         assert product(T, N, K)[0] == product(T, N, K, coded=1)[0] == shape
     assert {p[0] for p in G.PRODUCTS} == set(MAT)
+    for T, H, F in G.EXPERTS + G.LONG_ROWS:
+        assert experts(T, H, F, len(G.LOADS) if T == 700 else 2, 2) == "grouped"
+    assert min(G.LOADS) <= 160 < max(G.LOADS) and sum(G.LOADS) <= 1400
+    # a last tile of each number of fragments, of tall tiles and of wide ones
+    assert {(n % 128 + 31) // 32 for n in G.LOADS if n > 160} >= {1, 2, 3}
+    assert {(n + 31) // 32 for n in G.LOADS if n <= 160} == {1, 2, 3, 4, 5}
     for T, E in G.SILU_T:
         assert experts(T, 128, 1, E, 1) == ("thin" if T <= 2 else "small" if T <= 20 * E or T <= 32 else "grouped")
 
