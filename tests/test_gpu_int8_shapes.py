@@ -7,6 +7,7 @@ import torch
 import test_gpu_int8 as G
 from oracle import int8_oracle as Q
 from paper_2603_19172_amd import binding as B
+from paper_2603_19172_amd.layer import Int8Experts, Int8MoELayer
 from gpu_helpers import DEV
 from test_gpu_int8 import ctx  # noqa: F401  (a fixture)
 
@@ -224,3 +225,19 @@ def test_ffn_tiles_of_long_rows_match_the_oracle(ctx, T, H, F, out):  # noqa: F8
     off = (y[:T].double() - ref).abs()
     print("T=%d H=%d F=%d: worst %.2f of the bound" % (T, H, F, float((off / tol.clamp_min(1e-300)).max())), flush=True)
     assert (off <= tol).all() and (y[T] == 77).all()
+
+
+@pytest.mark.parametrize("T", [1, 33, 260])
+def test_layer_flags_an_absent_expert_where_it_is_chosen(ctx, T):  # noqa: F811
+    H, F, E, k = 192, 256, 16, 4
+    mats = [[G.randn(800 + 3 * e + i, *s, std=0.05) for i, s in enumerate(((F, H), (F, H), (H, F)))] for e in range(E)]
+    mats[3] = None
+    experts = Int8Experts(ctx, mats, DEV)
+    layer = Int8MoELayer(ctx, T, H, F, E, k, groups=4, top_groups=2, group_best=2)
+    logits, x = G.randn(70, T, E, dtype=torch.float32), G.randn(T, T, H)
+    for push in (-5.0, 5.0, -5.0):
+        bias = torch.zeros(E, device=DEV).index_fill(0, torch.tensor([3], device=DEV), push)
+        ctx.device_flags()
+        layer.step(x, experts, logits=logits, bias=bias)
+        assert bool((layer.idx == 3).any()) == (push > 0)
+        assert ctx.device_flags() == (B.FLAG_FORMAT_MISSING if push > 0 else 0)
