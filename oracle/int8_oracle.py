@@ -74,8 +74,8 @@ def matmul(xq, xs, wq, ws):
 
 def moe_ffn(x, idx, gate, experts, eps_h):
     """experts: per expert None or three (codes, scale) pairs, row-major.  Returns y [T, H]; a bound on what a kernel may be off
-    where the intermediate carries a relative error of eps_h, that a chance of 2e-9 an output exceeds; its mean square; and what it
-    may be off beside that where the pairs' outputs are rounded to fp16.  tests/test_gpu_int8.py derives them."""
+    where the intermediate carries a relative error of eps_h, that a chance of 2e-9 an output exceeds; its mean square; and what a
+    kernel might be off beside that that rounded the pairs' outputs to fp16 (the library's does not).  tests/test_gpu_int8.py derives them."""
     T, H = x.shape
     xq, xs = quantize_rows(x)
     y, var, drift, half, most = (np.zeros((T, H)) for _ in range(5))

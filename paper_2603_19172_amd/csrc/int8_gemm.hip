@@ -46,7 +46,7 @@ __device__ __forceinline__ bool i8_present(const dymoe_expert_i8& x)
 // until the experts' first positions are known, so that there is one pass of atomics.  The turns come in any order, and nothing that is
 // computed depends on it.  The sorted pairs and the tiles' experts pass through LDS where they fit: written from the threads that
 // know them, 16384 pairs cost 7 us in stores of four bytes each, and an expert's sixteen records 3 us in one thread.  16384 pairs of 128
-// experts 13.6 us with 2048 rows' codes beside it, 488 pairs 4.9: latencies of one workgroup's passes, not bytes.
+// experts 12.1 us with 2048 rows' codes beside it, 488 pairs 4.6: latencies of one workgroup's passes, not bytes.
 constexpr int kI8PlanThreads = 1024;
 constexpr int kI8PlanKeep = 16;
 constexpr int kI8PlanPairs = kI8PlanKeep * kI8PlanThreads;
@@ -258,7 +258,8 @@ __device__ __forceinline__ i32x16_t mfma_i8(const uint4 a, const uint4 b, const 
     return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4_t, a), __builtin_bit_cast(i32x4_t, b), c, 0, 0, 0);
 }
 
-// An output of a product: two roundings and the addition's, in every shape alike, whatever the compiler would contract.
+// An output of a product: the sum's conversion, its product with the row's scale and the multiply-add round once each, in every shape alike,
+// whatever the compiler would contract.
 __device__ __forceinline__ float i8_value(int sum, float xs, float sc, float add) { return fmaf((float)sum * xs, sc, add); }
 
 // a u / (1 + e^-a).  The instruction for powers of two takes t = -a log2 e, a product that rounds by up to 2^-24 of itself; at |a| = 80 that
@@ -279,7 +280,7 @@ __device__ __forceinline__ float silu_times(float a, float u)
 // rows' quantisation, which every workgroup then does for itself where the rows are few, costs no launch and hides behind them.
 // v_mfma_i32_16x16x64_i8: lane l holds weight row l % 16 and row l % 16 of the codes, columns 64 (l / 32) + 32 j + 16 (l / 16 % 2) of a
 // tile in its j-th product (any order of columns will do that is the same on both sides).
-// Bound by the weights' bytes: one token on two experts of 14336 x 4096, up 38.7 us (6.0 TB/s) and down 24.1 us (4.9 TB/s); a matrix of
+// Bound by the weights' bytes: one token on two experts of 14336 x 4096, up 39.1 us (6.0 TB/s) and down 24.1 us (4.9 TB/s); a matrix of
 // 128256 x 4096 and one token 83 us (6.3 TB/s).
 constexpr int kI8Ahead = 4;
 constexpr int kI8ThinWaves = 8;
@@ -545,9 +546,9 @@ __global__ __launch_bounds__(64 * kI8LastWaves) void i8_thin_down_kernel(const I
 //  * Several workgroups on a compute unit, one's waits, prologue and epilogue covered by the others' products.
 // Two shapes: S = 2, KT = 2 (128 accumulator registers a lane, two workgroups a compute unit) reads half as much LDS for a product; S = 1,
 // KT = 1 (64, four workgroups) has more loads on their way and twice as many workgroups, for calls that the weights' bytes bound.
-// 2048 x 14336 x 4096: 131 us, 1.84 POP/s (with random codes; the same kernel takes 102 us on zeros, since the clock follows the power: products from
-// registers alone reach 4.4 POP/s on quiet data and 3.4 on random).  Without its copies of rows it takes 129 us, without its loads
-// of weights 113, with neither 104 to 108: the products and their LDS reads are what is left.
+// 2048 x 14336 x 4096: 126 us, 1.91 POP/s, with random codes.  On a card where it took 131: 102 us on zeros, since the clock follows the power
+// (products from registers alone reach 4.4 POP/s on quiet data and 3.4 on random), 129 without its copies of rows, 113 without its loads
+// of weights, 104 to 108 with neither: the products and their LDS reads are what is left.
 template <int S>
 constexpr uint32_t kI8EpiRow = S == 2 ? 272 : 144;     // epilogue: bytes of a row of 32 S sums in LDS, 16 of them padding
 template <int S>
@@ -813,8 +814,8 @@ __device__ __forceinline__ void i8_tile(const I8Args& A, const int32_t* perm, co
 // wavefront, four tiles of weights on their way in registers, the rows' codes through registers into two LDS buffers.  Bytes on
 // their way are what sets the rate of such a stream; with the rows copied to LDS directly, as above, the loads of weights could run
 // ahead by one step only, because a count of outstanding loads that lets the copies through has to wait for all loads before them.
-// Eight experts of 14336 x 4096, 64 to 160 pairs each: up 230 us (4.1 TB/s of weights), without its products 217, without its rows 208; with
-// non-temporal loads of the weights 238.
+// Eight experts of 14336 x 4096, 64 to 160 pairs each: up 218 us (4.3 TB/s of weights).  On a card where it took 230: 217 without its products, 208
+// without its rows, 238 with non-temporal loads of the weights.
 constexpr int kI8Deep = 4;
 
 template <int MODE, int NTF>
@@ -904,9 +905,9 @@ __device__ __forceinline__ void i8_wide_tile(const I8Args& A, const int32_t* per
     i8_finish<MODE, NTF, 1>(A, perm, acc, sa, sb, row0, rows, bx, xs_base);
 }
 
-// Neighbouring units that an XCD takes at a time.  Plain products with 4, 8, 16, 32 and 64: 2048 x 14336 x 4096 140, 140, 142, 146 and 146 us,
-// 2048 x 4096 x 14336 149, 145.5, 148, 147 and 150, 2048 x 1536 x 2048 21, 22, 23, 23 and 36; the experts (2 of 8 of 14336 x 4096, 2048 tokens)
-// 915, 897, 878, 894 and 955.
+// Neighbouring units that an XCD takes at a time.  Calls with 4, 8, 16, 32 and 64, one card: 2048 x 14336 x 4096 133, 133, 137, 138 and 139 us,
+// 2048 x 4096 x 14336 151, 145, 149, 148 and 150, 2048 x 1536 x 2048 18.1, 18.2, 19.6, 19.2 and 30.5; the experts (2 of 8 of 14336 x 4096,
+// 2048 tokens) 942, 930, 914, 916 and 976.
 constexpr int kI8Run = 16, kI8RunPlain = 8;
 
 // columns of a workgroup's block
@@ -1103,9 +1104,9 @@ __global__ __launch_bounds__(256 * G, 4) void i8_split_kernel(const I8Args A)
 
 // Experts.  One that more than kI8TileWide pairs go to takes tiles of 128 rows and two strips a wavefront; the others, whose weights' bytes
 // bound them, one wide tile.  Runs of the two kinds alternate in proportion, so that the chip multiplies while it reads.
-// The whole call with 160, 128 and 96 as the wide tiles' limit, and with tall tiles alone: 512 tokens, 2 of 8 experts of 14336 x 4096 353, 368, 388
-// and 387 us, 2048 tokens 851, 874, 855 and 886; 2048 tokens, 8 of 128 experts of 768 x 2048 228, 235, 234 and 248, 512 tokens 157, 159, 158 and 158.
-// Up and down: 228 and 120 us (512 tokens, large experts; 4.1 TB/s of weights), 127 and 85 (2048, small ones, loads skewed).
+// The whole call with 160, 128 and 96 as the wide tiles' limit, and with tall tiles alone: 512 tokens, 2 of 8 experts of 14336 x 4096 355, 375, 392
+// and 393 us, 2048 tokens 913, 915, 916 and 914; 2048 tokens, 8 of 128 experts of 768 x 2048, loads skewed, 253, 250, 249 and 244, 512 tokens 137, 139,
+// 136 and 132.  Up and down: 218 and 111 us (512 tokens, large experts; 4.3 TB/s of weights), 115 and 88 (2048, small ones, loads skewed).
 template <int MODE>
 __global__ __launch_bounds__(256, 2) void i8_experts_kernel(const I8Args A)
 {
@@ -1180,7 +1181,7 @@ static dim3 i8_grid(long units, int kinds, int run)
 // shared before the end: weights and codes come straight into registers, D tiles of a wavefront on their way, and the sums meet in LDS.
 // A load of codes that lie row by row touches a line for each of its 64 lanes; the plain product therefore has its rows quantised into
 // the weights' tile layout (A.tiled), where it is 1 KiB of contiguous memory.
-// 61 x 1536 x 2048: 5.8 us (10.8 in tiles of 128 x 128); 61 tokens, 8 of 128 experts of 768 x 2048: up 61 us (6.5 TB/s), down 31.8 (6.3 TB/s).
+// 61 x 1536 x 2048: 6.2 us (10.8 in tiles of 128 x 128); 61 tokens, 8 of 128 experts of 768 x 2048: up 61 us (6.5 TB/s), down 31 (6.4 TB/s).
 template <int MODE, int NTF, int NW, int D>
 __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void i8_small_kernel(const I8Args A)
 {
@@ -1324,7 +1325,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void i8_small_kernel(cons
 }
 
 // y[t] = sum over the slots, in their order, of gate times the pair's output.  A workgroup takes 2048 outputs of a token.  Bound by the pairs'
-// bytes.
+// bytes: 16384 pairs of 2048 outputs 24 us (5.9 TB/s).
 __global__ __launch_bounds__(256) void i8_combine_kernel(const float* __restrict__ part, long ldp, const int32_t* __restrict__ where,
                                                          const float* __restrict__ gate, int H, int k, int out_dtype, int aligned,
                                                          void* __restrict__ y)

@@ -66,9 +66,9 @@ static inline I8FfnShape i8_ffn_choice(long T, long H, long F, long E, long k)
     const long P = T * k, Hp = (long)i8_round((size_t)H, 128), Fp = (long)i8_round((size_t)F, 128);
     if (T <= kI8FuseRows && P <= 64 && T * (Hp + 16) <= kI8FuseBytes && k * (Fp + 16) <= kI8FuseBytes) return I8FfnShape::kThin;
     // Tiles of 32 rows and a sum in LDS while an expert meets 20 pairs or fewer on average (or never more than 32): 64 tokens, 2 of 8 experts of
-    // 14336 x 4096 (16 pairs an expert) 239 us and 267 in wide tiles, 80 tokens (20) 255 / 269, 96 (24) 274 / 273, 128 (32) 386 / 281; 8 of 128 experts
-    // of 768 x 2048, 256 tokens (16) 128 / 143, 320 (20) 135.5 / 146.4, 384 (24) 146.2 / 149.4, 512 (32) 192 / 157; 32 tokens on all of 8 such experts
-    // 25.8 / 34.3.
+    // 14336 x 4096 (16 pairs an expert) 241 us and 262 in wide tiles, 80 tokens (20) 251 / 266, 96 (24) 266 / 268, 128 (32) 379 / 280; 8 of 128 experts
+    // of 768 x 2048, 256 tokens (16) 124 / 138, 320 (20) 132 / 142, 384 (24) 143 / 146, 512 (32) 182 / 156; 32 tokens on all of 8 such experts
+    // 26.6 / 28.9.
     return T <= 32 || P <= 20 * E ? I8FfnShape::kSmall : I8FfnShape::kGrouped;
 }
 

@@ -5,7 +5,7 @@
 // a bias the order of two experts depends on how s + b is rounded, and of 8192 tokens with 256 experts a few have neighbours nearer
 // than 32 bits tell apart.  A round of the top-k looks for the largest key, the compared value rounded to 32 bits in an order-preserving
 // pattern (six instructions through the vector unit); only where two experts share that pattern are the 64 bits looked at.
-// 8192 tokens, 8 of 256 experts in 4 of 8 groups: 15.4 us, bound by its 64-bit arithmetic and the rounds' dependent steps (the bytes take 2 us).  The
+// 8192 tokens, 8 of 256 experts in 4 of 8 groups: 14.7 us, bound by its 64-bit arithmetic and the rounds' dependent steps (the bytes take 2 us).  The
 // groups are 4.5 us of it, the exponentials 3; one token 5.5 us, and 2047 of 128 experts without groups: latencies.
 #include <float.h>
 
