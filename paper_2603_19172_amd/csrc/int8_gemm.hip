@@ -265,7 +265,8 @@ __device__ __forceinline__ float i8_value(int sum, float xs, float sc, float add
 // a u / (1 + e^-a).  The instruction for powers of two takes t = -a log2 e, a product that rounds by up to 2^-24 of itself; at |a| = 80 that
 // alone moves the power by 2^-18.  What it leaves out, -a - t ln 2, is an exact difference and goes to the result as the factor 1 + that.
 // In steps of 2^-24: exp 2, the factor 1.5, 1 + e^-a 1, the reciprocal 2, the products 1 each: 8.5 at most.  (Beyond 128 e^-a is 0
-// or infinite, and log2 e times a could leave the range.  512 tokens on eight experts of 14336 351 us, as with the rounded t alone.)
+// or infinite, and log2 e times a could leave the range; from -87.3 down the reciprocal is below the normal numbers, and the result 0.
+// 512 tokens on eight experts of 14336 351 us, as with the rounded t alone.)
 __device__ __forceinline__ float silu_times(float a, float u)
 {
     constexpr float kLn2 = 0x1.62e43p-1f, kRest = -0x1.05c61p-29f;          // their sum: ln 2 to 2^-54
