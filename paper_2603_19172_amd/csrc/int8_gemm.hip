@@ -5,6 +5,7 @@
 // the same bits.
 #include <type_traits>
 
+#include "expert_plan.hpp"
 #include "int8_device.hpp"
 #include "int8_rule.hpp"
 
@@ -12,150 +13,20 @@ namespace dymoe {
 
 int quantize_rows(dymoe_ctx* ctx, const void* x, int dtype, long rows, long K, long ldx, int tiles, void* codes, float* scale, hipStream_t st);
 
-// A tile of an expert: all that a workgroup has to know before its first load of weights.
-struct __attribute__((aligned(16))) I8TileRec {
-    int32_t first, pairs;             // the expert's first position, its pairs
-    int32_t tile0, tiles;             // its first tile, its tiles
-    dymoe_expert_i8 mat;
-};
+using I8TileRec = ExpertTile<dymoe_expert_i8>;
+using I8Plan = ExpertPlan<dymoe_expert_i8>;
 
-struct I8Plan {
-    int32_t* meta;        // [8]: tiles, wide tiles behind them
-    int32_t* perm;        // [P] position -> pair
-    int32_t* where;       // [P] pair -> position, -1: left out
-    I8TileRec* tiles;
-};
+__host__ __device__ inline I8Plan i8_plan(int32_t* p, long P) { return expert_plan<dymoe_expert_i8>(p, P); }
 
-__host__ __device__ inline I8Plan i8_plan(int32_t* p, long P)
-{
-    I8Plan r;
-    r.meta = p;
-    r.perm = r.meta + 8;
-    r.where = r.perm + P;
-    r.tiles = (I8TileRec*)(p + 8 + (2 * P + 3) / 4 * 4);
-    return r;
-}
+__device__ __forceinline__ bool i8_present(const dymoe_expert_i8& x) { return expert_present(x); }
 
-__device__ __forceinline__ bool i8_present(const dymoe_expert_i8& x)
-{
-    return (x.q[0] != nullptr) & (x.q[1] != nullptr) & (x.q[2] != nullptr) & (x.s[0] != nullptr) & (x.s[1] != nullptr) & (x.s[2] != nullptr);
-}
-
-// Counting sort of the pairs by expert and the list of tiles, by one workgroup: tall tiles first, then wide ones, by expert.  A pair's turn
-// in its expert is what the counter held before it: kept in registers (in `where` beyond the first kI8PlanKeep pairs of a thread)
-// until the experts' first positions are known, so that there is one pass of atomics.  The turns come in any order, and nothing that is
-// computed depends on it.  The sorted pairs and the tiles' experts pass through LDS where they fit: written from the threads that
-// know them, 16384 pairs cost 7 us in stores of four bytes each, and an expert's sixteen records 3 us in one thread.  16384 pairs of 128
-// experts 12.1 us with 2048 rows' codes beside it, 488 pairs 4.6: latencies of one workgroup's passes, not bytes.
-constexpr int kI8PlanThreads = 1024;
-constexpr int kI8PlanKeep = 16;
-constexpr int kI8PlanPairs = kI8PlanKeep * kI8PlanThreads;
-constexpr int kI8PlanTiles = 4096;
-
-static_assert(kI8PlanThreads == DYMOE_MAX_EXPERTS, "a thread for every expert");
-
-struct I8PlanLds {
-    int count[DYMOE_MAX_EXPERTS], at[DYMOE_MAX_EXPERTS], tile0[DYMOE_MAX_EXPERTS], wave[3][kI8PlanThreads / kWave];
-    uint16_t owner[kI8PlanTiles], perm[kI8PlanPairs];
-};
+using I8PlanLds = ExpertPlanLds;
+constexpr int kI8PlanThreads = kPlanThreads;
 
 __device__ __forceinline__ void i8_make_plan(I8PlanLds& lds, const int32_t* __restrict__ idx, const dymoe_expert_i8* __restrict__ table, long P, int E,
                                              int small, int32_t* __restrict__ plan, unsigned* __restrict__ flags)
 {
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
-    const I8Plan pp = i8_plan(plan, P);
-    int e_of[kI8PlanKeep], turn[kI8PlanKeep];
-#pragma unroll
-    for (int i = 0; i < kI8PlanKeep; i++) {
-        const long p = tid + (long)i * kI8PlanThreads;
-        e_of[i] = p < P ? idx[p] : -1;
-    }
-    const bool held = tid < E && i8_present(table[tid]);
-    lds.count[tid] = 0;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kI8PlanKeep; i++)
-        if ((unsigned)e_of[i] < (unsigned)E) turn[i] = atomicAdd(&lds.count[e_of[i]], 1);
-    for (long p = tid + (long)kI8PlanPairs; p < P; p += kI8PlanThreads) {
-        const int e = idx[p];
-        if ((unsigned)e < (unsigned)E) pp.where[p] = atomicAdd(&lds.count[e], 1);
-    }
-    __syncthreads();
-    int n = lds.count[tid];
-    if (n > 0 && !held) {
-        atomicOr(flags, DYMOE_FLAG_FORMAT_MISSING);
-        n = 0;
-    }
-    const bool one = !small && n <= kI8TileWide;             // a wide tile
-    const int rows = small ? kI8TileSmall : one ? kI8TileWide : kI8TileRows, m = (n + rows - 1) / rows;
-    const int n_in = wave_scan_dpp_i32(n), m2_in = wave_scan_dpp_i32(one ? 0 : m), m1_in = wave_scan_dpp_i32(one ? m : 0);
-    if (lane == kWave - 1) {
-        lds.wave[0][wave] = n_in;
-        lds.wave[1][wave] = m2_in;
-        lds.wave[2][wave] = m1_in;
-    }
-    __syncthreads();
-    int n0 = n_in - n, t2 = m2_in, t1 = m1_in, all2 = 0, all1 = 0;
-    for (int w = 0; w < kI8PlanThreads / kWave; w++) {
-        const int a2 = lds.wave[1][w], a1 = lds.wave[2][w];
-        if (w < wave) {
-            n0 += lds.wave[0][w];
-            t2 += a2;
-            t1 += a1;
-        }
-        all2 += a2;
-        all1 += a1;
-    }
-    const int t0 = one ? all2 + t1 - m : t2 - m;
-    // (in 16-byte pieces: a record put together first would pass through scratch memory)
-    auto record = [&](I8TileRec* to, int e, int first, int pairs, int tile0, int tiles) {
-        uint4* const at = (uint4*)to;
-        const uint2* const mat = (const uint2*)(table + e);
-        store_global(at, make_uint4((uint32_t)first, (uint32_t)pairs, (uint32_t)tile0, (uint32_t)tiles));
-#pragma unroll
-        for (int i = 0; i < 3; i++) {
-            const uint2 lo = load_global<uint2>(mat + 2 * i), hi = load_global<uint2>(mat + 2 * i + 1);
-            store_global(at + 1 + i, make_uint4(lo.x, lo.y, hi.x, hi.y));
-        }
-    };
-    lds.at[tid] = n > 0 ? n0 : -1;
-    lds.count[tid] = n;
-    lds.tile0[tid] = t0;
-    for (int i = 0; i < m; i++) {
-        if (t0 + i < kI8PlanTiles) lds.owner[t0 + i] = (uint16_t)tid;
-        else record(&pp.tiles[t0 + i], tid, n0, n, t0, m);
-    }
-    if (tid == 0) {
-        pp.meta[0] = all2;
-        pp.meta[1] = all1;
-    }
-    __syncthreads();
-    for (int i = tid; i < min(all1 + all2, kI8PlanTiles); i += kI8PlanThreads) {
-        const int e = lds.owner[i], c = lds.count[e];
-        const int per = small ? kI8TileSmall : c <= kI8TileWide ? kI8TileWide : kI8TileRows;
-        record(&pp.tiles[i], e, lds.at[e], c, lds.tile0[e], (c + per - 1) / per);
-    }
-    const bool fits = P <= kI8PlanPairs;
-    auto place = [&](long p, int x, int rank) {
-        int at = -1;
-        if ((unsigned)x < (unsigned)E && lds.at[x] >= 0) {
-            at = lds.at[x] + rank;
-            if (fits) lds.perm[at] = (uint16_t)p;
-            else pp.perm[at] = (int32_t)p;
-        }
-        pp.where[p] = at;
-    };
-#pragma unroll
-    for (int i = 0; i < kI8PlanKeep; i++) {
-        const long p = tid + (long)i * kI8PlanThreads;
-        if (p < P) place(p, e_of[i], turn[i]);
-    }
-    for (long p = tid + (long)kI8PlanPairs; p < P; p += kI8PlanThreads) place(p, idx[p], pp.where[p]);
-    if (!fits) return;
-    __syncthreads();
-    int sorted = 0;
-    for (int w = 0; w < kI8PlanThreads / kWave; w++) sorted += lds.wave[0][w];
-    for (int i = tid; i < sorted; i += kI8PlanThreads) pp.perm[i] = lds.perm[i];
+    make_expert_plan<kI8TileSmall, kI8TileWide, kI8TileRows>(lds, idx, table, P, E, small, plan, flags);
 }
 
 // The plan by the first workgroup, the codes of the activations by the others, four rows each: neither needs the other, and a launch of its
@@ -233,23 +104,7 @@ struct I8Args {
     int rows, Kp, N, k, out_dtype, aligned, tiled;     // aligned: the plain product's rows start where four outputs may be stored at once
 };
 
-// Memory that a wavefront's loads share a base in: the base in scalar registers, a lane's offset and the load's own in 32 bits each.
-struct I8Src {
-    __amdgpu_buffer_rsrc_t r;
-
-    __device__ __forceinline__ void set(const void* p, uint32_t bytes)
-    {
-        const uint64_t u = (uint64_t)p;
-        const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)u), hi = __builtin_amdgcn_readfirstlane((int)(uint32_t)(u >> 32));
-        r = __builtin_amdgcn_make_buffer_rsrc((void*)(((uint64_t)hi << 32) | lo), 0, (int)bytes, 0x00020000);
-    }
-    // NT: streamed through once
-    template <bool NT = false>
-    __device__ __forceinline__ uint4 load(uint32_t lane, uint32_t all) const
-    {
-        return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)lane, (int)all, NT ? 2 : 0));
-    }
-};
+using I8Src = BufferSrc;
 
 enum { kI8Plain = 0, kI8Up = 1, kI8Down = 2 };
 
@@ -261,19 +116,6 @@ __device__ __forceinline__ i32x16_t mfma_i8(const uint4 a, const uint4 b, const 
 // An output of a product: the sum's conversion, its product with the row's scale and the multiply-add round once each, in every shape alike,
 // whatever the compiler would contract.
 __device__ __forceinline__ float i8_value(int sum, float xs, float sc, float add) { return fmaf((float)sum * xs, sc, add); }
-
-// a u / (1 + e^-a).  The instruction for powers of two takes t = -a log2 e, a product that rounds by up to 2^-24 of itself; at |a| = 80 that
-// alone moves the power by 2^-18.  What it leaves out, -a - t ln 2, is an exact difference and goes to the result as the factor 1 + that.
-// In steps of 2^-24: exp 2, the factor 1.5, 1 + e^-a 1, the reciprocal 2, the products 1 each: 8.5 at most.  (Beyond 128 e^-a is 0
-// or infinite, and log2 e times a could leave the range; from -87.3 down the reciprocal is below the normal numbers, and the result 0.
-// 512 tokens on eight experts of 14336 351 us, as with the rounded t alone.)
-__device__ __forceinline__ float silu_times(float a, float u)
-{
-    constexpr float kLn2 = 0x1.62e43p-1f, kRest = -0x1.05c61p-29f;          // their sum: ln 2 to 2^-54
-    const float x = __builtin_amdgcn_fmed3f(a, -128.0f, 128.0f), t = x * -1.44269504f;
-    const float p = 1.0f + fmaf(t, -kRest, fmaf(t, -kLn2, -x));
-    return a * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_exp2f(t), p, 1.0f)) * u;
-}
 
 // ----------------------------------------------------------------------------
 // A few rows (decode): a stream of weights.  A workgroup owns 16 weight rows (of W1 and of W3 in the up projection), its wavefronts take the
@@ -627,26 +469,6 @@ __device__ __forceinline__ void i8_step(I8Strips<S, KT>& w, const I8Src (&q)[S],
     }
 }
 
-// four neighbouring outputs of a row
-__device__ __forceinline__ void i8_store4(void* out, long at, int dt, bool whole, int left, const float (&v)[4])
-{
-    if (whole) {
-        if (dt == DYMOE_OUT_F32) {
-            store_global((float*)out + at, make_float4(v[0], v[1], v[2], v[3]));
-        } else if (dt == DYMOE_OUT_F16) {
-            store_global((uint16_t*)out + at, make_uint2(pack_half2(v[0], v[1]), pack_half2(v[2], v[3])));
-        } else {
-            typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
-            const bf16x4_t b = {(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
-            store_global((uint16_t*)out + at, __builtin_bit_cast(uint2, b));
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; i++)
-        if (i < left) store_out(out, at + i, dt, v[i]);
-}
-
 // Epilogue.  A lane holds, of its token's row, four neighbouring outputs in each group of four registers; the wavefront turns a fragment
 // round in an LDS area of its own, so that a row leaves in whole lines.
 template <int MODE, int NTF, int S>
@@ -682,7 +504,7 @@ __device__ __forceinline__ void i8_finish(const I8Args& A, const int32_t* perm, 
                 const uint4 u = lds_read16(area + (uint32_t)rr * kI8EpiRow<S> + (uint32_t)(lane & 7) * 16u);
                 if (row >= rows || left <= 0) continue;
                 const float v[4] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)};
-                i8_store4(A.out, (long)(row0 + row) * A.ldo + n, dt, left >= 4, left, v);
+                store_out4(A.out, (long)(row0 + row) * A.ldo + n, dt, left >= 4, left, v);
             }
         }
         return;
@@ -720,7 +542,7 @@ __device__ __forceinline__ void i8_finish(const I8Args& A, const int32_t* perm, 
                 float v[4];
 #pragma unroll
                 for (int i = 0; i < 4; i++) v[i] = silu_times(i8_value((int)av[i], xs, c1[i], 0.0f), i8_value((int)uv[i], xs, c3[i], 0.0f));
-                i8_store4(A.out, (long)(row0 + row) * A.ldo + n, dt, left >= 4, left, v);
+                store_out4(A.out, (long)(row0 + row) * A.ldo + n, dt, left >= 4, left, v);
             }
             __syncthreads();
         }
@@ -746,7 +568,7 @@ __device__ __forceinline__ void i8_finish(const I8Args& A, const int32_t* perm, 
                 const float xs = A.xs[row0 + row];
 #pragma unroll
                 for (int i = 0; i < 4; i++) v[i] = i8_value((int)w4[i], xs, sc[i], add[i]);
-                i8_store4(A.out, (long)(row0 + row) * A.ldo + n, dt, left >= 4 && vec, left, v);
+                store_out4(A.out, (long)(row0 + row) * A.ldo + n, dt, left >= 4 && vec, left, v);
             }
         }
     }
@@ -1077,7 +899,7 @@ __device__ __forceinline__ void i8_split_tile(const I8Args& A, const I8Unit<1>& 
             float v[4];
 #pragma unroll
             for (int i = 0; i < 4; i++) v[i] = i8_value((int)sum[i], xs, sc[i], add[i]);
-            i8_store4(A.out, (long)(u.row0 + row) * A.ldo + n, A.out_dtype, left >= 4 && A.aligned, left, v);
+            store_out4(A.out, (long)(u.row0 + row) * A.ldo + n, A.out_dtype, left >= 4 && A.aligned, left, v);
         }
         __syncthreads();
     }
@@ -1321,7 +1143,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 2 : 3) void i8_small_kernel(cons
             if (MODE == kI8Up) v[i] = silu_times(v[i], i8_value(sum(NTF + f), xs, sb[m], 0.0f));
         }
         const bool whole = left >= 4 && (MODE != kI8Plain || A.aligned);
-        i8_store4(A.out, (long)(row0 + row) * A.ldo + n, MODE == kI8Plain ? A.out_dtype : DYMOE_OUT_F32, whole, left, v);
+        store_out4(A.out, (long)(row0 + row) * A.ldo + n, MODE == kI8Plain ? A.out_dtype : DYMOE_OUT_F32, whole, left, v);
     }
 }
 
@@ -1347,8 +1169,8 @@ __global__ __launch_bounds__(256) void i8_combine_kernel(const float* __restrict
         for (int i = 0; i < 8; i++) sum[i] = fmaf(g, v[i], sum[i]);
     }
     const float lo[4] = {sum[0], sum[1], sum[2], sum[3]}, hi[4] = {sum[4], sum[5], sum[6], sum[7]};
-    i8_store4(y, t * H + h, out_dtype, aligned && h + 4 <= H, H - h, lo);
-    i8_store4(y, t * H + h + 4, out_dtype, aligned && h + 8 <= H, H - h - 4, hi);
+    store_out4(y, t * H + h, out_dtype, aligned && h + 4 <= H, H - h, lo);
+    store_out4(y, t * H + h + 4, out_dtype, aligned && h + 8 <= H, H - h - 4, hi);
 }
 
 }  // namespace dymoe
