@@ -58,6 +58,7 @@ extern "C" {
 #define DYMOE_OUT_F32 1
 #define DYMOE_OUT_F16 2        /* the 8-bit integer operators and dymoe_route_scored, as a type of inputs and of outputs */
 #define DYMOE_DTYPE_I8 3       /* x_dtype of dymoe_matmul_int8: codes that dymoe_quantize_rows wrote */
+#define DYMOE_DTYPE_MX4 4      /* x_dtype of dymoe_matmul_mx4: codes that dymoe_quantize_mx4 wrote */
 
 /* score of dymoe_route_scored */
 #define DYMOE_SCORE_SOFTMAX 0
@@ -65,6 +66,10 @@ extern "C" {
 
 /* columns of a row that the 8-bit integer operators take: 127 * 127 * 131072 < 2^31 */
 #define DYMOE_INT8_MAX_K 131072
+
+/* the microscaled 4-bit format: columns of a block with a common power of two, and of a row that its operators take */
+#define DYMOE_MX4_BLOCK 32
+#define DYMOE_MX4_MAX_K 131072
 
 /* path of dymoe_moe_ffn_mixed */
 #define DYMOE_PATH_AUTO 0
@@ -581,6 +586,108 @@ int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, const int32_t
                        void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Rows to microscaled 4-bit floating point (tokens, or a weight matrix's channels): blocks of DYMOE_MX4_BLOCK = 32 columns, one byte a
+ * block for a power of two, four bits a value.  In a block, with a = max |x|:
+ *   e = floor(log2 a) - 2, at least -127;  byte = e + 127 (a = 0: 0)
+ *   code = x / 2^e to the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0 .. 7; ties to the even code; beyond 6: 6), bit 3 the sign of x
+ * The value a code stands for is 2^e times its number.  A block that holds an infinity or a NaN gets byte 255 and codes 0: it stands
+ * for NaN, and so is every sum that it enters; no other row is touched.
+ * x [rows,K] bf16, fp16 or fp32 (x_dtype: DYMOE_OUT_*), rows ldx values apart (any alignment of the type's own).  Kp = K rounded
+ * up to a multiple of 256; codes 16-byte aligned, the first of two columns in a byte's low half; scale 4-byte aligned:
+ *  DYMOE_LAYOUT_ROWMAJOR  codes [rows, Kp / 2], scale [rows, Kp / 32], zeros behind column K.
+ *  DYMOE_LAYOUT_TILE      over rows rounded up to a multiple of 32, zeros behind both ends, in tiles of 32 rows x 256 columns, tile
+ *    (nt, kt) at index nt * (Kp / 256) + kt.  "Lane" l = 32 * kb + r of a tile owns row 32 * nt + r, columns 256 * kt + 128 * kb .. + 128.
+ *    Codes: 4 KiB a tile, the lane's chunk c (32 columns) at byte c * 1024 + l * 16.  scale: 256 bytes a tile, the lane's four at
+ *    l * 4.  What the weights of the two calls below are held in.
+ * Limits: K <= DYMOE_MX4_MAX_K, rows < 2^31 - 32 (else DYMOE_ENOTSUP).
+ * dymoe_dequantize_mx4: the values that codes stand for, rounded once to out_dtype (bf16 and fp32 hold them exactly), y [rows,K], rows ldy
+ * >= K values apart; what lies between them is left as it was.
+ */
+int dymoe_quantize_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, long rows, long K, long ldx, int layout, uint8_t* codes,
+                       uint8_t* scale, void* stream);
+int dymoe_dequantize_mx4(dymoe_ctx* ctx, const uint8_t* codes, const uint8_t* scale, long rows, long K, int layout, int out_dtype,
+                         void* y, long ldy, void* stream);
+
+/*
+ * Matrix product in microscaled 4-bit floating point:
+ *   y[t,n] = sum over blocks b of 2^(ex[t,b] + ew[n,b]) sum_{j in b} xq[t,j] wq[n,j]  (+ bias[n])
+ * A block's sum is exact; the sum over blocks and the bias are taken in fp32 and rounded once to the output's type.  The order of the
+ * blocks belongs to the call's sizes: the same call gives the same bits, a row beside other rows may differ in its fp32 sum's last bits.
+ * x: bf16, fp16 or fp32 [T,K], rows ldx values apart: converted in the call as by dymoe_quantize_mx4 (workspace, x_scale
+ * ignored); or DYMOE_DTYPE_MX4: codes [T,Kp/2] and x_scale [T,Kp/32] that dymoe_quantize_mx4 wrote row-major, ldx = Kp (no workspace).
+ * w, w_scale: [N,K] as dymoe_quantize_mx4 writes it in DYMOE_LAYOUT_TILE.  bias [N] fp32 or NULL.
+ * y [T,N] in out_dtype (DYMOE_OUT_*), rows ldy >= N values apart; what lies between them is left as it was.
+ * workspace: dymoe_matmul_mx4_workspace_bytes(T, N, K) bytes (0 for invalid sizes), 256-byte aligned, scratch.
+ * Limits: K <= DYMOE_MX4_MAX_K; T, N <= 2^24, T / 32 times N / 32, both rounded up, < 2^23 (else DYMOE_ENOTSUP).
+ */
+size_t dymoe_matmul_mx4_workspace_bytes(int T, int N, int K);
+int dymoe_matmul_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, const uint8_t* x_scale, long ldx, const uint8_t* w,
+                     const uint8_t* w_scale, const float* bias, int T, int N, int K, int out_dtype, void* y, long ldy,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
+/* One expert in microscaled 4-bit floating point: W1, W3 [F,H] and W2 [H,F] as dymoe_quantize_mx4 writes them in DYMOE_LAYOUT_TILE
+ * (codes 16-byte, scale 4-byte aligned). */
+typedef struct {
+    const uint8_t* q[3];
+    const uint8_t* s[3];
+} dymoe_expert_mx4;
+
+/*
+ * SwiGLU experts in microscaled 4-bit floating point, activations and intermediate converted on the way:
+ *   y[t,:] = sum_{slot<k} w[t,slot] * W2_e q( silu(W1_e q(x_t)) * (W3_e q(x_t)) ),  e = idx[t,slot],
+ * q() the conversion of dymoe_quantize_mx4, the products those of dymoe_matmul_mx4.  The SwiGLU intermediate, each pair's output
+ * and the sum over the slots are held in fp32, rounded once to y's type.  The same call gives the same bits; the order of the fp32 sums
+ * belongs to the call's sizes and routing, so that beside other tokens an intermediate value next to the middle of two codes may get the
+ * other one.
+ * x [T,H] bf16, fp16 or fp32; idx [T,k] int32; w [T,k] fp32; table [E] of dymoe_expert_mx4 in device memory; y [T,H] in
+ * out_dtype (every row is written).  A pair whose index lies outside [0,E) contributes nothing, nor does one whose
+ * expert's entry holds a NULL (DYMOE_FLAG_FORMAT_MISSING, dymoe_device_flags).
+ * workspace: dymoe_moe_ffn_mx4_workspace_bytes(T,H,F,E,k) bytes (0 for invalid sizes), 256-byte aligned, scratch.
+ * Limits: any H, F up to DYMOE_MX4_MAX_K, E <= DYMOE_MAX_EXPERTS; T k < 2^29, T times H rounded up to 256 < 2^33, and a launch of
+ * fewer than 2^32 threads: T times H / 2048 rounded up < 2^24, (T k / 32 + min(E, T k)) times the larger of H / 32 and F / 32 rounded up
+ * < 2^23 (else DYMOE_ENOTSUP).
+ */
+size_t dymoe_moe_ffn_mx4_workspace_bytes(int T, int H, int F, int E, int k);
+int dymoe_moe_ffn_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, const int32_t* idx, const float* w,
+                      const dymoe_expert_mx4* table, int T, int H, int F, int E, int k, int out_dtype, void* y,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * How evenly a router that scores spreads its tokens, and the loss that a training run adds for it.  Over the tokens that take part (keep
+ * NULL: all T; else those with keep[t] != 0), M of them, with s the scores of dymoe_route_scored:
+ *   p[t,e] = s[t,e] / sum_e s[t,e];  counts[e] = (token, slot) pairs with idx[t,slot] = e;  counts[E] = M
+ *   mean[e] = sum_t p[t,e] / M;  loss = coef * E * sum_e counts[e] / (M k) * mean[e]   (M = 0: zeros)
+ * 1 * coef where all experts are as likely and as often chosen.  Masked logits (minus infinity, the type's lowest value) have p = 0, a token whose
+ * logits are all masked adds nothing to the means; a token with a NaN, or with plus infinity under softmax, that takes part
+ * makes them and the loss NaN.  Entries of idx outside [0,E) are not counted.  p comes in fp32, below 2^-126 of the largest: 0; sums over tokens in
+ * 64 bits, in an order that T and E fix.
+ * logits [T,E] bf16, fp16 or fp32 (dtype: DYMOE_OUT_*), idx [T,k] int32, keep [T] uint8 or NULL; counts [E+1] int32, mean [E] fp32,
+ * loss [1] fp32.  workspace: dymoe_route_balance_workspace_bytes(T, E) bytes (0 for invalid sizes), 256-byte aligned, scratch.
+ * Limits: 1 <= k <= E <= DYMOE_MAX_EXPERTS, k <= 64, T < 2^25 (else DYMOE_ENOTSUP).  One launch for up to 32 tokens, else two.
+ */
+size_t dymoe_route_balance_workspace_bytes(int T, int E);
+int dymoe_route_balance(dymoe_ctx* ctx, const void* logits, int dtype, const int32_t* idx, const uint8_t* keep, int T, int E, int k,
+                        int score, float coef, int32_t* counts, float* mean, float* loss, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/*
+ * Gradient of a router's logits: of the weights that dymoe_route_scored gave (dw [T,k] fp32 or NULL: the loss with respect to w), and
+ * of dymoe_route_balance's loss (counts as that call wrote them, or NULL; dloss [1] fp32 in device memory, NULL: 1), added:
+ *   the loss:  r p (g - sum_e p g) for tokens that take part,  g[e] = dloss * coef * E * counts[e] / (M^2 k)
+ *   w, renorm:  factor r q (dw - sum q dw) at the chosen experts, q[j] = s[idx[j]] / sum_j s[idx[j]]
+ *   w, without renorm:  factor s (dw - sum s dw) (softmax; dw 0 at experts that were not chosen), factor s (1 - s) dw (sigmoid)
+ * with r = 1 - s of a sigmoid, 1 of a softmax, and s, p as above.  The selection, its bias and groups have no gradient; counts are constants.  Masked
+ * logits have gradient 0, slots whose index lies outside [0,E) no part, an expert in several slots its slots' sum.  A token with a NaN, or
+ * with plus infinity under softmax, has NaN gradients (0 where neither part concerns it).  (Scores below e^-700, which dymoe_route_scored
+ * holds at that, are not held here.)
+ * logits, dtype, idx, keep, score as above, renorm and factor as in the forward call; grad [T,E] in grad_dtype (DYMOE_OUT_*), every
+ * value written, fp32 arithmetic, rounded once.  Limits as above; at least one of dw and counts.
+ */
+int dymoe_route_scored_backward(dymoe_ctx* ctx, const void* logits, int dtype, const int32_t* idx, const float* dw, int T, int E, int k,
+                                int score, int renorm, float factor, const int32_t* counts, float coef, const float* dloss,
+                                const uint8_t* keep, int grad_dtype, void* grad, void* stream);
+
+/*
  * Host-resident experts (Sec. 4.4.1, Phase-Adaptive Prefetcher): the weights a
  * later layer is predicted to need are copied from pinned host memory into
  * device buffers on a side stream while the compute stream works on the current
@@ -718,14 +825,15 @@ size_t dymoe_cache_bytes_resident(const dymoe_cache* cache);
  * Per-kernel timing (diagnostic; the paper reports only end-to-end latency,
  * Sec. 6.1 "Key Metrics", so these serve the roofline accounting).
  * dymoe_timing_enable: launches of the kernels whose bit is set in kernel_mask
- * (bit i = kernel id i, ids 0..28 in the order route, token_norm, importance,
+ * (bit i = kernel id i, ids 0..31 in the order route, token_norm, importance,
  * assign, quantize, gemv_phase1, gemv_phase2, gemv_combine, plan, gemm1, gemm2,
  * gemm_combine, stream_copy, decode_front, attn_stats, attn_colsum, gptq_group,
  * gptq_trail, gptq_hessian, gptq_factor, mfma_peak, route_select, route_scored, quantize_rows, matmul_int8,
- * int8_plan, int8_up, int8_down, int8_combine; gemv_combine is reserved: the decode path's
+ * int8_plan, int8_up, int8_down, int8_combine, mx4_rows, mx4_product, route_balance; gemv_combine is reserved: the decode path's
  * second phase writes y itself and no launch carries that id; route_select is the second of the two launches
  * dymoe_route_topk makes when it cuts the logits by experts as well as by tokens, route then names the first;
- * int8_down of a few tokens includes the sum over the slots) carry a start and a stop HIP event on the dispatch itself, so
+ * int8_down of a few tokens includes the sum over the slots; mx4_rows are the conversions, the experts' plan and their combination, mx4_product
+ * all products in that format, route_balance the loss's launches and the logits' gradient) carry a start and a stop HIP event on the dispatch itself, so
  * the interval is the kernel's execution time on the launch stream; 0 switches
  * timing off.  Either way, records not yet read are dropped.
  * dymoe_timing_read: waits for the recorded launches of `kernel`, drops their records and returns

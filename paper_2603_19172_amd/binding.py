@@ -8,6 +8,7 @@ if the shared library is missing, importing this module raises.
 """
 import ctypes as C
 import os
+import typing
 
 import torch
 
@@ -25,9 +26,10 @@ OK, EINVAL, ENOSPC, EHIP, ENOTSUP, ENOCTX = 0, -1, -2, -3, -4, -5
 PHASE_PREFILL, PHASE_DECODE = 0, 1
 FRONT_MAX_TOKENS = 16
 FLAG_FORMAT_MISSING = 1
-OUT_BF16, OUT_F32, OUT_F16, DTYPE_I8 = 0, 1, 2, 3
+OUT_BF16, OUT_F32, OUT_F16, DTYPE_I8, DTYPE_MX4 = 0, 1, 2, 3, 4
 SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 INT8_MAX_K = 131072
+MX4_BLOCK, MX4_MAX_K = 32, 131072
 PATH_AUTO, PATH_GEMV, PATH_GEMM = 0, 1, 2
 LAYOUT_ROWMAJOR, LAYOUT_TILE = 0, 1
 
@@ -49,12 +51,16 @@ EXPORTS = [
     "dymoe_timing_enable", "dymoe_timing_read", "dymoe_kernel_name",
     "dymoe_route_scored", "dymoe_quantize_rows", "dymoe_matmul_int8_workspace_bytes", "dymoe_matmul_int8",
     "dymoe_moe_ffn_int8_workspace_bytes", "dymoe_moe_ffn_int8",
+    "dymoe_quantize_mx4", "dymoe_dequantize_mx4", "dymoe_matmul_mx4_workspace_bytes", "dymoe_matmul_mx4",
+    "dymoe_moe_ffn_mx4_workspace_bytes", "dymoe_moe_ffn_mx4", "dymoe_route_balance_workspace_bytes", "dymoe_route_balance",
+    "dymoe_route_scored_backward",
 ]
 
 KERNELS = ["route", "token_norm", "importance", "assign", "quantize", "gemv_phase1",
            "gemv_phase2", "gemv_combine", "plan", "gemm1", "gemm2", "gemm_combine", "stream_copy", "decode_front",
            "attn_stats", "attn_colsum", "gptq_group", "gptq_trail", "gptq_hessian", "gptq_factor", "mfma_peak", "route_select",
-           "route_scored", "quantize_rows", "matmul_int8", "int8_plan", "int8_up", "int8_down", "int8_combine"]
+           "route_scored", "quantize_rows", "matmul_int8", "int8_plan", "int8_up", "int8_down", "int8_combine", "mx4_rows",
+           "mx4_product", "route_balance"]
 
 
 class ExpertFmt(C.Structure):
@@ -68,6 +74,20 @@ class ExpertFmt(C.Structure):
 class ExpertI8(C.Structure):
     """Mirror of dymoe_expert_i8."""
     _fields_ = [("q", C.c_void_p * 3), ("s", C.c_void_p * 3)]
+
+
+class ExpertMx4(C.Structure):
+    """Mirror of dymoe_expert_mx4."""
+    _fields_ = [("q", C.c_void_p * 3), ("s", C.c_void_p * 3)]
+
+
+class Mx4Matrix(typing.NamedTuple):
+    """A matrix of rows x cols values as Context.quantize_mx4 writes it: codes and exponent bytes, uint8, in one of the two layouts."""
+    codes: torch.Tensor
+    scale: torch.Tensor
+    rows: int
+    cols: int
+    layout: int
 
 
 CACHE_MAX_FORMATS, CACHE_MAX_EVICT = 4, 16
@@ -190,6 +210,24 @@ lib.dymoe_moe_ffn_int8_workspace_bytes.restype = _sz
 lib.dymoe_moe_ffn_int8_workspace_bytes.argtypes = [_i] * 5
 lib.dymoe_moe_ffn_int8.restype = _i
 lib.dymoe_moe_ffn_int8.argtypes = [_vp, _vp, _i, _vp, _vp, _vp] + [_i] * 6 + [_vp, _vp, _sz, _vp]
+lib.dymoe_quantize_mx4.restype = _i
+lib.dymoe_quantize_mx4.argtypes = [_vp, _vp, _i, _l, _l, _l, _i, _vp, _vp, _vp]
+lib.dymoe_dequantize_mx4.restype = _i
+lib.dymoe_dequantize_mx4.argtypes = [_vp, _vp, _vp, _l, _l, _i, _i, _vp, _l, _vp]
+lib.dymoe_matmul_mx4_workspace_bytes.restype = _sz
+lib.dymoe_matmul_mx4_workspace_bytes.argtypes = [_i] * 3
+lib.dymoe_matmul_mx4.restype = _i
+lib.dymoe_matmul_mx4.argtypes = [_vp, _vp, _i, _vp, _l, _vp, _vp, _vp, _i, _i, _i, _i, _vp, _l, _vp, _sz, _vp]
+lib.dymoe_moe_ffn_mx4_workspace_bytes.restype = _sz
+lib.dymoe_moe_ffn_mx4_workspace_bytes.argtypes = [_i] * 5
+lib.dymoe_moe_ffn_mx4.restype = _i
+lib.dymoe_moe_ffn_mx4.argtypes = [_vp, _vp, _i, _vp, _vp, _vp] + [_i] * 6 + [_vp, _vp, _sz, _vp]
+lib.dymoe_route_balance_workspace_bytes.restype = _sz
+lib.dymoe_route_balance_workspace_bytes.argtypes = [_i] * 2
+lib.dymoe_route_balance.restype = _i
+lib.dymoe_route_balance.argtypes = [_vp, _vp, _i, _vp, _vp] + [_i] * 4 + [C.c_float, _vp, _vp, _vp, _vp, _sz, _vp]
+lib.dymoe_route_scored_backward.restype = _i
+lib.dymoe_route_scored_backward.argtypes = [_vp, _vp, _i, _vp, _vp] + [_i] * 5 + [C.c_float, _vp, C.c_float, _vp, _vp, _i, _vp, _vp]
 
 
 lib.dymoe_timing_enable.restype = _i
@@ -303,6 +341,24 @@ def matmul_int8_workspace_bytes(T, N, K) -> int:
 
 def moe_ffn_int8_workspace_bytes(T, H, F, E, k) -> int:
     return int(lib.dymoe_moe_ffn_int8_workspace_bytes(T, H, F, E, k))
+
+
+def matmul_mx4_workspace_bytes(T, N, K) -> int:
+    return int(lib.dymoe_matmul_mx4_workspace_bytes(T, N, K))
+
+
+def moe_ffn_mx4_workspace_bytes(T, H, F, E, k) -> int:
+    return int(lib.dymoe_moe_ffn_mx4_workspace_bytes(T, H, F, E, k))
+
+
+def route_balance_workspace_bytes(T, E) -> int:
+    return int(lib.dymoe_route_balance_workspace_bytes(T, E))
+
+
+def mx4_shapes(rows, cols, layout):
+    """Shapes of the codes and of the exponents of a matrix in that layout."""
+    held, wide = _up(rows, 32) if layout == LAYOUT_TILE else rows, _up(cols, 256)
+    return (held, wide // 2), (held, wide // MX4_BLOCK)
 
 
 def format_present(entry, bits) -> bool:
@@ -629,6 +685,8 @@ class Context:
         E, rest = divmod(table.numel() * table.element_size(), C.sizeof(ExpertI8))
         if rest or not E or not table.is_contiguous():
             raise ValueError("the table has to be contiguous and of whole entries")
+        if getattr(table, "entries", "int8") != "int8":
+            raise ValueError("the table's experts are not in this format")
         if getattr(table, "sizes", (H, F)) != (H, F):
             raise ValueError("x and F say H = %d, F = %d; the table's experts are of H = %d, F = %d" % (H, F, *table.sizes))
         if y is None:
@@ -640,6 +698,114 @@ class Context:
                                       _at(y, dev, None, (T, H)), _at(workspace, dev, torch.uint8), workspace.numel(),
                                       _stream_of(dev, stream)), "dymoe_moe_ffn_int8")
         return y
+
+    # -- microscaled 4-bit floating point
+    def _mx4(self, m, layout, what):
+        """Device pointers of a matrix's codes and exponents, in the layout that the call reads."""
+        if m.layout != layout:
+            raise ValueError("%s is expected in %s" % (what, "the tile layout" if layout == LAYOUT_TILE else "row-major order"))
+        codes, scale = mx4_shapes(m.rows, m.cols, m.layout)
+        return _at(m.codes, self.device, torch.uint8, codes), _at(m.scale, self.device, torch.uint8, scale)
+
+    def quantize_mx4(self, x, layout=LAYOUT_ROWMAJOR, out=None, stream=None):
+        """x [rows, K] bf16 / fp16 / fp32, columns contiguous -> Mx4Matrix; out: (codes, exponents) to write, of mx4_shapes."""
+        (rows, K, pitch), dev = _matrix(x), self.device
+        codes, scale = mx4_shapes(rows, K, layout)
+        if out is None:
+            out = (_empty(codes, torch.uint8, x.device, stream), _empty(scale, torch.uint8, x.device, stream))
+        _check(lib.dymoe_quantize_mx4(self._h, _at(x, dev), _dtype_code(x), rows, K, pitch, layout, _at(out[0], dev, torch.uint8, codes),
+                                      _at(out[1], dev, torch.uint8, scale), _stream_of(dev, stream)), "dymoe_quantize_mx4")
+        return Mx4Matrix(out[0], out[1], rows, K, layout)
+
+    def dequantize_mx4(self, m, out_dtype=OUT_BF16, out=None, stream=None):
+        """The values of an Mx4Matrix, [rows, cols], of the type of `out` where that is given."""
+        if out is None:
+            out = _empty((m.rows, m.cols), _TORCH_OUT[out_dtype], m.codes.device, stream)
+        rows, cols, ldy = _matrix(out)
+        if (rows, cols) != (m.rows, m.cols):
+            raise ValueError("out has shape %s, expected %s" % (tuple(out.shape), (m.rows, m.cols)))
+        codes, scale = self._mx4(m, m.layout, "the matrix")
+        _check(lib.dymoe_dequantize_mx4(self._h, codes, scale, rows, cols, m.layout, _dtype_code(out), _at(out, self.device), ldy,
+                                        _stream_of(self.device, stream)), "dymoe_dequantize_mx4")
+        return out
+
+    def matmul_mx4(self, x, w, bias=None, out_dtype=OUT_BF16, y=None, workspace=None, stream=None):
+        """x [T, K] bf16 / fp16 / fp32, or a row-major Mx4Matrix; w: an Mx4Matrix in the tile layout.  Returns y [T, N], of the type of
+        `y` where that is given."""
+        dev, N = self.device, w.rows
+        if isinstance(x, Mx4Matrix):
+            T, K, dtype, pitch = x.rows, x.cols, DTYPE_MX4, _up(x.cols, 256)
+            (xp, xs), device = self._mx4(x, LAYOUT_ROWMAJOR, "x"), x.codes.device
+        else:
+            (T, K, pitch), dtype, xp, xs, device = _matrix(x), _dtype_code(x), _at(x, dev), None, x.device
+            if workspace is None:
+                workspace = _empty((matmul_mx4_workspace_bytes(T, N, K),), torch.uint8, device, stream)
+        if K != w.cols:
+            raise ValueError("x has %d columns, w %d" % (K, w.cols))
+        wp, ws = self._mx4(w, LAYOUT_TILE, "w")
+        if y is None:
+            y = _empty((T, N), _TORCH_OUT[out_dtype], device, stream)
+        rows, cols, ldy = _matrix(y)
+        if rows != T or cols != N:
+            raise ValueError("y has shape %s, expected %s" % (tuple(y.shape), (T, N)))
+        _check(lib.dymoe_matmul_mx4(self._h, xp, dtype, xs, pitch, wp, ws, _at(bias, dev, torch.float32, (N,)), T, N, K, _dtype_code(y),
+                                    _at(y, dev), ldy, _at(workspace, dev, torch.uint8), 0 if workspace is None else workspace.numel(),
+                                    _stream_of(dev, stream)), "dymoe_matmul_mx4")
+        return y
+
+    def moe_ffn_mx4(self, x, idx, w, table, F, out_dtype=OUT_BF16, y=None, workspace=None, stream=None):
+        """x [T, H] bf16 / fp16 / fp32; idx, w [T, k]; table: make_mx4_table's, or dymoe_expert_mx4 entries of the caller's own, whose
+        matrices then have to be of sizes H and F.  Returns y [T, H]."""
+        (T, H), k, dev = x.shape, idx.shape[1], self.device
+        E, rest = divmod(table.numel() * table.element_size(), C.sizeof(ExpertMx4))
+        if rest or not E or not table.is_contiguous():
+            raise ValueError("the table has to be contiguous and of whole entries")
+        if getattr(table, "entries", "mx4") != "mx4":
+            raise ValueError("the table's experts are not in this format")
+        if getattr(table, "sizes", (H, F)) != (H, F):
+            raise ValueError("x and F say H = %d, F = %d; the table's experts are of H = %d, F = %d" % (H, F, *table.sizes))
+        if y is None:
+            y = _empty((T, H), _TORCH_OUT[out_dtype], x.device, stream)
+        if workspace is None:
+            workspace = _empty((moe_ffn_mx4_workspace_bytes(T, H, F, E, k),), torch.uint8, x.device, stream)
+        _check(lib.dymoe_moe_ffn_mx4(self._h, _at(x, dev, None, (T, H)), _dtype_code(x), _at(idx, dev, torch.int32, (T, k)),
+                                     _at(w, dev, torch.float32, (T, k)), _at(table, dev), T, H, F, E, k, _dtype_code(y),
+                                     _at(y, dev, None, (T, H)), _at(workspace, dev, torch.uint8), workspace.numel(),
+                                     _stream_of(dev, stream)), "dymoe_moe_ffn_mx4")
+        return y
+
+    # -- the training side of a router that scores
+    def route_balance(self, logits, idx, coef, score=SCORE_SIGMOID, keep=None, counts=None, mean=None, loss=None, workspace=None, stream=None):
+        """logits [T, E] bf16 / fp16 / fp32, idx [T, k], keep [T] uint8 (0: a token of padding) -> counts [E + 1] int32 (the last: the
+        tokens that take part), mean [E] fp32, loss [1] fp32."""
+        (T, E), k, dev, dtype = logits.shape, idx.shape[1], self.device, _dtype_code(logits)
+        if counts is None:
+            counts = _empty((E + 1,), torch.int32, logits.device, stream)
+        if mean is None:
+            mean = _empty((E,), torch.float32, logits.device, stream)
+        if loss is None:
+            loss = _empty((1,), torch.float32, logits.device, stream)
+        if workspace is None:
+            workspace = _empty((route_balance_workspace_bytes(T, E),), torch.uint8, logits.device, stream)
+        _check(lib.dymoe_route_balance(self._h, _at(logits, dev, None, (T, E)), dtype, _at(idx, dev, torch.int32, (T, k)),
+                                       _at(keep, dev, torch.uint8, (T,)), T, E, k, score, coef, _at(counts, dev, torch.int32, (E + 1,)),
+                                       _at(mean, dev, torch.float32, (E,)), _at(loss, dev, torch.float32, (1,)),
+                                       _at(workspace, dev, torch.uint8), workspace.numel(), _stream_of(dev, stream)), "dymoe_route_balance")
+        return counts, mean, loss
+
+    def route_scored_backward(self, logits, idx, dw=None, score=SCORE_SIGMOID, renorm=True, factor=1.0, counts=None, coef=0.0, dloss=None,
+                              keep=None, grad_dtype=None, out=None, stream=None):
+        """The logits' gradient [T, E] of route_scored's weights (dw [T, k]) and of route_balance's loss (its counts and coef, dloss [1]
+        fp32 on the device); of the logits' type, of grad_dtype, or of that of `out`."""
+        (T, E), k, dev, dtype = logits.shape, idx.shape[1], self.device, _dtype_code(logits)
+        if out is None:
+            out = _empty((T, E), _TORCH_OUT[dtype if grad_dtype is None else grad_dtype], logits.device, stream)
+        _check(lib.dymoe_route_scored_backward(self._h, _at(logits, dev, None, (T, E)), dtype, _at(idx, dev, torch.int32, (T, k)),
+                                               _at(dw, dev, torch.float32, (T, k)), T, E, k, score, 1 if renorm else 0, factor,
+                                               _at(counts, dev, torch.int32, (E + 1,)), coef, _at(dloss, dev, torch.float32, (1,)),
+                                               _at(keep, dev, torch.uint8, (T,)), _dtype_code(out), _at(out, dev, None, (T, E)),
+                                               _stream_of(dev, stream)), "dymoe_route_scored_backward")
+        return out
 
     # -- S5
     def moe_ffn_mixed(self, x, idx, w, bits, table, F, out_dtype=OUT_BF16, path=PATH_AUTO,
@@ -682,6 +848,36 @@ def make_int8_table(experts, device):
             arr[e].q[i] = _ptr(codes, torch.int8)
             arr[e].s[i] = _ptr(scale, torch.float32)
     table = torch.frombuffer(bytearray(bytes(arr)), dtype=torch.uint8).to(device)
+    table.entries = "int8"
+    if size is not None:
+        table.sizes = (size[1], size[0])        # H, F: what the calls check theirs against
+    return table
+
+
+def make_mx4_table(experts, device):
+    """The device-resident dymoe_expert_mx4[E] of experts that are three Mx4Matrix each (W1, W3 [F, H], W2 [H, F]) in the tile layout,
+    on that device; an expert given as None has an empty entry.  The caller keeps the matrices alive."""
+    arr = (ExpertMx4 * len(experts))()
+    size, device = None, torch.empty(0, device=device).device
+    for e, mats in enumerate(experts):
+        if mats is None:
+            continue
+        F, H = mats[0].rows, mats[0].cols
+        if [(m.rows, m.cols, m.layout) for m in mats] != [(F, H, LAYOUT_TILE), (F, H, LAYOUT_TILE), (H, F, LAYOUT_TILE)] or (size or (F, H)) != (F, H):
+            raise ValueError("expert %d: W1, W3 [F, H] and W2 [H, F] in the tile layout, of one size in a table" % e)
+        size = (F, H)
+        for i, m in enumerate(mats):
+            codes, scale = mx4_shapes(m.rows, m.cols, m.layout)
+            if tuple(m.codes.shape) != codes or tuple(m.scale.shape) != scale:
+                raise ValueError("expert %d: codes and exponents of shapes %s and %s" % (e, codes, scale))
+            if m.codes.device != device or m.scale.device != device:
+                raise ValueError("expert %d: codes on %s and exponents on %s, the table's device is %s" % (e, m.codes.device, m.scale.device, device))
+            if m.codes.data_ptr() % 16 or m.scale.data_ptr() % 4:
+                raise ValueError("expert %d: codes have to be 16-byte aligned, exponents 4-byte" % e)
+            arr[e].q[i] = _ptr(m.codes, torch.uint8)
+            arr[e].s[i] = _ptr(m.scale, torch.uint8)
+    table = torch.frombuffer(bytearray(bytes(arr)), dtype=torch.uint8).to(device)
+    table.entries = "mx4"
     if size is not None:
         table.sizes = (size[1], size[0])        # H, F: what the calls check theirs against
     return table

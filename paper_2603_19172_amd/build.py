@@ -29,7 +29,7 @@ PER_FILE = {"quantize.hip": ["-ffp-contract=off"], "gptq.hip": ["-ffp-contract=o
 
 SOURCES = ["api.hip", "route.hip", "importance.hip", "quantize.hip", "ffn.hip", "ffn_gemv.hip",
            "ffn_gemm.hip", "plan.hip", "prefetch.hip", "attention.hip", "gptq.hip",
-           "route_scored.hip", "int8_rows.hip", "int8_gemm.hip", "expert_cache.cpp"]
+           "route_scored.hip", "int8_rows.hip", "int8_gemm.hip", "mx4_rows.hip", "mx4_gemm.hip", "route_train.hip", "expert_cache.cpp"]
 
 
 def _compile(src: str) -> str:

@@ -164,7 +164,7 @@ void dymoe_destroy(dymoe_ctx* ctx)
 int dymoe_timing_enable(dymoe_ctx* ctx, unsigned kernel_mask)
 {
     if (!ctx) return DYMOE_ENOCTX;
-    DYMOE_REQUIRE((kernel_mask >> DYMOE_K_COUNT) == 0);
+    DYMOE_REQUIRE(((uint64_t)kernel_mask >> DYMOE_K_COUNT) == 0);
     drop_timed(ctx);
     ctx->timing_mask = kernel_mask;
     return DYMOE_OK;
@@ -229,6 +229,9 @@ const char* dymoe_kernel_name(int kernel)
     case DYMOE_K_INT8_UP: return "i8_experts_kernel<1>";
     case DYMOE_K_INT8_DOWN: return "i8_experts_kernel<2>";
     case DYMOE_K_INT8_COMBINE: return "i8_combine_kernel";
+    case DYMOE_K_MX4_ROWS: return "mx4_quantize_kernel";
+    case DYMOE_K_MX4_PRODUCT: return "mx4_small_kernel";
+    case DYMOE_K_ROUTE_BALANCE: return "route_balance_kernel";
     default: return nullptr;
     }
 }

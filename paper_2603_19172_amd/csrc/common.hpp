@@ -40,6 +40,9 @@ enum {
     DYMOE_K_INT8_UP,
     DYMOE_K_INT8_DOWN,
     DYMOE_K_INT8_COMBINE,
+    DYMOE_K_MX4_ROWS,
+    DYMOE_K_MX4_PRODUCT,
+    DYMOE_K_ROUTE_BALANCE,
     DYMOE_K_COUNT
 };
 

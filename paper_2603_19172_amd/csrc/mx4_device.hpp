@@ -1,0 +1,81 @@
+// Device functions of the microscaled 4-bit format: numbers of one sign, two exponent and one fraction bit (0, 0.5, 1, 1.5, 2, 3, 4, 6), in
+// blocks of 32 with a common power of two in a byte (2^(byte - 127); 255: no number).
+#pragma once
+#include "int8_device.hpp"
+
+namespace dymoe {
+
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+
+// The exponent byte of a block whose largest magnitude has the fp32 pattern `a`: floor(log2 a) - 2 = (a >> 23) - 127 - 2, so that the largest
+// value lies in [4, 8) times the power of two; at least 2^-127 (subnormal peaks and blocks of zeros), 255 for infinity and NaN.
+__device__ __forceinline__ uint32_t mx4_exponent(uint32_t a)
+{
+    const int e = (int)(a >> 23);
+    return e == 255 ? 255u : (uint32_t)max(e - 2, 0);
+}
+
+// The power of two as the conversion instructions take it (their scale; 2^-127 is a subnormal fp32)
+__device__ __forceinline__ float mx4_unit(uint32_t byte) { return __uint_as_float(byte == 0 ? 0x00400000u : byte << 23); }
+
+// Codes of eight values, the first in the lowest four bits: x / unit to the nearest, ties to even, magnitudes beyond 6 to 6, with x's
+// sign.  The conversion instructions round so for every input; of a block that is no number all codes are 0.
+template <int DT>
+__device__ __forceinline__ uint32_t mx4_codes8(const Raw8<DT>& v, uint32_t byte)
+{
+    const float unit = mx4_unit(byte);
+    uint32_t q = 0;
+    if constexpr (DT == DYMOE_OUT_F32) {
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, __uint_as_float(v.a.x), __uint_as_float(v.a.y), unit, 0);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, __uint_as_float(v.a.z), __uint_as_float(v.a.w), unit, 1);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, __uint_as_float(v.b.x), __uint_as_float(v.b.y), unit, 2);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, __uint_as_float(v.b.z), __uint_as_float(v.b.w), unit, 3);
+    } else if constexpr (DT == DYMOE_OUT_F16) {
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(q, __builtin_bit_cast(half2_t, v.a.x), unit, 0);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(q, __builtin_bit_cast(half2_t, v.a.y), unit, 1);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(q, __builtin_bit_cast(half2_t, v.a.z), unit, 2);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(q, __builtin_bit_cast(half2_t, v.a.w), unit, 3);
+    } else {
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(bf16x2_t, v.a.x), unit, 0);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(bf16x2_t, v.a.y), unit, 1);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(bf16x2_t, v.a.z), unit, 2);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(q, __builtin_bit_cast(bf16x2_t, v.a.w), unit, 3);
+    }
+    return byte == 255u ? 0u : q;
+}
+
+// The largest of four neighbouring lanes'
+__device__ __forceinline__ uint32_t quad_max_u32(uint32_t v)
+{
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true));
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true));
+}
+
+// fp32 pattern of the magnitude that peak8 found
+template <int DT>
+__device__ __forceinline__ uint32_t peak_f32_bits(uint32_t m) { return __float_as_uint(peak_value<DT>(peak_bits<DT>(m))); }
+
+// byte of a tile-layout matrix that holds code (row, col), col a multiple of 2; and that of the exponent of the block of (row, col)
+__device__ __forceinline__ long mx4_tile_byte(long row, long col, long Kp)
+{
+    const long tile = (row >> 5) * (Kp >> 8) + (col >> 8);
+    const int in = (int)(col & 255);
+    return tile * 4096 + ((in & 127) >> 5) * 1024 + ((in >> 7) * 32 + (row & 31)) * 16 + (in & 31) / 2;
+}
+__device__ __forceinline__ long mx4_tile_exponent(long row, long col, long Kp)
+{
+    const long tile = (row >> 5) * (Kp >> 8) + (col >> 8);
+    const int in = (int)(col & 255);
+    return tile * 256 + ((in >> 7) * 32 + (row & 31)) * 4 + ((in & 127) >> 5);
+}
+
+// v_mfma_scale_f32_32x32x64_f8f6f4 on 4-bit numbers: lane l holds 32 numbers of row l % 32 of either operand and, in byte A or B of a
+// register, their exponent.  A block's products and their sum are exact; the sum and the accumulator are added in fp32.
+template <int A, int B>
+__device__ __forceinline__ float16_t mfma_mx4(const uint4 a, const uint4 b, const float16_t c, uint32_t sa, uint32_t sb)
+{
+    const i32x8_t x = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0}, y = {(int)b.x, (int)b.y, (int)b.z, (int)b.w, 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, A, (int)sa, B, (int)sb);
+}
+
+}  // namespace dymoe

@@ -1,0 +1,61 @@
+// Workspace layouts of the products in microscaled 4-bit floating point (host side).
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+#include "expert_plan.hpp"
+
+namespace dymoe {
+
+constexpr int kMx4TileCols = 256;     // columns of a tile of the weights: four matrix instructions
+constexpr int kMx4SmallRows = 32;     // token rows of a tile where experts meet few tokens: one fragment
+constexpr int kMx4TallRows = 128;     // and where they meet many
+
+static inline size_t mx4_round(size_t v, size_t m) { return (v + m - 1) / m * m; }
+
+struct Mx4FfnLayout {
+    size_t Hp, Fp;     // columns of the codes' rows: whole tiles
+    size_t xq, xs;     // [T, Hp / 2] codes and [T, Hp / 32] exponents of the activations
+    size_t hq, hs;     // [P, Fp / 2] and [P, Fp / 32] of the SwiGLU intermediate, by position (pairs sorted by expert)
+    size_t part;       // [P, H up to a multiple of 8] outputs of the pairs, by position, fp32
+    size_t plan;       // int32, see ExpertPlan
+    size_t total;
+    int max_tiles;
+};
+
+static inline Mx4FfnLayout mx4_ffn_layout(long T, long H, long F, long E, long k)
+{
+    Mx4FfnLayout L;
+    const size_t P = (size_t)T * (size_t)k;
+    L.Hp = mx4_round((size_t)H, kMx4TileCols);
+    L.Fp = mx4_round((size_t)F, kMx4TileCols);
+    L.max_tiles = (int)(P / kMx4SmallRows + ((size_t)E < P ? (size_t)E : P));
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t here = at; at += mx4_round(bytes, 256); return here; };
+    L.xq = take((size_t)T * L.Hp / 2);
+    L.xs = take((size_t)T * L.Hp / 32);
+    L.hq = take(P * L.Fp / 2);
+    L.hs = take(P * L.Fp / 32);
+    L.part = take(P * mx4_round((size_t)H, 8) * 4);
+    L.plan = take(expert_plan_bytes(P, (size_t)L.max_tiles));
+    L.total = at;
+    return L;
+}
+
+struct Mx4MatLayout {
+    size_t Kp;
+    size_t xq, xs;     // [T, Kp / 2] codes and [T, Kp / 32] exponents of the activations
+    size_t total;
+};
+
+static inline Mx4MatLayout mx4_mat_layout(long T, long K)
+{
+    Mx4MatLayout L;
+    L.Kp = mx4_round((size_t)K, kMx4TileCols);
+    L.xq = 0;
+    L.xs = mx4_round((size_t)T * L.Kp / 2, 256);
+    L.total = L.xs + mx4_round((size_t)T * L.Kp / 32, 256);
+    return L;
+}
+
+}  // namespace dymoe

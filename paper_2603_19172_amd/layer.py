@@ -241,3 +241,61 @@ class Int8MoELayer:
             logits = self.ctx.matmul_int8(x, router, y=self.logits, workspace=self.ws_router, stream=stream)
         self.ctx.route_scored(logits, self.k, bias=bias, idx=self.idx, w=self.gate, scores=self.scores, stream=stream, **self.routing)
         return self.ctx.moe_ffn_int8(x, self.idx, self.gate, experts.table, self.F, y=self.y, workspace=self.ws, stream=stream)
+
+
+class Mx4Experts:
+    """A layer's experts in microscaled 4-bit floating point: converted and laid out once from bf16 (or fp16, fp32) matrices, with the
+    dymoe_expert_mx4 table that points at them.  An expert given as None has no entry: its tokens' pairs are left out."""
+
+    def __init__(self, ctx, w, device):
+        # w: list over experts of [W1 [F,H], W3 [F,H], W2 [H,F]] tensors on `device`
+        sizes = {tuple(ex[0].shape) for ex in w if ex is not None}
+        if len(sizes) != 1:
+            raise ValueError("the experts of a layer have one size")
+        (self.F, self.H), self.E = sizes.pop(), len(w)
+        if any([tuple(m.shape) for m in ex] != [(self.F, self.H), (self.F, self.H), (self.H, self.F)] for ex in w if ex is not None):
+            raise ValueError("an expert is W1 [F, H], W3 [F, H], W2 [H, F]")
+        self.mats = [None if ex is None else [ctx.quantize_mx4(m, layout=B.LAYOUT_TILE) for m in ex] for ex in w]
+        self.table = B.make_mx4_table(self.mats, device)
+
+
+class Mx4MoELayer:
+    """A layer whose router scores (dymoe_route_scored) and whose experts are microscaled 4-bit numbers (dymoe_moe_ffn_mx4), every buffer
+    pre-allocated: a step is three library calls on one stream, or two where the caller has the logits.  balance() and backward() are
+    the router's side of a training step: the balance loss of the last step's routing, and its logits' gradient."""
+
+    def __init__(self, ctx, T, H, F, E, k, score=B.SCORE_SIGMOID, groups=1, top_groups=1, group_best=1, renorm=True, factor=1.0,
+                 out_dtype=B.OUT_BF16, device="cuda:0"):
+        self.ctx, self.T, self.H, self.F, self.E, self.k = ctx, T, H, F, E, k
+        self.routing = dict(score=score, groups=groups, top_groups=top_groups, group_best=group_best, renorm=renorm, factor=factor)
+        self.logits = torch.empty((T, E), dtype=torch.float32, device=device)
+        self.scores = torch.empty((T, E), dtype=torch.float32, device=device)
+        self.idx = torch.empty((T, k), dtype=torch.int32, device=device)
+        self.gate = torch.empty((T, k), dtype=torch.float32, device=device)
+        self.y = torch.empty((T, H), dtype=B._TORCH_OUT[out_dtype], device=device)
+        self.counts = torch.empty((E + 1,), dtype=torch.int32, device=device)
+        self.mean = torch.empty((E,), dtype=torch.float32, device=device)
+        self.loss = torch.empty((1,), dtype=torch.float32, device=device)
+        self.ws_router = torch.empty((B.matmul_mx4_workspace_bytes(T, E, H),), dtype=torch.uint8, device=device)
+        self.ws_balance = torch.empty((B.route_balance_workspace_bytes(T, E),), dtype=torch.uint8, device=device)
+        self.ws = torch.empty((B.moe_ffn_mx4_workspace_bytes(T, H, F, E, k),), dtype=torch.uint8, device=device)
+
+    def step(self, x, experts, router=None, logits=None, bias=None, stream=None):
+        """router: the [E, H] router as an Mx4Matrix in the tile layout; or logits [T, E] that the caller has."""
+        if (experts.E, experts.H, experts.F) != (self.E, self.H, self.F):
+            raise ValueError("the layer is made for other experts")
+        if logits is None:
+            logits = self.ctx.matmul_mx4(x, router, y=self.logits, workspace=self.ws_router, stream=stream)
+        self.ctx.route_scored(logits, self.k, bias=bias, idx=self.idx, w=self.gate, scores=self.scores, stream=stream, **self.routing)
+        return self.ctx.moe_ffn_mx4(x, self.idx, self.gate, experts.table, self.F, y=self.y, workspace=self.ws, stream=stream)
+
+    def balance(self, logits, coef, keep=None, stream=None):
+        """(counts [E + 1], mean [E], loss [1]) of the last step's choices under these logits."""
+        return self.ctx.route_balance(logits, self.idx, coef, score=self.routing["score"], keep=keep, counts=self.counts, mean=self.mean,
+                                      loss=self.loss, workspace=self.ws_balance, stream=stream)
+
+    def backward(self, logits, dw, coef=0.0, dloss=None, keep=None, out=None, stream=None):
+        """The logits' gradient of the last step's weights (dw [T, k]) and, with coef, of the last balance()'s loss."""
+        return self.ctx.route_scored_backward(logits, self.idx, dw=dw, score=self.routing["score"], renorm=self.routing["renorm"],
+                                              factor=self.routing["factor"], counts=self.counts if coef else None, coef=coef, dloss=dloss,
+                                              keep=keep, out=out, stream=stream)

@@ -1,0 +1,460 @@
+"""GPU parity of the microscaled 4-bit operators against their oracle (64 bits).
+
+Tolerances, from the formulas:
+* codes and exponents are equal; the values they stand for are too, rounded once to the output's type.
+* matmul: mx4_oracle.matmul's bound on an fp32 sum of the blocks; the bias's addition rounds once, 2^-24; the output's type adds half a step:
+  2^-8 (bf16), 2^-11 (fp16), 2^-24 (fp32) of the result, below 2^-14 half of 2^-24 for fp16.
+* moe_ffn: mx4_oracle.moe_ffn's bound, and the output's type.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import mx4_oracle as Q
+from paper_2603_19172_amd import binding as B
+from paper_2603_19172_amd.layer import Mx4Experts, Mx4MoELayer
+from gpu_helpers import DEV
+
+pytestmark = pytest.mark.gpu
+
+HALF = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11, torch.float32: 2.0 ** -24}
+OUT = {torch.bfloat16: B.OUT_BF16, torch.float16: B.OUT_F16, torch.float32: B.OUT_F32}
+LAYOUTS = [B.LAYOUT_ROWMAJOR, B.LAYOUT_TILE]
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = B.Context(0)
+    yield c
+    c.close()
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def randn(seed, *shape, dtype=torch.bfloat16, std=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g) * std).to(dtype).to(DEV)
+
+
+def same_bytes(m, x):
+    """m's codes and exponents are the oracle's for x."""
+    codes, byte = Q.quantize(f64(x))
+    q, s = Q.tiles(codes, byte) if m.layout == B.LAYOUT_TILE else (Q.packed(codes), byte)
+    assert np.array_equal(m.scale.cpu().numpy(), s)
+    assert np.array_equal(m.codes.cpu().numpy(), q)
+    return Q.values(codes, byte)[:, :x.shape[1]]
+
+
+# ------------------------------------------------------------------------------------------------------------------ rows
+
+def row_inputs(seed, rows, K, dtype):
+    x = randn(seed, rows, K, dtype=torch.float32)
+    if rows > 1:
+        x[1] = 0
+        x[1, ::3] = -0.0
+    if rows > 2:
+        x[2] *= 2.0 ** -20
+    if rows > 4:
+        x[3, K // 2] = math.inf
+        x[4, 0] = math.nan
+        x[4, K - 1] = -math.inf
+    if rows > 6:
+        x[5] = (torch.arange(K) % 63 - 31).to(DEV) / 4.0              # every number, every tie, everything beyond 6
+        x[6] = torch.arange(K).to(DEV) % 2 * 2.0 - 1.0
+    return x.to(dtype)
+
+
+@pytest.mark.parametrize("rows,K", [(1, 1), (7, 3), (5, 31), (33, 32), (8, 33), (9, 255), (32, 256), (7, 257), (70, 1000), (11, 4096), (31, 513),
+                                    (3, 14336), (2, 16390), (1, 131072), (64, 100), (1030, 520)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+def test_rows_there_and_back(ctx, rows, K, dtype):
+    x = row_inputs(rows + K, rows, K, dtype)
+    for layout in LAYOUTS:
+        m = ctx.quantize_mx4(x, layout=layout)
+        v = same_bytes(m, x)
+        for out in OUT:
+            y = ctx.dequantize_mx4(m, out_dtype=OUT[out])
+            want = torch.from_numpy(v).to(out)
+            assert y.dtype == out and torch.equal(torch.nan_to_num(y.cpu(), nan=12345.0), torch.nan_to_num(want, nan=12345.0))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_rows_of_every_value_of_the_type(ctx, dtype):
+    """Every finite value, in blocks with largest values from the range's two ends and its middle."""
+    bits = torch.arange(-(1 << 15), 1 << 15, dtype=torch.int32).to(torch.int16).view(dtype)
+    v = bits[torch.isfinite(bits)]
+    fi = torch.finfo(dtype)
+    rows = []
+    for peak in (fi.max, 1.0, 1.9921875, fi.tiny, fi.smallest_normal * 3, float(v[v > 0].min()), float(v[v > 0].min()) * 5):
+        p = torch.tensor(peak).to(dtype)
+        r = torch.where(v.abs().float() <= p.float(), v, torch.zeros((), dtype=dtype))
+        r[::32] = p
+        rows.append(r)
+    x = torch.stack(rows).to(DEV)
+    same_bytes(ctx.quantize_mx4(x), x)
+    y = ctx.dequantize_mx4(ctx.quantize_mx4(x), out_dtype=B.OUT_F32)
+    assert np.array_equal(f64(y), Q.values(*Q.quantize(f64(x)))[:, :x.shape[1]])
+
+
+def test_rows_of_32_bits_of_every_size(ctx):
+    g = torch.Generator().manual_seed(3)
+    x = torch.randint(-(1 << 31), (1 << 31) - 1, (300, 512), generator=g, dtype=torch.int64).to(torch.int32).view(torch.float32)
+    x = torch.where(torch.isfinite(x), x, torch.zeros(()))
+    near = torch.ldexp(torch.randn((100, 512), generator=g), torch.randint(-150, 120, (100, 1), generator=g))
+    x = torch.cat([x, near, near * 2.0 ** -100]).to(DEV)
+    same_bytes(ctx.quantize_mx4(x), x)
+    same_bytes(ctx.quantize_mx4(x, layout=B.LAYOUT_TILE), x)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("K,pitch,off", [(100, 101, 1), (257, 300, 3), (1024, 1031, 5), (64, 64, 1)])
+def test_rows_apart_and_unaligned(ctx, K, pitch, off, dtype):
+    rows = 6
+    flat = randn(K, rows * pitch + off, dtype=dtype)
+    x = flat[off:off + rows * pitch].view(rows, pitch)[:, :K]
+    codes, scale = B.mx4_shapes(rows + 2, K, B.LAYOUT_ROWMAJOR)
+    out = (torch.full(codes, 55, dtype=torch.uint8, device=DEV), torch.full(scale, 5, dtype=torch.uint8, device=DEV))
+    m = ctx.quantize_mx4(x, out=(out[0][:rows], out[1][:rows]))
+    v = same_bytes(m, x)
+    assert (out[0][rows:] == 55).all() and (out[1][rows:] == 5).all()
+    back = torch.full((rows * pitch + off + 9,), 7.0, dtype=dtype, device=DEV)
+    y = back[off:off + rows * pitch].view(rows, pitch)[:, :K]
+    ctx.dequantize_mx4(m, out=y)
+    assert np.array_equal(f64(y), v)
+    rest = back.clone()
+    rest[off:off + rows * pitch].view(rows, pitch)[:, :K] = 7.0
+    assert (rest == 7).all()
+
+
+def test_rows_of_more_than_one_launch(ctx):
+    rows, K = (1 << 25) + 45, 17
+    x = randn(8, 4096, K).repeat(-(-rows // 4096), 1)[:rows].contiguous()
+    x[-5:] *= 3.0
+    m = ctx.quantize_mx4(x)
+    y = ctx.dequantize_mx4(m)
+    cut = (1 << 25) - 64                             # both sides of the launches' border
+    assert np.array_equal(f64(y[cut:]), Q.values(*Q.quantize(f64(x[cut:])))[:, :K])
+    assert torch.equal(y[:4096], y[cut - cut % 4096 - 4096:cut - cut % 4096])
+
+
+# ------------------------------------------------------------------------------------------------------------------ product
+
+def weight(ctx, seed, N, K, std=0.05):
+    w = randn(seed, N, K, std=std)
+    return ctx.quantize_mx4(w, layout=B.LAYOUT_TILE), Q.values(*Q.quantize(f64(w)))[:, :K]
+
+
+def close(y, ref, bound, dtype):
+    assert y.dtype == dtype
+    tiny = 2.0 ** -25 if dtype == torch.float16 else 2.0 ** -133
+    off = np.abs(f64(y) - ref) - (bound * (1 + HALF[dtype]) + HALF[dtype] * np.abs(ref) + tiny)
+    assert (off <= 0).all(), off.max()
+
+
+SIZES = [(1, 1, 1), (1, 64, 128), (1, 4096, 4096), (1, 100, 14336), (2, 33, 129), (3, 200, 1000), (5, 31, 300), (8, 512, 640), (16, 1000, 257),
+         (17, 96, 2048), (31, 65, 77), (32, 64, 4224), (33, 160, 384), (61, 1536, 2048), (64, 520, 128), (65, 130, 1100), (127, 300, 640),
+         (128, 256, 256), (129, 257, 1408), (200, 1030, 520), (256, 512, 1024), (300, 700, 2000), (513, 770, 900), (1030, 300, 450)]
+
+
+@pytest.mark.parametrize("T,N,K", SIZES)
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32, torch.float16])
+def test_matmul_matches_the_oracle(ctx, T, N, K, out):
+    wt, wv = weight(ctx, N, N, K)
+    x = randn(T + K, T, K, dtype=out)
+    bias = randn(7, N, dtype=torch.float32)
+    prod, bound = Q.matmul(Q.values(*Q.quantize(f64(x)))[:, :K], wv)
+    for b in (None, bias):
+        y = ctx.matmul_mx4(x, wt, bias=b, out_dtype=OUT[out])
+        ref = prod if b is None else prod + f64(b)
+        close(y, ref, bound + 2.0 ** -24 * np.abs(ref), out)
+        # codes made beforehand give the same bits
+        assert torch.equal(y, ctx.matmul_mx4(ctx.quantize_mx4(x), wt, bias=b, out_dtype=OUT[out]))
+
+
+@pytest.mark.parametrize("T,N,K", [(1, 100, 300), (5, 100, 300), (40, 77, 200), (140, 300, 260), (300, 290, 500)])
+def test_matmul_strided_rows_and_what_lies_between(ctx, T, N, K):
+    wt, wv = weight(ctx, N, N, K)
+    flat = randn(T, T * (K + 5) + 3)
+    x = flat[3:].view(T, K + 5)[:, :K]
+    prod, bound = Q.matmul(Q.values(*Q.quantize(f64(x)))[:, :K], wv)
+    for out, gap in ((torch.bfloat16, 3), (torch.bfloat16, 8), (torch.float32, 1), (torch.float16, 7)):
+        y = torch.full((T + 2, N + gap), 77.0, dtype=out, device=DEV)
+        ctx.matmul_mx4(x, wt, y=y[:T, :N])
+        close(y[:T, :N], prod, bound, out)
+        assert (y[T:] == 77).all() and (y[:, N:] == 77).all()
+
+
+@pytest.mark.parametrize("T", [1, 4, 16, 20, 64, 130, 260])
+def test_matmul_row_that_is_no_number_stays_alone(ctx, T):
+    wt, _ = weight(ctx, 3, 300, 500)
+    x = randn(T, T, 500)
+    clean = ctx.matmul_mx4(x, wt)
+    x2 = x.clone()
+    x2[T // 2, 7] = math.nan
+    x2[T - 1, 499] = math.inf
+    y = ctx.matmul_mx4(x2, wt)
+    hit = torch.zeros(T, dtype=torch.bool, device=DEV)
+    hit[[T // 2, T - 1]] = True
+    assert torch.isnan(y[hit]).all() and torch.equal(y[~hit], clean[~hit])
+
+
+@pytest.mark.parametrize("T", [2, 70, 200])
+def test_matmul_channel_that_is_no_number_stays_alone(ctx, T):
+    w, x = randn(4, 90, 700, std=0.05), randn(5, T, 700)
+    clean = ctx.matmul_mx4(x, ctx.quantize_mx4(w, layout=B.LAYOUT_TILE))
+    w[[0, 33, 89], [1, 600, 699]] = torch.tensor([math.nan, math.inf, -math.inf], dtype=w.dtype, device=DEV)
+    y = ctx.matmul_mx4(x, ctx.quantize_mx4(w, layout=B.LAYOUT_TILE))
+    bad = torch.zeros(90, dtype=torch.bool, device=DEV)
+    bad[[0, 33, 89]] = True
+    assert torch.isnan(y[:, bad]).all() and torch.equal(y[:, ~bad], clean[:, ~bad])
+
+
+@pytest.mark.parametrize("T", [1, 40, 300])
+@pytest.mark.parametrize("low,high", [(2.0 ** -120, 2.0 ** 100), (2.0 ** 60, 2.0 ** 60), (2.0 ** -60, 2.0 ** -50)])
+def test_matmul_scales_far_apart(ctx, T, low, high):
+    """Blocks and channels at the ends of the exponents' range."""
+    N, K = 70, 600
+    x, w = randn(6, T, K, dtype=torch.float32), randn(7, N, K, dtype=torch.float32)
+    x[:, 32:64] *= low
+    x[:, 300:] *= low ** 0.5
+    w[::3] *= high
+    w[:, 32:64] *= 0.01
+    wt = ctx.quantize_mx4(w, layout=B.LAYOUT_TILE)
+    prod, bound = Q.matmul(Q.values(*Q.quantize(f64(x)))[:, :K], Q.values(*Q.quantize(f64(w)))[:, :K])
+    y = ctx.matmul_mx4(x, wt, out_dtype=B.OUT_F32)
+    close(y, prod, bound, torch.float32)
+
+
+def test_matmul_sums_that_32_bits_hold_are_exact(ctx):
+    """Blocks of one power of two: the sums are whole numbers of a quarter, and exact in every shape."""
+    for T, N, K in ((1, 130, 3000), (9, 130, 14336), (70, 130, 3000), (300, 300, 2048), (600, 800, 1100)):
+        g = torch.Generator().manual_seed(T)
+        numbers = torch.tensor(Q.NUMBERS, dtype=torch.float32)
+        x, w = (numbers[torch.randint(0, 8, (n, K), generator=g)] * (torch.randint(0, 2, (n, K), generator=g) * 2 - 1) for n in (T, N))
+        x[:, ::32], w[:, ::32] = 6.0, 6.0
+        y = ctx.matmul_mx4(x.to(DEV), ctx.quantize_mx4(w.to(DEV), layout=B.LAYOUT_TILE), out_dtype=B.OUT_F32)
+        assert np.array_equal(f64(y), f64(x) @ f64(w).T)
+
+
+@pytest.mark.parametrize("T", [1, 8, 40, 700])
+def test_matmul_many_outputs(ctx, T):
+    N, K = 33000, 256
+    wt, wv = weight(ctx, 9, N, K)
+    x = randn(9, T, K)
+    prod, bound = Q.matmul(Q.values(*Q.quantize(f64(x)))[:, :K], wv)
+    close(ctx.matmul_mx4(x, wt), prod, bound, torch.bfloat16)
+
+
+@pytest.mark.parametrize("T,N,K", [(1, 4096, 4096), (61, 1536, 2048), (300, 700, 2000), (1100, 2300, 1024)])
+def test_matmul_again_on_another_stream_and_in_a_graph(ctx, T, N, K):
+    wt, _ = weight(ctx, 2, N, K)
+    xs = [randn(s, T, K) for s in range(3)]
+    want = [ctx.matmul_mx4(x, wt) for x in xs]
+    for x, y in zip(xs, want):
+        assert torch.equal(ctx.matmul_mx4(x, wt), y)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = [ctx.matmul_mx4(x, wt, stream=side) for x in xs]
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    x, y = xs[0].clone(), torch.empty_like(want[0])
+    ws = torch.empty((B.matmul_mx4_workspace_bytes(T, N, K),), dtype=torch.uint8, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.matmul_mx4(x, wt, y=y, workspace=ws)
+    for src, ref in zip(xs, want):
+        x.copy_(src)
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, ref)
+
+
+# ------------------------------------------------------------------------------------------------------------------ experts
+
+def make_experts(ctx, seed, E, H, F, std=0.05, missing=()):
+    mats = [None if e in missing else [randn(seed + 3 * e + i, n, m, std=std) for i, (n, m) in enumerate(((F, H), (F, H), (H, F)))] for e in range(E)]
+    ex = Mx4Experts(ctx, mats, DEV)
+    vals = [None if m is None else [Q.values(*Q.quantize(f64(t)))[:, :t.shape[1]] for t in m] for m in mats]
+    return ex, vals
+
+
+def choices(seed, T, E, k, popular=0.0):
+    g = torch.Generator().manual_seed(seed)
+    top = (torch.randn((T, E), generator=g) - popular * torch.log(torch.arange(E) + 1.0)).softmax(-1).topk(k, dim=-1)
+    return top.indices.to(torch.int32).to(DEV), (top.values / top.values.sum(-1, keepdim=True)).float().to(DEV)
+
+
+def check_ffn(ctx, x, idx, gate, ex, vals, out=torch.bfloat16, **kw):
+    y = ctx.moe_ffn_mx4(x, idx, gate, ex.table, ex.F, out_dtype=OUT[out], **kw)
+    ref, bound = Q.moe_ffn(Q.values(*Q.quantize(f64(x)))[:, :x.shape[1]], idx.cpu().numpy(), f64(gate), vals)
+    close(y, ref, bound, out)
+    return y, ref
+
+
+FFN_SIZES = [(1, 8, 8, 1, 1), (1, 256, 512, 8, 2), (1, 2048, 768, 16, 8), (2, 100, 70, 5, 3), (3, 264, 1032, 8, 8), (7, 512, 300, 60, 4), (32, 384, 256, 8, 2),
+             (33, 128, 96, 4, 1), (61, 640, 768, 24, 8), (130, 256, 512, 3, 2), (300, 520, 264, 8, 2), (257, 256, 160, 40, 6), (700, 300, 520, 4, 2)]
+
+
+@pytest.mark.parametrize("T,H,F,E,k", FFN_SIZES)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+def test_experts_match_the_oracle(ctx, T, H, F, E, k, dtype):
+    ex, vals = make_experts(ctx, T, E, H, F)
+    idx, gate = choices(T + E, T, E, k)
+    check_ffn(ctx, randn(T + H, T, H, dtype=dtype), idx, gate, ex, vals, out=dtype)
+
+
+@pytest.mark.parametrize("T", [1, 3, 24, 90, 400])
+def test_experts_with_skewed_loads(ctx, T):
+    ex, vals = make_experts(ctx, 5, 30, 256, 288)
+    idx, gate = choices(T, T, 30, 5, popular=2.0)
+    check_ffn(ctx, randn(T, T, 256), idx, gate, ex, vals)
+
+
+@pytest.mark.parametrize("T", [1, 2, 6, 40, 300])
+def test_experts_left_out(ctx, T):
+    """Indices outside the table, experts without an entry, one expert in several slots, weights of 0."""
+    E, H, F, k = 6, 256, 160, 4
+    ex, vals = make_experts(ctx, 7, E, H, F, missing=(2,))
+    idx, gate = choices(T, T, E, k)
+    idx[0] = torch.tensor([5, -1, 5, 5], dtype=torch.int32)
+    if T > 2:
+        idx[1] = torch.tensor([-1, 6, 1 << 30, -(1 << 31)], dtype=torch.int32)
+        idx[2] = 2
+        gate[T - 1] = 0.0
+    ctx.device_flags()
+    y, ref = check_ffn(ctx, randn(T, T, H), idx, gate, ex, vals)
+    met = bool((idx == 2).any())
+    assert ctx.device_flags() == (B.FLAG_FORMAT_MISSING if met else 0) and ctx.device_flags() == 0
+    if T > 2:
+        assert (y[1] == 0).all() and (y[2] == 0).all() and (y[T - 1] == 0).all()
+
+
+@pytest.mark.parametrize("T", [1, 2, 5, 60, 500])
+def test_experts_token_that_is_no_number_stays_alone(ctx, T):
+    ex, _ = make_experts(ctx, 8, 5, 256, 200)
+    idx, gate = choices(T, T, 5, 2)
+    x = randn(T, T, 256)
+    clean = ctx.moe_ffn_mx4(x, idx, gate, ex.table, ex.F)
+    x2 = x.clone()
+    x2[T // 2, 255] = math.nan
+    y = ctx.moe_ffn_mx4(x2, idx, gate, ex.table, ex.F)
+    hit = torch.arange(T, device=DEV) == T // 2
+    assert torch.isnan(y[hit]).all() and torch.equal(y[~hit], clean[~hit])
+
+
+@pytest.mark.parametrize("T", [1, 30, 400])
+def test_experts_whose_intermediate_leaves_the_range(ctx, T):
+    """silu(a) u beyond fp32: infinite in its block, so that pair is no number; others' outputs are."""
+    H, F = 64, 64
+    w = [torch.zeros((F, H), device=DEV), torch.zeros((F, H), device=DEV), torch.zeros((H, F), device=DEV)]
+    w[0][0, 0], w[1][0, 0], w[2][3, 0] = 2.0 ** 100, 2.0 ** 100, 1.0
+    ex = Mx4Experts(ctx, [w], DEV)
+    x = torch.zeros((T, H), device=DEV)
+    x[:, 0] = 1.0
+    x[0, 0] = 0.0
+    y = ctx.moe_ffn_mx4(x, torch.zeros((T, 1), dtype=torch.int32, device=DEV), torch.ones((T, 1), device=DEV), ex.table, F, out_dtype=B.OUT_F32)
+    assert (y[0] == 0).all() and torch.isnan(y[1:]).all()
+
+
+def test_experts_intermediate_is_silu_to_32_bits(ctx):
+    """One feature at a time: what stands behind the conversion is silu(a) u, over the sigmoid's whole range."""
+    H, F = 32, 32
+    a = torch.cat([torch.linspace(-100, 100, 401), torch.tensor([1e-30, -1e-30, 0.0])]).to(DEV)
+    T = a.numel()
+    w1, w3, w2 = (torch.zeros(s, device=DEV) for s in ((F, H), (F, H), (H, F)))
+    w1[0, 0], w3[0, 1], w2[0, 0] = 1.0, 1.0, 1.0
+    x = torch.zeros((T, H), dtype=torch.float32, device=DEV)
+    x[:, 0], x[:, 1] = a, 1.0
+    ex = Mx4Experts(ctx, [[w1, w3, w2]], DEV)
+    vals = [[f64(w) for w in (w1, w3, w2)]]
+    check_ffn(ctx, x, torch.zeros((T, 1), dtype=torch.int32, device=DEV), torch.ones((T, 1), device=DEV), ex, vals, out=torch.float32)
+
+
+def test_experts_no_tokens(ctx):
+    ex, _ = make_experts(ctx, 1, 2, 64, 64)
+    y = ctx.moe_ffn_mx4(randn(1, 0, 64), torch.empty((0, 1), dtype=torch.int32, device=DEV), torch.empty((0, 1), device=DEV), ex.table, 64)
+    assert y.shape == (0, 64)
+
+
+@pytest.mark.parametrize("T", [1, 2, 5, 70, 400])
+def test_experts_again_with_any_workspace_another_stream_and_in_a_graph(ctx, T):
+    E, H, F, k = 7, 320, 416, 3
+    ex, _ = make_experts(ctx, 9, E, H, F)
+    sets = [(randn(s, T, H), *choices(s, T, E, k)) for s in range(3)]
+    want = [ctx.moe_ffn_mx4(*s, ex.table, F) for s in sets]
+    nb = B.moe_ffn_mx4_workspace_bytes(T, H, F, E, k)
+    for fill in (0, 255, 127):
+        buf = torch.full((nb + 512,), fill, dtype=torch.uint8, device=DEV)
+        y = torch.full((T + 1, H), 3.0, dtype=torch.bfloat16, device=DEV)
+        ctx.moe_ffn_mx4(*sets[1], ex.table, F, y=y[:T], workspace=buf[:nb])
+        assert torch.equal(y[:T], want[1]) and (y[T:] == 3).all() and (buf[nb:] == fill).all()
+    with pytest.raises(B.DymoeError) as err:
+        ctx.moe_ffn_mx4(*sets[1], ex.table, F, workspace=buf[:nb - 256])
+    assert err.value.code == B.ENOSPC
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = [ctx.moe_ffn_mx4(*s, ex.table, F, stream=side) for s in sets]
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    static = [t.clone() for t in sets[0]]
+    y, ws = torch.empty_like(want[0]), torch.empty((nb,), dtype=torch.uint8, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.moe_ffn_mx4(*static, ex.table, F, y=y, workspace=ws)
+    for s, ref in zip(sets, want):
+        for a, b in zip(static, s):
+            a.copy_(b)
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, ref)
+
+
+def test_two_graphs_that_share_a_workspace(ctx):
+    T, E, H, F, k = 40, 6, 256, 256, 2
+    ex, _ = make_experts(ctx, 11, E, H, F)
+    sets = [(randn(s, T, H), *choices(s, T, E, k)) for s in range(2)]
+    want = [ctx.moe_ffn_mx4(*s, ex.table, F) for s in sets]
+    ws = torch.empty((B.moe_ffn_mx4_workspace_bytes(T, H, F, E, k),), dtype=torch.uint8, device=DEV)
+    out = [torch.empty_like(w) for w in want]
+    graphs = []
+    for s, y in zip(sets, out):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            ctx.moe_ffn_mx4(*s, ex.table, F, y=y, workspace=ws)
+    for _ in range(3):
+        for gph in graphs:
+            gph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+        for y in out:
+            y.zero_()
+
+
+def test_layer_runs_router_experts_balance_and_gradient_together(ctx):
+    T, H, F, E, k = 50, 384, 256, 16, 4
+    ex, vals = make_experts(ctx, 12, E, H, F)
+    x, router = randn(13, T, H), ctx.quantize_mx4(randn(14, E, H, std=0.05), layout=B.LAYOUT_TILE)
+    bias = randn(15, E, dtype=torch.float32, std=0.05)
+    layer = Mx4MoELayer(ctx, T, H, F, E, k, groups=4, top_groups=2, group_best=2, factor=1.5)
+    y = layer.step(x, ex, router=router, bias=bias)
+    logits = ctx.matmul_mx4(x, router, out_dtype=B.OUT_F32)
+    assert torch.equal(logits, layer.logits)
+    idx, w = ctx.route_scored(logits, k, bias=bias, groups=4, top_groups=2, group_best=2, factor=1.5)
+    assert torch.equal(idx, layer.idx) and torch.equal(w, layer.gate)
+    ref, bound = Q.moe_ffn(Q.values(*Q.quantize(f64(x)))[:, :H], idx.cpu().numpy(), f64(w), vals)
+    close(y, ref, bound, torch.bfloat16)
+    keep = (torch.arange(T, device=DEV) % 5 != 0).to(torch.uint8)
+    counts, mean, loss = layer.balance(logits, 0.02, keep=keep)
+    c, m, l = Q.balance(f64(logits), idx.cpu().numpy(), 0.02, True, keep.cpu().numpy())
+    assert np.array_equal(counts.cpu().numpy(), c) and np.allclose(f64(mean), m, rtol=1e-5) and abs(float(loss) - l) <= 1e-5 * abs(l)
+    dw = randn(16, T, k, dtype=torch.float32)
+    grad = layer.backward(logits, dw, coef=0.02, keep=keep)
+    g, size = Q.backward(f64(logits), idx.cpu().numpy(), f64(dw), True, True, 1.5, c, float(np.float32(0.02)), 1.0, keep.cpu().numpy())
+    assert (np.abs(f64(grad) - g) <= 1e-5 * size).all()
+    assert torch.equal(y, layer.step(x, ex, logits=logits, bias=bias))
