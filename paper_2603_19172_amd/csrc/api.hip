@@ -52,6 +52,7 @@ int ffn_device_flags_address(unsigned** out);
 int ffn_gemm_init();
 int route_init();
 int i8_init();
+int mx4_init();
 
 }  // namespace dymoe
 
@@ -112,6 +113,7 @@ int dymoe_create(dymoe_ctx** out, int device)
         if (rc == DYMOE_OK) rc = dymoe::ffn_gemm_init();
         if (rc == DYMOE_OK) rc = dymoe::route_init();
         if (rc == DYMOE_OK) rc = dymoe::i8_init();
+        if (rc == DYMOE_OK) rc = dymoe::mx4_init();
         if (hipSetDevice(prev) != hipSuccess) rc = DYMOE_EHIP;
     }
     if (rc != DYMOE_OK) {

@@ -69,6 +69,15 @@ __device__ __forceinline__ long mx4_tile_exponent(long row, long col, long Kp)
     return tile * 256 + ((in >> 7) * 32 + (row & 31)) * 4 + ((in & 127) >> 5);
 }
 
+// 4 bytes a lane, global memory -> LDS[lds_addr_lane0 + 4 * lane]: lds_copy16's smaller brother
+__device__ __forceinline__ void lds_copy4(const char* base, uint32_t lane_offset, uint32_t lds_addr_lane0)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+                 :
+                 : "s"(lds_addr_lane0), "v"(lane_offset), "s"(base)
+                 : "memory");
+}
+
 // v_mfma_scale_f32_32x32x64_f8f6f4 on 4-bit numbers: lane l holds 32 numbers of row l % 32 of either operand and, in byte A or B of a
 // register, their exponent.  A block's products and their sum are exact; the sum and the accumulator are added in fp32.
 template <int A, int B>
