@@ -98,7 +98,9 @@ __device__ __forceinline__ void make_expert_plan(ExpertPlanLds& lds, const int32
         lds.wave[2][wave] = m1_in;
     }
     __syncthreads();
+    constexpr int kUnroll = WIDE > 0 ? kPlanThreads / kWave : 4;       // (16 without wide tiles: 14 registers to scratch memory)
     int n0 = n_in - n, t2 = m2_in, t1 = m1_in, all2 = 0, all1 = 0;
+#pragma unroll kUnroll
     for (int w = 0; w < kPlanThreads / kWave; w++) {
         const int a2 = lds.wave[1][w], a1 = lds.wave[2][w];
         if (w < wave) {

@@ -1173,15 +1173,6 @@ __global__ __launch_bounds__(256) void i8_combine_kernel(const float* __restrict
     store_out4(y, t * H + h + 4, out_dtype, aligned && h + 8 <= H, H - h - 4, hi);
 }
 
-// (ldp a multiple of 8)
-void experts_combine(dymoe_ctx* ctx, int kernel_id, const float* part, long ldp, const int32_t* where, const float* gate, int T, int H, int k,
-                     int out_dtype, void* y, hipStream_t st)
-{
-    const dim3 grid((unsigned)(T * ((H + 2047L) / 2048)));
-    dymoe_launch(ctx, kernel_id, i8_combine_kernel, grid, dim3(256), 0, st, part, ldp, where, gate, H, k, out_dtype,
-                 H % 4 == 0 && dymoe_aligned(y, 4 * dtype_bytes(out_dtype)), y);
-}
-
 }  // namespace dymoe
 
 using namespace dymoe;
@@ -1384,7 +1375,9 @@ extern "C" int dymoe_moe_ffn_int8(dymoe_ctx* ctx, const void* x, int x_dtype, co
     A.N = H;
     if (small) dymoe_launch(ctx, DYMOE_K_INT8_DOWN, i8_small_kernel<kI8Down, 1, 4, 1>, dim3((unsigned)down), dim3(256), 0, st, A);
     else dymoe_launch(ctx, DYMOE_K_INT8_DOWN, i8_experts_kernel<kI8Down>, down_grid, dim3(256), kI8Lds<2>, st, A);
-    experts_combine(ctx, DYMOE_K_INT8_COMBINE, (const float*)(ws + L.part), (long)L.Hp, i8_plan(plan, P).where, w, T, H, k, out_dtype, y, st);
+    const dim3 grid((unsigned)(T * ((H + 2047L) / 2048)));
+    dymoe_launch(ctx, DYMOE_K_INT8_COMBINE, i8_combine_kernel, grid, dim3(256), 0, st, (const float*)(ws + L.part), (long)L.Hp,
+                 i8_plan(plan, P).where, w, H, k, out_dtype, H % 4 == 0 && dymoe_aligned(y, 4 * dtype_bytes(out_dtype)), y);
     DYMOE_HIP_LAUNCH_CHECK();
     return DYMOE_OK;
 }

@@ -5,13 +5,11 @@
 
 #include "expert_plan.hpp"
 #include "mx4_device.hpp"
-#include "mx4_layout.hpp"
+#include "mx4_rule.hpp"
 
 namespace dymoe {
 
 int mx4_quantize(dymoe_ctx* ctx, const void* x, int dtype, long rows, long K, long ldx, int tiles, uint8_t* codes, uint8_t* scale, hipStream_t st);
-void experts_combine(dymoe_ctx* ctx, int kernel_id, const float* part, long ldp, const int32_t* where, const float* gate, int T, int H, int k,
-                     int out_dtype, void* y, hipStream_t st);
 
 using Mx4Plan = ExpertPlan<dymoe_expert_mx4>;
 
@@ -19,7 +17,7 @@ using Mx4Plan = ExpertPlan<dymoe_expert_mx4>;
 template <int DT>
 __global__ __launch_bounds__(kPlanThreads) void mx4_prep_kernel(const int32_t* __restrict__ idx, const dymoe_expert_mx4* __restrict__ table, long P,
                                                                 int E, int small, int32_t* __restrict__ plan, unsigned* __restrict__ flags,
-                                                                const char* __restrict__ x, long units, int per_row, int K, char* __restrict__ codes,
+                                                                const char* __restrict__ x, int units, int per_row, int K, char* __restrict__ codes,
                                                                 char* __restrict__ scale)
 {
     __shared__ ExpertPlanLds lds;
@@ -27,10 +25,11 @@ __global__ __launch_bounds__(kPlanThreads) void mx4_prep_kernel(const int32_t* _
         make_expert_plan<kMx4SmallRows, 0, kMx4TallRows>(lds, idx, table, P, E, small, plan, flags);
         return;
     }
-    const long unit = (blockIdx.x - 1L) * (kPlanThreads / kWave) + threadIdx.x / kWave;
+    const int unit = (int)(blockIdx.x - 1) * (kPlanThreads / kWave) + threadIdx.x / kWave;
     if (unit >= units) return;
-    const long row = unit / per_row;
-    const int col = (int)(unit - row * per_row) * 512 + (threadIdx.x & (kWave - 1)) * 8, Kp = (int)up_to(K, 256);
+    const int part = unit / per_row, col0 = (unit - part * per_row) * 512;
+    const long row = part;
+    const int col = col0 + (threadIdx.x & (kWave - 1)) * 8, Kp = (int)up_to(K, 256);
     const Raw8<DT> v = load8<DT>(x + row * K * dtype_bytes(DT), col, K);
     const uint32_t byte = mx4_exponent(quad_max_u32(peak_f32_bits<DT>(peak8<DT>(v, 0u)))), q = mx4_codes8<DT>(v, byte);
     if (col >= Kp) return;
@@ -41,7 +40,13 @@ __global__ __launch_bounds__(kPlanThreads) void mx4_prep_kernel(const int32_t* _
 enum { kMx4Plain = 0, kMx4Up = 1, kMx4Down = 2 };
 
 struct Mx4Args {
-    const char *x, *xs;               // codes of the rows, Kp / 2 bytes each, and their exponents, Kp / 32
+    const char *x, *xs;               // codes of the rows, Kp / 2 bytes each, and their exponents, Kp / 32; or the rows themselves
+    long ldx;                         // those: bytes from row to row
+    const int32_t* idx;               // and the experts of a few tokens' pairs, their weights and table
+    const float* gate;
+    const dymoe_expert_mx4* table;
+    unsigned* flags;
+    int x_dtype, K, E;
     const int32_t* plan;              // experts
     const char *w, *ws;               // the plain product
     const float* bias;
@@ -49,6 +54,7 @@ struct Mx4Args {
     uint8_t* out_scale;               // up: their exponents, ldo / 32
     long ldo, P;
     int rows, Kp, N, k, out_dtype, aligned;     // aligned: the plain product's rows start where four outputs may be stored at once
+    int splits;                       // tall tiles of the down projection: parts of K, P rows of outputs each
 };
 
 // A strip of 32 weight rows: codes and exponents.  One behind the last of the matrix has no bytes, and is read as zeros.
@@ -67,31 +73,86 @@ __device__ __forceinline__ uint32_t load_u32(const BufferSrc& s, uint32_t lane, 
     return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(s.r, (int)lane, (int)all, 0);
 }
 
+// The codes of `rows` rows into LDS, Kp / 2 + 16 bytes apart, and their exponents behind them, Kp / 32 apart, by a whole workgroup (mx4_fuse_bytes).
+__device__ __forceinline__ int mx4_lds_row(int Kp) { return (Kp >> 1) + 16; }
+
+template <int DT>
+__device__ __forceinline__ void mx4_rows_to_lds(const char* x, long ldx, int rows, int K, int Kp, char* lds)
+{
+    const int per = Kp >> 3, n = rows * per;
+    char* const exps = lds + rows * mx4_lds_row(Kp);
+    // (per is a multiple of 32 and so is the number of threads: four lanes that share a block are in step)
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        const int r = i / per, col = (i - r * per) * 8;
+        const Raw8<DT> v = load8<DT>(x + r * ldx, col, K);
+        const uint32_t byte = mx4_exponent(quad_max_u32(peak_f32_bits<DT>(peak8<DT>(v, 0u))));
+        *(uint32_t*)(lds + r * mx4_lds_row(Kp) + (col >> 1)) = mx4_codes8<DT>(v, byte);
+        if ((col & 31) == 0) exps[r * (Kp >> 5) + (col >> 5)] = (char)byte;
+    }
+    __syncthreads();
+}
+
+__device__ __forceinline__ void mx4_rows_to_lds(int dt, const char* x, long ldx, int rows, int K, int Kp, char* lds)
+{
+    if (dt == DYMOE_OUT_F32) mx4_rows_to_lds<DYMOE_OUT_F32>(x, ldx, rows, K, Kp, lds);
+    else if (dt == DYMOE_OUT_F16) mx4_rows_to_lds<DYMOE_OUT_F16>(x, ldx, rows, K, Kp, lds);
+    else mx4_rows_to_lds<DYMOE_OUT_BF16>(x, ldx, rows, K, Kp, lds);
+}
+
 // ----------------------------------------------------------------------------
-// Tiles of up to 32 NTF rows: a workgroup owns 32 weight rows (of W1 and of W3 in the up projection) and its NW wavefronts take the 256-column
-// tiles of K in turn.  Nothing is shared before the end: weights and codes come straight into registers, D tiles of a wavefront on their
-// way, and the sums meet in LDS.
-template <int MODE, int NTF, int NW, int D>
+// Tiles of up to 32 NTF rows where rows or columns are too few for the tiles below (decode batches, narrow matrices): a stream of weights.  KS
+// wavefronts share a strip of 32 weight rows (of W1 and of W3 in the up projection) and take the 256-column tiles of K in turn; a workgroup of NW
+// has NW / KS strips.  Nothing is shared before the end: weights and codes come straight into registers, D tiles of a wavefront on their
+// way, and the sums of a strip's wavefronts meet in LDS.
+// FUSE: the rows come as they are, few enough for every workgroup to convert them for itself, behind its first loads of weights; the experts' pairs
+// are then looked through by every workgroup too: the one of a pair that comes first among those of its expert (or 32, 64, ... behind
+// the first) takes the next 32 of them, and a pair's position is its number.
+template <int MODE, int NTF, int NW, int KS, int D, bool FUSE = false>
 __global__ __launch_bounds__(64 * NW) void mx4_small_kernel(const Mx4Args A)
 {
-    constexpr int S = MODE == kMx4Up ? 2 : 1, kSums = S * NTF, kRows = 32 * NTF;
-    __shared__ float s_red[4][kSums][16][kWave];
-    __shared__ uint32_t s_peak[NTF][4][32];
+    constexpr int S = MODE == kMx4Up ? 2 : 1, kSums = S * NTF, kRows = 32 * NTF, kStrips = NW / KS;
+    constexpr int kParts = KS > 4 ? 4 : KS;      // wavefronts that finish a strip
+    constexpr int kV = 16 / kParts;              // registers of a fragment that each of them finishes
+    static_assert(NW % KS == 0 && (KS == 8 || KS == 4 || KS == 2 || KS == 1), "");
+    static_assert(!FUSE || (MODE != kMx4Down && NTF == 1), "");
+    extern __shared__ __attribute__((aligned(16))) char s_rows[];
+    __shared__ float s_red[KS > 1 ? kStrips * kParts : 1][kSums][16][kWave];
+    __shared__ uint32_t s_peak[kStrips][NTF][kParts][32];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-    const int ln = lane & 31, kb = lane >> 5;
-    const int strips = (A.N + 31) / 32, nblk = MODE == kMx4Up ? (int)up_to(A.N, 256) / 32 : strips;
+    const int ln = lane & 31, kb = lane >> 5, mine = wave / KS, part = wave - mine * KS;
+    const int strips = (A.N + 31) / 32, all = MODE == kMx4Up ? (int)(A.ldo >> 5) : strips, nblk = (all + kStrips - 1) / kStrips;
     const Mx4Plan pp = expert_plan<dymoe_expert_mx4>(const_cast<int32_t*>(A.plan), A.P);
     int row0, rows, bx;
     Mx4Strip w[S];
     if (MODE == kMx4Plain) {
-        const int tiles = (A.rows + kRows - 1) / kRows;
-        bx = blockIdx.x / tiles;
-        row0 = (blockIdx.x - bx * tiles) * kRows;
+        const int tiles = (A.rows + kRows - 1) / kRows, block = blockIdx.x / tiles;
+        bx = block * kStrips + mine;
+        row0 = (blockIdx.x - block * tiles) * kRows;
         rows = min(kRows, A.rows - row0);
         w[0].set(A.w, A.ws, bx, strips, A.Kp);
+    } else if (FUSE) {
+        const int pair = blockIdx.x / nblk;
+        bx = (blockIdx.x - pair * nblk) * kStrips + mine;
+        const int my_e = lane < A.P ? A.idx[lane] : -1, e = __builtin_amdgcn_readlane(my_e, pair);
+        if ((unsigned)e >= (unsigned)A.E) return;
+        const uint64_t its = __ballot(my_e == e);
+        const int rank = __popcll(its & ((1ull << pair) - 1));
+        if (rank & (kRows - 1)) return;
+        const dymoe_expert_mx4 ex = A.table[e];
+        if (!expert_present(ex)) {
+            if (tid == 0) atomicOr(A.flags, DYMOE_FLAG_FORMAT_MISSING);
+            return;
+        }
+        rows = min(kRows, __popcll(its) - rank);
+        uint64_t left = its >> pair << pair;                 // this tile's pairs and those behind it
+        const int want = min(ln, rows - 1);
+        for (int i = 0; i < want; i++) left &= left - 1;
+        row0 = __builtin_ctzll(left);                        // this lane's pair
+        w[0].set(ex.q[0], ex.s[0], bx, strips, A.Kp);
+        w[S - 1].set(ex.q[1], ex.s[1], bx, strips, A.Kp);
     } else {
         const int tile = blockIdx.x / nblk;
-        bx = blockIdx.x - tile * nblk;
+        bx = (blockIdx.x - tile * nblk) * kStrips + mine;
         if (tile >= pp.meta[0]) return;
         const ExpertTile<dymoe_expert_mx4> t = pp.tiles[tile];
         const int i = (tile - t.tile0) * kRows;
@@ -117,6 +178,7 @@ __global__ __launch_bounds__(64 * NW) void mx4_small_kernel(const Mx4Args A)
         }
     };
     auto load_x = [&](Tile& t, int kt) {
+        if (FUSE) return;
 #pragma unroll
         for (int f = 0; f < NTF; f++) {
 #pragma unroll
@@ -125,12 +187,18 @@ __global__ __launch_bounds__(64 * NW) void mx4_small_kernel(const Mx4Args A)
         }
     };
     Tile ring[D];
-    int kt = wave;
+    int kt = part;
 #pragma unroll
     for (int d = 0; d < D; d++)
-        if (kt + d * NW < nkt) load_w(ring[d], kt + d * NW);               // (the weights need nothing of the rows)
+        if (kt + d * KS < nkt) load_w(ring[d], kt + d * KS);               // (the weights need nothing of the rows)
+    if (FUSE) {
+        mx4_rows_to_lds(A.x_dtype, A.x, A.ldx, A.rows, A.K, A.Kp, s_rows);
+        const int row = MODE == kMx4Up ? row0 / A.k : row0 + min(ln, rows - 1);
+        off[0] = (uint32_t)(row * mx4_lds_row(A.Kp)) + 64u * (uint32_t)kb;
+        offs[0] = (uint32_t)(A.rows * mx4_lds_row(A.Kp) + row * (A.Kp >> 5)) + 4u * (uint32_t)kb;
+    }
 #pragma unroll
-    for (int f = 0; f < NTF; f++) {
+    for (int f = 0; f < NTF && !FUSE; f++) {
         const int r = min(32 * f + ln, rows - 1);                            // rows behind the last: computed and dropped
         const uint32_t row = MODE == kMx4Up ? (uint32_t)(pp.perm[row0 + r] / A.k) : (uint32_t)r;
         off[f] = row * (uint32_t)(A.Kp >> 1) + 64u * (uint32_t)kb;
@@ -142,7 +210,7 @@ __global__ __launch_bounds__(64 * NW) void mx4_small_kernel(const Mx4Args A)
     xs.set(A.xs + from * (A.Kp >> 5), held * (uint32_t)(A.Kp >> 5));
 #pragma unroll
     for (int d = 0; d < D; d++)
-        if (kt + d * NW < nkt) load_x(ring[d], kt + d * NW);
+        if (kt + d * KS < nkt) load_x(ring[d], kt + d * KS);
     float16_t acc[S][NTF] = {};
     auto multiply = [&](const Tile& t) {
 #pragma unroll
@@ -159,98 +227,234 @@ __global__ __launch_bounds__(64 * NW) void mx4_small_kernel(const Mx4Args A)
 #pragma unroll
         for (int d = 0; d < D; d++) {
             if (kt < nkt) {
+                if (FUSE) {
+#pragma unroll
+                    for (int c = 0; c < 4; c++) ring[d].x[0][c] = *(const uint4*)(s_rows + off[0] + kt * 128 + c * 16);
+                    ring[d].xs[0] = *(const uint32_t*)(s_rows + offs[0] + kt * 8);
+                }
                 multiply(ring[d]);
                 __builtin_amdgcn_sched_barrier(0);
-                if (kt + D * NW < nkt) {
-                    load_w(ring[d], kt + D * NW);
-                    load_x(ring[d], kt + D * NW);
+                if (kt + D * KS < nkt) {
+                    load_w(ring[d], kt + D * KS);
+                    load_x(ring[d], kt + D * KS);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
-            kt += NW;
+            kt += KS;
         }
     }
-    auto put = [&](int at) {
+    // the strip's sums: register kV * part + i of this lane, from the wavefronts in their order
+    float sum[S][NTF][kV];
+    if constexpr (KS == 1) {
 #pragma unroll
         for (int s = 0; s < S; s++)
 #pragma unroll
             for (int f = 0; f < NTF; f++)
 #pragma unroll
-                for (int i = 0; i < 16; i++) s_red[at][s * NTF + f][i][lane] = acc[s][f][i];
-    };
-    if constexpr (NW == 8) {
-        if (wave >= 4) put(wave - 4);
-        __syncthreads();
-        if (wave < 4) {
+                for (int i = 0; i < 16; i++) sum[s][f][i] = acc[s][f][i];
+    } else {
+        const int at = mine * kParts + (part & (kParts - 1));
+        auto put = [&]() {
 #pragma unroll
             for (int s = 0; s < S; s++)
 #pragma unroll
                 for (int f = 0; f < NTF; f++)
 #pragma unroll
-                    for (int i = 0; i < 16; i++) acc[s][f][i] += s_red[wave][s * NTF + f][i][lane];
-            put(wave);                          // (its own place, read by none but it)
-        }
-    } else {
-        put(wave);
-    }
-    __syncthreads();
-    auto sum = [&](int at, int i) {
-        float all = s_red[0][at][i][lane];
+                    for (int i = 0; i < 16; i++) s_red[at][s * NTF + f][i][lane] = acc[s][f][i];
+        };
+        if constexpr (KS > kParts) {
+            if (part >= kParts) put();
+            __syncthreads();
+            if (part < kParts) {
 #pragma unroll
-        for (int w = 1; w < 4; w++) all += s_red[w][at][i][lane];
-        return all;
-    };
-    // a wavefront finishes four registers of a fragment: weight rows 8 g + 4 kb + 0 .. 3, token ln
-    constexpr int kGroups = NW / 4, kEach = (NTF + kGroups - 1) / kGroups;
-    const int g = wave & 3;
-    if constexpr (MODE == kMx4Up) {
-        uint32_t h[kEach][4];
+                for (int s = 0; s < S; s++)
 #pragma unroll
-        for (int j = 0; j < kEach; j++) {
-            const int f = (wave >> 2) + kGroups * j;
-            if (f >= NTF) continue;
-            uint32_t peak = 0;
+                    for (int f = 0; f < NTF; f++)
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                h[j][i] = __float_as_uint(silu_times(sum(f, 4 * g + i), sum(NTF + f, 4 * g + i)));
-                peak = max(peak, h[j][i] & 0x7fffffffu);
+                        for (int i = 0; i < 16; i++) acc[s][f][i] += s_red[at][s * NTF + f][i][lane];
+                put();                          // (its own place, read by none but it)
             }
-            const auto both = __builtin_amdgcn_permlane32_swap(peak, peak, false, false);
-            if (kb == 0) s_peak[f][g][ln] = max(both[0], both[1]);
+        } else {
+            put();
         }
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < kEach; j++) {
-            const int f = (wave >> 2) + kGroups * j, row = 32 * f + ln;
-            if (f >= NTF) continue;
-            const uint32_t byte = mx4_exponent(max(max(s_peak[f][0][ln], s_peak[f][1][ln]), max(s_peak[f][2][ln], s_peak[f][3][ln])));
+        for (int s = 0; s < S; s++)
+#pragma unroll
+            for (int f = 0; f < NTF; f++)
+#pragma unroll
+                for (int i = 0; i < kV; i++) {
+                    const int reg = kV * (part & (kParts - 1)) + i;
+                    float v = s_red[mine * kParts][s * NTF + f][reg][lane];
+#pragma unroll
+                    for (int q = 1; q < kParts; q++) v += s_red[mine * kParts + q][s * NTF + f][reg][lane];
+                    sum[s][f][i] = v;
+                }
+    }
+    // register 4 g + i: weight row 8 g + 4 kb + i, token ln
+    if constexpr (MODE == kMx4Up) {
+        uint32_t h[NTF][kV], peak[NTF];
+#pragma unroll
+        for (int f = 0; f < NTF; f++) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < kV; i++) {
+                h[f][i] = __float_as_uint(silu_times(sum[0][f][i], sum[S - 1][f][i]));
+                m = max(m, h[f][i] & 0x7fffffffu);
+            }
+            const auto both = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+            peak[f] = max(both[0], both[1]);
+            if (KS > 1 && part < kParts && kb == 0) s_peak[mine][f][part][ln] = peak[f];
+        }
+        if constexpr (KS > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int f = 0; f < NTF; f++)
+#pragma unroll
+                for (int q = 0; q < kParts; q++) peak[f] = max(peak[f], s_peak[mine][f][q][ln]);
+        }
+        if (part >= kParts || bx >= all) return;
+#pragma unroll
+        for (int f = 0; f < NTF; f++) {
+            const int row = 32 * f + ln;
+            const uint32_t byte = mx4_exponent(peak[f]);
             const float unit = mx4_unit(byte);
-            uint32_t q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, __uint_as_float(h[j][0]), __uint_as_float(h[j][1]), unit, 0);
-            q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, __uint_as_float(h[j][2]), __uint_as_float(h[j][3]), unit, 1);
-            const auto both = __builtin_amdgcn_permlane32_swap(q, q, false, false);
-            q = byte == 255u ? 0u : (both[0] & 0xffffu) | (both[1] << 16);
-            if (kb != 0 || row >= rows) continue;
-            const long at = (long)(row0 + row) * A.ldo + 32 * bx;
-            *(DYMOE_GLOBAL uint32_t*)((char*)A.out + at / 2 + 4 * g) = q;
-            if (g == 0) *(DYMOE_GLOBAL uint8_t*)(A.out_scale + at / 32) = (uint8_t)byte;
+            const long out = (FUSE ? (long)row0 : (long)(row0 + row)) * A.ldo + 32L * bx;
+#pragma unroll
+            for (int g = 0; g < kV / 4; g++) {
+                uint32_t q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, __uint_as_float(h[f][4 * g]), __uint_as_float(h[f][4 * g + 1]), unit, 0);
+                q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, __uint_as_float(h[f][4 * g + 2]), __uint_as_float(h[f][4 * g + 3]), unit, 1);
+                const auto both = __builtin_amdgcn_permlane32_swap(q, q, false, false);
+                q = byte == 255u ? 0u : (both[0] & 0xffffu) | (both[1] << 16);
+                if (kb == 0 && row < rows) *(DYMOE_GLOBAL uint32_t*)((char*)A.out + out / 2 + 4 * (kV / 4 * part + g)) = q;
+            }
+            if (kb == 0 && row < rows && part == 0) *(DYMOE_GLOBAL uint8_t*)(A.out_scale + out / 32) = (uint8_t)byte;
         }
     } else {
+        if (part >= kParts) return;
 #pragma unroll
-        for (int j = 0; j < kEach; j++) {
-            const int f = (wave >> 2) + kGroups * j, row = 32 * f + ln;
-            if (f >= NTF || row >= rows) continue;
-            const int n = 32 * bx + 8 * g + 4 * kb, left = A.N - n;
-            if (left <= 0) continue;
-            float v[4];
+        for (int f = 0; f < NTF; f++) {
+            const int row = 32 * f + ln;
+            if (row >= rows) continue;
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                v[i] = sum(f, 4 * g + i);
-                if (MODE == kMx4Plain && A.bias) v[i] += A.bias[min(n + i, A.N - 1)];
+            for (int g = 0; g < kV / 4; g++) {
+                const int n = 32 * bx + 8 * (kV / 4 * part + g) + 4 * kb, left = A.N - n;
+                if (left <= 0) continue;
+                float v[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    v[i] = sum[0][f][4 * g + i];
+                    if (MODE == kMx4Plain && A.bias) v[i] += A.bias[min(n + i, A.N - 1)];
+                }
+                const bool whole = left >= 4 && (MODE != kMx4Plain || A.aligned);
+                store_out4(A.out, (long)(row0 + row) * A.ldo + n, MODE == kMx4Plain ? A.out_dtype : DYMOE_OUT_F32, whole, left, v);
             }
-            const bool whole = left >= 4 && (MODE != kMx4Plain || A.aligned);
-            store_out4(A.out, (long)(row0 + row) * A.ldo + n, MODE == kMx4Plain ? A.out_dtype : DYMOE_OUT_F32, whole, left, v);
         }
     }
+}
+
+// The down projection of a few tokens with the sum over their slots: a workgroup owns 16 outputs of one token.  The tiles of its pairs, one pair behind
+// the other, are dealt to the wavefronts in equal runs, D tiles of a wavefront on their way; the intermediate's codes wait in LDS.  The
+// matrix instruction's 32 weight rows are those 16 twice (the second half of the lanes asks for the same lines): with 32 outputs a workgroup, one
+// token on 4096 outputs would have half as many workgroups as there are compute units.
+constexpr int kMx4LastWaves = 16;
+
+template <int D>
+__global__ __launch_bounds__(64 * kMx4LastWaves) void mx4_thin_down_kernel(const Mx4Args A)
+{
+    extern __shared__ __attribute__((aligned(16))) char s_rows[];
+    __shared__ float s_sum[kMx4LastWaves][16];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    // the workgroups of one strip go to one XCD, whose L2 then has the weights that several tokens need
+    const int nblk = (A.N + 15) / 16, j = blockIdx.x >> 3;
+    const int t = j % A.rows, bx = j / A.rows * 8 + (blockIdx.x & 7);
+    if (bx >= nblk) return;
+    const int k = A.k, nkt = A.Kp >> 8, strips = (A.N + 31) / 32, items = k * nkt;
+    const int first = items * wave / kMx4LastWaves, last = items * (wave + 1) / kMx4LastWaves;
+    const uint32_t row = (uint32_t)((lane >> 5) * 32 + (bx & 1) * 16 + (lane & 15));
+    struct Tile {
+        uint4 w[4];
+        uint32_t ws;
+    } ring[D];
+    Mx4Strip w;
+    int ask = first, ask_slot = first / nkt, ask_kt = first - ask_slot * nkt;
+    auto open = [&](int slot) {
+        // (an expert that is not there: a strip without bytes, read as zeros)
+        const int e = __builtin_amdgcn_readfirstlane(A.idx[t * k + slot]);
+        dymoe_expert_mx4 ex = {};
+        if ((unsigned)e < (unsigned)A.E) ex = A.table[e];
+        w.set(ex.q[2], ex.s[2], expert_present(ex) ? bx >> 1 : strips, strips, A.Kp);
+    };
+    auto request = [&](Tile& tl) {
+        if (ask >= last) return;
+#pragma unroll
+        for (int c = 0; c < 4; c++) tl.w[c] = w.q.template load<true>(row * 16u + (uint32_t)(c * 1024), (uint32_t)ask_kt * 4096u);
+        tl.ws = load_u32(w.s, row * 4u, (uint32_t)ask_kt * 256u);
+        ask++;
+        if (++ask_kt == nkt && ask < last) {
+            ask_kt = 0;
+            open(++ask_slot);
+        }
+    };
+    if (first < last) open(ask_slot);
+#pragma unroll
+    for (int d = 0; d < D; d++) request(ring[d]);
+    // the pairs' codes and exponents; zeros for one that is left out, whose row nobody wrote
+    const int per = A.Kp >> 5, exps = k * mx4_lds_row(A.Kp);             // 16-byte chunks of a row's codes, and bytes of its exponents
+    for (int i = tid; i < k * per; i += 64 * kMx4LastWaves) {
+        const int slot = i / per, c = i - slot * per, pair = t * k + slot, e = A.idx[pair];
+        uint4 q = make_uint4(0, 0, 0, 0);
+        uint8_t x = 0;
+        if ((unsigned)e < (unsigned)A.E && expert_present(A.table[e])) {
+            q = load_global<uint4>(A.x + ((long)pair * (A.Kp >> 1) + c * 16));
+            x = *(const DYMOE_GLOBAL uint8_t*)(A.xs + ((long)pair * per + c));
+        }
+        *(uint4*)(s_rows + slot * mx4_lds_row(A.Kp) + c * 16) = q;
+        s_rows[exps + slot * per + c] = (char)x;
+    }
+    __syncthreads();
+    float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    float16_t acc = {};
+    int slot = first / nkt, kt = first - slot * nkt;
+    const int half = lane >> 5;
+    for (int i = first; i < last;) {
+#pragma unroll
+        for (int d = 0; d < D; d++) {
+            if (i < last) {
+                const char* const xr = s_rows + slot * mx4_lds_row(A.Kp) + kt * 128 + half * 64;
+                const uint32_t xe = *(const uint32_t*)(s_rows + exps + slot * per + kt * 8 + half * 4);
+                acc = mfma_mx4<0, 0>(ring[d].w[0], *(const uint4*)xr, acc, ring[d].ws, xe);
+                acc = mfma_mx4<1, 1>(ring[d].w[1], *(const uint4*)(xr + 16), acc, ring[d].ws, xe);
+                acc = mfma_mx4<2, 2>(ring[d].w[2], *(const uint4*)(xr + 32), acc, ring[d].ws, xe);
+                acc = mfma_mx4<3, 3>(ring[d].w[3], *(const uint4*)(xr + 48), acc, ring[d].ws, xe);
+                __builtin_amdgcn_sched_barrier(0);
+                request(ring[d]);
+                __builtin_amdgcn_sched_barrier(0);
+                i++;
+                if (++kt == nkt || i == last) {
+                    // register 4 g + i holds row 8 g + 4 (lane / 32) + i, of which the first 16 are wanted
+                    const float gate = A.gate[t * k + slot];
+#pragma unroll
+                    for (int v = 0; v < 8; v++) y[v] = fmaf(gate, acc[v], y[v]);
+#pragma unroll
+                    for (int v = 0; v < 16; v++) acc[v] = 0.0f;
+                    kt = 0;
+                    slot++;
+                }
+            }
+        }
+    }
+    if ((lane & 31) == 0) {
+#pragma unroll
+        for (int v = 0; v < 8; v++) s_sum[wave][8 * (v >> 2) + 4 * half + (v & 3)] = y[v];
+    }
+    __syncthreads();
+    const int n = 16 * bx + tid;
+    if (tid >= 16 || n >= A.N) return;
+    float sum = s_sum[0][tid];
+#pragma unroll
+    for (int v = 1; v < kMx4LastWaves; v++) sum += s_sum[v][tid];
+    store_out(A.out, t * A.ldo + n, A.out_dtype, sum);
 }
 
 // ----------------------------------------------------------------------------
@@ -269,10 +473,10 @@ constexpr uint32_t kMx4EpiWave = 32 * kMx4EpiRow;
 
 __device__ __forceinline__ int mx4_turn(int row) { return (row >> 1) & 7; }      // (the row's parity is half of the banks already)
 
-template <int S>
+template <int S, int D>
 struct Mx4Weights {
-    uint4 r[2][S][4];              // codes of an even step and of an odd one
-    uint32_t e[2][S];              // exponents
+    uint4 r[D][S][4];              // codes of this step and of those behind it
+    uint32_t e[D][S];              // exponents
     Mx4Strip strip[S];
 
     __device__ __forceinline__ void codes(int p, int c, uint32_t lane16, int step)
@@ -287,20 +491,22 @@ struct Mx4Weights {
     }
 };
 
-template <int MODE, int NTF, int S>
-__device__ __forceinline__ void mx4_tile(const Mx4Args& A, const int32_t* perm, Mx4Weights<S>& w, int row0, int rows, int bx, uint32_t base)
+template <int MODE, int NTF, int S, int D, int RR>
+__device__ __forceinline__ void mx4_tile(const Mx4Args& A, const int32_t* perm, Mx4Weights<S, D>& w, int row0, int rows, int bx, int step0, int steps, void* out,
+                                         uint32_t base)
 {
     constexpr int kMask = 0x2 | 0x4;             // vector and scalar arithmetic may cross; products, LDS and memory accesses may not
     constexpr uint32_t kBuf = kMx4Buf<NTF>, kExp = 32u * NTF * kMx4Row;
     constexpr int kCopies = NTF + (NTF + 3) / 4;
+    constexpr int R = RR < 4 * NTF ? RR : 4 * NTF;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int ln = lane & 31, kb = lane >> 5;
     const uint32_t lane16 = (uint32_t)lane * 16u;
-    const int steps = A.Kp >> 8, end = steps - 1;
+    const int end = steps - 1;
     float16_t acc[S][NTF] = {};
     // copies: rows 32 i + 8 wave + lane / 8, chunk lane % 8 turned; exponents of fragment `wave` (and wave + 4)
-    const char* const xb = A.x + (MODE == kMx4Up ? 0 : (long)row0 * (A.Kp >> 1));
-    const char* const sb = A.xs + (MODE == kMx4Up ? 0 : (long)row0 * (A.Kp >> 5));
+    const char* const xb = A.x + (MODE == kMx4Up ? 0 : (long)row0 * (A.Kp >> 1)) + (long)step0 * 128;
+    const char* const sb = A.xs + (MODE == kMx4Up ? 0 : (long)row0 * (A.Kp >> 5)) + (long)step0 * 8;
     uint32_t off[NTF], offs[(NTF + 3) / 4];
     auto source = [&](int r) {                   // rows behind the last: computed and dropped
         r = min(r, rows - 1);
@@ -320,61 +526,79 @@ __device__ __forceinline__ void mx4_tile(const Mx4Args& A, const int32_t* perm, 
         for (int i = 0; i < (NTF + 3) / 4; i++)
             lds_copy4(sb + (long)step * 8, offs[i], __builtin_amdgcn_readfirstlane(base + buf + kExp + (uint32_t)(min(wave + 4 * i, NTF - 1) * 256)));
     };
-    copy(0, 0);
-    copy(min(1, end), kBuf);
 #pragma unroll
-    for (int p = 0; p < 2; p++) {
+    for (int p = 0; p < D; p++) copy(min(p, end), (uint32_t)p * kBuf);
 #pragma unroll
-        for (int c = 0; c < 4; c++) w.codes(p, c, lane16, min(p, end));
-        w.scales(p, lane16, min(p, end));
+    for (int p = 0; p < D; p++) {
+        // (in the loop's order: what the compiler waits for at the loop's head is then what a step behind another needs)
+        w.scales(p, lane16, step0 + min(p, end));
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int c = 0; c < 4; c++) {
+            w.codes(p, c, lane16, step0 + min(p, end));
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
-    wait_lds_copies<kCopies + 10 * S>();        // the first copies are older than everything else
+    wait_lds_copies<(D - 1) * kCopies + 5 * D * S>();        // the first copies are older than everything else
     __syncthreads();
     const uint32_t xa0 = base + (uint32_t)ln * kMx4Row + (((uint32_t)kb << 6) ^ ((uint32_t)mx4_turn(ln) << 4));
     const uint32_t xe0 = base + kExp + (uint32_t)ln * 8u + (uint32_t)kb * 4u;
     uint32_t at = 0;
-    // Step ks multiplies what its buffer and registers hold and requests the codes of the rows and of the weights two steps on.
-    auto step = [&](int ks, auto parity) __attribute__((always_inline)) {
-        constexpr int p = parity();
-        const int after = min(ks + 2, end);
-        copy(after, at == 0 ? 2 * kBuf : at - kBuf);
+    // Step ks multiplies what its buffer and registers hold and requests the codes of the rows and of the weights D steps on.
+    auto step = [&](int ks, auto slot) __attribute__((always_inline)) {
+        constexpr int p = slot();
+        const int after = min(ks + D, end);
+        // What a step waits for first is requested first, and the copies behind its first products: the compiler does not count them, so that
+        // a wait of its own for a load that copies were issued behind is one for younger loads too.
+        uint32_t now[S];
+#pragma unroll
+        for (int s = 0; s < S; s++) asm volatile("v_mov_b32 %0, %1" : "=v"(now[s]) : "v"(w.e[p][s]));      // (here, and not at the end of the loop)
+        __builtin_amdgcn_sched_barrier(kMask);
+        w.scales(p, lane16, step0 + after);
         uint32_t xe[NTF];
 #pragma unroll
         for (int f = 0; f < NTF; f++) xe[f] = lds_read4(xe0 + at + (uint32_t)f * 256u);
-        uint4 op = lds_read16(xa0 + at);
+        // the operands of the next R products of a chunk and a fragment are read while this one's are issued
+        uint4 op[R];
+        auto read = [&](int o) { return lds_read16(((xa0 + at) ^ (uint32_t)((o / NTF) << 4)) + (uint32_t)(o % NTF) * (32u * kMx4Row)); };
+#pragma unroll
+        for (int o = 0; o < R; o++) op[o] = read(o);
         auto chunk = [&](auto which) __attribute__((always_inline)) {
             constexpr int c = which();
 #pragma unroll
             for (int f = 0; f < NTF; f++) {
-                constexpr int last = NTF - 1;
-                uint4 nxt = op;
-                if (!(f == last && c == 3))
-                    nxt = lds_read16(((xa0 + at) ^ (uint32_t)((f == last ? c + 1 : c) << 4)) + (uint32_t)(f == last ? 0 : f + 1) * (32u * kMx4Row));
+                const int o = c * NTF + f;
                 __builtin_amdgcn_sched_barrier(kMask);
 #pragma unroll
-                for (int s = 0; s < S; s++) acc[s][f] = mfma_mx4<c, c>(w.r[p][s][c], op, acc[s][f], w.e[p][s], xe[f]);
-                op = nxt;
+                for (int s = 0; s < S; s++) acc[s][f] = mfma_mx4<c, c>(w.r[p][s][c], op[o % R], acc[s][f], now[s], xe[f]);
                 __builtin_amdgcn_sched_barrier(kMask);
+                if (o + R < 4 * NTF) op[o % R] = read(o + R);
             }
-            w.codes(p, c, lane16, after);
+            if constexpr (c == 0) copy(after, at == 0 ? D * kBuf : at - kBuf);         // (the buffer of the step before)
+            w.codes(p, c, lane16, step0 + after);
             __builtin_amdgcn_sched_barrier(kMask);
         };
         chunk(std::integral_constant<int, 0>());
         chunk(std::integral_constant<int, 1>());
         chunk(std::integral_constant<int, 2>());
         chunk(std::integral_constant<int, 3>());
-        w.scales(p, lane16, after);
-        __builtin_amdgcn_sched_barrier(kMask);
-        wait_lds_copies<kCopies + 10 * S>();    // behind the next step's copies: its and this step's loads of weights, this step's copies
+        // behind the next step's copies: the loads of codes of the step that asked for them, and all of the steps since
+        wait_lds_copies<4 * S + (D - 1) * (kCopies + 5 * S)>();
         __syncthreads();
-        at = at == 2 * kBuf ? 0 : at + kBuf;
+        at = at == D * kBuf ? 0 : at + kBuf;
     };
     int ks = 0;
-    for (; ks + 2 <= steps; ks += 2) {
+    for (; ks + D <= steps; ks += D) {
         step(ks, std::integral_constant<int, 0>());
         step(ks + 1, std::integral_constant<int, 1>());
+        if constexpr (D > 2) step(ks + 2, std::integral_constant<int, 2>());
+        if constexpr (D > 3) step(ks + 3, std::integral_constant<int, 3>());
     }
     if (ks < steps) step(ks, std::integral_constant<int, 0>());
+    if constexpr (D > 2)
+        if (ks + 1 < steps) step(ks + 1, std::integral_constant<int, 1>());
+    if constexpr (D > 3)
+        if (ks + 2 < steps) step(ks + 2, std::integral_constant<int, 2>());
     // (the copies requested beyond the end: the buffers are the epilogue's now)
     wait_lds_copies<0>();
     __syncthreads();
@@ -412,9 +636,9 @@ __device__ __forceinline__ void mx4_tile(const Mx4Args& A, const int32_t* perm, 
                 const uint4 all = make_uint4((a[0] & 0xffffu) | (a[1] << 16), (a[0] >> 16) | (a[1] & 0xffff0000u), (b[0] & 0xffffu) | (b[1] << 16),
                                              (b[0] >> 16) | (b[1] & 0xffff0000u));
                 if (row >= rows) continue;
-                const long out = (long)(row0 + row) * A.ldo + 32L * block;
-                if (kb == 0) store_global((char*)A.out + out / 2, all);
-                else *(DYMOE_GLOBAL uint8_t*)(A.out_scale + out / 32) = (uint8_t)byte;
+                const long at = (long)(row0 + row) * A.ldo + 32L * block;
+                if (kb == 0) store_global((char*)out + at / 2, all);
+                else *(DYMOE_GLOBAL uint8_t*)(A.out_scale + at / 32) = (uint8_t)byte;
             }
         }
     } else {
@@ -443,7 +667,7 @@ __device__ __forceinline__ void mx4_tile(const Mx4Args& A, const int32_t* perm, 
                     const uint4 u = lds_read16(area + (uint32_t)rr * kMx4EpiRow + (uint32_t)(lane & 7) * 16u);
                     if (row >= rows || left <= 0) continue;
                     const float v[4] = {__uint_as_float(u.x) + add[0], __uint_as_float(u.y) + add[1], __uint_as_float(u.z) + add[2], __uint_as_float(u.w) + add[3]};
-                    store_out4(A.out, (long)(row0 + row) * A.ldo + n, dt, left >= 4 && vec, left, v);
+                    store_out4(out, (long)(row0 + row) * A.ldo + n, dt, left >= 4 && vec, left, v);
                 }
             }
         }
@@ -462,7 +686,7 @@ __device__ __forceinline__ uint32_t mx4_lds_base(char* p) { return (uint32_t)(ui
 template <int MODE, int S>
 constexpr int kMx4Cols = 128 * (MODE == kMx4Up ? S / 2 : S);
 
-template <int MODE, int MAXF, int S>
+template <int MODE, int MAXF, int S, int D, int RR>
 __global__ __launch_bounds__(256, MAXF * S <= 8 ? 2 : 1) void mx4_tall_kernel(const Mx4Args A)
 {
     extern __shared__ __attribute__((aligned(1024))) char lds_raw[];
@@ -472,8 +696,9 @@ __global__ __launch_bounds__(256, MAXF * S <= 8 ? 2 : 1) void mx4_tall_kernel(co
     const int strips = (A.N + 31) / 32, nblk = (int)(((MODE == kMx4Up ? A.ldo : A.N) + kCols - 1) / kCols);
     const Mx4Plan pp = expert_plan<dymoe_expert_mx4>(const_cast<int32_t*>(A.plan), A.P);
     const long unit = mx4_unit_of_group();
-    Mx4Weights<S> w;
-    int row0, rows, bx;
+    Mx4Weights<S, D> w;
+    int row0, rows, bx, step0 = 0, steps = A.Kp >> 8;
+    void* out = A.out;
     if (MODE == kMx4Plain) {
         const int tiles = (A.rows + kRows - 1) / kRows;
         if (unit >= (long)tiles * nblk) return;
@@ -483,9 +708,17 @@ __global__ __launch_bounds__(256, MAXF * S <= 8 ? 2 : 1) void mx4_tall_kernel(co
 #pragma unroll
         for (int s = 0; s < S; s++) w.strip[s].set(A.w, A.ws, (4L * bx + wave) * S + s, strips, A.Kp);
     } else {
-        if (unit >= (long)pp.meta[0] * nblk) return;
-        const ExpertTile<dymoe_expert_mx4> t = pp.tiles[unit / nblk];
-        const long local = unit - (long)t.tile0 * nblk;
+        const int splits = MODE == kMx4Down ? A.splits : 1;
+        if (unit >= (long)pp.meta[0] * nblk * splits) return;
+        const ExpertTile<dymoe_expert_mx4> t = pp.tiles[unit / (nblk * splits)];
+        long local = unit - (long)t.tile0 * (nblk * splits);
+        if (MODE == kMx4Down) {
+            const int part = (int)(local / ((long)t.tiles * nblk));
+            local -= (long)part * t.tiles * nblk;
+            step0 = steps * part / splits;
+            steps = steps * (part + 1) / splits - step0;
+            out = (float*)out + part * A.P * A.ldo;
+        }
         bx = (int)(local / t.tiles);
         const int i = (int)(local - (long)bx * t.tiles) * kRows;
         row0 = t.first + i;
@@ -497,27 +730,71 @@ __global__ __launch_bounds__(256, MAXF * S <= 8 ? 2 : 1) void mx4_tall_kernel(co
         }
     }
     // one instantiation per number of fragments of 32 rows: the accumulators then sit in fixed registers for the whole loop
-#define DYMOE_MX4_TILE(NTF) mx4_tile<MODE, NTF, S>(A, pp.perm, w, row0, rows, bx, base)
+#define DYMOE_MX4_TILE(NTF) mx4_tile<MODE, NTF, S, D, RR>(A, pp.perm, w, row0, rows, bx, step0, steps, out, base)
     switch ((rows + 31) >> 5) {
     case 1: DYMOE_MX4_TILE(1); break;
-    case 2: DYMOE_MX4_TILE(2); break;
-    case 3: DYMOE_MX4_TILE(3); break;
+    case 2: DYMOE_MX4_TILE(MAXF < 2 ? MAXF : 2); break;
+    case 3: DYMOE_MX4_TILE(MAXF < 3 ? MAXF : 3); break;
     default: DYMOE_MX4_TILE(MAXF); break;
     }
 #undef DYMOE_MX4_TILE
 }
 
-template <int MAXF>
-constexpr int kMx4Lds = 3 * kMx4Buf<MAXF>;
-static_assert(4 * kMx4EpiWave <= 3 * kMx4Buf<4>, "the epilogue areas fit in the buffers of a whole tile");
+template <int MAXF, int D>
+constexpr int kMx4Lds = (int)((D + 1) * kMx4Buf<MAXF>) > (int)(4 * kMx4EpiWave) ? (int)((D + 1) * kMx4Buf<MAXF>) : (int)(4 * kMx4EpiWave);
+static_assert(4 * kMx4EpiWave <= kMx4Lds<4, 2> && 4 * kMx4EpiWave <= kMx4Lds<2, 2> && 4 * kMx4EpiWave <= 2 * kMx4Lds<1, 3>, "the epilogue areas fit in the buffers of a whole tile");
+
+// A shape's instantiation: the tile's fragments of 32 rows, strips of a wavefront, steps ahead, operands ahead.
+#define DYMOE_MX4_TILE32(MODE) mx4_tall_kernel<MODE, 1, 1, 4, 4>
+#define DYMOE_MX4_TILE64(MODE) mx4_tall_kernel<MODE, 2, 1, 3, 4>
+#define DYMOE_MX4_TILE64W(MODE) mx4_tall_kernel<MODE, 2, 2, 2, 4>
+#define DYMOE_MX4_TILE128(MODE) mx4_tall_kernel<MODE, 4, 2, 2, 3>
 
 // per-device set-up, with the device current
 int mx4_init()
 {
     auto allow = [](const void* f, int bytes) { return hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess; };
-    const bool ok = allow((const void*)mx4_tall_kernel<kMx4Plain, 4, 2>, kMx4Lds<4>) && allow((const void*)mx4_tall_kernel<kMx4Up, 4, 2>, kMx4Lds<4>) &&
-                    allow((const void*)mx4_tall_kernel<kMx4Down, 4, 2>, kMx4Lds<4>);
+    bool ok = allow((const void*)DYMOE_MX4_TILE32(kMx4Plain), kMx4Lds<1, 4>) && allow((const void*)DYMOE_MX4_TILE64(kMx4Plain), kMx4Lds<2, 3>) &&
+              allow((const void*)DYMOE_MX4_TILE64W(kMx4Plain), kMx4Lds<2, 2>) && allow((const void*)DYMOE_MX4_TILE128(kMx4Plain), kMx4Lds<4, 2>);
+    ok = ok && allow((const void*)DYMOE_MX4_TILE128(kMx4Up), kMx4Lds<4, 2>) && allow((const void*)DYMOE_MX4_TILE128(kMx4Down), kMx4Lds<4, 2>);
+    ok = ok && allow((const void*)mx4_small_kernel<kMx4Plain, 1, 8, 8, 1, true>, (int)kMx4FuseBytes) &&
+         allow((const void*)mx4_small_kernel<kMx4Up, 1, 4, 4, 1, true>, (int)kMx4FuseBytes) && allow((const void*)mx4_thin_down_kernel<2>, (int)kMx4FuseBytes);
     return ok ? DYMOE_OK : DYMOE_EHIP;
+}
+
+// y[t] = sum over the slots, in their order, of gate times the pair's output, which is the sum of its parts.  A workgroup takes 2048 outputs of a
+// token.  Bound by the pairs' bytes: 16376 pairs of 2048 outputs 21.5 us (6.2 TB/s).
+template <int PARTS>
+__global__ __launch_bounds__(256) void mx4_combine_kernel(const float* __restrict__ part, long ldp, long P, const int32_t* __restrict__ where,
+                                                          const float* __restrict__ gate, int H, int k, int out_dtype, int aligned,
+                                                          void* __restrict__ y)
+{
+    const int blocks = (H + 2047) / 2048;
+    const long t = blockIdx.x / blocks;
+    const int h = (int)(blockIdx.x - t * blocks) * 2048 + threadIdx.x * 8;
+    if (h >= H) return;
+    constexpr int kAhead = PARTS > 1 ? 2 : 4;
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll kAhead
+    for (int j = 0; j < k; j++) {
+        const int at = where[t * k + j];
+        if (at < 0) continue;
+        const float g = gate[t * k + j];
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int p = 0; p < PARTS; p++) {
+            const float* const from = part + (p * P + at) * ldp + h;
+            const float4 a = load_global<float4>(from), b = load_global<float4>(from + 4);
+            const float w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int i = 0; i < 8; i++) v[i] = p == 0 ? w[i] : v[i] + w[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) sum[i] = fmaf(g, v[i], sum[i]);
+    }
+    const float lo[4] = {sum[0], sum[1], sum[2], sum[3]}, hi[4] = {sum[4], sum[5], sum[6], sum[7]};
+    store_out4(y, t * H + h, out_dtype, aligned && h + 4 <= H, H - h, lo);
+    store_out4(y, t * H + h + 4, out_dtype, aligned && h + 8 <= H, H - h - 4, hi);
 }
 
 // a launch's threads have to stay below 2^32
@@ -555,10 +832,15 @@ extern "C" int dymoe_matmul_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, cons
     if (T == 0) return DYMOE_OK;
     hipStream_t st = (hipStream_t)stream;
     char* const ws = (char*)workspace;
+    const Mx4MatChoice c = mx4_mat_choice(T, N, K, coded, ctx->num_cu);
     Mx4Args A = {};
     A.x = (const char*)x;
     A.xs = (const char*)x_scale;
-    if (!coded) {
+    if (c.fuse) {
+        A.ldx = ldx * dtype_bytes(x_dtype);
+        A.x_dtype = x_dtype;
+        A.K = K;
+    } else if (!coded) {
         const int rc = mx4_quantize(ctx, x, x_dtype, T, K, ldx, 0, (uint8_t*)ws + L.xq, (uint8_t*)ws + L.xs, st);
         if (rc != DYMOE_OK) return rc;
         A.x = ws + L.xq;
@@ -574,10 +856,21 @@ extern "C" int dymoe_matmul_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, cons
     A.N = N;
     A.out_dtype = out_dtype;
     A.aligned = dymoe_aligned(y, 4 * dtype_bytes(out_dtype)) && ldy % 4 == 0;
-    if (T > 64)
-        dymoe_launch(ctx, DYMOE_K_MX4_PRODUCT, mx4_tall_kernel<kMx4Plain, 4, 2>, mx4_grid((T + 127L) / 128 * ((N + 255L) / 256)), dim3(256), kMx4Lds<4>, st, A);
-    else
-        dymoe_launch(ctx, DYMOE_K_MX4_PRODUCT, mx4_small_kernel<kMx4Plain, 1, 8, 1>, dim3((unsigned)groups), dim3(512), 0, st, A);
+    const long n128 = (N + 127L) / 128, n256 = (N + 255L) / 256;
+    auto run = [&](void (*kernel)(const Mx4Args), dim3 grid, int threads, int lds) {
+        dymoe_launch(ctx, DYMOE_K_MX4_PRODUCT, kernel, grid, dim3((unsigned)threads), lds, st, A);
+    };
+    switch (c.shape) {
+    case Mx4MatShape::kSmall:
+        if (c.fuse) run(mx4_small_kernel<kMx4Plain, 1, 8, 8, 1, true>, dim3((unsigned)groups), 512, (int)mx4_fuse_bytes(T, L.Kp));
+        else if (c.waves == 8) run(mx4_small_kernel<kMx4Plain, 1, 8, 8, 1>, dim3((unsigned)groups), 512, 0);
+        else run(mx4_small_kernel<kMx4Plain, 1, 4, 4, 1>, dim3((unsigned)groups), 256, 0);
+        break;
+    case Mx4MatShape::kTile32: run(DYMOE_MX4_TILE32(kMx4Plain), mx4_grid((T + 31L) / 32 * n128), 256, kMx4Lds<1, 4>); break;
+    case Mx4MatShape::kTile64: run(DYMOE_MX4_TILE64(kMx4Plain), mx4_grid((T + 63L) / 64 * n128), 256, kMx4Lds<2, 3>); break;
+    case Mx4MatShape::kTile64w: run(DYMOE_MX4_TILE64W(kMx4Plain), mx4_grid((T + 63L) / 64 * n256), 256, kMx4Lds<2, 2>); break;
+    default: run(DYMOE_MX4_TILE128(kMx4Plain), mx4_grid((T + 127L) / 128 * n256), 256, kMx4Lds<4, 2>);
+    }
     DYMOE_HIP_LAUNCH_CHECK();
     return DYMOE_OK;
 }
@@ -604,47 +897,81 @@ extern "C" int dymoe_moe_ffn_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, con
     if (P >= 1L << 29 || (long)T * up_to(H, kMx4TileCols) / 2 >= 1L << 32) return DYMOE_ENOTSUP;      // (32-bit offsets into the codes)
     const Mx4FfnLayout L = mx4_ffn_layout(T, H, F, E, k);
     if (workspace_bytes < L.total) return DYMOE_ENOSPC;
-    const long up = (long)L.max_tiles * (long)(L.Fp / 32), down = (long)L.max_tiles * ((H + 31L) / 32);
+    const long up = (long)L.max_tiles * (long)(L.Fp / 32), down = (long)L.max_tiles * ((H + 31L) / 32);     // workgroups at most
     if (!fits_grid(up, 512) || !fits_grid(down, 512) || !fits_grid(T * ((H + 2047L) / 2048), 256)) return DYMOE_ENOTSUP;
     if (!ctx) return DYMOE_ENOCTX;
     if (T == 0) return DYMOE_OK;
     hipStream_t st = (hipStream_t)stream;
     char* const ws = (char*)workspace;
-    int32_t* const plan = (int32_t*)(ws + L.plan);
-    const int per_row = (int)((L.Hp + 511) / 512);
-    const long units = (long)T * per_row;
-    const dim3 grid((unsigned)(1 + (units + 15) / 16));
-    auto prep = mx4_prep_kernel<DYMOE_OUT_BF16>;
-    if (x_dtype == DYMOE_OUT_F32) prep = mx4_prep_kernel<DYMOE_OUT_F32>;
-    else if (x_dtype == DYMOE_OUT_F16) prep = mx4_prep_kernel<DYMOE_OUT_F16>;
-    const int small = T <= 32 || P <= 20L * E;
-    const long tall = P / kMx4TallRows + (E < P ? E : P);
-    dymoe_launch(ctx, DYMOE_K_MX4_ROWS, prep, grid, dim3(kPlanThreads), 0, st, idx, table, P, E, small, plan, ctx->device_flags, (const char*)x,
-                 units, per_row, H, ws + L.xq, ws + L.xs);
+    const Mx4FfnChoice c = mx4_ffn_choice(T, H, F, E, k, ctx->num_cu);
     Mx4Args A = {};
-    A.x = ws + L.xq;
-    A.xs = ws + L.xs;
-    A.plan = plan;
     A.out = ws + L.hq;
     A.out_scale = (uint8_t*)ws + L.hs;
     A.ldo = (long)L.Fp;
     A.P = P;
+    A.rows = T;
     A.Kp = (int)L.Hp;
     A.N = F;
     A.k = k;
-    A.rows = T;
-    if (small) dymoe_launch(ctx, DYMOE_K_MX4_PRODUCT, mx4_small_kernel<kMx4Up, 1, 8, 1>, dim3((unsigned)up), dim3(512), 0, st, A);
-    else dymoe_launch(ctx, DYMOE_K_MX4_PRODUCT, mx4_tall_kernel<kMx4Up, 4, 2>, mx4_grid(tall * (long)(L.Fp / 128)), dim3(256), kMx4Lds<4>, st, A);
-    A.x = ws + L.hq;
-    A.xs = ws + L.hs;
-    A.out = ws + L.part;
-    A.ldo = (long)mx4_round((size_t)H, 8);
-    A.Kp = (int)L.Fp;
-    A.N = H;
-    if (small) dymoe_launch(ctx, DYMOE_K_MX4_PRODUCT, mx4_small_kernel<kMx4Down, 1, 8, 1>, dim3((unsigned)down), dim3(512), 0, st, A);
-    else dymoe_launch(ctx, DYMOE_K_MX4_PRODUCT, mx4_tall_kernel<kMx4Down, 4, 2>, mx4_grid(tall * ((H + 255L) / 256)), dim3(256), kMx4Lds<4>, st, A);
-    experts_combine(ctx, DYMOE_K_MX4_ROWS, (const float*)(ws + L.part), A.ldo, expert_plan<dymoe_expert_mx4>(plan, P).where, w, T, H, k, out_dtype,
-                    y, st);
+    A.splits = 1;
+    auto run = [&](void (*kernel)(const Mx4Args), dim3 grid, int threads, int lds) {
+        dymoe_launch(ctx, DYMOE_K_MX4_PRODUCT, kernel, grid, dim3((unsigned)threads), lds, st, A);
+    };
+    // from the up to the down projection
+    auto turn = [&](void* out, long ldo, int dt) {
+        A.x = ws + L.hq;
+        A.xs = ws + L.hs;
+        A.out = out;
+        A.ldo = ldo;
+        A.Kp = (int)L.Fp;
+        A.N = H;
+        A.out_dtype = dt;
+    };
+    if (c.shape == Mx4FfnShape::kThin) {
+        A.x = (const char*)x;
+        A.ldx = (long)H * dtype_bytes(x_dtype);
+        A.x_dtype = x_dtype;
+        A.K = H;
+        A.idx = idx;
+        A.gate = w;
+        A.table = table;
+        A.flags = ctx->device_flags;
+        A.E = E;
+        run(mx4_small_kernel<kMx4Up, 1, 4, 4, 1, true>, dim3((unsigned)(P * (long)(L.Fp / 32))), 256, (int)mx4_fuse_bytes(T, L.Hp));
+        turn(y, H, out_dtype);
+        run(mx4_thin_down_kernel<2>, dim3((unsigned)(8L * T * (((H + 15L) / 16 + 7) / 8))), 64 * kMx4LastWaves, (int)mx4_fuse_bytes(k, L.Fp));
+        DYMOE_HIP_LAUNCH_CHECK();
+        return DYMOE_OK;
+    }
+    const bool small = c.shape == Mx4FfnShape::kSmall;
+    int32_t* const plan = (int32_t*)(ws + L.plan);
+    const int per_row = (int)((L.Hp + 511) / 512);
+    const int units = T * per_row;              // (below 2^23: T times H is below 2^33)
+    auto prep = mx4_prep_kernel<DYMOE_OUT_BF16>;
+    if (x_dtype == DYMOE_OUT_F32) prep = mx4_prep_kernel<DYMOE_OUT_F32>;
+    else if (x_dtype == DYMOE_OUT_F16) prep = mx4_prep_kernel<DYMOE_OUT_F16>;
+    dymoe_launch(ctx, DYMOE_K_MX4_ROWS, prep, dim3((unsigned)(1 + (units + 15) / 16)), dim3(kPlanThreads), 0, st, idx, table, P, E, (int)small, plan,
+                 ctx->device_flags, (const char*)x, units, per_row, H, ws + L.xq, ws + L.xs);
+    A.x = ws + L.xq;
+    A.xs = ws + L.xs;
+    A.plan = plan;
+    const long tall = P / kMx4TallRows + (E < P ? E : P);
+    auto strips = [&](long n, int each) { return dim3((unsigned)(L.max_tiles * ((n + each - 1) / each))); };
+    const long fs = (long)(L.Fp / 32), hs = (H + 31L) / 32;
+    if (!small) run(DYMOE_MX4_TILE128(kMx4Up), mx4_grid(tall * (long)(L.Fp / 128)), 256, kMx4Lds<4, 2>);
+    else if (c.up_waves == 4) run(mx4_small_kernel<kMx4Up, 1, 4, 4, 1>, strips(fs, 1), 256, 0);
+    else if (c.up_waves == 2) run(mx4_small_kernel<kMx4Up, 1, 4, 2, 1>, strips(fs, 2), 256, 0);
+    else run(mx4_small_kernel<kMx4Up, 1, 4, 1, 1>, strips(fs, 4), 256, 0);
+    turn(ws + L.part, (long)mx4_round((size_t)H, 8), DYMOE_OUT_F32);
+    A.splits = c.splits;
+    if (!small) run(DYMOE_MX4_TILE128(kMx4Down), mx4_grid(tall * ((H + 255L) / 256) * c.splits), 256, kMx4Lds<4, 2>);
+    else if (c.down_waves == 8) run(mx4_small_kernel<kMx4Down, 1, 8, 8, 1>, strips(hs, 1), 512, 0);
+    else if (c.down_waves == 4) run(mx4_small_kernel<kMx4Down, 1, 4, 4, 1>, strips(hs, 1), 256, 0);
+    else if (c.down_waves == 2) run(mx4_small_kernel<kMx4Down, 1, 4, 2, 1>, strips(hs, 2), 256, 0);
+    else run(mx4_small_kernel<kMx4Down, 1, 4, 1, 1>, strips(hs, 4), 256, 0);
+    auto combine = c.splits == 1 ? mx4_combine_kernel<1> : c.splits == 2 ? mx4_combine_kernel<2> : mx4_combine_kernel<4>;
+    dymoe_launch(ctx, DYMOE_K_MX4_ROWS, combine, dim3((unsigned)(T * ((H + 2047L) / 2048))), dim3(256), 0, st, (const float*)(ws + L.part), A.ldo, P,
+                 expert_plan<dymoe_expert_mx4>(plan, P).where, w, H, k, out_dtype, H % 4 == 0 && dymoe_aligned(y, 4 * dtype_bytes(out_dtype)), y);
     DYMOE_HIP_LAUNCH_CHECK();
     return DYMOE_OK;
 }

@@ -10,6 +10,8 @@ namespace dymoe {
 constexpr int kMx4TileCols = 256;     // columns of a tile of the weights: four matrix instructions
 constexpr int kMx4SmallRows = 32;     // token rows of a tile where experts meet few tokens: one fragment
 constexpr int kMx4TallRows = 128;     // and where they meet many
+constexpr size_t kMx4SplitPairs = 8192;   // pairs up to which they may be
+constexpr int kMx4MostSplits = 4;     // parts that the down projection's K is cut into at most
 
 static inline size_t mx4_round(size_t v, size_t m) { return (v + m - 1) / m * m; }
 
@@ -17,7 +19,7 @@ struct Mx4FfnLayout {
     size_t Hp, Fp;     // columns of the codes' rows: whole tiles
     size_t xq, xs;     // [T, Hp / 2] codes and [T, Hp / 32] exponents of the activations
     size_t hq, hs;     // [P, Fp / 2] and [P, Fp / 32] of the SwiGLU intermediate, by position (pairs sorted by expert)
-    size_t part;       // [P, H up to a multiple of 8] outputs of the pairs, by position, fp32
+    size_t part;       // parts of [P, H up to a multiple of 8] outputs of the pairs, by position, fp32
     size_t plan;       // int32, see ExpertPlan
     size_t total;
     int max_tiles;
@@ -36,7 +38,8 @@ static inline Mx4FfnLayout mx4_ffn_layout(long T, long H, long F, long E, long k
     L.xs = take((size_t)T * L.Hp / 32);
     L.hq = take(P * L.Fp / 2);
     L.hs = take(P * L.Fp / 32);
-    L.part = take(P * mx4_round((size_t)H, 8) * 4);
+    // (more than one part only where the pairs are few: see mx4_ffn_choice)
+    L.part = take((P <= kMx4SplitPairs ? kMx4MostSplits : 1) * P * mx4_round((size_t)H, 8) * 4);
     L.plan = take(expert_plan_bytes(P, (size_t)L.max_tiles));
     L.total = at;
     return L;

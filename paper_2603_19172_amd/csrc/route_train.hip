@@ -46,28 +46,33 @@ __device__ __forceinline__ float scaled_score(float l, float m, bool sigmoid)
 {
     if (l == -__builtin_inff()) return 0.0f;
     if (!sigmoid) return exp_neg(l - m);
-    return exp_neg(fminf(l, 0.0f) - fminf(m, 0.0f)) / (1.0f + exp_neg(-fabsf(l)));
+    return exp_neg(fminf(l, 0.0f) - fminf(m, 0.0f)) * __builtin_amdgcn_rcpf(1.0f + exp_neg(-fabsf(l)));
 }
 
 // 1 - s of a sigmoid
 __device__ __forceinline__ float rest_of(float l)
 {
     const float e = exp_neg(-fabsf(l));
-    return (l > 0.0f ? e : 1.0f) / (1.0f + e);
+    return (l > 0.0f ? e : 1.0f) * __builtin_amdgcn_rcpf(1.0f + e);
 }
 
 // The scores of a token, up to a common factor, and one over their sum (0 where there are none).  Returns whether one is no number.
 template <int NPL, int DT>
-__device__ __forceinline__ bool token_scores(const char* logits, long t, int E, int lane, bool sigmoid, float (&l)[NPL], float (&u)[NPL], float& m,
-                                             float& inv)
+__device__ __forceinline__ void load_token(const char* logits, long t, int E, int lane, float (&raw)[NPL])
 {
-    bool bad = false;
 #pragma unroll
     for (int i = 0; i < NPL; i++) {
         const int e = lane + 64 * i;
-        l[i] = -__builtin_inff();
-        if (e < E) l[i] = masked_logit<DT>(load_logit<DT>(logits, t * E + e), bad);
+        raw[i] = e < E ? load_logit<DT>(logits, t * E + e) : -__builtin_inff();
     }
+}
+
+template <int NPL, int DT>
+__device__ __forceinline__ bool token_scores(const float (&raw)[NPL], bool sigmoid, float (&l)[NPL], float (&u)[NPL], float& m, float& inv)
+{
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < NPL; i++) l[i] = masked_logit<DT>(raw[i], bad);
     m = l[0];
 #pragma unroll
     for (int i = 1; i < NPL; i++) m = fmaxf(m, l[i]);
@@ -80,7 +85,7 @@ __device__ __forceinline__ bool token_scores(const char* logits, long t, int E, 
         sum += u[i];
     }
     sum = wave_sum(sum);
-    inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+    inv = sum > 0.0f ? __builtin_amdgcn_rcpf(sum) : 0.0f;
     return __ballot(bad) != 0;
 }
 
@@ -96,9 +101,22 @@ __device__ __forceinline__ void balance_finish(const double* sums, const int* of
         double sum = 0.0;
         int c = 0;
         if (slice < slices || slices == 1) {
-            for (int g = slices > 1 ? slice : 0; g < groups && e <= E; g += slices) {
-                if (e < E) sum += sums[(long)g * E + e];
-                c += often[(long)g * (E + 1) + e];
+            // (eight workgroups' at a time: one after the other their loads cost 45 us for 256 of them)
+            const int first = slices > 1 ? slice : 0;
+            for (int g0 = first; g0 < groups && e <= E; g0 += 8 * slices) {
+                double v[8];
+                int n8[8];
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const int g = g0 + i * slices;
+                    v[i] = g < groups && e < E ? sums[(long)g * E + e] : 0.0;
+                    n8[i] = g < groups ? often[(long)g * (E + 1) + e] : 0;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    sum += v[i];
+                    c += n8[i];
+                }
             }
         }
         if (slices > 1) {
@@ -159,14 +177,27 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void route_balance_kernel(const
 #pragma unroll
     for (int i = 0; i < NPL; i++) acc[i] = 0.0;
     int tokens = 0;
-    for (long t = (long)blockIdx.x * kBalanceWaves + wave; t < T; t += (long)gridDim.x * kBalanceWaves) {
-        if (keep && keep[t] == 0) continue;
-        if (lane < k) {
-            const int e = idx[t * k + lane];
-            if ((unsigned)e < (unsigned)E) atomicAdd(&s_often[e], 1);
-        }
+    // the next token's loads are on their way while this one is worked on
+    float raw[NPL];
+    int chosen = -1, part = 1;
+    const long step = (long)gridDim.x * kBalanceWaves;
+    auto request = [&](long t) {
+        load_token<NPL, DT>(logits, t, E, lane, raw);
+        chosen = lane < k ? idx[t * k + lane] : -1;
+        part = keep ? keep[t] : 1;
+    };
+    long t = (long)blockIdx.x * kBalanceWaves + wave;
+    if (t < T) request(t);
+    for (; t < T; t += step) {
+        float now[NPL];
+#pragma unroll
+        for (int i = 0; i < NPL; i++) now[i] = raw[i];
+        const int e = chosen, in = part;
+        if (t + step < T) request(t + step);
+        if (in == 0) continue;
+        if ((unsigned)e < (unsigned)E) atomicAdd(&s_often[e], 1);
         float l[NPL], u[NPL], m, inv;
-        const bool bad = token_scores<NPL, DT>(logits, t, E, lane, sigmoid, l, u, m, inv);
+        const bool bad = token_scores<NPL, DT>(now, sigmoid, l, u, m, inv);
 #pragma unroll
         for (int i = 0; i < NPL; i++) acc[i] += bad ? (double)__builtin_nanf("") : (double)(u[i] * inv);
         tokens++;
@@ -255,8 +286,9 @@ __global__ __launch_bounds__(256) void route_grad_kernel(const RouteGradArgs A)
         for (int i = 0; i < NPL; i++) g[i] = lane + 64 * i < E ? c * (float)A.counts[lane + 64 * i] : 0.0f;
     }
     for (long t = (long)blockIdx.x * 4 + wave; t < A.T; t += (long)gridDim.x * 4) {
-        float l[NPL], u[NPL], m, inv;
-        bool bad = token_scores<NPL, DT>(A.logits, t, E, lane, sigmoid, l, u, m, inv);
+        float raw[NPL], l[NPL], u[NPL], m, inv;
+        load_token<NPL, DT>(A.logits, t, E, lane, raw);
+        bool bad = token_scores<NPL, DT>(raw, sigmoid, l, u, m, inv);
         float out[NPL];
 #pragma unroll
         for (int i = 0; i < NPL; i++) out[i] = 0.0f;
