@@ -36,15 +36,27 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const char* __restric
     Raw8<DT> v[CH];
 #pragma unroll
     for (int c = 0; c < CH; c++) v[c] = load8<DT>(src, at.col + c * S::kCols, real);
+    uint32_t bytes = 0;
 #pragma unroll
     for (int c = 0; c < CH; c++) {
         const long col = at.col + c * S::kCols;
         const uint32_t byte = mx4_exponent(quad_max_u32(peak_f32_bits<DT>(peak8<DT>(v[c], 0u))));
         const uint32_t q = mx4_codes8<DT>(v[c], byte);
+        if (TILES) bytes |= byte << (8 * c);
         if (col >= Kp || at.row >= out_rows) continue;
         *(DYMOE_GLOBAL uint32_t*)(codes + (TILES ? mx4_tile_byte(at.row, col, Kp) : (at.row * Kp + col) / 2)) = q;
-        if ((col & 31) == 0)
-            *(DYMOE_GLOBAL uint8_t*)(scale + (TILES ? mx4_tile_exponent(at.row, col, Kp) : (at.row * Kp + col) / 32)) = (uint8_t)byte;
+        if (!TILES && (col & 31) == 0) *(DYMOE_GLOBAL uint8_t*)(scale + (at.row * Kp + col) / 32) = (uint8_t)byte;
+    }
+    if constexpr (TILES) {
+        // four lanes hold the exponents of blocks 0, 2, 4, 6 of a row of the tile, the four beside them 1, 3, 5, 7: a word for each half of the tile
+        static_assert(CH * S::kCols == 256, "a tile at a time");
+        const int lane = threadIdx.x & (kWave - 1);
+        const uint32_t other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)bytes, 0x141, 0xF, 0xF, true);       // row_half_mirror: from the four beside
+        const bool upper = lane & 4;
+        const uint32_t even = upper ? other : bytes, odd = upper ? bytes : other;
+        const uint32_t word = __builtin_amdgcn_perm(odd, even, upper ? 0x07030602u : 0x05010400u);
+        if ((lane & 3) == 0 && at.row < out_rows)
+            *(DYMOE_GLOBAL uint32_t*)(scale + mx4_tile_exponent(at.row, at.col - (lane & 7) * 8 + (upper ? 128 : 0), Kp)) = word;
     }
 }
 

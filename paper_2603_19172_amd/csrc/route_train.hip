@@ -41,19 +41,15 @@ __device__ __forceinline__ float masked_logit(float v, bool& bad)
     return v > lowest ? v : -__builtin_inff();
 }
 
-// s e^(-min(m, 0)) of a sigmoid, e^(l - m) of a softmax
-__device__ __forceinline__ float scaled_score(float l, float m, bool sigmoid)
+// s e^(-min(m, 0)) of a sigmoid, e^(l - m) of a softmax; rest: 1 - s of a sigmoid, 1 of a softmax
+__device__ __forceinline__ float scaled_score(float l, float m, bool sigmoid, float& rest)
 {
-    if (l == -__builtin_inff()) return 0.0f;
-    if (!sigmoid) return exp_neg(l - m);
-    return exp_neg(fminf(l, 0.0f) - fminf(m, 0.0f)) * __builtin_amdgcn_rcpf(1.0f + exp_neg(-fabsf(l)));
-}
-
-// 1 - s of a sigmoid
-__device__ __forceinline__ float rest_of(float l)
-{
-    const float e = exp_neg(-fabsf(l));
-    return (l > 0.0f ? e : 1.0f) * __builtin_amdgcn_rcpf(1.0f + e);
+    const bool masked = l == -__builtin_inff();
+    rest = 1.0f;
+    if (!sigmoid) return masked ? 0.0f : exp_neg(l - m);
+    const float e = exp_neg(-fabsf(l)), one = __builtin_amdgcn_rcpf(1.0f + e);
+    rest = masked ? 0.0f : (l > 0.0f ? e : 1.0f) * one;
+    return masked ? 0.0f : exp_neg(fminf(l, 0.0f) - fminf(m, 0.0f)) * one;
 }
 
 // The scores of a token, up to a common factor, and one over their sum (0 where there are none).  Returns whether one is no number.
@@ -68,7 +64,8 @@ __device__ __forceinline__ void load_token(const char* logits, long t, int E, in
 }
 
 template <int NPL, int DT>
-__device__ __forceinline__ bool token_scores(const float (&raw)[NPL], bool sigmoid, float (&l)[NPL], float (&u)[NPL], float& m, float& inv)
+__device__ __forceinline__ bool token_scores(const float (&raw)[NPL], bool sigmoid, float (&l)[NPL], float (&u)[NPL], float (&rest)[NPL], float& m,
+                                             float& inv)
 {
     bool bad = false;
 #pragma unroll
@@ -81,80 +78,12 @@ __device__ __forceinline__ bool token_scores(const float (&raw)[NPL], bool sigmo
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < NPL; i++) {
-        u[i] = scaled_score(l[i], m, sigmoid);
+        u[i] = scaled_score(l[i], m, sigmoid, rest[i]);
         sum += u[i];
     }
     sum = wave_sum(sum);
     inv = sum > 0.0f ? __builtin_amdgcn_rcpf(sum) : 0.0f;
     return __ballot(bad) != 0;
-}
-
-// counts, means and the loss from the sums of `groups` workgroups, by one workgroup
-__device__ __forceinline__ void balance_finish(const double* sums, const int* often, int groups, int E, int k, float coef, int32_t* counts, float* mean,
-                                               float* loss, double* s_part, int* s_often)
-{
-    const int tid = threadIdx.x, n = blockDim.x;
-    const int slices = max(1, n / (E + 1)), slice = tid / (E + 1);
-    // expert E: the tokens that take part
-    for (int e0 = 0; e0 <= E; e0 += n) {
-        const int e = e0 + (slices > 1 ? tid - slice * (E + 1) : tid);
-        double sum = 0.0;
-        int c = 0;
-        if (slice < slices || slices == 1) {
-            // (eight workgroups' at a time: one after the other their loads cost 45 us for 256 of them)
-            const int first = slices > 1 ? slice : 0;
-            for (int g0 = first; g0 < groups && e <= E; g0 += 8 * slices) {
-                double v[8];
-                int n8[8];
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    const int g = g0 + i * slices;
-                    v[i] = g < groups && e < E ? sums[(long)g * E + e] : 0.0;
-                    n8[i] = g < groups ? often[(long)g * (E + 1) + e] : 0;
-                }
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    sum += v[i];
-                    c += n8[i];
-                }
-            }
-        }
-        if (slices > 1) {
-            s_part[tid] = sum;
-            s_often[tid] = c;
-            __syncthreads();
-            if (slice == 0 && e <= E) {
-                for (int s = 1; s < slices; s++) {
-                    sum += s_part[tid + s * (E + 1)];
-                    c += s_often[tid + s * (E + 1)];
-                }
-            }
-            __syncthreads();
-        }
-        if ((slices == 1 || slice == 0) && e <= E) {
-            counts[e] = c;
-            if (e < E) s_part[e] = sum;
-            s_often[e] = c;
-        }
-    }
-    __syncthreads();
-    const int tokens = s_often[E];
-    const double inv = tokens > 0 ? 1.0 / (double)tokens : 0.0;
-    double term = 0.0;
-    for (int e = tid; e < E; e += n) {
-        const double p = s_part[e] * inv;
-        mean[e] = (float)p;
-        term += (double)s_often[e] * p;
-    }
-    __syncthreads();
-    // the loss: lane by lane, then in LDS, in a fixed order
-    s_part[tid] = term;
-    __syncthreads();
-    for (int d = n / 2; d > 0; d /= 2) {
-        if (tid < d) s_part[tid] += s_part[tid + d];
-        __syncthreads();
-    }
-    if (tid == 0) *loss = (float)((double)coef * (double)E * inv / (double)k * s_part[0]);
 }
 
 constexpr int kBalanceFinish = 1024;      // threads of the second launch
@@ -165,7 +94,7 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void route_balance_kernel(const
                                                                            const uint8_t* __restrict__ keep, int T, int E, int k, int sigmoid,
                                                                            double* __restrict__ sums, int* __restrict__ often, float coef,
                                                                            int32_t* __restrict__ counts, float* __restrict__ mean,
-                                                                           float* __restrict__ loss)
+                                                                           float* __restrict__ loss, int* __restrict__ done)
 {
     constexpr int kHalf = kBalanceWaves / 2;
     __shared__ double s_sum[kHalf][64 * NPL < 128 ? 128 : 64 * NPL];
@@ -196,8 +125,8 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void route_balance_kernel(const
         if (t + step < T) request(t + step);
         if (in == 0) continue;
         if ((unsigned)e < (unsigned)E) atomicAdd(&s_often[e], 1);
-        float l[NPL], u[NPL], m, inv;
-        const bool bad = token_scores<NPL, DT>(now, sigmoid, l, u, m, inv);
+        float l[NPL], u[NPL], rest[NPL], m, inv;
+        const bool bad = token_scores<NPL, DT>(now, sigmoid, l, u, rest, m, inv);
 #pragma unroll
         for (int i = 0; i < NPL; i++) acc[i] += bad ? (double)__builtin_nanf("") : (double)(u[i] * inv);
         tokens++;
@@ -221,6 +150,7 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void route_balance_kernel(const
         else sums[(long)blockIdx.x * E + e] = sum;
     }
     if (!ONE) {
+        if (blockIdx.x == 0 && tid == 0) *done = 0;       // (for the launch behind this one)
         for (int e = tid; e <= E; e += blockDim.x) often[(long)blockIdx.x * (E + 1) + e] = s_often[e];
         return;
     }
@@ -246,13 +176,77 @@ __global__ __launch_bounds__(64 * kBalanceWaves) void route_balance_kernel(const
     if (tid == 0) *loss = (float)((double)coef * (double)E * inv / (double)k * s_term[0]);
 }
 
+// Counts, means and the loss from the sums of `groups` workgroups: a workgroup joins them for 32 experts, 32 threads each; the one that comes last adds
+// up the workgroups' shares of the loss.  (By one workgroup for all experts, 256 of them and 256 workgroups' sums took 46 us one after
+// the other and 14 us eight at a time: its chain of loads.)
 __global__ __launch_bounds__(kBalanceFinish) void route_balance_finish_kernel(const double* __restrict__ sums, const int* __restrict__ often, int groups,
                                                                               int E, int k, float coef, int32_t* __restrict__ counts,
-                                                                              float* __restrict__ mean, float* __restrict__ loss)
+                                                                              float* __restrict__ mean, float* __restrict__ loss,
+                                                                              double* __restrict__ terms, int* __restrict__ done)
 {
-    __shared__ double s_part[kBalanceFinish];
-    __shared__ int s_often[kBalanceFinish + 1];
-    balance_finish(sums, often, groups, E, k, coef, counts, mean, loss, s_part, s_often);
+    __shared__ double s_sum[32][33];
+    __shared__ int s_often[32][33], s_tokens[kBalanceFinish / kWave];
+    static_assert(kBalanceGroups <= 8 * 32 && kBalanceFinish == 32 * 32, "eight workgroups' sums a thread");
+    const int tid = threadIdx.x, col = tid & 31, slice = tid >> 5, e = blockIdx.x * 32 + col;
+    double v[8];
+    int n[8], tokens = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const int g = slice + 32 * i;
+        const bool in = g < groups && e < E;
+        v[i] = in ? sums[(long)g * E + e] : 0.0;
+        n[i] = in ? often[(long)g * (E + 1) + e] : 0;
+    }
+    if (tid < groups) tokens = often[(long)tid * (E + 1) + E];
+    double sum = v[0];
+    int c = n[0];
+#pragma unroll
+    for (int i = 1; i < 8; i++) {
+        sum += v[i];
+        c += n[i];
+    }
+    s_sum[slice][col] = sum;
+    s_often[slice][col] = c;
+    tokens = wave_sum_dpp_i32(tokens);
+    if ((tid & (kWave - 1)) == 0) s_tokens[tid / kWave] = tokens;
+    __syncthreads();
+    if (tid < kWave) {
+        tokens = 0;
+        for (int w = 0; w < kBalanceFinish / kWave; w++) tokens += s_tokens[w];
+        const double inv = tokens > 0 ? 1.0 / (double)tokens : 0.0;
+        double term = 0.0;
+        if (tid < 32 && e < E) {
+            sum = s_sum[0][col];
+            c = s_often[0][col];
+            for (int i = 1; i < 32; i++) {
+                sum += s_sum[i][col];
+                c += s_often[i][col];
+            }
+            counts[e] = c;
+            const double p = sum * inv;
+            mean[e] = (float)p;
+            term = (double)c * p;
+        }
+        if (tid == 0 && blockIdx.x == 0) counts[E] = tokens;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) term += __shfl_xor(term, o, kWave);
+        if (tid == 0) {
+            __hip_atomic_store(&terms[blockIdx.x], term, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            const bool last = __hip_atomic_fetch_add(done, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+            if (last) {
+                double all = 0.0;
+                for (unsigned w = 0; w < gridDim.x; w++) all += __hip_atomic_load(&terms[w], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                *loss = (float)((double)coef * (double)E * inv / (double)k * all);
+            }
+        }
+    }
+}
+
+// Between a wavefront's LDS accesses that other lanes' are ordered with: nothing to wait for, but the compiler may not carry values across.
+__device__ __forceinline__ void lds_in_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 }
 
 struct RouteGradArgs {
@@ -274,6 +268,7 @@ struct RouteGradArgs {
 template <int NPL, int DT>
 __global__ __launch_bounds__(256) void route_grad_kernel(const RouteGradArgs A)
 {
+    __shared__ float s_area[4][64 * NPL];
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, E = A.E, k = A.k;
     const bool sigmoid = A.sigmoid;
     float g[NPL];
@@ -286,9 +281,19 @@ __global__ __launch_bounds__(256) void route_grad_kernel(const RouteGradArgs A)
         for (int i = 0; i < NPL; i++) g[i] = lane + 64 * i < E ? c * (float)A.counts[lane + 64 * i] : 0.0f;
     }
     for (long t = (long)blockIdx.x * 4 + wave; t < A.T; t += (long)gridDim.x * 4) {
-        float raw[NPL], l[NPL], u[NPL], m, inv;
+        float raw[NPL], l[NPL], u[NPL], rest[NPL], m, inv;
         load_token<NPL, DT>(A.logits, t, E, lane, raw);
-        bool bad = token_scores<NPL, DT>(raw, sigmoid, l, u, m, inv);
+        // (a slot's loads are on their way beside them)
+        int e = -1;
+        float dw = 0.0f, x = -__builtin_inff();
+        bool ignored = false;
+        if (A.dw && lane < k) {
+            e = A.idx[t * k + lane];
+            dw = A.dw[t * k + lane];
+            if ((unsigned)e >= (unsigned)E) e = -1;
+            else x = masked_logit<DT>(load_logit<DT>(A.logits, t * E + e), ignored);
+        }
+        bool bad = token_scores<NPL, DT>(raw, sigmoid, l, u, rest, m, inv);
         float out[NPL];
 #pragma unroll
         for (int i = 0; i < NPL; i++) out[i] = 0.0f;
@@ -302,38 +307,43 @@ __global__ __launch_bounds__(256) void route_grad_kernel(const RouteGradArgs A)
             for (int i = 0; i < NPL; i++) out[i] = u[i] * inv * (g[i] - dot);
         }
         if (A.dw) {
-            int e = -1;
-            float x = -__builtin_inff(), dw = 0.0f;
-            if (lane < k) {
-                e = A.idx[t * k + lane];
-                bool ignored = false;
-                if ((unsigned)e < (unsigned)E) {
-                    x = masked_logit<DT>(load_logit<DT>(A.logits, t * E + e), ignored);
-                    dw = A.dw[t * k + lane];
-                } else {
-                    e = -1;
-                }
-            }
-            float v, row = 0.0f;
+            float v, row = 0.0f, unused;
             if (A.renorm) {
-                const float top = wave_max_dpp(x), s = scaled_score(x, top, sigmoid), sum = wave_sum(s);
+                const float top = wave_max_dpp(x), s = scaled_score(x, top, sigmoid, unused), sum = wave_sum(s);
                 const float q = sum > 0.0f ? s / sum : 0.0f;
                 const float dot = wave_sum(q != 0.0f ? q * dw : 0.0f);
                 v = q != 0.0f ? A.factor * (q * (dw - dot)) : 0.0f;
             } else if (sigmoid) {
-                v = x > -__builtin_inff() ? A.factor * (scaled_score(x, 0.0f, true) * dw) : 0.0f;
+                v = x > -__builtin_inff() ? A.factor * (scaled_score(x, 0.0f, true, unused) * dw) : 0.0f;
             } else {
-                const float s = scaled_score(x, m, false) * inv;
+                const float s = scaled_score(x, m, false, unused) * inv;
                 const float one = s != 0.0f ? s * dw : 0.0f;
                 v = A.factor * one;
                 row = A.factor * wave_sum(one);
             }
-            // to the lanes that hold the experts
-            for (int j = 0; j < k; j++) {
-                const int to = __builtin_amdgcn_readlane(e, j);
-                const float add = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), j));
+            // To the lanes that hold the experts, through an LDS area of the wavefront's own (its LDS accesses execute in order).  An expert in
+            // several slots (a slot finds another's number where it left its own): their sum, slot after slot.
+            float* const area = s_area[wave];
+            if (e >= 0) area[e] = __int_as_float(lane);
+            lds_in_order();
+            const bool again = e >= 0 && __float_as_int(area[max(e, 0)]) != lane;
+            if (__ballot(again) == 0) {
+                lds_in_order();
 #pragma unroll
-                for (int i = 0; i < NPL; i++) out[i] += to == lane + 64 * i ? add : 0.0f;
+                for (int i = 0; i < NPL; i++) area[lane + 64 * i] = 0.0f;
+                lds_in_order();
+                if (e >= 0) area[e] = v;
+                lds_in_order();
+#pragma unroll
+                for (int i = 0; i < NPL; i++) out[i] += area[lane + 64 * i];
+                lds_in_order();
+            } else {
+                for (int j = 0; j < k; j++) {
+                    const int to = __builtin_amdgcn_readlane(e, j);
+                    const float add = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), j));
+#pragma unroll
+                    for (int i = 0; i < NPL; i++) out[i] += to == lane + 64 * i ? add : 0.0f;
+                }
             }
             if (row != 0.0f) {
 #pragma unroll
@@ -343,11 +353,9 @@ __global__ __launch_bounds__(256) void route_grad_kernel(const RouteGradArgs A)
         bad = bad && (part || A.dw);
 #pragma unroll
         for (int i = 0; i < NPL; i++) {
-            const int e = lane + 64 * i;
-            if (e >= E) continue;
-            float v = out[i];
-            if (sigmoid) v = l[i] == -__builtin_inff() ? 0.0f : v * rest_of(l[i]);
-            store_out(A.grad, t * E + e, A.grad_dtype, bad ? __builtin_nanf("") : v);
+            const int to = lane + 64 * i;
+            if (to >= E) continue;
+            store_out(A.grad, t * E + to, A.grad_dtype, bad ? __builtin_nanf("") : out[i] * rest[i]);
         }
     }
 }
@@ -355,7 +363,7 @@ __global__ __launch_bounds__(256) void route_grad_kernel(const RouteGradArgs A)
 static long balance_groups(long T) { return T <= kBalanceOne ? 1 : T < kBalanceGroups * (long)kBalanceWaves ? (T + kBalanceWaves - 1) / kBalanceWaves : kBalanceGroups; }
 
 struct BalanceLayout {
-    size_t sums, often, total;
+    size_t sums, often, terms, done, total;
 };
 
 static BalanceLayout balance_layout(long T, long E)
@@ -364,7 +372,9 @@ static BalanceLayout balance_layout(long T, long E)
     const size_t g = (size_t)balance_groups(T);
     L.sums = 0;
     L.often = g * (size_t)E * 8;
-    L.total = (L.often + g * (size_t)(E + 1) * 4 + 255) / 256 * 256;
+    L.terms = (L.often + g * (size_t)(E + 1) * 4 + 7) / 8 * 8;
+    L.done = L.terms + (size_t)(E + 31) / 32 * 8;
+    L.total = (L.done + 4 + 255) / 256 * 256;
     return L;
 }
 
@@ -375,12 +385,12 @@ static void route_balance_launch(dymoe_ctx* ctx, const void* logits, const int32
     const int groups = (int)balance_groups(T);
     const BalanceLayout L = balance_layout(T, E);
     double* const sums = (double*)(ws + L.sums);
-    int* const often = (int*)(ws + L.often);
+    int *const often = (int*)(ws + L.often), *const done = (int*)(ws + L.done);
 #define DYMOE_BALANCE(NPL)                                                                                                              \
     do {                                                                                                                                \
         auto kernel = groups == 1 ? route_balance_kernel<NPL, DT, true> : route_balance_kernel<NPL, DT, false>;                          \
         dymoe_launch(ctx, DYMOE_K_ROUTE_BALANCE, kernel, dim3((unsigned)groups), dim3(64 * kBalanceWaves), 0, st, (const char*)logits,   \
-                     idx, keep, T, E, k, sigmoid, sums, often, coef, counts, mean, loss);                                                \
+                     idx, keep, T, E, k, sigmoid, sums, often, coef, counts, mean, loss, done);                                          \
     } while (0)
     if (E <= 64) DYMOE_BALANCE(1);
     else if (E <= 128) DYMOE_BALANCE(2);
@@ -389,8 +399,8 @@ static void route_balance_launch(dymoe_ctx* ctx, const void* logits, const int32
     else DYMOE_BALANCE(16);
 #undef DYMOE_BALANCE
     if (groups > 1)
-        dymoe_launch(ctx, DYMOE_K_ROUTE_BALANCE, route_balance_finish_kernel, dim3(1), dim3(kBalanceFinish), 0, st, sums, often, groups, E, k, coef, counts,
-                     mean, loss);
+        dymoe_launch(ctx, DYMOE_K_ROUTE_BALANCE, route_balance_finish_kernel, dim3((unsigned)((E + 31) / 32)), dim3(kBalanceFinish), 0, st, sums, often, groups, E, k,
+                     coef, counts, mean, loss, (double*)(ws + L.terms), done);
 }
 
 template <int DT>
