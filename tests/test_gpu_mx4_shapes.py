@@ -25,7 +25,7 @@ TALL = [(200, 264, 1000, 2, 1, 1), (300, 700, 520, 4, 2, 1), (200, 264, 2100, 2,
         (420, 520, 256, 2, 2, 1)]
 
 # T, H, F, E, k, waves of the up and of the down projection: experts in strips
-STRIPS = [(20, 1100, 300, 6, 2, 4, 2), (5, 300, 2500, 4, 2, 2, 8), (30, 200, 70, 40, 8, 1, 1), (9, 640, 1100, 4, 2, 2, 4), (250, 1100, 2300, 60, 4, 1, 1)]
+STRIPS = [(20, 1100, 300, 6, 2, 4, 2), (5, 300, 2500, 4, 2, 2, 8), (30, 200, 70, 40, 8, 1, 1), (9, 640, 1100, 4, 2, 2, 4), (250, 800, 1300, 60, 4, 1, 1)]
 
 # T, H, F, E, k: a few pairs
 THIN = [(1, 4096, 1000, 2, 2), (2, 1030, 3100, 4, 2), (1, 270, 300, 64, 64), (4, 520, 770, 128, 8), (8, 256, 256, 64, 2), (1, 100, 14336, 3, 1)]
@@ -117,3 +117,72 @@ def test_a_long_rows_products(ctx):  # noqa: F811
         x = G.randn(T, T, K)
         prod, bound = Q.matmul(Q.values(*Q.quantize(G.f64(x))), wv)
         G.close(ctx.matmul_mx4(x, wt, out_dtype=B.OUT_F32), prod, bound, torch.float32)
+
+
+@pytest.mark.parametrize("T,N", [(1, 160), (40, 160), (300, 160), (1500, 5000)])
+def test_products_at_the_ends_of_the_range(ctx, T, N):  # noqa: F811
+    """One sum of 512 equal products: subnormal ones are kept, those beyond the range are infinite, zeros stay zeros beside any power of two."""
+    K = 512
+    x, w = torch.ones((T, K), device=DEV), torch.ones((N, K), device=DEV)
+    w[1], w[2], w[3, ::2] = 0.0, -1.0, -1.0
+    for ex, ew in ((-70, -60), (-75, -70), (-100, -100), (60, 60), (100, 100), (-126, 120)):
+        y = ctx.matmul_mx4(x * 2.0 ** ex, ctx.quantize_mx4(w * 2.0 ** ew, layout=B.LAYOUT_TILE), out_dtype=B.OUT_F32)
+        want = torch.full((N,), 512 * 2.0 ** ex * 2.0 ** ew, dtype=torch.float64).float()
+        want[1], want[2], want[3] = 0.0, -want[2], 0.0
+        assert torch.equal(y, want.to(DEV).expand(T, N)), (ex, ew)
+
+
+@pytest.mark.parametrize("T", [2, 40, 300])
+def test_calls_at_once_on_two_streams(ctx, T):  # noqa: F811
+    """Workspaces of their own: nothing else is shared."""
+    H, F, E, k = 256, 512, 8, 2
+    ex, _ = G.make_experts(ctx, 25, E, H, F)
+    wt, _ = G.weight(ctx, 26, 400, H)
+    x, logits = G.randn(27, T, H), G.randn(28, T, E, dtype=torch.float32)
+    idx, gate = G.choices(28, T, E, k)
+    calls = (lambda: ctx.moe_ffn_mx4(x, idx, gate, ex.table, F), lambda: ctx.matmul_mx4(x, wt),
+             lambda: ctx.route_balance(logits, idx, 0.1)[1], lambda: ctx.dequantize_mx4(ctx.quantize_mx4(x)))
+    want = [c() for c in calls]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    for i in range(24):
+        with torch.cuda.stream(streams[i % 2]):
+            got.append(calls[(i + i // 4) % 4]())
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want[(i + i // 4) % 4]) for i, y in enumerate(got))
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_memory_of_a_call_belongs_to_its_stream(ctx, monkeypatch, handle):  # noqa: F811
+    """What a call on another stream allocates is not given to the current stream's work before the call has run."""
+    x, wt = G.randn(3, 200, 512), G.weight(ctx, 9, 300, 512)[0]
+    ex, _ = G.make_experts(ctx, 9, 4, 512, 256)
+    idx, gate = G.choices(9, 200, 4, 2)
+    logits = G.randn(4, 200, 4, dtype=torch.float32)
+    want = ctx.matmul_mx4(x, wt), ctx.moe_ffn_mx4(x, idx, gate, ex.table, 256), ctx.route_balance(logits, idx, 0.1)[1]
+    taken, empty = [], B._empty
+
+    def spy(shape, dtype, device, stream):
+        t = empty(shape, dtype, device, stream)
+        taken.append((t.data_ptr(), t.numel(), dtype))
+        return t
+    monkeypatch.setattr(B, "_empty", spy)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    stream = s.cuda_stream if handle else s
+    got = (ctx.matmul_mx4(x, wt, stream=stream), ctx.moe_ffn_mx4(x, idx, gate, ex.table, 256, stream=stream),
+           ctx.route_balance(logits, idx, 0.1, stream=stream)[1])
+    assert len(taken) == 2 + 2 + 4
+    for ptr, n, dtype in taken:
+        assert all(torch.empty(n, dtype=dtype, device=DEV).data_ptr() != ptr for _ in range(2))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_tensors_on_another_device_are_refused(ctx):  # noqa: F811
+    x, wt = G.randn(3, 8, 512), G.weight(ctx, 9, 32, 512)[0]
+    for call in (lambda: ctx.matmul_mx4(x.cpu(), wt), lambda: ctx.matmul_mx4(x, wt._replace(codes=wt.codes.cpu())), lambda: ctx.quantize_mx4(x.cpu()),
+                 lambda: ctx.dequantize_mx4(wt._replace(scale=wt.scale.cpu())), lambda: ctx.matmul_mx4(x, wt, bias=torch.zeros(32)),
+                 lambda: ctx.route_balance(x.float(), torch.zeros((8, 2), dtype=torch.int32), 0.1)):
+        with pytest.raises(ValueError, match="device"):
+            call()

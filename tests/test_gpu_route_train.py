@@ -255,3 +255,26 @@ def test_rows_behind_the_last_are_left(ctx):
     counts = torch.full((E + 3,), 7, dtype=torch.int32, device=DEV)
     ctx.route_balance(logits, idx, 0.1, counts=counts[:E + 1])
     assert (grad[T:] == 7).all() and (counts[E + 1:] == 7).all()
+
+
+def test_as_many_tokens_as_the_calls_take(ctx):
+    T, E = (1 << 25) - 1, 2
+    logits = torch.zeros((T, E), dtype=torch.bfloat16, device=DEV)
+    logits[::4, 1] = 1.0
+    idx = (torch.arange(T, device=DEV) % 4 == 0).to(torch.int32)[:, None].contiguous()
+    counts, mean, loss = ctx.route_balance(logits, idx, 1.0, score=B.SCORE_SOFTMAX)
+    many = -(-T // 4)
+    assert counts.tolist() == [T - many, many, T]
+    p = math.e / (1.0 + math.e)
+    want = [((T - many) * 0.5 + many * (1 - p)) / T, ((T - many) * 0.5 + many * p) / T]
+    assert all(abs(float(m) - w) <= EPS * w for m, w in zip(mean, want))
+    assert abs(float(loss) - 2 * ((T - many) / T * want[0] + many / T * want[1])) <= 2 * EPS
+    dw = torch.ones((T, 1), device=DEV)
+    grad = ctx.route_scored_backward(logits, idx, dw=dw, score=B.SCORE_SOFTMAX, renorm=False)
+    for i in (0, 1, T // 2 // 4 * 4, T - 1):
+        q = p if i % 4 == 0 else 0.5
+        g = q * (1 - q)
+        w = [-g, g] if i % 4 == 0 else [g, -g]
+        assert all(abs(float(a) - b) <= (3 * EPS + 2.0 ** -8) * g for a, b in zip(grad[i], w))
+    for r in (0, 1, 2, 3):
+        assert (grad[r::4] == grad[r]).all()
