@@ -55,6 +55,26 @@ __device__ __forceinline__ uint32_t quad_max_u32(uint32_t v)
 template <int DT>
 __device__ __forceinline__ uint32_t peak_f32_bits(uint32_t m) { return __float_as_uint(peak_value<DT>(peak_bits<DT>(m))); }
 
+// 8 and 16 bytes at an address of any alignment (rows of an odd number of 16-bit values), stored at once
+typedef uint32_t any8_t __attribute__((ext_vector_type(2), aligned(2)));
+
+// Four neighbouring outputs of a row, `left` of them inside it
+__device__ __forceinline__ void store_any4(void* out, long at, int dt, int left, const float (&v)[4])
+{
+    if (left < 4) {
+#pragma unroll
+        for (int i = 0; i < 3; i++)
+            if (i < left) store_out(out, at + i, dt, v[i]);
+    } else if (dt == DYMOE_OUT_F32) {
+        *(DYMOE_GLOBAL any16_t*)((float*)out + at) = any16_t{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    } else if (dt == DYMOE_OUT_F16) {
+        *(DYMOE_GLOBAL any8_t*)((uint16_t*)out + at) = any8_t{pack_half2(v[0], v[1]), pack_half2(v[2], v[3])};
+    } else {
+        const bf16x2_t a = {(__bf16)v[0], (__bf16)v[1]}, b = {(__bf16)v[2], (__bf16)v[3]};
+        *(DYMOE_GLOBAL any8_t*)((uint16_t*)out + at) = any8_t{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
+    }
+}
+
 // byte of a tile-layout matrix that holds code (row, col), col a multiple of 2; and that of the exponent of the block of (row, col)
 __device__ __forceinline__ long mx4_tile_byte(long row, long col, long Kp)
 {

@@ -53,7 +53,7 @@ struct Mx4Args {
     void* out;                        // up: codes of the intermediate's rows, ldo / 2 bytes each
     uint8_t* out_scale;               // up: their exponents, ldo / 32
     long ldo, P;
-    int rows, Kp, N, k, out_dtype, aligned;     // aligned: the plain product's rows start where four outputs may be stored at once
+    int rows, Kp, N, k, out_dtype;
     int splits;                       // tall tiles of the down projection: parts of K, P rows of outputs each
 };
 
@@ -346,8 +346,7 @@ __global__ __launch_bounds__(64 * NW) void mx4_small_kernel(const Mx4Args A)
                     v[i] = sum[0][f][4 * g + i];
                     if (MODE == kMx4Plain && A.bias) v[i] += A.bias[min(n + i, A.N - 1)];
                 }
-                const bool whole = left >= 4 && (MODE != kMx4Plain || A.aligned);
-                store_out4(A.out, (long)(row0 + row) * A.ldo + n, MODE == kMx4Plain ? A.out_dtype : DYMOE_OUT_F32, whole, left, v);
+                store_any4(A.out, (long)(row0 + row) * A.ldo + n, MODE == kMx4Plain ? A.out_dtype : DYMOE_OUT_F32, left, v);
             }
         }
     }
@@ -647,7 +646,6 @@ __device__ __forceinline__ void mx4_tile(const Mx4Args& A, const int32_t* perm, 
         // the wavefront turns a fragment round in an LDS area of its own, so that a row leaves in whole lines
         constexpr int kOut = 8 * S;                 // lanes to a row of the wavefront's 32 S sums
         const uint32_t area = base + (uint32_t)wave * kMx4EpiWave<S>, wr = area + (uint32_t)ln * kMx4EpiRow<S> + (uint32_t)kb * 16u;
-        const bool vec = MODE != kMx4Plain || A.aligned;
         const int dt = MODE == kMx4Plain ? A.out_dtype : DYMOE_OUT_F32;
         const int n = (4 * bx + wave) * 32 * S + 4 * (lane & (kOut - 1)), left = A.N - n;
         float add[4] = {0.f, 0.f, 0.f, 0.f};
@@ -670,7 +668,7 @@ __device__ __forceinline__ void mx4_tile(const Mx4Args& A, const int32_t* perm, 
                 const uint4 u = lds_read16(area + (uint32_t)rr * kMx4EpiRow<S> + (uint32_t)(lane & (kOut - 1)) * 16u);
                 if (row >= rows || left <= 0) continue;
                 const float v[4] = {__uint_as_float(u.x) + add[0], __uint_as_float(u.y) + add[1], __uint_as_float(u.z) + add[2], __uint_as_float(u.w) + add[3]};
-                store_out4(out, (long)(row0 + row) * A.ldo + n, dt, left >= 4 && vec, left, v);
+                store_any4(out, (long)(row0 + row) * A.ldo + n, dt, left, v);
             }
         }
     }
@@ -768,8 +766,7 @@ int mx4_init()
 // token.  Bound by the pairs' bytes: 16376 pairs of 2048 outputs 21.5 us (6.2 TB/s).
 template <int PARTS>
 __global__ __launch_bounds__(256) void mx4_combine_kernel(const float* __restrict__ part, long ldp, long P, const int32_t* __restrict__ where,
-                                                          const float* __restrict__ gate, int H, int k, int out_dtype, int aligned,
-                                                          void* __restrict__ y)
+                                                          const float* __restrict__ gate, int H, int k, int out_dtype, void* __restrict__ y)
 {
     const int blocks = (H + 2047) / 2048;
     const long t = blockIdx.x / blocks;
@@ -795,8 +792,8 @@ __global__ __launch_bounds__(256) void mx4_combine_kernel(const float* __restric
         for (int i = 0; i < 8; i++) sum[i] = fmaf(g, v[i], sum[i]);
     }
     const float lo[4] = {sum[0], sum[1], sum[2], sum[3]}, hi[4] = {sum[4], sum[5], sum[6], sum[7]};
-    store_out4(y, t * H + h, out_dtype, aligned && h + 4 <= H, H - h, lo);
-    store_out4(y, t * H + h + 4, out_dtype, aligned && h + 8 <= H, H - h - 4, hi);
+    store_any4(y, t * H + h, out_dtype, H - h, lo);
+    store_any4(y, t * H + h + 4, out_dtype, H - h - 4, hi);
 }
 
 // a launch's threads have to stay below 2^32
@@ -857,7 +854,6 @@ extern "C" int dymoe_matmul_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, cons
     A.Kp = (int)L.Kp;
     A.N = N;
     A.out_dtype = out_dtype;
-    A.aligned = dymoe_aligned(y, 4 * dtype_bytes(out_dtype)) && ldy % 4 == 0;
     const long n128 = (N + 127L) / 128, n256 = (N + 255L) / 256;
     auto run = [&](void (*kernel)(const Mx4Args), dim3 grid, int threads, int lds) {
         dymoe_launch(ctx, DYMOE_K_MX4_PRODUCT, kernel, grid, dim3((unsigned)threads), lds, st, A);
@@ -973,7 +969,7 @@ extern "C" int dymoe_moe_ffn_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, con
     else run(mx4_small_kernel<kMx4Down, 1, 4, 1, 1>, strips(hs, 4), 256, 0);
     auto combine = c.splits == 1 ? mx4_combine_kernel<1> : c.splits == 2 ? mx4_combine_kernel<2> : mx4_combine_kernel<4>;
     dymoe_launch(ctx, DYMOE_K_MX4_ROWS, combine, dim3((unsigned)(T * ((H + 2047L) / 2048))), dim3(256), 0, st, (const float*)(ws + L.part), A.ldo, P,
-                 expert_plan<dymoe_expert_mx4>(plan, P).where, w, H, k, out_dtype, H % 4 == 0 && dymoe_aligned(y, 4 * dtype_bytes(out_dtype)), y);
+                 expert_plan<dymoe_expert_mx4>(plan, P).where, w, H, k, out_dtype, y);
     DYMOE_HIP_LAUNCH_CHECK();
     return DYMOE_OK;
 }

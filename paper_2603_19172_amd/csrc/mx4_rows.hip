@@ -70,17 +70,22 @@ __device__ __forceinline__ float mx4_value(uint32_t q, int i, float unit, bool n
     return number ? s * unit : __builtin_nanf("");
 }
 
+// eight values of a row, `left` of them inside it (a stream that this kernel does not read again: non-temporal, 8191 rows of 14336 53 us and 70)
 template <int DT>
-__device__ __forceinline__ void mx4_store8(void* y, long at, int left, bool whole, const float (&v)[8])
+__device__ __forceinline__ void mx4_store8(void* y, long at, int left, const float (&v)[8])
 {
-    const float lo[4] = {v[0], v[1], v[2], v[3]}, hi[4] = {v[4], v[5], v[6], v[7]};
-    // (a stream that this kernel does not read again: non-temporal, 8191 rows of 14336 53 us and 70)
-    if (whole && left >= 8 && DT == DYMOE_OUT_F32) {
-        store_global_nt((float*)y + at, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
-        store_global_nt((float*)y + at + 4, make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])));
+    if (left < 8) {
+#pragma unroll
+        for (int i = 0; i < 7; i++)
+            if (i < left) store_out(y, at + i, DT, v[i]);
         return;
     }
-    if (whole && left >= 8) {
+    if constexpr (DT == DYMOE_OUT_F32) {
+#pragma unroll
+        for (int i = 0; i < 8; i += 4)
+            __builtin_nontemporal_store(any16_t{__float_as_uint(v[i]), __float_as_uint(v[i + 1]), __float_as_uint(v[i + 2]), __float_as_uint(v[i + 3])},
+                                        (DYMOE_GLOBAL any16_t*)((float*)y + at + i));
+    } else {
         uint32_t u[4];
 #pragma unroll
         for (int i = 0; i < 4; i++) {
@@ -90,16 +95,13 @@ __device__ __forceinline__ void mx4_store8(void* y, long at, int left, bool whol
                 u[i] = __builtin_bit_cast(uint32_t, b);
             }
         }
-        store_global_nt((uint16_t*)y + at, make_uint4(u[0], u[1], u[2], u[3]));
-        return;
+        __builtin_nontemporal_store(any16_t{u[0], u[1], u[2], u[3]}, (DYMOE_GLOBAL any16_t*)((uint16_t*)y + at));
     }
-    store_out4(y, at, DT, whole && left >= 4, left, lo);
-    store_out4(y, at + 4, DT, whole && left >= 8, left - 4, hi);
 }
 
 template <int DT, int TILES, int CH>
 __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scale, long rows, int K,
-                                                             long units, int per_row, void* __restrict__ y, long ldy, int whole)
+                                                             long units, int per_row, void* __restrict__ y, long ldy)
 {
     using S = Mx4Spread<TILES>;
     const long unit = (long)blockIdx.x * 4 + threadIdx.x / kWave;
@@ -123,7 +125,7 @@ __global__ __launch_bounds__(256) void mx4_dequantize_kernel(const uint8_t* __re
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; i++) v[i] = mx4_value(q[c], i, unit2, e[c] != 255u);
-        mx4_store8<DT>(y, at.row * ldy + col, (int)(K - col), whole, v);
+        mx4_store8<DT>(y, at.row * ldy + col, (int)(K - col), v);
     }
 }
 
@@ -170,11 +172,10 @@ static int mx4_dequantize_launch(dymoe_ctx* ctx, const uint8_t* codes, const uin
     const long Kp = up_to(K, 256);
     const int per_row = (int)((Kp + CH * S::kCols - 1) / (CH * S::kCols));
     const long step = mx4_rows_launch(rows, TILES, per_row);
-    const int whole = dymoe_aligned(y, 16) && ldy * dtype_bytes(DT) % 16 == 0;
     for (long r = 0; r < rows; r += step) {
         const long n = rows - r < step ? rows - r : step, units = (n + S::kRows - 1) / S::kRows * per_row;
         dymoe_launch(ctx, DYMOE_K_MX4_ROWS, mx4_dequantize_kernel<DT, TILES, CH>, dim3((unsigned)((units + 3) / 4)), dim3(256), 0, st,
-                     codes + r * Kp / 2, scale + r * Kp / 32, n, (int)K, units, per_row, (char*)y + r * ldy * dtype_bytes(DT), ldy, whole);
+                     codes + r * Kp / 2, scale + r * Kp / 32, n, (int)K, units, per_row, (char*)y + r * ldy * dtype_bytes(DT), ldy);
     }
     DYMOE_HIP_LAUNCH_CHECK();
     return DYMOE_OK;
