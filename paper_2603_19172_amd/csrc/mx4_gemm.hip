@@ -362,7 +362,7 @@ template <int D>
 __global__ __launch_bounds__(64 * kMx4LastWaves) void mx4_thin_down_kernel(const Mx4Args A)
 {
     extern __shared__ __attribute__((aligned(16))) char s_rows[];
-    __shared__ float s_sum[kMx4LastWaves][16];
+    __shared__ float s_sum[kMx4LastWaves][16], s_gate[64];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     // the workgroups of one strip go to one XCD, whose L2 then has the weights that several tokens need
     const int nblk = (A.N + 15) / 16, j = blockIdx.x >> 3;
@@ -398,13 +398,15 @@ __global__ __launch_bounds__(64 * kMx4LastWaves) void mx4_thin_down_kernel(const
     if (first < last) open(ask_slot);
 #pragma unroll
     for (int d = 0; d < D; d++) request(ring[d]);
-    // the pairs' codes and exponents; zeros for one that is left out, whose row nobody wrote
+    // the pairs' codes and exponents; zeros for one that is left out, whose row nobody wrote and whose weight may be no number
     const int per = A.Kp >> 5, exps = k * mx4_lds_row(A.Kp);             // 16-byte chunks of a row's codes, and bytes of its exponents
     for (int i = tid; i < k * per; i += 64 * kMx4LastWaves) {
         const int slot = i / per, c = i - slot * per, pair = t * k + slot, e = A.idx[pair];
         uint4 q = make_uint4(0, 0, 0, 0);
         uint8_t x = 0;
-        if ((unsigned)e < (unsigned)A.E && expert_present(A.table[e])) {
+        const bool here = (unsigned)e < (unsigned)A.E && expert_present(A.table[e]);
+        if (c == 0) s_gate[slot] = here ? A.gate[pair] : 0.0f;
+        if (here) {
             q = load_global<uint4>(A.x + ((long)pair * (A.Kp >> 1) + c * 16));
             x = *(const DYMOE_GLOBAL uint8_t*)(A.xs + ((long)pair * per + c));
         }
@@ -432,7 +434,7 @@ __global__ __launch_bounds__(64 * kMx4LastWaves) void mx4_thin_down_kernel(const
                 i++;
                 if (++kt == nkt || i == last) {
                     // register 4 g + i holds row 8 g + 4 (lane / 32) + i, of which the first 16 are wanted
-                    const float gate = A.gate[t * k + slot];
+                    const float gate = s_gate[slot];
 #pragma unroll
                     for (int v = 0; v < 8; v++) y[v] = fmaf(gate, acc[v], y[v]);
 #pragma unroll
@@ -944,7 +946,7 @@ extern "C" int dymoe_moe_ffn_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, con
     const bool small = c.shape == Mx4FfnShape::kSmall;
     int32_t* const plan = (int32_t*)(ws + L.plan);
     const int per_row = (int)((L.Hp + 511) / 512);
-    const int units = T * per_row;              // (below 2^23: T times H is below 2^33)
+    const int units = T * per_row;              // (at most 2^25: T times Hp is below 2^33)
     auto prep = mx4_prep_kernel<DYMOE_OUT_BF16>;
     if (x_dtype == DYMOE_OUT_F32) prep = mx4_prep_kernel<DYMOE_OUT_F32>;
     else if (x_dtype == DYMOE_OUT_F16) prep = mx4_prep_kernel<DYMOE_OUT_F16>;

@@ -334,6 +334,22 @@ def test_experts_left_out(ctx, T):
         assert (y[1] == 0).all() and (y[2] == 0).all() and (y[T - 1] == 0).all()
 
 
+@pytest.mark.parametrize("T", [1, 2, 5, 40, 300])
+@pytest.mark.parametrize("weight", [float("nan"), float("inf")])
+def test_experts_left_out_whatever_their_weight(ctx, T, weight):
+    H, F, E, k = 300, 200, 6, 3
+    ex, _ = make_experts(ctx, 8, E, H, F, missing=(5,))
+    x = randn(9, T, H)
+    idx, gate = choices(10, T, 5, k)
+    for at, e in ((0, -1), (T - 1, 5), (T // 2, 6)):
+        idx[at, at % k] = e
+    out = (idx < 0) | (idx >= 5)
+    ref = ctx.moe_ffn_mx4(x, idx, gate.masked_fill(out, 0.0), ex.table, F)
+    y = ctx.moe_ffn_mx4(x, idx, gate.masked_fill(out, weight), ex.table, F)
+    ctx.device_flags()
+    assert torch.isfinite(ref).all() and torch.equal(y, ref)
+
+
 @pytest.mark.parametrize("T", [1, 2, 5, 60, 500])
 def test_experts_token_that_is_no_number_stays_alone(ctx, T):
     ex, _ = make_experts(ctx, 8, 5, 256, 200)
