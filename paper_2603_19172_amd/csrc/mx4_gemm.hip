@@ -104,7 +104,7 @@ __device__ __forceinline__ void mx4_rows_to_lds(int dt, const char* x, long ldx,
 // wavefronts share a strip of 32 weight rows (of W1 and of W3 in the up projection) and take the 256-column tiles of K in turn; a workgroup of NW
 // has NW / KS strips.  Nothing is shared before the end: weights and codes come straight into registers, D tiles of a wavefront on their
 // way, and the sums of a strip's wavefronts meet in LDS.
-// Bound by the weights' bytes: 61 tokens on 8 of 128 experts of 768 x 2048, up 34.9 us (5.9 TB/s), down 19.2 (5.4); 61 x 1536 x 2048 5.1 us, a
+// Bound by the weights' bytes: 61 tokens on 8 of 128 experts of 768 x 2048, up 34.9 us (6.0 TB/s), down 19.2 (5.4); 61 x 1536 x 2048 5.1 us, a
 // start, eight wavefronts' share of K and the sums' way through LDS.
 // FUSE: the rows come as they are, few enough for every workgroup to convert them for itself, behind its first loads of weights; the experts' pairs
 // are then looked through by every workgroup too: the one of a pair that comes first among those of its expert (or 32, 64, ... behind
@@ -472,7 +472,7 @@ __global__ __launch_bounds__(64 * kMx4LastWaves) void mx4_thin_down_kernel(const
 //    cycles).
 // 2047 x 14336 x 4096: 78 us, 3.1 PFLOP/s, the matrix units busy in 39 % of the cycles, 65 us with zeros in place of random codes (the clock is
 // the power's to set); 8192 x 8192 x 8192 4.0 PFLOP/s, 5.5 with zeros, of 5.3 to 6.4 that these instructions reach on random codes from registers alone.
-// Experts with 128 rows each, 8 of 14336 x 4096: the stream of weights, 4.1 TB/s beside the rows' copies from L2 (with 8 rows 5.6): a
+// Experts with 128 rows each, 8 of 14336 x 4096: the stream of weights, 3.9 TB/s beside the rows' copies from L2 (with 8 rows 5.6): a
 // compute unit's requests for either wait in one queue.
 constexpr uint32_t kMx4Row = 128;           // bytes of a row of a step
 template <int NTF>
