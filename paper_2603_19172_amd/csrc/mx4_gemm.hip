@@ -104,12 +104,14 @@ __device__ __forceinline__ void mx4_rows_to_lds(int dt, const char* x, long ldx,
 // wavefronts share a strip of 32 weight rows (of W1 and of W3 in the up projection) and take the 256-column tiles of K in turn; a workgroup of NW
 // has NW / KS strips.  Nothing is shared before the end: weights and codes come straight into registers, D tiles of a wavefront on their
 // way, and the sums of a strip's wavefronts meet in LDS.
-// Bound by the weights' bytes: 61 tokens on 8 of 128 experts of 768 x 2048, up 34.9 us (6.0 TB/s), down 19.2 (5.4); 61 x 1536 x 2048 5.1 us, a
+// Bound by the weights' bytes: 61 tokens on 8 of 128 experts of 768 x 2048, up 34.9 us (6.0 TB/s), down 19.2 (5.4); 61 x 1536 x 2048 3.6 us, a
 // start, eight wavefronts' share of K and the sums' way through LDS.
+// XT: the rows lie in tiles as the weights do, and a load of theirs is 1 KiB of contiguous memory too: 222 x 1295 x 9025 18.8 us and 22.3 row by row,
+// 61 x 1536 x 2048 3.6 / 4.4.  A call that converts its rows writes them so.
 // FUSE: the rows come as they are, few enough for every workgroup to convert them for itself, behind its first loads of weights; the experts' pairs
 // are then looked through by every workgroup too: the one of a pair that comes first among those of its expert (or 32, 64, ... behind
 // the first) takes the next 32 of them, and a pair's position is its number.
-template <int MODE, int NTF, int NW, int KS, int D, bool FUSE = false>
+template <int MODE, int NTF, int NW, int KS, int D, bool FUSE = false, bool XT = false>
 __global__ __launch_bounds__(64 * NW) void mx4_small_kernel(const Mx4Args A)
 {
     constexpr int S = MODE == kMx4Up ? 2 : 1, kSums = S * NTF, kRows = 32 * NTF, kStrips = NW / KS;
@@ -184,8 +186,8 @@ __global__ __launch_bounds__(64 * NW) void mx4_small_kernel(const Mx4Args A)
 #pragma unroll
         for (int f = 0; f < NTF; f++) {
 #pragma unroll
-            for (int c = 0; c < 4; c++) t.x[f][c] = x.load(off[f] + (uint32_t)c * 16u, (uint32_t)kt * 128u);
-            t.xs[f] = load_u32(xs, offs[f], (uint32_t)kt * 8u);
+            for (int c = 0; c < 4; c++) t.x[f][c] = x.load(off[f] + (uint32_t)c * (XT ? 1024u : 16u), (uint32_t)kt * (XT ? 4096u : 128u));
+            t.xs[f] = load_u32(xs, offs[f], (uint32_t)kt * (XT ? 256u : 8u));
         }
     };
     Tile ring[D];
@@ -201,13 +203,18 @@ __global__ __launch_bounds__(64 * NW) void mx4_small_kernel(const Mx4Args A)
     }
 #pragma unroll
     for (int f = 0; f < NTF && !FUSE; f++) {
+        if (XT) {
+            off[f] = (uint32_t)f * 16u * (uint32_t)A.Kp + lane16;
+            offs[f] = (uint32_t)f * (uint32_t)A.Kp + lane4;
+            continue;
+        }
         const int r = min(32 * f + ln, rows - 1);                            // rows behind the last: computed and dropped
         const uint32_t row = MODE == kMx4Up ? (uint32_t)(pp.perm[row0 + r] / A.k) : (uint32_t)r;
         off[f] = row * (uint32_t)(A.Kp >> 1) + 64u * (uint32_t)kb;
         offs[f] = row * (uint32_t)(A.Kp >> 5) + 4u * (uint32_t)kb;
     }
     const long from = MODE == kMx4Up ? 0 : row0;
-    const uint32_t held = MODE == kMx4Up ? A.rows : rows;
+    const uint32_t held = XT ? (uint32_t)(rows + 31) / 32u * 32u : MODE == kMx4Up ? A.rows : rows;
     x.set(A.x + from * (A.Kp >> 1), held * (uint32_t)(A.Kp >> 1));
     xs.set(A.xs + from * (A.Kp >> 5), held * (uint32_t)(A.Kp >> 5));
 #pragma unroll
@@ -469,7 +476,7 @@ __global__ __launch_bounds__(64 * kMx4LastWaves) void mx4_thin_down_kernel(const
 //    issued.
 //  * The rows' codes and exponents are shared by the wavefronts through three LDS buffers that global memory fills directly, two steps ahead; the 16-byte chunks of
 //    a row's 128 bytes are turned by its number, which spreads the operand reads (one chunk of 32 rows) over all banks (conflicts in 2.5 % of the
-//    cycles).
+//    cycles).  Rows in tiles (XT) come and lie in the operand's order by themselves: 512 x 4096 x 14336 27.4 us in all, 32.4 row by row.
 // 2047 x 14336 x 4096: 78 us, 3.1 PFLOP/s, the matrix units busy in 39 % of the cycles, 65 us with zeros in place of random codes (the clock is
 // the power's to set); 8192 x 8192 x 8192 4.0 PFLOP/s, 5.5 with zeros, of 5.3 to 6.4 that these instructions reach on random codes from registers alone.
 // Experts with 128 rows each, 8 of 14336 x 4096: the stream of weights, 3.9 TB/s beside the rows' copies from L2 (with 8 rows 5.6): a
@@ -502,7 +509,7 @@ struct Mx4Weights {
     }
 };
 
-template <int MODE, int NTF, int S, int D, int RR>
+template <int MODE, int NTF, int S, int D, int RR, bool XT>
 __device__ __forceinline__ void mx4_tile(const Mx4Args& A, const int32_t* perm, Mx4Weights<S, D>& w, int row0, int rows, int bx, int step0, int steps, void* out,
                                          uint32_t base)
 {
@@ -515,9 +522,10 @@ __device__ __forceinline__ void mx4_tile(const Mx4Args& A, const int32_t* perm, 
     const uint32_t lane16 = (uint32_t)lane * 16u;
     const int end = steps - 1;
     float16_t acc[S][NTF] = {};
-    // copies: rows 32 i + 8 wave + lane / 8, chunk lane % 8 turned; exponents of fragment `wave` (and wave + 4)
-    const char* const xb = A.x + (MODE == kMx4Up ? 0 : (long)row0 * (A.Kp >> 1)) + (long)step0 * 128;
-    const char* const sb = A.xs + (MODE == kMx4Up ? 0 : (long)row0 * (A.Kp >> 5)) + (long)step0 * 8;
+    // copies: rows 32 i + 8 wave + lane / 8, chunk lane % 8 turned (XT: chunk `wave` of all rows); exponents of fragment `wave` (and wave + 4)
+    constexpr long kStepX = XT ? 4096 : 128, kStepE = XT ? 256 : 8;
+    const char* const xb = A.x + (MODE == kMx4Up ? 0 : (long)row0 * (A.Kp >> 1)) + step0 * kStepX;
+    const char* const sb = A.xs + (MODE == kMx4Up ? 0 : (long)row0 * (A.Kp >> 5)) + step0 * kStepE;
     uint32_t off[NTF], offs[(NTF + 3) / 4];
     auto source = [&](int r) {                   // rows behind the last: computed and dropped
         r = min(r, rows - 1);
@@ -525,17 +533,19 @@ __device__ __forceinline__ void mx4_tile(const Mx4Args& A, const int32_t* perm, 
     };
     const int rb = 8 * wave + (lane >> 3);
 #pragma unroll
-    for (int i = 0; i < NTF; i++) off[i] = source(32 * i + rb) * (uint32_t)(A.Kp >> 1) + 16u * (uint32_t)((lane & 7) ^ mx4_turn(rb));
+    for (int i = 0; i < NTF; i++)
+        off[i] = XT ? (uint32_t)i * 16u * (uint32_t)A.Kp + (uint32_t)wave * 1024u + lane16 : source(32 * i + rb) * (uint32_t)(A.Kp >> 1) + 16u * (uint32_t)((lane & 7) ^ mx4_turn(rb));
     // (wavefronts without a fragment of their own copy the last one's exponents again: the count of copies is then every wavefront's)
 #pragma unroll
-    for (int i = 0; i < (NTF + 3) / 4; i++) offs[i] = source(32 * min(wave + 4 * i, NTF - 1) + (lane >> 1)) * (uint32_t)(A.Kp >> 5) + 4u * (uint32_t)(lane & 1);
+    for (int i = 0; i < (NTF + 3) / 4; i++)
+        offs[i] = XT ? (uint32_t)min(wave + 4 * i, NTF - 1) * (uint32_t)A.Kp + (lane16 >> 2) : source(32 * min(wave + 4 * i, NTF - 1) + (lane >> 1)) * (uint32_t)(A.Kp >> 5) + 4u * (uint32_t)(lane & 1);
     auto copy = [&](int step, uint32_t buf) {
 #pragma unroll
         for (int i = 0; i < NTF; i++)
-            lds_copy16(xb + (long)step * 128, off[i], __builtin_amdgcn_readfirstlane(base + buf + (uint32_t)(i * 4096 + wave * 1024)));
+            lds_copy16(xb + step * kStepX, off[i], __builtin_amdgcn_readfirstlane(base + buf + (uint32_t)(i * 4096 + wave * 1024)));
 #pragma unroll
         for (int i = 0; i < (NTF + 3) / 4; i++)
-            lds_copy4(sb + (long)step * 8, offs[i], __builtin_amdgcn_readfirstlane(base + buf + kExp + (uint32_t)(min(wave + 4 * i, NTF - 1) * 256)));
+            lds_copy4(sb + step * kStepE, offs[i], __builtin_amdgcn_readfirstlane(base + buf + kExp + (uint32_t)(min(wave + 4 * i, NTF - 1) * 256)));
     };
 #pragma unroll
     for (int p = 0; p < D; p++) copy(min(p, end), (uint32_t)p * kBuf);
@@ -552,8 +562,8 @@ __device__ __forceinline__ void mx4_tile(const Mx4Args& A, const int32_t* perm, 
     }
     wait_lds_copies<(D - 1) * kCopies + 5 * D * S>();        // the first copies are older than everything else
     __syncthreads();
-    const uint32_t xa0 = base + (uint32_t)ln * kMx4Row + (((uint32_t)kb << 6) ^ ((uint32_t)mx4_turn(ln) << 4));
-    const uint32_t xe0 = base + kExp + (uint32_t)ln * 8u + (uint32_t)kb * 4u;
+    const uint32_t xa0 = XT ? base + lane16 : base + (uint32_t)ln * kMx4Row + (((uint32_t)kb << 6) ^ ((uint32_t)mx4_turn(ln) << 4));
+    const uint32_t xe0 = base + kExp + (XT ? lane16 >> 2 : (uint32_t)ln * 8u + (uint32_t)kb * 4u);
     uint32_t at = 0;
     // Step ks multiplies what its buffer and registers hold and requests the codes of the rows and of the weights D steps on.
     auto step = [&](int ks, auto slot) __attribute__((always_inline)) {
@@ -571,7 +581,7 @@ __device__ __forceinline__ void mx4_tile(const Mx4Args& A, const int32_t* perm, 
         for (int f = 0; f < NTF; f++) xe[f] = lds_read4(xe0 + at + (uint32_t)f * 256u);
         // the operands of the next R products of a chunk and a fragment are read while this one's are issued
         uint4 op[R];
-        auto read = [&](int o) { return lds_read16(((xa0 + at) ^ (uint32_t)((o / NTF) << 4)) + (uint32_t)(o % NTF) * (32u * kMx4Row)); };
+        auto read = [&](int o) { return XT ? lds_read16(xa0 + at + (uint32_t)((o / NTF) * 1024 + (o % NTF) * 4096)) : lds_read16(((xa0 + at) ^ (uint32_t)((o / NTF) << 4)) + (uint32_t)(o % NTF) * (32u * kMx4Row)); };
 #pragma unroll
         for (int o = 0; o < R; o++) op[o] = read(o);
         auto chunk = [&](auto which) __attribute__((always_inline)) {
@@ -696,7 +706,7 @@ __device__ __forceinline__ uint32_t mx4_lds_base(char* p) { return (uint32_t)(ui
 template <int MODE, int S>
 constexpr int kMx4Cols = 128 * (MODE == kMx4Up ? S / 2 : S);
 
-template <int MODE, int MAXF, int S, int D, int RR>
+template <int MODE, int MAXF, int S, int D, int RR, bool XT = false>
 __global__ __launch_bounds__(256, MAXF * S <= 8 ? 2 : 1) void mx4_tall_kernel(const Mx4Args A)
 {
     extern __shared__ __attribute__((aligned(1024))) char lds_raw[];
@@ -740,7 +750,7 @@ __global__ __launch_bounds__(256, MAXF * S <= 8 ? 2 : 1) void mx4_tall_kernel(co
         }
     }
     // one instantiation per number of fragments of 32 rows: the accumulators then sit in fixed registers for the whole loop
-#define DYMOE_MX4_TILE(NTF) mx4_tile<MODE, NTF, S, D, RR>(A, pp.perm, w, row0, rows, bx, step0, steps, out, base)
+#define DYMOE_MX4_TILE(NTF) mx4_tile<MODE, NTF, S, D, RR, XT>(A, pp.perm, w, row0, rows, bx, step0, steps, out, base)
     switch ((rows + 31) >> 5) {
     case 1: DYMOE_MX4_TILE(1); break;
     case 2: DYMOE_MX4_TILE(MAXF < 2 ? MAXF : 2); break;
@@ -755,18 +765,22 @@ template <int MAXF, int S, int D>
 constexpr int kMx4Lds = (int)((D + 1) * kMx4Buf<MAXF> > 4 * kMx4EpiWave<S> ? (D + 1) * kMx4Buf<MAXF> : 4 * kMx4EpiWave<S>);
 
 // A shape's instantiation: the tile's fragments of 32 rows, strips of a wavefront, steps ahead, operands ahead.
-#define DYMOE_MX4_TILE32(MODE) mx4_tall_kernel<MODE, 1, 1, 4, 4>
-#define DYMOE_MX4_TILE64(MODE) mx4_tall_kernel<MODE, 2, 1, 3, 4>
-#define DYMOE_MX4_TILE64W(MODE) mx4_tall_kernel<MODE, 2, 2, 2, 4>
-#define DYMOE_MX4_TILE128(MODE) mx4_tall_kernel<MODE, 4, 2, 2, 3>
+#define DYMOE_MX4_TILE32(MODE, XT) mx4_tall_kernel<MODE, 1, 1, 4, 4, XT>
+#define DYMOE_MX4_TILE64(MODE, XT) mx4_tall_kernel<MODE, 2, 1, 3, 4, XT>
+#define DYMOE_MX4_TILE64W(MODE, XT) mx4_tall_kernel<MODE, 2, 2, 2, 4, XT>
+#define DYMOE_MX4_TILE128(MODE, XT) mx4_tall_kernel<MODE, 4, 2, 2, 3, XT>
 
 // per-device set-up, with the device current
 int mx4_init()
 {
     auto allow = [](const void* f, int bytes) { return hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess; };
-    bool ok = allow((const void*)DYMOE_MX4_TILE32(kMx4Plain), kMx4Lds<1, 1, 4>) && allow((const void*)DYMOE_MX4_TILE64(kMx4Plain), kMx4Lds<2, 1, 3>) &&
-              allow((const void*)DYMOE_MX4_TILE64W(kMx4Plain), kMx4Lds<2, 2, 2>) && allow((const void*)DYMOE_MX4_TILE128(kMx4Plain), kMx4Lds<4, 2, 2>);
-    ok = ok && allow((const void*)DYMOE_MX4_TILE128(kMx4Up), kMx4Lds<4, 2, 2>) && allow((const void*)DYMOE_MX4_TILE128(kMx4Down), kMx4Lds<4, 2, 2>);
+    auto plain = [&](auto xt) {
+        constexpr bool XT = decltype(xt)::value;
+        return allow((const void*)DYMOE_MX4_TILE32(kMx4Plain, XT), kMx4Lds<1, 1, 4>) && allow((const void*)DYMOE_MX4_TILE64(kMx4Plain, XT), kMx4Lds<2, 1, 3>) &&
+               allow((const void*)DYMOE_MX4_TILE64W(kMx4Plain, XT), kMx4Lds<2, 2, 2>) && allow((const void*)DYMOE_MX4_TILE128(kMx4Plain, XT), kMx4Lds<4, 2, 2>);
+    };
+    bool ok = plain(std::false_type()) && plain(std::true_type());
+    ok = ok && allow((const void*)DYMOE_MX4_TILE128(kMx4Up, false), kMx4Lds<4, 2, 2>) && allow((const void*)DYMOE_MX4_TILE128(kMx4Down, false), kMx4Lds<4, 2, 2>);
     ok = ok && allow((const void*)mx4_small_kernel<kMx4Plain, 1, 8, 8, 1, true>, (int)kMx4FuseBytes) &&
          allow((const void*)mx4_small_kernel<kMx4Up, 1, 4, 4, 1, true>, (int)kMx4FuseBytes) && allow((const void*)mx4_thin_down_kernel<2>, (int)kMx4FuseBytes);
     return ok ? DYMOE_OK : DYMOE_EHIP;
@@ -850,7 +864,7 @@ extern "C" int dymoe_matmul_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, cons
         A.x_dtype = x_dtype;
         A.K = K;
     } else if (!coded) {
-        const int rc = mx4_quantize(ctx, x, x_dtype, T, K, ldx, 0, (uint8_t*)ws + L.xq, (uint8_t*)ws + L.xs, st);
+        const int rc = mx4_quantize(ctx, x, x_dtype, T, K, ldx, 1, (uint8_t*)ws + L.xq, (uint8_t*)ws + L.xs, st);
         if (rc != DYMOE_OK) return rc;
         A.x = ws + L.xq;
         A.xs = ws + L.xs;
@@ -868,17 +882,24 @@ extern "C" int dymoe_matmul_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, cons
     auto run = [&](void (*kernel)(const Mx4Args), dim3 grid, int threads, int lds) {
         dymoe_launch(ctx, DYMOE_K_MX4_PRODUCT, kernel, grid, dim3((unsigned)threads), lds, st, A);
     };
-    switch (c.shape) {
-    case Mx4MatShape::kSmall:
-        if (c.fuse) run(mx4_small_kernel<kMx4Plain, 1, 8, 8, 1, true>, dim3((unsigned)groups), 512, (int)mx4_fuse_bytes(T, L.Kp));
-        else if (c.waves == 8) run(mx4_small_kernel<kMx4Plain, 1, 8, 8, 1>, dim3((unsigned)groups), 512, 0);
-        else run(mx4_small_kernel<kMx4Plain, 1, 4, 4, 1>, dim3((unsigned)groups), 256, 0);
-        break;
-    case Mx4MatShape::kTile32: run(DYMOE_MX4_TILE32(kMx4Plain), mx4_grid((T + 31L) / 32 * n128), 256, kMx4Lds<1, 1, 4>); break;
-    case Mx4MatShape::kTile64: run(DYMOE_MX4_TILE64(kMx4Plain), mx4_grid((T + 63L) / 64 * n128), 256, kMx4Lds<2, 1, 3>); break;
-    case Mx4MatShape::kTile64w: run(DYMOE_MX4_TILE64W(kMx4Plain), mx4_grid((T + 63L) / 64 * n256), 256, kMx4Lds<2, 2, 2>); break;
-    default: run(DYMOE_MX4_TILE128(kMx4Plain), mx4_grid((T + 127L) / 128 * n256), 256, kMx4Lds<4, 2, 2>);
-    }
+    // rows converted in the call lie in tiles, codes made before row by row
+    auto launch = [&](auto xt) {
+        constexpr bool XT = decltype(xt)::value;
+        const long t32 = (T + 31L) / 32, t64 = (T + 63L) / 64, t128 = (T + 127L) / 128;
+        switch (c.shape) {
+        case Mx4MatShape::kSmall:
+            if (c.waves == 8) run(mx4_small_kernel<kMx4Plain, 1, 8, 8, 1, false, XT>, dim3((unsigned)groups), 512, 0);
+            else run(mx4_small_kernel<kMx4Plain, 1, 4, 4, 1, false, XT>, dim3((unsigned)groups), 256, 0);
+            break;
+        case Mx4MatShape::kTile32: run(DYMOE_MX4_TILE32(kMx4Plain, XT), mx4_grid(t32 * n128), 256, kMx4Lds<1, 1, 4>); break;
+        case Mx4MatShape::kTile64: run(DYMOE_MX4_TILE64(kMx4Plain, XT), mx4_grid(t64 * n128), 256, kMx4Lds<2, 1, 3>); break;
+        case Mx4MatShape::kTile64w: run(DYMOE_MX4_TILE64W(kMx4Plain, XT), mx4_grid(t64 * n256), 256, kMx4Lds<2, 2, 2>); break;
+        default: run(DYMOE_MX4_TILE128(kMx4Plain, XT), mx4_grid(t128 * n256), 256, kMx4Lds<4, 2, 2>);
+        }
+    };
+    if (c.fuse) run(mx4_small_kernel<kMx4Plain, 1, 8, 8, 1, true, false>, dim3((unsigned)groups), 512, (int)mx4_fuse_bytes(T, L.Kp));
+    else if (coded) launch(std::false_type());
+    else launch(std::true_type());
     DYMOE_HIP_LAUNCH_CHECK();
     return DYMOE_OK;
 }
@@ -966,13 +987,13 @@ extern "C" int dymoe_moe_ffn_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, con
     const long tall = P / kMx4TallRows + (E < P ? E : P);
     auto strips = [&](long n, int each) { return dim3((unsigned)(L.max_tiles * ((n + each - 1) / each))); };
     const long fs = (long)(L.Fp / 32), hs = (H + 31L) / 32;
-    if (!small) run(DYMOE_MX4_TILE128(kMx4Up), mx4_grid(tall * (long)(L.Fp / 128)), 256, kMx4Lds<4, 2, 2>);
+    if (!small) run(DYMOE_MX4_TILE128(kMx4Up, false), mx4_grid(tall * (long)(L.Fp / 128)), 256, kMx4Lds<4, 2, 2>);
     else if (c.up_waves == 4) run(mx4_small_kernel<kMx4Up, 1, 4, 4, 1>, strips(fs, 1), 256, 0);
     else if (c.up_waves == 2) run(mx4_small_kernel<kMx4Up, 1, 4, 2, 1>, strips(fs, 2), 256, 0);
     else run(mx4_small_kernel<kMx4Up, 1, 4, 1, 1>, strips(fs, 4), 256, 0);
     turn(ws + L.part, (long)mx4_round((size_t)H, 8), DYMOE_OUT_F32);
     A.splits = c.splits;
-    if (!small) run(DYMOE_MX4_TILE128(kMx4Down), mx4_grid(tall * ((H + 255L) / 256) * c.splits), 256, kMx4Lds<4, 2, 2>);
+    if (!small) run(DYMOE_MX4_TILE128(kMx4Down, false), mx4_grid(tall * ((H + 255L) / 256) * c.splits), 256, kMx4Lds<4, 2, 2>);
     else if (c.down_waves == 8) run(mx4_small_kernel<kMx4Down, 1, 8, 8, 1>, strips(hs, 1), 512, 0);
     else if (c.down_waves == 4) run(mx4_small_kernel<kMx4Down, 1, 4, 4, 1>, strips(hs, 1), 256, 0);
     else if (c.down_waves == 2) run(mx4_small_kernel<kMx4Down, 1, 4, 2, 1>, strips(hs, 2), 256, 0);

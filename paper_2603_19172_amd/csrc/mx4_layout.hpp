@@ -56,8 +56,9 @@ static inline Mx4MatLayout mx4_mat_layout(long T, long K)
     Mx4MatLayout L;
     L.Kp = mx4_round((size_t)K, kMx4TileCols);
     L.xq = 0;
-    L.xs = mx4_round((size_t)T * L.Kp / 2, 256);
-    L.total = L.xs + mx4_round((size_t)T * L.Kp / 32, 256);
+    const size_t rows = mx4_round((size_t)T, 32);
+    L.xs = rows * L.Kp / 2;
+    L.total = L.xs + rows * L.Kp / 32;
     return L;
 }
 

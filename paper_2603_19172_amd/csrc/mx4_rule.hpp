@@ -34,13 +34,14 @@ static inline Mx4MatChoice mx4_mat_choice(long T, long N, long K, bool coded, lo
     // Eight wavefronts while the strips are fewer than 400: 1 x 4096 x 14336 13.2 and 15.4 with four, 61 x 1536 x 2048 7.4 / 7.2; 1 x 14336 x 4096 10.8 /
     // 10.4, 64 x 4096 x 4096 9.7 / 9.4.
     const Mx4MatChoice small = {Mx4MatShape::kSmall, fuse, strips * t32 < 400 ? 8 : 4};
-    // Strips while tiles of 32 x 128 are few (64 x 4096 x 4096, 64 of them: 9.4 and 11.5 in tiles; 512 x 768 x 2048, 96: 8.4 / 9.6; 128 x 4096 x 4096, 128:
-    // 13.6 / 11.8; 64 x 14336 x 4096, 224: 21.8 / 13.3), then the largest tiles that still are one for each compute unit (256 x 4096 x 4096 in tiles of
-    // 32 12.6, of 64 14.2, of 128 x 256 23; 512 x 4096 x 4096 18.8, 15.2, 24; 1024 x 4096 x 4096 31, 23.3, of 64 x 256 21, of 128 25.6;
-    // 2048 x 4096 x 4096 36 of 64, 33 of 64 x 256, 31.5 of 128).
-    if (T <= 32 || t32 * n128 <= num_cu * 3 / 8) return small;
+    // Strips while tiles of 32 x 128 are few, so that each strip has a compute unit (64 x 4096 x 4096, 64 of them: 8.6 and 9.5 in tiles; 256 x 798 x 7548, 56:
+    // 13.3 / 13.8; 222 x 1295 x 9025, 77: 23.2 / 15.6; 96 x 4096 x 4096, 96: 11.4 / 10.2), or somewhat more with a short K (512 x 768 x 2048, 96: 7.8 / 8.5;
+    // 128 x 4096 x 4096, 128: 11.8 / 9.8); then the largest tiles that still are one for each compute unit, two of 64 x 128 (256 x 4096 x 4096 in tiles of
+    // 32 11.3, of 64 12.1, of 128 x 256 22; 512 x 4096 x 4096 15.7, 13.9, 23; 2047 x 2048 x 2048 18.7, 15.7, of 64 x 256 16.3, of 128 20.5;
+    // 512 x 14336 x 4096 35, 28.6, 27.4, 28.2; 2047 x 4096 x 4096 42, 32.4, 31.3, 30.9).
+    if (T <= 32 || t32 * n128 <= num_cu / 4 || (t32 * n128 <= num_cu * 3 / 8 && K <= 2048)) return small;
     if (t32 * n128 <= num_cu) return {Mx4MatShape::kTile32, false, 0};
-    if (t64 * n128 <= num_cu) return {Mx4MatShape::kTile64, false, 0};
+    if (t64 * n128 <= 2 * num_cu) return {Mx4MatShape::kTile64, false, 0};
     return {t128 * n256 < num_cu ? Mx4MatShape::kTile64w : Mx4MatShape::kTile128, false, 0};
 }
 

@@ -15,9 +15,9 @@ pytestmark = pytest.mark.gpu
 
 # shape, T, N, K: steps of 256 columns from one to more than a shape has on their way, odd and even, last tiles of every number of fragments
 PRODUCTS = [("small", 3, 13001, 300), ("small", 30, 12900, 777), ("small", 90, 1500, 2600), ("small", 40, 70, 9000),
-            ("tile32", 97, 3201, 1300), ("tile32", 130, 2600, 256), ("tile32", 250, 1900, 1537), ("tile32", 33, 14000, 300),
+            ("tile32", 97, 3201, 1300), ("tile32", 130, 2600, 256), ("tile32", 250, 1900, 1537), ("tile32", 33, 14000, 300), ("tile32", 222, 1295, 2300),
             ("tile64", 500, 2500, 520), ("tile64", 449, 2700, 1100), ("tile64", 610, 1700, 2049), ("tile64", 520, 2300, 200),
-            ("tile64w", 900, 5000, 300), ("tile64w", 935, 4100, 800), ("tile64w", 1030, 4700, 1100),
+            ("tile64w", 900, 5000, 300), ("tile64w", 935, 4500, 800), ("tile64w", 1030, 4700, 1100),
             ("tile128", 1950, 5000, 257), ("tile128", 2091, 4300, 520), ("tile128", 2113, 4000, 1025), ("tile128", 2170, 4000, 200)]
 
 # T, H, F, E, k, splits: experts in tall tiles

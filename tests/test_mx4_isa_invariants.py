@@ -36,10 +36,10 @@ def test_counted_waits_cover_the_copies():
     lines = _assembly("mx4_gemm.hip")
     in_asm = {k for b in _blocks(lines) for k in range(b[0], b[1] + 1)}
     kernels = _kernels(lines)
-    assert len(kernels) == 6
+    assert len(kernels) == 10
     loops = 0
     for name, rows in kernels.items():
-        ahead = int(re.search(r"Li(\d+)ELi(\d+)EEEvNS", name).group(1))       # ..., steps ahead, operands ahead
+        ahead = int(re.search(r"Li(\d+)ELi(\d+)ELb[01]EEEvNS", name).group(1))       # ..., steps ahead, operands ahead, rows in tiles
         for piece in _straight(lines, rows):
             if sum("v_mfma" in lines[i] for i in piece) == 0 or sum("s_barrier" in lines[i] for i in piece) != ahead:
                 continue                                                          # (the last steps' pieces hold one each: the same code)
@@ -70,7 +70,7 @@ def test_counted_waits_cover_the_copies():
             per = [sum(k == "copy" and s == x for k, s in queue) for x in range(ahead, 2 * ahead)]
             assert len(set(per)) == 1 and per[0] >= 2
     # every number of fragments of every kernel
-    assert loops >= 1 + 2 + 2 + 3 * 4
+    assert loops >= 2 * (1 + 2 + 2 + 4) + 2 * 4
 
 
 def test_the_loop_waits_for_no_load_of_its_own_step():
@@ -78,7 +78,7 @@ def test_the_loop_waits_for_no_load_of_its_own_step():
     lines = _assembly("mx4_gemm.hip")
     in_asm = {k for b in _blocks(lines) for k in range(b[0], b[1] + 1)}
     for name, rows in _kernels(lines).items():
-        strips, ahead = (int(v) for v in re.search(r"Li\d+ELi\d+ELi(\d+)ELi(\d+)ELi\d+EEEvNS", name).groups())
+        strips, ahead = (int(v) for v in re.search(r"Li\d+ELi\d+ELi(\d+)ELi(\d+)ELi\d+ELb[01]EEEvNS", name).groups())
         for piece in _straight(lines, rows):
             if sum("v_mfma" in lines[i] for i in piece) == 0 or sum("s_barrier" in lines[i] for i in piece) != ahead:
                 continue

@@ -76,9 +76,11 @@ def test_both_sides_of_each_line(product, experts):
     assert product(1, 4096, 4096) == ("small", True, 8) and product(1, 4096, 4096, coded=1) == ("small", False, 8)
     assert product(4, 4096, 4096)[1] and not product(5, 4096, 4096)[1] and product(32, 4096, 512)[1] and not product(33, 64, 64)[1]
     assert product(8, 12768, 4096) == ("small", False, 8) and product(8, 12800, 4096) == ("small", False, 4)
-    assert product(32, 1 << 24, 512)[0] == "small" and product(33, 6144, 512)[0] == "small" and product(33, 6145, 512)[0] == "tile32"
-    assert product(64, 16384, 512)[0] == "tile32" and product(64, 16385, 512)[0] == "tile64" and product(64, 32769, 512)[0] == "tile64w"
-    assert product(64, 65280, 512)[0] == "tile64w" and product(64, 65281, 512)[0] == "tile128"
+    assert product(32, 1 << 24, 512)[0] == "small" and product(33, 6144, 2048)[0] == "small" and product(33, 6145, 2048)[0] == "tile32"
+    assert product(33, 4096, 2049)[0] == "small" and product(33, 4097, 2049)[0] == "tile32"
+    assert product(64, 16384, 512)[0] == "tile32" and product(64, 16385, 512)[0] == "tile64" and product(64, 65536, 512)[0] == "tile64"
+    assert product(64, 65537, 512)[0] == "tile128" and product(128, 32769, 512)[0] == "tile64w"
+    assert product(128, 65280, 512)[0] == "tile64w" and product(128, 65281, 512)[0] == "tile128"
     assert experts(2, 4096, 14336, 8, 2)[0] == "thin" and experts(3, 4096, 14336, 8, 2)[0] == "small"
     assert experts(4, 2048, 768, 128, 8)[0] == "thin" and experts(5, 2048, 768, 128, 8)[0] == "small" and experts(1, 128, 128, 128, 65)[0] == "small"
     assert experts(1, 131072, 768, 8, 2)[0] == "small" and experts(1, 2048, 131072, 8, 1)[0] == "small"
