@@ -17,7 +17,7 @@ static inline size_t mx4_round(size_t v, size_t m) { return (v + m - 1) / m * m;
 
 struct Mx4FfnLayout {
     size_t Hp, Fp;     // columns of the codes' rows: whole tiles
-    size_t xq, xs;     // [T, Hp / 2] codes and [T, Hp / 32] exponents of the activations
+    size_t xq, xs;     // [Hp / 256, T, 128] codes and [Hp / 256, T, 8] exponents of the activations
     size_t hq, hs;     // [P, Fp / 2] and [P, Fp / 32] of the SwiGLU intermediate, by position (pairs sorted by expert)
     size_t part;       // parts of [P, H up to a multiple of 8] outputs of the pairs, by position, fp32
     size_t plan;       // int32, see ExpertPlan
