@@ -54,8 +54,8 @@ struct Mx4Args {
     const int32_t* plan;              // experts
     const char *w, *ws;               // the plain product
     const float* bias;
-    void* out;                        // up: codes of the intermediate's rows, ldo / 2 bytes each
-    uint8_t* out_scale;               // up: their exponents, ldo / 32
+    void* out;                        // up: codes of the intermediate's rows, ldo / 2 bytes each, or in tiles (tall ones)
+    uint8_t* out_scale;               // up: their exponents
     long ldo, P;
     int rows, Kp, N, k, out_dtype;
     int splits;                       // tall tiles of the down projection: parts of K, P rows of outputs each
@@ -515,7 +515,7 @@ struct Mx4Weights {
 };
 
 template <int MODE, int NTF, int S, int D, int RR, bool XT>
-__device__ __forceinline__ void mx4_tile(const Mx4Args& A, const int32_t* perm, Mx4Weights<S, D>& w, int row0, int rows, int bx, int step0, int steps, void* out,
+__device__ __forceinline__ void mx4_tile(const Mx4Args& A, const int32_t* perm, Mx4Weights<S, D>& w, int row0, int rows, long held_at, int bx, int step0, int steps, void* out,
                                          uint32_t base)
 {
     constexpr int kMask = 0x2 | 0x4;             // vector and scalar arithmetic may cross; products, LDS and memory accesses may not
@@ -529,8 +529,8 @@ __device__ __forceinline__ void mx4_tile(const Mx4Args& A, const int32_t* perm, 
     float16_t acc[S][NTF] = {};
     // copies: rows 32 i + 8 wave + lane / 8, chunk lane % 8 turned (XT: chunk `wave` of all rows); exponents of fragment `wave` (and wave + 4)
     const long kStepX = XT ? 4096 : MODE == kMx4Up ? A.rows * 128L : 128, kStepE = kStepX >> 4;
-    const char* const xb = A.x + (MODE == kMx4Up ? 0 : (long)row0 * (A.Kp >> 1)) + step0 * kStepX;
-    const char* const sb = A.xs + (MODE == kMx4Up ? 0 : (long)row0 * (A.Kp >> 5)) + step0 * kStepE;
+    const char* const xb = A.x + (MODE == kMx4Up ? 0 : held_at * (A.Kp >> 1)) + step0 * kStepX;
+    const char* const sb = A.xs + (MODE == kMx4Up ? 0 : held_at * (A.Kp >> 5)) + step0 * kStepE;
     uint32_t off[NTF], offs[(NTF + 3) / 4];
     auto source = [&](int r) {                   // rows behind the last: computed and dropped
         r = min(r, rows - 1);
@@ -629,7 +629,9 @@ __device__ __forceinline__ void mx4_tile(const Mx4Args& A, const int32_t* perm, 
     wait_lds_copies<0>();
     __syncthreads();
 
-    // A lane holds, of its token's row, four neighbouring outputs in each group of four registers.
+    // A lane holds, of its token's row, four neighbouring outputs in each group of four registers.  The intermediate goes into tiles, where a fragment's
+    // 32 rows of a block are 512 bytes, and comes back as the down projection's rows: 512 tokens, 2 of 8 experts of 14336 x 4096 212 -> 202 us, 2047
+    // tokens 459 -> 438.  (Not from strips: tiles of few rows would read all 32, 61 tokens on 8 of 128 experts of 768 x 2048 63 -> 66.)
     if constexpr (MODE == kMx4Up) {
         // the halves of a wavefront hold a block together: 16 numbers each
 #pragma unroll
@@ -662,9 +664,8 @@ __device__ __forceinline__ void mx4_tile(const Mx4Args& A, const int32_t* perm, 
                 const uint4 all = make_uint4((a[0] & 0xffffu) | (a[1] << 16), (a[0] >> 16) | (a[1] & 0xffff0000u), (b[0] & 0xffffu) | (b[1] << 16),
                                              (b[0] >> 16) | (b[1] & 0xffff0000u));
                 if (row >= rows) continue;
-                const long at = (long)(row0 + row) * A.ldo + 32L * block;
-                if (kb == 0) store_global((char*)out + at / 2, all);
-                else *(DYMOE_GLOBAL uint8_t*)(A.out_scale + at / 32) = (uint8_t)byte;
+                if (kb == 0) store_global((char*)out + mx4_tile_byte(held_at + row, 32L * block, A.ldo), all);
+                else *(DYMOE_GLOBAL uint8_t*)(A.out_scale + mx4_tile_exponent(held_at + row, 32L * block, A.ldo)) = (uint8_t)byte;
             }
         }
     } else {
@@ -723,6 +724,7 @@ __global__ __launch_bounds__(256, MAXF * S <= 8 ? 2 : 1) void mx4_tall_kernel(co
     const long unit = mx4_unit_of_group();
     Mx4Weights<S, D> w;
     int row0, rows, bx, step0 = 0, steps = A.Kp >> 8;
+    long held_at;
     void* out = A.out;
     if (MODE == kMx4Plain) {
         const int tiles = (A.rows + kRows - 1) / kRows;
@@ -730,6 +732,7 @@ __global__ __launch_bounds__(256, MAXF * S <= 8 ? 2 : 1) void mx4_tall_kernel(co
         bx = (int)(unit / tiles);
         row0 = (int)(unit - (long)bx * tiles) * kRows;
         rows = min(kRows, A.rows - row0);
+        held_at = row0;
 #pragma unroll
         for (int s = 0; s < S; s++) w.strip[s].set(A.w, A.ws, (4L * bx + wave) * S + s, strips, A.Kp);
     } else {
@@ -748,6 +751,7 @@ __global__ __launch_bounds__(256, MAXF * S <= 8 ? 2 : 1) void mx4_tall_kernel(co
         const int i = (int)(local - (long)bx * t.tiles) * kRows;
         row0 = t.first + i;
         rows = min(kRows, t.pairs - i);
+        held_at = 32L * (t.first / 32 + t.tile0) + i;
 #pragma unroll
         for (int s = 0; s < S; s++) {
             if (MODE == kMx4Up) w.strip[s].set(s & 1 ? t.mat.q[1] : t.mat.q[0], s & 1 ? t.mat.s[1] : t.mat.s[0], (4L * bx + wave) * (S / 2) + s / 2, strips, A.Kp);
@@ -755,7 +759,7 @@ __global__ __launch_bounds__(256, MAXF * S <= 8 ? 2 : 1) void mx4_tall_kernel(co
         }
     }
     // one instantiation per number of fragments of 32 rows: the accumulators then sit in fixed registers for the whole loop
-#define DYMOE_MX4_TILE(NTF) mx4_tile<MODE, NTF, S, D, RR, XT>(A, pp.perm, w, row0, rows, bx, step0, steps, out, base)
+#define DYMOE_MX4_TILE(NTF) mx4_tile<MODE, NTF, S, D, RR, XT>(A, pp.perm, w, row0, rows, held_at, bx, step0, steps, out, base)
     switch ((rows + 31) >> 5) {
     case 1: DYMOE_MX4_TILE(1); break;
     case 2: DYMOE_MX4_TILE(MAXF < 2 ? MAXF : 2); break;
@@ -785,7 +789,7 @@ int mx4_init()
                allow((const void*)DYMOE_MX4_TILE64W(kMx4Plain, XT), kMx4Lds<2, 2, 2>) && allow((const void*)DYMOE_MX4_TILE128(kMx4Plain, XT), kMx4Lds<4, 2, 2>);
     };
     bool ok = plain(std::false_type()) && plain(std::true_type());
-    ok = ok && allow((const void*)DYMOE_MX4_TILE128(kMx4Up, false), kMx4Lds<4, 2, 2>) && allow((const void*)DYMOE_MX4_TILE128(kMx4Down, false), kMx4Lds<4, 2, 2>);
+    ok = ok && allow((const void*)DYMOE_MX4_TILE128(kMx4Up, false), kMx4Lds<4, 2, 2>) && allow((const void*)DYMOE_MX4_TILE128(kMx4Down, true), kMx4Lds<4, 2, 2>);
     ok = ok && allow((const void*)mx4_small_kernel<kMx4Plain, 1, 8, 8, 1, true>, (int)kMx4FuseBytes) &&
          allow((const void*)mx4_small_kernel<kMx4Up, 1, 4, 4, 1, true>, (int)kMx4FuseBytes) && allow((const void*)mx4_thin_down_kernel<2>, (int)kMx4FuseBytes);
     return ok ? DYMOE_OK : DYMOE_EHIP;
@@ -998,7 +1002,7 @@ extern "C" int dymoe_moe_ffn_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, con
     else run(mx4_small_kernel<kMx4Up, 1, 4, 1, 1>, strips(fs, 4), 256, 0);
     turn(ws + L.part, (long)mx4_round((size_t)H, 8), DYMOE_OUT_F32);
     A.splits = c.splits;
-    if (!small) run(DYMOE_MX4_TILE128(kMx4Down, false), mx4_grid(tall * ((H + 255L) / 256) * c.splits), 256, kMx4Lds<4, 2, 2>);
+    if (!small) run(DYMOE_MX4_TILE128(kMx4Down, true), mx4_grid(tall * ((H + 255L) / 256) * c.splits), 256, kMx4Lds<4, 2, 2>);
     else if (c.down_waves == 8) run(mx4_small_kernel<kMx4Down, 1, 8, 8, 1>, strips(hs, 1), 512, 0);
     else if (c.down_waves == 4) run(mx4_small_kernel<kMx4Down, 1, 4, 4, 1>, strips(hs, 1), 256, 0);
     else if (c.down_waves == 2) run(mx4_small_kernel<kMx4Down, 1, 4, 2, 1>, strips(hs, 2), 256, 0);

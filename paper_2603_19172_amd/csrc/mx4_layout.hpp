@@ -18,7 +18,7 @@ static inline size_t mx4_round(size_t v, size_t m) { return (v + m - 1) / m * m;
 struct Mx4FfnLayout {
     size_t Hp, Fp;     // columns of the codes' rows: whole tiles
     size_t xq, xs;     // [Hp / 256, T, 128] codes and [Hp / 256, T, 8] exponents of the activations
-    size_t hq, hs;     // [P, Fp / 2] and [P, Fp / 32] of the SwiGLU intermediate, by position (pairs sorted by expert)
+    size_t hq, hs;     // codes and exponents of the SwiGLU intermediate, row by row by position (pairs sorted by expert) or in tiles, see below
     size_t part;       // parts of [P, H up to a multiple of 8] outputs of the pairs, by position, fp32
     size_t plan;       // int32, see ExpertPlan
     size_t total;
@@ -36,8 +36,12 @@ static inline Mx4FfnLayout mx4_ffn_layout(long T, long H, long F, long E, long k
     auto take = [&](size_t bytes) { const size_t here = at; at += mx4_round(bytes, 256); return here; };
     L.xq = take((size_t)T * L.Hp / 2);
     L.xs = take((size_t)T * L.Hp / 32);
-    L.hq = take(P * L.Fp / 2);
-    L.hs = take(P * L.Fp / 32);
+    // Strips: by position.  Tall tiles: in tiles of 32 rows as the weights are, an expert's pairs from a tile's first row on: the expert whose first position is f and whose first
+    // tile is number j begins at tile f / 32 + j: the next has at least j + 1, and (f + n) / 32 + 1 >= f / 32 + n / 32 rounded up.  The
+    // last ends before P / 32 + P / 128 + the number of experts.
+    const size_t held = mx4_round(P + P / 4 + 32 * ((size_t)E < P ? (size_t)E : P), 32);
+    L.hq = take(held * L.Fp / 2);
+    L.hs = take(held * L.Fp / 32);
     // (more than one part only where the pairs are few: see mx4_ffn_choice)
     L.part = take((P <= kMx4SplitPairs ? kMx4MostSplits : 1) * P * mx4_round((size_t)H, 8) * 4);
     L.plan = take(expert_plan_bytes(P, (size_t)L.max_tiles));
@@ -47,7 +51,7 @@ static inline Mx4FfnLayout mx4_ffn_layout(long T, long H, long F, long E, long k
 
 struct Mx4MatLayout {
     size_t Kp;
-    size_t xq, xs;     // [T, Kp / 2] codes and [T, Kp / 32] exponents of the activations
+    size_t xq, xs;     // codes and exponents of the activations, whole tiles of 32 rows
     size_t total;
 };
 
