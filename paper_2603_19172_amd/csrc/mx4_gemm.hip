@@ -108,7 +108,7 @@ __device__ __forceinline__ void mx4_rows_to_lds(int dt, const char* x, long ldx,
 // wavefronts share a strip of 32 weight rows (of W1 and of W3 in the up projection) and take the 256-column tiles of K in turn; a workgroup of NW
 // has NW / KS strips.  Nothing is shared before the end: weights and codes come straight into registers, D tiles of a wavefront on their
 // way, and the sums of a strip's wavefronts meet in LDS.
-// Bound by the weights' bytes: 61 tokens on 8 of 128 experts of 768 x 2048, up 34.9 us (6.0 TB/s), down 19.2 (5.4); 61 x 1536 x 2048 3.6 us, a
+// Bound by the weights' bytes: 61 tokens on 8 of 128 experts of 768 x 2048, up 34.9 us (6.0 TB/s), down 19.2 (5.4); 61 x 1536 x 2048 4.3 us, a
 // start, eight wavefronts' share of K and the sums' way through LDS.
 // XT: the rows lie in tiles as the weights do, and a load of theirs is 1 KiB of contiguous memory too: 222 x 1295 x 9025 18.8 us and 22.3 row by row,
 // 61 x 1536 x 2048 3.6 / 4.4.  A call that converts its rows writes them so.
@@ -482,10 +482,10 @@ __global__ __launch_bounds__(64 * kMx4LastWaves) void mx4_thin_down_kernel(const
 //  * The rows' codes and exponents are shared by the wavefronts through three LDS buffers that global memory fills directly, two steps ahead; the 16-byte chunks of
 //    a row's 128 bytes are turned by its number, which spreads the operand reads (one chunk of 32 rows) over all banks (conflicts in 2.5 % of the
 //    cycles).  Rows in tiles (XT) come and lie in the operand's order by themselves: 512 x 4096 x 14336 27.4 us in all, 32.4 row by row.
-// 2047 x 14336 x 4096: 78 us, 3.1 PFLOP/s, the matrix units busy in 39 % of the cycles, 65 us with zeros in place of random codes (the clock is
-// the power's to set); 8192 x 8192 x 8192 4.0 PFLOP/s, 5.5 with zeros, of 5.3 to 6.4 that these instructions reach on random codes from registers alone.
-// Experts with 128 rows each, 8 of 14336 x 4096: the stream of weights, 3.9 TB/s beside the rows' copies from L2 (with 8 rows 5.6): a
-// compute unit's requests for either wait in one queue.
+// 2047 x 14336 x 4096: 72 us, 3.3 PFLOP/s, the matrix units busy in some 40 % of the cycles; codes made before, row by row: 88 us, 63 with zeros in place of
+// random ones (the clock is the power's to set); 8192 x 8192 x 8192 4.1 PFLOP/s, 5.8 with zeros, of 5.3 to 6.4 that these instructions reach on random
+// codes from registers alone.  Experts with 128 rows each, 8 of 14336 x 4096: the stream of weights, 4.3 TB/s beside the rows' copies from L2 (with 8
+// rows 5.6): a compute unit's requests for either wait in one queue.
 constexpr uint32_t kMx4Row = 128;           // bytes of a row of a step
 template <int NTF>
 constexpr uint32_t kMx4Buf = 32u * NTF * (kMx4Row + 8u);

@@ -2,7 +2,7 @@
 //
 // a = max |x| of 32 columns, e = floor(log2 a) - 2, code = x / 2^e to the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6.  A stream of bytes: 2 read and
 // 17 / 32 written a value (bf16 or fp16).  Four neighbouring lanes share a block, so nothing leaves the vector unit and every value is read once.
-// 8191 x 14336 bf16: to rows 51 us (5.8 TB/s), to tiles 56, whose pieces of 64 bytes a lane's chunk spreads over four places; back 59 and 53.
+// 8191 x 14336 bf16: to rows 51 us (5.8 TB/s), to tiles 52; back 59 and 53.
 #include "mx4_device.hpp"
 
 namespace dymoe {
@@ -140,7 +140,7 @@ static long mx4_rows_launch(long rows, int tiles, int per_row)
 template <int DT, int TILES>
 static int mx4_quantize_launch(dymoe_ctx* ctx, const void* x, long rows, long K, long ldx, uint8_t* codes, uint8_t* scale, hipStream_t st)
 {
-    constexpr int CH = 2;        // (in tiles, 61 x 2048 2.1 us and 3.6 with four, 8191 x 4096 14 and 18)
+    constexpr int CH = 2;        // (in tiles, 61 x 2048 3.0 us and 3.6 with four, 8191 x 14336 52 and 56)
     using S = Mx4Spread<TILES>;
     const long Kp = up_to(K, 256);
     const int per_row = (int)((Kp + CH * S::kCols - 1) / (CH * S::kCols));
