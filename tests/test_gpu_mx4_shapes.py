@@ -119,6 +119,41 @@ def test_a_long_rows_products(ctx):  # noqa: F811
         G.close(ctx.matmul_mx4(x, wt, out_dtype=B.OUT_F32), prod, bound, torch.float32)
 
 
+def test_products_of_codes_beyond_32_bits_of_bytes(ctx):  # noqa: F811
+    """70000 rows of 131072 columns, 4.6e9 bytes of codes: one row and its negative, sums of +-1 that 32 bits hold."""
+    T, N, K = 70000, 40, 131072
+    g = torch.Generator().manual_seed(5)
+    one = lambda *shape: (torch.randint(0, 2, shape, generator=g) * 2 - 1).half().to(DEV)  # noqa: E731
+    row, w, sign = one(1, K), one(N, K), one(T, 1)
+    wt = ctx.quantize_mx4(w, layout=B.LAYOUT_TILE)
+    x = sign * row
+    ref = sign.float() * (row.double() @ w.double().T).float()
+    assert torch.equal(ctx.matmul_mx4(x, wt, out_dtype=B.OUT_F32), ref)
+    for layout in (B.LAYOUT_ROWMAJOR, B.LAYOUT_TILE):
+        m = ctx.quantize_mx4(x, layout=layout)
+        if layout == B.LAYOUT_ROWMAJOR:
+            assert torch.equal(ctx.matmul_mx4(m, wt, out_dtype=B.OUT_F32), ref)
+        assert torch.equal(ctx.dequantize_mx4(m, out_dtype=B.OUT_F16), x)
+        del m
+    torch.cuda.empty_cache()
+
+
+def test_experts_with_an_intermediate_beyond_32_bits_of_bytes(ctx):  # noqa: F811
+    """Two kinds of token on four entries of one expert: every row has the bits of its kind, those of fewer tokens in the same shape."""
+    T, H, F, E = 60000, 256, 131072, 4
+    mats = [ctx.quantize_mx4(G.randn(i, n, m, std=0.05), layout=B.LAYOUT_TILE) for i, (n, m) in enumerate(((F, H), (F, H), (H, F)))]
+    table = B.make_mx4_table([mats] * E, DEV)
+    kind = G.randn(4, 2, H)
+    x = kind.repeat(T // 2, 1)
+    idx = torch.randint(0, E, (T, 1), generator=torch.Generator().manual_seed(6)).int().to(DEV)
+    gate = torch.ones((T, 1), device=DEV)
+    few = ctx.moe_ffn_mx4(x[:9000], idx[:9000].contiguous(), gate[:9000].contiguous(), table, F, out_dtype=B.OUT_F32)
+    assert torch.equal(few, few[:2].repeat(4500, 1)) and torch.isfinite(few).all() and (few.abs().amax(dim=1) > 0).all()
+    y = ctx.moe_ffn_mx4(x, idx, gate, table, F, out_dtype=B.OUT_F32)
+    assert torch.equal(y, few[:2].repeat(T // 2, 1))
+    torch.cuda.empty_cache()
+
+
 @pytest.mark.parametrize("T,N", [(1, 160), (40, 160), (300, 160), (1500, 5000)])
 def test_products_at_the_ends_of_the_range(ctx, T, N):  # noqa: F811
     """One sum of 512 equal products: subnormal ones are kept, those beyond the range are infinite, zeros stay zeros beside any power of two."""
