@@ -262,7 +262,8 @@ class Mx4Experts:
 class Mx4MoELayer:
     """A layer whose router scores (dymoe_route_scored) and whose experts are microscaled 4-bit numbers (dymoe_moe_ffn_mx4), every buffer
     pre-allocated: a step is three library calls on one stream, or two where the caller has the logits.  balance() and backward() are
-    the router's side of a training step: the balance loss of the last step's routing, and its logits' gradient."""
+    the router's side of a training step: the balance loss of the last step's routing, and its logits' gradient.  Another step overwrites
+    the choices (idx) and leaves the counts behind: for a gradient after that, give copies of both."""
 
     def __init__(self, ctx, T, H, F, E, k, score=B.SCORE_SIGMOID, groups=1, top_groups=1, group_best=1, renorm=True, factor=1.0,
                  out_dtype=B.OUT_BF16, device="cuda:0"):
@@ -279,23 +280,43 @@ class Mx4MoELayer:
         self.ws_router = torch.empty((B.matmul_mx4_workspace_bytes(T, E, H),), dtype=torch.uint8, device=device)
         self.ws_balance = torch.empty((B.route_balance_workspace_bytes(T, E),), dtype=torch.uint8, device=device)
         self.ws = torch.empty((B.moe_ffn_mx4_workspace_bytes(T, H, F, E, k),), dtype=torch.uint8, device=device)
+        self._routed = self._balanced = False       # whether idx is a step's, and counts that step's
 
     def step(self, x, experts, router=None, logits=None, bias=None, stream=None):
         """router: the [E, H] router as an Mx4Matrix in the tile layout; or logits [T, E] that the caller has."""
         if (experts.E, experts.H, experts.F) != (self.E, self.H, self.F):
             raise ValueError("the layer is made for other experts")
+        self._routed = self._balanced = False
         if logits is None:
             logits = self.ctx.matmul_mx4(x, router, y=self.logits, workspace=self.ws_router, stream=stream)
         self.ctx.route_scored(logits, self.k, bias=bias, idx=self.idx, w=self.gate, scores=self.scores, stream=stream, **self.routing)
+        self._routed = True
         return self.ctx.moe_ffn_mx4(x, self.idx, self.gate, experts.table, self.F, y=self.y, workspace=self.ws, stream=stream)
 
-    def balance(self, logits, coef, keep=None, stream=None):
-        """(counts [E + 1], mean [E], loss [1]) of the last step's choices under these logits."""
-        return self.ctx.route_balance(logits, self.idx, coef, score=self.routing["score"], keep=keep, counts=self.counts, mean=self.mean,
-                                      loss=self.loss, workspace=self.ws_balance, stream=stream)
+    def _choices(self, idx):
+        if idx is None and not self._routed:
+            raise RuntimeError("no step() has made choices")
+        return self.idx if idx is None else idx
 
-    def backward(self, logits, dw, coef=0.0, dloss=None, keep=None, out=None, stream=None):
-        """The logits' gradient of the last step's weights (dw [T, k]) and, with coef, of the last balance()'s loss."""
-        return self.ctx.route_scored_backward(logits, self.idx, dw=dw, score=self.routing["score"], renorm=self.routing["renorm"],
-                                              factor=self.routing["factor"], counts=self.counts if coef else None, coef=coef, dloss=dloss,
+    def balance(self, logits, coef, keep=None, idx=None, stream=None):
+        """(counts [E + 1], mean [E], loss [1]) of the last step's choices under these logits, or of the idx given: the layer's buffers."""
+        chosen = self._choices(idx)
+        self._balanced = False
+        out = self.ctx.route_balance(logits, chosen, coef, score=self.routing["score"], keep=keep, counts=self.counts, mean=self.mean,
+                                     loss=self.loss, workspace=self.ws_balance, stream=stream)
+        self._balanced = idx is None
+        return out
+
+    def backward(self, logits, dw, coef=0.0, dloss=None, keep=None, out=None, idx=None, counts=None, stream=None):
+        """The logits' gradient of the last step's weights (dw [T, k]) and, with coef, of its balance()'s loss; with idx, of the choices
+        given, and counts are then theirs."""
+        chosen = self._choices(idx)
+        if coef and counts is None:
+            if idx is not None:
+                raise ValueError("choices of the caller's own come with their counts")
+            if not self._balanced:
+                raise RuntimeError("balance() has not counted the last step's choices")
+            counts = self.counts
+        return self.ctx.route_scored_backward(logits, chosen, dw=dw, score=self.routing["score"], renorm=self.routing["renorm"],
+                                              factor=self.routing["factor"], counts=counts if coef else None, coef=coef, dloss=dloss,
                                               keep=keep, out=out, stream=stream)
