@@ -298,7 +298,7 @@ class Mx4MoELayer:
             raise RuntimeError("no step() has made choices")
         return self.idx if idx is None else idx
 
-    def balance(self, logits, coef, keep=None, idx=None, stream=None):
+    def balance(self, logits, coef, keep=None, stream=None, idx=None):
         """(counts [E + 1], mean [E], loss [1]) of the last step's choices under these logits, or of the idx given: the layer's buffers."""
         chosen = self._choices(idx)
         self._balanced = False
@@ -307,7 +307,7 @@ class Mx4MoELayer:
         self._balanced = idx is None
         return out
 
-    def backward(self, logits, dw, coef=0.0, dloss=None, keep=None, out=None, idx=None, counts=None, stream=None):
+    def backward(self, logits, dw, coef=0.0, dloss=None, keep=None, out=None, stream=None, idx=None, counts=None):
         """The logits' gradient of the last step's weights (dw [T, k]) and, with coef, of its balance()'s loss; with idx, of the choices
         given, and counts are then theirs."""
         chosen = self._choices(idx)
