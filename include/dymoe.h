@@ -642,7 +642,7 @@ typedef struct {
  * x [T,H] bf16, fp16 or fp32; idx [T,k] int32; w [T,k] fp32; table [E] of dymoe_expert_mx4 in device memory; y [T,H] in
  * out_dtype (every row is written).  A pair whose index lies outside [0,E) contributes nothing, nor does one whose
  * expert's entry holds a NULL (DYMOE_FLAG_FORMAT_MISSING, dymoe_device_flags).
- * workspace: dymoe_moe_ffn_mx4_workspace_bytes(T,H,F,E,k) bytes (0 for invalid sizes), 256-byte aligned, scratch.
+ * workspace: dymoe_moe_ffn_mx4_workspace_bytes(T,H,F,E,k) bytes (0 for invalid sizes; no fewer for a larger T), 256-byte aligned, scratch.
  * Limits: any H, F up to DYMOE_MX4_MAX_K, E <= DYMOE_MAX_EXPERTS; T k < 2^29, T times H rounded up to 256 < 2^33, and a launch of
  * fewer than 2^32 threads: T times H / 2048 rounded up < 2^24, (T k / 32 + min(E, T k)) times the larger of H / 32 and F / 32 rounded up
  * < 2^23 (else DYMOE_ENOTSUP).

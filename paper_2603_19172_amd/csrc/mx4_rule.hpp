@@ -80,11 +80,7 @@ static inline Mx4FfnChoice mx4_ffn_choice(long T, long H, long F, long E, long k
     if (T <= 32 || P <= 20 * E)
         return {Mx4FfnShape::kSmall, mx4_strip_waves(tiles * ((F + 31) / 32), (long)Hp / kMx4TileCols, 4),
                 mx4_strip_waves(tiles * ((H + 31) / 32), (long)Fp / kMx4TileCols, 8), 1};
-    // The down projection's K in parts while its tiles are fewer than two for each compute unit.
-    const long units = (P / kMx4TallRows + (E < P ? E : P)) * ((H + 255) / 256), steps = (long)Fp / kMx4TileCols;
-    int splits = 1;
-    while (P <= (long)kMx4SplitPairs && splits < kMx4MostSplits && units * splits < 2 * num_cu && steps / (2 * splits) >= 4) splits *= 2;
-    return {Mx4FfnShape::kTall, 0, 0, splits};
+    return {Mx4FfnShape::kTall, 0, 0, mx4_ffn_parts(P, H, F, E, num_cu)};
 }
 
 }  // namespace dymoe
