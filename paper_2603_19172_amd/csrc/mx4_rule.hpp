@@ -30,10 +30,11 @@ static inline Mx4MatChoice mx4_mat_choice(long T, long N, long K, bool coded, lo
     const long strips = (N + 31) / 32, t32 = (T + 31) / 32, t64 = (T + 63) / 64, t128 = (T + 127) / 128, n128 = (N + 127) / 128, n256 = (N + 255) / 256;
     // The conversion inside saves a launch while it is little: 1 x 4096 x 4096 6.1 and 7.7 with a launch of its own, 4 rows 7.0 / 7.9, 8 rows 8.4 / 7.9;
     // 8 x 1536 x 2048 5.8 / 6.8, 16 rows 7.2 / 7.0.
-    const bool fuse = !coded && T <= 32 && T * K <= 16 << 10 && mx4_fuse_bytes(T, mx4_round((size_t)K, kMx4TileCols)) <= kMx4FuseBytes;
-    // Eight wavefronts while the strips are fewer than 400: 1 x 4096 x 14336 13.2 and 15.4 with four, 61 x 1536 x 2048 7.4 / 7.2; 1 x 14336 x 4096 10.8 /
-    // 10.4, 64 x 4096 x 4096 9.7 / 9.4.
-    const Mx4MatChoice small = {Mx4MatShape::kSmall, fuse, strips * t32 < 400 ? 8 : 4};
+    const bool inside = T <= 32 && T * K <= 16 << 10 && mx4_fuse_bytes(T, mx4_round((size_t)K, kMx4TileCols)) <= kMx4FuseBytes;
+    // Eight wavefronts while the strips are fewer than 400: 1 x 4096 x 14336 13.2 and 15.4 with four, 61 x 1536 x 2048 7.4 / 7.2; kernels alone, codes made
+    // before, 1 x 14336 x 4096 7.8 / 7.3, 2 x 33000 x 2100 10.8 / 9.5.  But always where rows are converted inside (1 x 14336 x 4096 7.4 / 8.0,
+    // 32 x 14336 x 512 5.6 / 5.95, 2 x 33000 x 2100 12.1 / 11.7), and for codes of such rows, so that the order of the sums is the sizes' and not x's type's.
+    const Mx4MatChoice small = {Mx4MatShape::kSmall, inside && !coded, inside || strips * t32 < 400 ? 8 : 4};
     // Strips while tiles of 32 x 128 are few, so that each strip has a compute unit (64 x 4096 x 4096, 64 of them: 8.6 and 9.5 in tiles; 256 x 798 x 7548, 56:
     // 13.3 / 13.8; 222 x 1295 x 9025, 77: 23.2 / 15.6; 96 x 4096 x 4096, 96: 11.4 / 10.2), or somewhat more with a short K (512 x 768 x 2048, 96: 7.8 / 8.5;
     // 128 x 4096 x 4096, 128: 11.8 / 9.8); then the largest tiles that still are one for each compute unit, two of 64 x 128 (256 x 4096 x 4096 in tiles of

@@ -96,3 +96,9 @@ def test_any_chip_and_any_size_has_a_shape(product, experts, num_cu):
     for T, H, F, E, k in ((1, 1, 1, 1, 1), (1 << 22, 64, 64, 8, 8), (1000, 131072, 131072, 1024, 10), (64, 64, 131072, 1, 1)):
         shape, up, down, splits = experts(T, H, F, E, k, num_cu)
         assert shape in FFN and up in (0, 1, 2, 4) and down in (0, 1, 2, 4, 8) and splits in (1, 2, 4)
+
+
+def test_rows_and_their_codes_are_summed_alike(product):
+    for T, N, K in ((1, 12769, 4096), (1, 14336, 4096), (4, 13001, 4096), (5, 13001, 4096), (32, 12800, 512), (33, 12800, 512), (1, 4096, 14336), (8, 12800, 4096)):
+        (shape, fuse, waves), coded = product(T, N, K), product(T, N, K, coded=1)
+        assert coded == (shape, False, waves) and (waves == 8 or not fuse), (T, N, K)
