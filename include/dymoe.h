@@ -677,7 +677,7 @@ int dymoe_route_balance(dymoe_ctx* ctx, const void* logits, int dtype, const int
  *   w, renorm:  factor r q (dw - sum q dw) at the chosen experts, q[j] = s[idx[j]] / sum_j s[idx[j]]
  *   w, without renorm:  factor s (dw - sum s dw) (softmax; dw 0 at experts that were not chosen), factor s (1 - s) dw (sigmoid)
  * with r = 1 - s of a sigmoid, 1 of a softmax, and s, p as above.  The selection, its bias and groups have no gradient; counts are constants.  Masked
- * logits have gradient 0, slots whose index lies outside [0,E) no part, an expert in several slots its slots' sum.  A token with a NaN, or
+ * logits have gradient 0 (whatever dw and dloss are), slots whose index lies outside [0,E) no part, an expert in several slots its slots' sum.  A token with a NaN, or
  * with plus infinity under softmax, has NaN gradients (0 where neither part concerns it).  (Scores below e^-700, which dymoe_route_scored
  * holds at that, are not held here.)
  * logits, dtype, idx, keep, score as above, renorm and factor as in the forward call; grad [T,E] in grad_dtype (DYMOE_OUT_*), every

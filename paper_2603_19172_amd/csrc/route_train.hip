@@ -356,7 +356,9 @@ __global__ __launch_bounds__(256) void route_grad_kernel(const RouteGradArgs A)
         for (int i = 0; i < NPL; i++) {
             const int to = lane + 64 * i;
             if (to >= E) continue;
-            store_out(A.grad, t * E + to, A.grad_dtype, bad ? __builtin_nanf("") : out[i] * rest[i]);
+            // (a masked logit's terms are products with 0, and what they are taken of may be no number)
+            const float grad = l[i] == -__builtin_inff() ? 0.0f : out[i] * rest[i];
+            store_out(A.grad, t * E + to, A.grad_dtype, bad ? __builtin_nanf("") : grad);
         }
     }
 }
