@@ -611,8 +611,10 @@ int dymoe_dequantize_mx4(dymoe_ctx* ctx, const uint8_t* codes, const uint8_t* sc
 /*
  * Matrix product in microscaled 4-bit floating point:
  *   y[t,n] = sum over blocks b of 2^(ex[t,b] + ew[n,b]) sum_{j in b} xq[t,j] wq[n,j]  (+ bias[n])
- * A block's sum is exact; the sum over blocks and the bias are taken in fp32 and rounded once to the output's type.  The order of the
- * blocks belongs to the call's sizes: the same call gives the same bits, a row beside other rows may differ in its fp32 sum's last bits.
+ * A block's products and their sum are exact.  The sum over blocks is fp32, a block at a time and rounded each time; beside a block it loses what
+ * it holds below 2^-22 of that block's largest product, so that large products which cancel cost it its last bits.  The bias is added in fp32,
+ * the result rounded once to the output's type.  The order of the blocks belongs to the call's sizes: the same call gives the same bits, and so do
+ * rows and codes made from them; a row beside other rows may differ in its fp32 sum's last bits.
  * x: bf16, fp16 or fp32 [T,K], rows ldx values apart: converted in the call as by dymoe_quantize_mx4 (workspace, x_scale
  * ignored); or DYMOE_DTYPE_MX4: codes [T,Kp/2] and x_scale [T,Kp/32] that dymoe_quantize_mx4 wrote row-major, ldx = Kp (no workspace).
  * w, w_scale: [N,K] as dymoe_quantize_mx4 writes it in DYMOE_LAYOUT_TILE.  bias [N] fp32 or NULL.

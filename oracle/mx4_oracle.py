@@ -72,7 +72,8 @@ def tiles(codes, byte):
 def matmul(xv, wv):
     """The product of two matrices of values, and a bound on what fp32 sums of its blocks may be off: a matrix instruction adds two blocks'
     exact sums to what is there, which is two roundings at most, each of 2^-24 of a number no larger than the sum of the blocks'
-    magnitudes; and the parts that a shape splits K into meet in at most 16 additions."""
+    magnitudes; and the parts that a shape splits K into meet in at most 16 additions.  (For blocks of like sizes.  Beside a block whose products are much
+    larger than its sum the instruction cuts what is there: tests/test_gpu_mx4_bits.py has the bound for those.)"""
     T, K = xv.shape
     y = xv @ wv.T
     mag = np.zeros_like(y)

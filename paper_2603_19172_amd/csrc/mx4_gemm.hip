@@ -1,6 +1,6 @@
 // Products in microscaled 4-bit floating point: a matrix (dymoe_matmul_mx4) and a layer's SwiGLU experts (dymoe_moe_ffn_mx4).
 //   y[t, n] = sum over blocks b of 32 columns of 2^(ex[t, b] + ew[n, b]) sum_{j in b} xq[t, j] wq[n, j]
-// A block's sum is exact; the sum over the blocks is taken in fp32, in an order that belongs to the shape of the call.
+// A block's sum is exact; the sum over the blocks is taken in fp32 (mfma_mx4), in an order that belongs to the shape of the call.
 #include <type_traits>
 
 #include "expert_plan.hpp"

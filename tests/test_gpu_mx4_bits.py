@@ -1,11 +1,11 @@
 """GPU tests of what the microscaled 4-bit products owe bit for bit: rows converted in a call and codes made before it meet in the same sums, and
 sums that 32 bits hold are exact whatever a row's length.
 
-Tolerance of sums whose blocks are of sizes far apart, or cancel: a matrix instruction adds two blocks' sums and what is there.  The three are
-aligned to the largest of the products and of what is there, M, and cut at 2^-23 of its power of two (beside 1 and -1, 2^-23 comes through
-and 2^-24 does not), so each loses less than 2^-23 M = 2 steps of 2^-24; the result rounds once, 7 steps of 2^-24 M in all: 8 here.  M is at most
-the instruction's largest product, and those add up to at most sum |x| |w|, plus the blocks' sums so far, at most sum over blocks |sum|: for K / 64
-instructions (8 K / 64 + 16) 2^-24 sum over blocks |sum| + 8 2^-24 sum |x| |w|, with 16 for the additions of the parts that K is dealt to.
+Tolerance of sums whose blocks are of sizes far apart, or cancel, in steps of 2^-24: a matrix instruction adds a block's exact sum to what is there and
+rounds, half a step of a number no larger than the blocks' magnitudes, sum over blocks |sum|; and before that it cuts what is there, by less than a
+step of the power of two of the block's largest product (0.5 counted as 1: at most 4 times the product; 16 - 16 leaves 2^-20 beside it and not 2^-21,
+0.25 - 0.25 leaves 2^-24 and not 2^-25).  Largest products of all blocks add up to at most sum |x| |w|.  With another step for a block's
+sum beside what is there, and 16 for the additions of the parts that K is dealt to: (2 K / 32 + 16) sum over blocks |sum| + 4 sum |x| |w|.
 """
 import numpy as np
 import pytest
@@ -33,7 +33,7 @@ def product(xv, wv):
     mag = np.zeros((T, len(wv)))
     for b in range(0, K, 32):
         mag += np.abs(xv[:, b:b + 32] @ wv[:, b:b + 32].T)
-    return xv @ wv.T, ((8 * (Q.up(K, 256) // 64) + 16) * mag + 8 * (np.abs(xv) @ np.abs(wv).T)) * 2.0 ** -24
+    return xv @ wv.T, ((2 * (Q.up(K, 256) // 32) + 16) * mag + 4 * (np.abs(xv) @ np.abs(wv).T)) * 2.0 ** -24
 
 
 # both sides of the rule's lines: rows converted by every workgroup or in a launch of their own, K dealt to eight wavefronts or to four
@@ -51,3 +51,14 @@ def test_rows_and_their_codes_give_the_same_bits(ctx, T, N, K):  # noqa: F811
             assert torch.equal(y, ctx.matmul_mx4(m, wt, bias=b, out_dtype=B.OUT_F32))
     prod, bound = product(Q.values(*Q.quantize(G.f64(x)))[:, :K], Q.values(*Q.quantize(G.f64(w)))[:, :K])
     G.close(ctx.matmul_mx4(x, wt, out_dtype=B.OUT_F32), prod, bound, torch.float32)
+
+
+# the shapes by rows and outputs, as test_gpu_mx4_shapes.PRODUCTS names them
+@pytest.mark.parametrize("T,N,K", [(1, 300, 14336), (3, 13001, 300), (40, 70, 9000), (130, 2600, 256), (222, 1295, 2300), (500, 2500, 520), (520, 2300, 200),
+                                   (900, 5000, 300), (1950, 5000, 257), (2091, 4300, 520)])
+def test_blocks_that_cancel_or_are_far_apart(ctx, T, N, K):  # noqa: F811
+    x, w = spread(T, T, K), spread(N, N, K, std=0.05)
+    x[:, 1::2], w[:, 1::2] = x[:, 0:K - K % 2:2], torch.where(torch.arange(K // 2, device=DEV) % 5 > 0, -w[:, 0:K - K % 2:2], w[:, 0:K - K % 2:2])
+    prod, bound = product(Q.values(*Q.quantize(G.f64(x)))[:, :K], Q.values(*Q.quantize(G.f64(w)))[:, :K])
+    y = ctx.matmul_mx4(x, ctx.quantize_mx4(w, layout=B.LAYOUT_TILE), out_dtype=B.OUT_F32)
+    G.close(y, prod, bound, torch.float32)
