@@ -620,7 +620,7 @@ int dymoe_dequantize_mx4(dymoe_ctx* ctx, const uint8_t* codes, const uint8_t* sc
  * w, w_scale: [N,K] as dymoe_quantize_mx4 writes it in DYMOE_LAYOUT_TILE.  bias [N] fp32 or NULL.
  * y [T,N] in out_dtype (DYMOE_OUT_*), rows ldy >= N values apart; what lies between them is left as it was.
  * workspace: dymoe_matmul_mx4_workspace_bytes(T, N, K) bytes (0 for invalid sizes), 256-byte aligned, scratch.
- * Limits: K <= DYMOE_MX4_MAX_K; T, N <= 2^24, T / 32 times N / 32, both rounded up, < 2^23 (else DYMOE_ENOTSUP).
+ * Limits: K <= DYMOE_MX4_MAX_K; T, N <= 2^24, T / 128 times N / 256, both rounded up, <= 2^24 - 64 (else DYMOE_ENOTSUP).
  */
 size_t dymoe_matmul_mx4_workspace_bytes(int T, int N, int K);
 int dymoe_matmul_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, const uint8_t* x_scale, long ldx, const uint8_t* w,
@@ -646,8 +646,8 @@ typedef struct {
  * expert's entry holds a NULL (DYMOE_FLAG_FORMAT_MISSING, dymoe_device_flags).
  * workspace: dymoe_moe_ffn_mx4_workspace_bytes(T,H,F,E,k) bytes (0 for invalid sizes; no fewer for a larger T), 256-byte aligned, scratch.
  * Limits: any H, F up to DYMOE_MX4_MAX_K, E <= DYMOE_MAX_EXPERTS; T k < 2^29, T times H rounded up to 256 < 2^33, and a launch of
- * fewer than 2^32 threads: T times H / 2048 rounded up < 2^24, (T k / 32 + min(E, T k)) times the larger of H / 32 and F / 32 rounded up
- * < 2^23 (else DYMOE_ENOTSUP).
+ * fewer than 2^32 threads: T times H / 2048 rounded up < 2^24, (T k / 128 rounded down + min(E, T k)) times the larger of H / 256 rounded up and
+ * twice F / 256 rounded up <= 2^24 - 64 (else DYMOE_ENOTSUP).
  */
 size_t dymoe_moe_ffn_mx4_workspace_bytes(int T, int H, int F, int E, int k);
 int dymoe_moe_ffn_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, const int32_t* idx, const float* w,

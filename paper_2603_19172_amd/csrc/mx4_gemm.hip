@@ -704,7 +704,8 @@ __device__ __forceinline__ void mx4_tile(const Mx4Args& A, const int32_t* perm, 
 // weights (the tiles of a matrix or expert, for one column block) are neighbours.
 constexpr int kMx4Run = 8;
 __device__ __forceinline__ long mx4_unit_of_group() { return ((long)(blockIdx.x >> 3) / kMx4Run * 8 + (blockIdx.x & 7)) * kMx4Run + (blockIdx.x >> 3) % kMx4Run; }
-static dim3 mx4_grid(long units) { return dim3((unsigned)(((units + kMx4Run - 1) / kMx4Run + 7) / 8 * 8 * kMx4Run)); }
+static long mx4_groups(long units) { return ((units + kMx4Run - 1) / kMx4Run + 7) / 8 * 8 * kMx4Run; }
+static dim3 mx4_grid(long units) { return dim3((unsigned)mx4_groups(units)); }
 
 __device__ __forceinline__ uint32_t mx4_lds_base(char* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)p; }
 
@@ -858,8 +859,9 @@ extern "C" int dymoe_matmul_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, cons
     if (K > DYMOE_MX4_MAX_K || T > (1 << 24) || N > (1 << 24)) return DYMOE_ENOTSUP;
     const Mx4MatLayout L = mx4_mat_layout(T, K);
     if (!coded && T > 0 && workspace_bytes < L.total) return DYMOE_ENOSPC;
-    const long groups = (T + 31L) / 32 * ((N + 31L) / 32);
-    if (!fits_grid(groups, 512)) return DYMOE_ENOTSUP;
+    // (the other shapes are taken while tiles are few, or with up to 32 rows: 2^19 strips of 512 threads at most)
+    const long n128 = (N + 127L) / 128, n256 = (N + 255L) / 256, t128 = (T + 127L) / 128;
+    if (!fits_grid(mx4_groups(t128 * n256), 256)) return DYMOE_ENOTSUP;
     if (!ctx) return DYMOE_ENOCTX;
     if (T == 0) return DYMOE_OK;
     hipStream_t st = (hipStream_t)stream;
@@ -887,14 +889,14 @@ extern "C" int dymoe_matmul_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, cons
     A.Kp = (int)L.Kp;
     A.N = N;
     A.out_dtype = out_dtype;
-    const long n128 = (N + 127L) / 128, n256 = (N + 255L) / 256;
+    const long groups = (T + 31L) / 32 * ((N + 31L) / 32);
     auto run = [&](void (*kernel)(const Mx4Args), dim3 grid, int threads, int lds) {
         dymoe_launch(ctx, DYMOE_K_MX4_PRODUCT, kernel, grid, dim3((unsigned)threads), lds, st, A);
     };
     // rows converted in the call lie in tiles, codes made before row by row
     auto launch = [&](auto xt) {
         constexpr bool XT = decltype(xt)::value;
-        const long t32 = (T + 31L) / 32, t64 = (T + 63L) / 64, t128 = (T + 127L) / 128;
+        const long t32 = (T + 31L) / 32, t64 = (T + 63L) / 64;
         switch (c.shape) {
         case Mx4MatShape::kSmall:
             if (c.waves == 8) run(mx4_small_kernel<kMx4Plain, 1, 8, 8, 1, false, XT>, dim3((unsigned)groups), 512, 0);
@@ -935,8 +937,12 @@ extern "C" int dymoe_moe_ffn_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, con
     if (P >= 1L << 29 || (long)T * up_to(H, kMx4TileCols) / 2 >= 1L << 32) return DYMOE_ENOTSUP;      // (32-bit offsets into the codes)
     const Mx4FfnLayout L = mx4_ffn_layout(T, H, F, E, k);
     if (workspace_bytes < L.total) return DYMOE_ENOSPC;
-    const long up = (long)L.max_tiles * (long)(L.Fp / 32), down = (long)L.max_tiles * ((H + 31L) / 32);     // workgroups at most
-    if (!fits_grid(up, 512) || !fits_grid(down, 512) || !fits_grid(T * ((H + 2047L) / 2048), 256)) return DYMOE_ENOTSUP;
+    // Tall tiles' workgroups; K is in parts only where they are few.  (Strips are taken for up to 20 E pairs, or 32 tokens: 2048 tiles of 4096 strips at
+    // most, four to a workgroup of 256 threads.)
+    const long tall = P / kMx4TallRows + (E < P ? E : P);
+    if (!fits_grid(mx4_groups(tall * (long)(L.Fp / 128)), 256) || !fits_grid(mx4_groups(tall * ((H + 255L) / 256)), 256) ||
+        !fits_grid(T * ((H + 2047L) / 2048), 256))
+        return DYMOE_ENOTSUP;
     if (!ctx) return DYMOE_ENOCTX;
     if (T == 0) return DYMOE_OK;
     hipStream_t st = (hipStream_t)stream;
@@ -993,7 +999,6 @@ extern "C" int dymoe_moe_ffn_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, con
     A.x = ws + L.xq;
     A.xs = ws + L.xs;
     A.plan = plan;
-    const long tall = P / kMx4TallRows + (E < P ? E : P);
     auto strips = [&](long n, int each) { return dim3((unsigned)(L.max_tiles * ((n + each - 1) / each))); };
     const long fs = (long)(L.Fp / 32), hs = (H + 31L) / 32;
     if (!small) run(DYMOE_MX4_TILE128(kMx4Up, false), mx4_grid(tall * (long)(L.Fp / 128)), 256, kMx4Lds<4, 2, 2>);
