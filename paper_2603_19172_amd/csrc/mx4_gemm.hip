@@ -104,10 +104,10 @@ __device__ __forceinline__ void mx4_rows_to_lds(int dt, const char* x, long ldx,
 }
 
 // ----------------------------------------------------------------------------
-// Tiles of up to 32 NTF rows where rows or columns are too few for the tiles below (decode batches, narrow matrices): a stream of weights.  KS
+// Tiles of up to 32 rows where rows or columns are too few for the tiles below (decode batches, narrow matrices): a stream of weights.  KS
 // wavefronts share a strip of 32 weight rows (of W1 and of W3 in the up projection) and take the 256-column tiles of K in turn; a workgroup of NW
-// has NW / KS strips.  Nothing is shared before the end: weights and codes come straight into registers, D tiles of a wavefront on their
-// way, and the sums of a strip's wavefronts meet in LDS.
+// has NW / KS strips.  Nothing is shared before the end: weights and codes come straight into registers, a tile ahead of a wavefront's products, and
+// the sums of a strip's wavefronts meet in LDS.
 // Bound by the weights' bytes: 61 tokens on 8 of 128 experts of 768 x 2048, up 34.9 us (6.0 TB/s), down 19.2 (5.4); 61 x 1536 x 2048 4.3 us, a
 // start, eight wavefronts' share of K and the sums' way through LDS.
 // XT: the rows lie in tiles as the weights do, and a load of theirs is 1 KiB of contiguous memory too: 222 x 1295 x 9025 18.8 us and 22.3 row by row,
@@ -115,17 +115,17 @@ __device__ __forceinline__ void mx4_rows_to_lds(int dt, const char* x, long ldx,
 // FUSE: the rows come as they are, few enough for every workgroup to convert them for itself, behind its first loads of weights; the experts' pairs
 // are then looked through by every workgroup too: the one of a pair that comes first among those of its expert (or 32, 64, ... behind
 // the first) takes the next 32 of them, and a pair's position is its number.
-template <int MODE, int NTF, int NW, int KS, int D, bool FUSE = false, bool XT = false>
+template <int MODE, int NW, int KS, bool FUSE = false, bool XT = false>
 __global__ __launch_bounds__(64 * NW) void mx4_small_kernel(const Mx4Args A)
 {
-    constexpr int S = MODE == kMx4Up ? 2 : 1, kSums = S * NTF, kRows = 32 * NTF, kStrips = NW / KS;
+    constexpr int S = MODE == kMx4Up ? 2 : 1, kRows = 32, kStrips = NW / KS;
     constexpr int kParts = KS > 4 ? 4 : KS;      // wavefronts that finish a strip
     constexpr int kV = 16 / kParts;              // registers of a fragment that each of them finishes
     static_assert(NW % KS == 0 && (KS == 8 || KS == 4 || KS == 2 || KS == 1), "");
-    static_assert(!FUSE || (MODE != kMx4Down && NTF == 1), "");
+    static_assert(!FUSE || MODE != kMx4Down, "");
     extern __shared__ __attribute__((aligned(16))) char s_rows[];
-    __shared__ float s_red[KS > 1 ? kStrips * kParts : 1][kSums][16][kWave];
-    __shared__ uint32_t s_peak[kStrips][NTF][kParts][32];
+    __shared__ float s_red[KS > 1 ? kStrips * kParts : 1][S][16][kWave];
+    __shared__ uint32_t s_peak[kStrips][kParts][32];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int ln = lane & 31, kb = lane >> 5, mine = wave / KS, part = wave - mine * KS;
     const int strips = (A.N + 31) / 32, all = MODE == kMx4Up ? (int)(A.ldo >> 5) : strips, nblk = (all + kStrips - 1) / kStrips;
@@ -170,14 +170,15 @@ __global__ __launch_bounds__(64 * NW) void mx4_small_kernel(const Mx4Args A)
         if (MODE == kMx4Up) w[S - 1].set(t.mat.q[1], t.mat.s[1], bx, strips, A.Kp);
     }
     struct Tile {
-        uint4 w[S][4], x[NTF][4];
-        uint32_t ws[S], xs[NTF];
+        uint4 w[S][4], x[4];
+        uint32_t ws[S], xs;
     };
     const uint32_t lane16 = (uint32_t)lane * 16u, lane4 = (uint32_t)lane * 4u;
     const int nkt = A.Kp >> 8;
-    uint32_t off[NTF], offs[NTF];
+    uint32_t off, offs;
     const uint32_t step_x = XT ? 4096u : MODE == kMx4Up ? (uint32_t)A.rows * 128u : 128u;
     BufferSrc x, xs;
+    // (the tile as an argument: captured, the compiler copies all of its registers once more in every step)
     auto load_w = [&](Tile& t, int kt) {
 #pragma unroll
         for (int s = 0; s < S; s++) {
@@ -189,92 +190,69 @@ __global__ __launch_bounds__(64 * NW) void mx4_small_kernel(const Mx4Args A)
     auto load_x = [&](Tile& t, int kt) {
         if (FUSE) return;
 #pragma unroll
-        for (int f = 0; f < NTF; f++) {
-#pragma unroll
-            for (int c = 0; c < 4; c++) t.x[f][c] = x.load(off[f] + (uint32_t)c * (XT ? 1024u : 16u), (uint32_t)kt * step_x);
-            t.xs[f] = load_u32(xs, offs[f], (uint32_t)kt * (step_x >> 4));
-        }
+        for (int c = 0; c < 4; c++) t.x[c] = x.load(off + (uint32_t)c * (XT ? 1024u : 16u), (uint32_t)kt * step_x);
+        t.xs = load_u32(xs, offs, (uint32_t)kt * (step_x >> 4));
     };
-    Tile ring[D];
+    Tile tile;
     int kt = part;
-#pragma unroll
-    for (int d = 0; d < D; d++)
-        if (kt + d * KS < nkt) load_w(ring[d], kt + d * KS);               // (the weights need nothing of the rows)
+    if (kt < nkt) load_w(tile, kt);               // (the weights need nothing of the rows)
     if (FUSE) {
         mx4_rows_to_lds(A.x_dtype, A.x, A.ldx, A.rows, A.K, A.Kp, s_rows);
         const int row = MODE == kMx4Up ? row0 / A.k : row0 + min(ln, rows - 1);
-        off[0] = (uint32_t)(row * mx4_lds_row(A.Kp)) + 64u * (uint32_t)kb;
-        offs[0] = (uint32_t)(A.rows * mx4_lds_row(A.Kp) + row * (A.Kp >> 5)) + 4u * (uint32_t)kb;
-    }
-#pragma unroll
-    for (int f = 0; f < NTF && !FUSE; f++) {
-        if (XT) {
-            off[f] = (uint32_t)f * 16u * (uint32_t)A.Kp + lane16;
-            offs[f] = (uint32_t)f * (uint32_t)A.Kp + lane4;
-            continue;
-        }
-        const int r = min(32 * f + ln, rows - 1);                            // rows behind the last: computed and dropped
+        off = (uint32_t)(row * mx4_lds_row(A.Kp)) + 64u * (uint32_t)kb;
+        offs = (uint32_t)(A.rows * mx4_lds_row(A.Kp) + row * (A.Kp >> 5)) + 4u * (uint32_t)kb;
+    } else if (XT) {
+        off = lane16;
+        offs = lane4;
+    } else {
+        const int r = min(ln, rows - 1);                                     // rows behind the last: computed and dropped
         const uint32_t row = MODE == kMx4Up ? (uint32_t)(pp.perm[row0 + r] / A.k) : (uint32_t)r;
-        off[f] = row * (MODE == kMx4Up ? 128u : (uint32_t)(A.Kp >> 1)) + 64u * (uint32_t)kb;
-        offs[f] = row * (MODE == kMx4Up ? 8u : (uint32_t)(A.Kp >> 5)) + 4u * (uint32_t)kb;
+        off = row * (MODE == kMx4Up ? 128u : (uint32_t)(A.Kp >> 1)) + 64u * (uint32_t)kb;
+        offs = row * (MODE == kMx4Up ? 8u : (uint32_t)(A.Kp >> 5)) + 4u * (uint32_t)kb;
     }
     const long from = MODE == kMx4Up ? 0 : row0;
     const uint32_t held = XT ? (uint32_t)(rows + 31) / 32u * 32u : MODE == kMx4Up ? A.rows : rows;
     x.set(A.x + from * (A.Kp >> 1), held * (uint32_t)(A.Kp >> 1));
     xs.set(A.xs + from * (A.Kp >> 5), held * (uint32_t)(A.Kp >> 5));
-#pragma unroll
-    for (int d = 0; d < D; d++)
-        if (kt + d * KS < nkt) load_x(ring[d], kt + d * KS);
-    float16_t acc[S][NTF] = {};
+    if (kt < nkt) load_x(tile, kt);
+    float16_t acc[S] = {};
     auto multiply = [&](const Tile& t) {
 #pragma unroll
-        for (int s = 0; s < S; s++)
-#pragma unroll
-            for (int f = 0; f < NTF; f++) {
-                acc[s][f] = mfma_mx4<0, 0>(t.w[s][0], t.x[f][0], acc[s][f], t.ws[s], t.xs[f]);
-                acc[s][f] = mfma_mx4<1, 1>(t.w[s][1], t.x[f][1], acc[s][f], t.ws[s], t.xs[f]);
-                acc[s][f] = mfma_mx4<2, 2>(t.w[s][2], t.x[f][2], acc[s][f], t.ws[s], t.xs[f]);
-                acc[s][f] = mfma_mx4<3, 3>(t.w[s][3], t.x[f][3], acc[s][f], t.ws[s], t.xs[f]);
-            }
-    };
-    while (kt < nkt) {
-#pragma unroll
-        for (int d = 0; d < D; d++) {
-            if (kt < nkt) {
-                if (FUSE) {
-#pragma unroll
-                    for (int c = 0; c < 4; c++) ring[d].x[0][c] = *(const uint4*)(s_rows + off[0] + kt * 128 + c * 16);
-                    ring[d].xs[0] = *(const uint32_t*)(s_rows + offs[0] + kt * 8);
-                }
-                multiply(ring[d]);
-                __builtin_amdgcn_sched_barrier(0);
-                if (kt + D * KS < nkt) {
-                    load_w(ring[d], kt + D * KS);
-                    load_x(ring[d], kt + D * KS);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            kt += KS;
+        for (int s = 0; s < S; s++) {
+            acc[s] = mfma_mx4<0, 0>(t.w[s][0], t.x[0], acc[s], t.ws[s], t.xs);
+            acc[s] = mfma_mx4<1, 1>(t.w[s][1], t.x[1], acc[s], t.ws[s], t.xs);
+            acc[s] = mfma_mx4<2, 2>(t.w[s][2], t.x[2], acc[s], t.ws[s], t.xs);
+            acc[s] = mfma_mx4<3, 3>(t.w[s][3], t.x[3], acc[s], t.ws[s], t.xs);
         }
+    };
+    for (; kt < nkt; kt += KS) {
+        if (FUSE) {
+#pragma unroll
+            for (int c = 0; c < 4; c++) tile.x[c] = *(const uint4*)(s_rows + off + kt * 128 + c * 16);
+            tile.xs = *(const uint32_t*)(s_rows + offs + kt * 8);
+        }
+        multiply(tile);
+        __builtin_amdgcn_sched_barrier(0);
+        if (kt + KS < nkt) {
+            load_w(tile, kt + KS);
+            load_x(tile, kt + KS);
+        }
+        __builtin_amdgcn_sched_barrier(0);
     }
     // the strip's sums: register kV * part + i of this lane, from the wavefronts in their order
-    float sum[S][NTF][kV];
+    float sum[S][kV];
     if constexpr (KS == 1) {
 #pragma unroll
         for (int s = 0; s < S; s++)
 #pragma unroll
-            for (int f = 0; f < NTF; f++)
-#pragma unroll
-                for (int i = 0; i < 16; i++) sum[s][f][i] = acc[s][f][i];
+            for (int i = 0; i < 16; i++) sum[s][i] = acc[s][i];
     } else {
         const int at = mine * kParts + (part & (kParts - 1));
         auto put = [&]() {
 #pragma unroll
             for (int s = 0; s < S; s++)
 #pragma unroll
-                for (int f = 0; f < NTF; f++)
-#pragma unroll
-                    for (int i = 0; i < 16; i++) s_red[at][s * NTF + f][i][lane] = acc[s][f][i];
+                for (int i = 0; i < 16; i++) s_red[at][s][i][lane] = acc[s][i];
         };
         if constexpr (KS > kParts) {
             if (part >= kParts) put();
@@ -283,9 +261,7 @@ __global__ __launch_bounds__(64 * NW) void mx4_small_kernel(const Mx4Args A)
 #pragma unroll
                 for (int s = 0; s < S; s++)
 #pragma unroll
-                    for (int f = 0; f < NTF; f++)
-#pragma unroll
-                        for (int i = 0; i < 16; i++) acc[s][f][i] += s_red[at][s * NTF + f][i][lane];
+                    for (int i = 0; i < 16; i++) acc[s][i] += s_red[at][s][i][lane];
                 put();                          // (its own place, read by none but it)
             }
         } else {
@@ -295,73 +271,56 @@ __global__ __launch_bounds__(64 * NW) void mx4_small_kernel(const Mx4Args A)
 #pragma unroll
         for (int s = 0; s < S; s++)
 #pragma unroll
-            for (int f = 0; f < NTF; f++)
+            for (int i = 0; i < kV; i++) {
+                const int reg = kV * (part & (kParts - 1)) + i;
+                float v = s_red[mine * kParts][s][reg][lane];
 #pragma unroll
-                for (int i = 0; i < kV; i++) {
-                    const int reg = kV * (part & (kParts - 1)) + i;
-                    float v = s_red[mine * kParts][s * NTF + f][reg][lane];
-#pragma unroll
-                    for (int q = 1; q < kParts; q++) v += s_red[mine * kParts + q][s * NTF + f][reg][lane];
-                    sum[s][f][i] = v;
-                }
+                for (int q = 1; q < kParts; q++) v += s_red[mine * kParts + q][s][reg][lane];
+                sum[s][i] = v;
+            }
     }
     // register 4 g + i: weight row 8 g + 4 kb + i, token ln
     if constexpr (MODE == kMx4Up) {
-        uint32_t h[NTF][kV], peak[NTF];
+        uint32_t h[kV], m = 0;
 #pragma unroll
-        for (int f = 0; f < NTF; f++) {
-            uint32_t m = 0;
-#pragma unroll
-            for (int i = 0; i < kV; i++) {
-                h[f][i] = __float_as_uint(silu_times(sum[0][f][i], sum[S - 1][f][i]));
-                m = max(m, h[f][i] & 0x7fffffffu);
-            }
-            const auto both = __builtin_amdgcn_permlane32_swap(m, m, false, false);
-            peak[f] = max(both[0], both[1]);
-            if (KS > 1 && part < kParts && kb == 0) s_peak[mine][f][part][ln] = peak[f];
+        for (int i = 0; i < kV; i++) {
+            h[i] = __float_as_uint(silu_times(sum[0][i], sum[S - 1][i]));
+            m = max(m, h[i] & 0x7fffffffu);
         }
+        const auto halves = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+        uint32_t peak = max(halves[0], halves[1]);
         if constexpr (KS > 1) {
+            if (part < kParts && kb == 0) s_peak[mine][part][ln] = peak;
             __syncthreads();
 #pragma unroll
-            for (int f = 0; f < NTF; f++)
-#pragma unroll
-                for (int q = 0; q < kParts; q++) peak[f] = max(peak[f], s_peak[mine][f][q][ln]);
+            for (int q = 0; q < kParts; q++) peak = max(peak, s_peak[mine][q][ln]);
         }
         if (part >= kParts || bx >= all) return;
+        const uint32_t byte = mx4_exponent(peak);
+        const float unit = mx4_unit(byte);
+        const long out = (FUSE ? (long)row0 : (long)(row0 + ln)) * A.ldo + 32L * bx;
 #pragma unroll
-        for (int f = 0; f < NTF; f++) {
-            const int row = 32 * f + ln;
-            const uint32_t byte = mx4_exponent(peak[f]);
-            const float unit = mx4_unit(byte);
-            const long out = (FUSE ? (long)row0 : (long)(row0 + row)) * A.ldo + 32L * bx;
-#pragma unroll
-            for (int g = 0; g < kV / 4; g++) {
-                uint32_t q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, __uint_as_float(h[f][4 * g]), __uint_as_float(h[f][4 * g + 1]), unit, 0);
-                q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, __uint_as_float(h[f][4 * g + 2]), __uint_as_float(h[f][4 * g + 3]), unit, 1);
-                const auto both = __builtin_amdgcn_permlane32_swap(q, q, false, false);
-                q = byte == 255u ? 0u : (both[0] & 0xffffu) | (both[1] << 16);
-                if (kb == 0 && row < rows) *(DYMOE_GLOBAL uint32_t*)((char*)A.out + out / 2 + 4 * (kV / 4 * part + g)) = q;
-            }
-            if (kb == 0 && row < rows && part == 0) *(DYMOE_GLOBAL uint8_t*)(A.out_scale + out / 32) = (uint8_t)byte;
+        for (int g = 0; g < kV / 4; g++) {
+            uint32_t q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, __uint_as_float(h[4 * g]), __uint_as_float(h[4 * g + 1]), unit, 0);
+            q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, __uint_as_float(h[4 * g + 2]), __uint_as_float(h[4 * g + 3]), unit, 1);
+            const auto both = __builtin_amdgcn_permlane32_swap(q, q, false, false);
+            q = byte == 255u ? 0u : (both[0] & 0xffffu) | (both[1] << 16);
+            if (kb == 0 && ln < rows) *(DYMOE_GLOBAL uint32_t*)((char*)A.out + out / 2 + 4 * (kV / 4 * part + g)) = q;
         }
+        if (kb == 0 && ln < rows && part == 0) *(DYMOE_GLOBAL uint8_t*)(A.out_scale + out / 32) = (uint8_t)byte;
     } else {
-        if (part >= kParts) return;
+        if (part >= kParts || ln >= rows) return;
 #pragma unroll
-        for (int f = 0; f < NTF; f++) {
-            const int row = 32 * f + ln;
-            if (row >= rows) continue;
+        for (int g = 0; g < kV / 4; g++) {
+            const int n = 32 * bx + 8 * (kV / 4 * part + g) + 4 * kb, left = A.N - n;
+            if (left <= 0) continue;
+            float v[4];
 #pragma unroll
-            for (int g = 0; g < kV / 4; g++) {
-                const int n = 32 * bx + 8 * (kV / 4 * part + g) + 4 * kb, left = A.N - n;
-                if (left <= 0) continue;
-                float v[4];
-#pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    v[i] = sum[0][f][4 * g + i];
-                    if (MODE == kMx4Plain && A.bias) v[i] += A.bias[min(n + i, A.N - 1)];
-                }
-                store_any4(A.out, (long)(row0 + row) * A.ldo + n, MODE == kMx4Plain ? A.out_dtype : DYMOE_OUT_F32, left, v);
+            for (int i = 0; i < 4; i++) {
+                v[i] = sum[0][4 * g + i];
+                if (MODE == kMx4Plain && A.bias) v[i] += A.bias[min(n + i, A.N - 1)];
             }
+            store_any4(A.out, (long)(row0 + ln) * A.ldo + n, MODE == kMx4Plain ? A.out_dtype : DYMOE_OUT_F32, left, v);
         }
     }
 }
@@ -791,8 +750,8 @@ int mx4_init()
     };
     bool ok = plain(std::false_type()) && plain(std::true_type());
     ok = ok && allow((const void*)DYMOE_MX4_TILE128(kMx4Up, false), kMx4Lds<4, 2, 2>) && allow((const void*)DYMOE_MX4_TILE128(kMx4Down, true), kMx4Lds<4, 2, 2>);
-    ok = ok && allow((const void*)mx4_small_kernel<kMx4Plain, 1, 8, 8, 1, true>, (int)kMx4FuseBytes) &&
-         allow((const void*)mx4_small_kernel<kMx4Up, 1, 4, 4, 1, true>, (int)kMx4FuseBytes) && allow((const void*)mx4_thin_down_kernel<2>, (int)kMx4FuseBytes);
+    ok = ok && allow((const void*)mx4_small_kernel<kMx4Plain, 8, 8, true>, (int)kMx4FuseBytes) &&
+         allow((const void*)mx4_small_kernel<kMx4Up, 4, 4, true>, (int)kMx4FuseBytes) && allow((const void*)mx4_thin_down_kernel<2>, (int)kMx4FuseBytes);
     return ok ? DYMOE_OK : DYMOE_EHIP;
 }
 
@@ -899,8 +858,8 @@ extern "C" int dymoe_matmul_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, cons
         const long t32 = (T + 31L) / 32, t64 = (T + 63L) / 64;
         switch (c.shape) {
         case Mx4MatShape::kSmall:
-            if (c.waves == 8) run(mx4_small_kernel<kMx4Plain, 1, 8, 8, 1, false, XT>, dim3((unsigned)groups), 512, 0);
-            else run(mx4_small_kernel<kMx4Plain, 1, 4, 4, 1, false, XT>, dim3((unsigned)groups), 256, 0);
+            if (c.waves == 8) run(mx4_small_kernel<kMx4Plain, 8, 8, false, XT>, dim3((unsigned)groups), 512, 0);
+            else run(mx4_small_kernel<kMx4Plain, 4, 4, false, XT>, dim3((unsigned)groups), 256, 0);
             break;
         case Mx4MatShape::kTile32: run(DYMOE_MX4_TILE32(kMx4Plain, XT), mx4_grid(t32 * n128), 256, kMx4Lds<1, 1, 4>); break;
         case Mx4MatShape::kTile64: run(DYMOE_MX4_TILE64(kMx4Plain, XT), mx4_grid(t64 * n128), 256, kMx4Lds<2, 1, 3>); break;
@@ -908,7 +867,7 @@ extern "C" int dymoe_matmul_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, cons
         default: run(DYMOE_MX4_TILE128(kMx4Plain, XT), mx4_grid(t128 * n256), 256, kMx4Lds<4, 2, 2>);
         }
     };
-    if (c.fuse) run(mx4_small_kernel<kMx4Plain, 1, 8, 8, 1, true, false>, dim3((unsigned)groups), 512, (int)mx4_fuse_bytes(T, L.Kp));
+    if (c.fuse) run(mx4_small_kernel<kMx4Plain, 8, 8, true, false>, dim3((unsigned)groups), 512, (int)mx4_fuse_bytes(T, L.Kp));
     else if (coded) launch(std::false_type());
     else launch(std::true_type());
     DYMOE_HIP_LAUNCH_CHECK();
@@ -981,7 +940,7 @@ extern "C" int dymoe_moe_ffn_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, con
         A.table = table;
         A.flags = ctx->device_flags;
         A.E = E;
-        run(mx4_small_kernel<kMx4Up, 1, 4, 4, 1, true>, dim3((unsigned)(P * (long)(L.Fp / 32))), 256, (int)mx4_fuse_bytes(T, L.Hp));
+        run(mx4_small_kernel<kMx4Up, 4, 4, true>, dim3((unsigned)(P * (long)(L.Fp / 32))), 256, (int)mx4_fuse_bytes(T, L.Hp));
         turn(y, H, out_dtype);
         run(mx4_thin_down_kernel<2>, dim3((unsigned)(8L * T * (((H + 15L) / 16 + 7) / 8))), 64 * kMx4LastWaves, (int)mx4_fuse_bytes(k, L.Fp));
         DYMOE_HIP_LAUNCH_CHECK();
@@ -1002,16 +961,16 @@ extern "C" int dymoe_moe_ffn_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, con
     auto strips = [&](long n, int each) { return dim3((unsigned)(L.max_tiles * ((n + each - 1) / each))); };
     const long fs = (long)(L.Fp / 32), hs = (H + 31L) / 32;
     if (!small) run(DYMOE_MX4_TILE128(kMx4Up, false), mx4_grid(tall * (long)(L.Fp / 128)), 256, kMx4Lds<4, 2, 2>);
-    else if (c.up_waves == 4) run(mx4_small_kernel<kMx4Up, 1, 4, 4, 1>, strips(fs, 1), 256, 0);
-    else if (c.up_waves == 2) run(mx4_small_kernel<kMx4Up, 1, 4, 2, 1>, strips(fs, 2), 256, 0);
-    else run(mx4_small_kernel<kMx4Up, 1, 4, 1, 1>, strips(fs, 4), 256, 0);
+    else if (c.up_waves == 4) run(mx4_small_kernel<kMx4Up, 4, 4>, strips(fs, 1), 256, 0);
+    else if (c.up_waves == 2) run(mx4_small_kernel<kMx4Up, 4, 2>, strips(fs, 2), 256, 0);
+    else run(mx4_small_kernel<kMx4Up, 4, 1>, strips(fs, 4), 256, 0);
     turn(ws + L.part, (long)mx4_round((size_t)H, 8), DYMOE_OUT_F32);
     A.splits = c.splits;
     if (!small) run(DYMOE_MX4_TILE128(kMx4Down, true), mx4_grid(tall * ((H + 255L) / 256) * c.splits), 256, kMx4Lds<4, 2, 2>);
-    else if (c.down_waves == 8) run(mx4_small_kernel<kMx4Down, 1, 8, 8, 1>, strips(hs, 1), 512, 0);
-    else if (c.down_waves == 4) run(mx4_small_kernel<kMx4Down, 1, 4, 4, 1>, strips(hs, 1), 256, 0);
-    else if (c.down_waves == 2) run(mx4_small_kernel<kMx4Down, 1, 4, 2, 1>, strips(hs, 2), 256, 0);
-    else run(mx4_small_kernel<kMx4Down, 1, 4, 1, 1>, strips(hs, 4), 256, 0);
+    else if (c.down_waves == 8) run(mx4_small_kernel<kMx4Down, 8, 8>, strips(hs, 1), 512, 0);
+    else if (c.down_waves == 4) run(mx4_small_kernel<kMx4Down, 4, 4>, strips(hs, 1), 256, 0);
+    else if (c.down_waves == 2) run(mx4_small_kernel<kMx4Down, 4, 2>, strips(hs, 2), 256, 0);
+    else run(mx4_small_kernel<kMx4Down, 4, 1>, strips(hs, 4), 256, 0);
     auto combine = c.splits == 1 ? mx4_combine_kernel<1> : c.splits == 2 ? mx4_combine_kernel<2> : mx4_combine_kernel<4>;
     dymoe_launch(ctx, DYMOE_K_MX4_ROWS, combine, dim3((unsigned)(T * ((H + 2047L) / 2048))), dim3(256), 0, st, (const float*)(ws + L.part), A.ldo, P,
                  expert_plan<dymoe_expert_mx4>(plan, P).where, w, H, k, out_dtype, y);
