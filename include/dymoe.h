@@ -638,7 +638,7 @@ typedef struct {
  * SwiGLU experts in microscaled 4-bit floating point, activations and intermediate converted on the way:
  *   y[t,:] = sum_{slot<k} w[t,slot] * W2_e q( silu(W1_e q(x_t)) * (W3_e q(x_t)) ),  e = idx[t,slot],
  * q() the conversion of dymoe_quantize_mx4, the products those of dymoe_matmul_mx4.  The SwiGLU intermediate, each pair's output
- * and the sum over the slots are held in fp32, rounded once to y's type.  The same call gives the same bits; the order of the fp32 sums
+ * and the sum over the slots are held in fp32, rounded once to y's type (silu(a) is 0 from a = -87.3 down, where e^-a passes 2^126).  The same call gives the same bits; the order of the fp32 sums
  * belongs to the call's sizes and routing, so that beside other tokens an intermediate value next to the middle of two codes may get the
  * other one.
  * x [T,H] bf16, fp16 or fp32; idx [T,k] int32; w [T,k] fp32; table [E] of dymoe_expert_mx4 in device memory; y [T,H] in

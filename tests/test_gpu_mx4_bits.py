@@ -62,3 +62,61 @@ def test_blocks_that_cancel_or_are_far_apart(ctx, T, N, K):  # noqa: F811
     prod, bound = product(Q.values(*Q.quantize(G.f64(x)))[:, :K], Q.values(*Q.quantize(G.f64(w)))[:, :K])
     y = ctx.matmul_mx4(x, ctx.quantize_mx4(w, layout=B.LAYOUT_TILE), out_dtype=B.OUT_F32)
     G.close(y, prod, bound, torch.float32)
+
+
+def ones(seed, *shape):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    return (torch.randint(0, 2, shape, generator=g, device=DEV, dtype=torch.int8) * 2 - 1).half()
+
+
+def exact(x, w):
+    """Products of +-1, in 64 bits, a piece of K at a time."""
+    return sum(x[:, c:c + 16384].double() @ w[:, c:c + 16384].double().T.contiguous() for c in range(0, x.shape[1], 16384))
+
+
+# strips with one row and more, of eight wavefronts and of four, rows converted inside; tiles of 32, 64 and (64 x 256) rows: a block that is left out shows
+@pytest.mark.parametrize("T,N,K", [(1, 40, 131072), (5, 300, 131071), (33, 40, 131072), (1, 12900, 16384), (1, 40, 16384), (1, 12900, 16500), (33, 12900, 9000),
+                                   (2080, 128, 131072), (2080, 520, 40000), (935, 4500, 20000)])
+def test_long_sums_that_32_bits_hold_are_exact(ctx, T, N, K):  # noqa: F811
+    x, w = ones(T, T, K), ones(N, N, K)
+    want = exact(x, w)
+    wt = ctx.quantize_mx4(w, layout=B.LAYOUT_TILE)
+    for a in (x, ctx.quantize_mx4(x)):
+        assert torch.equal(ctx.matmul_mx4(a, wt, out_dtype=B.OUT_F32).double(), want)
+
+
+# strips with K dealt to four wavefronts, tall tiles; K = H of the up projection, K = F of the down projection
+@pytest.mark.parametrize("T,E", [(1, 2), (40, 2), (40, 8), (300, 2)])
+def test_long_rows_of_experts(ctx, T, E):  # noqa: F811
+    """Up: sums of +-1 over 131072 columns, a 2^-8 of each; the intermediate comes back through W2 = 1 on a diagonal.  A block that is left out moves
+    a sum by 5 of 256 on average, and one code in twenty or so with it."""
+    H, F = 131072, 64
+    x, w1, w3, w2 = ones(1, T, H), ones(2, F, H) / 256, ones(3, F, H) / 256, torch.zeros((H, F), dtype=torch.half, device=DEV)
+    w2[torch.arange(F), torch.arange(F)] = 1.0
+    mats = [ctx.quantize_mx4(m, layout=B.LAYOUT_TILE) for m in (w1, w3, w2)]
+    table = B.make_mx4_table([mats] * E, DEV)
+    idx = (torch.arange(T, device=DEV) % E).int()[:, None].contiguous()
+    y = ctx.moe_ffn_mx4(x, idx, torch.ones((T, 1), device=DEV), table, F, out_dtype=B.OUT_F32)
+    a, u = exact(x, w1), exact(x, w3)
+    h = a / (1.0 + torch.exp(-a)) * u
+    # silu and its product are off by 9 steps of 2^-24; on either side of a border within 16
+    lo, hi = (Q.values(*Q.quantize(G.f64(h * (1 + d)))) for d in (-16 * 2.0 ** -24, 16 * 2.0 ** -24))
+    got = G.f64(y[:, :F])
+    assert ((got == lo[:, :F]) | (got == hi[:, :F])).all() and (lo == hi).mean() > 0.99 and (y[:, F:] == 0).all()
+
+
+@pytest.mark.parametrize("T,E", [(1, 2), (20, 2), (40, 8), (300, 2)])
+def test_long_intermediates_of_experts(ctx, T, E):  # noqa: F811
+    """Down: an intermediate of which every value is 1.5 (silu of 2^30 is 2^30), its signs those of W3, in a sum over 131072 of them."""
+    H, F = 64, 131072
+    sign, w2 = ones(4, F), ones(5, H, F)
+    w1, w3 = torch.zeros((F, H), device=DEV), torch.zeros((F, H), device=DEV)
+    w1[:, 0], w3[:, 32] = 1.0, sign.float()
+    x = torch.zeros((T, H), device=DEV)
+    x[:, 0], x[:, 32] = 2.0 ** 30, 1.5 * 2.0 ** -30 * (torch.arange(T, device=DEV) % 2 * 2 - 1)
+    mats = [ctx.quantize_mx4(m, layout=B.LAYOUT_TILE) for m in (w1, w3, w2)]
+    table = B.make_mx4_table([mats] * E, DEV)
+    idx = (torch.arange(T, device=DEV) % E).int()[:, None].contiguous()
+    y = ctx.moe_ffn_mx4(x, idx, torch.ones((T, 1), device=DEV), table, F, out_dtype=B.OUT_F32)
+    want = 1.5 * (torch.arange(T, device=DEV) % 2 * 2 - 1)[:, None] * (w2.double() @ sign.double())[None]
+    assert torch.equal(y.double(), want.expand(T, H))
