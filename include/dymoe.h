@@ -665,7 +665,8 @@ int dymoe_moe_ffn_mx4(dymoe_ctx* ctx, const void* x, int x_dtype, const int32_t*
  * 64 bits, in an order that T and E fix.
  * logits [T,E] bf16, fp16 or fp32 (dtype: DYMOE_OUT_*), idx [T,k] int32, keep [T] uint8 or NULL; counts [E+1] int32, mean [E] fp32,
  * loss [1] fp32.  workspace: dymoe_route_balance_workspace_bytes(T, E) bytes (0 for invalid sizes), 256-byte aligned, scratch.
- * Limits: 1 <= k <= E <= DYMOE_MAX_EXPERTS, k <= 64, T < 2^25 (else DYMOE_ENOTSUP).  One launch for up to 32 tokens, else two.
+ * Limits: 1 <= k <= E <= DYMOE_MAX_EXPERTS, k <= 64, T < 2^25 (else DYMOE_ENOTSUP; T k < 2^31 is what a count of one expert may come to).  One launch
+ * for up to 32 tokens, else two.
  */
 size_t dymoe_route_balance_workspace_bytes(int T, int E);
 int dymoe_route_balance(dymoe_ctx* ctx, const void* logits, int dtype, const int32_t* idx, const uint8_t* keep, int T, int E, int k,

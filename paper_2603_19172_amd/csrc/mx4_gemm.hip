@@ -110,8 +110,8 @@ __device__ __forceinline__ void mx4_rows_to_lds(int dt, const char* x, long ldx,
 // the sums of a strip's wavefronts meet in LDS.
 // Bound by the weights' bytes: 61 tokens on 8 of 128 experts of 768 x 2048, up 34.9 us (6.0 TB/s), down 19.2 (5.4); 61 x 1536 x 2048 4.3 us, a
 // start, eight wavefronts' share of K and the sums' way through LDS.
-// XT: the rows lie in tiles as the weights do, and a load of theirs is 1 KiB of contiguous memory too: 222 x 1295 x 9025 18.8 us and 22.3 row by row,
-// 61 x 1536 x 2048 3.6 / 4.4.  A call that converts its rows writes them so.
+// XT: the rows lie in tiles as the weights do, and a load of theirs is 1 KiB of contiguous memory too: 61 x 1536 x 2048 4.1 us and 5.0 row by row.  A
+// call that converts its rows writes them so.
 // FUSE: the rows come as they are, few enough for every workgroup to convert them for itself, behind its first loads of weights; the experts' pairs
 // are then looked through by every workgroup too: the one of a pair that comes first among those of its expert (or 32, 64, ... behind
 // the first) takes the next 32 of them, and a pair's position is its number.
@@ -329,7 +329,7 @@ __global__ __launch_bounds__(64 * NW) void mx4_small_kernel(const Mx4Args A)
 // the other, are dealt to the wavefronts in equal runs, D tiles of a wavefront on their way; the intermediate's codes wait in LDS.  The
 // matrix instruction's 32 weight rows are those 16 twice (the second half of the lanes asks for the same lines): with 32 outputs a workgroup, one
 // token on 4096 outputs would have half as many workgroups as there are compute units.  Bound by the weights' bytes and its own start: two
-// experts of 14336 x 4096 13.6 us (4.6 TB/s; the up projection before it 21.9, 5.7).
+// experts of 14336 x 4096 13.8 us (4.5 TB/s; the up projection before it 22.0, 5.7).
 constexpr int kMx4LastWaves = 16;
 
 template <int D>
@@ -440,10 +440,10 @@ __global__ __launch_bounds__(64 * kMx4LastWaves) void mx4_thin_down_kernel(const
 //    issued.
 //  * The rows' codes and exponents are shared by the wavefronts through three LDS buffers that global memory fills directly, two steps ahead; the 16-byte chunks of
 //    a row's 128 bytes are turned by its number, which spreads the operand reads (one chunk of 32 rows) over all banks (conflicts in 2.5 % of the
-//    cycles).  Rows in tiles (XT) come and lie in the operand's order by themselves: 512 x 4096 x 14336 27.4 us in all, 32.4 row by row.
-// 2047 x 14336 x 4096: 72 us, 3.3 PFLOP/s, the matrix units busy in some 40 % of the cycles; codes made before, row by row: 88 us, 63 with zeros in place of
-// random ones (the clock is the power's to set); 8192 x 8192 x 8192 4.1 PFLOP/s, 5.8 with zeros, of 5.3 to 6.4 that these instructions reach on random
-// codes from registers alone.  Experts with 128 rows each, 8 of 14336 x 4096: the stream of weights, 4.3 TB/s beside the rows' copies from L2 (with 8
+//    cycles).  Rows in tiles (XT) come and lie in the operand's order by themselves: 512 x 4096 x 14336 22.9 us, 28.7 row by row.
+// 2047 x 14336 x 4096: 72 to 77 us from box to box, 3.1 to 3.3 PFLOP/s, the matrix units busy in 51 % of a compute unit's busy cycles and 37 % of the launch's;
+// codes made before, row by row: 80 us beside 77; with zeros in place of random codes 62 and 58 (the clock is the power's to set); 8192 x 8192 x 8192
+// 4.0 PFLOP/s, 4.7 with zeros, of 5.3 to 6.4 that these instructions reach on random codes from registers alone.  Experts with 128 rows each, 8 of 14336 x 4096: the stream of weights, 4.3 TB/s beside the rows' copies from L2 (with 8
 // rows 5.6): a compute unit's requests for either wait in one queue.
 constexpr uint32_t kMx4Row = 128;           // bytes of a row of a step
 template <int NTF>
@@ -756,7 +756,7 @@ int mx4_init()
 }
 
 // y[t] = sum over the slots, in their order, of gate times the pair's output, which is the sum of its parts.  A workgroup takes 2048 outputs of a
-// token.  Bound by the pairs' bytes: 16376 pairs of 2048 outputs 21.5 us (6.2 TB/s).
+// token.  Bound by the pairs' bytes: 16376 pairs of 2048 outputs 22.1 us (6.1 TB/s).
 template <int PARTS>
 __global__ __launch_bounds__(256) void mx4_combine_kernel(const float* __restrict__ part, long ldp, long P, const int32_t* __restrict__ where,
                                                           const float* __restrict__ gate, int H, int k, int out_dtype, void* __restrict__ y)

@@ -2,7 +2,7 @@
 //
 // a = max |x| of 32 columns, e = floor(log2 a) - 2, code = x / 2^e to the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6.  A stream of bytes: 2 read and
 // 17 / 32 written a value (bf16 or fp16).  Four neighbouring lanes share a block, so nothing leaves the vector unit and every value is read once.
-// 8191 x 14336 bf16: to rows 51 us (5.8 TB/s), to tiles 52; back 59 and 53.
+// 8191 x 14336 bf16: to rows 51 us (5.8 TB/s), to tiles 53; back 61 and 55.
 #include "mx4_device.hpp"
 
 namespace dymoe {

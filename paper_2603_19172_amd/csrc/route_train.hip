@@ -3,7 +3,7 @@
 // A token's shares p = s / sum s come from fp32 exponentials of differences to its largest logit, so that no scores are too small to be
 // divided; with sigmoids u = e^(min(l, 0) - min(m, 0)) / (1 + e^-|l|) is s e^(-min(m, 0)).  One wavefront per token, lane l holding experts l,
 // l + 64, ...  Sums over tokens are held in 64 bits and taken in an order that follows from T and E alone.
-// Latencies and vector arithmetic, not bytes: 8191 tokens of 256 experts, fp32, loss 6.9 + 5.7 us, gradient 10.0 (16.8 MB: 3.3); 24 of 128 4.6 and 3.8.
+// Latencies and vector arithmetic, not bytes: 8191 tokens of 256 experts, fp32, loss 6.9 + 5.8 us, gradient 9.8 (16.8 MB: 3.3); 24 of 128 4.6 and 3.9.
 #include <float.h>
 
 #include "int8_device.hpp"
