@@ -263,7 +263,8 @@ class Mx4MoELayer:
     """A layer whose router scores (dymoe_route_scored) and whose experts are microscaled 4-bit numbers (dymoe_moe_ffn_mx4), every buffer
     pre-allocated: a step is three library calls on one stream, or two where the caller has the logits.  balance() and backward() are
     the router's side of a training step: the balance loss of the last step's routing, and its logits' gradient.  Another step overwrites
-    the choices (idx) and leaves the counts behind: for a gradient after that, give copies of both."""
+    the choices (idx) and leaves the counts behind: for a gradient after that, give copies of both.  (A replayed graph does not pass through
+    here: what belongs together is captured together.)"""
 
     def __init__(self, ctx, T, H, F, E, k, score=B.SCORE_SIGMOID, groups=1, top_groups=1, group_best=1, renorm=True, factor=1.0,
                  out_dtype=B.OUT_BF16, device="cuda:0"):
